@@ -9,8 +9,18 @@ from . import binding
 from .binding import (AS_PATH_SIMT, AS_PATH_TENSOR, AS_STAB_EXACT, AS_STAB_PAPER, AsError)
 from .binding import as_select_block_rates as select_block_rates
 
+_BLOCK_FP8 = ("BlockFp8", "empty_fp8", "fp8_last_status", "matmul_fp8", "quantize_fp8", "rms_norm")
 __all__ = ["binding", "HybridAttention", "AS_PATH_SIMT", "AS_PATH_TENSOR", "AS_STAB_EXACT",
-           "AS_STAB_PAPER", "AsError", "select_block_rates"]
+           "AS_STAB_PAPER", "AsError", "select_block_rates", *_BLOCK_FP8]
+
+
+def __getattr__(name):
+    """The 8-bit projections, which import PyTorch, when they are first asked for."""
+    if name not in _BLOCK_FP8:
+        raise AttributeError("module %r has no attribute %r" % (__name__, name))
+    from . import block_fp8
+    globals().update({n: getattr(block_fp8, n) for n in _BLOCK_FP8})
+    return globals()[name]
 
 
 def _stream_ptr(stream):

@@ -17,6 +17,7 @@ AS_ERR_ALLOC, AS_ERR_WORKSPACE, AS_ERR_CUDA, AS_ERR_DEVICE_TIMEOUT, AS_ERR_INFEA
 AS_STAB_PAPER, AS_STAB_EXACT = 0, 1
 AS_ACT_RELU = 0
 AS_PATH_TENSOR, AS_PATH_SIMT = 0, 1
+AS_DTYPE_BF16, AS_DTYPE_F32 = 0, 1
 AS_KERNEL_KPASS, AS_KERNEL_REDUCE, AS_KERNEL_QPASS, AS_NUM_KERNELS = 0, 1, 2, 3
 
 
@@ -39,6 +40,31 @@ class as_hybrid_attn_desc_t(C.Structure):
 
 class as_phi_weights_t(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("wq1", "bq1", "wq2", "bq2", "wk1", "bk1", "wk2", "bk2")]
+
+
+class as_rows_t(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("dtype", C.c_int32), ("head_dim", C.c_int32), ("tokens", C.c_int64),
+                ("stride_batch", C.c_int64), ("stride_head", C.c_int64), ("stride_token", C.c_int64)]
+
+
+class as_fp8_matrix_t(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("pitch", C.c_int64), ("scales", C.c_void_p), ("scale_rows", C.c_int64)]
+
+
+class as_rms_norm_t(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("cols", C.c_int32), ("rows", C.c_int64), ("x", as_rows_t), ("residual", as_rows_t),
+                ("residual_out", as_rows_t), ("out", as_rows_t), ("out8", as_fp8_matrix_t), ("weight", C.c_void_p),
+                ("weight_dtype", C.c_int32), ("eps", C.c_float)]
+
+
+class as_quantize_fp8_t(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("cols", C.c_int32), ("rows", C.c_int64), ("x", as_rows_t), ("out", as_fp8_matrix_t),
+                ("block_rows", C.c_int32), ("reserved", C.c_int32)]
+
+
+class as_matmul_fp8_t(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("cols", C.c_int32), ("rows", C.c_int64), ("out_cols", C.c_int64),
+                ("a", as_fp8_matrix_t), ("w", as_fp8_matrix_t), ("bias", C.c_void_p), ("out", as_rows_t)]
 
 
 class AsError(RuntimeError):
@@ -87,6 +113,13 @@ def lib() -> C.CDLL:
                                                   + [C.c_void_p, C.c_void_p, C.c_void_p],
             "as_select_block_rates": [C.c_int32, C.c_int32, C.POINTER(C.c_double), C.POINTER(C.c_double), C.c_double,
                                       C.POINTER(C.c_int32), C.POINTER(C.c_double), C.POINTER(C.c_double)],
+            # the argument structs of the next three: an instance's address, or bytes of the same layout
+            "as_rms_norm": [C.c_void_p, C.c_void_p],
+            "as_quantize_fp8": [C.c_void_p, C.c_void_p],
+            "as_matmul_fp8": [H, C.c_void_p, C.c_void_p],
+            "as_fp8_create": [C.POINTER(H)],
+            "as_fp8_destroy": [H],
+            "as_fp8_last_status": [H, C.c_void_p],
         }
         for name, args in sigs.items():
             fn = getattr(L, name)
@@ -293,3 +326,33 @@ def as_select_block_rates(cost, err, budget):
     _check(lib().as_select_block_rates(n_blocks, n_rates, flat_c, flat_e, float(budget), choice,
                                        C.byref(tc), C.byref(te)), "as_select_block_rates")
     return list(choice), tc.value, te.value
+
+
+def as_rms_norm(args, stream_ptr) -> None:
+    """`args`: an as_rms_norm_t, or bytes of its layout (cheaper to make).  A row's root-mean-square norm, see include/as_fp8.h."""
+    _check(lib().as_rms_norm(args if isinstance(args, bytes) else C.addressof(args), stream_ptr or None), "as_rms_norm")
+
+
+def as_quantize_fp8(args, stream_ptr) -> None:
+    """`args`: an as_quantize_fp8_t, or bytes of its layout.  A matrix in 8-bit form."""
+    _check(lib().as_quantize_fp8(args if isinstance(args, bytes) else C.addressof(args), stream_ptr or None), "as_quantize_fp8")
+
+
+def as_matmul_fp8(ctx, args, stream_ptr) -> None:
+    """`args`: an as_matmul_fp8_t, or bytes of its layout.  The product of two matrices in 8-bit form."""
+    _check(lib().as_matmul_fp8(ctx, args if isinstance(args, bytes) else C.addressof(args), stream_ptr or None), "as_matmul_fp8")
+
+
+def as_fp8_create() -> C.c_void_p:
+    h = C.c_void_p()
+    _check(lib().as_fp8_create(C.byref(h)), "as_fp8_create")
+    return h
+
+
+def as_fp8_destroy(ctx) -> None:
+    _check(lib().as_fp8_destroy(ctx), "as_fp8_destroy")
+
+
+def as_fp8_last_status(ctx, stream_ptr) -> int:
+    """Returns the status code instead of raising, as as_hybrid_attn_last_status."""
+    return lib().as_fp8_last_status(ctx, stream_ptr or None)

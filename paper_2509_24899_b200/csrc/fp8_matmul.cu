@@ -1,0 +1,464 @@
+// out = a w^T + bias of two matrices in 8-bit form, on the tensor cores' block-scaled kind: an MMA takes 32 columns of 8-bit values from shared memory and the
+// power-of-two scales of their rows from tensor memory, and adds their product in fp32 to its accumulator there.
+//
+// A pair of CTAs (cta_group::2) computes a tile of 256 rows of a and BN rows of w: each holds 128 rows of a, half of the rows of w and the tile's 128 rows
+// of results, so that an operand byte in shared memory is used 2 * BN or 512 times.  The grid is persistent, one CTA per SM; a tile's results are read out
+// while the next one is computed, from the other of two accumulators.
+//
+//   warp 0       copies of a and w (TMA, 128 columns a stage, 128-byte swizzle), told by the leading CTA's barrier
+//   warp 1       the MMAs (leading CTA only): four of 32 columns a stage, which share the byte of their scale words that the stage's block of 128 columns has
+//   warp 2       allocates tensor memory
+//   warps 4-7    scales: the words of 512 columns (one for each of the CTA's rows of a, one for each of the tile's rows of w) from global memory into tensor memory,
+//                the same for each of the four quarters of the lanes, a ring of four
+//   warps 8-11   results: tensor memory -> registers, bias, bf16, a swizzled strip of shared memory per warp, rows of 128 bytes to global memory
+#include <new>
+
+#include "fp8_common.cuh"
+#include "tensor_common.cuh"
+
+namespace {
+
+using namespace as_fp8;
+using namespace sm100;
+
+constexpr int MM_THREADS = 384;
+constexpr int BM = 128;                     // rows of a per CTA
+constexpr int BK = 128;                     // columns of a stage, one scale
+constexpr int MAX_BN = 224;                 // two accumulators, and the scales beside them in 512 columns of tensor memory
+constexpr int MAX_STAGES = 10;
+constexpr int SF_SLOTS = 4;
+constexpr int SMEM_MAX = 227 * 1024;
+
+// tensor memory: accumulators at 0 and 256, scale slots (words of a: 4 columns, of w: 8) in the 32 columns behind each
+AS_DEV constexpr uint32_t sf_col(int slot) { return (slot < 2 ? 224u : 480u - 32u) + 16u * (uint32_t)slot; }
+static_assert(224 + 16 * 2 == 256 && 480 - 32 + 16 * 2 == 480 && 480 - 32 + 16 * 4 == 512, "scale slots fill what the accumulators leave");
+
+enum { B_FULL = 0, B_EMPTY = B_FULL + MAX_STAGES, B_SFULL = B_EMPTY + MAX_STAGES, B_SEMPTY = B_SFULL + SF_SLOTS, B_AFULL = B_SEMPTY + SF_SLOTS,
+       B_AEMPTY = B_AFULL + 2, B_COUNT = B_AEMPTY + 2 };
+// head of shared memory: barriers, tensor-memory address, abort flag; bias and staging of the four result warps; then the stages
+constexpr int HEAD_BYTES = 512;
+constexpr int STAGING = 32 * 128 + 256;     // per warp: 32 rows of 128 bytes, 64 biases
+constexpr int STAGING_OFF = HEAD_BYTES;
+constexpr int STAGES_OFF = (STAGING_OFF + 4 * STAGING + 1023) / 1024 * 1024;
+static_assert(B_COUNT * 8 + 8 <= HEAD_BYTES, "");
+
+struct MMParams {
+  const uint8_t *sa, *sw;
+  const __nv_bfloat16* bias;
+  Rows out;
+  uint32_t* status;
+  long long sa_rows, sw_rows;
+  int M, N, kb;                             // kb: blocks of 128 columns
+  int bn, stages, nt;
+  long long tiles;
+  bool vec;                                 // results move 16 bytes at a time
+};
+
+// ---------------------------------------------------------------- instructions of CTA pairs and of the block-scaled kind
+template <int CG>
+AS_DEV void alloc_tmem(uint32_t slot) {
+  if constexpr (CG == 1) { tmem_alloc(slot, 512); tmem_relinquish(); }
+  else asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;\n\ttcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::"r"(slot) : "memory");
+}
+template <int CG>
+AS_DEV void free_tmem(uint32_t at) {
+  if constexpr (CG == 1) tmem_dealloc(at, 512);
+  else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(at) : "memory");
+}
+// Copy of a box; a pair's copies are told to the leading CTA's barrier, each lands in its own CTA's shared memory.
+template <int CG>
+AS_DEV void load_box(uint32_t dst, const CUtensorMap* m, uint32_t bar, int x, int y) {
+  if constexpr (CG == 1)
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(x), "r"(y) : "memory");
+  else
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4}], [%2];"
+                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(x), "r"(y) : "memory");
+}
+// One arrival at `bar`, of both CTAs of a pair, when the MMAs issued so far have completed.
+template <int CG>
+AS_DEV void commit(uint32_t bar) {
+  if constexpr (CG == 1) tc_commit(bar);
+  else asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+}
+template <int CG>
+AS_DEV void mma_scaled(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
+  if constexpr (CG == 1)
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+  else
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+                 "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+}
+// Instruction descriptor of the kind: e4m3 operands (format 0), both K-major, scales of type ue8m0; the byte of the scale words at 4 (w) and 29 (a).
+AS_DEV constexpr uint32_t scaled_idesc(int M, int N) { return (uint32_t)(N >> 3) << 17 | 1u << 23 | (uint32_t)(M >> 7) << 27; }
+AS_DEV constexpr uint32_t scale_byte_of(int k) { return (uint32_t)k << 4 | (uint32_t)k << 29; }
+
+AS_DEV uint32_t cta_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
+// The address of the leading CTA's copy of a shared-memory word, for arrivals and copies across the pair.
+AS_DEV uint32_t leaders(uint32_t addr) { uint32_t r; asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr)); return r; }
+template <int CG>
+AS_DEV void arrive_leader(uint32_t bar) {
+  if constexpr (CG == 1) mbar_arrive(bar);
+  else asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(leaders(bar)) : "memory");
+}
+template <int CG>
+AS_DEV void pair_sync() {
+  if constexpr (CG == 2) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// A wait for arrivals from both CTAs: as mbar_wait, but what the peer wrote ahead of its arrival is visible as well.
+template <int CG>
+AS_DEV bool wait_pair(uint32_t bar, uint32_t parity, const WaitCtx& w) {
+  const bool ok = mbar_wait(bar, parity, w);
+  if constexpr (CG == 2) asm volatile("fence.acq_rel.cluster;" ::: "memory");
+  return ok;
+}
+
+AS_DEV void tmem_st4(uint32_t at, const uint32_t (&r)[4]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+}
+AS_DEV void tmem_st8(uint32_t at, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
+
+// A position in a ring of barriers: the slot, and the parity of the turn.
+struct Ring {
+  int slot = 0;
+  uint32_t turn = 0;
+  AS_DEV void next(int n) { if (++slot == n) { slot = 0; turn ^= 1u; } }
+};
+
+template <int CG>
+struct Ctx {
+  uint32_t sbase, tmem;
+  WaitCtx wc;
+  uint32_t rank;                             // of the CTA in its pair
+  long long unit, units;                     // this pair (CTA), all of them: tiles unit, unit + units, ...
+  AS_DEV uint32_t bar(int i) const { return sbase + 8 * i; }
+  AS_DEV bool wait(int i, uint32_t parity) const { return mbar_wait(bar(i), parity, wc); }
+};
+
+// ---------------------------------------------------------------- roles
+template <int CG>
+AS_DEV void mm_copies(const MMParams& p, const Ctx<CG>& c, const CUtensorMap* ma, const CUtensorMap* mw) {
+  const int rows_w = p.bn / CG;
+  const uint32_t stage_bytes = (uint32_t)(BM + rows_w) * BK;
+  Ring r;
+  for (long long t = c.unit; t < p.tiles; t += c.units) {
+    const int m0 = (int)(t / p.nt) * (BM * CG) + (int)c.rank * BM, n0 = (int)(t % p.nt) * p.bn + (int)c.rank * rows_w;
+    for (int k = 0; k < p.kb; ++k) {
+      if (!c.wait(B_EMPTY + r.slot, r.turn ^ 1u)) goto out;
+      const uint32_t at = c.sbase + STAGES_OFF + (uint32_t)r.slot * stage_bytes;
+      if (c.rank == 0) mbar_expect_tx(c.bar(B_FULL + r.slot), stage_bytes * CG);
+      const uint32_t bar = CG == 1 ? c.bar(B_FULL + r.slot) : leaders(c.bar(B_FULL + r.slot));
+      load_box<CG>(at, ma, bar, k * BK, m0);
+      load_box<CG>(at + BM * BK, mw, bar, k * BK, n0);
+      r.next(p.stages);
+    }
+  }
+out:
+  // Every copy has landed, and every MMA has read its operands, before the CTA may end: the last turn of each stage has been given back (a stage
+  // that was never used passes at once).
+  for (int s = 0; s < p.stages; ++s) {
+    if (!c.wait(B_EMPTY + r.slot, r.turn ^ 1u)) break;
+    r.next(p.stages);
+  }
+}
+
+template <int CG>
+AS_DEV void mm_issue(const MMParams& p, const Ctx<CG>& c) {
+  const uint32_t stage_bytes = (uint32_t)(BM + p.bn / CG) * BK;
+  const uint32_t idesc0 = scaled_idesc(BM * CG, p.bn);
+  Ring r, sf;
+  uint32_t buf = 0, turn = 0;
+  for (long long t = c.unit; t < p.tiles; t += c.units) {
+    if (!wait_pair<CG>(c.bar(B_AEMPTY + buf), turn ^ 1u, c.wc)) return;
+    tc_fence_after();
+    const uint32_t d = c.tmem + buf * 256u;
+    for (int k = 0; k < p.kb; ++k) {
+      if (k % 4 == 0) {
+        if (!wait_pair<CG>(c.bar(B_SFULL + sf.slot), sf.turn, c.wc)) return;
+        tc_fence_after();
+      }
+      if (!c.wait(B_FULL + r.slot, r.turn)) return;
+      tc_fence_after();
+      const uint32_t at = c.sbase + STAGES_OFF + (uint32_t)r.slot * stage_bytes;
+      const uint64_t da = make_sdesc(at, 16, 1024), db = make_sdesc(at + BM * BK, 16, 1024);
+      const uint32_t idesc = idesc0 | scale_byte_of(k % 4), s = c.tmem + sf_col(sf.slot);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mma_scaled<CG>(d, da + 2 * i, db + 2 * i, idesc, s, s + 8, (k | i) != 0 ? 1u : 0u);
+      commit<CG>(c.bar(B_EMPTY + r.slot));
+      r.next(p.stages);
+      if (k % 4 == 3 || k == p.kb - 1) {
+        commit<CG>(c.bar(B_SEMPTY + sf.slot));
+        sf.next(SF_SLOTS);
+      }
+    }
+    commit<CG>(c.bar(B_AFULL + buf));
+    buf ^= 1u;
+    if (buf == 0) turn ^= 1u;
+  }
+}
+
+template <int CG>
+AS_DEV void mm_scales(const MMParams& p, const Ctx<CG>& c, int lane, int quarter) {
+  const uint32_t lanes = (uint32_t)quarter * 32u << 16;
+  const int groups = (p.kb + 3) / 4;
+  const uint32_t ones = 0x7f7f7f7fu;         // rows that are not there
+  Ring sf;
+  for (long long t = c.unit; t < p.tiles; t += c.units) {
+    const int m0 = (int)(t / p.nt) * (BM * CG) + (int)c.rank * BM, n0 = (int)(t % p.nt) * p.bn;
+    for (int g = 0; g < groups; ++g) {
+      uint32_t a[4], w[8];
+      const uint32_t* ga = reinterpret_cast<const uint32_t*>(p.sa) + (long long)g * p.sa_rows;
+      const uint32_t* gw = reinterpret_cast<const uint32_t*>(p.sw) + (long long)g * p.sw_rows;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) { const int m = m0 + 32 * j + lane; a[j] = m < p.M ? __ldg(ga + m) : ones; }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) { const int n = n0 + 32 * j + lane; w[j] = 32 * j < p.bn && n < p.N ? __ldg(gw + n) : ones; }
+      const bool ok = c.wait(B_SEMPTY + sf.slot, sf.turn ^ 1u);
+      if (!__all_sync(0xffffffffu, ok)) return;
+      tc_fence_after();
+      const uint32_t at = c.tmem + lanes + sf_col(sf.slot);
+      tmem_st4(at, a);
+      tmem_st8(at + 8, w);
+      tmem_st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) arrive_leader<CG>(c.bar(B_SFULL + sf.slot));
+      sf.next(SF_SLOTS);
+    }
+  }
+}
+
+// A strip of 32 rows and up to 64 columns of results on its way out.
+template <int CG>
+AS_DEV void mm_results(const MMParams& p, const Ctx<CG>& c, int lane, int quarter) {
+  const uint32_t lanes = (uint32_t)quarter * 32u << 16;
+  const uint32_t strip = c.sbase + STAGING_OFF + (uint32_t)quarter * STAGING, sbias = strip + 32 * 128;
+  __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out.data);
+  uint32_t buf = 0, turn = 0;
+  for (long long t = c.unit; t < p.tiles; t += c.units) {
+    const int m0 = (int)(t / p.nt) * (BM * CG) + (int)c.rank * BM + quarter * 32, n0 = (int)(t % p.nt) * p.bn;
+    const long long my_row = m0 + lane < p.M ? p.out.row((unsigned)(m0 + lane)) : 0;
+    if (!mbar_wait_warp(c.bar(B_AFULL + buf), turn, c.wc)) return;
+    tc_fence_after();
+    for (int c0 = 0; c0 < p.bn; c0 += 64) {
+      const bool wide = c0 + 32 < p.bn;
+      uint32_t x[32], y[32];
+      tmem_ld32(c.tmem + lanes + buf * 256u + c0, x);
+      if (wide) tmem_ld32(c.tmem + lanes + buf * 256u + c0 + 32, y);
+      if (p.bias != nullptr) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int n = n0 + c0 + 32 * j + lane;
+          const float b = n < p.N ? __bfloat162float(p.bias[n]) : 0.f;
+          asm volatile("st.shared.f32 [%0], %1;" ::"r"(sbias + (32 * j + lane) * 4), "f"(b) : "memory");
+        }
+        __syncwarp();
+      }
+      tmem_ld_wait(x);
+      if (wide) tmem_ld_wait(y);
+      if (c0 + 64 >= p.bn) {                  // the accumulator has been read
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) arrive_leader<CG>(c.bar(B_AEMPTY + buf));
+      }
+      // this lane's row into the strip, 16 bytes a chunk, chunks xored with the row
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (h == 1 && !wide) break;
+        uint32_t(&v)[32] = h == 0 ? x : y;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float f[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(v[8 * i + j]);
+          if (p.bias != nullptr) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              float b0, b1, b2, b3;
+              asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(b0), "=f"(b1), "=f"(b2), "=f"(b3) : "r"(sbias + (32 * h + 8 * i + 4 * j) * 4) : "memory");
+              f[4 * j] += b0; f[4 * j + 1] += b1; f[4 * j + 2] += b2; f[4 * j + 3] += b3;
+            }
+          }
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(strip + swz128_chunk_offset((uint32_t)lane, (uint32_t)(4 * h + i))),
+                       "r"(pack_bf16(f[0], f[1])), "r"(pack_bf16(f[2], f[3])), "r"(pack_bf16(f[4], f[5])), "r"(pack_bf16(f[6], f[7])) : "memory");
+        }
+      }
+      __syncwarp();
+      if (p.vec) {
+        const int ch = lane & 7, n = n0 + c0 + ch * 8;
+        const bool there = n < p.N && (ch < 4 || wide);
+        const long long col = there ? p.out.col((unsigned)n) : 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int r = i * 4 + lane / 8;
+          const long long row = __shfl_sync(0xffffffffu, my_row, r);
+          uint32_t a0, a1, a2, a3;
+          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(a0), "=r"(a1), "=r"(a2), "=r"(a3) : "r"(strip + swz128_chunk_offset((uint32_t)r, (uint32_t)ch)) : "memory");
+          if (there && m0 + r < p.M) *reinterpret_cast<uint4*>(out + row + col) = make_uint4(a0, a1, a2, a3);
+        }
+      } else {
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+          const int k = 32 * h + lane, n = n0 + c0 + k;
+          const bool there = n < p.N && c0 + k < p.bn;
+          const long long col = there ? p.out.col((unsigned)n) : 0;
+#pragma unroll 4
+          for (int r = 0; r < 32; ++r) {
+            const long long row = __shfl_sync(0xffffffffu, my_row, r);
+            uint16_t v;
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(strip + swz128_chunk_offset((uint32_t)r, (uint32_t)(k / 8)) + (k % 8) * 2) : "memory");
+            if (there && m0 + r < p.M) *reinterpret_cast<uint16_t*>(out + row + col) = v;
+          }
+        }
+      }
+      __syncwarp();
+    }
+    buf ^= 1u;
+    if (buf == 0) turn ^= 1u;
+  }
+}
+
+template <int CG>
+__global__ void __launch_bounds__(MM_THREADS, 1)
+matmul_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mw, const __grid_constant__ MMParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);      // the same in both CTAs of a pair
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + 8 * B_COUNT);
+  volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem + 8 * B_COUNT + 4);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  Ctx<CG> c{smem_u32(smem), 0u, WaitCtx{p.status, abort_flag}, CG == 1 ? 0u : cta_rank(), blockIdx.x / CG, gridDim.x / CG};
+  if (threadIdx.x == 0) {
+    *abort_flag = 0u;
+    for (int s = 0; s < MAX_STAGES; ++s) { mbar_init(c.bar(B_FULL + s), 1); mbar_init(c.bar(B_EMPTY + s), 1); }
+    for (int s = 0; s < SF_SLOTS; ++s) { mbar_init(c.bar(B_SFULL + s), 4 * CG); mbar_init(c.bar(B_SEMPTY + s), 1); }
+    for (int s = 0; s < 2; ++s) { mbar_init(c.bar(B_AFULL + s), 1); mbar_init(c.bar(B_AEMPTY + s), 4 * CG); }
+    fence_barrier_init();
+    fence_proxy_async();
+    tma_prefetch_desc(&ma); tma_prefetch_desc(&mw);
+  }
+  if (warp == 2) { alloc_tmem<CG>(smem_u32(tmem_slot)); griddep_launch(); }
+  tc_fence_before();
+  __syncthreads();
+  pair_sync<CG>();                             // the peer's barriers stand before anything arrives there
+  tc_fence_after();
+  c.tmem = *tmem_slot;
+  griddep_wait();
+  if (warp == 0) {
+    if (elect_one()) mm_copies<CG>(p, c, &ma, &mw);
+    __syncwarp();
+  } else if (warp == 1) {
+    if (c.rank == 0 && elect_one()) mm_issue<CG>(p, c);
+    __syncwarp();
+  } else if (warp >= 4 && warp < 8) {
+    mm_scales<CG>(p, c, lane, warp - 4);
+  } else if (warp >= 8) {
+    mm_results<CG>(p, c, lane, warp - 8);
+  }
+  if (*abort_flag != 0u) {                     // a wait ran out: copies and MMAs under way get 20 us (they take two) before memory is given back
+    const long long t0 = clock64();
+    while (clock64() - t0 < 40000) {}
+  }
+  tc_fence_before();
+  __syncthreads();
+  pair_sync<CG>();                             // nothing of this CTA is reached from the peer any more
+  if (warp == 2) {
+    tc_fence_after();
+    free_tmem<CG>(c.tmem);
+  }
+}
+
+template <int CG>
+cudaError_t launch(const CUtensorMap& ma, const CUtensorMap& mw, const MMParams& p, int units, size_t smem, cudaStream_t st) {
+  cudaLaunchAttribute attr[2]{};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = CG; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(units * CG)); cfg.blockDim = dim3(MM_THREADS); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+  cfg.attrs = attr; cfg.numAttrs = CG == 1 ? 1 : 2;
+  return cudaLaunchKernelEx(&cfg, matmul_kernel<CG>, ma, mw, p);
+}
+
+}  // namespace
+
+struct as_fp8_context_s {
+  int device = -1, sms = 0;
+  uint32_t* status = nullptr;
+};
+
+extern "C" as_status_t as_fp8_create(as_fp8_context_t* out) {
+  if (out == nullptr) return AS_ERR_INVALID_ARG;
+  int dev = 0, major = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return AS_ERR_CUDA;
+  if (major != 10) return AS_ERR_ARCH;
+  if (as_tensor_init() != cudaSuccess || as_tc::opt_in_smem(matmul_kernel<1>, SMEM_MAX) != cudaSuccess || as_tc::opt_in_smem(matmul_kernel<2>, SMEM_MAX) != cudaSuccess)
+    return AS_ERR_CUDA;
+  as_fp8_context_s* h = new (std::nothrow) as_fp8_context_s;
+  if (h == nullptr) return AS_ERR_ALLOC;
+  h->device = dev;
+  h->sms = sms;
+  if (cudaMalloc(&h->status, 256) != cudaSuccess) { delete h; return AS_ERR_ALLOC; }
+  if (cudaMemset(h->status, 0, 256) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) { cudaFree(h->status); delete h; return AS_ERR_CUDA; }
+  *out = h;
+  return AS_OK;
+}
+
+extern "C" as_status_t as_fp8_destroy(as_fp8_context_t h) {
+  if (h == nullptr) return AS_OK;
+  cudaFree(h->status);
+  delete h;
+  return AS_OK;
+}
+
+extern "C" as_status_t as_fp8_last_status(as_fp8_context_t h, void* cuda_stream) {
+  if (h == nullptr) return AS_ERR_INVALID_ARG;
+  const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  uint32_t word = 0;
+  if (cudaMemcpyAsync(&word, h->status, 4, cudaMemcpyDeviceToHost, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) return AS_ERR_CUDA;
+  if (word == 0) return AS_OK;
+  if (cudaMemsetAsync(h->status, 0, 4, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) return AS_ERR_CUDA;
+  return AS_ERR_DEVICE_TIMEOUT;
+}
+
+extern "C" as_status_t as_matmul_fp8(as_fp8_context_t h, const as_matmul_fp8_t* a, void* cuda_stream) {
+  if (h == nullptr || a == nullptr || a->struct_size != sizeof(as_matmul_fp8_t)) return AS_ERR_INVALID_ARG;
+  if (a->cols < 1 || a->cols > (1 << 20) || a->rows < 0 || a->rows > (1ll << 30) || a->out_cols < 1 || a->out_cols > (1ll << 24)) return AS_ERR_INVALID_ARG;
+  if (!matrix_ok(a->a, a->rows, a->cols) || !matrix_ok(a->w, a->out_cols, a->cols) || !aligned(a->bias, 2)) return AS_ERR_INVALID_ARG;
+  if (!rows_ok(a->out, a->rows, a->out_cols) || a->out.dtype != AS_DTYPE_BF16 || !apart(a->out, a->rows, a->out_cols)) return AS_ERR_INVALID_ARG;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return AS_ERR_CUDA;
+  if (dev != h->device) return AS_ERR_INVALID_ARG;
+  MMParams p{};
+  p.out = rows_of(a->out, a->rows, a->out_cols);
+  if (p.out.split && a->out_cols * (long long)a->out.head_dim > (1ll << 32)) return AS_ERR_UNSUPPORTED;
+  if (a->rows == 0) return AS_OK;
+  p.M = (int)a->rows; p.N = (int)a->out_cols; p.kb = (a->cols + BK - 1) / BK;
+  p.sa = static_cast<const uint8_t*>(a->a.scales); p.sa_rows = a->a.scale_rows;
+  p.sw = static_cast<const uint8_t*>(a->w.scales); p.sw_rows = a->w.scale_rows;
+  p.bias = static_cast<const __nv_bfloat16*>(a->bias);
+  p.status = h->status;
+  p.vec = rows_vec(a->out);
+  const int CG = p.M > BM ? 2 : 1;
+  p.bn = 192;
+  p.nt = (p.N + p.bn - 1) / p.bn;
+  p.tiles = ((long long)p.M + BM * CG - 1) / (BM * CG) * p.nt;
+  const int stage = (BM + p.bn / CG) * BK;
+  p.stages = (SMEM_MAX - 1024 - STAGES_OFF) / stage;
+  if (p.stages > MAX_STAGES) p.stages = MAX_STAGES;
+  const size_t smem = 1024 + STAGES_OFF + (size_t)p.stages * stage;
+  CUtensorMap ma, mw;
+  if (!as_tc::make_map_bytes(&ma, a->a.data, a->cols, p.M, a->a.pitch, BM) || !as_tc::make_map_bytes(&mw, a->w.data, a->cols, p.N, a->w.pitch, p.bn / CG)) return AS_ERR_CUDA;
+  const int units = (int)(p.tiles < h->sms / CG ? p.tiles : h->sms / CG);
+  const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const cudaError_t e = CG == 2 ? launch<2>(ma, mw, p, units, smem, st) : launch<1>(ma, mw, p, units, smem, st);
+  return e == cudaSuccess ? AS_OK : AS_ERR_CUDA;
+}

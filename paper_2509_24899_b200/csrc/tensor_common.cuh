@@ -66,6 +66,9 @@ AS_DEV void store_row_chunk(uint8_t* tile, uint32_t row, uint32_t c0, const uint
 // 3-D bf16 tensor [slices][rows][cols] (cols contiguous) viewed through boxes of 64 cols x box_rows rows
 // with the 128-byte swizzle.  False when the driver entry point is missing or rejects the arguments.
 bool make_map(CUtensorMap* m, const void* base, int cols, int rows, int slices, int box_rows);
+// 2-D tensor of bytes [rows][pitch], `cols` of them a row, viewed through boxes of 128 bytes x box_rows rows with the 128-byte
+// swizzle; what lies outside reads as 0.
+bool make_map_bytes(CUtensorMap* m, const void* base, long long cols, long long rows, long long pitch, int box_rows);
 
 template <typename K>
 cudaError_t opt_in_smem(K kernel, int bytes) {
