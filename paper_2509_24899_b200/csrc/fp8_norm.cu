@@ -25,59 +25,118 @@ struct NormParams {
 };
 
 
-// 8 elements of a row: a vector where VEC, else elements 32 columns apart, each there if its column is.
+// Pairs of fp32 values, added and multiplied two at a time.
+AS_DEV float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+AS_DEV float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\tfma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+AS_DEV float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+// The largest of |a|, |b|, |c|; NaN if one of them is.
+AS_DEV float max_abs(float a, float b, float c) {
+  float d;
+  asm("{\n\t.reg .f32 x, y, z;\n\tabs.f32 x, %1;\n\tabs.f32 y, %2;\n\tabs.f32 z, %3;\n\tmax.NaN.f32 %0, x, y, z;\n\t}" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+
+// 8 elements of a row as they come: a vector where VEC, else elements 32 columns apart, 0 where there is no column.
+template <typename T, bool VEC> struct Raw { T e[8]; };
+template <> struct Raw<__nv_bfloat16, true> { uint4 a; };
+template <> struct Raw<float, true> { float4 a, b; };
+
 template <typename T, bool VEC>
-AS_DEV void load8(const Rows& m, long long row, int c0, int cols, float (&v)[8]) {
+AS_DEV void fetch(const Rows& m, long long row, int c0, int cols, Raw<T, VEC>& v) {
   const T* base = static_cast<const T*>(m.data) + row;
   if constexpr (VEC) {
+    v = Raw<T, VEC>{};
     if (c0 < cols) {
       const T* at = base + m.col(c0);
-      if constexpr (sizeof(T) == 2) {
-        const uint4 u = *reinterpret_cast<const uint4*>(at);
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
-      } else {
-        const float4 a = *reinterpret_cast<const float4*>(at), b = *reinterpret_cast<const float4*>(at + 4);
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = 0.f;
+      if constexpr (sizeof(T) == 2) v.a = *reinterpret_cast<const uint4*>(at);
+      else { v.a = *reinterpret_cast<const float4*>(at); v.b = *reinterpret_cast<const float4*>(at + 4); }
     }
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int c = c0 + 32 * i;
-      v[i] = c < cols ? (float)base[m.col(c)] : 0.f;
+      v.e[i] = c < cols ? base[m.col(c)] : (T)0.f;
     }
   }
 }
+template <typename T, bool VEC>
+AS_DEV void values(const Raw<T, VEC>& v, float2 (&f)[4]) {
+  if constexpr (!VEC) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = make_float2((float)v.e[2 * i], (float)v.e[2 * i + 1]);
+  } else if constexpr (sizeof(T) == 2) {
+    const uint32_t w[4] = {v.a.x, v.a.y, v.a.z, v.a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+  } else {
+    f[0] = make_float2(v.a.x, v.a.y); f[1] = make_float2(v.a.z, v.a.w); f[2] = make_float2(v.b.x, v.b.y); f[3] = make_float2(v.b.z, v.b.w);
+  }
+}
+template <typename T, bool VEC>
+AS_DEV void load8(const Rows& m, long long row, int c0, int cols, float2 (&f)[4]) {
+  Raw<T, VEC> v;
+  fetch<T, VEC>(m, row, c0, cols, v);
+  values<T, VEC>(v, f);
+}
 
 template <typename T, bool VEC>
-AS_DEV void store8(const Rows& m, long long row, int c0, int cols, const float (&v)[8]) {
+AS_DEV void store8(const Rows& m, long long row, int c0, int cols, const float2 (&v)[4]) {
   T* base = static_cast<T*>(m.data) + row;
   if constexpr (VEC) {
     if (c0 >= cols) return;
     T* at = base + m.col(c0);
     if constexpr (sizeof(T) == 2) {
-      *reinterpret_cast<uint4*>(at) = make_uint4(sm100::pack_bf16(v[0], v[1]), sm100::pack_bf16(v[2], v[3]), sm100::pack_bf16(v[4], v[5]), sm100::pack_bf16(v[6], v[7]));
+      *reinterpret_cast<uint4*>(at) = make_uint4(sm100::pack_bf16(v[0].x, v[0].y), sm100::pack_bf16(v[1].x, v[1].y), sm100::pack_bf16(v[2].x, v[2].y), sm100::pack_bf16(v[3].x, v[3].y));
     } else {
-      *reinterpret_cast<float4*>(at) = make_float4(v[0], v[1], v[2], v[3]);
-      *reinterpret_cast<float4*>(at + 4) = make_float4(v[4], v[5], v[6], v[7]);
+      *reinterpret_cast<float4*>(at) = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
+      *reinterpret_cast<float4*>(at + 4) = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
     }
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int c = c0 + 32 * i;
+      const float f = i % 2 ? v[i / 2].y : v[i / 2].x;
       if (c >= cols) continue;
-      if constexpr (sizeof(T) == 2) base[m.col(c)] = __float2bfloat16_rn(v[i]);
-      else base[m.col(c)] = v[i];
+      if constexpr (sizeof(T) == 2) base[m.col(c)] = __float2bfloat16_rn(f);
+      else base[m.col(c)] = f;
     }
   }
 }
 
+// The largest |value| of each of the two blocks of 128 columns in a warp's vector, as bits (NaN is above infinity), for every lane.
+template <bool VEC>
+AS_DEV void block_max(const float2 (&v)[4], int lane, uint32_t (&top)[2]) {
+  const float lo = max_abs(v[0].x, v[0].y, v[1].x), hi = max_abs(v[2].x, v[2].y, v[3].x);
+  if constexpr (VEC) {                        // lanes 0-15 hold the first one
+    const uint32_t t = __float_as_uint(max_abs(max_abs(lo, v[1].y, v[3].y), hi, 0.f));
+    top[0] = __reduce_max_sync(0xffffffffu, lane < 16 ? t : 0u);
+    top[1] = __reduce_max_sync(0xffffffffu, lane < 16 ? 0u : t);
+  } else {                                    // every lane holds four values of each
+    top[0] = __reduce_max_sync(0xffffffffu, __float_as_uint(max_abs(lo, v[1].y, 0.f)));
+    top[1] = __reduce_max_sync(0xffffffffu, __float_as_uint(max_abs(hi, v[3].y, 0.f)));
+  }
+}
+
 // NORM: y = t * rsqrt(mean t^2 + eps) * w, else y = x.  R: the residual's type (void: none).  FP8: y in 8-bit form, else in bf16.
+//
+// The weights multiply t while the sum of squares is on its way between the lanes, and so do the blocks' largest values go round: both turns of a row's reductions
+// overlap, and the row's scale enters last.  (In the formula's order, with one value an instruction, a row took 850 instructions instead of 450 and the norm of 32760 x 1536
+// with a residual in bf16 131 us: the arithmetic, not memory, was the bound.)
 template <typename X, typename R, bool NORM, bool FP8, bool VEC, int NV>
 __global__ void __launch_bounds__(THREADS) norm_kernel(const __grid_constant__ NormParams p) {
   griddep_launch();
@@ -88,105 +147,109 @@ __global__ void __launch_bounds__(THREADS) norm_kernel(const __grid_constant__ N
   const long long row = (long long)blockIdx.x * per + slot;
   const bool live = slot < per && row < p.rows;
   const unsigned r = live ? (unsigned)row : 0u;
+  const int cols = live ? p.cols : 0;                         // of a row that is not there nothing is read or written
   const int first = piece * (NV * 256);                       // columns of this warp
   const int c0 = first + (VEC ? lane * 8 : lane);
-  float v[NV][8];
+  float2 v[NV][4];
   griddep_wait();
-  if (live) {
+  {
+    Raw<X, VEC> x[NV];
     const long long xr = p.x.row(r);
 #pragma unroll
-    for (int j = 0; j < NV; ++j) load8<X, VEC>(p.x, xr, c0 + j * 256, p.cols, v[j]);
+    for (int j = 0; j < NV; ++j) fetch<X, VEC>(p.x, xr, c0 + j * 256, cols, x[j]);
     if constexpr (!__is_same(R, void)) {
+      Raw<R, VEC> t[NV];
       const long long rr = p.r.row(r), wr = p.ro.row(r);
-      float t[NV][8];
 #pragma unroll
-      for (int j = 0; j < NV; ++j) load8<R, VEC>(p.r, rr, c0 + j * 256, p.cols, t[j]);
+      for (int j = 0; j < NV; ++j) fetch<R, VEC>(p.r, rr, c0 + j * 256, cols, t[j]);
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
+        float2 u[4];
+        values<X, VEC>(x[j], v[j]);
+        values<R, VEC>(t[j], u);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[j][i] += t[j][i];
-        store8<R, VEC>(p.ro, wr, c0 + j * 256, p.cols, v[j]);
+        for (int i = 0; i < 4; ++i) v[j][i] = add2(v[j][i], u[i]);
+        store8<R, VEC>(p.ro, wr, c0 + j * 256, cols, v[j]);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) values<X, VEC>(x[j], v[j]);
+    }
+  }
+  float scale = 1.f;
+  float2 sum2 = make_float2(0.f, 0.f);
+  if constexpr (NORM) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum2 = fma2(v[j][i], v[j][i], sum2);
+    if (p.w != nullptr) {
+      Rows m{};
+      m.data = const_cast<void*>(p.w);
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        float2 w[4];
+        if (p.w_f32) load8<float, VEC>(m, 0, c0 + j * 256, cols, w);
+        else load8<__nv_bfloat16, VEC>(m, 0, c0 + j * 256, cols, w);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[j][i] = mul2(v[j][i], w[i]);
       }
     }
   }
+  uint32_t top[NV][2];
+  if constexpr (FP8) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) block_max<VEC>(v[j], lane, top[j]);
+  }
   if constexpr (NORM) {
-    float sum = 0.f;
-    if (live) {
+    float sum = sum2.x + sum2.y;
 #pragma unroll
-      for (int j = 0; j < NV; ++j)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum = fmaf(v[j][i], v[j][i], sum);
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    }
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if (p.W > 1) {                                            // the same for every thread of the launch
       if (lane == 0) part[warp] = sum;
       __syncthreads();
       sum = 0.f;
-      if (live) for (int i = 0; i < p.W; ++i) sum += part[slot * p.W + i];
+      for (int i = 0; i < p.W; ++i) sum += part[min(slot * p.W + i, THREADS / 32 - 1)];
     }
-    if (!live) return;
-    const float scale = rsqrtf(sum / (float)p.cols + p.eps);
+    scale = rsqrtf(sum / (float)p.cols + p.eps);
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      float w[8];
-      if (p.w == nullptr) {
+    for (int j = 0; j < NV; ++j)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = 1.f;
-      } else {
-        Rows m{};
-        m.data = const_cast<void*>(p.w);
-        if (p.w_f32) load8<float, VEC>(m, 0, c0 + j * 256, p.cols, w);
-        else load8<__nv_bfloat16, VEC>(m, 0, c0 + j * 256, p.cols, w);
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[j][i] = v[j][i] * scale * w[i];
-    }
+      for (int i = 0; i < 4; ++i) v[j][i] = mul2(v[j][i], make_float2(scale, scale));
   }
   if (!live) return;
   if constexpr (!FP8) {
     const long long wr = p.o.row(r);
 #pragma unroll
-    for (int j = 0; j < NV; ++j) store8<__nv_bfloat16, VEC>(p.o, wr, c0 + j * 256, p.cols, v[j]);
+    for (int j = 0; j < NV; ++j) store8<__nv_bfloat16, VEC>(p.o, wr, c0 + j * 256, cols, v[j]);
   } else {
     uint8_t* q = p.q + (long long)r * p.pitch;
     uint32_t pair[NV];                                        // the bytes of a vector's two blocks, the first one's in the low byte
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int c = c0 + j * 256;
+      uint32_t byte[2];
+      float inv[2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        if constexpr (NORM) top[j][b] = __float_as_uint(__uint_as_float(top[j][b]) * scale);
+        byte[b] = scale_byte(top[j][b]);
+        inv[b] = inverse_scale(byte[b]);
+      }
       if constexpr (VEC) {
-        uint32_t top = 0u;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[j][i]) & 0x7fffffffu);   // as bits, NaN is above infinity
-#pragma unroll
-        for (int o = 8; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-        const uint32_t byte = scale_byte(top);
-        const float inv = inverse_scale(byte);
-        const uint32_t other = __shfl_xor_sync(0xffffffffu, byte, 16);
-        pair[j] = lane < 16 ? byte | other << 8 : other | byte << 8;
+        const float f = lane < 16 ? inv[0] : inv[1];
         uint32_t w[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = pack_e4m3(v[j][2 * i] * inv, v[j][2 * i + 1] * inv);
-        if (c < p.cols) *reinterpret_cast<uint2*>(q + c) = make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
+        for (int i = 0; i < 4; ++i) { const float2 y = mul2(v[j][i], make_float2(f, f)); w[i] = pack_e4m3(y.x, y.y); }
+        if (c < cols) *reinterpret_cast<uint2*>(q + c) = make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
       } else {
-        uint32_t top[2] = {0u, 0u};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top[i / 4] = max(top[i / 4], __float_as_uint(v[j][i]) & 0x7fffffffu);
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          top[b] = __reduce_max_sync(0xffffffffu, top[b]);
-          top[b] = scale_byte(top[b]);
-          const float inv = inverse_scale(top[b]);
-#pragma unroll
-          for (int i = 4 * b; i < 4 * b + 4; ++i)
-            if (c + 32 * i < p.cols) q[c + 32 * i] = (uint8_t)pack_e4m3(v[j][i] * inv, 0.f);
-        }
-        pair[j] = top[0] | top[1] << 8;
+        for (int i = 0; i < 8; ++i)
+          if (c + 32 * i < cols) q[c + 32 * i] = (uint8_t)pack_e4m3((i % 2 ? v[j][i / 2].y : v[j][i / 2].x) * inv[i / 4], 0.f);
       }
       // blocks behind the last column keep the byte 0
-      const int k = (first + j * 256) / 128;
-      if (128 * k >= p.cols) pair[j] = 0u;
-      else if (128 * (k + 1) >= p.cols) pair[j] &= 0xffu;
+      const int k = first + j * 256;
+      pair[j] = k + 128 < p.cols ? byte[0] | byte[1] << 8 : k < p.cols ? byte[0] : 0u;
     }
     // four blocks' bytes are a word: lane g writes the one of this warp's group g
 #pragma unroll
@@ -206,7 +269,7 @@ __global__ void __launch_bounds__(THREADS) quantize_block_kernel(const __grid_co
   __shared__ uint32_t part[THREADS / 32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int c0 = blockIdx.x * 128, row0 = blockIdx.y * 128;
-  float v[8][8];
+  float2 v[8][4];
   uint32_t top = 0u;
   griddep_wait();
 #pragma unroll
@@ -218,11 +281,12 @@ __global__ void __launch_bounds__(THREADS) quantize_block_kernel(const __grid_co
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int row = row0 + warp * 16 + j * 2 + i / 4, c = c0 + i % 4 * 32 + lane;
-        v[j][i] = row < p.rows && c < p.cols ? (float)static_cast<const X*>(p.x.data)[p.x.row(row) + p.x.col(c)] : 0.f;
+        const float f = row < p.rows && c < p.cols ? (float)static_cast<const X*>(p.x.data)[p.x.row(row) + p.x.col(c)] : 0.f;
+        if (i % 2) v[j][i / 2].y = f; else v[j][i / 2].x = f;
       }
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[j][i]) & 0x7fffffffu);
+    for (int i = 0; i < 4; ++i) top = max(top, __float_as_uint(max_abs(v[j][i].x, v[j][i].y, 0.f)));
   }
   top = __reduce_max_sync(0xffffffffu, top);
   if (lane == 0) part[warp] = top;
@@ -237,13 +301,13 @@ __global__ void __launch_bounds__(THREADS) quantize_block_kernel(const __grid_co
       const int row = row0 + j * 16 + warp * 2 + lane / 16, c = c0 + lane % 16 * 8;
       uint32_t w[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = pack_e4m3(v[j][2 * i] * inv, v[j][2 * i + 1] * inv);
+      for (int i = 0; i < 4; ++i) w[i] = pack_e4m3(v[j][i].x * inv, v[j][i].y * inv);
       if (row < p.rows && c < p.cols) *reinterpret_cast<uint2*>(p.q + (long long)row * p.pitch + c) = make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int row = row0 + warp * 16 + j * 2 + i / 4, c = c0 + i % 4 * 32 + lane;
-        if (row < p.rows && c < p.cols) p.q[(long long)row * p.pitch + c] = (uint8_t)pack_e4m3(v[j][i] * inv, 0.f);
+        if (row < p.rows && c < p.cols) p.q[(long long)row * p.pitch + c] = (uint8_t)pack_e4m3((i % 2 ? v[j][i / 2].y : v[j][i / 2].x) * inv, 0.f);
       }
     }
   }
