@@ -60,10 +60,9 @@ inline bool apart(const as_rows_t& x, long long rows, long long cols) {
   return true;
 }
 
-// 16 bytes at a time?
-inline bool rows_vec(const as_rows_t& x) {
-  const long long mask = 7;
-  return aligned(x.data, 16) && ((x.head_dim | x.stride_batch | x.stride_head | x.stride_token) & mask) == 0;
+// Whether rows can move `bytes` at a time (16, 32), with 8 or 16 bf16 columns: address, strides and heads are multiples of as much.
+inline bool rows_vec(const as_rows_t& x, int bytes) {
+  return aligned(x.data, bytes) && ((x.head_dim | x.stride_batch | x.stride_head | x.stride_token) & (bytes / 2 - 1)) == 0;
 }
 
 inline Rows rows_of(const as_rows_t& x, long long rows, long long cols) {

@@ -446,7 +446,7 @@ extern "C" as_status_t as_matmul_fp8(as_fp8_context_t h, const as_matmul_fp8_t* 
   p.sw = static_cast<const uint8_t*>(a->w.scales); p.sw_rows = a->w.scale_rows;
   p.bias = static_cast<const __nv_bfloat16*>(a->bias);
   p.status = h->status;
-  p.vec = rows_vec(a->out);
+  p.vec = rows_vec(a->out, 16);
   const int CG = p.M > BM ? 2 : 1;
   p.bn = 192;
   p.nt = (p.N + p.bn - 1) / p.bn;
