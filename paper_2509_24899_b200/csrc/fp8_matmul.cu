@@ -37,7 +37,7 @@ enum { B_FULL = 0, B_EMPTY = B_FULL + MAX_STAGES, B_SFULL = B_EMPTY + MAX_STAGES
        B_AEMPTY = B_AFULL + 2, B_COUNT = B_AEMPTY + 2 };
 // head of shared memory: barriers, tensor-memory address, abort flag; bias and staging of the four result warps; then the stages
 constexpr int HEAD_BYTES = 512;
-constexpr int STAGING = 32 * 128 + 256;     // per warp: 32 rows of 128 bytes, 64 biases
+constexpr int STAGING = 32 * 128 + 4 * MAX_BN;      // per warp: 32 rows of 128 bytes, a tile's biases
 constexpr int STAGING_OFF = HEAD_BYTES;
 constexpr int STAGES_OFF = (STAGING_OFF + 4 * STAGING + 1023) / 1024 * 1024;
 static_assert(B_COUNT * 8 + 8 <= HEAD_BYTES, "");
@@ -99,23 +99,18 @@ AS_DEV constexpr uint32_t scale_byte_of(int k) { return (uint32_t)k << 4 | (uint
 AS_DEV uint32_t cta_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
 // The address of the leading CTA's copy of a shared-memory word, for arrivals and copies across the pair.
 AS_DEV uint32_t leaders(uint32_t addr) { uint32_t r; asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr)); return r; }
+// Arrives at the leading CTA's barrier behind this warp's accesses to tensor memory, which tcgen05.wait has seen to the end and tcgen05.fence orders: nothing else is
+// handed over, so nothing is released (a release to the cluster waits for the warp's stores to global memory, and an acquire of it by the warp that issues the MMAs took 700 clk
+// each time: 36 % of the products' time).
 template <int CG>
 AS_DEV void arrive_leader(uint32_t bar) {
   if constexpr (CG == 1) mbar_arrive(bar);
-  else asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(leaders(bar)) : "memory");
+  else asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(leaders(bar)) : "memory");
 }
 template <int CG>
 AS_DEV void pair_sync() {
   if constexpr (CG == 2) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// A wait for arrivals from both CTAs: as mbar_wait, but what the peer wrote ahead of its arrival is visible as well.
-template <int CG>
-AS_DEV bool wait_pair(uint32_t bar, uint32_t parity, const WaitCtx& w) {
-  const bool ok = mbar_wait(bar, parity, w);
-  if constexpr (CG == 2) asm volatile("fence.acq_rel.cluster;" ::: "memory");
-  return ok;
-}
-
 AS_DEV void tmem_st4(uint32_t at, const uint32_t (&r)[4]) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
 }
@@ -168,6 +163,7 @@ out:
   }
 }
 
+// One lane walks the loop.
 template <int CG>
 AS_DEV void mm_issue(const MMParams& p, const Ctx<CG>& c) {
   const uint32_t stage_bytes = (uint32_t)(BM + p.bn / CG) * BK;
@@ -175,14 +171,11 @@ AS_DEV void mm_issue(const MMParams& p, const Ctx<CG>& c) {
   Ring r, sf;
   uint32_t buf = 0, turn = 0;
   for (long long t = c.unit; t < p.tiles; t += c.units) {
-    if (!wait_pair<CG>(c.bar(B_AEMPTY + buf), turn ^ 1u, c.wc)) return;
-    tc_fence_after();
+    if (!c.wait(B_AEMPTY + buf, turn ^ 1u)) return;
     const uint32_t d = c.tmem + buf * 256u;
     for (int k = 0; k < p.kb; ++k) {
-      if (k % 4 == 0) {
-        if (!wait_pair<CG>(c.bar(B_SFULL + sf.slot), sf.turn, c.wc)) return;
-        tc_fence_after();
-      }
+      if (k % 4 == 0)
+        if (!c.wait(B_SFULL + sf.slot, sf.turn)) return;
       if (!c.wait(B_FULL + r.slot, r.turn)) return;
       tc_fence_after();
       const uint32_t at = c.sbase + STAGES_OFF + (uint32_t)r.slot * stage_bytes;
@@ -203,38 +196,50 @@ AS_DEV void mm_issue(const MMParams& p, const Ctx<CG>& c) {
   }
 }
 
+// The words of the next 512 columns are on their way from global memory while those of the ones before wait for their slot.
 template <int CG>
 AS_DEV void mm_scales(const MMParams& p, const Ctx<CG>& c, int lane, int quarter) {
   const uint32_t lanes = (uint32_t)quarter * 32u << 16;
   const int groups = (p.kb + 3) / 4;
   const uint32_t ones = 0x7f7f7f7fu;         // rows that are not there
+  uint32_t a[4], w[8];
+  auto fetch = [&](long long t, int g) {
+    if (t >= p.tiles) return;
+    const int m0 = (int)(t / p.nt) * (BM * CG) + (int)c.rank * BM + lane, n0 = (int)(t % p.nt) * p.bn + lane;
+    const uint32_t* ga = reinterpret_cast<const uint32_t*>(p.sa) + (long long)g * p.sa_rows;
+    const uint32_t* gw = reinterpret_cast<const uint32_t*>(p.sw) + (long long)g * p.sw_rows;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) a[j] = m0 + 32 * j < p.M ? __ldg(ga + m0 + 32 * j) : ones;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = 32 * j < p.bn && n0 + 32 * j < p.N ? __ldg(gw + n0 + 32 * j) : ones;
+  };
   Ring sf;
-  for (long long t = c.unit; t < p.tiles; t += c.units) {
-    const int m0 = (int)(t / p.nt) * (BM * CG) + (int)c.rank * BM, n0 = (int)(t % p.nt) * p.bn;
-    for (int g = 0; g < groups; ++g) {
-      uint32_t a[4], w[8];
-      const uint32_t* ga = reinterpret_cast<const uint32_t*>(p.sa) + (long long)g * p.sa_rows;
-      const uint32_t* gw = reinterpret_cast<const uint32_t*>(p.sw) + (long long)g * p.sw_rows;
+  long long t = c.unit;
+  int g = 0;
+  fetch(t, g);
+  while (t < p.tiles) {
+    uint32_t a0[4], w0[8];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) { const int m = m0 + 32 * j + lane; a[j] = m < p.M ? __ldg(ga + m) : ones; }
+    for (int j = 0; j < 4; ++j) a0[j] = a[j];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) { const int n = n0 + 32 * j + lane; w[j] = 32 * j < p.bn && n < p.N ? __ldg(gw + n) : ones; }
-      const bool ok = c.wait(B_SEMPTY + sf.slot, sf.turn ^ 1u);
-      if (!__all_sync(0xffffffffu, ok)) return;
-      tc_fence_after();
-      const uint32_t at = c.tmem + lanes + sf_col(sf.slot);
-      tmem_st4(at, a);
-      tmem_st8(at + 8, w);
-      tmem_st_wait();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) arrive_leader<CG>(c.bar(B_SFULL + sf.slot));
-      sf.next(SF_SLOTS);
-    }
+    for (int j = 0; j < 8; ++j) w0[j] = w[j];
+    if (++g == groups) { g = 0; t += c.units; }
+    fetch(t, g);
+    const bool ok = c.wait(B_SEMPTY + sf.slot, sf.turn ^ 1u);
+    if (!__all_sync(0xffffffffu, ok)) return;
+    tc_fence_after();
+    const uint32_t at = c.tmem + lanes + sf_col(sf.slot);
+    tmem_st4(at, a0);
+    tmem_st8(at + 8, w0);
+    tmem_st_wait();
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) arrive_leader<CG>(c.bar(B_SFULL + sf.slot));
+    sf.next(SF_SLOTS);
   }
 }
 
-// A strip of 32 rows and up to 64 columns of results on its way out.
+// Results of a tile: this warp's 32 rows, 64 columns at a time.
 template <int CG>
 AS_DEV void mm_results(const MMParams& p, const Ctx<CG>& c, int lane, int quarter) {
   const uint32_t lanes = (uint32_t)quarter * 32u << 16;
@@ -244,6 +249,15 @@ AS_DEV void mm_results(const MMParams& p, const Ctx<CG>& c, int lane, int quarte
   for (long long t = c.unit; t < p.tiles; t += c.units) {
     const int m0 = (int)(t / p.nt) * (BM * CG) + (int)c.rank * BM + quarter * 32, n0 = (int)(t % p.nt) * p.bn;
     const long long my_row = m0 + lane < p.M ? p.out.row((unsigned)(m0 + lane)) : 0;
+    if (p.bias != nullptr) {                  // the tile's biases, while its products run
+#pragma unroll
+      for (int j = 0; j < MAX_BN / 32; ++j) {
+        const int n = n0 + 32 * j + lane;
+        const float b = 32 * j < p.bn && n < p.N ? __bfloat162float(p.bias[n]) : 0.f;
+        asm volatile("st.shared.f32 [%0], %1;" ::"r"(sbias + (32 * j + lane) * 4), "f"(b) : "memory");
+      }
+      __syncwarp();
+    }
     if (!mbar_wait_warp(c.bar(B_AFULL + buf), turn, c.wc)) return;
     tc_fence_after();
     for (int c0 = 0; c0 < p.bn; c0 += 64) {
@@ -251,15 +265,6 @@ AS_DEV void mm_results(const MMParams& p, const Ctx<CG>& c, int lane, int quarte
       uint32_t x[32], y[32];
       tmem_ld32(c.tmem + lanes + buf * 256u + c0, x);
       if (wide) tmem_ld32(c.tmem + lanes + buf * 256u + c0 + 32, y);
-      if (p.bias != nullptr) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int n = n0 + c0 + 32 * j + lane;
-          const float b = n < p.N ? __bfloat162float(p.bias[n]) : 0.f;
-          asm volatile("st.shared.f32 [%0], %1;" ::"r"(sbias + (32 * j + lane) * 4), "f"(b) : "memory");
-        }
-        __syncwarp();
-      }
       tmem_ld_wait(x);
       if (wide) tmem_ld_wait(y);
       if (c0 + 64 >= p.bn) {                  // the accumulator has been read
@@ -272,35 +277,40 @@ AS_DEV void mm_results(const MMParams& p, const Ctx<CG>& c, int lane, int quarte
       for (int h = 0; h < 2; ++h) {
         if (h == 1 && !wide) break;
         uint32_t(&v)[32] = h == 0 ? x : y;
+        if (p.bias != nullptr) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            float4 b;
+            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(b.x), "=f"(b.y), "=f"(b.z), "=f"(b.w) : "r"(sbias + (c0 + 32 * h + 4 * j) * 4));
+            v[4 * j] = __float_as_uint(__uint_as_float(v[4 * j]) + b.x); v[4 * j + 1] = __float_as_uint(__uint_as_float(v[4 * j + 1]) + b.y);
+            v[4 * j + 2] = __float_as_uint(__uint_as_float(v[4 * j + 2]) + b.z); v[4 * j + 3] = __float_as_uint(__uint_as_float(v[4 * j + 3]) + b.w);
+          }
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          float f[8];
+          uint32_t w[4];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(v[8 * i + j]);
-          if (p.bias != nullptr) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              float b0, b1, b2, b3;
-              asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(b0), "=f"(b1), "=f"(b2), "=f"(b3) : "r"(sbias + (32 * h + 8 * i + 4 * j) * 4) : "memory");
-              f[4 * j] += b0; f[4 * j + 1] += b1; f[4 * j + 2] += b2; f[4 * j + 3] += b3;
-            }
-          }
-          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(strip + swz128_chunk_offset((uint32_t)lane, (uint32_t)(4 * h + i))),
-                       "r"(pack_bf16(f[0], f[1])), "r"(pack_bf16(f[2], f[3])), "r"(pack_bf16(f[4], f[5])), "r"(pack_bf16(f[6], f[7])) : "memory");
+          for (int j = 0; j < 4; ++j) w[j] = pack_bf16(__uint_as_float(v[8 * i + 2 * j]), __uint_as_float(v[8 * i + 2 * j + 1]));
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(strip + swz128_chunk_offset((uint32_t)lane, (uint32_t)(4 * h + i))), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3])
+                       : "memory");
         }
       }
       __syncwarp();
       if (p.vec) {
+        // eight lanes a row, 16 bytes a lane
         const int ch = lane & 7, n = n0 + c0 + ch * 8;
         const bool there = n < p.N && (ch < 4 || wide);
-        const long long col = there ? p.out.col((unsigned)n) : 0;
+        __nv_bfloat16* at = out + (there ? p.out.col((unsigned)n) : 0);
+        uint4 w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[i].x), "=r"(w[i].y), "=r"(w[i].z), "=r"(w[i].w)
+                       : "r"(strip + swz128_chunk_offset((uint32_t)(i * 4 + lane / 8), (uint32_t)ch)) : "memory");
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int r = i * 4 + lane / 8;
           const long long row = __shfl_sync(0xffffffffu, my_row, r);
-          uint32_t a0, a1, a2, a3;
-          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(a0), "=r"(a1), "=r"(a2), "=r"(a3) : "r"(strip + swz128_chunk_offset((uint32_t)r, (uint32_t)ch)) : "memory");
-          if (there && m0 + r < p.M) *reinterpret_cast<uint4*>(out + row + col) = make_uint4(a0, a1, a2, a3);
+          if (there && m0 + r < p.M) *reinterpret_cast<uint4*>(at + row) = w[i];
         }
       } else {
 #pragma unroll 1
@@ -308,11 +318,11 @@ AS_DEV void mm_results(const MMParams& p, const Ctx<CG>& c, int lane, int quarte
           const int k = 32 * h + lane, n = n0 + c0 + k;
           const bool there = n < p.N && c0 + k < p.bn;
           const long long col = there ? p.out.col((unsigned)n) : 0;
-#pragma unroll 4
+#pragma unroll 8
           for (int r = 0; r < 32; ++r) {
             const long long row = __shfl_sync(0xffffffffu, my_row, r);
             uint16_t v;
-            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(strip + swz128_chunk_offset((uint32_t)r, (uint32_t)(k / 8)) + (k % 8) * 2) : "memory");
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(strip + swz128_chunk_offset((uint32_t)r, (uint32_t)(k / 8)) + (k % 8) * 2));
             if (there && m0 + r < p.M) *reinterpret_cast<uint16_t*>(out + row + col) = v;
           }
         }
