@@ -10,7 +10,8 @@
 //   warp 2       allocates tensor memory
 //   warps 4-7    scales: the words of 512 columns (one for each of the CTA's rows of a, one for each of the tile's rows of w) from global memory into tensor memory,
 //                the same for each of the four quarters of the lanes, a ring of four
-//   warps 8-11   results: tensor memory -> registers, bias, bf16, a swizzled strip of shared memory per warp, rows of 128 bytes to global memory
+//   warps 8-15   results: tensor memory -> registers, bias, bf16, a strip of shared memory per warp, from where TMA takes it (or the warp itself does, in
+//                layouts that TMA has no boxes for)
 #include <new>
 
 #include "fp8_common.cuh"
@@ -21,26 +22,28 @@ namespace {
 using namespace as_fp8;
 using namespace sm100;
 
-constexpr int MM_THREADS = 384;
+constexpr int MM_THREADS = 512;
 constexpr int BM = 128;                     // rows of a per CTA
 constexpr int BK = 128;                     // columns of a stage, one scale
-constexpr int MAX_BN = 224;                 // two accumulators, and the scales beside them in 512 columns of tensor memory
+constexpr int MAX_BN = 224;                 // two accumulators of it, and the scales, fill the 512 columns of tensor memory; tiles are multiples of 32 wide
 constexpr int MAX_STAGES = 10;
 constexpr int SF_SLOTS = 4;
 constexpr int SMEM_MAX = 227 * 1024;
 
-// tensor memory: accumulators at 0 and 256, scale slots (words of a: 4 columns, of w: 8) in the 32 columns behind each
-AS_DEV constexpr uint32_t sf_col(int slot) { return (slot < 2 ? 224u : 480u - 32u) + 16u * (uint32_t)slot; }
-static_assert(224 + 16 * 2 == 256 && 480 - 32 + 16 * 2 == 480 && 480 - 32 + 16 * 4 == 512, "scale slots fill what the accumulators leave");
+// tensor memory: accumulators at 0 and 256, scale slots (words of a: 4 columns, of w: 8) two behind each
+AS_DEV constexpr uint32_t sf_col(int slot) { return (slot < 2 ? 224u : 448u) + 16u * (uint32_t)slot; }
 
 enum { B_FULL = 0, B_EMPTY = B_FULL + MAX_STAGES, B_SFULL = B_EMPTY + MAX_STAGES, B_SEMPTY = B_SFULL + SF_SLOTS, B_AFULL = B_SEMPTY + SF_SLOTS,
        B_AEMPTY = B_AFULL + 2, B_COUNT = B_AEMPTY + 2 };
-// head of shared memory: barriers, tensor-memory address, abort flag; bias and staging of the four result warps; then the stages
-constexpr int HEAD_BYTES = 512;
-constexpr int STAGING = 32 * 128 + 4 * MAX_BN;      // per warp: 32 rows of 128 bytes, a tile's biases
-constexpr int STAGING_OFF = HEAD_BYTES;
-constexpr int STAGES_OFF = (STAGING_OFF + 4 * STAGING + 1023) / 1024 * 1024;
-static_assert(B_COUNT * 8 + 8 <= HEAD_BYTES, "");
+// shared memory: barriers, tensor-memory address, abort flag; for each of the eight result warps a strip of 32 rows x 32 columns of results, and its biases; then the
+// stages.  (Strips twice as large cost a stage, and the products 3 %.)
+constexpr int STRIP = 32 * 64;
+constexpr int STRIPS_OFF = 1024;
+constexpr int BIAS_OFF = STRIPS_OFF + 8 * STRIP;
+constexpr int STAGES_OFF = BIAS_OFF + 8 * 128;
+static_assert(B_COUNT * 8 + 8 <= STRIPS_OFF && STAGES_OFF % 1024 == 0, "");
+// Byte of 16-byte chunk `ch` of a strip's row: the 64-byte swizzle.
+AS_DEV uint32_t swz64(int row, int ch) { return (uint32_t)(row * 64 + ((ch ^ (row >> 1 & 3)) << 4)); }
 
 struct MMParams {
   const uint8_t *sa, *sw;
@@ -51,7 +54,7 @@ struct MMParams {
   int M, N, kb;                             // kb: blocks of 128 columns
   int bn, stages, nt;
   long long tiles;
-  bool vec;                                 // results move 16 bytes at a time
+  bool vec, copies;                         // results move 16 bytes at a time, or in boxes of 32 rows x 32 columns by TMA
 };
 
 // ---------------------------------------------------------------- instructions of CTA pairs and of the block-scaled kind
@@ -74,6 +77,11 @@ AS_DEV void load_box(uint32_t dst, const CUtensorMap* m, uint32_t bar, int x, in
   else
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4}], [%2];"
                  ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(x), "r"(y) : "memory");
+}
+// Copy of a strip of results out: column of the head, token, head, batch entry.
+AS_DEV void store_box(const CUtensorMap* m, uint32_t src, int x, int t, int h, int b) {
+  asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];"
+               ::"l"(reinterpret_cast<uint64_t>(m)), "r"(src), "r"(x), "r"(t), "r"(h), "r"(b) : "memory");
 }
 // One arrival at `bar`, of both CTAs of a pair, when the MMAs issued so far have completed.
 template <int CG>
@@ -239,104 +247,114 @@ AS_DEV void mm_scales(const MMParams& p, const Ctx<CG>& c, int lane, int quarter
   }
 }
 
-// Results of a tile: this warp's 32 rows, 64 columns at a time.
+// Results of a tile: this warp's 32 rows, every second 32 columns, through a strip of shared memory.
 template <int CG>
-AS_DEV void mm_results(const MMParams& p, const Ctx<CG>& c, int lane, int quarter) {
+AS_DEV void mm_results(const MMParams& p, const Ctx<CG>& c, const CUtensorMap* mo, int lane, int warp) {
+  const int quarter = warp & 3, half = warp >> 2;
   const uint32_t lanes = (uint32_t)quarter * 32u << 16;
-  const uint32_t strip = c.sbase + STAGING_OFF + (uint32_t)quarter * STAGING, sbias = strip + 32 * 128;
+  const uint32_t strip = c.sbase + STRIPS_OFF + (uint32_t)warp * STRIP, sbias = c.sbase + BIAS_OFF + (uint32_t)warp * 128;
   __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out.data);
   uint32_t buf = 0, turn = 0;
   for (long long t = c.unit; t < p.tiles; t += c.units) {
     const int m0 = (int)(t / p.nt) * (BM * CG) + (int)c.rank * BM + quarter * 32, n0 = (int)(t % p.nt) * p.bn;
     const long long my_row = m0 + lane < p.M ? p.out.row((unsigned)(m0 + lane)) : 0;
-    if (p.bias != nullptr) {                  // the tile's biases, while its products run
+    // a strip's store is one copy where its rows belong to one batch entry
+    const unsigned batch = p.out.batched ? (unsigned)m0 / p.out.tokens : 0u, token = (unsigned)m0 - batch * p.out.tokens;
+    const bool whole = p.copies && (int)token + min(32, p.M - m0) <= (int)p.out.tokens;
+    // biases of this lane's column in each strip, while the products run
+    float bias[(MAX_BN / 32 + 1) / 2];
 #pragma unroll
-      for (int j = 0; j < MAX_BN / 32; ++j) {
-        const int n = n0 + 32 * j + lane;
-        const float b = 32 * j < p.bn && n < p.N ? __bfloat162float(p.bias[n]) : 0.f;
-        asm volatile("st.shared.f32 [%0], %1;" ::"r"(sbias + (32 * j + lane) * 4), "f"(b) : "memory");
-      }
-      __syncwarp();
+    for (int j = 0; j < (MAX_BN / 32 + 1) / 2; ++j) {
+      const int n = n0 + 64 * j + 32 * half + lane;
+      bias[j] = p.bias != nullptr && n < p.N ? __bfloat162float(p.bias[n]) : 0.f;
     }
-    if (!mbar_wait_warp(c.bar(B_AFULL + buf), turn, c.wc)) return;
+    if (!mbar_wait_warp(c.bar(B_AFULL + buf), turn, c.wc)) break;
     tc_fence_after();
-    for (int c0 = 0; c0 < p.bn; c0 += 64) {
-      const bool wide = c0 + 32 < p.bn;
-      uint32_t x[32], y[32];
+    if (32 * half >= p.bn) {
+      __syncwarp();
+      if (lane == 0) arrive_leader<CG>(c.bar(B_AEMPTY + buf));
+    }
+#pragma unroll
+    for (int j = 0; j < (MAX_BN / 32 + 1) / 2; ++j) {
+      const int c0 = 64 * j + 32 * half, n1 = n0 + c0;
+      if (c0 >= p.bn) break;
+      uint32_t x[32];
       tmem_ld32(c.tmem + lanes + buf * 256u + c0, x);
-      if (wide) tmem_ld32(c.tmem + lanes + buf * 256u + c0 + 32, y);
+      if (lane == 0) tma_store_wait_read();   // the copy of the strip before has read it
+      if (p.bias != nullptr) asm volatile("st.shared.f32 [%0], %1;" ::"r"(sbias + lane * 4), "f"(bias[j]) : "memory");
+      __syncwarp();
       tmem_ld_wait(x);
-      if (wide) tmem_ld_wait(y);
-      if (c0 + 64 >= p.bn) {                  // the accumulator has been read
+      if (c0 + 64 >= p.bn) {                  // this warp has read its part of the accumulator
         tc_fence_before();
         __syncwarp();
         if (lane == 0) arrive_leader<CG>(c.bar(B_AEMPTY + buf));
       }
-      // this lane's row into the strip, 16 bytes a chunk, chunks xored with the row
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        if (h == 1 && !wide) break;
-        uint32_t(&v)[32] = h == 0 ? x : y;
-        if (p.bias != nullptr) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            float4 b;
-            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(b.x), "=f"(b.y), "=f"(b.z), "=f"(b.w) : "r"(sbias + (c0 + 32 * h + 4 * j) * 4));
-            v[4 * j] = __float_as_uint(__uint_as_float(v[4 * j]) + b.x); v[4 * j + 1] = __float_as_uint(__uint_as_float(v[4 * j + 1]) + b.y);
-            v[4 * j + 2] = __float_as_uint(__uint_as_float(v[4 * j + 2]) + b.z); v[4 * j + 3] = __float_as_uint(__uint_as_float(v[4 * j + 3]) + b.w);
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t w[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) w[j] = pack_bf16(__uint_as_float(v[8 * i + 2 * j]), __uint_as_float(v[8 * i + 2 * j + 1]));
-          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(strip + swz128_chunk_offset((uint32_t)lane, (uint32_t)(4 * h + i))), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3])
-                       : "memory");
-        }
-      }
-      __syncwarp();
-      if (p.vec) {
-        // eight lanes a row, 16 bytes a lane
-        const int ch = lane & 7, n = n0 + c0 + ch * 8;
-        const bool there = n < p.N && (ch < 4 || wide);
-        __nv_bfloat16* at = out + (there ? p.out.col((unsigned)n) : 0);
-        uint4 w[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[i].x), "=r"(w[i].y), "=r"(w[i].z), "=r"(w[i].w)
-                       : "r"(strip + swz128_chunk_offset((uint32_t)(i * 4 + lane / 8), (uint32_t)ch)) : "memory");
+      if (p.bias != nullptr) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const int r = i * 4 + lane / 8;
+          float4 b;
+          asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(b.x), "=f"(b.y), "=f"(b.z), "=f"(b.w) : "r"(sbias + i * 16) : "memory");
+          x[4 * i] = __float_as_uint(__uint_as_float(x[4 * i]) + b.x); x[4 * i + 1] = __float_as_uint(__uint_as_float(x[4 * i + 1]) + b.y);
+          x[4 * i + 2] = __float_as_uint(__uint_as_float(x[4 * i + 2]) + b.z); x[4 * i + 3] = __float_as_uint(__uint_as_float(x[4 * i + 3]) + b.w);
+        }
+      }
+      // this lane's row of 64 bytes into the strip, with the 64-byte swizzle
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = pack_bf16(__uint_as_float(x[8 * i + 2 * k]), __uint_as_float(x[8 * i + 2 * k + 1]));
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(strip + swz64(lane, i)), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+      }
+      if (whole) {
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0 && m0 < p.M && n1 < p.N) {
+          const unsigned head = p.out.hd == p.N ? 0u : (unsigned)n1 / (unsigned)p.out.hd;
+          store_box(mo, strip, n1 - (int)head * p.out.hd, (int)token, (int)head, (int)batch);
+          tma_store_commit();
+        }
+      } else if (p.vec) {
+        __syncwarp();
+        // four lanes a row, 16 bytes a lane
+        const int ch = lane & 3, n = n1 + ch * 8;
+        const bool there = n < p.N;
+        __nv_bfloat16* at = out + (there ? p.out.col((unsigned)n) : 0);
+        uint4 w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[i].x), "=r"(w[i].y), "=r"(w[i].z), "=r"(w[i].w) : "r"(strip + swz64(i * 8 + lane / 4, ch)) : "memory");
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = i * 8 + lane / 4;
           const long long row = __shfl_sync(0xffffffffu, my_row, r);
           if (there && m0 + r < p.M) *reinterpret_cast<uint4*>(at + row) = w[i];
         }
+        __syncwarp();
       } else {
-#pragma unroll 1
-        for (int h = 0; h < 2; ++h) {
-          const int k = 32 * h + lane, n = n0 + c0 + k;
-          const bool there = n < p.N && c0 + k < p.bn;
-          const long long col = there ? p.out.col((unsigned)n) : 0;
+        __syncwarp();
+        const bool there = n1 + lane < p.N;
+        __nv_bfloat16* at = out + (there ? p.out.col((unsigned)(n1 + lane)) : 0);
 #pragma unroll 8
-          for (int r = 0; r < 32; ++r) {
-            const long long row = __shfl_sync(0xffffffffu, my_row, r);
-            uint16_t v;
-            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(strip + swz128_chunk_offset((uint32_t)r, (uint32_t)(k / 8)) + (k % 8) * 2));
-            if (there && m0 + r < p.M) *reinterpret_cast<uint16_t*>(out + row + col) = v;
-          }
+        for (int r = 0; r < 32; ++r) {
+          const long long row = __shfl_sync(0xffffffffu, my_row, r);
+          uint16_t v;
+          asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(strip + swz64(r, lane / 8) + (lane % 8) * 2) : "memory");
+          if (there && m0 + r < p.M) *reinterpret_cast<uint16_t*>(at + row) = v;
         }
+        __syncwarp();
       }
-      __syncwarp();
     }
     buf ^= 1u;
     if (buf == 0) turn ^= 1u;
   }
+  if (lane == 0) tma_store_wait_read();       // (the writes land by the end of the kernel)
 }
 
 template <int CG>
 __global__ void __launch_bounds__(MM_THREADS, 1)
-matmul_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mw, const __grid_constant__ MMParams p) {
+matmul_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mw, const __grid_constant__ CUtensorMap mo,
+              const __grid_constant__ MMParams p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);      // the same in both CTAs of a pair
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + 8 * B_COUNT);
@@ -347,7 +365,7 @@ matmul_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CU
     *abort_flag = 0u;
     for (int s = 0; s < MAX_STAGES; ++s) { mbar_init(c.bar(B_FULL + s), 1); mbar_init(c.bar(B_EMPTY + s), 1); }
     for (int s = 0; s < SF_SLOTS; ++s) { mbar_init(c.bar(B_SFULL + s), 4 * CG); mbar_init(c.bar(B_SEMPTY + s), 1); }
-    for (int s = 0; s < 2; ++s) { mbar_init(c.bar(B_AFULL + s), 1); mbar_init(c.bar(B_AEMPTY + s), 4 * CG); }
+    for (int s = 0; s < 2; ++s) { mbar_init(c.bar(B_AFULL + s), 1); mbar_init(c.bar(B_AEMPTY + s), 8 * CG); }
     fence_barrier_init();
     fence_proxy_async();
     tma_prefetch_desc(&ma); tma_prefetch_desc(&mw);
@@ -368,7 +386,7 @@ matmul_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CU
   } else if (warp >= 4 && warp < 8) {
     mm_scales<CG>(p, c, lane, warp - 4);
   } else if (warp >= 8) {
-    mm_results<CG>(p, c, lane, warp - 8);
+    mm_results<CG>(p, c, &mo, lane, warp - 8);
   }
   if (*abort_flag != 0u) {                     // a wait ran out: copies and MMAs under way get 20 us (they take two) before memory is given back
     const long long t0 = clock64();
@@ -384,7 +402,7 @@ matmul_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CU
 }
 
 template <int CG>
-cudaError_t launch(const CUtensorMap& ma, const CUtensorMap& mw, const MMParams& p, int units, size_t smem, cudaStream_t st) {
+cudaError_t launch(const CUtensorMap& ma, const CUtensorMap& mw, const CUtensorMap& mo, const MMParams& p, int units, size_t smem, cudaStream_t st) {
   cudaLaunchAttribute attr[2]{};
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -393,7 +411,7 @@ cudaError_t launch(const CUtensorMap& ma, const CUtensorMap& mw, const MMParams&
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(units * CG)); cfg.blockDim = dim3(MM_THREADS); cfg.dynamicSmemBytes = smem; cfg.stream = st;
   cfg.attrs = attr; cfg.numAttrs = CG == 1 ? 1 : 2;
-  return cudaLaunchKernelEx(&cfg, matmul_kernel<CG>, ma, mw, p);
+  return cudaLaunchKernelEx(&cfg, matmul_kernel<CG>, ma, mw, mo, p);
 }
 
 }  // namespace
@@ -465,10 +483,12 @@ extern "C" as_status_t as_matmul_fp8(as_fp8_context_t h, const as_matmul_fp8_t* 
   p.stages = (SMEM_MAX - 1024 - STAGES_OFF) / stage;
   if (p.stages > MAX_STAGES) p.stages = MAX_STAGES;
   const size_t smem = 1024 + STAGES_OFF + (size_t)p.stages * stage;
-  CUtensorMap ma, mw;
+  CUtensorMap ma, mw, mo{};
+  // results leave by TMA where 32 columns are of one head (a map that the driver does not take leaves that to the warps)
+  p.copies = p.vec && (a->out.head_dim == p.N || a->out.head_dim % 32 == 0) && as_tc::make_map_rows(&mo, a->out, p.M, p.N, 32);
   if (!as_tc::make_map_bytes(&ma, a->a.data, a->cols, p.M, a->a.pitch, BM) || !as_tc::make_map_bytes(&mw, a->w.data, a->cols, p.N, a->w.pitch, p.bn / CG)) return AS_ERR_CUDA;
   const int units = (int)(p.tiles < h->sms / CG ? p.tiles : h->sms / CG);
   const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const cudaError_t e = CG == 2 ? launch<2>(ma, mw, p, units, smem, st) : launch<1>(ma, mw, p, units, smem, st);
+  const cudaError_t e = CG == 2 ? launch<2>(ma, mw, mo, p, units, smem, st) : launch<1>(ma, mw, mo, p, units, smem, st);
   return e == cudaSuccess ? AS_OK : AS_ERR_CUDA;
 }
