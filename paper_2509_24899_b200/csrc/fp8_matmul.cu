@@ -12,6 +12,7 @@
 //                the same for each of the four quarters of the lanes, a ring of four
 //   warps 8-15   results: tensor memory -> registers, bias, bf16, a strip of shared memory per warp, from where TMA takes it (or the warp itself does, in
 //                layouts that TMA has no boxes for)
+#include <algorithm>
 #include <new>
 
 #include "fp8_common.cuh"
@@ -401,6 +402,138 @@ matmul_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CU
   }
 }
 
+// ---------------------------------------------------------------- few rows
+// Up to 8 rows of a, where a tile of the pair would be empty but for some and few CTAs would walk all columns: here w is read once, by all SMs, into the operands
+// of the warps' own matrix instructions (16 rows of w, 8 of a, 32 columns).  A CTA takes units of 16 rows of w; its warps take every sixteenth block of 128 columns each, with one
+// scale for a row and block: four instructions into fresh sums, which are scaled and added up in fp32.  Which columns an instruction calls its k-th does not matter as
+// long as both operands agree: a lane holds columns 16 q .. 16 q + 15 of each half of its rows' block, so that four lanes copy 64 bytes in a run.  The warps' sums meet in shared memory, in the order of the warps.
+//
+// What bounds it is the latency of memory, and then the number of copies: a lane's operands come by asynchronous copies into slots that its warp alone reads, FEW_AHEAD blocks ahead and
+// on into the next unit, one copy for all scales of a block.  (2 rows by w of 1536 x 1536, 9216 x 1536, 1536 x 6144, 6144 x 6144: straight into registers 2.7, 5.5, 5.7, 13.2 us;
+// two CTAs of 8 warps 2.6, 4.5, 6.4, 12.7; one of 16 warps 2.0, 5.0, 4.0, 10.5 us (3.6 TB/s).)
+constexpr int FEW_ROWS = 8;
+constexpr int FEW_WARPS = 16, FEW_COLS = 16;
+constexpr int FEW_AHEAD = 3;                // blocks of a warp under way; one CTA an SM
+constexpr int FEW_SLOT = 6 * 512 + 128;     // bytes of a warp's block: per lane 64 of w and 32 of a, the scale words of 16 rows of w and 8 of a
+constexpr int FEW_SMEM = FEW_WARPS * FEW_AHEAD * FEW_SLOT;
+
+struct FewParams {
+  const uint8_t *a, *w, *sa, *sw;
+  const __nv_bfloat16* bias;
+  Rows out;
+  long long a_pitch, w_pitch, sa_rows, sw_rows;
+  int M, N, K, units;
+};
+
+// 16 bytes, of which `bytes` come from memory and the rest are 0: of w past the first-level cache, of a, which every CTA reads, through it (past it they all
+// meet at the same lines of the second one: eight times as long).
+AS_DEV void few_copy_w(uint32_t dst, const void* src, int bytes) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory"); }
+AS_DEV void few_copy_a(uint32_t dst, const void* src, int bytes) { asm volatile("cp.async.ca.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory"); }
+AS_DEV void few_copy4(uint32_t dst, const void* src) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory"); }
+AS_DEV void few_read(uint32_t at, uint32_t (&r)[4]) {
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+// 2^(e - 127) of a scale byte: exact for 0 (a subnormal number), NaN for 255.
+AS_DEV float few_scale(uint32_t e) { return __uint_as_float(e == 0u ? 0x00400000u : e == 255u ? 0x7fc00000u : e << 23); }
+
+__global__ void __launch_bounds__(FEW_WARPS * 32, 1) few_rows_kernel(const __grid_constant__ FewParams p) {
+  griddep_launch();
+  extern __shared__ __align__(16) uint8_t slots[];
+  __shared__ float sums[2][FEW_WARPS][FEW_ROWS][FEW_COLS + 1];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane / 4, q = lane % 4;
+  const int kb = (p.K + BK - 1) / BK;
+  const uint32_t mine = smem_u32(slots) + (uint32_t)warp * (FEW_AHEAD * FEW_SLOT) + lane * 16;
+  griddep_wait();
+  const uint8_t* ar = p.a + (long long)min(g, p.M - 1) * p.a_pitch;   // rows that are not there are read as the last one, and their results not written
+  int unit = blockIdx.x, block = warp, slot = 0;                      // what is asked for next
+  auto ask = [&] {
+    if (block < kb && unit < p.units) {
+      const uint32_t at = mine + slot * FEW_SLOT;
+      const int c = block * BK + q * 16, n = unit * FEW_COLS + g;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int bytes = max(0, min(16, p.K - c - 64 * i)), c1 = bytes > 0 ? c + 64 * i : 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) few_copy_w(at + (2 * h + i) * 512, p.w + (long long)min(n + 8 * h, p.N - 1) * p.w_pitch + c1, bytes);
+        if (g < p.M) few_copy_a(at + (4 + i) * 512, ar + c1, bytes);  // (a row that is not there leaves its results, which are not written, to chance)
+      }
+      const uint8_t* scale = q < 2 ? p.sw + ((long long)(block / 4) * p.sw_rows + min(n + 8 * q, p.N - 1)) * 4 : p.sa + ((long long)(block / 4) * p.sa_rows + min(g, p.M - 1)) * 4;
+      if (q < 3) few_copy4(at - lane * 16 + 6 * 512 + (8 * q + g) * 4, scale);
+      if (++slot == FEW_AHEAD) slot = 0;
+      if ((block += FEW_WARPS) >= kb) { block = warp; unit += gridDim.x; }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");              // (an empty group where there is nothing left: the waits below count groups)
+  };
+#pragma unroll
+  for (int i = 0; i < FEW_AHEAD - 1; ++i) ask();
+  int take = 0, turn = 0;
+  for (int u = blockIdx.x; u < p.units; u += gridDim.x, turn ^= 1) {
+    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int k = warp; k < kb; k += FEW_WARPS) {
+      __syncwarp();                                                   // every lane has read the slot that is filled next
+      ask();
+      asm volatile("cp.async.wait_group %0;" ::"n"(FEW_AHEAD - 1) : "memory");
+      __syncwarp();                                                   // the other lanes' scales have come as well
+      const uint32_t at = mine + take * FEW_SLOT;
+      if (++take == FEW_AHEAD) take = 0;
+      uint32_t w[2][2][4], a[2][4];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        few_read(at + i * 512, w[0][i]);
+        few_read(at + (2 + i) * 512, w[1][i]);
+        few_read(at + (4 + i) * 512, a[i]);
+      }
+      float d[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(w[0][i / 2][2 * (i % 2)]), "r"(w[1][i / 2][2 * (i % 2)]), "r"(w[0][i / 2][2 * (i % 2) + 1]), "r"(w[1][i / 2][2 * (i % 2) + 1]), "r"(a[i / 2][2 * (i % 2)]),
+                       "r"(a[i / 2][2 * (i % 2) + 1]));
+      float f[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {                                   // rows g and g + 8 of w, rows 2 q and 2 q + 1 of a
+        uint32_t e;
+        asm volatile("ld.shared.u8 %0, [%1];" : "=r"(e) : "r"(at - lane * 16 + 6 * 512 + (j < 2 ? 8 * j + g : 16 + 2 * q + j - 2) * 4 + k % 4) : "memory");
+        f[j] = few_scale(e);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[j] = fmaf(d[j] * f[j / 2], f[2 + j % 2], acc[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sums[turn][warp][2 * q + j % 2][g + 8 * (j / 2)] = acc[j];
+    __syncthreads();                                                  // (one for a unit: the next one's sums go to the other half)
+    if (threadIdx.x < FEW_ROWS * FEW_COLS) {
+      const int m = threadIdx.x / FEW_COLS, j = threadIdx.x % FEW_COLS, n = u * FEW_COLS + j;
+      if (m < p.M && n < p.N) {
+        float f = 0.f;
+#pragma unroll
+        for (int i = 0; i < FEW_WARPS; ++i) f += sums[turn][i][m][j];
+        if (p.bias != nullptr) f += __bfloat162float(p.bias[n]);
+        static_cast<__nv_bfloat16*>(p.out.data)[p.out.row((unsigned)m) + p.out.col((unsigned)n)] = __float2bfloat16_rn(f);
+      }
+    }
+  }
+}
+
+// The shape of a tile: CTAs that share it and rows of w, by the time that its turns take on all SMs: turns x blocks of 128 columns x ns a block, and what the reading out of
+// the last turn's results and the meeting of a pair add.  (Measured, ns a block with all SMs busy, 7800 x 4608 x 1536; a single CTA's tile is shorter for
+// few rows and takes no meeting, a pair's is faster from 128 rows of w on.)
+struct Tile { int cg, bn; };
+Tile tile_of(int M, int N, int kb, int sms) {
+  static const int ns[2][7] = {{230, 250, 265, 300, 345, 385, 440}, {228, 230, 240, 262, 297, 320, 380}};
+  Tile best{1, 32};
+  double least = 1e300;
+  for (int cg = 1; cg <= 2; ++cg)
+    for (int i = 0; i < 7; ++i) {
+      const int bn = 32 * (i + 1);
+      const long long tiles = ((long long)M + BM * cg - 1) / (BM * cg) * ((N + bn - 1) / bn), turns = (tiles + sms / cg - 1) / (sms / cg);
+      const double t = (double)turns * kb * ns[cg - 1][i] + 7. * bn + (cg == 2 ? 400. : 0.);
+      if (t < least) { least = t; best = {cg, bn}; }
+    }
+  return best;
+}
+
 template <int CG>
 cudaError_t launch(const CUtensorMap& ma, const CUtensorMap& mw, const CUtensorMap& mo, const MMParams& p, int units, size_t smem, cudaStream_t st) {
   cudaLaunchAttribute attr[2]{};
@@ -428,7 +561,8 @@ extern "C" as_status_t as_fp8_create(as_fp8_context_t* out) {
       cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
     return AS_ERR_CUDA;
   if (major != 10) return AS_ERR_ARCH;
-  if (as_tensor_init() != cudaSuccess || as_tc::opt_in_smem(matmul_kernel<1>, SMEM_MAX) != cudaSuccess || as_tc::opt_in_smem(matmul_kernel<2>, SMEM_MAX) != cudaSuccess)
+  if (as_tensor_init() != cudaSuccess || as_tc::opt_in_smem(matmul_kernel<1>, SMEM_MAX) != cudaSuccess || as_tc::opt_in_smem(matmul_kernel<2>, SMEM_MAX) != cudaSuccess ||
+      as_tc::opt_in_smem(few_rows_kernel, FEW_SMEM) != cudaSuccess)
     return AS_ERR_CUDA;
   as_fp8_context_s* h = new (std::nothrow) as_fp8_context_s;
   if (h == nullptr) return AS_ERR_ALLOC;
@@ -465,30 +599,44 @@ extern "C" as_status_t as_matmul_fp8(as_fp8_context_t h, const as_matmul_fp8_t* 
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return AS_ERR_CUDA;
   if (dev != h->device) return AS_ERR_INVALID_ARG;
-  MMParams p{};
-  p.out = rows_of(a->out, a->rows, a->out_cols);
-  if (p.out.split && a->out_cols * (long long)a->out.head_dim > (1ll << 32)) return AS_ERR_UNSUPPORTED;
+  const Rows out = rows_of(a->out, a->rows, a->out_cols);
+  if (out.split && a->out_cols * (long long)a->out.head_dim > (1ll << 32)) return AS_ERR_UNSUPPORTED;
   if (a->rows == 0) return AS_OK;
+  const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  if (a->rows <= FEW_ROWS) {
+    FewParams p{};
+    p.a = static_cast<const uint8_t*>(a->a.data); p.a_pitch = a->a.pitch;
+    p.w = static_cast<const uint8_t*>(a->w.data); p.w_pitch = a->w.pitch;
+    p.sa = static_cast<const uint8_t*>(a->a.scales); p.sa_rows = a->a.scale_rows;
+    p.sw = static_cast<const uint8_t*>(a->w.scales); p.sw_rows = a->w.scale_rows;
+    p.bias = static_cast<const __nv_bfloat16*>(a->bias);
+    p.out = out;
+    p.M = (int)a->rows; p.N = (int)a->out_cols; p.K = a->cols;
+    p.units = (p.N + FEW_COLS - 1) / FEW_COLS;
+    const cudaError_t e = as_launch_dependent(few_rows_kernel, dim3((unsigned)std::min(p.units, h->sms)), dim3(FEW_WARPS * 32), FEW_SMEM, st, p);
+    return e == cudaSuccess ? AS_OK : AS_ERR_CUDA;
+  }
+  MMParams p{};
+  p.out = out;
   p.M = (int)a->rows; p.N = (int)a->out_cols; p.kb = (a->cols + BK - 1) / BK;
   p.sa = static_cast<const uint8_t*>(a->a.scales); p.sa_rows = a->a.scale_rows;
   p.sw = static_cast<const uint8_t*>(a->w.scales); p.sw_rows = a->w.scale_rows;
   p.bias = static_cast<const __nv_bfloat16*>(a->bias);
   p.status = h->status;
   p.vec = rows_vec(a->out, 16);
-  const int CG = p.M > BM ? 2 : 1;
-  p.bn = 192;
+  const Tile tile = tile_of(p.M, p.N, p.kb, h->sms);
+  const int CG = tile.cg;
+  p.bn = tile.bn;
   p.nt = (p.N + p.bn - 1) / p.bn;
   p.tiles = ((long long)p.M + BM * CG - 1) / (BM * CG) * p.nt;
   const int stage = (BM + p.bn / CG) * BK;
-  p.stages = (SMEM_MAX - 1024 - STAGES_OFF) / stage;
-  if (p.stages > MAX_STAGES) p.stages = MAX_STAGES;
+  p.stages = std::min((SMEM_MAX - 1024 - STAGES_OFF) / stage, MAX_STAGES);
   const size_t smem = 1024 + STAGES_OFF + (size_t)p.stages * stage;
   CUtensorMap ma, mw, mo{};
   // results leave by TMA where 32 columns are of one head (a map that the driver does not take leaves that to the warps)
   p.copies = p.vec && (a->out.head_dim == p.N || a->out.head_dim % 32 == 0) && as_tc::make_map_rows(&mo, a->out, p.M, p.N, 32);
   if (!as_tc::make_map_bytes(&ma, a->a.data, a->cols, p.M, a->a.pitch, BM) || !as_tc::make_map_bytes(&mw, a->w.data, a->cols, p.N, a->w.pitch, p.bn / CG)) return AS_ERR_CUDA;
-  const int units = (int)(p.tiles < h->sms / CG ? p.tiles : h->sms / CG);
-  const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const int units = (int)std::min<long long>(p.tiles, h->sms / CG);
   const cudaError_t e = CG == 2 ? launch<2>(ma, mw, mo, p, units, smem, st) : launch<1>(ma, mw, mo, p, units, smem, st);
   return e == cudaSuccess ? AS_OK : AS_ERR_CUDA;
 }
