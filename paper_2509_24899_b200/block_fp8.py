@@ -17,9 +17,11 @@ import torch
 
 from . import binding
 
-_BF16, _F32, _E4M3 = torch.bfloat16, torch.float32, torch.float8_e4m3fn
+_BF16, _F32, _E4M3, _U8 = torch.bfloat16, torch.float32, torch.float8_e4m3fn, torch.uint8
+_FLOATS, _BF16_ONLY = (_BF16, _F32), (_BF16,)
+_current_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 _DTYPES = {_BF16: binding.AS_DTYPE_BF16, _F32: binding.AS_DTYPE_F32}
-# as_rows_t is QiiqqqQ-like: address, dtype, head_dim, tokens, strides of batch, head, token; as_fp8_matrix_t: address, pitch, scales, scale_rows
+# as_rows_t: address, dtype, head_dim, tokens, strides of batch, head, token; as_fp8_matrix_t: address, pitch, scales, scale_rows
 _ROWS, _MATRIX = "Qiiqqqq", "QqQq"
 _NORM = struct.Struct("=Iiq" + 4 * _ROWS + _MATRIX + "Qif")
 _QUANT = struct.Struct("=Iiq" + _ROWS + _MATRIX + "ii")
@@ -46,62 +48,63 @@ class BlockFp8(NamedTuple):
 
 def empty_fp8(rows: int, cols: int, device=None) -> BlockFp8:
     """Room for a matrix in 8-bit form."""
-    pitch = (cols + 15) & -16
-    data = torch.empty((rows, pitch), dtype=_E4M3, device=device or "cuda")
-    scales = torch.empty(((cols + 511) // 512, rows, 4), dtype=torch.uint8, device=device or "cuda")
-    return BlockFp8(data if pitch == cols else data[:, :cols], scales)
+    device = device or "cuda"
+    return BlockFp8(torch.empty_strided((rows, cols), ((cols + 15) & -16, 1), dtype=_E4M3, device=device),
+                    torch.empty_strided(((cols + 511) // 512, rows, 4), (4 * rows, 4, 1), dtype=torch.uint8, device=device))
 
 
 def _refuse(where, what):
     raise ValueError("%s: %s" % (where, what))
 
 
-def _rows(t, where, name):
-    """((rows, cols), as_rows_t's fields) of a tensor."""
+def _rows(t, here, where, name):
+    """(rows, cols, as_rows_t's fields) of a tensor on device `here`."""
     dtype = _DTYPES.get(t.dtype)
-    if dtype is None or not t.is_cuda:
-        _refuse(where, "%s is a bf16 or fp32 CUDA tensor, not %s on %s" % (name, t.dtype, t.device))
-    if t.dim() == 2:
-        (rows, cols), (st, one) = t.shape, t.stride()
-        # a single row or column leaves its stride open
-        if one != 1 and cols > 1:
-            _refuse(where, "%s's columns lie next to each other; strides are %s" % (name, t.stride()))
-        return (rows, cols), (t.data_ptr(), dtype, cols, rows, 0, 0, st if rows > 1 else 0)
-    if t.dim() != 4:
-        _refuse(where, "%s is [rows, cols] or [B, H, N, d], not %s" % (name, tuple(t.shape)))
-    (b, h, n, d), (sb, sh, st, one) = t.shape, t.stride()
+    if dtype is None or t.get_device() != here:
+        _refuse(where, "%s is a bf16 or fp32 tensor on the current device, cuda:%d, not %s on %s" % (name, here, t.dtype, t.device))
+    shape, strides = t.shape, t.stride()
+    if len(shape) == 2:
+        rows, cols = shape
+        if strides[1] != 1 and cols > 1:      # a single row or column leaves its stride open
+            _refuse(where, "%s's columns lie next to each other; strides are %s" % (name, strides))
+        return rows, cols, (t.data_ptr(), dtype, cols, rows, 0, 0, strides[0] if rows > 1 else 0)
+    if len(shape) != 4:
+        _refuse(where, "%s is [rows, cols] or [B, H, N, d], not %s" % (name, tuple(shape)))
+    (b, h, n, d), (sb, sh, st, one) = shape, strides
     if one != 1 and d > 1:
-        _refuse(where, "%s's columns of a head lie next to each other; strides are %s" % (name, t.stride()))
-    return (b * n, h * d), (t.data_ptr(), dtype, d, n, sb if b > 1 else 0, sh if h > 1 else 0, st if n > 1 else 0)
+        _refuse(where, "%s's columns of a head lie next to each other; strides are %s" % (name, strides))
+    return b * n, h * d, (t.data_ptr(), dtype, d, n, sb if b > 1 else 0, sh if h > 1 else 0, st if n > 1 else 0)
 
 
-def _matrix(m, where, name):
-    """((rows, cols), as_fp8_matrix_t's fields) of a pair."""
+def _matrix(m, here, where, name):
+    """(rows, cols, as_fp8_matrix_t's fields) of a pair on device `here`."""
     data, scales = m
-    if data.dtype != _E4M3 or scales.dtype != torch.uint8 or not data.is_cuda or not scales.is_cuda or data.dim() != 2:
-        _refuse(where, "%s is a pair of CUDA tensors, float8_e4m3fn [rows, cols] and uint8 scales" % name)
-    rows, cols = data.shape
-    st, one = data.stride()
-    groups, srows, four = scales.shape if scales.dim() == 3 else (0, 0, 0)
-    sg, sr, s1 = scales.stride() if scales.dim() == 3 else (0, 0, 0)
-    if groups != (cols + 511) // 512 or srows != rows or four != 4:
-        _refuse(where, "%s's scales for %s are [%d, %d, 4], not %s" % (name, tuple(data.shape), (cols + 511) // 512, rows, tuple(scales.shape)))
+    if data.dtype != _E4M3 or scales.dtype != _U8 or data.get_device() != here or scales.get_device() != here:
+        _refuse(where, "%s is a pair of tensors on the current device, cuda:%d: float8_e4m3fn [rows, cols] and uint8 scales" % (name, here))
+    shape = data.shape
+    if len(shape) != 2:
+        _refuse(where, "%s's values are [rows, cols], not %s" % (name, tuple(shape)))
+    rows, cols = shape
+    groups = (cols + 511) // 512
+    if tuple(scales.shape) != (groups, rows, 4):
+        _refuse(where, "%s's scales for %s are %s, not %s" % (name, tuple(shape), (groups, rows, 4), tuple(scales.shape)))
     if rows == 0:
-        return (0, cols), (data.data_ptr() or 16, (cols + 15) & -16, scales.data_ptr() or 16, 0)
+        return 0, cols, (16, (cols + 15) & -16, 16, 0)
+    (st, one), (sg, sr, s1) = data.stride(), scales.stride()
     if (one != 1 and cols > 1) or s1 != 1 or (sr != 4 and rows > 1) or (groups > 1 and (sg % 4 or sg < 4 * rows)):
         _refuse(where, "%s's strides are %s and %s: values and the four bytes of a row lie next to each other" % (name, data.stride(), scales.stride()))
-    return (rows, cols), (data.data_ptr(), st if rows > 1 else (cols + 15) & -16, scales.data_ptr(), sg // 4 if groups > 1 else rows)
+    return rows, cols, (data.data_ptr(), st if rows > 1 else (cols + 15) & -16, scales.data_ptr(), sg // 4 if groups > 1 else rows)
 
 
-def _stream(stream):
-    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+def _vector(t, n, dtypes, here, where, name):
+    """Address of n values next to each other."""
+    if t.dtype not in dtypes or t.get_device() != here or t.shape != (n,) or (n > 1 and t.stride(0) != 1):
+        _refuse(where, "%s is %d values of %s next to each other on cuda:%d" % (name, n, " or ".join(str(d) for d in dtypes), here))
+    return t.data_ptr()
 
 
-def _same_device(where, *tensors):
-    here = torch._C._cuda_getDevice()
-    for t in tensors:
-        if t is not None and t.get_device() != here:
-            _refuse(where, "all tensors are on the current device, cuda:%d" % here)
+def _stream(stream, here):
+    return stream.cuda_stream if stream is not None else _raw_stream(here)
 
 
 def rms_norm(x, weight=None, residual=None, eps=1e-6, fp8=False, out=None, residual_out=None, stream=None):
@@ -113,53 +116,49 @@ def rms_norm(x, weight=None, residual=None, eps=1e-6, fp8=False, out=None, resid
     residual_out  where t goes, in the residual's type; may be `residual` itself
 
     Returns y, or (y, t) with a residual.  Up to 16384 columns."""
-    (rows, cols), xr = _rows(x, "rms_norm", "x")
-    rr = tr = _NONE_ROWS
+    here = _current_device()
+    rows, cols, xr = _rows(x, here, "rms_norm", "x")
+    rr = tr = yr = _NONE_ROWS
+    ym = _NONE_MATRIX
     if residual is not None:
-        shape, rr = _rows(residual, "rms_norm", "residual")
+        r, c, rr = _rows(residual, here, "rms_norm", "residual")
         if residual_out is None:
-            residual_out = torch.empty(residual.shape, dtype=residual.dtype, device=residual.device)
-        to, tr = _rows(residual_out, "rms_norm", "residual_out")
-        if shape != (rows, cols) or to != shape or residual_out.dtype != residual.dtype:
+            residual_out = torch.empty_like(residual)
+        r1, c1, tr = _rows(residual_out, here, "rms_norm", "residual_out")
+        if r != rows or c != cols or r1 != rows or c1 != cols or residual_out.dtype != residual.dtype:
             _refuse("rms_norm", "residual and residual_out are %d x %d of one type" % (rows, cols))
     elif residual_out is not None:
         _refuse("rms_norm", "residual_out needs a residual")
     wp = wd = 0
     if weight is not None:
-        wd = _DTYPES.get(weight.dtype, -1)
-        if wd < 0 or weight.shape != (cols,) or (weight.stride(0) != 1 and cols > 1):
-            _refuse("rms_norm", "weight is %d bf16 or fp32 values next to each other" % cols)
-        wp = weight.data_ptr()
-    yr, ym = _NONE_ROWS, _NONE_MATRIX
+        wp, wd = _vector(weight, cols, _FLOATS, here, "rms_norm", "weight"), _DTYPES[weight.dtype]
     if fp8:
         if out is None:
-            out = empty_fp8(rows, cols)
-        shape, ym = _matrix(out, "rms_norm", "out")
-        _same_device("rms_norm", x, weight, residual, residual_out, *out)
+            out = empty_fp8(rows, cols, x.device)
+        r, c, ym = _matrix(out, here, "rms_norm", "out")
     else:
         if out is None:
             out = torch.empty(x.shape, dtype=_BF16, device=x.device)
-        shape, yr = _rows(out, "rms_norm", "out")
-        _same_device("rms_norm", x, weight, residual, residual_out, out)
-    if shape != (rows, cols):
+        r, c, yr = _rows(out, here, "rms_norm", "out")
+    if r != rows or c != cols:
         _refuse("rms_norm", "out stands for %d x %d" % (rows, cols))
     if rows and cols:
-        binding.as_rms_norm(_NORM.pack(_NORM.size, cols, rows, *xr, *rr, *tr, *yr, *ym, wp, wd, eps), _stream(stream))
+        binding.as_rms_norm(_NORM.pack(_NORM.size, cols, rows, *xr, *rr, *tr, *yr, *ym, wp, wd, eps), _stream(stream, here))
     return out if residual is None else (out, residual_out)
 
 
 def quantize_fp8(x, block_rows=1, out=None, stream=None) -> BlockFp8:
     """x (bf16 or fp32, [rows, cols] or [B, H, N, d]) in 8-bit form; block_rows: rows that share a scale, 1 for activations and
-    128 for weights."""
-    (rows, cols), xr = _rows(x, "quantize_fp8", "x")
+    128 for weights.  Up to 16384 columns."""
+    here = _current_device()
+    rows, cols, xr = _rows(x, here, "quantize_fp8", "x")
     if out is None:
-        out = empty_fp8(rows, cols)
-    shape, om = _matrix(out, "quantize_fp8", "out")
-    if shape != (rows, cols):
+        out = empty_fp8(rows, cols, x.device)
+    r, c, om = _matrix(out, here, "quantize_fp8", "out")
+    if r != rows or c != cols:
         _refuse("quantize_fp8", "out is %d x %d" % (rows, cols))
-    _same_device("quantize_fp8", x, *out)
     if rows and cols:
-        binding.as_quantize_fp8(_QUANT.pack(_QUANT.size, cols, rows, *xr, *om, block_rows, 0), _stream(stream))
+        binding.as_quantize_fp8(_QUANT.pack(_QUANT.size, cols, rows, *xr, *om, block_rows, 0), _stream(stream, here))
     return out
 
 
@@ -167,14 +166,13 @@ _contexts = {}
 _lock = threading.Lock()
 
 
-def _context():
-    dev = torch._C._cuda_getDevice()
-    ctx = _contexts.get(dev)
+def _context(here):
+    ctx = _contexts.get(here)
     if ctx is None:
         with _lock:
-            ctx = _contexts.get(dev)
+            ctx = _contexts.get(here)
             if ctx is None:
-                ctx = _contexts[dev] = binding.as_fp8_create()
+                ctx = _contexts[here] = binding.as_fp8_create()
     return ctx
 
 
@@ -184,28 +182,25 @@ def matmul_fp8(a, w, bias=None, out=None, stream=None):
 
     The first call on a device sets the device's context up (it allocates 256 bytes and synchronises): make it outside of a
     stream capture."""
-    (m, k), am = _matrix(a, "matmul_fp8", "a")
-    (n, wk), wm = _matrix(w, "matmul_fp8", "w")
+    here = _current_device()
+    m, k, am = _matrix(a, here, "matmul_fp8", "a")
+    n, wk, wm = _matrix(w, here, "matmul_fp8", "w")
     if wk != k:
         _refuse("matmul_fp8", "a has %d columns, w %d" % (k, wk))
-    bp = 0
-    if bias is not None:
-        if bias.dtype != _BF16 or bias.shape != (n,) or (bias.stride(0) != 1 and n > 1):
-            _refuse("matmul_fp8", "bias is %d bf16 values next to each other" % n)
-        bp = bias.data_ptr()
+    bp = 0 if bias is None else _vector(bias, n, _BF16_ONLY, here, "matmul_fp8", "bias")
     if out is None:
-        out = torch.empty((m, n), dtype=_BF16, device=a[0].device)
-    shape, orow = _rows(out, "matmul_fp8", "out")
-    if shape != (m, n) or out.dtype != _BF16:
+        out = torch.empty_strided((m, n), (n, 1), dtype=_BF16, device=a[0].device)
+    r, c, orow = _rows(out, here, "matmul_fp8", "out")
+    if r != m or c != n or out.dtype != _BF16:
         _refuse("matmul_fp8", "out stands for %d x %d in bf16" % (m, n))
-    _same_device("matmul_fp8", a[0], a[1], w[0], w[1], bias, out)
     if m and n:
         if k == 0:
             _refuse("matmul_fp8", "there are no columns to sum over")
-        binding.as_matmul_fp8(_context(), _MATMUL.pack(_MATMUL.size, k, m, n, *am, *wm, bp, *orow), _stream(stream))
+        binding.as_matmul_fp8(_context(here), _MATMUL.pack(_MATMUL.size, k, m, n, *am, *wm, bp, *orow), _stream(stream, here))
     return out
 
 
 def fp8_last_status(stream=None) -> int:
     """AS_OK, or AS_ERR_DEVICE_TIMEOUT if a wait inside a product on this device ran out since the last call; synchronises."""
-    return binding.as_fp8_last_status(_context(), _stream(stream))
+    here = _current_device()
+    return binding.as_fp8_last_status(_context(here), _stream(stream, here))

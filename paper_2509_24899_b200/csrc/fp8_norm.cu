@@ -211,8 +211,6 @@ __global__ void __launch_bounds__(THREADS, goes_on<X, R, MOVE> ? 2 : 1) norm_ker
   const int c0 = first + (MOVE == MOVE_ELEMENT ? lane : (lane & (LANES - 1)) * 16);
   long long row = (long long)blockIdx.x * per + slot;
   const bool weighs = NORM && p.w != nullptr, early = weighs && !p.w_f32 && MOVE != MOVE_ELEMENT && !GOES_ON;
-  Rows weights{};
-  weights.data = const_cast<void*>(p.w);
   Raw<__nv_bfloat16, MOVE> w16[NV];                           // weights in bf16 come beside x: behind it they would cost a row their latency once more
   Raw<X, MOVE> x[NV];
   auto fetch_x = [&](long long at) {                          // of a row that is not there nothing is read or written
@@ -225,6 +223,8 @@ __global__ void __launch_bounds__(THREADS, goes_on<X, R, MOVE> ? 2 : 1) norm_ker
   // next to each other, so that a warp reads each piece without bank conflicts
   extern __shared__ uint4 kept[];
   griddep_wait();
+  Rows weights{};
+  weights.data = const_cast<void*>(p.w);
   fetch_x(row);
   if constexpr (GOES_ON) {
     if (weighs && !p.w_f32) {
@@ -307,17 +307,53 @@ __global__ void __launch_bounds__(THREADS, goes_on<X, R, MOVE> ? 2 : 1) norm_ker
   }
   float scale = 1.f;
   if constexpr (NORM) {
-    float sum = sum2.x + sum2.y;
+    // over the row's lanes and warps
+    auto row_sum = [&](float sum) {
 #pragma unroll
-    for (int o = LANES / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if constexpr (LANES == 32)
-      if (p.W > 1) {                                          // the same for every thread of the launch
-        if (lane == 0) part[warp] = sum;
-        __syncthreads();
-        sum = 0.f;
-        for (int i = 0; i < p.W; ++i) sum += part[min(slot * p.W + i, THREADS / 32 - 1)];
-      }
+      for (int o = LANES / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      if constexpr (LANES == 32)
+        if (p.W > 1) {                                        // the same for every thread of the launch
+          if (lane == 0) part[warp] = sum;
+          __syncthreads();
+          sum = 0.f;
+          for (int i = 0; i < p.W; ++i) sum += part[min(slot * p.W + i, THREADS / 32 - 1)];
+        }
+      return sum;
+    };
+    const float sum = row_sum(sum2.x + sum2.y);
     scale = rsqrtf(sum / (float)p.cols + p.eps);
+    // squares that fp32 does not hold (|t| from 2^64 / sqrt(cols) on): the row once more, as it was written, times 2^-64
+    const bool over = !(sum <= 3.402823466e38f);
+    bool again = __any_sync(0xffffffffu, over);
+    if constexpr (LANES == 32)
+      if (p.W > 1) again = __syncthreads_or(over);            // (behind it the sums have been read)
+    if (again) {
+      constexpr float DOWN = 5.421010862e-20f;                // 2^-64
+      float2 small = make_float2(0.f, 0.f);
+#pragma unroll 1
+      for (int j = 0; j < NV; ++j) {
+        float2 u[8];
+        if constexpr (__is_same(R, void)) { Raw<X, MOVE> t; fetch<X, MOVE>(p.x, p.x.row(r), c0 + j * 512, cols, t); values<X, MOVE>(t, u); }
+        else { Raw<R, MOVE> t; fetch<R, MOVE>(p.ro, p.ro.row(r), c0 + j * 512, cols, t); values<R, MOVE>(t, u); }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { u[i] = mul2(u[i], make_float2(DOWN, DOWN)); small = fma2(u[i], u[i], small); }
+      }
+      const float s = row_sum(small.x + small.y);
+      if constexpr (LANES == 32)
+        if (p.W > 1) __syncthreads();
+      if (over) {
+        scale = rsqrtf(s / (float)p.cols + p.eps * DOWN * DOWN);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[j][i] = mul2(v[j][i], make_float2(DOWN, DOWN));
+          if constexpr (FP8) {
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b) top[j][b] = __float_as_uint(__uint_as_float(top[j][b]) * DOWN);
+          }
+        }
+      }
+    }
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
@@ -370,8 +406,6 @@ __global__ void __launch_bounds__(THREADS, goes_on<X, R, MOVE> ? 2 : 1) norm_ker
     }
   }
   if constexpr (!GOES_ON) return;
-  if constexpr (NORM && LANES == 32)
-    if (p.W > 1) __syncthreads();                             // the sums have been read
   }
 }
 
