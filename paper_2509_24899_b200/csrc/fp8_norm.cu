@@ -181,6 +181,9 @@ AS_DEV uint32_t block_max(const float2 (&f)[8]) {
 // Element by element: of block b of the warp's four, for all lanes.
 AS_DEV uint32_t block_max_elements(const float2 (&f)[8], int b) { return __reduce_max_sync(0xffffffffu, __float_as_uint(max_abs2(f[2 * b], max_abs2(f[2 * b + 1], 0.f)))); }
 
+constexpr float DOWN = 5.421010862e-20f;       // 2^-64
+constexpr float MOST = 3.402823466e38f;
+
 // NORM: y = t * rsqrt(mean t^2 + eps) * w, else y = x.  R: the residual's type (void: none).  FP8: y in 8-bit form, else in bf16.  LANES: of a row
 // in a warp (8, 16: with one vector).
 //
@@ -261,11 +264,23 @@ __global__ void __launch_bounds__(THREADS, goes_on<X, R, MOVE> ? 2 : 1) norm_ker
     if constexpr (GOES_ON) fetch_x(row + (long long)gridDim.x * per);
   }
   float2 sum2 = make_float2(0.f, 0.f);
+  float small = 0.f;
   if constexpr (NORM) {
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum2 = fma2(v[j][i], v[j][i], sum2);
+    // 2^-128 of it, for rows whose squares fp32 does not hold (|t| from 2^64 / sqrt(cols) on)
+    if (!(sum2.x + sum2.y <= MOST)) {
+      float2 s = make_float2(0.f, 0.f);
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { const float2 u = mul2(v[j][i], make_float2(DOWN, DOWN)); s = fma2(u, u, s); }
+      small = s.x + s.y;
+    } else {
+      small = (sum2.x + sum2.y) * DOWN * DOWN;
+    }
     if (early) {
 #pragma unroll
       for (int j = 0; j < NV; ++j) scale_values<__nv_bfloat16, MOVE>(w16[j], v[j]);
@@ -322,23 +337,12 @@ __global__ void __launch_bounds__(THREADS, goes_on<X, R, MOVE> ? 2 : 1) norm_ker
     };
     const float sum = row_sum(sum2.x + sum2.y);
     scale = rsqrtf(sum / (float)p.cols + p.eps);
-    // squares that fp32 does not hold (|t| from 2^64 / sqrt(cols) on): the row once more, as it was written, times 2^-64
-    const bool over = !(sum <= 3.402823466e38f);
+    const bool over = !(sum <= MOST);
     bool again = __any_sync(0xffffffffu, over);
     if constexpr (LANES == 32)
       if (p.W > 1) again = __syncthreads_or(over);            // (behind it the sums have been read)
     if (again) {
-      constexpr float DOWN = 5.421010862e-20f;                // 2^-64
-      float2 small = make_float2(0.f, 0.f);
-#pragma unroll 1
-      for (int j = 0; j < NV; ++j) {
-        float2 u[8];
-        if constexpr (__is_same(R, void)) { Raw<X, MOVE> t; fetch<X, MOVE>(p.x, p.x.row(r), c0 + j * 512, cols, t); values<X, MOVE>(t, u); }
-        else { Raw<R, MOVE> t; fetch<R, MOVE>(p.ro, p.ro.row(r), c0 + j * 512, cols, t); values<R, MOVE>(t, u); }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) { u[i] = mul2(u[i], make_float2(DOWN, DOWN)); small = fma2(u[i], u[i], small); }
-      }
-      const float s = row_sum(small.x + small.y);
+      const float s = row_sum(small);
       if constexpr (LANES == 32)
         if (p.W > 1) __syncthreads();
       if (over) {
