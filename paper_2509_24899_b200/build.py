@@ -1,4 +1,5 @@
-"""Builds libas_hybrid_attn.so in-tree with nvcc for sm_100a (cross-compiles without a GPU)."""
+"""Builds libas_hybrid_attn.so in-tree with nvcc for sm_100a (cross-compiles without a GPU), and beside it as_torch_calls.so, the module of the calls that take
+PyTorch tensors (csrc/torch_calls.cpp), with g++."""
 from __future__ import annotations
 
 import os
@@ -9,6 +10,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "lib", "libas_hybrid_attn.so")
+TORCH_CALLS = os.path.join(PKG, "lib", "as_torch_calls.so")
 SOURCES = ["as_hybrid_attn.cu", "simt_path.cu", "tensor_init.cu", "tensor_qpass.cu", "tensor_qstream.cu", "tensor_kpass.cu", "backward_simt.cu", "backward_tensor.cu", "backward_tensor_d64.cu", "no_alloc.cu",
            "block_rates.cu", "fp8_norm.cu", "fp8_matmul.cu"]
 
@@ -17,19 +19,50 @@ def _sources():
     return [os.path.join(CSRC, s) for s in SOURCES if os.path.exists(os.path.join(CSRC, s))]
 
 
+def _older(target: str, deps) -> bool:
+    return not os.path.exists(target) or any(os.path.getmtime(d) > os.path.getmtime(target) for d in deps)
+
+
+def _headers():
+    inc = os.path.join(ROOT, "include")
+    return [os.path.join(inc, f) for f in os.listdir(inc) if f.endswith(".h")]
+
+
 def _stale() -> bool:
-    if not os.path.exists(LIB):
-        return True
-    t = os.path.getmtime(LIB)
-    deps = _sources() + [os.path.join(CSRC, "as_internal.h"), os.path.join(ROOT, "include", "as_hybrid_attn.h")]
+    deps = _sources() + _headers()
     deps += [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".h", ".cuh"))]
-    return any(os.path.getmtime(d) > t for d in deps)
+    return _older(LIB, deps)
+
+
+def build_torch_calls(force: bool = False) -> str:
+    """Compiles the module of the calls that take PyTorch tensors when it is missing or older than its source; returns its path."""
+    source = os.path.join(CSRC, "torch_calls.cpp")
+    if not force and not _older(TORCH_CALLS, [source] + _headers()):
+        return TORCH_CALLS
+    import sysconfig
+
+    import torch
+    libs, inc = (os.path.join(os.path.dirname(torch.__file__), d) for d in ("lib", "include"))
+    cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+           "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_paths()["include"], "-I", os.path.join(cuda, "include")]
+    cmd += ["-isystem", inc, "-isystem", os.path.join(inc, "torch", "csrc", "api", "include"), source, "-o", TORCH_CALLS, "-L", os.path.dirname(LIB), "-l:" + os.path.basename(LIB), "-Wl,-rpath,$ORIGIN",
+            "-L", libs, "-ltorch_python", "-ltorch_cuda", "-ltorch_cpu", "-ltorch", "-lc10_cuda", "-lc10"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError("%s failed:\n%s%s" % (cmd[0], res.stdout, res.stderr))
+    return TORCH_CALLS
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compiles the library when it is missing or older than its sources; returns its path."""
-    if not force and not _stale():
-        return LIB
+    """Compiles the library, and the module beside it, where they are missing or older than their sources; returns the library's path."""
+    if force or _stale():
+        _build_library(verbose)
+    build_torch_calls(force)
+    return LIB
+
+
+def _build_library(verbose: bool) -> None:
     os.makedirs(os.path.dirname(LIB), exist_ok=True)
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "--threads", "4",
@@ -43,7 +76,6 @@ def build(force: bool = False, verbose: bool = False) -> str:
         sys.stderr.write(res.stdout + res.stderr)
     if res.returncode != 0:
         raise RuntimeError("nvcc failed:\n" + res.stdout + res.stderr)
-    return LIB
 
 
 if __name__ == "__main__":
