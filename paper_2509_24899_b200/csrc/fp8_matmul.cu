@@ -516,19 +516,22 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 1) few_rows_kernel(const __gri
   }
 }
 
-// The shape of a tile: CTAs that share it and rows of w, by the time that its turns take on all SMs: turns x blocks of 128 columns x ns a block, and what the reading out of
-// the last turn's results and the meeting of a pair add.  (Measured, ns a block with all SMs busy, 7800 x 4608 x 1536; a single CTA's tile is shorter for
-// few rows and takes no meeting, a pair's is faster from 128 rows of w on.)
+// The shape of a tile - CTAs that share it, rows of w - by the time that its turns take on all SMs: turns x blocks of 128 columns x ns a block, and what the reading out
+// of the last turn's results and the meeting of a pair add.  ns: measured with all SMs busy, at 7800 x 4608 x 1536 and what the largest products make of it: up to 128 rows of w the copies
+// of a bound a block, 64 bytes a clock into an SM (a pair halves those of w), above them the MMAs, and power: at 32760 x 4608 x 1536, back to back, 192 and 224 rows take
+// 212 and 209 us at 1.45 GHz.  The last turn counts half of what it leaves idle, as the clock rises meanwhile; a single turn counts whole.
+// Few rows go to single CTAs and narrow tiles: 512 x 1536 x 1536 takes 6.1 us with {1, 64}, 7.2 with {2, 192}.
 struct Tile { int cg, bn; };
 Tile tile_of(int M, int N, int kb, int sms) {
-  static const int ns[2][7] = {{230, 250, 265, 300, 345, 385, 440}, {228, 230, 240, 262, 297, 320, 380}};
+  static const int ns[2][7] = {{230, 250, 265, 300, 345, 385, 440}, {228, 230, 240, 262, 297, 320, 365}};
   Tile best{1, 32};
   double least = 1e300;
   for (int cg = 1; cg <= 2; ++cg)
     for (int i = 0; i < 7; ++i) {
       const int bn = 32 * (i + 1);
-      const long long tiles = ((long long)M + BM * cg - 1) / (BM * cg) * ((N + bn - 1) / bn), turns = (tiles + sms / cg - 1) / (sms / cg);
-      const double t = (double)turns * kb * ns[cg - 1][i] + 7. * bn + (cg == 2 ? 400. : 0.);
+      const long long tiles = ((long long)M + BM * cg - 1) / (BM * cg) * ((N + bn - 1) / bn), units = sms / cg, whole = (tiles + units - 1) / units;
+      const double turns = whole == 1 ? 1. : 0.5 * ((double)tiles / units + whole);
+      const double t = turns * kb * ns[cg - 1][i] + 7. * bn + (cg == 2 ? 400. : 0.);
       if (t < least) { least = t; best = {cg, bn}; }
     }
   return best;
