@@ -16,6 +16,7 @@
 #include <new>
 
 #include "fp8_common.cuh"
+#include "fp8_maps.h"
 #include "tensor_common.cuh"
 
 namespace {

@@ -5,7 +5,6 @@
 
 #include <cuda.h>
 
-#include "as_fp8.h"
 #include "as_internal.h"
 #include "sm100_ptx.cuh"
 #include "sm100_tmem_wide.cuh"
@@ -67,12 +66,6 @@ AS_DEV void store_row_chunk(uint8_t* tile, uint32_t row, uint32_t c0, const uint
 // 3-D bf16 tensor [slices][rows][cols] (cols contiguous) viewed through boxes of 64 cols x box_rows rows
 // with the 128-byte swizzle.  False when the driver entry point is missing or rejects the arguments.
 bool make_map(CUtensorMap* m, const void* base, int cols, int rows, int slices, int box_rows);
-// 2-D tensor of bytes [rows][pitch], `cols` of them a row, viewed through boxes of 128 bytes x box_rows rows with the 128-byte
-// swizzle; what lies outside reads as 0.
-bool make_map_bytes(CUtensorMap* m, const void* base, long long cols, long long rows, long long pitch, int box_rows);
-// A bf16 matrix [rows, cols] in rows or heads (as_rows_t) as a 4-D tensor: column of a head, token, head, batch entry; boxes of 32 columns x box_rows tokens
-// with the 64-byte swizzle.
-bool make_map_rows(CUtensorMap* m, const as_rows_t& x, long long rows, long long cols, int box_rows);
 
 template <typename K>
 cudaError_t opt_in_smem(K kernel, int bytes) {

@@ -3,6 +3,7 @@
 #include <mutex>
 
 #include "backward_common.h"
+#include "fp8_maps.h"
 #include "tensor_common.cuh"
 
 namespace {
