@@ -190,7 +190,8 @@ constexpr float MOST = 3.402823466e38f;
 // The weights multiply t while the sum of squares is on its way between the lanes, and so do the blocks' largest values go round: both turns of a row's reductions
 // overlap, and the row's scale enters last.  What counts is the number of instructions: with 8 columns a lane, one value an instruction and the formula's order a row of 1536
 // columns with a residual in bf16 took 131 us for 32760 rows; in pairs, weights ahead of the scale, 62 us; with 16 columns a lane, whose loads are half as many and whose
-// scales are a third as much work, 55 us (6.4 TB/s).  Without a residual 54, 38 and 28 us (5.4 TB/s), the last with CTAs that go on; the 8-bit form alone 34, 26 and 25 us.
+// scales are a third as much work, 56 us (6.3 TB/s).  Without a residual 54, 38 and 30 us (5.0 TB/s), the last with CTAs that go on; the 8-bit form alone 34, 26 and 25 us
+// (6.1 TB/s).  Rows further ahead, as asynchronous copies into shared memory, did not help there: 35 and 27 us with four rows under way, for the instructions that it takes.
 // With x in bf16 and no residual a CTA goes on from row to row: its weights stay in shared memory, and a row's loads are under way while the one before it is
 // worked on.  (With a residual or in fp32 there is enough under way without that, and no room for it.)  Two CTAs an SM.
 template <typename X, typename R, int MOVE> constexpr bool goes_on = sizeof(X) == 2 && __is_same(R, void) && MOVE != MOVE_ELEMENT;
@@ -270,7 +271,7 @@ __global__ void __launch_bounds__(THREADS, goes_on<X, R, MOVE> ? 2 : 1) norm_ker
     for (int j = 0; j < NV; ++j)
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum2 = fma2(v[j][i], v[j][i], sum2);
-    // 2^-128 of it, for rows whose squares fp32 does not hold (|t| from 2^64 / sqrt(cols) on)
+    // 2^-128 of it, for rows whose squares fp32 does not hold (|t| from 2^64 / sqrt(cols) on).  That there are such rows costs the others up to 2 us of 30.
     if (!(sum2.x + sum2.y <= MOST)) {
       float2 s = make_float2(0.f, 0.f);
 #pragma unroll
@@ -288,7 +289,7 @@ __global__ void __launch_bounds__(THREADS, goes_on<X, R, MOVE> ? 2 : 1) norm_ker
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
         if ((MOVE == MOVE_ELEMENT || GOES_ON) && !p.w_f32) {
-          Raw<__nv_bfloat16, MOVE> w;
+          Raw<__nv_bfloat16, MOVE> w{};
           if constexpr (GOES_ON) {
             if ((first / 512 + j) * 512 < p.cols) {
               const uint4* at = kept + (first / 512 + j) * 64 + (lane & (LANES - 1));
@@ -338,25 +339,15 @@ __global__ void __launch_bounds__(THREADS, goes_on<X, R, MOVE> ? 2 : 1) norm_ker
     const float sum = row_sum(sum2.x + sum2.y);
     scale = rsqrtf(sum / (float)p.cols + p.eps);
     const bool over = !(sum <= MOST);
-    bool again = __any_sync(0xffffffffu, over);
+    bool again = over;                                        // (the sum of all lanes of a row is one value)
+    if constexpr (LANES < 32) again = __any_sync(0xffffffffu, over);
     if constexpr (LANES == 32)
       if (p.W > 1) again = __syncthreads_or(over);            // (behind it the sums have been read)
     if (again) {
       const float s = row_sum(small);
       if constexpr (LANES == 32)
         if (p.W > 1) __syncthreads();
-      if (over) {
-        scale = rsqrtf(s / (float)p.cols + p.eps * DOWN * DOWN);
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) v[j][i] = mul2(v[j][i], make_float2(DOWN, DOWN));
-          if constexpr (FP8) {
-#pragma unroll
-            for (int b = 0; b < BLOCKS; ++b) top[j][b] = __float_as_uint(__uint_as_float(top[j][b]) * DOWN);
-          }
-        }
-      }
+      if (over) scale = rsqrtf(s / (float)p.cols + p.eps * DOWN * DOWN) * DOWN;
     }
 #pragma unroll
     for (int j = 0; j < NV; ++j)

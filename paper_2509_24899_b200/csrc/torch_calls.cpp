@@ -101,12 +101,19 @@ PyObject* empty(at::IntArrayRef size, at::IntArrayRef stride, at::ScalarType typ
 PyObject* empty_contiguous(at::IntArrayRef size, at::ScalarType type, int here) {
   return THPVariable_Wrap(at::Tensor(at::detail::empty_cuda(size, type, at::Device(at::kCUDA, (c10::DeviceIndex)here), std::nullopt)));
 }
-// A BlockFp8 of new tensors.
+// A BlockFp8 of new tensors, which share one allocation (two take 0.3 us more).
 PyObject* empty_pair(int64_t rows, int64_t cols, int here) {
+  const int64_t pitch = (cols + 15) / 16 * 16, groups = (cols + 511) / 512, values = (rows * pitch + 255) / 256 * 256;
+  const at::Tensor whole(at::detail::empty_cuda({values + 4 * groups * rows}, at::kByte, at::Device(at::kCUDA, (c10::DeviceIndex)here), std::nullopt));
+  auto part = [&](at::ScalarType type, at::IntArrayRef size, at::IntArrayRef stride, int64_t from) {
+    at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::TensorImpl::VIEW, c10::Storage(whole.storage()), whole.key_set(), c10::scalarTypeToTypeMeta(type));
+    t.unsafeGetTensorImpl()->set_sizes_and_strides(size, stride, from);
+    return THPVariable_Wrap(std::move(t));
+  };
   PyObject* two = PyTuple_New(2);
   if (two == nullptr) return nullptr;
-  PyTuple_SET_ITEM(two, 0, empty({rows, cols}, {(cols + 15) / 16 * 16, 1}, at::kFloat8_e4m3fn, here));
-  PyTuple_SET_ITEM(two, 1, empty({(cols + 511) / 512, rows, 4}, {4 * rows, 4, 1}, at::kByte, here));
+  PyTuple_SET_ITEM(two, 0, part(at::kFloat8_e4m3fn, {rows, cols}, {pitch, 1}, 0));
+  PyTuple_SET_ITEM(two, 1, part(at::kByte, {groups, rows, 4}, {4 * rows, 4, 1}, values));
   PyObject* args = PyTuple_Pack(1, two);
   Py_DECREF(two);
   if (args == nullptr) return nullptr;
