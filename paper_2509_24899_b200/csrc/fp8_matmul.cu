@@ -404,26 +404,28 @@ matmul_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CU
 }
 
 // ---------------------------------------------------------------- few rows
-// Up to 8 rows of a, where a tile of the pair would be empty but for some and few CTAs would walk all columns: here w is read once, by all SMs, into the operands
-// of the warps' own matrix instructions (16 rows of w, 8 of a, 32 columns).  A CTA takes units of 16 rows of w; its warps take every sixteenth block of 128 columns each, with one
-// scale for a row and block: four instructions into fresh sums, which are scaled and added up in fp32.  Which columns an instruction calls its k-th does not matter as
-// long as both operands agree: a lane holds columns 16 q .. 16 q + 15 of each half of its rows' block, so that four lanes copy 64 bytes in a run.  The warps' sums meet in shared memory, in the order of the warps.
+// Few rows of a, where a tile of the pair would be empty but for some and few CTAs would walk all columns: here w is read by all SMs, into the operands of the warps' own matrix
+// instructions (16 rows of w, 8 of a, 32 columns).  A CTA takes units of 16 rows of w by 8 or 16 of a; its warps take every sixteenth block of 128 columns each, with one scale for a
+// row and block: four instructions into fresh sums, which are scaled and added up in fp32.  Which columns an instruction calls its k-th does not matter as long as both
+// operands agree: a lane holds columns 16 q .. 16 q + 15 of each half of its rows' block, so that four lanes copy 64 bytes in a run.  The warps' sums meet in shared
+// memory, in the order of the warps.
 //
-// What bounds it is the latency of memory, and then the number of copies: a lane's operands come by asynchronous copies into slots that its warp alone reads, FEW_AHEAD blocks ahead and
+// What bounds it is the latency of memory, and then the number of copies: a warp's operands come by asynchronous copies into slots that it alone reads, two or three blocks ahead and
 // on into the next unit, one copy for all scales of a block.  (2 rows by w of 1536 x 1536, 9216 x 1536, 1536 x 6144, 6144 x 6144: straight into registers 2.7, 5.5, 5.7, 13.2 us;
-// two CTAs of 8 warps 2.6, 4.5, 6.4, 12.7; one of 16 warps 2.0, 5.0, 4.0, 10.5 us (3.6 TB/s).)
-constexpr int FEW_ROWS = 8;
+// two CTAs of 8 warps an SM 2.6, 4.5, 6.4, 12.7; one of 16 warps 2.1, 5.1, 4.1, 10.7 us (3.5 TB/s).)
 constexpr int FEW_WARPS = 16, FEW_COLS = 16;
-constexpr int FEW_AHEAD = 3;                // blocks of a warp under way; one CTA an SM
-constexpr int FEW_SLOT = 6 * 512 + 128;     // bytes of a warp's block: per lane 64 of w and 32 of a, the scale words of 16 rows of w and 8 of a
-constexpr int FEW_SMEM = FEW_WARPS * FEW_AHEAD * FEW_SLOT;
+// With NT tiles of 8 rows of a: blocks of a warp under way (one CTA an SM), bytes of one: per lane 64 of w and 32 NT of a, the scale words of 16 rows of w and 8 NT of a
+__host__ __device__ constexpr int few_ahead(int nt) { return nt == 1 ? 3 : 2; }
+__host__ __device__ constexpr int few_slot(int nt) { return (4 + 2 * nt) * 512 + 64 + 32 * nt + (nt == 1 ? 32 : 0); }
+constexpr int few_smem(int nt) { return FEW_WARPS * few_ahead(nt) * few_slot(nt); }
+static_assert(few_slot(1) % 128 == 0 && few_slot(2) % 128 == 0, "");
 
 struct FewParams {
   const uint8_t *a, *w, *sa, *sw;
   const __nv_bfloat16* bias;
   Rows out;
   long long a_pitch, w_pitch, sa_rows, sw_rows;
-  int M, N, K, units;
+  int M, N, K, units, mt;                   // mt: units of a tile of w, one for each 8 NT rows of a
 };
 
 // 16 bytes, of which `bytes` come from memory and the rest are 0: of w past the first-level cache, of a, which every CTA reads, through it (past it they all
@@ -437,79 +439,96 @@ AS_DEV void few_read(uint32_t at, uint32_t (&r)[4]) {
 // 2^(e - 127) of a scale byte: exact for 0 (a subnormal number), NaN for 255.
 AS_DEV float few_scale(uint32_t e) { return __uint_as_float(e == 0u ? 0x00400000u : e == 255u ? 0x7fc00000u : e << 23); }
 
+template <int NT>
 __global__ void __launch_bounds__(FEW_WARPS * 32, 1) few_rows_kernel(const __grid_constant__ FewParams p) {
+  constexpr int AHEAD = few_ahead(NT), SLOT = few_slot(NT), SCALES = (4 + 2 * NT) * 512;
   griddep_launch();
   extern __shared__ __align__(16) uint8_t slots[];
-  __shared__ float sums[2][FEW_WARPS][FEW_ROWS][FEW_COLS + 1];
+  __shared__ float sums[2][FEW_WARPS][8 * NT][FEW_COLS + 1];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane / 4, q = lane % 4;
   const int kb = (p.K + BK - 1) / BK;
-  const uint32_t mine = smem_u32(slots) + (uint32_t)warp * (FEW_AHEAD * FEW_SLOT) + lane * 16;
+  const uint32_t mine = smem_u32(slots) + (uint32_t)warp * (AHEAD * SLOT);
   griddep_wait();
-  const uint8_t* ar = p.a + (long long)min(g, p.M - 1) * p.a_pitch;   // rows that are not there are read as the last one, and their results not written
-  int unit = blockIdx.x, block = warp, slot = 0;                      // what is asked for next
+  int unit = blockIdx.x, block = warp, slot = 0;                      // what is asked for next, and its first rows of w and a
+  int n1 = (NT == 1 ? unit : unit / p.mt) * FEW_COLS, m1 = NT == 1 ? 0 : unit % p.mt * (8 * NT);
   auto ask = [&] {
     if (block < kb && unit < p.units) {
-      const uint32_t at = mine + slot * FEW_SLOT;
-      const int c = block * BK + q * 16, n = unit * FEW_COLS + g;
+      const uint32_t at = mine + slot * SLOT, own = at + lane * 16;
+      const int c = block * BK + q * 16, n = n1 + g, m0 = m1;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int bytes = max(0, min(16, p.K - c - 64 * i)), c1 = bytes > 0 ? c + 64 * i : 0;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) few_copy_w(at + (2 * h + i) * 512, p.w + (long long)min(n + 8 * h, p.N - 1) * p.w_pitch + c1, bytes);
-        if (g < p.M) few_copy_a(at + (4 + i) * 512, ar + c1, bytes);  // (a row that is not there leaves its results, which are not written, to chance)
+        for (int h = 0; h < 2; ++h) few_copy_w(own + (2 * h + i) * 512, p.w + (long long)min(n + 8 * h, p.N - 1) * p.w_pitch + c1, bytes);
+#pragma unroll
+        for (int t = 0; t < NT; ++t)        // (a row that is not there leaves its results, which are not written, to chance)
+          if (m0 + 8 * t + g < p.M) few_copy_a(own + (4 + 2 * t + i) * 512, p.a + (long long)(m0 + 8 * t + g) * p.a_pitch + c1, bytes);
       }
-      const uint8_t* scale = q < 2 ? p.sw + ((long long)(block / 4) * p.sw_rows + min(n + 8 * q, p.N - 1)) * 4 : p.sa + ((long long)(block / 4) * p.sa_rows + min(g, p.M - 1)) * 4;
-      if (q < 3) few_copy4(at - lane * 16 + 6 * 512 + (8 * q + g) * 4, scale);
-      if (++slot == FEW_AHEAD) slot = 0;
-      if ((block += FEW_WARPS) >= kb) { block = warp; unit += gridDim.x; }
+      const uint8_t* scale = q < 2 ? p.sw + ((long long)(block / 4) * p.sw_rows + min(n + 8 * q, p.N - 1)) * 4
+                                   : p.sa + ((long long)(block / 4) * p.sa_rows + min(m0 + 8 * (q - 2) + g, p.M - 1)) * 4;
+      if (q < 2 + NT) few_copy4(at + SCALES + (8 * q + g) * 4, scale);
+      if (++slot == AHEAD) slot = 0;
+      if ((block += FEW_WARPS) >= kb) {
+        block = warp;
+        unit += gridDim.x;
+        n1 = (NT == 1 ? unit : unit / p.mt) * FEW_COLS;
+        m1 = NT == 1 ? 0 : unit % p.mt * (8 * NT);
+      }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");              // (an empty group where there is nothing left: the waits below count groups)
   };
 #pragma unroll
-  for (int i = 0; i < FEW_AHEAD - 1; ++i) ask();
+  for (int i = 0; i < AHEAD - 1; ++i) ask();
   int take = 0, turn = 0;
   for (int u = blockIdx.x; u < p.units; u += gridDim.x, turn ^= 1) {
-    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+    float acc[NT][4] = {};
     for (int k = warp; k < kb; k += FEW_WARPS) {
       __syncwarp();                                                   // every lane has read the slot that is filled next
       ask();
-      asm volatile("cp.async.wait_group %0;" ::"n"(FEW_AHEAD - 1) : "memory");
+      asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD - 1) : "memory");
       __syncwarp();                                                   // the other lanes' scales have come as well
-      const uint32_t at = mine + take * FEW_SLOT;
-      if (++take == FEW_AHEAD) take = 0;
-      uint32_t w[2][2][4], a[2][4];
+      const uint32_t at = mine + take * SLOT, own = at + lane * 16;
+      if (++take == AHEAD) take = 0;
+      auto scale_of = [&](int i) {
+        uint32_t e;
+        asm volatile("ld.shared.u8 %0, [%1];" : "=r"(e) : "r"(at + SCALES + i * 4 + k % 4) : "memory");
+        return few_scale(e);
+      };
+      uint32_t w[2][2][4];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        few_read(at + i * 512, w[0][i]);
-        few_read(at + (2 + i) * 512, w[1][i]);
-        few_read(at + (4 + i) * 512, a[i]);
+        few_read(own + i * 512, w[0][i]);
+        few_read(own + (2 + i) * 512, w[1][i]);
       }
-      float d[4] = {0.f, 0.f, 0.f, 0.f};
+      const float f0 = scale_of(g), f1 = scale_of(8 + g);             // rows g and g + 8 of w; of a: rows 2 q and 2 q + 1 of each tile
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                     : "r"(w[0][i / 2][2 * (i % 2)]), "r"(w[1][i / 2][2 * (i % 2)]), "r"(w[0][i / 2][2 * (i % 2) + 1]), "r"(w[1][i / 2][2 * (i % 2) + 1]), "r"(a[i / 2][2 * (i % 2)]),
-                       "r"(a[i / 2][2 * (i % 2) + 1]));
-      float f[4];
+      for (int t = 0; t < NT; ++t) {
+        uint32_t a[2][4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {                                   // rows g and g + 8 of w, rows 2 q and 2 q + 1 of a
-        uint32_t e;
-        asm volatile("ld.shared.u8 %0, [%1];" : "=r"(e) : "r"(at - lane * 16 + 6 * 512 + (j < 2 ? 8 * j + g : 16 + 2 * q + j - 2) * 4 + k % 4) : "memory");
-        f[j] = few_scale(e);
+        for (int i = 0; i < 2; ++i) few_read(own + (4 + 2 * t + i) * 512, a[i]);
+        const float fa[2] = {scale_of(16 + 8 * t + 2 * q), scale_of(17 + 8 * t + 2 * q)};
+        float d[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                       : "r"(w[0][i / 2][2 * (i % 2)]), "r"(w[1][i / 2][2 * (i % 2)]), "r"(w[0][i / 2][2 * (i % 2) + 1]), "r"(w[1][i / 2][2 * (i % 2) + 1]),
+                         "r"(a[i / 2][2 * (i % 2)]), "r"(a[i / 2][2 * (i % 2) + 1]));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[t][j] = fmaf(d[j] * (j < 2 ? f0 : f1), fa[j % 2], acc[t][j]);
       }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) acc[j] = fmaf(d[j] * f[j / 2], f[2 + j % 2], acc[j]);
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) sums[turn][warp][2 * q + j % 2][g + 8 * (j / 2)] = acc[j];
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sums[turn][warp][8 * t + 2 * q + j % 2][g + 8 * (j / 2)] = acc[t][j];
     __syncthreads();                                                  // (one for a unit: the next one's sums go to the other half)
-    if (threadIdx.x < FEW_ROWS * FEW_COLS) {
-      const int m = threadIdx.x / FEW_COLS, j = threadIdx.x % FEW_COLS, n = u * FEW_COLS + j;
+    if (threadIdx.x < 8 * NT * FEW_COLS) {
+      const int i0 = threadIdx.x / FEW_COLS, j = threadIdx.x % FEW_COLS, n = (NT == 1 ? u : u / p.mt) * FEW_COLS + j, m = (NT == 1 ? 0 : u % p.mt * (8 * NT)) + i0;
       if (m < p.M && n < p.N) {
         float f = 0.f;
 #pragma unroll
-        for (int i = 0; i < FEW_WARPS; ++i) f += sums[turn][i][m][j];
+        for (int i = 0; i < FEW_WARPS; ++i) f += sums[turn][i][i0][j];
         if (p.bias != nullptr) f += __bfloat162float(p.bias[n]);
         static_cast<__nv_bfloat16*>(p.out.data)[p.out.row((unsigned)m) + p.out.col((unsigned)n)] = __float2bfloat16_rn(f);
       }
@@ -522,20 +541,29 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 1) few_rows_kernel(const __gri
 // of a bound a block, 64 bytes a clock into an SM (a pair halves those of w), above them the MMAs, and power: at 32760 x 4608 x 1536, back to back, 192 and 224 rows take
 // 212 and 209 us at 1.45 GHz.  The last turn counts half of what it leaves idle, as the clock rises meanwhile; a single turn counts whole.
 // Few rows go to single CTAs and narrow tiles: 512 x 1536 x 1536 takes 6.1 us with {1, 64}, 7.2 with {2, 192}.
-struct Tile { int cg, bn; };
+struct Tile { int cg, bn; double ns; };
 Tile tile_of(int M, int N, int kb, int sms) {
   static const int ns[2][7] = {{230, 250, 265, 300, 345, 385, 440}, {228, 230, 240, 262, 297, 320, 365}};
-  Tile best{1, 32};
-  double least = 1e300;
+  Tile best{1, 32, 1e300};
   for (int cg = 1; cg <= 2; ++cg)
     for (int i = 0; i < 7; ++i) {
       const int bn = 32 * (i + 1);
       const long long tiles = ((long long)M + BM * cg - 1) / (BM * cg) * ((N + bn - 1) / bn), units = sms / cg, whole = (tiles + units - 1) / units;
       const double turns = whole == 1 ? 1. : 0.5 * ((double)tiles / units + whole);
       const double t = turns * kb * ns[cg - 1][i] + 7. * bn + (cg == 2 ? 400. : 0.);
-      if (t < least) { least = t; best = {cg, bn}; }
+      if (t < best.ns) best = {cg, bn, t};
     }
   return best;
+}
+
+// Whether a product goes to few_rows_kernel: up to 16 rows of a, and up to 256 where its turns - units of 16 rows of a and of w, sixteen blocks of 128 columns at a time - take
+// less than the tile's: 1.5 us each, the first one 0.7, from 0.5 us less of setting up.  (us by the one and the other: 16 rows by 1536 x 1536 2.6 and 5.3, by 6144 x 6144 14.3 and 22;
+// 32 rows by 1536 x 1536 4.3 and 5.3, by 9216 x 1536 13.8 and 7.5; 64 rows by 512 x 1280 2.7 and 4.8, by 1536 x 1536 6.0 and 5.3; 256 rows by 128 x 2392 3.8 and 6.9.)
+bool few_rows(int M, int N, int kb, int sms, const Tile& tile) {
+  if (M <= 16) return true;
+  if (M > 256) return false;
+  const long long units = (long long)((N + FEW_COLS - 1) / FEW_COLS) * ((M + 15) / 16), turns = (units + sms - 1) / sms * ((kb + FEW_WARPS - 1) / FEW_WARPS);
+  return 700. + 1500. * (double)(turns - 1) < tile.ns + 500.;
 }
 
 template <int CG>
@@ -566,7 +594,7 @@ extern "C" as_status_t as_fp8_create(as_fp8_context_t* out) {
     return AS_ERR_CUDA;
   if (major != 10) return AS_ERR_ARCH;
   if (as_tensor_init() != cudaSuccess || as_tc::opt_in_smem(matmul_kernel<1>, SMEM_MAX) != cudaSuccess || as_tc::opt_in_smem(matmul_kernel<2>, SMEM_MAX) != cudaSuccess ||
-      as_tc::opt_in_smem(few_rows_kernel, FEW_SMEM) != cudaSuccess)
+      as_tc::opt_in_smem(few_rows_kernel<1>, few_smem(1)) != cudaSuccess || as_tc::opt_in_smem(few_rows_kernel<2>, few_smem(2)) != cudaSuccess)
     return AS_ERR_CUDA;
   as_fp8_context_s* h = new (std::nothrow) as_fp8_context_s;
   if (h == nullptr) return AS_ERR_ALLOC;
@@ -607,7 +635,9 @@ extern "C" as_status_t as_matmul_fp8(as_fp8_context_t h, const as_matmul_fp8_t* 
   if (out.split && a->out_cols * (long long)a->out.head_dim > (1ll << 32)) return AS_ERR_UNSUPPORTED;
   if (a->rows == 0) return AS_OK;
   const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  if (a->rows <= FEW_ROWS) {
+  const int kb = (a->cols + BK - 1) / BK;
+  const Tile tile = tile_of((int)a->rows, (int)a->out_cols, kb, h->sms);
+  if (few_rows((int)a->rows, (int)a->out_cols, kb, h->sms, tile)) {
     FewParams p{};
     p.a = static_cast<const uint8_t*>(a->a.data); p.a_pitch = a->a.pitch;
     p.w = static_cast<const uint8_t*>(a->w.data); p.w_pitch = a->w.pitch;
@@ -616,19 +646,20 @@ extern "C" as_status_t as_matmul_fp8(as_fp8_context_t h, const as_matmul_fp8_t* 
     p.bias = static_cast<const __nv_bfloat16*>(a->bias);
     p.out = out;
     p.M = (int)a->rows; p.N = (int)a->out_cols; p.K = a->cols;
-    p.units = (p.N + FEW_COLS - 1) / FEW_COLS;
-    const cudaError_t e = as_launch_dependent(few_rows_kernel, dim3((unsigned)std::min(p.units, h->sms)), dim3(FEW_WARPS * 32), FEW_SMEM, st, p);
+    p.mt = p.M <= 8 ? 1 : (p.M + 15) / 16;
+    p.units = (p.N + FEW_COLS - 1) / FEW_COLS * p.mt;
+    const dim3 grid((unsigned)std::min(p.units, h->sms)), block(FEW_WARPS * 32);
+    const cudaError_t e = p.M <= 8 ? as_launch_dependent(few_rows_kernel<1>, grid, block, few_smem(1), st, p) : as_launch_dependent(few_rows_kernel<2>, grid, block, few_smem(2), st, p);
     return e == cudaSuccess ? AS_OK : AS_ERR_CUDA;
   }
   MMParams p{};
   p.out = out;
-  p.M = (int)a->rows; p.N = (int)a->out_cols; p.kb = (a->cols + BK - 1) / BK;
+  p.M = (int)a->rows; p.N = (int)a->out_cols; p.kb = kb;
   p.sa = static_cast<const uint8_t*>(a->a.scales); p.sa_rows = a->a.scale_rows;
   p.sw = static_cast<const uint8_t*>(a->w.scales); p.sw_rows = a->w.scale_rows;
   p.bias = static_cast<const __nv_bfloat16*>(a->bias);
   p.status = h->status;
   p.vec = rows_vec(a->out, 16);
-  const Tile tile = tile_of(p.M, p.N, p.kb, h->sms);
   const int CG = tile.cg;
   p.bn = tile.bn;
   p.nt = (p.N + p.bn - 1) / p.bn;

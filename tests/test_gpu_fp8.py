@@ -183,7 +183,8 @@ def operands(M, N, K, seed=0):
 SHAPES = [(1, 1, 1), (1, 16, 16), (1, 15, 128), (2, 9216, 129), (3, 17, 1001), (7, 40, 2048), (8, 1000, 1536), (8, 33, 6145), (5, 5000, 15), (4, 31, 127),
           (9, 16, 128), (9, 1, 1), (31, 77, 130), (33, 1536, 512), (127, 224, 640), (128, 225, 513), (129, 192, 1024), (255, 193, 17), (256, 256, 256), (257, 31, 999),
           (500, 1000, 1160), (1000, 64, 4096), (1001, 4608, 128), (2047, 1536, 384), (2300, 1337, 700), (4096, 160, 256), (7800, 1536, 512), (20011, 448, 257),
-          (300, 20000, 192), (12345, 96, 64), (640, 640, 16384)]
+          (300, 20000, 192), (12345, 96, 64), (640, 640, 16384),
+          (16, 5000, 1536), (17, 1000, 2000), (24, 15, 6145), (40, 512, 1280), (64, 130, 2392), (100, 17, 130), (256, 128, 2392), (256, 64, 100), (15, 3000, 4100)]
 
 
 @pytest.mark.parametrize("M,N,K", SHAPES)
