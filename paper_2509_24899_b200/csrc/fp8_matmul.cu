@@ -12,6 +12,8 @@
 //                the same for each of the four quarters of the lanes, a ring of four
 //   warps 8-15   results: tensor memory -> registers, bias, bf16, a strip of shared memory per warp, from where TMA takes it (or the warp itself does, in
 //                layouts that TMA has no boxes for)
+//
+// Few tiles with long columns: a cluster of single CTAs shares a tile's columns (PARTS).  Few rows of a: few_rows_kernel, further down.
 #include <algorithm>
 #include <new>
 
@@ -55,6 +57,7 @@ struct MMParams {
   long long sa_rows, sw_rows;
   int M, N, kb;                             // kb: blocks of 128 columns
   int bn, stages, nt;
+  int parts;                                // CTAs of a cluster that share a tile's columns of a and w (1: none)
   long long tiles;
   bool vec, copies;                         // results move 16 bytes at a time, or in boxes of 32 rows x 32 columns by TMA
 };
@@ -117,10 +120,7 @@ AS_DEV void arrive_leader(uint32_t bar) {
   if constexpr (CG == 1) mbar_arrive(bar);
   else asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(leaders(bar)) : "memory");
 }
-template <int CG>
-AS_DEV void pair_sync() {
-  if constexpr (CG == 2) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
+AS_DEV void cluster_sync() { asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 AS_DEV void tmem_st4(uint32_t at, const uint32_t (&r)[4]) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
 }
@@ -142,6 +142,7 @@ struct Ctx {
   WaitCtx wc;
   uint32_t rank;                             // of the CTA in its pair
   long long unit, units;                     // this pair (CTA), all of them: tiles unit, unit + units, ...
+  int kb0, kb1;                              // its blocks of 128 columns; kb0 is a multiple of 4
   AS_DEV uint32_t bar(int i) const { return sbase + 8 * i; }
   AS_DEV bool wait(int i, uint32_t parity) const { return mbar_wait(bar(i), parity, wc); }
 };
@@ -154,7 +155,7 @@ AS_DEV void mm_copies(const MMParams& p, const Ctx<CG>& c, const CUtensorMap* ma
   Ring r;
   for (long long t = c.unit; t < p.tiles; t += c.units) {
     const int m0 = (int)(t / p.nt) * (BM * CG) + (int)c.rank * BM, n0 = (int)(t % p.nt) * p.bn + (int)c.rank * rows_w;
-    for (int k = 0; k < p.kb; ++k) {
+    for (int k = c.kb0; k < c.kb1; ++k) {
       if (!c.wait(B_EMPTY + r.slot, r.turn ^ 1u)) goto out;
       const uint32_t at = c.sbase + STAGES_OFF + (uint32_t)r.slot * stage_bytes;
       if (c.rank == 0) mbar_expect_tx(c.bar(B_FULL + r.slot), stage_bytes * CG);
@@ -183,7 +184,7 @@ AS_DEV void mm_issue(const MMParams& p, const Ctx<CG>& c) {
   for (long long t = c.unit; t < p.tiles; t += c.units) {
     if (!c.wait(B_AEMPTY + buf, turn ^ 1u)) return;
     const uint32_t d = c.tmem + buf * 256u;
-    for (int k = 0; k < p.kb; ++k) {
+    for (int k = c.kb0; k < c.kb1; ++k) {
       if (k % 4 == 0)
         if (!c.wait(B_SFULL + sf.slot, sf.turn)) return;
       if (!c.wait(B_FULL + r.slot, r.turn)) return;
@@ -192,10 +193,10 @@ AS_DEV void mm_issue(const MMParams& p, const Ctx<CG>& c) {
       const uint64_t da = make_sdesc(at, 16, 1024), db = make_sdesc(at + BM * BK, 16, 1024);
       const uint32_t idesc = idesc0 | scale_byte_of(k % 4), s = c.tmem + sf_col(sf.slot);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) mma_scaled<CG>(d, da + 2 * i, db + 2 * i, idesc, s, s + 8, (k | i) != 0 ? 1u : 0u);
+      for (int i = 0; i < 4; ++i) mma_scaled<CG>(d, da + 2 * i, db + 2 * i, idesc, s, s + 8, k > c.kb0 || i > 0 ? 1u : 0u);
       commit<CG>(c.bar(B_EMPTY + r.slot));
       r.next(p.stages);
-      if (k % 4 == 3 || k == p.kb - 1) {
+      if (k % 4 == 3 || k == c.kb1 - 1) {
         commit<CG>(c.bar(B_SEMPTY + sf.slot));
         sf.next(SF_SLOTS);
       }
@@ -210,7 +211,7 @@ AS_DEV void mm_issue(const MMParams& p, const Ctx<CG>& c) {
 template <int CG>
 AS_DEV void mm_scales(const MMParams& p, const Ctx<CG>& c, int lane, int quarter) {
   const uint32_t lanes = (uint32_t)quarter * 32u << 16;
-  const int groups = (p.kb + 3) / 4;
+  const int g0 = c.kb0 / 4, groups = (c.kb1 + 3) / 4;
   const uint32_t ones = 0x7f7f7f7fu;         // rows that are not there
   uint32_t a[4], w[8];
   auto fetch = [&](long long t, int g) {
@@ -225,7 +226,7 @@ AS_DEV void mm_scales(const MMParams& p, const Ctx<CG>& c, int lane, int quarter
   };
   Ring sf;
   long long t = c.unit;
-  int g = 0;
+  int g = g0;
   fetch(t, g);
   while (t < p.tiles) {
     uint32_t a0[4], w0[8];
@@ -233,7 +234,7 @@ AS_DEV void mm_scales(const MMParams& p, const Ctx<CG>& c, int lane, int quarter
     for (int j = 0; j < 4; ++j) a0[j] = a[j];
 #pragma unroll
     for (int j = 0; j < 8; ++j) w0[j] = w[j];
-    if (++g == groups) { g = 0; t += c.units; }
+    if (++g == groups) { g = g0; t += c.units; }
     fetch(t, g);
     const bool ok = c.wait(B_SEMPTY + sf.slot, sf.turn ^ 1u);
     if (!__all_sync(0xffffffffu, ok)) return;
@@ -353,7 +354,59 @@ AS_DEV void mm_results(const MMParams& p, const Ctx<CG>& c, const CUtensorMap* m
   if (lane == 0) tma_store_wait_read();       // (the writes land by the end of the kernel)
 }
 
-template <int CG>
+// A tile whose columns of a and w are shared by a cluster of CTAs: each leaves its sums in its shared memory, in fp32 and where the stages were, and adds up a part of the tile's 8-column
+// pieces over all of them, in the order of their ranks.
+constexpr int PART_PAD = 16;                  // bytes behind a row of sums, so that rows begin in other banks
+AS_DEV void part_leave(const MMParams& p, const Ctx<1>& c, int lane, int warp) {
+  const int quarter = warp & 3, half = warp >> 2;
+  if (!mbar_wait_warp(c.bar(B_AFULL), 0, c.wc)) return;
+  tc_fence_after();
+  const uint32_t row = c.sbase + STAGES_OFF + (uint32_t)(quarter * 32 + lane) * (uint32_t)(p.bn * 4 + PART_PAD);
+  for (int c0 = 32 * half; c0 < p.bn; c0 += 64) {
+    uint32_t x[32];
+    tmem_ld32(c.tmem + ((uint32_t)quarter * 32u << 16) + c0, x);
+    tmem_ld_wait(x);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(row + c0 * 4 + i * 16), "r"(x[4 * i]), "r"(x[4 * i + 1]), "r"(x[4 * i + 2]), "r"(x[4 * i + 3]) : "memory");
+  }
+}
+AS_DEV void part_add(const MMParams& p, const Ctx<1>& c, int rank) {
+  const int m0 = (int)(c.unit / p.nt) * BM, n0 = (int)(c.unit % p.nt) * p.bn, across = p.bn / 8, pieces = BM * across;
+  __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out.data);
+  for (int e = pieces * rank / p.parts + threadIdx.x; e < pieces * (rank + 1) / p.parts; e += MM_THREADS) {
+    const int r = e / across, n = n0 + e % across * 8, m = m0 + r;
+    if (m >= p.M || n >= p.N) continue;
+    const uint32_t at = c.sbase + STAGES_OFF + (uint32_t)r * (uint32_t)(p.bn * 4 + PART_PAD) + (uint32_t)(e % across) * 32u;
+    float f[8] = {};
+    for (int q = 0; q < p.parts; ++q) {
+      uint32_t from;
+      asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(from) : "r"(at), "r"(q));
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float4 v;
+        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(from + 16 * h) : "memory");
+        f[4 * h] += v.x; f[4 * h + 1] += v.y; f[4 * h + 2] += v.z; f[4 * h + 3] += v.w;
+      }
+    }
+    if (p.bias != nullptr) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (n + i < p.N) f[i] += __bfloat162float(p.bias[n + i]);
+    }
+    const long long row = p.out.row((unsigned)m);
+    if (p.vec) {
+      *reinterpret_cast<uint4*>(out + row + p.out.col((unsigned)n)) = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (n + i < p.N) out[row + p.out.col((unsigned)(n + i))] = __float2bfloat16_rn(f[i]);
+    }
+  }
+}
+
+// PARTS: p.parts CTAs share a tile, one tile each cluster (CG == 1).
+template <int CG, bool PARTS>
 __global__ void __launch_bounds__(MM_THREADS, 1)
 matmul_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mw, const __grid_constant__ CUtensorMap mo,
               const __grid_constant__ MMParams p) {
@@ -362,7 +415,13 @@ matmul_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CU
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + 8 * B_COUNT);
   volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem + 8 * B_COUNT + 4);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  Ctx<CG> c{smem_u32(smem), 0u, WaitCtx{p.status, abort_flag}, CG == 1 ? 0u : cta_rank(), blockIdx.x / CG, gridDim.x / CG};
+  const uint32_t in_cluster = CG == 1 && !PARTS ? 0u : cta_rank();
+  const int sharing = PARTS ? p.parts : CG, groups = (p.kb + 3) / 4;
+  Ctx<CG> c{smem_u32(smem), 0u, WaitCtx{p.status, abort_flag}, PARTS ? 0u : in_cluster, blockIdx.x / sharing, gridDim.x / sharing, 0, p.kb};
+  if constexpr (PARTS) {
+    c.kb0 = groups * (int)in_cluster / p.parts * 4;
+    c.kb1 = min(groups * ((int)in_cluster + 1) / p.parts * 4, p.kb);
+  }
   if (threadIdx.x == 0) {
     *abort_flag = 0u;
     for (int s = 0; s < MAX_STAGES; ++s) { mbar_init(c.bar(B_FULL + s), 1); mbar_init(c.bar(B_EMPTY + s), 1); }
@@ -375,7 +434,7 @@ matmul_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CU
   if (warp == 2) { alloc_tmem<CG>(smem_u32(tmem_slot)); griddep_launch(); }
   tc_fence_before();
   __syncthreads();
-  pair_sync<CG>();                             // the peer's barriers stand before anything arrives there
+  if constexpr (CG == 2) cluster_sync();       // the peer's barriers stand before anything arrives there
   tc_fence_after();
   c.tmem = *tmem_slot;
   griddep_wait();
@@ -388,7 +447,13 @@ matmul_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CU
   } else if (warp >= 4 && warp < 8) {
     mm_scales<CG>(p, c, lane, warp - 4);
   } else if (warp >= 8) {
-    mm_results<CG>(p, c, &mo, lane, warp - 8);
+    if constexpr (PARTS) part_leave(p, c, lane, warp - 8);
+    else mm_results<CG>(p, c, &mo, lane, warp - 8);
+  }
+  if constexpr (PARTS) {
+    __syncthreads();
+    cluster_sync();                            // all sums of the tile stand
+    part_add(p, c, (int)in_cluster);
   }
   if (*abort_flag != 0u) {                     // a wait ran out: copies and MMAs under way get 20 us (they take two) before memory is given back
     const long long t0 = clock64();
@@ -396,7 +461,7 @@ matmul_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CU
   }
   tc_fence_before();
   __syncthreads();
-  pair_sync<CG>();                             // nothing of this CTA is reached from the peer any more
+  if constexpr (CG == 2 || PARTS) cluster_sync();        // nothing of this CTA is reached from the others any more
   if (warp == 2) {
     tc_fence_after();
     free_tmem<CG>(c.tmem);
@@ -541,17 +606,27 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 1) few_rows_kernel(const __gri
 // of a bound a block, 64 bytes a clock into an SM (a pair halves those of w), above them the MMAs, and power: at 32760 x 4608 x 1536, back to back, 192 and 224 rows take
 // 212 and 209 us at 1.45 GHz.  The last turn counts half of what it leaves idle, as the clock rises meanwhile; a single turn counts whole.
 // Few rows go to single CTAs and narrow tiles: 512 x 1536 x 1536 takes 6.1 us with {1, 64}, 7.2 with {2, 192}.
-struct Tile { int cg, bn; double ns; };
-Tile tile_of(int M, int N, int kb, int sms) {
+struct Tile { int cg, bn, parts; double ns; };
+//
+// Few tiles with long columns go to clusters of CTAs that share a tile's columns, by whole groups of four blocks, as many as the device holds at once (`clusters`, by size): 2 us more
+// for the meeting and the sums, and more with every CTA beyond two (128 x 1536 x 6144 14.0 us by single CTAs, 9.4 by three, 9.6 by five; 512 x 1536 x 6144 15.0, 11.5 by two, 13.2 by three;
+// 300 x 512 x 4096 10.1 and 8.0; but 512 x 1536 x 1536 5.9 and 8.1, 1024 x 512 x 2048 6.5 and 7.4).
+constexpr int MAX_PARTS = 8;
+Tile tile_of(int M, int N, int kb, int sms, const int (&clusters)[MAX_PARTS + 1]) {
   static const int ns[2][7] = {{230, 250, 265, 300, 345, 385, 440}, {228, 230, 240, 262, 297, 320, 365}};
-  Tile best{1, 32, 1e300};
+  Tile best{1, 32, 1, 1e300};
   for (int cg = 1; cg <= 2; ++cg)
     for (int i = 0; i < 7; ++i) {
       const int bn = 32 * (i + 1);
       const long long tiles = ((long long)M + BM * cg - 1) / (BM * cg) * ((N + bn - 1) / bn), units = sms / cg, whole = (tiles + units - 1) / units;
       const double turns = whole == 1 ? 1. : 0.5 * ((double)tiles / units + whole);
       const double t = turns * kb * ns[cg - 1][i] + 7. * bn + (cg == 2 ? 400. : 0.);
-      if (t < best.ns) best = {cg, bn, t};
+      if (t < best.ns) best = {cg, bn, 1, t};
+      const int groups = (kb + 3) / 4;
+      for (int parts = 2; cg == 1 && parts <= std::min(MAX_PARTS, groups); ++parts) {
+        const double shared = 4. * ((groups + parts - 1) / parts) * ns[0][i] + 7. * bn + 2000. + 8. * std::max(bn - 64, 0) + (parts - 2) * (700. + 10. * (bn - 32));
+        if (tiles <= clusters[parts] && shared < best.ns) best = {1, bn, parts, shared};
+      }
     }
   return best;
 }
@@ -566,23 +641,25 @@ bool few_rows(int M, int N, int kb, int sms, const Tile& tile) {
   return 700. + 1500. * (double)(turns - 1) < tile.ns + 500.;
 }
 
-template <int CG>
+template <int CG, bool PARTS>
 cudaError_t launch(const CUtensorMap& ma, const CUtensorMap& mw, const CUtensorMap& mo, const MMParams& p, int units, size_t smem, cudaStream_t st) {
+  const int sharing = PARTS ? p.parts : CG;
   cudaLaunchAttribute attr[2]{};
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = CG; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  attr[1].val.clusterDim.x = sharing; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(units * CG)); cfg.blockDim = dim3(MM_THREADS); cfg.dynamicSmemBytes = smem; cfg.stream = st;
-  cfg.attrs = attr; cfg.numAttrs = CG == 1 ? 1 : 2;
-  return cudaLaunchKernelEx(&cfg, matmul_kernel<CG>, ma, mw, mo, p);
+  cfg.gridDim = dim3((unsigned)(units * sharing)); cfg.blockDim = dim3(MM_THREADS); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+  cfg.attrs = attr; cfg.numAttrs = sharing == 1 ? 1 : 2;
+  return cudaLaunchKernelEx(&cfg, matmul_kernel<CG, PARTS>, ma, mw, mo, p);
 }
 
 }  // namespace
 
 struct as_fp8_context_s {
   int device = -1, sms = 0;
+  int clusters[MAX_PARTS + 1] = {};          // of so many CTAs that the device holds at once
   uint32_t* status = nullptr;
 };
 
@@ -593,13 +670,23 @@ extern "C" as_status_t as_fp8_create(as_fp8_context_t* out) {
       cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
     return AS_ERR_CUDA;
   if (major != 10) return AS_ERR_ARCH;
-  if (as_tensor_init() != cudaSuccess || as_tc::opt_in_smem(matmul_kernel<1>, SMEM_MAX) != cudaSuccess || as_tc::opt_in_smem(matmul_kernel<2>, SMEM_MAX) != cudaSuccess ||
+  if (as_tensor_init() != cudaSuccess || as_tc::opt_in_smem(matmul_kernel<1, false>, SMEM_MAX) != cudaSuccess || as_tc::opt_in_smem(matmul_kernel<2, false>, SMEM_MAX) != cudaSuccess ||
+      as_tc::opt_in_smem(matmul_kernel<1, true>, SMEM_MAX) != cudaSuccess ||
       as_tc::opt_in_smem(few_rows_kernel<1>, few_smem(1)) != cudaSuccess || as_tc::opt_in_smem(few_rows_kernel<2>, few_smem(2)) != cudaSuccess)
     return AS_ERR_CUDA;
   as_fp8_context_s* h = new (std::nothrow) as_fp8_context_s;
   if (h == nullptr) return AS_ERR_ALLOC;
   h->device = dev;
   h->sms = sms;
+  for (int parts = 2; parts <= MAX_PARTS; ++parts) {
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = parts; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)parts); cfg.blockDim = dim3(MM_THREADS); cfg.dynamicSmemBytes = SMEM_MAX;
+    cfg.attrs = &attr; cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&h->clusters[parts], matmul_kernel<1, true>, &cfg) != cudaSuccess) { delete h; return AS_ERR_CUDA; }
+  }
   if (cudaMalloc(&h->status, 256) != cudaSuccess) { delete h; return AS_ERR_ALLOC; }
   if (cudaMemset(h->status, 0, 256) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) { cudaFree(h->status); delete h; return AS_ERR_CUDA; }
   *out = h;
@@ -636,7 +723,7 @@ extern "C" as_status_t as_matmul_fp8(as_fp8_context_t h, const as_matmul_fp8_t* 
   if (a->rows == 0) return AS_OK;
   const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   const int kb = (a->cols + BK - 1) / BK;
-  const Tile tile = tile_of((int)a->rows, (int)a->out_cols, kb, h->sms);
+  const Tile tile = tile_of((int)a->rows, (int)a->out_cols, kb, h->sms, h->clusters);
   if (few_rows((int)a->rows, (int)a->out_cols, kb, h->sms, tile)) {
     FewParams p{};
     p.a = static_cast<const uint8_t*>(a->a.data); p.a_pitch = a->a.pitch;
@@ -661,7 +748,7 @@ extern "C" as_status_t as_matmul_fp8(as_fp8_context_t h, const as_matmul_fp8_t* 
   p.status = h->status;
   p.vec = rows_vec(a->out, 16);
   const int CG = tile.cg;
-  p.bn = tile.bn;
+  p.bn = tile.bn; p.parts = tile.parts;
   p.nt = (p.N + p.bn - 1) / p.bn;
   p.tiles = ((long long)p.M + BM * CG - 1) / (BM * CG) * p.nt;
   const int stage = (BM + p.bn / CG) * BK;
@@ -672,6 +759,7 @@ extern "C" as_status_t as_matmul_fp8(as_fp8_context_t h, const as_matmul_fp8_t* 
   p.copies = p.vec && (a->out.head_dim == p.N || a->out.head_dim % 32 == 0) && as_tc::make_map_rows(&mo, a->out, p.M, p.N, 32);
   if (!as_tc::make_map_bytes(&ma, a->a.data, a->cols, p.M, a->a.pitch, BM) || !as_tc::make_map_bytes(&mw, a->w.data, a->cols, p.N, a->w.pitch, p.bn / CG)) return AS_ERR_CUDA;
   const int units = (int)std::min<long long>(p.tiles, h->sms / CG);
-  const cudaError_t e = CG == 2 ? launch<2>(ma, mw, mo, p, units, smem, st) : launch<1>(ma, mw, mo, p, units, smem, st);
+  const cudaError_t e = tile.parts > 1 ? launch<1, true>(ma, mw, mo, p, (int)p.tiles, smem, st)
+                                       : CG == 2 ? launch<2, false>(ma, mw, mo, p, units, smem, st) : launch<1, false>(ma, mw, mo, p, units, smem, st);
   return e == cudaSuccess ? AS_OK : AS_ERR_CUDA;
 }

@@ -184,7 +184,8 @@ SHAPES = [(1, 1, 1), (1, 16, 16), (1, 15, 128), (2, 9216, 129), (3, 17, 1001), (
           (9, 16, 128), (9, 1, 1), (31, 77, 130), (33, 1536, 512), (127, 224, 640), (128, 225, 513), (129, 192, 1024), (255, 193, 17), (256, 256, 256), (257, 31, 999),
           (500, 1000, 1160), (1000, 64, 4096), (1001, 4608, 128), (2047, 1536, 384), (2300, 1337, 700), (4096, 160, 256), (7800, 1536, 512), (20011, 448, 257),
           (300, 20000, 192), (12345, 96, 64), (640, 640, 16384),
-          (16, 5000, 1536), (17, 1000, 2000), (24, 15, 6145), (40, 512, 1280), (64, 130, 2392), (100, 17, 130), (256, 128, 2392), (256, 64, 100), (15, 3000, 4100)]
+          (16, 5000, 1536), (17, 1000, 2000), (24, 15, 6145), (40, 512, 1280), (64, 130, 2392), (100, 17, 130), (256, 128, 2392), (256, 64, 100), (15, 3000, 4100),
+          (128, 1536, 6144), (300, 512, 4096), (512, 1536, 6144), (129, 321, 6145), (77, 3000, 8200), (200, 1, 16384), (1000, 200, 5121), (640, 40, 3585)]
 
 
 @pytest.mark.parametrize("M,N,K", SHAPES)
@@ -194,11 +195,11 @@ def test_matmul_shapes(ops, M, N, K):
     R.check_matmul(ops.matmul_fp8(a, w, bias=bias), a, w, bias)
 
 
-@pytest.mark.parametrize("M", [2, 40, 700])
+@pytest.mark.parametrize("M,K", [(2, 300), (40, 300), (700, 300), (260, 4200)])
 @pytest.mark.parametrize("B,H,d", [(2, 3, 64), (2, 4, 128), (1, 5, 32), (2, 6, 16), (2, 3, 40), (1, 7, 9), (2, 2, 8)])
-def test_matmul_into_heads(ops, M, B, H, d):
+def test_matmul_into_heads(ops, M, K, B, H, d):
     """Strips that TMA takes, that cross into the next batch entry, that warps store 16 bytes or an element at a time; nothing else is written."""
-    a, w, bias = operands(M, H * d, 300, seed=M)
+    a, w, bias = operands(M, H * d, K, seed=M)
     box = Guarded(M * H * d * 2)
     out = box.view(BF16, (B, H, M // B, d))
     assert ops.matmul_fp8(a, w, bias=bias, out=out) is out
@@ -293,7 +294,7 @@ def test_no_rows(ops):
 
 # ------------------------------------------------------------------------------------------------ calls
 def test_same_bits_every_time(ops):
-    for M, N, K in ((2, 1000, 1536), (700, 1000, 1536), (5000, 1536, 512)):
+    for M, N, K in ((2, 1000, 1536), (40, 200, 1000), (300, 512, 4096), (700, 1000, 1536), (5000, 1536, 512)):
         a, w, bias = operands(M, N, K)
         first = ops.matmul_fp8(a, w, bias=bias)
         for _ in range(3):
