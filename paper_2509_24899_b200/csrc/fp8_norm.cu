@@ -285,26 +285,27 @@ __global__ void __launch_bounds__(THREADS, goes_on<X, R, MOVE> ? 2 : 1) norm_ker
     if (early) {
 #pragma unroll
       for (int j = 0; j < NV; ++j) scale_values<__nv_bfloat16, MOVE>(w16[j], v[j]);
+    } else if (weighs && !p.w_f32) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        Raw<__nv_bfloat16, MOVE> w{};
+        if constexpr (GOES_ON) {
+          if ((first / 512 + j) * 512 < p.cols) {
+            const uint4* at = kept + (first / 512 + j) * 64 + (lane & (LANES - 1));
+            reinterpret_cast<uint4*>(w.w)[0] = at[0];
+            reinterpret_cast<uint4*>(w.w)[1] = at[32];
+          }
+        } else {
+          fetch<__nv_bfloat16, MOVE>(weights, 0, c0 + j * 512, cols, w);
+        }
+        scale_values<__nv_bfloat16, MOVE>(w, v[j]);
+      }
     } else if (weighs) {
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
-        if ((MOVE == MOVE_ELEMENT || GOES_ON) && !p.w_f32) {
-          Raw<__nv_bfloat16, MOVE> w{};
-          if constexpr (GOES_ON) {
-            if ((first / 512 + j) * 512 < p.cols) {
-              const uint4* at = kept + (first / 512 + j) * 64 + (lane & (LANES - 1));
-              reinterpret_cast<uint4*>(w.w)[0] = at[0];
-              reinterpret_cast<uint4*>(w.w)[1] = at[32];
-            }
-          } else {
-            fetch<__nv_bfloat16, MOVE>(weights, 0, c0 + j * 512, cols, w);
-          }
-          scale_values<__nv_bfloat16, MOVE>(w, v[j]);
-        } else {
-          Raw<float, MOVE> w;
-          fetch<float, MOVE>(weights, 0, c0 + j * 512, cols, w);
-          scale_values<float, MOVE>(w, v[j]);
-        }
+        Raw<float, MOVE> w;
+        fetch<float, MOVE>(weights, 0, c0 + j * 512, cols, w);
+        scale_values<float, MOVE>(w, v[j]);
       }
     }
   }
