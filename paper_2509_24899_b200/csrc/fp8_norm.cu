@@ -190,14 +190,16 @@ constexpr float MOST = 3.402823466e38f;
 // The weights multiply t while the sum of squares is on its way between the lanes, and so do the blocks' largest values go round: both turns of a row's reductions
 // overlap, and the row's scale enters last.  What counts is the number of instructions: with 8 columns a lane, one value an instruction and the formula's order a row of 1536
 // columns with a residual in bf16 took 131 us for 32760 rows; in pairs, weights ahead of the scale, 62 us; with 16 columns a lane, whose loads are half as many and whose
-// scales are a third as much work, 56 us (6.3 TB/s).  Without a residual 54, 38 and 30 us (5.0 TB/s), the last with CTAs that go on; the 8-bit form alone 34, 26 and 25 us
+// scales are a third as much work, 56 us (6.3 TB/s).  Without a residual 54, 38 and 29 us (5.2 TB/s), the last with CTAs that go on; the 8-bit form alone 34, 26 and 25 us
 // (6.1 TB/s).  Rows further ahead, as asynchronous copies into shared memory, did not help there: 35 and 27 us with four rows under way, for the instructions that it takes.
 // With x in bf16 and no residual a CTA goes on from row to row: its weights stay in shared memory, and a row's loads are under way while the one before it is
 // worked on.  (With a residual or in fp32 there is enough under way without that, and no room for it.)  Two CTAs an SM.
 template <typename X, typename R, int MOVE> constexpr bool goes_on = sizeof(X) == 2 && __is_same(R, void) && MOVE != MOVE_ELEMENT;
 
+__host__ __device__ constexpr int ctas_of_sm(bool goes_on, int move, int nv) { return goes_on ? 2 : move != MOVE_ELEMENT ? 1 : nv == 1 ? 4 : nv == 2 ? 2 : 1; }
+
 template <typename X, typename R, bool NORM, bool FP8, int MOVE, int NV, int LANES>
-__global__ void __launch_bounds__(THREADS, goes_on<X, R, MOVE> ? 2 : 1) norm_kernel(const __grid_constant__ NormParams p) {
+__global__ void __launch_bounds__(THREADS, ctas_of_sm(goes_on<X, R, MOVE>, MOVE, NV)) norm_kernel(const __grid_constant__ NormParams p) {
   griddep_launch();
   __shared__ float part[THREADS / 32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -472,7 +474,9 @@ __global__ void __launch_bounds__(THREADS) quantize_block_kernel(const __grid_co
 struct Split { int lanes, W, NV; };
 Split split_of(int cols, int move) {
   if (move != MOVE_ELEMENT && cols <= 256) return {cols <= 128 ? 8 : 16, 1, 1};
-  const int most = move != MOVE_ELEMENT && cols <= 8 * 1536 ? 3 : 4;          // a fourth vector does not fit the registers of two CTAs beside the next row
+  // A fourth vector does not fit the registers of two CTAs beside the next row.  Element by element latency counts, so as many warps as there are take one vector each (32760 x 1537 with a
+  // residual in bf16 198 us, by two vectors a warp 230, by four 514; 8000 x 4001 alone to 8 bits 46 and 104).
+  const int most = move != MOVE_ELEMENT ? (cols <= 8 * 1536 ? 3 : 4) : cols <= 4096 ? 1 : cols <= 8192 ? 2 : 4;
   const int W = (cols + 512 * most - 1) / (512 * most);
   return {32, W, (cols + 512 * W - 1) / (512 * W)};
 }
