@@ -72,14 +72,15 @@ AS_DEV void store32(void* at, const uint32_t (&w)[8]) {
 template <typename T, int MOVE> struct Raw { uint32_t w[4 * sizeof(T)]; };
 template <typename T> struct Raw<T, MOVE_ELEMENT> { T e[16]; };
 
-template <typename T, int MOVE>
+// SPLIT: element by element, whether columns belong to heads that lie apart; asked once for all loads, as a branch at each would make it wait for the one before it.
+template <typename T, int MOVE, bool SPLIT = true>
 AS_DEV void fetch(const Rows& m, long long row, int c0, int cols, Raw<T, MOVE>& v) {
   const T* base = static_cast<const T*>(m.data) + row;
   if constexpr (MOVE == MOVE_ELEMENT) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const int c = c0 + 32 * i;
-      v.e[i] = c < cols ? base[m.col(c)] : (T)0.f;
+      v.e[i] = c < cols ? base[SPLIT ? m.col(c) : c] : (T)0.f;
     }
   } else {
     v = Raw<T, MOVE>{};
@@ -98,6 +99,17 @@ AS_DEV void fetch(const Rows& m, long long row, int c0, int cols, Raw<T, MOVE>& 
           for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(v.w)[h * (int)sizeof(T) / 2 + i] = at[i];
         }
     }
+  }
+}
+// All vectors of a row, 512 columns apart.
+template <typename T, int MOVE, int NV>
+AS_DEV void fetch_row(const Rows& m, long long row, int c0, int cols, Raw<T, MOVE> (&v)[NV]) {
+  if (MOVE == MOVE_ELEMENT && !m.split) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) fetch<T, MOVE, false>(m, row, c0 + j * 512, cols, v[j]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) fetch<T, MOVE, true>(m, row, c0 + j * 512, cols, v[j]);
   }
 }
 template <typename T, int MOVE>
@@ -135,14 +147,16 @@ template <typename T, int MOVE>
 AS_DEV void store16(const Rows& m, long long row, int c0, int cols, const float2 (&f)[8]) {
   T* base = static_cast<T*>(m.data) + row;
   if constexpr (MOVE == MOVE_ELEMENT) {
+    auto store = [&](auto at) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int c = c0 + 32 * i;
-      const float x = i % 2 ? f[i / 2].y : f[i / 2].x;
-      if (c >= cols) continue;
-      if constexpr (sizeof(T) == 2) base[m.col(c)] = __float2bfloat16_rn(x);
-      else base[m.col(c)] = x;
-    }
+      for (int i = 0; i < 16; ++i) {
+        const int c = c0 + 32 * i;
+        const float x = i % 2 ? f[i / 2].y : f[i / 2].x;
+        if (c < cols) base[at(c)] = (T)x;
+      }
+    };
+    if (m.split) store([&](int c) { return m.col(c); });
+    else store([](int c) { return c; });
   } else {
     uint32_t w[4 * sizeof(T)];
 #pragma unroll
@@ -222,8 +236,7 @@ __global__ void __launch_bounds__(THREADS, ctas_of_sm(goes_on<X, R, MOVE>, MOVE,
   auto fetch_x = [&](long long at) {                          // of a row that is not there nothing is read or written
     const bool there = slot < per && at < p.rows;
     const long long xr = there ? p.x.row((unsigned)at) : 0;
-#pragma unroll
-    for (int j = 0; j < NV; ++j) fetch<X, MOVE>(p.x, xr, c0 + j * 512, there ? p.cols : 0, x[j]);
+    fetch_row<X, MOVE, NV>(p.x, xr, c0, there ? p.cols : 0, x);
   };
   // weights in bf16 of a CTA that goes on: the 32 bytes of column vector u of the row as two pieces of 16 bytes, the vectors of a group of four blocks
   // next to each other, so that a warp reads each piece without bank conflicts
@@ -252,8 +265,7 @@ __global__ void __launch_bounds__(THREADS, ctas_of_sm(goes_on<X, R, MOVE>, MOVE,
     if constexpr (!__is_same(R, void)) {
       Raw<R, MOVE> t[NV];
       const long long rr = p.r.row(r), wr = p.ro.row(r);
-#pragma unroll
-      for (int j = 0; j < NV; ++j) fetch<R, MOVE>(p.r, rr, c0 + j * 512, cols, t[j]);
+      fetch_row<R, MOVE, NV>(p.r, rr, c0, cols, t);
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
         values<X, MOVE>(x[j], v[j]);
@@ -298,7 +310,7 @@ __global__ void __launch_bounds__(THREADS, ctas_of_sm(goes_on<X, R, MOVE>, MOVE,
             reinterpret_cast<uint4*>(w.w)[1] = at[32];
           }
         } else {
-          fetch<__nv_bfloat16, MOVE>(weights, 0, c0 + j * 512, cols, w);
+          fetch<__nv_bfloat16, MOVE, MOVE != MOVE_ELEMENT>(weights, 0, c0 + j * 512, cols, w);
         }
         scale_values<__nv_bfloat16, MOVE>(w, v[j]);
       }
@@ -306,7 +318,7 @@ __global__ void __launch_bounds__(THREADS, ctas_of_sm(goes_on<X, R, MOVE>, MOVE,
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
         Raw<float, MOVE> w;
-        fetch<float, MOVE>(weights, 0, c0 + j * 512, cols, w);
+        fetch<float, MOVE, MOVE != MOVE_ELEMENT>(weights, 0, c0 + j * 512, cols, w);
         scale_values<float, MOVE>(w, v[j]);
       }
     }
@@ -407,6 +419,21 @@ __global__ void __launch_bounds__(THREADS, ctas_of_sm(goes_on<X, R, MOVE>, MOVE,
   }
 }
 
+// Four elements of a row, 32 columns apart.
+template <typename X>
+AS_DEV void fetch_four(const Rows& m, long long row, int c0, int cols, X* e) {
+  const X* base = static_cast<const X*>(m.data) + row;
+  long long at[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) at[i] = c0 + 32 * i;
+  if (m.split) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) at[i] = m.col(c0 + 32 * i);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) e[i] = c0 + 32 * i < cols ? base[at[i]] : (X)0.f;
+}
+
 // A scale for 128 rows and 128 columns: a CTA per block, a thread's 64 elements in registers: 8 lanes a row and 16 columns a lane, or element by
 // element 4 columns of each of 16 rows.  The CTA of a group's last block writes the bytes behind it as well.
 template <typename X, int MOVE>
@@ -427,10 +454,12 @@ __global__ void __launch_bounds__(THREADS) quantize_block_kernel(const __grid_co
       values<X, MOVE>(x, v[j]);
     } else {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int row = row0 + warp * 16 + j * 4 + i / 4, c = c0 + i % 4 * 32 + lane;
-        const float f = row < p.rows && c < p.cols ? (float)static_cast<const X*>(p.x.data)[p.x.row(row) + p.x.col(c)] : 0.f;
-        if (i % 2) v[j][i / 2].y = f; else v[j][i / 2].x = f;
+      for (int r = 0; r < 4; ++r) {
+        const int row = row0 + warp * 16 + j * 4 + r;
+        Raw<X, MOVE> x;                       // (its first four: 32 columns apart)
+        fetch_four<X>(p.x, row < p.rows ? p.x.row(row) : 0, c0 + lane, row < p.rows ? p.cols : 0, x.e);
+        v[j][2 * r] = make_float2((float)x.e[0], (float)x.e[1]);
+        v[j][2 * r + 1] = make_float2((float)x.e[2], (float)x.e[3]);
       }
     }
 #pragma unroll
