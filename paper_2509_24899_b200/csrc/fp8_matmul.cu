@@ -57,7 +57,7 @@ struct MMParams {
   long long sa_rows, sw_rows;
   int M, N, kb;                             // kb: blocks of 128 columns
   int bn, stages, nt;
-  int parts;                                // CTAs of a cluster that share a tile's columns of a and w (1: none)
+  int sharers;                              // CTAs of a cluster that share a tile's columns of a and w (1: none)
   long long tiles;
   bool vec, copies;                         // results move 16 bytes at a time, or in boxes of 32 rows x 32 columns by TMA
 };
@@ -374,12 +374,12 @@ AS_DEV void part_leave(const MMParams& p, const Ctx<1>& c, int lane, int warp) {
 AS_DEV void part_add(const MMParams& p, const Ctx<1>& c, int rank) {
   const int m0 = (int)(c.unit / p.nt) * BM, n0 = (int)(c.unit % p.nt) * p.bn, across = p.bn / 8, pieces = BM * across;
   __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out.data);
-  for (int e = pieces * rank / p.parts + threadIdx.x; e < pieces * (rank + 1) / p.parts; e += MM_THREADS) {
+  for (int e = pieces * rank / p.sharers + threadIdx.x; e < pieces * (rank + 1) / p.sharers; e += MM_THREADS) {
     const int r = e / across, n = n0 + e % across * 8, m = m0 + r;
     if (m >= p.M || n >= p.N) continue;
     const uint32_t at = c.sbase + STAGES_OFF + (uint32_t)r * (uint32_t)(p.bn * 4 + PART_PAD) + (uint32_t)(e % across) * 32u;
     float f[8] = {};
-    for (int q = 0; q < p.parts; ++q) {
+    for (int q = 0; q < p.sharers; ++q) {
       uint32_t from;
       asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(from) : "r"(at), "r"(q));
 #pragma unroll
@@ -405,7 +405,7 @@ AS_DEV void part_add(const MMParams& p, const Ctx<1>& c, int rank) {
   }
 }
 
-// PARTS: p.parts CTAs share a tile, one tile each cluster (CG == 1).
+// PARTS: p.sharers CTAs share a tile, one tile each cluster (CG == 1).
 template <int CG, bool PARTS>
 __global__ void __launch_bounds__(MM_THREADS, 1)
 matmul_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mw, const __grid_constant__ CUtensorMap mo,
@@ -416,11 +416,11 @@ matmul_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CU
   volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem + 8 * B_COUNT + 4);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t in_cluster = CG == 1 && !PARTS ? 0u : cta_rank();
-  const int sharing = PARTS ? p.parts : CG, groups = (p.kb + 3) / 4;
+  const int sharing = PARTS ? p.sharers : CG, groups = (p.kb + 3) / 4;
   Ctx<CG> c{smem_u32(smem), 0u, WaitCtx{p.status, abort_flag}, PARTS ? 0u : in_cluster, blockIdx.x / sharing, gridDim.x / sharing, 0, p.kb};
   if constexpr (PARTS) {
-    c.kb0 = groups * (int)in_cluster / p.parts * 4;
-    c.kb1 = min(groups * ((int)in_cluster + 1) / p.parts * 4, p.kb);
+    c.kb0 = groups * (int)in_cluster / p.sharers * 4;
+    c.kb1 = min(groups * ((int)in_cluster + 1) / p.sharers * 4, p.kb);
   }
   if (threadIdx.x == 0) {
     *abort_flag = 0u;
@@ -643,7 +643,7 @@ bool few_rows(int M, int N, int kb, int sms, const Tile& tile) {
 
 template <int CG, bool PARTS>
 cudaError_t launch(const CUtensorMap& ma, const CUtensorMap& mw, const CUtensorMap& mo, const MMParams& p, int units, size_t smem, cudaStream_t st) {
-  const int sharing = PARTS ? p.parts : CG;
+  const int sharing = PARTS ? p.sharers : CG;
   cudaLaunchAttribute attr[2]{};
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -748,7 +748,7 @@ extern "C" as_status_t as_matmul_fp8(as_fp8_context_t h, const as_matmul_fp8_t* 
   p.status = h->status;
   p.vec = rows_vec(a->out, 16);
   const int CG = tile.cg;
-  p.bn = tile.bn; p.parts = tile.parts;
+  p.bn = tile.bn; p.sharers = tile.parts;
   p.nt = (p.N + p.bn - 1) / p.bn;
   p.tiles = ((long long)p.M + BM * CG - 1) / (BM * CG) * p.nt;
   const int stage = (BM + p.bn / CG) * BK;
