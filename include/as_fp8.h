@@ -91,7 +91,7 @@ typedef struct {
   as_fp8_matrix_t a;        /* [M, K] */
   as_fp8_matrix_t w;        /* [N, K] */
   const void* bias;         /* [N] bf16, 2-byte aligned, or NULL */
-  as_rows_t out;            /* [M, N] bf16 */
+  as_rows_t out;            /* [M, N] bf16; heads that lie apart: N * head_dim up to 2^32 */
 } as_matmul_fp8_t;
 
 /* t = x + residual in fp32; y = t * rsqrt(mean(t^2) + eps) * weight from the unrounded t; t is rounded once into residual_out, y
