@@ -33,6 +33,18 @@ bool status(as_status_t s, const char* where) {
   return false;
 }
 
+// An object that is given back or let go.
+struct Held {
+  PyObject* o;
+  explicit Held(PyObject* p = nullptr) : o(p) {}
+  ~Held() { Py_XDECREF(o); }
+  Held(const Held&) = delete;
+  Held& operator=(const Held&) = delete;
+  PyObject* give() { PyObject* p = o; o = nullptr; return p; }
+  void take(PyObject* p) { Py_XDECREF(o); o = p; }
+  void share(PyObject* p) { Py_INCREF(p); take(p); }
+};
+
 const at::Tensor* tensor_of(PyObject* o, int here, const char* where, const char* name) {
   if (!THPVariable_Check(o)) { refuse(where, name, "is no tensor"); return nullptr; }
   const at::Tensor& t = THPVariable_Unpack(o);
@@ -63,14 +75,19 @@ const at::Tensor* rows_of(PyObject* o, int here, const char* where, const char* 
   return t;
 }
 
+// The tensors of a pair, held for as long as the call uses them: what hands them out need not keep them (an iterator does not).
+struct Pair { Held data, scales; };
+
 // A pair (e4m3 values, scales) as an as_fp8_matrix_t.
-bool matrix_of(PyObject* pair, int here, const char* where, const char* name, as_fp8_matrix_t& m, int64_t& rows, int64_t& cols) {
+bool matrix_of(PyObject* pair, int here, const char* where, const char* name, Pair& hold, as_fp8_matrix_t& m, int64_t& rows, int64_t& cols) {
   PyObject* fast = PySequence_Fast(pair, "a matrix in 8-bit form is a pair of tensors");
   if (fast == nullptr) return false;
   if (PySequence_Fast_GET_SIZE(fast) != 2) { Py_DECREF(fast); return refuse(where, name, "is no pair of tensors"); }
-  const at::Tensor* data = tensor_of(PySequence_Fast_GET_ITEM(fast, 0), here, where, name);
-  const at::Tensor* scales = data == nullptr ? nullptr : tensor_of(PySequence_Fast_GET_ITEM(fast, 1), here, where, name);
-  Py_DECREF(fast);                            // (the pair holds them)
+  hold.data.share(PySequence_Fast_GET_ITEM(fast, 0));
+  hold.scales.share(PySequence_Fast_GET_ITEM(fast, 1));
+  Py_DECREF(fast);
+  const at::Tensor* data = tensor_of(hold.data.o, here, where, name);
+  const at::Tensor* scales = data == nullptr ? nullptr : tensor_of(hold.scales.o, here, where, name);
   if (scales == nullptr) return false;
   if (data->scalar_type() != at::kFloat8_e4m3fn || scales->scalar_type() != at::kByte || data->dim() != 2 || scales->dim() != 3)
     return refuse(where, name, "is no pair of float8_e4m3fn [rows, cols] and uint8 [ceil(cols / 512), rows, 4]");
@@ -122,18 +139,6 @@ PyObject* empty_pair(int64_t rows, int64_t cols, int here) {
   return made;
 }
 
-// An object that is given back or let go.
-struct Held {
-  PyObject* o;
-  explicit Held(PyObject* p = nullptr) : o(p) {}
-  ~Held() { Py_XDECREF(o); }
-  Held(const Held&) = delete;
-  Held& operator=(const Held&) = delete;
-  PyObject* give() { PyObject* p = o; o = nullptr; return p; }
-  void take(PyObject* p) { Py_XDECREF(o); o = p; }
-  void share(PyObject* p) { Py_INCREF(p); take(p); }
-};
-
 bool context_of(int here, as_fp8_context_t& ctx) {
   if (here < 0 || here >= 64) return status(AS_ERR_UNSUPPORTED, "as_fp8_create");
   std::lock_guard<std::mutex> hold(g_lock);
@@ -166,6 +171,7 @@ PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   if (PyErr_Occurred()) return nullptr;
   if (a[1] != Py_None && !vector_of(a[1], cols, true, here, where, "weight", p.weight, p.weight_dtype)) return nullptr;
   Held out, total;
+  Pair pair;
   if (a[2] != Py_None) {
     const at::Tensor* t = rows_of(a[2], here, where, "residual", p.residual, r, c);
     if (t == nullptr) return nullptr;
@@ -185,7 +191,7 @@ PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   else if (fp8) out.take(empty_pair(rows, cols, here));
   else out.take(empty_contiguous(x->sizes(), at::kBFloat16, here));
   if (out.o == nullptr) return nullptr;
-  if (fp8 ? !matrix_of(out.o, here, where, "out", p.out8, r, c) : rows_of(out.o, here, where, "out", p.out, r, c) == nullptr) return nullptr;
+  if (fp8 ? !matrix_of(out.o, here, where, "out", pair, p.out8, r, c) : rows_of(out.o, here, where, "out", p.out, r, c) == nullptr) return nullptr;
   if (r != rows || c != cols) { refuse(where, "out", "has not x's rows and columns"); return nullptr; }
   if (rows > 0 && cols > 0 && !status(as_rms_norm(&p, current_stream(here)), "as_rms_norm")) return nullptr;
   if (total.o == nullptr) return out.give();
@@ -208,9 +214,10 @@ PyObject* quantize_fp8(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   if (PyErr_Occurred()) return nullptr;
   p.block_rows = block == 1 || block == 128 ? (int32_t)block : 0;
   Held out;
+  Pair pair;
   if (a[2] != Py_None) out.share(a[2]);
   else out.take(empty_pair(rows, cols, here));
-  if (out.o == nullptr || !matrix_of(out.o, here, where, "out", p.out, r, c)) return nullptr;
+  if (out.o == nullptr || !matrix_of(out.o, here, where, "out", pair, p.out, r, c)) return nullptr;
   if (r != rows || c != cols) { refuse(where, "out", "has not x's rows and columns"); return nullptr; }
   if (rows > 0 && cols > 0 && !status(as_quantize_fp8(&p, current_stream(here)), "as_quantize_fp8")) return nullptr;
   return out.give();
@@ -225,7 +232,8 @@ PyObject* matmul_fp8(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   const int here = c10::cuda::current_device();
   as_matmul_fp8_t p{};
   int64_t m, k, n, wk, r, c;
-  if (!matrix_of(a[0], here, where, "a", p.a, m, k) || !matrix_of(a[1], here, where, "w", p.w, n, wk)) return nullptr;
+  Pair of_a, of_w;
+  if (!matrix_of(a[0], here, where, "a", of_a, p.a, m, k) || !matrix_of(a[1], here, where, "w", of_w, p.w, n, wk)) return nullptr;
   if (k != wk) { refuse(where, "w", "has not a's columns"); return nullptr; }
   if (k == 0 && m > 0 && n > 0) { refuse(where, "a", "has no columns to sum over"); return nullptr; }
   int32_t dtype;
