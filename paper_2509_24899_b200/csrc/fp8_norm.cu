@@ -196,7 +196,7 @@ AS_DEV uint32_t block_max(const float2 (&f)[8]) {
 // Element by element: of block b of the warp's four, for all lanes.
 AS_DEV uint32_t block_max_elements(const float2 (&f)[8], int b) { return __reduce_max_sync(0xffffffffu, __float_as_uint(max_abs2(f[2 * b], max_abs2(f[2 * b + 1], 0.f)))); }
 
-constexpr float DOWN = 5.421010862e-20f;       // 2^-64
+constexpr float DOWN = 8.271806126e-25f;       // 2^-80: |t| below 2^128 becomes 2^48 at most, and the sum of 16384 squares 2^110
 constexpr float MOST = 3.402823466e38f;
 
 // NORM: y = t * rsqrt(mean t^2 + eps) * w, else y = x.  R: the residual's type (void: none).  FP8: y in 8-bit form, else in bf16.  LANES: of a row
@@ -286,7 +286,7 @@ __global__ void __launch_bounds__(THREADS, ctas_of_sm(goes_on<X, R, MOVE>, MOVE,
     for (int j = 0; j < NV; ++j)
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum2 = fma2(v[j][i], v[j][i], sum2);
-    // 2^-128 of it, for rows whose squares fp32 does not hold (|t| from 2^64 / sqrt(cols) on).  That there are such rows costs the others up to 2 us of 30.
+    // 2^-160 of it, for rows whose squares fp32 does not hold (|t| from 2^64 / sqrt(cols) on).  That there are such rows costs the others up to 2 us of 30.
     if (!(sum2.x + sum2.y <= MOST)) {
       float2 s = make_float2(0.f, 0.f);
 #pragma unroll

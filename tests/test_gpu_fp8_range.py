@@ -1,0 +1,77 @@
+"""The 8-bit projections at the ends of fp32's range, against their formulas in 64 bits."""
+import pytest
+import torch
+
+from tests import _fp8 as R
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+# The sum of squares: at most 64 values a lane one after another, 5 steps between lanes, 8 warps, each a rounding of 2^-24 of the sum, so half of 77 of them for its root; two
+# ulp (2^-22) for rsqrt; three products of 2^-24; a factor below fp32's normal numbers has 22 bits (2^-22).  In all below 2^-18; twice that.
+SLACK = 2.0 ** -17
+KINDS = [(BF16, None), (BF16, BF16), (BF16, F32), (F32, None), (F32, F32)]
+WIDTHS = [100, 128, 200, 256, 1536, 1537, 2049, 5000, 16384]
+
+
+@pytest.fixture(scope="module", autouse=True)
+def ops():
+    import paper_2509_24899_b200 as pkg
+    yield pkg
+    torch.cuda.synchronize()
+    assert pkg.fp8_last_status() == 0
+
+
+def randn(*shape, dtype=BF16, seed=0, gain=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return (torch.randn(shape, generator=g, device="cuda") * gain).to(dtype)
+
+
+def close_bf16(y, ref):
+    """Half a spacing of bf16 (2^-8 relative; 2^-134 below its normal numbers) and the slack, which is as much of fp32's smallest normal number."""
+    off = (y.to(R.F64) - ref).abs()
+    assert bool((off <= ref.abs() * (2.0 ** -8 + SLACK) + 2.0 ** -134).all()), float((off / ref.abs().clamp(min=1e-38)).max())
+
+
+def check_norm(ops, x, w, r, eps=1e-6):
+    """Both forms of the output, and the residual."""
+    y, t = R.norm64(x, w, r, eps)
+    assert bool(t.isfinite().all()) and bool(y.isfinite().all())
+    got = ops.rms_norm(x, w, residual=r, eps=eps)
+    close_bf16(R.rows_of(got if r is None else got[0]), y)
+    if r is not None:
+        assert torch.equal(got[1], (x.float() + r.float()).to(r.dtype))
+    got = ops.rms_norm(x, w, residual=r, eps=eps, fp8=True)
+    R.check_form(got if r is None else got[0], y, slack=SLACK)
+
+
+def rows_with(cols, x, residual, gains, rows=13):
+    """x (and a residual): ordinary rows, and from row 2 on every second one times one of the gains."""
+    xv = randn(rows, cols, dtype=F32, seed=cols).clamp(-4, 4)
+    rv = None if residual is None else randn(rows, cols, dtype=F32, seed=cols + 1).clamp(-4, 4)
+    for i, gain in enumerate(gains):
+        xv[2 + 2 * i] *= gain
+        if rv is not None:
+            rv[2 + 2 * i] *= gain
+    return xv.to(x), rv if rv is None else rv.to(residual)
+
+
+# ------------------------------------------------------------------------------------------------ large values
+@pytest.mark.parametrize("cols", WIDTHS)
+@pytest.mark.parametrize("x,residual", KINDS)
+def test_norm_of_rows_up_to_the_largest_numbers(ops, cols, x, residual):
+    """Rows whose largest values are near fp32's largest (4 + 4 times 4e37 of 3.4e38), without weights and with ones up to 1."""
+    xv, r = rows_with(cols, x, residual, (1e19, 1e30, 1e36, 1e37, 4e37))
+    check_norm(ops, xv, None, r)
+    check_norm(ops, xv, torch.linspace(-1, 1, cols, device="cuda").to(BF16), r)
+    # every value the same, the largest that the type has
+    top = torch.full((3, cols), torch.finfo(x).max, dtype=x, device="cuda")
+    check_norm(ops, top, None, None)
+
+
+@pytest.mark.parametrize("cols", [100, 200, 1536, 1537, 5000])
+@pytest.mark.parametrize("x,residual", KINDS)
+def test_norm_goes_by_the_sum_as_it_was_added(ops, cols, x, residual):
+    """Rows whose squares fp32 does not hold: their mean is that of the unrounded sum for every type of the residual, as in ordinary rows."""
+    xv, r = rows_with(cols, x, residual, (1e19, 3e19, 1e25, 1e30, 1e35))
+    check_norm(ops, xv, randn(cols, seed=2).clamp(-1, 1), r)
