@@ -202,19 +202,24 @@ constexpr float MOST = 3.402823466e38f;
 // NORM: y = t * rsqrt(mean t^2 + eps) * w, else y = x.  R: the residual's type (void: none).  FP8: y in 8-bit form, else in bf16.  LANES: of a row
 // in a warp (8, 16: with one vector).
 //
-// The weights multiply t while the sum of squares is on its way between the lanes, and so do the blocks' largest values go round: both turns of a row's reductions
-// overlap, and the row's scale enters last.  What counts is the number of instructions: with 8 columns a lane, one value an instruction and the formula's order a row of 1536
-// columns with a residual in bf16 took 131 us for 32760 rows; in pairs, weights ahead of the scale, 62 us; with 16 columns a lane, whose loads are half as many and whose
-// scales are a third as much work, 56 us (6.3 TB/s).  Without a residual 54, 38 and 29 us (5.2 TB/s), the last with CTAs that go on; the 8-bit form alone 34, 26 and 25 us
-// (6.1 TB/s).  Rows further ahead, as asynchronous copies into shared memory, did not help there: 35 and 27 us with four rows under way, for the instructions that it takes.
+// The order is the formula's: sum of squares, the row's scale times t, the weights, the blocks' largest values.  (Weights ahead of the scale let the block's reductions run beside
+// the row's, which gained 0.4 us of 29, 0.3 of 56 and nothing of 82; but t * w may lie beyond fp32 where the normed value times w does not.)  What counts is the number of
+// instructions: with 8 columns a lane, one value an instruction, a row of 1536 columns with a residual in bf16 took 131 us for 32760 rows, in pairs 62 us; with 16 columns a lane, whose
+// loads are half as many and whose scales are a third as much work, 56 us (6.3 TB/s).  Without a residual 54, 38 and 29 us (5.1 TB/s), the last with CTAs that go on; the 8-bit form
+// alone 34, 26 and 25 us (6.1 TB/s; 29 us where the largest values of one vector wait for those of the vector before).  Rows further ahead, as asynchronous copies into shared memory,
+// did not help there: 35 and 27 us with four rows under way, for the instructions that it takes.
 // With x in bf16 and no residual a CTA goes on from row to row: its weights stay in shared memory, and a row's loads are under way while the one before it is
 // worked on.  (With a residual or in fp32 there is enough under way without that, and no room for it.)  Two CTAs an SM.
 template <typename X, typename R, int MOVE> constexpr bool goes_on = sizeof(X) == 2 && __is_same(R, void) && MOVE != MOVE_ELEMENT;
 
-__host__ __device__ constexpr int ctas_of_sm(bool goes_on, int move, int nv) { return goes_on ? 2 : move != MOVE_ELEMENT ? 1 : nv == 1 ? 4 : nv == 2 ? 2 : 1; }
+// x_bytes: of an element of x.  In bf16 beside a residual three vectors fit 128 registers, two CTAs (32760 x 1536 with a residual in fp32 82 us; left to itself the compiler takes 130, and one CTA
+// 103 us).
+__host__ __device__ constexpr int ctas_of_sm(bool goes_on, int move, int nv, int x_bytes) {
+  return goes_on ? 2 : move != MOVE_ELEMENT ? (x_bytes == 2 && nv <= 3 ? 2 : 1) : nv == 1 ? 4 : nv == 2 ? 2 : 1;
+}
 
 template <typename X, typename R, bool NORM, bool FP8, int MOVE, int NV, int LANES>
-__global__ void __launch_bounds__(THREADS, ctas_of_sm(goes_on<X, R, MOVE>, MOVE, NV)) norm_kernel(const __grid_constant__ NormParams p) {
+__global__ void __launch_bounds__(THREADS, ctas_of_sm(goes_on<X, R, MOVE>, MOVE, NV, (int)sizeof(X))) norm_kernel(const __grid_constant__ NormParams p) {
   griddep_launch();
   __shared__ float part[THREADS / 32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -279,24 +284,49 @@ __global__ void __launch_bounds__(THREADS, ctas_of_sm(goes_on<X, R, MOVE>, MOVE,
     }
     if constexpr (GOES_ON) fetch_x(row + (long long)gridDim.x * per);
   }
-  float2 sum2 = make_float2(0.f, 0.f);
-  float small = 0.f;
   if constexpr (NORM) {
+    float2 sum2 = make_float2(0.f, 0.f);
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum2 = fma2(v[j][i], v[j][i], sum2);
-    // 2^-160 of it, for rows whose squares fp32 does not hold (|t| from 2^64 / sqrt(cols) on).  That there are such rows costs the others up to 2 us of 30.
-    if (!(sum2.x + sum2.y <= MOST)) {
-      float2 s = make_float2(0.f, 0.f);
+    // over the row's lanes and warps
+    auto row_sum = [&](float sum) {
+#pragma unroll
+      for (int o = LANES / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      if constexpr (LANES == 32)
+        if (p.W > 1) {                                        // the same for every thread of the launch
+          if (lane == 0) part[warp] = sum;
+          __syncthreads();
+          sum = 0.f;
+          for (int i = 0; i < p.W; ++i) sum += part[min(slot * p.W + i, THREADS / 32 - 1)];
+        }
+      return sum;
+    };
+    const float sum = row_sum(sum2.x + sum2.y);
+    float scale = rsqrtf(sum / (float)p.cols + p.eps);
+    // rows whose squares fp32 does not hold (|t| from 2^64 / sqrt(cols) on): 2^-160 of the sum
+    const bool over = !(sum <= MOST);
+    bool again = over;                                        // (the sum of all lanes of a row is one value)
+    if constexpr (LANES < 32) again = __any_sync(0xffffffffu, over);
+    if constexpr (LANES == 32)
+      if (p.W > 1) again = __syncthreads_or(over);            // (behind it the sums have been read)
+    if (again) {
+      float2 s2 = make_float2(0.f, 0.f);
 #pragma unroll
       for (int j = 0; j < NV; ++j)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) { const float2 u = mul2(v[j][i], make_float2(DOWN, DOWN)); s = fma2(u, u, s); }
-      small = s.x + s.y;
-    } else {
-      small = (sum2.x + sum2.y) * DOWN * DOWN;
+        for (int i = 0; i < 8; ++i) { const float2 u = mul2(v[j][i], make_float2(DOWN, DOWN)); s2 = fma2(u, u, s2); }
+      const float s = row_sum(s2.x + s2.y);
+      if constexpr (LANES == 32)
+        if (p.W > 1) __syncthreads();
+      if (over) scale = rsqrtf(s / (float)p.cols + p.eps * DOWN * DOWN) * DOWN;
     }
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[j][i] = mul2(v[j][i], make_float2(scale, scale));
+    // the weights last, as in the formula: t * w may lie beyond fp32 where the normed value times w does not
     if (early) {
 #pragma unroll
       for (int j = 0; j < NV; ++j) scale_values<__nv_bfloat16, MOVE>(w16[j], v[j]);
@@ -324,9 +354,14 @@ __global__ void __launch_bounds__(THREADS, ctas_of_sm(goes_on<X, R, MOVE>, MOVE,
       }
     }
   }
-  constexpr int BLOCKS = MOVE == MOVE_ELEMENT ? 4 : 1;         // of a vector whose largest values a lane has
-  uint32_t top[NV][BLOCKS];
-  if constexpr (FP8) {
+  if constexpr (!FP8) {
+    const long long wr = p.o.row(r);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) store16<__nv_bfloat16, MOVE>(p.o, wr, c0 + j * 512, cols, v[j]);
+  } else {
+    uint8_t* q = p.q + (long long)r * p.pitch;
+    constexpr int BLOCKS = MOVE == MOVE_ELEMENT ? 4 : 1;      // of a vector whose largest values a lane has
+    uint32_t top[NV][BLOCKS];                                 // of all vectors at once: their turns between the lanes overlap
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       if constexpr (MOVE == MOVE_ELEMENT) {
@@ -336,46 +371,6 @@ __global__ void __launch_bounds__(THREADS, ctas_of_sm(goes_on<X, R, MOVE>, MOVE,
         top[j][0] = block_max(v[j]);
       }
     }
-  }
-  float scale = 1.f;
-  if constexpr (NORM) {
-    // over the row's lanes and warps
-    auto row_sum = [&](float sum) {
-#pragma unroll
-      for (int o = LANES / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-      if constexpr (LANES == 32)
-        if (p.W > 1) {                                        // the same for every thread of the launch
-          if (lane == 0) part[warp] = sum;
-          __syncthreads();
-          sum = 0.f;
-          for (int i = 0; i < p.W; ++i) sum += part[min(slot * p.W + i, THREADS / 32 - 1)];
-        }
-      return sum;
-    };
-    const float sum = row_sum(sum2.x + sum2.y);
-    scale = rsqrtf(sum / (float)p.cols + p.eps);
-    const bool over = !(sum <= MOST);
-    bool again = over;                                        // (the sum of all lanes of a row is one value)
-    if constexpr (LANES < 32) again = __any_sync(0xffffffffu, over);
-    if constexpr (LANES == 32)
-      if (p.W > 1) again = __syncthreads_or(over);            // (behind it the sums have been read)
-    if (again) {
-      const float s = row_sum(small);
-      if constexpr (LANES == 32)
-        if (p.W > 1) __syncthreads();
-      if (over) scale = rsqrtf(s / (float)p.cols + p.eps * DOWN * DOWN) * DOWN;
-    }
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[j][i] = mul2(v[j][i], make_float2(scale, scale));
-  }
-  if constexpr (!FP8) {
-    const long long wr = p.o.row(r);
-#pragma unroll
-    for (int j = 0; j < NV; ++j) store16<__nv_bfloat16, MOVE>(p.o, wr, c0 + j * 512, cols, v[j]);
-  } else {
-    uint8_t* q = p.q + (long long)r * p.pitch;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int c = c0 + j * 512, group = first / 512 + j;
@@ -383,7 +378,6 @@ __global__ void __launch_bounds__(THREADS, ctas_of_sm(goes_on<X, R, MOVE>, MOVE,
       float inv[BLOCKS];
 #pragma unroll
       for (int b = 0; b < BLOCKS; ++b) {
-        if constexpr (NORM) top[j][b] = __float_as_uint(__uint_as_float(top[j][b]) * scale);    // as the largest of the products: rounding keeps the order
         byte[b] = scale_byte(top[j][b]);
         inv[b] = inverse_scale(byte[b]);
       }

@@ -75,3 +75,17 @@ def test_norm_goes_by_the_sum_as_it_was_added(ops, cols, x, residual):
     """Rows whose squares fp32 does not hold: their mean is that of the unrounded sum for every type of the residual, as in ordinary rows."""
     xv, r = rows_with(cols, x, residual, (1e19, 3e19, 1e25, 1e30, 1e35))
     check_norm(ops, xv, randn(cols, seed=2).clamp(-1, 1), r)
+
+
+# ------------------------------------------------------------------------------------------------ weights
+@pytest.mark.parametrize("cols", WIDTHS)
+@pytest.mark.parametrize("x,residual", KINDS)
+@pytest.mark.parametrize("wd", [BF16, F32])
+def test_norm_with_large_and_small_weights(ops, cols, x, residual, wd):
+    """Values times weights that lie beyond fp32's range on either side, and normed values times weights that do not."""
+    xv, r = rows_with(cols, x, residual, (1e10, 1e19, 1e30, 1e36, 4e37))
+    w = torch.exp(torch.linspace(-30, 30, cols, device="cuda")).to(wd)
+    check_norm(ops, xv, w, r)
+    check_norm(ops, xv, w.flip(0) * 1e20, r)
+    xv, r = rows_with(cols, x, residual, (1e-4, 1e-6, 1e-8, 1e-10, 1e-12))
+    check_norm(ops, xv, w * 1e-24, r, eps=1e-12)
