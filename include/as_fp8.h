@@ -95,7 +95,8 @@ typedef struct {
 } as_matmul_fp8_t;
 
 /* t = x + residual in fp32; y = t * rsqrt(mean(t^2) + eps) * weight from the unrounded t; t is rounded once into residual_out, y
- * once into out or out8.  rows == 0 launches nothing. */
+ * once into out or out8.  Holds for every finite t and every y within the output's range, whatever their squares or t * weight are in fp32; a row of
+ * zeros with eps == 0 is NaN, as in the formula.  rows == 0 launches nothing. */
 AS_API as_status_t as_rms_norm(const as_rms_norm_t* args, void* cuda_stream);
 
 /* The 8-bit form of x. */

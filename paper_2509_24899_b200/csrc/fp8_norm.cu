@@ -197,6 +197,8 @@ AS_DEV uint32_t block_max(const float2 (&f)[8]) {
 AS_DEV uint32_t block_max_elements(const float2 (&f)[8], int b) { return __reduce_max_sync(0xffffffffu, __float_as_uint(max_abs2(f[2 * b], max_abs2(f[2 * b + 1], 0.f)))); }
 
 constexpr float DOWN = 8.271806126e-25f;       // 2^-80: |t| below 2^128 becomes 2^48 at most, and the sum of 16384 squares 2^110
+constexpr float UP = 1.267650600e30f;          // 2^100: fp32's smallest number becomes 2^-49, and what LEAST lets through 2^57 at most
+constexpr float LEAST = 7.888609052e-31f;      // 2^-100: squares that fp32 rounds below its normal numbers are 2^-150 off, 2^-50 of it
 constexpr float MOST = 3.402823466e38f;
 
 // NORM: y = t * rsqrt(mean t^2 + eps) * w, else y = x.  R: the residual's type (void: none).  FP8: y in 8-bit form, else in bf16.  LANES: of a row
@@ -304,23 +306,32 @@ __global__ void __launch_bounds__(THREADS, ctas_of_sm(goes_on<X, R, MOVE>, MOVE,
       return sum;
     };
     const float sum = row_sum(sum2.x + sum2.y);
-    float scale = rsqrtf(sum / (float)p.cols + p.eps);
-    // rows whose squares fp32 does not hold (|t| from 2^64 / sqrt(cols) on): 2^-160 of the sum
-    const bool over = !(sum <= MOST);
-    bool again = over;                                        // (the sum of all lanes of a row is one value)
-    if constexpr (LANES < 32) again = __any_sync(0xffffffffu, over);
+    const float mean = sum / (float)p.cols + p.eps;
+    float scale = rsqrtf(mean);
+    // Rows whose squares fp32 does not hold (|t| from 2^64 / sqrt(cols) on), or whose squares vanish with an eps that does as well, are summed again times a power of two.
+    const bool over = !(sum <= MOST), under = live && mean < LEAST;
+    bool again = over || under;                               // (the sum of all lanes of a row is one value)
+    if constexpr (LANES < 32) again = __any_sync(0xffffffffu, again);
     if constexpr (LANES == 32)
-      if (p.W > 1) again = __syncthreads_or(over);            // (behind it the sums have been read)
+      if (p.W > 1) again = __syncthreads_or(again);           // (behind it the sums have been read)
     if (again) {
+      const float factor = over ? DOWN : UP;
       float2 s2 = make_float2(0.f, 0.f);
 #pragma unroll
       for (int j = 0; j < NV; ++j)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) { const float2 u = mul2(v[j][i], make_float2(DOWN, DOWN)); s2 = fma2(u, u, s2); }
-      const float s = row_sum(s2.x + s2.y);
+        for (int i = 0; i < 8; ++i) { const float2 u = mul2(v[j][i], make_float2(factor, factor)); s2 = fma2(u, u, s2); }
+      const float s = row_sum(s2.x + s2.y), once = rsqrtf(s / (float)p.cols + p.eps * factor * factor);
       if constexpr (LANES == 32)
         if (p.W > 1) __syncthreads();
-      if (over) scale = rsqrtf(s / (float)p.cols + p.eps * DOWN * DOWN) * DOWN;
+      if (over) scale = once * DOWN;
+      if (under) {                                            // the row's scale may lie beyond fp32: t takes the factor first
+        scale = once;
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[j][i] = mul2(v[j][i], make_float2(UP, UP));
+      }
     }
 #pragma unroll
     for (int j = 0; j < NV; ++j)

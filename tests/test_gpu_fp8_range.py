@@ -89,3 +89,16 @@ def test_norm_with_large_and_small_weights(ops, cols, x, residual, wd):
     check_norm(ops, xv, w.flip(0) * 1e20, r)
     xv, r = rows_with(cols, x, residual, (1e-4, 1e-6, 1e-8, 1e-10, 1e-12))
     check_norm(ops, xv, w * 1e-24, r, eps=1e-12)
+
+
+# ------------------------------------------------------------------------------------------------ small values
+@pytest.mark.parametrize("cols", WIDTHS)
+@pytest.mark.parametrize("x,residual", KINDS)
+@pytest.mark.parametrize("eps", [0.0, 1e-38, 1e-30, 1e-20])
+def test_norm_of_rows_whose_squares_are_too_small(ops, cols, x, residual, eps):
+    """Rows whose squares vanish in fp32 with an eps that does as well, or nearly."""
+    xv, r = rows_with(cols, x, residual, (1e-12, 1e-16, 1e-20, 1e-26, 1e-33))
+    check_norm(ops, xv, None, r, eps=eps)
+    check_norm(ops, xv, randn(cols, seed=2), r, eps=eps)
+    # every value the same, the smallest that the type has
+    check_norm(ops, torch.full((3, cols), torch.finfo(x).smallest_normal * torch.finfo(x).eps, dtype=x, device="cuda"), None, None, eps=eps)
