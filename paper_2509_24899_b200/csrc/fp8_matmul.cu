@@ -501,8 +501,15 @@ AS_DEV void few_copy4(uint32_t dst, const void* src) { asm volatile("cp.async.ca
 AS_DEV void few_read(uint32_t at, uint32_t (&r)[4]) {
   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
 }
-// 2^(e - 127) of a scale byte: exact for 0 (a subnormal number), NaN for 255.
-AS_DEV float few_scale(uint32_t e) { return __uint_as_float(e == 0u ? 0x00400000u : e == 255u ? 0x7fc00000u : e << 23); }
+// 2^(e - 127) of a scale byte (NaN for 255) as two factors of about half its exponent.  A block's sum is multiplied by the first factors of both matrices' scales and then by the
+// second ones: as one scale after the other it would leave fp32's range where the product of both scales does not.  The halves that are rounded down take 2^-63 of w's scale
+// and 2^-64 of a's, the others 2^-64 and 2^-63, so that a product of two lies between 2^-127 and 2^127 and is exact; the second is at least the first, so a sum
+// between them overflows, or loses bits, only where the result does.
+struct FewScale { float first, second; };
+template <int OF_W> AS_DEV FewScale few_scale(uint32_t e) {
+  const uint32_t h = e >> 1;
+  return {__uint_as_float(e == 255u ? 0x7fc00000u : (h + 63u + OF_W) << 23), __uint_as_float((e - h + 64u - OF_W) << 23)};
+}
 
 template <int NT>
 __global__ void __launch_bounds__(FEW_WARPS * 32, 1) few_rows_kernel(const __grid_constant__ FewParams p) {
@@ -554,10 +561,10 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 1) few_rows_kernel(const __gri
       __syncwarp();                                                   // the other lanes' scales have come as well
       const uint32_t at = mine + take * SLOT, own = at + lane * 16;
       if (++take == AHEAD) take = 0;
-      auto scale_of = [&](int i) {
+      auto byte_of = [&](int i) {
         uint32_t e;
         asm volatile("ld.shared.u8 %0, [%1];" : "=r"(e) : "r"(at + SCALES + i * 4 + k % 4) : "memory");
-        return few_scale(e);
+        return e;
       };
       uint32_t w[2][2][4];
 #pragma unroll
@@ -565,13 +572,13 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 1) few_rows_kernel(const __gri
         few_read(own + i * 512, w[0][i]);
         few_read(own + (2 + i) * 512, w[1][i]);
       }
-      const float f0 = scale_of(g), f1 = scale_of(8 + g);             // rows g and g + 8 of w; of a: rows 2 q and 2 q + 1 of each tile
+      const FewScale fw[2] = {few_scale<1>(byte_of(g)), few_scale<1>(byte_of(8 + g))};      // rows g and g + 8 of w; of a: rows 2 q and 2 q + 1 of each tile
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         uint32_t a[2][4];
 #pragma unroll
         for (int i = 0; i < 2; ++i) few_read(own + (4 + 2 * t + i) * 512, a[i]);
-        const float fa[2] = {scale_of(16 + 8 * t + 2 * q), scale_of(17 + 8 * t + 2 * q)};
+        const FewScale fa[2] = {few_scale<0>(byte_of(16 + 8 * t + 2 * q)), few_scale<0>(byte_of(17 + 8 * t + 2 * q))};
         float d[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -580,7 +587,7 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 1) few_rows_kernel(const __gri
                        : "r"(w[0][i / 2][2 * (i % 2)]), "r"(w[1][i / 2][2 * (i % 2)]), "r"(w[0][i / 2][2 * (i % 2) + 1]), "r"(w[1][i / 2][2 * (i % 2) + 1]),
                          "r"(a[i / 2][2 * (i % 2)]), "r"(a[i / 2][2 * (i % 2) + 1]));
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[t][j] = fmaf(d[j] * (j < 2 ? f0 : f1), fa[j % 2], acc[t][j]);
+        for (int j = 0; j < 4; ++j) acc[t][j] = fmaf(d[j] * (fw[j / 2].first * fa[j % 2].first), fw[j / 2].second * fa[j % 2].second, acc[t][j]);
       }
     }
 #pragma unroll

@@ -102,3 +102,27 @@ def test_norm_of_rows_whose_squares_are_too_small(ops, cols, x, residual, eps):
     check_norm(ops, xv, randn(cols, seed=2), r, eps=eps)
     # every value the same, the smallest that the type has
     check_norm(ops, torch.full((3, cols), torch.finfo(x).smallest_normal * torch.finfo(x).eps, dtype=x, device="cuda"), None, None, eps=eps)
+
+
+# ------------------------------------------------------------------------------------------------ scales of a product
+@pytest.mark.parametrize("M", [3, 11, 150, 700])
+@pytest.mark.parametrize("ea,ew", [((0, 40), (214, 254)), ((214, 254), (0, 40)), ((0, 3), (252, 254)), ((127, 254), (0, 127)), ((230, 250), (4, 24)), ((0, 10), (120, 254)),
+                                   ((67, 127), (67, 127))])
+def test_matmul_of_opposed_scales(ops, M, ea, ew):
+    """Scales each of which takes a block's sum beyond fp32's range, on either side, while both together do not."""
+    K, N = 1100, 140
+    a, w = R.pair_of(randn(M, K, dtype=R.F64, seed=5)), R.pair_of(randn(N, K, dtype=R.F64, seed=6), 128)
+    g = torch.Generator(device="cuda").manual_seed(9)
+    for pair, (lo, hi) in ((a, ea), (w, ew)):
+        pair[1].copy_(torch.randint(lo, hi + 1, pair[1].shape, generator=g, device="cuda").to(torch.uint8))
+    # no sum may pass bf16's largest number: block by block, e_a + e_w of at most 254 + 100
+    e = torch.minimum(a[1].amax(1, keepdim=True).to(torch.int64) + w[1].amax(1, keepdim=True).to(torch.int64), torch.full((), 354, device="cuda"))
+    for pair, other in ((a, w), (w, a)):
+        pair[1].copy_(torch.minimum(pair[1].to(torch.int64), e - other[1].amax(1, keepdim=True).to(torch.int64)).to(torch.uint8))
+    av, wv = R.value64(a), R.value64(w)
+    ref, size = av @ wv.T, av.abs() @ wv.abs().T
+    # as check_matmul, and half a spacing of bf16 and of fp32 for each block below their normal numbers
+    tol = ref.abs() * 2.0 ** -8 + size * 2.0 ** -23 * 2 * (K / 32 + 2) + 2.0 ** -134 + 9 * 2.0 ** -149
+    assert float(size.max()) < 3e38
+    off = (ops.matmul_fp8(a, w).to(R.F64) - ref).abs()
+    assert bool((off <= tol).all()), float((off / tol).max())
