@@ -113,6 +113,11 @@ AS_API as_status_t as_fp8_destroy(as_fp8_context_t ctx);
  * AS_ERR_CUDA. */
 AS_API as_status_t as_fp8_last_status(as_fp8_context_t ctx, void* cuda_stream);
 
+/* Test aid: enqueues a one-CTA kernel whose bounded wait, the one that the products use, runs out after about limit_cycles SM clocks
+ * (1 .. 1e8) and sets the context's status word as a time-out inside a product does; no copy and no tensor-core operation is in
+ * flight.  Like the products it lets the launch behind it set up before it waits. */
+AS_API as_status_t as_fp8_debug_expire_wait(as_fp8_context_t ctx, int64_t limit_cycles, void* cuda_stream);
+
 /* out[m, n] = sum_k a[m, k] w[n, k] + bias[n], products of the 8-bit values times both scales, summed in fp32, rounded once to
  * bf16.  A scale byte of 255 makes the row's (column's) results NaN.  rows == 0 launches nothing. */
 AS_API as_status_t as_matmul_fp8(as_fp8_context_t ctx, const as_matmul_fp8_t* args, void* cuda_stream);

@@ -120,6 +120,7 @@ def lib() -> C.CDLL:
             "as_fp8_create": [C.POINTER(H)],
             "as_fp8_destroy": [H],
             "as_fp8_last_status": [H, C.c_void_p],
+            "as_fp8_debug_expire_wait": [H, C.c_int64, C.c_void_p],
         }
         for name, args in sigs.items():
             fn = getattr(L, name)
@@ -356,3 +357,8 @@ def as_fp8_destroy(ctx) -> None:
 def as_fp8_last_status(ctx, stream_ptr) -> int:
     """Returns the status code instead of raising, as as_hybrid_attn_last_status."""
     return lib().as_fp8_last_status(ctx, stream_ptr or None)
+
+
+def as_fp8_debug_expire_wait(ctx, limit_cycles: int, stream_ptr) -> None:
+    """Test aid: a bounded wait that runs out, see include/as_fp8.h."""
+    _check(lib().as_fp8_debug_expire_wait(ctx, int(limit_cycles), stream_ptr or None), "as_fp8_debug_expire_wait")

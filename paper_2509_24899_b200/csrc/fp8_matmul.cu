@@ -717,6 +717,14 @@ extern "C" as_status_t as_fp8_last_status(as_fp8_context_t h, void* cuda_stream)
   return AS_ERR_DEVICE_TIMEOUT;
 }
 
+extern "C" as_status_t as_fp8_debug_expire_wait(as_fp8_context_t h, int64_t limit_cycles, void* cuda_stream) {
+  int dev = 0;
+  if (h == nullptr || limit_cycles < 1 || limit_cycles > 100000000) return AS_ERR_INVALID_ARG;       // at most about 50 ms
+  if (cudaGetDevice(&dev) != cudaSuccess) return AS_ERR_CUDA;
+  if (dev != h->device) return AS_ERR_INVALID_ARG;
+  return as_tensor_expire_wait(h->status, limit_cycles, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? AS_OK : AS_ERR_CUDA;
+}
+
 extern "C" as_status_t as_matmul_fp8(as_fp8_context_t h, const as_matmul_fp8_t* a, void* cuda_stream) {
   if (h == nullptr || a == nullptr || a->struct_size != sizeof(as_matmul_fp8_t)) return AS_ERR_INVALID_ARG;
   if (a->cols < 1 || a->cols > (1 << 20) || a->rows < 0 || a->rows > (1ll << 30) || a->out_cols < 1 || a->out_cols > (1ll << 24)) return AS_ERR_INVALID_ARG;

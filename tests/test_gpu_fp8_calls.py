@@ -41,3 +41,54 @@ def test_what_is_no_pair_is_refused(ops):
     for bad in (None, 3):
         with pytest.raises(TypeError):
             ops.matmul_fp8(bad, a)
+
+
+# ------------------------------------------------------------------------------------------------ status
+def product_of(a, w, out):
+    """as_matmul_fp8_t of a w^T into rows."""
+    import ctypes as C
+
+    from paper_2509_24899_b200 import binding as b
+    matrix = [b.as_fp8_matrix_t(m.data.data_ptr(), m.data.stride(0), m.scales.data_ptr(), m.data.shape[0]) for m in (a, w)]
+    return b.as_matmul_fp8_t(C.sizeof(b.as_matmul_fp8_t), a.data.shape[1], a.data.shape[0], w.data.shape[0], *matrix, None,
+                             b.as_rows_t(out.data_ptr(), b.AS_DTYPE_BF16, out.shape[1], out.shape[0], 0, 0, out.stride(0)))
+
+
+@pytest.fixture()
+def context():
+    from paper_2509_24899_b200 import binding
+    ctx = binding.as_fp8_create()
+    yield ctx
+    torch.cuda.synchronize()
+    binding.as_fp8_destroy(ctx)
+
+
+@pytest.mark.parametrize("M,N,K", [(2, 300, 1000), (200, 1536, 6144), (700, 1000, 512), (5000, 1536, 512)])
+def test_a_wait_that_runs_out_is_reported_once_and_the_context_stays_usable(ops, context, M, N, K):
+    """The time-out in its safe form: a kernel of its own whose wait nothing feeds, on the context's status word.  Products behind it on the stream, before and after
+    the word has been read, are right."""
+    from paper_2509_24899_b200 import binding
+    a, w = ops.quantize_fp8(randn(M, K, seed=1)), ops.quantize_fp8(randn(N, K, seed=2, gain=0.05), block_rows=128)
+    want = ops.matmul_fp8(a, w)
+    out = [torch.full((M, N), 7.0, dtype=BF16, device="cuda") for _ in range(3)]
+    st = torch.cuda.current_stream().cuda_stream
+    assert binding.as_fp8_last_status(context, st) == 0
+    binding.as_matmul_fp8(context, product_of(a, w, out[0]), st)
+    assert binding.as_fp8_last_status(context, st) == 0
+    binding.as_fp8_debug_expire_wait(context, 2_000_000, st)                   # about a millisecond
+    binding.as_matmul_fp8(context, product_of(a, w, out[1]), st)
+    assert binding.as_fp8_last_status(context, st) == binding.AS_ERR_DEVICE_TIMEOUT
+    assert binding.as_fp8_last_status(context, st) == 0                        # read and cleared
+    binding.as_matmul_fp8(context, product_of(a, w, out[2]), st)
+    assert binding.as_fp8_last_status(context, st) == 0
+    assert all(torch.equal(o, want) for o in out)
+    assert ops.fp8_last_status() == 0                                          # another context's word
+
+
+def test_expire_wait_refuses(ops, context):
+    from paper_2509_24899_b200 import binding
+    for ctx, limit in ((None, 1000), (context, 0), (context, -1), (context, 100_000_001)):
+        with pytest.raises(ops.AsError) as e:
+            binding.as_fp8_debug_expire_wait(ctx, limit, 0)
+        assert e.value.status == binding.AS_ERR_INVALID_ARG
+    assert binding.as_fp8_last_status(context, 0) == 0
