@@ -15,6 +15,7 @@
 //
 // Few tiles with long columns: a cluster of single CTAs shares a tile's columns (PARTS).  Few rows of a: few_rows_kernel, further down.
 #include <algorithm>
+#include <mutex>
 #include <new>
 
 #include "fp8_common.cuh"
@@ -662,12 +663,17 @@ cudaError_t launch(const CUtensorMap& ma, const CUtensorMap& mw, const CUtensorM
   return cudaLaunchKernelEx(&cfg, matmul_kernel<CG, PARTS>, ma, mw, mo, p);
 }
 
+// The status word is read and cleared in one step: a bit that a product on another stream raises stands before it or after it.
+constexpr int TAKEN = 32;
+__global__ void take_status_kernel(uint32_t* status) { status[TAKEN] = atomicExch(status, 0u); }
+
 }  // namespace
 
 struct as_fp8_context_s {
   int device = -1, sms = 0;
   int clusters[MAX_PARTS + 1] = {};          // of so many CTAs that the device holds at once
   uint32_t* status = nullptr;
+  std::mutex reading;                        // of the word behind the status word, where a read leaves what it took
 };
 
 extern "C" as_status_t as_fp8_create(as_fp8_context_t* out) {
@@ -711,10 +717,11 @@ extern "C" as_status_t as_fp8_last_status(as_fp8_context_t h, void* cuda_stream)
   if (h == nullptr) return AS_ERR_INVALID_ARG;
   const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   uint32_t word = 0;
-  if (cudaMemcpyAsync(&word, h->status, 4, cudaMemcpyDeviceToHost, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) return AS_ERR_CUDA;
-  if (word == 0) return AS_OK;
-  if (cudaMemsetAsync(h->status, 0, 4, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) return AS_ERR_CUDA;
-  return AS_ERR_DEVICE_TIMEOUT;
+  std::lock_guard<std::mutex> hold(h->reading);
+  take_status_kernel<<<1, 1, 0, st>>>(h->status);
+  if (cudaGetLastError() != cudaSuccess || cudaMemcpyAsync(&word, h->status + TAKEN, 4, cudaMemcpyDeviceToHost, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess)
+    return AS_ERR_CUDA;
+  return word == 0 ? AS_OK : AS_ERR_DEVICE_TIMEOUT;
 }
 
 extern "C" as_status_t as_fp8_debug_expire_wait(as_fp8_context_t h, int64_t limit_cycles, void* cuda_stream) {

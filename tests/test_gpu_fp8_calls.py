@@ -92,3 +92,36 @@ def test_expire_wait_refuses(ops, context):
             binding.as_fp8_debug_expire_wait(ctx, limit, 0)
         assert e.value.status == binding.AS_ERR_INVALID_ARG
     assert binding.as_fp8_last_status(context, 0) == 0
+
+
+def test_status_read_from_two_streams(ops, context):
+    """Reads on one stream while waits run out on another: every time-out is reported, by a read under way or by the next one (by both, where the threads of the kernel that
+    waits give up one after the other), and none when all of them are over."""
+    import threading
+
+    from paper_2509_24899_b200 import binding
+    side, reader = torch.cuda.Stream(), torch.cuda.Stream()
+    timeouts, stop = [], threading.Event()
+
+    def read():
+        while not stop.is_set():
+            timeouts.append(binding.as_fp8_last_status(context, reader.cuda_stream) == binding.AS_ERR_DEVICE_TIMEOUT)
+
+    thread = threading.Thread(target=read)
+    thread.start()
+    raised = 0
+    try:
+        for _ in range(100):
+            before = sum(timeouts)
+            binding.as_fp8_debug_expire_wait(context, 2000, side.cuda_stream)
+            raised += 1
+            side.synchronize()
+            seen = binding.as_fp8_last_status(context, side.cuda_stream) == binding.AS_ERR_DEVICE_TIMEOUT
+            n = len(timeouts)
+            while len(timeouts) < n + 2 and thread.is_alive():
+                pass
+            assert seen + sum(timeouts) - before >= 1
+    finally:
+        stop.set()
+        thread.join()
+    assert raised == 100 and binding.as_fp8_last_status(context, 0) == 0
