@@ -34,6 +34,9 @@ struct Rows {
 };
 
 // ---------------------------------------------------------------- host: checks, and the form above
+// What a call returns when one of CUDA's has failed; the error does not stay behind for the library's next launch, which would report it as its own.
+inline as_status_t failed(as_status_t status = AS_ERR_CUDA) { cudaGetLastError(); return status; }
+
 inline bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
 inline bool rows_ok(const as_rows_t& x, long long rows, long long cols) {

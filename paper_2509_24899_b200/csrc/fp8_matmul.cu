@@ -681,12 +681,12 @@ extern "C" as_status_t as_fp8_create(as_fp8_context_t* out) {
   int dev = 0, major = 0, sms = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
       cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-    return AS_ERR_CUDA;
+    return failed();
   if (major != 10) return AS_ERR_ARCH;
   if (as_tensor_init() != cudaSuccess || as_tc::opt_in_smem(matmul_kernel<1, false>, SMEM_MAX) != cudaSuccess || as_tc::opt_in_smem(matmul_kernel<2, false>, SMEM_MAX) != cudaSuccess ||
       as_tc::opt_in_smem(matmul_kernel<1, true>, SMEM_MAX) != cudaSuccess ||
       as_tc::opt_in_smem(few_rows_kernel<1>, few_smem(1)) != cudaSuccess || as_tc::opt_in_smem(few_rows_kernel<2>, few_smem(2)) != cudaSuccess)
-    return AS_ERR_CUDA;
+    return failed();
   as_fp8_context_s* h = new (std::nothrow) as_fp8_context_s;
   if (h == nullptr) return AS_ERR_ALLOC;
   h->device = dev;
@@ -698,10 +698,10 @@ extern "C" as_status_t as_fp8_create(as_fp8_context_t* out) {
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)parts); cfg.blockDim = dim3(MM_THREADS); cfg.dynamicSmemBytes = SMEM_MAX;
     cfg.attrs = &attr; cfg.numAttrs = 1;
-    if (cudaOccupancyMaxActiveClusters(&h->clusters[parts], matmul_kernel<1, true>, &cfg) != cudaSuccess) { delete h; return AS_ERR_CUDA; }
+    if (cudaOccupancyMaxActiveClusters(&h->clusters[parts], matmul_kernel<1, true>, &cfg) != cudaSuccess) { delete h; return failed(); }
   }
-  if (cudaMalloc(&h->status, 256) != cudaSuccess) { delete h; return AS_ERR_ALLOC; }
-  if (cudaMemset(h->status, 0, 256) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) { cudaFree(h->status); delete h; return AS_ERR_CUDA; }
+  if (cudaMalloc(&h->status, 256) != cudaSuccess) { delete h; return failed(AS_ERR_ALLOC); }
+  if (cudaMemset(h->status, 0, 256) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) { cudaFree(h->status); delete h; return failed(); }
   *out = h;
   return AS_OK;
 }
@@ -720,16 +720,16 @@ extern "C" as_status_t as_fp8_last_status(as_fp8_context_t h, void* cuda_stream)
   std::lock_guard<std::mutex> hold(h->reading);
   take_status_kernel<<<1, 1, 0, st>>>(h->status);
   if (cudaGetLastError() != cudaSuccess || cudaMemcpyAsync(&word, h->status + TAKEN, 4, cudaMemcpyDeviceToHost, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess)
-    return AS_ERR_CUDA;
+    return failed();
   return word == 0 ? AS_OK : AS_ERR_DEVICE_TIMEOUT;
 }
 
 extern "C" as_status_t as_fp8_debug_expire_wait(as_fp8_context_t h, int64_t limit_cycles, void* cuda_stream) {
   int dev = 0;
   if (h == nullptr || limit_cycles < 1 || limit_cycles > 100000000) return AS_ERR_INVALID_ARG;       // at most about 50 ms
-  if (cudaGetDevice(&dev) != cudaSuccess) return AS_ERR_CUDA;
+  if (cudaGetDevice(&dev) != cudaSuccess) return failed();
   if (dev != h->device) return AS_ERR_INVALID_ARG;
-  return as_tensor_expire_wait(h->status, limit_cycles, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? AS_OK : AS_ERR_CUDA;
+  return as_tensor_expire_wait(h->status, limit_cycles, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? AS_OK : failed();
 }
 
 extern "C" as_status_t as_matmul_fp8(as_fp8_context_t h, const as_matmul_fp8_t* a, void* cuda_stream) {
@@ -738,7 +738,7 @@ extern "C" as_status_t as_matmul_fp8(as_fp8_context_t h, const as_matmul_fp8_t* 
   if (!matrix_ok(a->a, a->rows, a->cols) || !matrix_ok(a->w, a->out_cols, a->cols) || !aligned(a->bias, 2)) return AS_ERR_INVALID_ARG;
   if (!rows_ok(a->out, a->rows, a->out_cols) || a->out.dtype != AS_DTYPE_BF16 || !apart(a->out, a->rows, a->out_cols)) return AS_ERR_INVALID_ARG;
   int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return AS_ERR_CUDA;
+  if (cudaGetDevice(&dev) != cudaSuccess) return failed();
   if (dev != h->device) return AS_ERR_INVALID_ARG;
   const Rows out = rows_of(a->out, a->rows, a->out_cols);
   if (out.split && a->out_cols * (long long)a->out.head_dim > (1ll << 32)) return AS_ERR_UNSUPPORTED;
@@ -759,7 +759,7 @@ extern "C" as_status_t as_matmul_fp8(as_fp8_context_t h, const as_matmul_fp8_t* 
     p.units = (p.N + FEW_COLS - 1) / FEW_COLS * p.mt;
     const dim3 grid((unsigned)std::min(p.units, h->sms)), block(FEW_WARPS * 32);
     const cudaError_t e = p.M <= 8 ? as_launch_dependent(few_rows_kernel<1>, grid, block, few_smem(1), st, p) : as_launch_dependent(few_rows_kernel<2>, grid, block, few_smem(2), st, p);
-    return e == cudaSuccess ? AS_OK : AS_ERR_CUDA;
+    return e == cudaSuccess ? AS_OK : failed();
   }
   MMParams p{};
   p.out = out;
@@ -779,9 +779,9 @@ extern "C" as_status_t as_matmul_fp8(as_fp8_context_t h, const as_matmul_fp8_t* 
   CUtensorMap ma, mw, mo{};
   // results leave by TMA where 32 columns are of one head (a map that the driver does not take leaves that to the warps)
   p.copies = p.vec && (a->out.head_dim == p.N || a->out.head_dim % 32 == 0) && as_tc::make_map_rows(&mo, a->out, p.M, p.N, 32);
-  if (!as_tc::make_map_bytes(&ma, a->a.data, a->cols, p.M, a->a.pitch, BM) || !as_tc::make_map_bytes(&mw, a->w.data, a->cols, p.N, a->w.pitch, p.bn / CG)) return AS_ERR_CUDA;
+  if (!as_tc::make_map_bytes(&ma, a->a.data, a->cols, p.M, a->a.pitch, BM) || !as_tc::make_map_bytes(&mw, a->w.data, a->cols, p.N, a->w.pitch, p.bn / CG)) return failed();
   const int units = (int)std::min<long long>(p.tiles, h->sms / CG);
   const cudaError_t e = tile.parts > 1 ? launch<1, true>(ma, mw, mo, p, (int)p.tiles, smem, st)
                                        : CG == 2 ? launch<2, false>(ma, mw, mo, p, units, smem, st) : launch<1, false>(ma, mw, mo, p, units, smem, st);
-  return e == cudaSuccess ? AS_OK : AS_ERR_CUDA;
+  return e == cudaSuccess ? AS_OK : failed();
 }

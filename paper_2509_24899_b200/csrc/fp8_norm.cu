@@ -564,7 +564,7 @@ as_status_t device_ok(int* sms) {
   int dev = 0, major = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
       cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-    return AS_ERR_CUDA;
+    return failed();
   return major == 10 ? AS_OK : AS_ERR_ARCH;
 }
 
@@ -611,7 +611,7 @@ extern "C" as_status_t as_rms_norm(const as_rms_norm_t* a, void* cuda_stream) {
   if (a->x.dtype == AS_DTYPE_F32) e = res ? launch_out<float, float, true>(p, fp8, move, s, st) : launch_out<float, void, true>(p, fp8, move, s, st);
   else if (!res) e = launch_out<bf, void, true>(p, fp8, move, s, st);
   else e = a->residual.dtype == AS_DTYPE_BF16 ? launch_out<bf, bf, true>(p, fp8, move, s, st) : launch_out<bf, float, true>(p, fp8, move, s, st);
-  return e == cudaSuccess ? AS_OK : AS_ERR_CUDA;
+  return e == cudaSuccess ? AS_OK : failed();
 }
 
 extern "C" as_status_t as_quantize_fp8(const as_quantize_fp8_t* a, void* cuda_stream) {
@@ -641,5 +641,5 @@ extern "C" as_status_t as_quantize_fp8(const as_quantize_fp8_t* a, void* cuda_st
     if (f32) e = move == MOVE32 ? run(quantize_block_kernel<float, MOVE32>) : move == MOVE16 ? run(quantize_block_kernel<float, MOVE16>) : run(quantize_block_kernel<float, MOVE_ELEMENT>);
     else e = move == MOVE32 ? run(quantize_block_kernel<bf, MOVE32>) : move == MOVE16 ? run(quantize_block_kernel<bf, MOVE16>) : run(quantize_block_kernel<bf, MOVE_ELEMENT>);
   }
-  return e == cudaSuccess ? AS_OK : AS_ERR_CUDA;
+  return e == cudaSuccess ? AS_OK : failed();
 }

@@ -125,3 +125,32 @@ def test_status_read_from_two_streams(ops, context):
         stop.set()
         thread.join()
     assert raised == 100 and binding.as_fp8_last_status(context, 0) == 0
+
+
+def test_an_error_of_a_call_stays_with_it(ops):
+    """A context that cannot be made (its allocation is refused inside a stream capture) leaves no error behind for the library's next launch.  In a process of its own, as
+    the refusal ends the capture as well."""
+    import subprocess
+    import sys
+    text = """
+import torch
+from paper_2509_24899_b200 import AsError, HybridAttention, binding, workloads as W
+op = HybridAttention.from_workload(W.CONFIGS["tiny"])
+x = torch.zeros(8, device="cuda")
+refused = False
+try:
+    with torch.cuda.graph(torch.cuda.CUDAGraph()):
+        x.add_(1)
+        try:
+            binding.as_fp8_create()
+        except AsError:
+            refused = True
+except RuntimeError:
+    pass
+binding.as_hybrid_attn_debug_expire_wait(op.handle, 1000, 0)
+print("refused" if refused else "made", op.last_status())
+"""
+    run = subprocess.run([sys.executable, "-c", text], capture_output=True, text=True, timeout=300)
+    assert run.stdout.split()[:1] == ["refused"] and "AsError" not in run.stderr, run.stdout + run.stderr[-2000:]
+    from paper_2509_24899_b200 import binding
+    assert int(run.stdout.split()[1]) == binding.AS_ERR_DEVICE_TIMEOUT
