@@ -1,6 +1,7 @@
 // The calls of block_fp8.py: checks of the tensors, allocation of outputs, the argument structs of as_fp8.h, the call.  In C++ because these calls take 2 to 6 us on the GPU where
 // there are few rows, and the same steps in Python took 9 to 11 us of the CPU's time (here 3 to 5).  A module of its own beside libas_hybrid_attn.so, which itself knows nothing of
 // PyTorch.
+#include <ATen/core/grad_mode.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
@@ -49,6 +50,7 @@ const at::Tensor* tensor_of(PyObject* o, int here, const char* where, const char
   if (!THPVariable_Check(o)) { refuse(where, name, "is no tensor"); return nullptr; }
   const at::Tensor& t = THPVariable_Unpack(o);
   if (!t.is_cuda() || t.get_device() != here || t.layout() != at::kStrided) { refuse(where, name, "is not a strided tensor on the current CUDA device"); return nullptr; }
+  if (t.requires_grad() && at::GradMode::is_enabled()) { refuse(where, name, "requires a gradient, which these calls have none of: detach it, or call under torch.no_grad()"); return nullptr; }
   return &t;
 }
 

@@ -26,9 +26,13 @@ class Fp8AttentionLayer:
         for name in "qkvo":
             if tuple(weights[name].shape) != (H * d, H * d):
                 raise ValueError("Fp8AttentionLayer: weight %r is %d x %d, not %s" % (name, H * d, H * d, tuple(weights[name].shape)))
-        self._w8 = {name: quantize_fp8(weights[name], block_rows=128) for name in "qkvo"}
-        self._bias = {name: weights.get("bias_" + name) for name in "qkvo"}
-        self._norm = {name: weights.get(name) for name in ("norm", "norm_q", "norm_k")}
+
+        def frozen(name):
+            return None if weights.get(name) is None else weights[name].detach()
+
+        self._w8 = {name: quantize_fp8(frozen(name), block_rows=128) for name in "qkvo"}
+        self._bias = {name: frozen("bias_" + name) for name in "qkvo"}
+        self._norm = {name: frozen(name) for name in ("norm", "norm_q", "norm_k")}
 
     def forward(self, hidden, residual):
         """hidden [B N, H d] bf16, residual [B N, H d] bf16 or fp32 -> (y [B N, H d] bf16, the next residual)."""

@@ -154,3 +154,43 @@ print("refused" if refused else "made", op.last_status())
     assert run.stdout.split()[:1] == ["refused"] and "AsError" not in run.stderr, run.stdout + run.stderr[-2000:]
     from paper_2509_24899_b200 import binding
     assert int(run.stdout.split()[1]) == binding.AS_ERR_DEVICE_TIMEOUT
+
+
+# ------------------------------------------------------------------------------------------------ gradients
+def test_tensors_that_require_gradients_are_refused(ops):
+    """Each input, and an output that is given; nothing is refused where gradients are off or the tensor is detached."""
+    x, r, w, bias = randn(4, 256, seed=1), randn(4, 256, seed=2), randn(256, seed=3), randn(64, seed=4)
+    a8, w8 = ops.quantize_fp8(x), ops.quantize_fp8(randn(64, 256, seed=5), block_rows=128)
+    calls = [(x, lambda: ops.rms_norm(x, w, residual=r)), (w, lambda: ops.rms_norm(x, w)), (r, lambda: ops.rms_norm(x, w, residual=r, fp8=True)),
+             (r, lambda: ops.rms_norm(x, residual=randn(4, 256), residual_out=r)), (r, lambda: ops.rms_norm(x, out=r)),
+             (x, lambda: ops.quantize_fp8(x)), (bias, lambda: ops.matmul_fp8(a8, w8, bias=bias))]
+    for tensor, call in calls:
+        call()
+        tensor.requires_grad_()
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+        with torch.no_grad():
+            call()
+        with torch.inference_mode():
+            call()
+        tensor.requires_grad_(False)
+        call()
+
+
+def test_layer_of_parameters(ops):
+    """Weights that are a module's parameters are taken as the constants that they are for the layer; what it is called on is refused where it requires a gradient."""
+    from paper_2509_24899_b200 import HybridAttention, workloads as W
+    from paper_2509_24899_b200.fp8_layer import Fp8AttentionLayer
+    wl = W.CONFIGS["tiny"]
+    D, rows = wl.H * wl.d, wl.B * wl.N
+    data = W.generate(wl, wq_gain=2e-3)
+    phi = {n: torch.from_numpy(data[n].view("int16")).cuda().view(BF16) for n in ("wq", "wk")}
+    plain = {n: randn(D, D, seed=i, gain=D ** -0.5) for i, n in enumerate("qkvo")} | {"bias_q": randn(D, seed=9), "norm": randn(D, seed=10), "norm_k": None}
+    hidden, residual = randn(rows, D, seed=30), randn(rows, D, seed=31)
+    attention = HybridAttention.from_workload(wl)
+    y, total = Fp8AttentionLayer(attention, plain, phi).forward(hidden, residual)
+    layer = Fp8AttentionLayer(attention, {n: None if t is None else torch.nn.Parameter(t) for n, t in plain.items()}, phi)
+    got = layer.forward(hidden, residual)
+    assert torch.equal(got[0], y) and torch.equal(got[1], total)
+    with pytest.raises(ValueError, match="gradient"):
+        layer.forward(hidden.requires_grad_(), residual)
