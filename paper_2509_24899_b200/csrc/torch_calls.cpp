@@ -53,6 +53,11 @@ const at::Tensor* tensor_of(PyObject* o, int here, const char* where, const char
   if (t.requires_grad() && at::GradMode::is_enabled()) { refuse(where, name, "requires a gradient, which these calls have none of: detach it, or call under torch.no_grad()"); return nullptr; }
   return &t;
 }
+// A tensor of the caller's that the call has written: what autograd has saved of it is no longer there.  (Inference tensors keep no count.)
+void written(PyObject* o) {
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
 
 // [rows, cols] or [B, H, N, d] as an as_rows_t.  A single row, column or head leaves its stride open.
 const at::Tensor* rows_of(PyObject* o, int here, const char* where, const char* name, as_rows_t& r, int64_t& rows, int64_t& cols) {
@@ -79,6 +84,7 @@ const at::Tensor* rows_of(PyObject* o, int here, const char* where, const char* 
 
 // The tensors of a pair, held for as long as the call uses them: what hands them out need not keep them (an iterator does not).
 struct Pair { Held data, scales; };
+void written(const Pair& pair) { written(pair.data.o); written(pair.scales.o); }
 
 // A pair (e4m3 values, scales) as an as_fp8_matrix_t.
 bool matrix_of(PyObject* pair, int here, const char* where, const char* name, Pair& hold, as_fp8_matrix_t& m, int64_t& rows, int64_t& cols) {
@@ -196,6 +202,8 @@ PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   if (fp8 ? !matrix_of(out.o, here, where, "out", pair, p.out8, r, c) : rows_of(out.o, here, where, "out", p.out, r, c) == nullptr) return nullptr;
   if (r != rows || c != cols) { refuse(where, "out", "has not x's rows and columns"); return nullptr; }
   if (rows > 0 && cols > 0 && !status(as_rms_norm(&p, current_stream(here)), "as_rms_norm")) return nullptr;
+  if (a[5] != Py_None) { if (fp8) written(pair); else written(out.o); }
+  if (a[6] != Py_None) written(total.o);
   if (total.o == nullptr) return out.give();
   return PyTuple_Pack(2, out.o, total.o);
   END_HANDLE_TH_ERRORS
@@ -222,6 +230,7 @@ PyObject* quantize_fp8(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   if (out.o == nullptr || !matrix_of(out.o, here, where, "out", pair, p.out, r, c)) return nullptr;
   if (r != rows || c != cols) { refuse(where, "out", "has not x's rows and columns"); return nullptr; }
   if (rows > 0 && cols > 0 && !status(as_quantize_fp8(&p, current_stream(here)), "as_quantize_fp8")) return nullptr;
+  if (a[2] != Py_None) written(pair);
   return out.give();
   END_HANDLE_TH_ERRORS
 }
@@ -252,6 +261,7 @@ PyObject* matmul_fp8(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     as_fp8_context_t ctx;
     if (!context_of(here, ctx) || !status(as_matmul_fp8(ctx, &p, current_stream(here)), "as_matmul_fp8")) return nullptr;
   }
+  if (a[3] != Py_None) written(out.o);
   return out.give();
   END_HANDLE_TH_ERRORS
 }

@@ -177,6 +177,34 @@ def test_tensors_that_require_gradients_are_refused(ops):
         call()
 
 
+def test_given_outputs_count_as_modified_in_place(ops):
+    """A backward pass that needs a tensor which a call has written since says so."""
+    x, w8 = randn(4, 256, seed=1), ops.quantize_fp8(randn(256, 256, seed=5), block_rows=128)
+    x8 = ops.quantize_fp8(x)
+    for call in (lambda t: ops.rms_norm(x, out=t), lambda t: ops.rms_norm(x, residual=t, residual_out=t), lambda t: ops.rms_norm(x, residual=x, residual_out=t, fp8=True),
+                 lambda t: ops.matmul_fp8(x8, w8, out=t)):
+        saved, p = randn(4, 256, seed=7), torch.ones(4, 256, dtype=BF16, device="cuda", requires_grad=True)
+        loss = (p * saved).sum()
+        version = saved._version
+        call(saved)
+        assert saved._version == version + 1
+        with pytest.raises(RuntimeError, match="inplace"):
+            loss.backward()
+    pair = ops.empty_fp8(4, 256)
+    for i, call in enumerate((lambda: ops.quantize_fp8(x, out=pair), lambda: ops.rms_norm(x, fp8=True, out=pair))):
+        call()
+        assert pair.data._version == pair.scales._version == i + 1
+    # inputs are not modified, and inference tensors, which keep no count, are taken
+    version = [t._version for t in (x, *x8, *w8)]
+    ops.matmul_fp8(x8, w8)
+    ops.rms_norm(x, residual=x)
+    assert version == [t._version for t in (x, *x8, *w8)]
+    with torch.inference_mode():
+        out = torch.empty(4, 256, dtype=BF16, device="cuda")
+        assert torch.equal(ops.rms_norm(x, out=out), ops.rms_norm(x))
+    assert torch.equal(ops.rms_norm(x, out=out), ops.rms_norm(x))
+
+
 def test_layer_of_parameters(ops):
     """Weights that are a module's parameters are taken as the constants that they are for the layer; what it is called on is refused where it requires a gradient."""
     from paper_2509_24899_b200 import HybridAttention, workloads as W
