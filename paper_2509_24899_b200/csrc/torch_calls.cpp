@@ -149,10 +149,13 @@ PyObject* empty_pair(int64_t rows, int64_t cols, int here) {
 
 bool context_of(int here, as_fp8_context_t& ctx) {
   if (here < 0 || here >= 64) return status(AS_ERR_UNSUPPORTED, "as_fp8_create");
-  std::lock_guard<std::mutex> hold(g_lock);
-  if (g_contexts[here] == nullptr && !status(as_fp8_create(&g_contexts[here]), "as_fp8_create")) return false;
-  ctx = g_contexts[here];
-  return true;
+  as_status_t s = AS_OK;
+  {
+    std::lock_guard<std::mutex> hold(g_lock);
+    if (g_contexts[here] == nullptr) s = as_fp8_create(&g_contexts[here]);
+    ctx = g_contexts[here];
+  }
+  return status(s, "as_fp8_create");        // behind the lock: making the exception runs Python code, which may let another thread in here
 }
 
 void* current_stream(int here) { return c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)here).stream(); }

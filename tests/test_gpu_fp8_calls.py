@@ -222,3 +222,40 @@ def test_layer_of_parameters(ops):
     assert torch.equal(got[0], y) and torch.equal(got[1], total)
     with pytest.raises(ValueError, match="gradient"):
         layer.forward(hidden.requires_grad_(), residual)
+
+
+# ------------------------------------------------------------------------------------------------ threads
+def test_a_context_that_cannot_be_made_holds_no_other_thread_up(ops):
+    """Two threads whose calls are the first on a device, where setting its context up is refused (inside a stream capture): each gets its exception, also while the
+    other's is being made, which runs Python code.  In a process of its own, as the refusal ends the capture as well."""
+    import subprocess
+    import sys
+    text = """
+import threading, time, torch
+from paper_2509_24899_b200 import block_fp8
+seen = []
+class Slow(RuntimeError):
+    def __init__(self, status, where):
+        seen.append(status)
+        time.sleep(1)
+block_fp8._calls.set_classes(block_fp8.BlockFp8, Slow)
+x = torch.zeros(8, device="cuda")
+def call():
+    try:
+        block_fp8.fp8_last_status()
+    except Slow:
+        seen.append("raised")
+threads = [threading.Thread(target=call) for _ in range(3)]
+try:
+    with torch.cuda.graph(torch.cuda.CUDAGraph()):
+        x.add_(1)
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+except RuntimeError:
+    pass
+print(seen.count("raised"), len(seen), max(s for s in seen if s != "raised") > 0)
+"""
+    run = subprocess.run([sys.executable, "-c", text], capture_output=True, text=True, timeout=120)
+    assert run.stdout.split() == ["3", "6", "True"], run.stdout + run.stderr[-2000:]
