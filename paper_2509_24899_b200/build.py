@@ -11,6 +11,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "lib", "libas_hybrid_attn.so")
 TORCH_CALLS = os.path.join(PKG, "lib", "as_torch_calls.so")
+BUILT_FOR = TORCH_CALLS + ".built_for"          # the PyTorch and Python that it was compiled against
 SOURCES = ["as_hybrid_attn.cu", "simt_path.cu", "tensor_init.cu", "tensor_qpass.cu", "tensor_qstream.cu", "tensor_kpass.cu", "backward_simt.cu", "backward_tensor.cu", "backward_tensor_d64.cu", "no_alloc.cu",
            "block_rates.cu", "fp8_norm.cu", "fp8_matmul.cu"]
 
@@ -34,14 +35,27 @@ def _stale() -> bool:
     return _older(LIB, deps)
 
 
+def torch_key() -> str:
+    """What the module of the calls that take PyTorch tensors depends on beside its sources."""
+    import torch
+    return "torch %s, python %s" % (torch.__version__, sys.version.split()[0])
+
+
+def _torch_calls_stale() -> bool:
+    if _older(TORCH_CALLS, [os.path.join(CSRC, "torch_calls.cpp")] + _headers()) or not os.path.exists(BUILT_FOR):
+        return True
+    with open(BUILT_FOR) as f:
+        return f.read() != torch_key()
+
+
 def build_torch_calls(force: bool = False) -> str:
-    """Compiles the module of the calls that take PyTorch tensors when it is missing or older than its source; returns its path."""
-    source = os.path.join(CSRC, "torch_calls.cpp")
-    if not force and not _older(TORCH_CALLS, [source] + _headers()):
+    """Compiles the module of the calls that take PyTorch tensors when it is missing, older than its source or made for another PyTorch or Python; returns its path."""
+    if not force and not _torch_calls_stale():
         return TORCH_CALLS
     import sysconfig
 
     import torch
+    source = os.path.join(CSRC, "torch_calls.cpp")
     libs, inc = (os.path.join(os.path.dirname(torch.__file__), d) for d in ("lib", "include"))
     cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
@@ -51,6 +65,8 @@ def build_torch_calls(force: bool = False) -> str:
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError("%s failed:\n%s%s" % (cmd[0], res.stdout, res.stderr))
+    with open(BUILT_FOR, "w") as f:
+        f.write(torch_key())
     return TORCH_CALLS
 
 
