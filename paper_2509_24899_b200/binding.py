@@ -113,7 +113,7 @@ def lib() -> C.CDLL:
                                                   + [C.c_void_p, C.c_void_p, C.c_void_p],
             "as_select_block_rates": [C.c_int32, C.c_int32, C.POINTER(C.c_double), C.POINTER(C.c_double), C.c_double,
                                       C.POINTER(C.c_int32), C.POINTER(C.c_double), C.POINTER(C.c_double)],
-            # the argument structs of the next three: an instance's address, or bytes of the same layout
+            # the argument structs of the next three: an instance's address
             "as_rms_norm": [C.c_void_p, C.c_void_p],
             "as_quantize_fp8": [C.c_void_p, C.c_void_p],
             "as_matmul_fp8": [H, C.c_void_p, C.c_void_p],
@@ -330,18 +330,18 @@ def as_select_block_rates(cost, err, budget):
 
 
 def as_rms_norm(args, stream_ptr) -> None:
-    """`args`: an as_rms_norm_t, or bytes of its layout (cheaper to make).  A row's root-mean-square norm, see include/as_fp8.h."""
-    _check(lib().as_rms_norm(args if isinstance(args, bytes) else C.addressof(args), stream_ptr or None), "as_rms_norm")
+    """`args`: an as_rms_norm_t.  A row's root-mean-square norm, see include/as_fp8.h."""
+    _check(lib().as_rms_norm(C.addressof(args), stream_ptr or None), "as_rms_norm")
 
 
 def as_quantize_fp8(args, stream_ptr) -> None:
-    """`args`: an as_quantize_fp8_t, or bytes of its layout.  A matrix in 8-bit form."""
-    _check(lib().as_quantize_fp8(args if isinstance(args, bytes) else C.addressof(args), stream_ptr or None), "as_quantize_fp8")
+    """`args`: an as_quantize_fp8_t.  A matrix in 8-bit form."""
+    _check(lib().as_quantize_fp8(C.addressof(args), stream_ptr or None), "as_quantize_fp8")
 
 
 def as_matmul_fp8(ctx, args, stream_ptr) -> None:
-    """`args`: an as_matmul_fp8_t, or bytes of its layout.  The product of two matrices in 8-bit form."""
-    _check(lib().as_matmul_fp8(ctx, args if isinstance(args, bytes) else C.addressof(args), stream_ptr or None), "as_matmul_fp8")
+    """`args`: an as_matmul_fp8_t.  The product of two matrices in 8-bit form."""
+    _check(lib().as_matmul_fp8(ctx, C.addressof(args), stream_ptr or None), "as_matmul_fp8")
 
 
 def as_fp8_create() -> C.c_void_p:

@@ -259,3 +259,66 @@ print(seen.count("raised"), len(seen), max(s for s in seen if s != "raised") > 0
 """
     run = subprocess.run([sys.executable, "-c", text], capture_output=True, text=True, timeout=120)
     assert run.stdout.split() == ["3", "6", "True"], run.stdout + run.stderr[-2000:]
+
+
+# ------------------------------------------------------------------------------------------------ C entries
+def test_the_product_refuses(ops, context):
+    """Arguments that the C entry does not take, one at a time, through the binding; the output stays as it was, and the call without the change runs."""
+    from paper_2509_24899_b200 import binding as b
+    M, N, K = 20, 48, 200
+    a, w = ops.quantize_fp8(randn(M, K, seed=1)), ops.quantize_fp8(randn(N, K, seed=2), block_rows=128)
+    out = torch.full((M, N), 7.0, dtype=BF16, device="cuda")
+
+    def rows(data=out.data_ptr(), dtype=b.AS_DTYPE_BF16, head_dim=N, tokens=M, sb=0, sh=0, st=N):
+        return b.as_rows_t(data, dtype, head_dim, tokens, sb, sh, st)
+
+    def matrix(m, data=None, pitch=None, scales=None, scale_rows=None):
+        first = lambda x, y: y if x is None else x           # noqa: E731
+        return b.as_fp8_matrix_t(first(data, m.data.data_ptr()), first(pitch, m.data.stride(0)), first(scales, m.scales.data_ptr()), first(scale_rows, m.data.shape[0]))
+
+    bad = [dict(struct_size=8), dict(cols=0), dict(cols=(1 << 20) + 1), dict(rows=-1), dict(rows=(1 << 30) + 1), dict(out_cols=0), dict(out_cols=(1 << 24) + 1), dict(bias=1),
+           dict(a=matrix(a, data=0)), dict(a=matrix(a, data=a.data.data_ptr() + 8)), dict(a=matrix(a, pitch=192)), dict(a=matrix(a, pitch=216)), dict(a=matrix(a, scales=0)),
+           dict(a=matrix(a, scales=a.scales.data_ptr() + 2)), dict(a=matrix(a, scale_rows=M - 1)), dict(w=matrix(w, scale_rows=N - 1)), dict(w=matrix(w, data=0)),
+           dict(out=rows(data=0)), dict(out=rows(data=out.data_ptr() + 1)), dict(out=rows(dtype=b.AS_DTYPE_F32)), dict(out=rows(head_dim=0)), dict(out=rows(head_dim=20)),
+           dict(out=rows(tokens=0)), dict(out=rows(tokens=3)), dict(out=rows(st=-N)), dict(out=rows(st=N - 1)), dict(out=rows(st=0)), dict(out=rows(head_dim=16, sh=8)),
+           dict(out=rows(tokens=10, sb=N, st=N))]
+    for change in bad:
+        args = product_of(a, w, out)
+        for field, value in change.items():
+            setattr(args, field, value)
+        with pytest.raises(ops.AsError) as e:
+            b.as_matmul_fp8(context, args, 0)
+        assert e.value.status == b.AS_ERR_INVALID_ARG, change
+    # more columns in heads that lie apart than an index takes
+    args = product_of(a, w, out)
+    args.out_cols, args.out, args.w = 1 << 24, rows(head_dim=1 << 23, sh=1 << 30, st=1 << 40), matrix(w, scale_rows=1 << 24)
+    with pytest.raises(ops.AsError) as e:
+        b.as_matmul_fp8(context, args, 0)
+    assert e.value.status == b.AS_ERR_UNSUPPORTED
+    torch.cuda.synchronize()
+    assert bool((out == 7).all())
+    args = product_of(a, w, out)
+    args.rows, args.a, args.out = 0, matrix(a, scale_rows=0), rows(tokens=0)
+    b.as_matmul_fp8(context, args, 0)                                          # no rows: nothing to do
+    torch.cuda.synchronize()
+    assert bool((out == 7).all())
+    b.as_matmul_fp8(context, product_of(a, w, out), 0)
+    R.check_matmul(out, a, w)
+
+
+def test_norm_and_8_bit_form_through_the_binding(ops):
+    import ctypes as C
+
+    from paper_2509_24899_b200 import binding as b
+    x, y = randn(5, 200, seed=1), torch.empty(5, 200, dtype=BF16, device="cuda")
+    form = ops.empty_fp8(5, 200)
+    rows = [b.as_rows_t(t.data_ptr(), b.AS_DTYPE_BF16, 200, 5, 0, 0, 200) for t in (x, y)]
+    matrix = b.as_fp8_matrix_t(form.data.data_ptr(), form.data.stride(0), form.scales.data_ptr(), 5)
+    args = b.as_rms_norm_t(struct_size=C.sizeof(b.as_rms_norm_t), cols=200, rows=5, x=rows[0], out=rows[1], eps=1e-6)
+    b.as_rms_norm(args, 0)
+    assert torch.equal(y, ops.rms_norm(x))
+    b.as_quantize_fp8(b.as_quantize_fp8_t(C.sizeof(b.as_quantize_fp8_t), 200, 5, rows[0], matrix, 1, 0), 0)
+    assert all(torch.equal(s.view(torch.uint8), t.view(torch.uint8)) for s, t in zip(form, ops.quantize_fp8(x)))
+    args.eps = -1.0
+    with pytest.raises(ops.AsError):
+        b.as_rms_norm(args, 0)
