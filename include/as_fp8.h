@@ -40,7 +40,7 @@ enum { AS_DTYPE_BF16 = 0, AS_DTYPE_F32 = 1 };
  *
  * in elements.  [rows, cols] with a row stride: tokens = rows, head_dim = cols.  The attention's [B, H, N, d]: tokens = N,
  * head_dim = d, its strides.  tokens divides rows and head_dim divides cols; strides are not negative, and those of an output
- * keep its elements apart.  data == NULL: no such matrix.  Where head_dim, the strides and the address are all
+ * keep its elements apart; an output shares no memory with another one, nor with an input in another layout.  data == NULL: no such matrix.  Where head_dim, the strides and the address are all
  * multiples of 8 elements (16 bytes), rows move 16 bytes at a time; otherwise element by element. */
 typedef struct {
   void* data;
@@ -76,7 +76,7 @@ typedef struct {
 typedef struct {
   uint32_t struct_size;     /* sizeof(as_quantize_fp8_t) */
   int32_t cols;             /* 1 .. 16384 */
-  int64_t rows;             /* 0 .. 2^31 - 1 */
+  int64_t rows;             /* 0 .. 2^31 - 1; with block_rows == 128 up to 65535 * 128 */
   as_rows_t x;              /* bf16 or fp32 */
   as_fp8_matrix_t out;
   int32_t block_rows;       /* rows that share a scale: 1 (activations) or 128 (weights) */

@@ -85,7 +85,7 @@ def rms_norm(x, weight=None, residual=None, eps=1e-6, fp8=False, out=None, resid
 
 def quantize_fp8(x, block_rows=1, out=None, stream=None) -> BlockFp8:
     """x (bf16 or fp32, [rows, cols] or [B, H, N, d]) in 8-bit form; block_rows: rows that share a scale, 1 for activations and
-    128 for weights.  Up to 16384 columns."""
+    128 for weights (up to 65535 * 128 rows).  Up to 16384 columns."""
     return _on(stream, _calls.quantize_fp8, x, block_rows, out)
 
 

@@ -478,7 +478,7 @@ matmul_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CU
 //
 // What bounds it is the latency of memory, and then the number of copies: a warp's operands come by asynchronous copies into slots that it alone reads, two or three blocks ahead and
 // on into the next unit, one copy for all scales of a block.  (2 rows by w of 1536 x 1536, 9216 x 1536, 1536 x 6144, 6144 x 6144: straight into registers 2.7, 5.5, 5.7, 13.2 us;
-// two CTAs of 8 warps an SM 2.6, 4.5, 6.4, 12.7; one of 16 warps 2.1, 5.1, 4.1, 10.7 us (3.5 TB/s).)
+// two CTAs of 8 warps an SM 2.6, 4.5, 6.4, 12.7; one of 16 warps 2.0, 4.8, 4.0, 10.5 us (3.6 TB/s).)
 constexpr int FEW_WARPS = 16, FEW_COLS = 16;
 // With NT tiles of 8 rows of a: blocks of a warp under way (one CTA an SM), bytes of one: per lane 64 of w and 32 NT of a, the scale words of 16 rows of w and 8 NT of a
 __host__ __device__ constexpr int few_ahead(int nt) { return nt == 1 ? 3 : 2; }
@@ -609,16 +609,16 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 1) few_rows_kernel(const __gri
   }
 }
 
-// The shape of a tile - CTAs that share it, rows of w - by the time that its turns take on all SMs: turns x blocks of 128 columns x ns a block, and what the reading out
-// of the last turn's results and the meeting of a pair add.  ns: measured with all SMs busy, at 7800 x 4608 x 1536 and what the largest products make of it: up to 128 rows of w the copies
-// of a bound a block, 64 bytes a clock into an SM (a pair halves those of w), above them the MMAs, and power: at 32760 x 4608 x 1536, back to back, 192 and 224 rows take
-// 212 and 209 us at 1.45 GHz.  The last turn counts half of what it leaves idle, as the clock rises meanwhile; a single turn counts whole.
-// Few rows go to single CTAs and narrow tiles: 512 x 1536 x 1536 takes 6.1 us with {1, 64}, 7.2 with {2, 192}.
-struct Tile { int cg, bn, parts; double ns; };
+// The shape of a tile - CTAs that share its rows or its columns, rows of w - by the time that its turns take on all SMs: turns x blocks of 128 columns x ns a block, and what the
+// reading out of the last turn's results and the meeting of a pair add.  ns: measured with all SMs busy, at 7800 x 4608 x 1536 and what the largest products make of it.  What a block
+// takes is its copies at every width, 64 bytes a clock into an SM (a pair halves those of w): with 192 rows of w a pair's 28672 bytes an SM are 448 clk beside 384 of MMAs, with 224
+// 30720 and 480 beside 448.  At 32760 x 4608 x 1536, back to back, 192 and 224 rows take 212 and 209 us at 1.45 GHz.  The last turn counts half of what it leaves idle, as the clock
+// rises meanwhile; a single turn counts whole.  Few rows go to single CTAs and narrow tiles: 512 x 1536 x 1536 takes 6.1 us with {1, 64}, 7.2 with {2, 192}.
 //
 // Few tiles with long columns go to clusters of CTAs that share a tile's columns, by whole groups of four blocks, as many as the device holds at once (`clusters`, by size): 2 us more
 // for the meeting and the sums, and more with every CTA beyond two (128 x 1536 x 6144 14.0 us by single CTAs, 9.4 by three, 9.6 by five; 512 x 1536 x 6144 15.0, 11.5 by two, 13.2 by three;
 // 300 x 512 x 4096 10.1 and 8.0; but 512 x 1536 x 1536 5.9 and 8.1, 1024 x 512 x 2048 6.5 and 7.4).
+struct Tile { int cg, bn, parts; double ns; };
 constexpr int MAX_PARTS = 8;
 Tile tile_of(int M, int N, int kb, int sms, const int (&clusters)[MAX_PARTS + 1]) {
   static const int ns[2][7] = {{230, 250, 265, 300, 345, 385, 440}, {228, 230, 240, 262, 297, 320, 365}};
@@ -640,8 +640,9 @@ Tile tile_of(int M, int N, int kb, int sms, const int (&clusters)[MAX_PARTS + 1]
 }
 
 // Whether a product goes to few_rows_kernel: up to 16 rows of a, and up to 256 where its turns - units of 16 rows of a and of w, sixteen blocks of 128 columns at a time - take
-// less than the tile's: 1.5 us each, the first one 0.7, from 0.5 us less of setting up.  (us by the one and the other: 16 rows by 1536 x 1536 2.6 and 5.3, by 6144 x 6144 14.3 and 22;
-// 32 rows by 1536 x 1536 4.3 and 5.3, by 9216 x 1536 13.8 and 7.5; 64 rows by 512 x 1280 2.7 and 4.8, by 1536 x 1536 6.0 and 5.3; 256 rows by 128 x 2392 3.8 and 6.9.)
+// less than the tile's: 1.5 us each, the first one 0.7, from 0.5 us less of setting up.  (us by the one and the other: 16 rows by 1536 x 1536 2.8 and 5.3, by 9216 x 1536 7.5 and 7.9,
+// by 1536 x 6144 6.0 and 9.8, by 6144 x 6144 14.7 and 16.6; the exception is a wide w of short rows, 20000 x 192 10.2 and 5.6.  32 rows by 1536 x 1536 4.3 and 5.3, by 9216 x 1536
+// 13.8 and 7.5; 64 rows by 512 x 1280 2.7 and 4.8, by 1536 x 1536 6.0 and 5.3; 256 rows by 128 x 2392 3.8 and 6.9.)
 bool few_rows(int M, int N, int kb, int sms, const Tile& tile) {
   if (M <= 16) return true;
   if (M > 256) return false;

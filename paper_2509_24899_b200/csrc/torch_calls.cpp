@@ -19,7 +19,7 @@ PyObject *g_block_fp8 = nullptr, *g_as_error = nullptr;      // the classes Bloc
 std::mutex g_lock;
 as_fp8_context_t g_contexts[64] = {};
 
-// A refusal: `what` with the Python value's repr where there is one.
+// A refusal: the call, the argument's name and what is wrong with it.
 bool refuse(const char* where, const char* name, const char* what) {
   PyErr_Format(PyExc_ValueError, "%s: %s %s", where, name, what);
   return false;

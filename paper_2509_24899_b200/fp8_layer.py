@@ -6,6 +6,10 @@
     y = o Wo + bo                                                        quantize_fp8 from heads, matmul_fp8
 
 No tensor is copied or permuted between the calls.  Weights are frozen: they are brought to their 8-bit form once.
+
+Nothing stands between the norms of q and k and the attention: a model that turns them there (a rotary embedding) makes the same calls itself, with its own step in between.  q, k and
+v come from three products, each of which lands where it is needed; one product with the three weights on top of each other gives rows [B N, 3 H d], of which the norms take their
+thirds as they lie, but v would be copied into heads (the attention takes contiguous ones).
 """
 from __future__ import annotations
 
