@@ -40,8 +40,9 @@ enum { AS_DTYPE_BF16 = 0, AS_DTYPE_F32 = 1 };
  *
  * in elements.  [rows, cols] with a row stride: tokens = rows, head_dim = cols.  The attention's [B, H, N, d]: tokens = N,
  * head_dim = d, its strides.  tokens divides rows and head_dim divides cols; strides are not negative, and those of an output
- * keep its elements apart; an output shares no memory with another one, nor with an input in another layout.  data == NULL: no such matrix.  Where head_dim, the strides and the address are all
- * multiples of 8 elements (16 bytes), rows move 16 bytes at a time; otherwise element by element. */
+ * keep its elements apart; an output shares no memory with another one, nor with an input in another layout.  data == NULL: no
+ * such matrix.  Where head_dim, the strides and the address are all multiples of 8 elements (16 bytes), rows move 16 bytes at a
+ * time; otherwise element by element. */
 typedef struct {
   void* data;
   int32_t dtype;            /* AS_DTYPE_BF16 | AS_DTYPE_F32 */
