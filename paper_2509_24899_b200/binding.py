@@ -18,6 +18,10 @@ AS_STAB_PAPER, AS_STAB_EXACT = 0, 1
 AS_ACT_RELU = 0
 AS_PATH_TENSOR, AS_PATH_SIMT = 0, 1
 AS_DTYPE_BF16, AS_DTYPE_F32 = 0, 1
+AS_ROTARY_INTERLEAVED, AS_ROTARY_HALF, AS_ROTARY_MAX_AXES = 0, 1, 4
+AS_ROTARY_PLAIN, AS_ROTARY_LINEAR, AS_ROTARY_NTK, AS_ROTARY_YARN = 0, 1, 2, 3
+AS_NORM_NONE, AS_NORM_HEAD, AS_NORM_ROW = 0, 1, 2
+AS_ACT_NONE, AS_ACT_SILU, AS_ACT_GELU, AS_ACT_GELU_TANH = -1, 1, 2, 3
 AS_KERNEL_KPASS, AS_KERNEL_REDUCE, AS_KERNEL_QPASS, AS_NUM_KERNELS = 0, 1, 2, 3
 
 
@@ -67,6 +71,38 @@ class as_matmul_fp8_t(C.Structure):
                 ("a", as_fp8_matrix_t), ("w", as_fp8_matrix_t), ("bias", C.c_void_p), ("out", as_rows_t)]
 
 
+class as_rotary_axis_t(C.Structure):
+    _fields_ = [("size", C.c_int32), ("pairs", C.c_int32), ("scaling", C.c_int32), ("reserved", C.c_int32), ("base", C.c_double), ("factor", C.c_double), ("original", C.c_double)]
+
+
+class as_rotation_t(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("n_axes", C.c_int32), ("size", C.c_int32 * AS_ROTARY_MAX_AXES), ("pairs", C.c_int32 * AS_ROTARY_MAX_AXES), ("layout", C.c_int32),
+                ("inverse", C.c_int32), ("position_bytes", C.c_int32), ("positions", C.c_void_p), ("positions_stride", C.c_int64), ("first", C.c_int64)]
+
+
+class as_qk_norm_rotary_t(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("norm", C.c_int32), ("rows", C.c_int64), ("head_dim", C.c_int32), ("q_heads", C.c_int32), ("k_heads", C.c_int32), ("eps", C.c_float),
+                ("q", as_rows_t), ("k", as_rows_t), ("q_out", as_rows_t), ("k_out", as_rows_t), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("weight_dtype", C.c_int32),
+                ("reserved", C.c_int32), ("rotation", as_rotation_t)]
+
+
+class as_qk_norm_rotary_backward_t(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("reserved", C.c_int32), ("fwd", C.POINTER(as_qk_norm_rotary_t)), ("dq", as_rows_t), ("dk", as_rows_t), ("dq_out", as_rows_t), ("dk_out", as_rows_t),
+                ("dq_weight", C.c_void_p), ("dk_weight", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
+
+
+class as_linear_t(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("activation", C.c_int32), ("rows", C.c_int64), ("cols", C.c_int64), ("out_cols", C.c_int64), ("x", as_rows_t), ("w", as_rows_t),
+                ("residual", as_rows_t), ("out", as_rows_t), ("pre", as_rows_t), ("bias", C.c_void_p), ("gate", C.c_void_p), ("bias_dtype", C.c_int32), ("gate_dtype", C.c_int32),
+                ("gates", C.c_int64), ("gate_stride", C.c_int64), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
+
+
+class as_linear_backward_t(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("activation", C.c_int32), ("rows", C.c_int64), ("cols", C.c_int64), ("out_cols", C.c_int64), ("dy", as_rows_t), ("x", as_rows_t), ("w", as_rows_t),
+                ("pre", as_rows_t), ("dx", as_rows_t), ("dw", as_rows_t), ("gate", C.c_void_p), ("dbias", C.c_void_p), ("dgate", C.c_void_p), ("bias_dtype", C.c_int32), ("gate_dtype", C.c_int32),
+                ("gates", C.c_int64), ("gate_stride", C.c_int64), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
+
+
 class AsError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -114,6 +150,14 @@ def lib() -> C.CDLL:
             "as_select_block_rates": [C.c_int32, C.c_int32, C.POINTER(C.c_double), C.POINTER(C.c_double), C.c_double,
                                       C.POINTER(C.c_int32), C.POINTER(C.c_double), C.POINTER(C.c_double)],
             # the argument structs of the next three: an instance's address
+            "as_rotary_table": [C.POINTER(as_rotary_axis_t), C.c_int32, C.c_void_p, C.c_void_p],
+            "as_qk_norm_rotary": [C.c_void_p, C.c_void_p],
+            "as_qk_norm_rotary_backward": [C.c_void_p, C.c_void_p],
+            "as_qk_norm_rotary_backward_workspace_bytes": [C.c_void_p, C.POINTER(C.c_uint64)],
+            "as_linear": [H, C.c_void_p, C.c_void_p],
+            "as_linear_workspace_bytes": [H, C.c_void_p, C.POINTER(C.c_uint64)],
+            "as_linear_backward": [H, C.c_void_p, C.c_void_p],
+            "as_linear_backward_workspace_bytes": [H, C.c_void_p, C.POINTER(C.c_uint64)],
             "as_rms_norm": [C.c_void_p, C.c_void_p],
             "as_quantize_fp8": [C.c_void_p, C.c_void_p],
             "as_matmul_fp8": [H, C.c_void_p, C.c_void_p],
@@ -362,3 +406,47 @@ def as_fp8_last_status(ctx, stream_ptr) -> int:
 def as_fp8_debug_expire_wait(ctx, limit_cycles: int, stream_ptr) -> None:
     """Test aid: a bounded wait that runs out, see include/as_fp8.h."""
     _check(lib().as_fp8_debug_expire_wait(ctx, int(limit_cycles), stream_ptr or None), "as_fp8_debug_expire_wait")
+
+
+def as_rotary_table(axes, table_ptr, stream_ptr) -> None:
+    """`axes`: as_rotary_axis_t instances, see include/as_layer.h."""
+    array = (as_rotary_axis_t * len(axes))(*axes)
+    _check(lib().as_rotary_table(array, len(axes), table_ptr or None, stream_ptr or None), "as_rotary_table")
+
+
+def as_qk_norm_rotary(args, stream_ptr) -> None:
+    """`args`: an as_qk_norm_rotary_t."""
+    _check(lib().as_qk_norm_rotary(C.addressof(args), stream_ptr or None), "as_qk_norm_rotary")
+
+
+def as_qk_norm_rotary_backward(args, stream_ptr) -> None:
+    """`args`: an as_qk_norm_rotary_backward_t."""
+    _check(lib().as_qk_norm_rotary_backward(C.addressof(args), stream_ptr or None), "as_qk_norm_rotary_backward")
+
+
+def as_qk_norm_rotary_backward_workspace_bytes(args) -> int:
+    n = C.c_uint64()
+    _check(lib().as_qk_norm_rotary_backward_workspace_bytes(C.addressof(args), C.byref(n)), "as_qk_norm_rotary_backward_workspace_bytes")
+    return n.value
+
+
+def as_linear(ctx, args, stream_ptr) -> None:
+    """`args`: an as_linear_t."""
+    _check(lib().as_linear(ctx, C.addressof(args), stream_ptr or None), "as_linear")
+
+
+def as_linear_workspace_bytes(ctx, args) -> int:
+    n = C.c_uint64()
+    _check(lib().as_linear_workspace_bytes(ctx, C.addressof(args), C.byref(n)), "as_linear_workspace_bytes")
+    return n.value
+
+
+def as_linear_backward(ctx, args, stream_ptr) -> None:
+    """`args`: an as_linear_backward_t."""
+    _check(lib().as_linear_backward(ctx, C.addressof(args), stream_ptr or None), "as_linear_backward")
+
+
+def as_linear_backward_workspace_bytes(ctx, args) -> int:
+    n = C.c_uint64()
+    _check(lib().as_linear_backward_workspace_bytes(ctx, C.addressof(args), C.byref(n)), "as_linear_backward_workspace_bytes")
+    return n.value

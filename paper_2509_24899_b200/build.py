@@ -1,5 +1,5 @@
 """Builds libas_hybrid_attn.so in-tree with nvcc for sm_100a (cross-compiles without a GPU), and beside it as_torch_calls.so, the module of the calls that take
-PyTorch tensors (csrc/torch_calls.cpp), with g++."""
+PyTorch tensors (csrc/torch_calls.cpp, torch_layer_calls.cpp), with g++."""
 from __future__ import annotations
 
 import os
@@ -13,7 +13,8 @@ LIB = os.path.join(PKG, "lib", "libas_hybrid_attn.so")
 TORCH_CALLS = os.path.join(PKG, "lib", "as_torch_calls.so")
 BUILT_FOR = TORCH_CALLS + ".built_for"          # the PyTorch and Python that it was compiled against
 SOURCES = ["as_hybrid_attn.cu", "simt_path.cu", "tensor_init.cu", "tensor_qpass.cu", "tensor_qstream.cu", "tensor_kpass.cu", "backward_simt.cu", "backward_tensor.cu", "backward_tensor_d64.cu", "no_alloc.cu",
-           "block_rates.cu", "fp8_norm.cu", "fp8_matmul.cu"]
+           "block_rates.cu", "fp8_norm.cu", "fp8_matmul.cu", "rotary.cu", "linear.cu"]
+TORCH_SOURCES = ["torch_calls.cpp", "torch_layer_calls.cpp"]
 
 
 def _sources():
@@ -42,7 +43,7 @@ def torch_key() -> str:
 
 
 def _torch_calls_stale() -> bool:
-    if _older(TORCH_CALLS, [os.path.join(CSRC, "torch_calls.cpp")] + _headers()) or not os.path.exists(BUILT_FOR):
+    if _older(TORCH_CALLS, [os.path.join(CSRC, f) for f in TORCH_SOURCES + ["torch_args.h"]] + _headers()) or not os.path.exists(BUILT_FOR):
         return True
     with open(BUILT_FOR) as f:
         return f.read() != torch_key()
@@ -55,12 +56,12 @@ def build_torch_calls(force: bool = False) -> str:
     import sysconfig
 
     import torch
-    source = os.path.join(CSRC, "torch_calls.cpp")
+    sources = [os.path.join(CSRC, f) for f in TORCH_SOURCES]
     libs, inc = (os.path.join(os.path.dirname(torch.__file__), d) for d in ("lib", "include"))
     cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
            "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_paths()["include"], "-I", os.path.join(cuda, "include")]
-    cmd += ["-isystem", inc, "-isystem", os.path.join(inc, "torch", "csrc", "api", "include"), source, "-o", TORCH_CALLS, "-L", os.path.dirname(LIB), "-l:" + os.path.basename(LIB), "-Wl,-rpath,$ORIGIN",
+    cmd += ["-isystem", inc, "-isystem", os.path.join(inc, "torch", "csrc", "api", "include"), *sources, "-o", TORCH_CALLS, "-L", os.path.dirname(LIB), "-l:" + os.path.basename(LIB), "-Wl,-rpath,$ORIGIN",
             "-L", libs, "-ltorch_python", "-ltorch_cuda", "-ltorch_cpu", "-ltorch", "-lc10_cuda", "-lc10"]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:

@@ -19,7 +19,10 @@
 #include <new>
 
 #include "fp8_common.cuh"
+#include "fp8_context.h"
 #include "fp8_maps.h"
+#include "linear_plan.h"
+#include "sm100_pairs.cuh"
 #include "tensor_common.cuh"
 
 namespace {
@@ -63,38 +66,7 @@ struct MMParams {
   bool vec, copies;                         // results move 16 bytes at a time, or in boxes of 32 rows x 32 columns by TMA
 };
 
-// ---------------------------------------------------------------- instructions of CTA pairs and of the block-scaled kind
-template <int CG>
-AS_DEV void alloc_tmem(uint32_t slot) {
-  if constexpr (CG == 1) { tmem_alloc(slot, 512); tmem_relinquish(); }
-  else asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;\n\ttcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::"r"(slot) : "memory");
-}
-template <int CG>
-AS_DEV void free_tmem(uint32_t at) {
-  if constexpr (CG == 1) tmem_dealloc(at, 512);
-  else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(at) : "memory");
-}
-// Copy of a box; a pair's copies are told to the leading CTA's barrier, each lands in its own CTA's shared memory.
-template <int CG>
-AS_DEV void load_box(uint32_t dst, const CUtensorMap* m, uint32_t bar, int x, int y) {
-  if constexpr (CG == 1)
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(x), "r"(y) : "memory");
-  else
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4}], [%2];"
-                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(x), "r"(y) : "memory");
-}
-// Copy of a strip of results out: column of the head, token, head, batch entry.
-AS_DEV void store_box(const CUtensorMap* m, uint32_t src, int x, int t, int h, int b) {
-  asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];"
-               ::"l"(reinterpret_cast<uint64_t>(m)), "r"(src), "r"(x), "r"(t), "r"(h), "r"(b) : "memory");
-}
-// One arrival at `bar`, of both CTAs of a pair, when the MMAs issued so far have completed.
-template <int CG>
-AS_DEV void commit(uint32_t bar) {
-  if constexpr (CG == 1) tc_commit(bar);
-  else asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
-}
+// ---------------------------------------------------------------- instructions of the block-scaled kind
 template <int CG>
 AS_DEV void mma_scaled(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
   if constexpr (CG == 1)
@@ -110,18 +82,6 @@ AS_DEV void mma_scaled(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint3
 AS_DEV constexpr uint32_t scaled_idesc(int M, int N) { return (uint32_t)(N >> 3) << 17 | 1u << 23 | (uint32_t)(M >> 7) << 27; }
 AS_DEV constexpr uint32_t scale_byte_of(int k) { return (uint32_t)k << 4 | (uint32_t)k << 29; }
 
-AS_DEV uint32_t cta_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
-// The address of the leading CTA's copy of a shared-memory word, for arrivals and copies across the pair.
-AS_DEV uint32_t leaders(uint32_t addr) { uint32_t r; asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr)); return r; }
-// Arrives at the leading CTA's barrier behind this warp's accesses to tensor memory, which tcgen05.wait has seen to the end and tcgen05.fence orders: nothing else is
-// handed over, so nothing is released (a release to the cluster waits for the warp's stores to global memory, and an acquire of it by the warp that issues the MMAs took 700 clk
-// each time: 36 % of the products' time).
-template <int CG>
-AS_DEV void arrive_leader(uint32_t bar) {
-  if constexpr (CG == 1) mbar_arrive(bar);
-  else asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(leaders(bar)) : "memory");
-}
-AS_DEV void cluster_sync() { asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 AS_DEV void tmem_st4(uint32_t at, const uint32_t (&r)[4]) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
 }
@@ -129,13 +89,6 @@ AS_DEV void tmem_st8(uint32_t at, const uint32_t (&r)[8]) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
 }
-
-// A position in a ring of barriers: the slot, and the parity of the turn.
-struct Ring {
-  int slot = 0;
-  uint32_t turn = 0;
-  AS_DEV void next(int n) { if (++slot == n) { slot = 0; turn ^= 1u; } }
-};
 
 template <int CG>
 struct Ctx {
@@ -619,7 +572,6 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 1) few_rows_kernel(const __gri
 // for the meeting and the sums, and more with every CTA beyond two (128 x 1536 x 6144 14.0 us by single CTAs, 9.4 by three, 9.6 by five; 512 x 1536 x 6144 15.0, 11.5 by two, 13.2 by three;
 // 300 x 512 x 4096 10.1 and 8.0; but 512 x 1536 x 1536 5.9 and 8.1, 1024 x 512 x 2048 6.5 and 7.4).
 struct Tile { int cg, bn, parts; double ns; };
-constexpr int MAX_PARTS = 8;
 Tile tile_of(int M, int N, int kb, int sms, const int (&clusters)[MAX_PARTS + 1]) {
   static const int ns[2][7] = {{230, 250, 265, 300, 345, 385, 440}, {228, 230, 240, 262, 297, 320, 365}};
   Tile best{1, 32, 1, 1e300};
@@ -670,13 +622,6 @@ __global__ void take_status_kernel(uint32_t* status) { status[TAKEN] = atomicExc
 
 }  // namespace
 
-struct as_fp8_context_s {
-  int device = -1, sms = 0;
-  int clusters[MAX_PARTS + 1] = {};          // of so many CTAs that the device holds at once
-  uint32_t* status = nullptr;
-  std::mutex reading;                        // of the word behind the status word, where a read leaves what it took
-};
-
 extern "C" as_status_t as_fp8_create(as_fp8_context_t* out) {
   if (out == nullptr) return AS_ERR_INVALID_ARG;
   int dev = 0, major = 0, sms = 0;
@@ -684,7 +629,7 @@ extern "C" as_status_t as_fp8_create(as_fp8_context_t* out) {
       cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
     return failed();
   if (major != 10) return AS_ERR_ARCH;
-  if (as_tensor_init() != cudaSuccess || as_tc::opt_in_smem(matmul_kernel<1, false>, SMEM_MAX) != cudaSuccess || as_tc::opt_in_smem(matmul_kernel<2, false>, SMEM_MAX) != cudaSuccess ||
+  if (as_tensor_init() != cudaSuccess || as_linear_init() != cudaSuccess || as_tc::opt_in_smem(matmul_kernel<1, false>, SMEM_MAX) != cudaSuccess || as_tc::opt_in_smem(matmul_kernel<2, false>, SMEM_MAX) != cudaSuccess ||
       as_tc::opt_in_smem(matmul_kernel<1, true>, SMEM_MAX) != cudaSuccess ||
       as_tc::opt_in_smem(few_rows_kernel<1>, few_smem(1)) != cudaSuccess || as_tc::opt_in_smem(few_rows_kernel<2>, few_smem(2)) != cudaSuccess)
     return failed();

@@ -1,0 +1,983 @@
+// Linear layers in bf16: out = residual + gate * act(x w^T + bias), and the gradients dx = dz w, dw = dz^T x, on the tensor cores.
+//
+// One kernel does the three products; they differ in which of an operand's two indices lies in a run in memory, which the copies (boxes of 64 elements by rows) and the operand
+// descriptors say.  A pair of CTAs (cta_group::2) computes a tile of 256 rows by up to 256 columns: each holds 128 rows of the first operand, half of the tile's columns of the second
+// and 128 rows of results.  The grid is persistent, one CTA an SM; a tile's results are read out while the next one is computed, from the other of two accumulators.
+//
+//   warp 0       copies (TMA, 64 steps of the summed index a stage, 128-byte swizzle), told by the leading CTA's barrier
+//   warp 1       the MMAs (leading CTA only)
+//   warp 2       allocates tensor memory
+//   warps 4-11   results: tensor memory -> a strip of shared memory per warp (32 x 32 sums), read back so that 8 lanes hold a row's 32 columns: bias, activation, gate
+//                and residual go by 4 columns a lane, rows in runs of 64 or 128 bytes
+//
+// What bounds it is the tensor pipe and the operands' bytes into an SM, which for 256 x 256 are level: 64 bytes a clock beside 8192 operations.
+//
+// Where the tiles are too few for the SMs, the summed index is cut into parts; their sums go to the workspace in fp32 and finish_kernel adds them up in order.  Few rows of
+// x: linear_few_kernel, further down.
+#include <algorithm>
+
+#include "as_layer.h"
+#include "fp8_common.cuh"
+#include "fp8_context.h"
+#include "linear_plan.h"
+#include "sm100_pairs.cuh"
+#include "tensor_common.cuh"
+
+namespace {
+
+using namespace as_fp8;
+using namespace sm100;
+typedef __nv_bfloat16 bf;
+
+constexpr int LIN_THREADS = 384;
+constexpr int BM = LIN_BM, BK = LIN_BK;
+constexpr int MAX_STAGES = 10;
+constexpr int SMEM_MAX = 227 * 1024;
+constexpr uint32_t BOX = 64 * 128;          // bytes of a box of 64 x 64
+
+enum { B_FULL = 0, B_EMPTY = B_FULL + MAX_STAGES, B_AFULL = B_EMPTY + MAX_STAGES, B_AEMPTY = B_AFULL + 2, B_COUNT = B_AEMPTY + 2 };
+constexpr int STRIP = 32 * 128;
+constexpr int STRIPS_OFF = 1024;
+constexpr int STAGES_OFF = STRIPS_OFF + 8 * STRIP;
+static_assert(B_COUNT * 8 + 8 <= STRIPS_OFF && STAGES_OFF % 1024 == 0, "");
+
+// ---------------------------------------------------------------- what follows a sum
+struct Epilogue {
+  Rows out, res, pre;                        // data == nullptr: not there
+  const void *bias, *gate;
+  long long gate_stride;
+  unsigned gate_rows;                        // rows that share a gate
+  int N, act;
+  bool out_f32, res_f32, bias_f32, gate_f32;
+  bool vec;                                  // four columns move at once
+};
+
+AS_DEV float ld1(const void* p, bool f32, long long i) { return f32 ? static_cast<const float*>(p)[i] : __bfloat162float(static_cast<const bf*>(p)[i]); }
+AS_DEV float4 ld4(const void* p, bool f32, long long i) {
+  if (f32) return *reinterpret_cast<const float4*>(static_cast<const float*>(p) + i);
+  const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const bf*>(p) + i);
+  return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u));
+}
+AS_DEV void st4(void* p, bool f32, long long i, float4 v) {
+  if (f32) *reinterpret_cast<float4*>(static_cast<float*>(p) + i) = v;
+  else *reinterpret_cast<uint2*>(static_cast<bf*>(p) + i) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+}
+AS_DEV void st1(void* p, bool f32, long long i, float v) {
+  if (f32) static_cast<float*>(p)[i] = v;
+  else static_cast<bf*>(p)[i] = __float2bfloat16_rn(v);
+}
+
+// 1 / (1 + e^-x): e^-x is 2^(-x log2 e), infinite for what is far below 0, where the quotient is 0.
+AS_DEV float sigmoid(float x) { return __fdividef(1.f, 1.f + ex2(-1.442695041f * x)); }
+constexpr float GELU_A = 1.5957691216f, GELU_B = 0.044715f;      // 2 sqrt(2 / pi): gelu_tanh(z) = z sigmoid(A (z + B z^3)), as 1 + tanh(u) = 2 sigmoid(2 u)
+AS_DEV float activated(float z, int act) {
+  switch (act) {
+    case AS_ACT_RELU: return z < 0.f ? 0.f : z;                  // (NaN stays)
+    case AS_ACT_SILU: return z == -INFINITY ? 0.f : z * sigmoid(z);
+    case AS_ACT_GELU: return z == -INFINITY ? 0.f : 0.5f * z * erfcf(-0.7071067812f * z);
+    case AS_ACT_GELU_TANH: return z == -INFINITY ? 0.f : z * sigmoid(GELU_A * z * fmaf(GELU_B * z, z, 1.f));
+    default: return z;
+  }
+}
+// (act(z), act'(z))
+AS_DEV float2 activated2(float z, int act) {
+  switch (act) {
+    case AS_ACT_RELU: return make_float2(z < 0.f ? 0.f : z, z > 0.f ? 1.f : z != z ? z : 0.f);
+    case AS_ACT_SILU: {
+      const float s = sigmoid(z), t = sigmoid(-z);
+      return make_float2(z == -INFINITY ? 0.f : z * s, fabsf(z) > 200.f ? s : s * fmaf(z, t, 1.f));
+    }
+    case AS_ACT_GELU: {
+      const float c = 0.5f * erfcf(-0.7071067812f * z);
+      return make_float2(z == -INFINITY ? 0.f : z * c, fabsf(z) > 30.f ? c : fmaf(z * 0.3989422804f, ex2(-0.7213475204f * z * z), c));
+    }
+    case AS_ACT_GELU_TANH: {
+      const float q = GELU_B * z * z, u = GELU_A * z * (1.f + q), s = sigmoid(u), t = sigmoid(-u);
+      return make_float2(z == -INFINITY ? 0.f : z * s, fabsf(z) > 30.f ? s : fmaf(z * s, t * GELU_A * fmaf(3.f, q, 1.f), s));
+    }
+    default: return make_float2(z, 1.f);
+  }
+}
+
+// Sums of columns n .. n + 3 of row m, on to out and pre.
+struct Column4 { float4 bias; bool gates_alike; float4 gate; };
+AS_DEV Column4 columns_of(const Epilogue& e, int n) {
+  Column4 c{make_float4(0.f, 0.f, 0.f, 0.f), e.gate != nullptr && e.gate_rows == 0u, make_float4(1.f, 1.f, 1.f, 1.f)};
+  float *b = &c.bias.x, *g = &c.gate.x;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (n + i < e.N) {
+      if (e.bias != nullptr) b[i] = ld1(e.bias, e.bias_f32, n + i);
+      if (c.gates_alike) g[i] = ld1(e.gate, e.gate_f32, n + i);
+    }
+  return c;
+}
+AS_DEV void finish4(const Epilogue& e, const Column4& c, int m, int n, float4 v) {
+  v.x += c.bias.x; v.y += c.bias.y; v.z += c.bias.z; v.w += c.bias.w;
+  float* f = &v.x;
+  if (e.vec) {
+    if (e.pre.data != nullptr) st4(e.pre.data, false, e.pre.row((unsigned)m) + e.pre.col((unsigned)n), v);
+    if (e.act != AS_ACT_NONE) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) f[i] = activated(f[i], e.act);
+    }
+    if (e.gate != nullptr) {
+      const float4 g = c.gates_alike ? c.gate : ld4(e.gate, e.gate_f32, (long long)((unsigned)m / e.gate_rows) * e.gate_stride + n);
+      v.x *= g.x; v.y *= g.y; v.z *= g.z; v.w *= g.w;
+    }
+    if (e.res.data != nullptr) {
+      const float4 r = ld4(e.res.data, e.res_f32, e.res.row((unsigned)m) + e.res.col((unsigned)n));
+      v.x += r.x; v.y += r.y; v.z += r.z; v.w += r.w;
+    }
+    st4(e.out.data, e.out_f32, e.out.row((unsigned)m) + e.out.col((unsigned)n), v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (n + i >= e.N) continue;
+      float x = f[i];
+      if (e.pre.data != nullptr) st1(e.pre.data, false, e.pre.row((unsigned)m) + e.pre.col((unsigned)(n + i)), x);
+      x = activated(x, e.act);
+      if (e.gate != nullptr) x *= c.gates_alike ? (&c.gate.x)[i] : ld1(e.gate, e.gate_f32, (long long)((unsigned)m / e.gate_rows) * e.gate_stride + n + i);
+      if (e.res.data != nullptr) x += ld1(e.res.data, e.res_f32, e.res.row((unsigned)m) + e.res.col((unsigned)(n + i)));
+      st1(e.out.data, e.out_f32, e.out.row((unsigned)m) + e.out.col((unsigned)(n + i)), x);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- the products
+struct GemmParams {
+  Epilogue e;
+  float* part;                              // sums of parts [parts][M][pitch], or nullptr
+  uint32_t* status;
+  long long part_pitch, units;              // units: tiles x parts
+  int M, T, mt_entry;                       // rows of results in entries of T, of mt_entry tiles each
+  int bn, nt, stages, parts;
+  int ksteps, ks_entry;                     // steps of BK of the summed index, where it is rows: of an entry
+  int a_hd, b_hd;                           // columns of a head of the operands, multiples of 64 (INT32_MAX: there are no heads)
+};
+
+template <int CG>
+AS_DEV void load_box4(uint32_t dst, const CUtensorMap* m, uint32_t bar, int x, int t, int h, int b) {
+  if constexpr (CG == 1)
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(x), "r"(t), "r"(h), "r"(b) : "memory");
+  else
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4, %5, %6}], [%2];"
+                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(x), "r"(t), "r"(h), "r"(b) : "memory");
+}
+template <int CG>
+AS_DEV void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  if constexpr (CG == 1) mma_ss(d, a, b, idesc, accumulate);
+  else
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+
+template <int CG>
+struct Ctx {
+  uint32_t sbase, tmem;
+  WaitCtx wc;
+  uint32_t rank;                             // of the CTA in its pair
+  long long unit, step;                      // this pair's units: unit, unit + step, ...
+  AS_DEV uint32_t bar(int i) const { return sbase + 8 * i; }
+  AS_DEV bool wait(int i, uint32_t parity) const { return mbar_wait(bar(i), parity, wc); }
+};
+// A unit of work: a tile and a part of the summed index.
+struct Unit { int entry, t0, n0, k0, k1, part; };
+template <int CG>
+AS_DEV Unit unit_of(const GemmParams& p, long long u) {
+  Unit w;
+  const long long tile = u / p.parts;
+  w.part = (int)(u - tile * p.parts);
+  const int mt = (int)(tile / p.nt);
+  w.n0 = (int)(tile - (long long)mt * p.nt) * p.bn;
+  w.entry = mt / p.mt_entry;
+  w.t0 = (mt - w.entry * p.mt_entry) * (BM * CG);
+  w.k0 = (int)((long long)p.ksteps * w.part / p.parts);
+  w.k1 = (int)((long long)p.ksteps * (w.part + 1) / p.parts);
+  return w;
+}
+
+// A_MN, B_MN: the operand's rows or columns of the result lie in a run in memory (else the summed index does).
+template <int CG, bool A_MN, bool B_MN>
+AS_DEV void lin_copies(const GemmParams& p, const Ctx<CG>& c, const CUtensorMap* ma, const CUtensorMap* mb) {
+  const int rows_b = p.bn / CG;
+  const uint32_t stage_bytes = (uint32_t)(BM + rows_b) * BK * 2;
+  Ring r;
+  for (long long u = c.unit; u < p.units; u += c.step) {
+    const Unit w = unit_of<CG>(p, u);
+    const int m0 = w.t0 + (int)c.rank * BM, n0 = w.n0 + (int)c.rank * rows_b;
+    for (int k = w.k0; k < w.k1; ++k) {
+      if (!c.wait(B_EMPTY + r.slot, r.turn ^ 1u)) goto out;
+      {
+        const uint32_t at = c.sbase + STAGES_OFF + (uint32_t)r.slot * stage_bytes, bt = at + BM * BK * 2;
+        if (c.rank == 0) mbar_expect_tx(c.bar(B_FULL + r.slot), stage_bytes * CG);
+        const uint32_t bar = CG == 1 ? c.bar(B_FULL + r.slot) : leaders(c.bar(B_FULL + r.slot));
+        const int ke = A_MN ? k / p.ks_entry : 0, kt = (k - ke * p.ks_entry) * BK;       // entry and row of the summed index
+        if constexpr (A_MN) {
+#pragma unroll
+          for (int i = 0; i < BM / 64; ++i) {
+            const int col = m0 + 64 * i, h = col / p.a_hd;
+            load_box4<CG>(at + i * BOX, ma, bar, col - h * p.a_hd, kt, h, ke);
+          }
+        } else {
+          const int col = k * BK, h = col / p.a_hd;
+          load_box4<CG>(at, ma, bar, col - h * p.a_hd, m0, h, w.entry);
+        }
+        if constexpr (B_MN) {
+          for (int i = 0; i < rows_b / 64; ++i) {
+            const int col = n0 + 64 * i, h = col / p.b_hd;
+            load_box4<CG>(bt + i * BOX, mb, bar, col - h * p.b_hd, A_MN ? kt : k * BK, h, ke);
+          }
+        } else {
+          load_box4<CG>(bt, mb, bar, k * BK, n0, 0, 0);
+        }
+      }
+      r.next(p.stages);
+    }
+  }
+out:
+  // every copy has landed, and every MMA has read its operands, before the CTA may end
+  for (int s = 0; s < p.stages; ++s) {
+    if (!c.wait(B_EMPTY + r.slot, r.turn ^ 1u)) break;
+    r.next(p.stages);
+  }
+}
+
+template <int CG, bool A_MN, bool B_MN>
+AS_DEV void lin_issue(const GemmParams& p, const Ctx<CG>& c) {
+  const uint32_t stage_bytes = (uint32_t)(BM + p.bn / CG) * BK * 2;
+  const uint32_t idesc = make_idesc(BM * CG, 0, A_MN, B_MN) | (uint32_t)(p.bn >> 3) << 17;
+  Ring r;
+  uint32_t buf = 0, turn = 0;
+  for (long long u = c.unit; u < p.units; u += c.step) {
+    const Unit w = unit_of<CG>(p, u);
+    if (!c.wait(B_AEMPTY + buf, turn ^ 1u)) return;
+    const uint32_t d = c.tmem + buf * 256u;
+    for (int k = w.k0; k < w.k1; ++k) {
+      if (!c.wait(B_FULL + r.slot, r.turn)) return;
+      tc_fence_after();
+      const uint32_t at = c.sbase + STAGES_OFF + (uint32_t)r.slot * stage_bytes;
+      const uint64_t da = make_sdesc(at, A_MN ? BOX : 16, 1024), db = make_sdesc(at + BM * BK * 2, B_MN ? BOX : 16, 1024);
+#pragma unroll
+      for (int i = 0; i < BK / 16; ++i) mma<CG>(d, da + (A_MN ? 128 : 2) * i, db + (B_MN ? 128 : 2) * i, idesc, k > w.k0 || i > 0 ? 1u : 0u);
+      commit<CG>(c.bar(B_EMPTY + r.slot));
+      r.next(p.stages);
+    }
+    commit<CG>(c.bar(B_AFULL + buf));
+    buf ^= 1u;
+    if (buf == 0) turn ^= 1u;
+  }
+}
+
+// Results of a tile: this warp's 32 rows, every second 32 columns.
+template <int CG>
+AS_DEV void lin_results(const GemmParams& p, const Ctx<CG>& c, int lane, int warp) {
+  const int quarter = warp & 3, half = warp >> 2;
+  const uint32_t lanes = (uint32_t)quarter * 32u << 16;
+  const uint32_t strip = c.sbase + STRIPS_OFF + (uint32_t)warp * STRIP;
+  const int chunk = lane & 7;
+  uint32_t buf = 0, turn = 0;
+  for (long long u = c.unit; u < p.units; u += c.step) {
+    const Unit w = unit_of<CG>(p, u);
+    const int t0 = w.t0 + (int)c.rank * BM + quarter * 32, m0 = w.entry * p.T + t0, rows = min(32, p.T - t0);
+    if (!mbar_wait_warp(c.bar(B_AFULL + buf), turn, c.wc)) break;
+    tc_fence_after();
+    if (32 * half >= p.bn) {
+      __syncwarp();
+      if (lane == 0) arrive_leader<CG>(c.bar(B_AEMPTY + buf));
+    }
+    for (int c0 = 32 * half; c0 < p.bn; c0 += 64) {
+      const int n = w.n0 + c0 + 4 * chunk;
+      uint32_t x[32];
+      tmem_ld32(c.tmem + lanes + buf * 256u + c0, x);
+      Column4 cols{};
+      if (p.part == nullptr) cols = columns_of(p.e, n);
+      tmem_ld_wait(x);
+      if (c0 + 64 >= p.bn) {                  // this warp has read its part of the accumulator
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) arrive_leader<CG>(c.bar(B_AEMPTY + buf));
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(strip + swz128_chunk_offset(lane, i)), "r"(x[4 * i]), "r"(x[4 * i + 1]), "r"(x[4 * i + 2]), "r"(x[4 * i + 3]) : "memory");
+      __syncwarp();
+      if (n < p.e.N) {
+#pragma unroll 4
+        for (int i = 0; i < 8; ++i) {
+          const int r = i * 4 + lane / 8;
+          float4 v;
+          asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(strip + swz128_chunk_offset(r, chunk)) : "memory");
+          if (r >= rows) continue;
+          if (p.part != nullptr) *reinterpret_cast<float4*>(p.part + ((long long)w.part * p.M + m0 + r) * p.part_pitch + n) = v;
+          else finish4(p.e, cols, m0 + r, n, v);
+        }
+      }
+      __syncwarp();
+    }
+    buf ^= 1u;
+    if (buf == 0) turn ^= 1u;
+  }
+}
+
+template <int CG, bool A_MN, bool B_MN>
+__global__ void __launch_bounds__(LIN_THREADS, 1)
+linear_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb, const __grid_constant__ GemmParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);      // the same in both CTAs of a pair
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + 8 * B_COUNT);
+  volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem + 8 * B_COUNT + 4);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  Ctx<CG> c{smem_u32(smem), 0u, WaitCtx{p.status, abort_flag}, CG == 1 ? 0u : cta_rank(), blockIdx.x / CG, gridDim.x / CG};
+  if (threadIdx.x == 0) {
+    *abort_flag = 0u;
+    for (int s = 0; s < MAX_STAGES; ++s) { mbar_init(c.bar(B_FULL + s), 1); mbar_init(c.bar(B_EMPTY + s), 1); }
+    for (int s = 0; s < 2; ++s) { mbar_init(c.bar(B_AFULL + s), 1); mbar_init(c.bar(B_AEMPTY + s), 8 * CG); }
+    fence_barrier_init();
+    fence_proxy_async();
+    tma_prefetch_desc(&ma); tma_prefetch_desc(&mb);
+  }
+  if (warp == 2) { alloc_tmem<CG>(smem_u32(tmem_slot)); griddep_launch(); }
+  tc_fence_before();
+  __syncthreads();
+  if constexpr (CG == 2) cluster_sync();       // the peer's barriers stand before anything arrives there
+  tc_fence_after();
+  c.tmem = *tmem_slot;
+  griddep_wait();
+  if (warp == 0) {
+    if (elect_one()) lin_copies<CG, A_MN, B_MN>(p, c, &ma, &mb);
+    __syncwarp();
+  } else if (warp == 1) {
+    if (c.rank == 0 && elect_one()) lin_issue<CG, A_MN, B_MN>(p, c);
+    __syncwarp();
+  } else if (warp >= 4) {
+    lin_results<CG>(p, c, lane, warp - 4);
+  }
+  if (*abort_flag != 0u) {                     // a wait ran out: copies and MMAs under way get 20 us (they take two) before memory is given back
+    const long long t0 = clock64();
+    while (clock64() - t0 < 40000) {}
+  }
+  tc_fence_before();
+  __syncthreads();
+  if constexpr (CG == 2) cluster_sync();       // nothing of this CTA is reached from the other any more
+  if (warp == 2) {
+    tc_fence_after();
+    free_tmem<CG>(c.tmem);
+  }
+}
+
+// Sums of parts, in their order, and what follows them: four columns a thread.
+struct FinishParams { Epilogue e; const float* part; long long pitch; int M, parts; };
+__global__ void __launch_bounds__(256) finish_kernel(const __grid_constant__ FinishParams p) {
+  griddep_launch();
+  const int across = (int)(p.pitch / 4);
+  griddep_wait();
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < (long long)p.M * across; i += (long long)gridDim.x * 256) {
+    const int m = (int)(i / across), n = (int)(i - (long long)m * across) * 4;
+    if (n >= p.e.N) continue;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int q = 0; q < p.parts; ++q) {
+      const float4 x = *reinterpret_cast<const float4*>(p.part + ((long long)q * p.M + m) * p.pitch + n);
+      v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+    }
+    finish4(p.e, columns_of(p.e, n), m, n, v);
+  }
+}
+
+// ---------------------------------------------------------------- few rows
+// Few rows of x: w is read by all SMs, into the operands of the warps' own matrix instructions (16 rows of w, 8 of x, 16 columns), as a tile of the pair would be empty but for some rows
+// and few CTAs would walk all columns.  A CTA takes units of 16 rows of w by 8 NT of x; its warps take every sixteenth block of 64 columns each.  Which columns an instruction calls its
+// k-th does not matter as long as both operands agree: a lane holds columns 16 q .. 16 q + 15 of its rows' block.  The warps' sums meet in shared memory, in the order of the warps.
+// Bound by the bytes of w and the latency of memory: operands come by asynchronous copies into slots that a warp alone reads, blocks ahead and on into the next unit.
+constexpr int FEW_WARPS = 16, FEW_ROWS_W = 16;
+__host__ __device__ constexpr int few_ahead(int nt) { return nt == 1 ? 4 : 3; }
+__host__ __device__ constexpr int few_slot(int nt) { return (4 + 2 * nt) * 512; }
+constexpr int few_smem(int nt) { return FEW_WARPS * few_ahead(nt) * few_slot(nt); }
+
+struct FewParams {
+  Epilogue e;
+  Rows x;
+  const bf* w;
+  long long w_pitch;
+  int M, K, units, mt;                      // mt: units of 16 rows of w, one for each 8 NT rows of x
+};
+AS_DEV void few_copy_w(uint32_t dst, const void* src, int bytes) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory"); }
+AS_DEV void few_copy_x(uint32_t dst, const void* src, int bytes) { asm volatile("cp.async.ca.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory"); }
+AS_DEV void few_read(uint32_t at, uint32_t (&r)[4]) {
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+
+template <int NT>
+__global__ void __launch_bounds__(FEW_WARPS * 32, 1) linear_few_kernel(const __grid_constant__ FewParams p) {
+  constexpr int AHEAD = few_ahead(NT), SLOT = few_slot(NT);
+  griddep_launch();
+  extern __shared__ __align__(16) uint8_t slots[];
+  __shared__ float sums[2][FEW_WARPS][8 * NT][FEW_ROWS_W + 1];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane / 4, q = lane % 4;
+  const int kb = (p.K + BK - 1) / BK;
+  const uint32_t mine = smem_u32(slots) + (uint32_t)warp * (AHEAD * SLOT);
+  griddep_wait();
+  int unit = blockIdx.x, block = warp, slot = 0;                      // what is asked for next, and its first rows of w and x
+  int n1 = unit / p.mt * FEW_ROWS_W, m1 = unit % p.mt * (8 * NT);
+  auto ask = [&] {
+    if (block < kb && unit < p.units) {
+      const uint32_t own = mine + slot * SLOT + lane * 16;
+      const int c = block * BK + q * 16, n = n1 + g;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {                                   // 8 columns each
+        const int bytes = 2 * max(0, min(8, p.K - c - 8 * i)), c1 = bytes > 0 ? c + 8 * i : 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) few_copy_w(own + (2 * h + i) * 512, p.w + (long long)min(n + 8 * h, p.e.N - 1) * p.w_pitch + c1, bytes);
+        const long long col = p.x.col((unsigned)c1);
+#pragma unroll
+        for (int t = 0; t < NT; ++t)        // (a row that is not there leaves its results, which are not written, to chance)
+          if (m1 + 8 * t + g < p.M) few_copy_x(own + (4 + 2 * t + i) * 512, static_cast<const bf*>(p.x.data) + p.x.row((unsigned)(m1 + 8 * t + g)) + col, bytes);
+      }
+      if (++slot == AHEAD) slot = 0;
+      if ((block += FEW_WARPS) >= kb) {
+        block = warp;
+        unit += gridDim.x;
+        n1 = unit / p.mt * FEW_ROWS_W;
+        m1 = unit % p.mt * (8 * NT);
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");              // (an empty group where there is nothing left: the waits below count groups)
+  };
+#pragma unroll
+  for (int i = 0; i < AHEAD - 1; ++i) ask();
+  int take = 0, turn = 0;
+  for (int u = blockIdx.x; u < p.units; u += gridDim.x, turn ^= 1) {
+    float acc[NT][4] = {};
+    for (int k = warp; k < kb; k += FEW_WARPS) {
+      ask();                                                          // (a lane fills and reads its own 16 bytes of each piece: nothing to wait for in the other lanes)
+      asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD - 1) : "memory");
+      const uint32_t own = mine + take * SLOT + lane * 16;
+      if (++take == AHEAD) take = 0;
+      uint32_t w[2][2][4];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        few_read(own + i * 512, w[0][i]);
+        few_read(own + (2 + i) * 512, w[1][i]);
+      }
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        uint32_t x[2][4];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) few_read(own + (4 + 2 * t + i) * 512, x[i]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                       : "+f"(acc[t][0]), "+f"(acc[t][1]), "+f"(acc[t][2]), "+f"(acc[t][3])
+                       : "r"(w[0][i / 2][2 * (i % 2)]), "r"(w[1][i / 2][2 * (i % 2)]), "r"(w[0][i / 2][2 * (i % 2) + 1]), "r"(w[1][i / 2][2 * (i % 2) + 1]),
+                         "r"(x[i / 2][2 * (i % 2)]), "r"(x[i / 2][2 * (i % 2) + 1]));
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sums[turn][warp][8 * t + 2 * q + j % 2][g + 8 * (j / 2)] = acc[t][j];
+    __syncthreads();                                                  // (one for a unit: the next one's sums go to the other half)
+    if (threadIdx.x < 8 * NT * FEW_ROWS_W) {
+      const int i0 = threadIdx.x / FEW_ROWS_W, j = threadIdx.x % FEW_ROWS_W, n = u / p.mt * FEW_ROWS_W + j, m = u % p.mt * (8 * NT) + i0;
+      if (m < p.M && n < p.e.N) {
+        float f = 0.f;
+#pragma unroll
+        for (int i = 0; i < FEW_WARPS; ++i) f += sums[turn][i][i0][j];
+        const Epilogue& e = p.e;
+        if (e.bias != nullptr) f += ld1(e.bias, e.bias_f32, n);
+        if (e.pre.data != nullptr) st1(e.pre.data, false, e.pre.row((unsigned)m) + e.pre.col((unsigned)n), f);
+        f = activated(f, e.act);
+        if (e.gate != nullptr) f *= ld1(e.gate, e.gate_f32, (e.gate_rows == 0u ? 0ll : (long long)((unsigned)m / e.gate_rows) * e.gate_stride) + n);
+        if (e.res.data != nullptr) f += ld1(e.res.data, e.res_f32, e.res.row((unsigned)m) + e.res.col((unsigned)n));
+        st1(e.out.data, e.out_f32, e.out.row((unsigned)m) + e.out.col((unsigned)n), f);
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------- dz, and sums over rows
+// dz = dy * gate * act'(pre) in bf16, the sums of dz and of dy * act(pre) over runs of rows, which do not cross from one gate's rows to another's.  A lane has 8 columns, a warp
+// every eighth row of the run; the warps' sums meet in shared memory in their order.  One pass over dy and pre: HBM bytes.
+struct DzParams {
+  Rows dy, pre;
+  const void* gate;
+  bf* dz;                                    // [M][pitch], or nullptr
+  float *part_b, *part_g;                    // [gates * runs][N], or nullptr
+  long long gate_stride, pitch;
+  int N, act, rows_gate, runs;               // rows that share a gate; runs of them
+  bool dy_f32, gate_f32, vec;
+};
+constexpr int DZ_COLS = 256;
+
+__global__ void __launch_bounds__(256) dz_kernel(const __grid_constant__ DzParams p) {
+  griddep_launch();
+  __shared__ float room[8][DZ_COLS + 8];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int n = blockIdx.x * DZ_COLS + lane * 8, gate = blockIdx.y / p.runs, run = blockIdx.y - gate * p.runs;
+  const long long r0 = (long long)p.rows_gate * run / p.runs, r1 = (long long)p.rows_gate * (run + 1) / p.runs, first = (long long)gate * p.rows_gate;
+  griddep_wait();
+  float g[8], sb[8] = {}, sg[8] = {};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) g[i] = p.gate != nullptr && n + i < p.N ? ld1(p.gate, p.gate_f32, (long long)gate * p.gate_stride + n + i) : 1.f;
+  if (n < p.N) {
+#pragma unroll 2
+    for (long long r = r0 + warp; r < r1; r += 8) {
+      const unsigned m = (unsigned)(first + r);
+      float d[8], z[8] = {};
+      const long long dr = p.dy.row(m), pr = p.pre.data != nullptr ? p.pre.row(m) : 0;
+      if (p.vec) {
+        const long long dc = dr + p.dy.col((unsigned)n);
+        *reinterpret_cast<float4*>(d) = ld4(p.dy.data, p.dy_f32, dc);
+        *reinterpret_cast<float4*>(d + 4) = ld4(p.dy.data, p.dy_f32, dc + 4);
+        if (p.pre.data != nullptr) {
+          const uint4 w = *reinterpret_cast<const uint4*>(static_cast<const bf*>(p.pre.data) + pr + p.pre.col((unsigned)n));
+          const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) { z[2 * i] = __uint_as_float(u[i] << 16); z[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          d[i] = n + i < p.N ? ld1(p.dy.data, p.dy_f32, dr + p.dy.col((unsigned)(n + i))) : 0.f;
+          if (p.pre.data != nullptr) z[i] = n + i < p.N ? ld1(p.pre.data, false, pr + p.pre.col((unsigned)(n + i))) : 0.f;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float2 a = activated2(z[i], p.act);
+        sg[i] = fmaf(d[i], a.x, sg[i]);
+        d[i] = d[i] * g[i] * a.y;
+        sb[i] += d[i];
+      }
+      if (p.dz != nullptr) {
+        bf* at = p.dz + (long long)m * p.pitch + n;
+        if (n + 8 <= p.N) {
+          *reinterpret_cast<uint4*>(at) = make_uint4(pack_bf16(d[0], d[1]), pack_bf16(d[2], d[3]), pack_bf16(d[4], d[5]), pack_bf16(d[6], d[7]));
+        } else {
+          for (int i = 0; i < 8; ++i)
+            if (n + i < p.N) at[i] = __float2bfloat16_rn(d[i]);
+        }
+      }
+    }
+  }
+  auto leave = [&](const float (&s)[8], float* part) {
+    if (part == nullptr) return;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) room[warp][lane * 8 + i] = s[i];
+    __syncthreads();
+    const int c = blockIdx.x * DZ_COLS + threadIdx.x;
+    if (c < p.N) {
+      float f = 0.f;
+#pragma unroll
+      for (int w = 0; w < 8; ++w) f += room[w][threadIdx.x];
+      part[(long long)blockIdx.y * p.N + c] = f;
+    }
+  };
+  leave(sb, p.part_b);
+  leave(sg, p.part_g);
+}
+
+// Columns' sums over runs of rows, in order: block row 0 all of them (the bias), 1 + i those of gate i.
+struct ColumnSumParams { const float *part_b, *part_g; void *dbias, *dgate; int N, runs, gates; bool b_f32, g_f32; };
+__global__ void __launch_bounds__(256) column_sum_kernel(const __grid_constant__ ColumnSumParams p) {
+  griddep_launch();
+  __shared__ float some[8][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+  const bool of_bias = blockIdx.y == 0;
+  griddep_wait();
+  const float* part = of_bias ? p.part_b : p.part_g;
+  if (part == nullptr) return;
+  const long long first = of_bias ? 0 : (long long)(blockIdx.y - 1) * p.runs, rows = of_bias ? (long long)p.gates * p.runs : p.runs;
+  const long long r0 = first + rows * warp / 8, r1 = first + rows * (warp + 1) / 8;
+  float s = 0.f;
+  if (c < p.N) {
+#pragma unroll 8
+    for (long long r = r0; r < r1; ++r) s += part[r * p.N + c];
+  }
+  some[warp][lane] = s;
+  __syncthreads();
+  if (warp == 0 && c < p.N) {
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s += some[i][lane];
+    if (of_bias) st1(p.dbias, p.b_f32, c, s);
+    else st1(p.dgate, p.g_f32, (long long)(blockIdx.y - 1) * p.N + c, s);
+  }
+}
+
+// A matrix into rows a multiple of 16 bytes apart, for operands that the copies cannot read as they lie.
+struct GatherParams { Rows x; bf* out; long long pitch; int rows, cols; };
+__global__ void __launch_bounds__(256) gather_kernel(const __grid_constant__ GatherParams p) {
+  griddep_launch();
+  griddep_wait();
+  const int across = (p.cols + 255) / 256;
+  for (long long i = blockIdx.x; i < (long long)p.rows * across; i += gridDim.x) {
+    const int r = (int)(i / across), c = (int)(i - (long long)r * across) * 256 + threadIdx.x;
+    if (c < p.cols) p.out[(long long)r * p.pitch + c] = static_cast<const bf*>(p.x.data)[p.x.row((unsigned)r) + p.x.col((unsigned)c)];
+  }
+}
+
+// ---------------------------------------------------------------- host
+using as_lin::Plan;
+using as_lin::plan_of;
+
+template <int CG, bool A_MN, bool B_MN>
+cudaError_t launch(const CUtensorMap& ma, const CUtensorMap& mb, const GemmParams& p, int units, size_t smem, cudaStream_t st) {
+  cudaLaunchAttribute attr[2]{};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = CG; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(units * CG)); cfg.blockDim = dim3(LIN_THREADS); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+  cfg.attrs = attr; cfg.numAttrs = CG == 1 ? 1 : 2;
+  return cudaLaunchKernelEx(&cfg, linear_kernel<CG, A_MN, B_MN>, ma, mb, p);
+}
+
+// Whether four columns of a matrix move at once.
+bool vec4(const as_rows_t& x) {
+  return x.data == nullptr || (aligned(x.data, x.dtype == AS_DTYPE_BF16 ? 8 : 16) && ((x.head_dim | x.stride_batch | x.stride_head | x.stride_token) & 3) == 0);
+}
+
+// An operand as the copies read it: rows in entries of T.
+as_rows_t in_entries(as_rows_t x, long long rows, long long T) {
+  if (x.tokens == rows && T != rows) { x.stride_batch = T * x.stride_token; x.tokens = T; }
+  return x;
+}
+as_rows_t plain_rows(const void* data, long long rows, long long cols, long long pitch) {
+  as_rows_t x{};
+  x.data = const_cast<void*>(data); x.dtype = AS_DTYPE_BF16; x.head_dim = (int32_t)cols; x.tokens = rows; x.stride_token = pitch;
+  return x;
+}
+long long pitch_of(long long cols) { return (cols + 7) / 8 * 8; }
+uint64_t up256(uint64_t n) { return (n + 255) & ~255ull; }
+
+// Whether the copies can read a matrix as it lies: strides that are multiples of 16 bytes, heads that boxes of 64 columns do not cross.
+bool box_ok(const as_rows_t& x, long long rows, long long cols) {
+  if (x.dtype != AS_DTYPE_BF16 || !aligned(x.data, 16)) return false;
+  const long long heads = cols / x.head_dim, entries = rows / x.tokens;
+  if (heads > 1 && (x.head_dim % 64 != 0 || x.stride_head <= 0 || x.stride_head % 8 != 0)) return false;
+  if (x.tokens > 1 && (x.stride_token <= 0 || x.stride_token % 8 != 0)) return false;
+  return entries <= 1 || (x.stride_batch > 0 && x.stride_batch % 8 == 0);
+}
+// The same matrix without entries where their rows go on from one to the next.
+as_rows_t joined(as_rows_t x, long long rows) {
+  if (x.tokens != rows && (x.tokens == 1 || x.stride_batch == x.tokens * x.stride_token)) {
+    if (x.tokens == 1) x.stride_token = x.stride_batch;
+    x.tokens = rows;
+    x.stride_batch = 0;
+  }
+  return x;
+}
+// Entries of few rows leave the tiles of 256 (or steps of 64) that hold them empty: above 1.25 times the rows a copy is shorter.
+bool entries_ok(const as_rows_t& x, long long rows) {
+  if (x.tokens == rows) return true;
+  return (rows / x.tokens) * ((x.tokens + 255) / 256 * 256) * 4 <= std::max<long long>(rows, 256) * 5;
+}
+
+// What one product needs and where.
+struct Operand { as_rows_t rows; bool copy; as_rows_t from; };       // copy: `from` is brought into a dense form in the workspace first
+Operand operand_of(const as_rows_t& x, long long rows, long long cols) {
+  Operand o{joined(x, rows), false, x};
+  if (!box_ok(o.rows, rows, cols) || !entries_ok(o.rows, rows)) {
+    o.copy = true;
+    o.rows = plain_rows(nullptr, rows, cols, pitch_of(cols));
+  }
+  return o;
+}
+uint64_t copy_bytes(const Operand& o, long long rows) { return o.copy ? up256((uint64_t)rows * (uint64_t)o.rows.stride_token * 2) : 0; }
+
+cudaError_t run_copy(Operand& o, long long rows, long long cols, uint8_t*& room, int sms, cudaStream_t st) {
+  if (!o.copy) return cudaSuccess;
+  o.rows.data = room;
+  GatherParams g{};
+  g.x = rows_of(o.from, rows, cols);
+  g.out = reinterpret_cast<bf*>(room); g.pitch = o.rows.stride_token;
+  g.rows = (int)rows; g.cols = (int)cols;
+  room += copy_bytes(o, rows);
+  const long long pieces = rows * ((cols + 255) / 256);
+  return as_launch_dependent(gather_kernel, dim3((unsigned)std::min<long long>(pieces, 16ll * sms)), dim3(256), 0, st, g);
+}
+
+// One product on the tensor cores.  a [M, K] and b [N, K] by their meaning; A_MN, B_MN: they lie with M (N) in a run, as [K rows, M columns].
+struct Product {
+  as_rows_t a, b;
+  bool a_mn, b_mn;
+  long long M, N, K;                         // K: the summed index
+  long long T;                               // entries of the rows of results, or of the summed index where a_mn
+};
+uint64_t part_bytes(const Product& q, const Plan& plan) { return plan.parts == 1 ? 0 : up256((uint64_t)plan.parts * (uint64_t)q.M * (uint64_t)((q.N + 3) / 4 * 4) * 4); }
+Plan plan_for(const Product& q, int sms) {
+  const long long entries = q.a_mn ? 1 : q.M / q.T;
+  const long long ksteps = q.a_mn ? (q.K / q.T) * ((q.T + BK - 1) / BK) : (q.K + BK - 1) / BK;
+  return plan_of(entries, q.a_mn ? q.M : q.T, q.M, q.N, ksteps, q.b_mn, sms);
+}
+
+cudaError_t run_product(as_fp8_context_t h, const Product& q, const Epilogue& e, void* part, cudaStream_t st) {
+  const Plan plan = plan_for(q, h->sms);
+  GemmParams p{};
+  p.e = e;
+  p.status = h->status;
+  p.M = (int)q.M;
+  p.T = (int)(q.a_mn ? q.M : q.T);
+  p.mt_entry = (p.T + BM * plan.cg - 1) / (BM * plan.cg);
+  p.bn = plan.bn; p.parts = plan.parts;
+  p.nt = (int)((q.N + plan.bn - 1) / plan.bn);
+  p.ks_entry = (int)(q.a_mn ? (q.T + BK - 1) / BK : 1);
+  p.ksteps = (int)(q.a_mn ? (q.K / q.T) * p.ks_entry : (q.K + BK - 1) / BK);
+  p.units = (q.a_mn ? 1 : q.M / q.T) * p.mt_entry * (long long)p.nt * p.parts;
+  if (plan.parts > 1) { p.part = static_cast<float*>(part); p.part_pitch = (q.N + 3) / 4 * 4; }
+  const int stage = (BM + plan.bn / plan.cg) * BK * 2;
+  p.stages = std::min((SMEM_MAX - 1024 - STAGES_OFF) / stage, MAX_STAGES);
+  const size_t smem = 1024 + STAGES_OFF + (size_t)p.stages * stage;
+  CUtensorMap ma, mb;
+  const long long a_rows = q.a_mn ? q.K : q.M, a_cols = q.a_mn ? q.M : q.K, b_rows = q.b_mn ? q.K : q.N, b_cols = q.b_mn ? q.N : q.K;
+  // (boxes behind the last column of a matrix without heads begin at their column, a multiple of 64, not at what is left of it behind a "head" of any width: a copy has to begin on 16 bytes)
+  p.a_hd = q.a.head_dim == a_cols ? INT32_MAX : q.a.head_dim;
+  p.b_hd = q.b.head_dim == b_cols ? INT32_MAX : q.b.head_dim;
+  if (!as_tc::make_map_boxes(&ma, in_entries(q.a, a_rows, q.T), a_rows, a_cols, q.a_mn ? 64 : BM) ||
+      !as_tc::make_map_boxes(&mb, q.a_mn ? in_entries(q.b, b_rows, q.T) : q.b, b_rows, b_cols, q.b_mn ? 64 : plan.bn / plan.cg))
+    return cudaErrorInvalidValue;
+  const int units = (int)std::min<long long>(p.units, h->sms / plan.cg);
+  cudaError_t err;
+  if (plan.cg == 2) err = q.a_mn ? launch<2, true, true>(ma, mb, p, units, smem, st) : q.b_mn ? launch<2, false, true>(ma, mb, p, units, smem, st) : launch<2, false, false>(ma, mb, p, units, smem, st);
+  else err = q.a_mn ? launch<1, true, true>(ma, mb, p, units, smem, st) : q.b_mn ? launch<1, false, true>(ma, mb, p, units, smem, st) : launch<1, false, false>(ma, mb, p, units, smem, st);
+  if (err != cudaSuccess || plan.parts == 1) return err;
+  FinishParams f{};
+  f.e = e; f.part = p.part; f.pitch = p.part_pitch; f.M = p.M; f.parts = p.parts;
+  const long long pieces = (q.M * (p.part_pitch / 4) + 255) / 256;
+  return as_launch_dependent(finish_kernel, dim3((unsigned)std::min<long long>(pieces, 8ll * h->sms)), dim3(256), 0, st, f);
+}
+
+bool dtype_ok(int t) { return t == AS_DTYPE_BF16 || t == AS_DTYPE_F32; }
+bool act_ok(int a) { return a >= AS_ACT_NONE && a <= AS_ACT_GELU_TANH; }
+bool vector_ok(const void* p, int dtype) { return p == nullptr || (dtype_ok(dtype) && aligned(p, dtype == AS_DTYPE_BF16 ? 2 : 4)); }
+bool sizes_ok(long long rows, long long cols, long long out_cols) {
+  return rows >= 0 && rows <= (1ll << 30) && cols >= 1 && cols <= (1 << 20) && out_cols >= 1 && out_cols <= (1 << 20);
+}
+bool gate_ok(const void* gate, int dtype, long long gates, long long stride, long long rows, long long n) {
+  if (gate == nullptr) return true;
+  return vector_ok(gate, dtype) && gates >= 1 && gates <= 65534 && rows % gates == 0 && (gates == 1 || stride >= 0) && n >= 1;
+}
+bool heads_fit(const as_rows_t& x, long long cols) { return x.data == nullptr || x.head_dim == cols || cols * (long long)x.head_dim <= (1ll << 32); }
+
+as_status_t device_of(as_fp8_context_t h) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return failed();
+  return dev == h->device ? AS_OK : AS_ERR_INVALID_ARG;
+}
+
+as_status_t linear_ok(as_fp8_context_t h, const as_linear_t* a) {
+  if (h == nullptr || a == nullptr || a->struct_size != sizeof(as_linear_t) || !sizes_ok(a->rows, a->cols, a->out_cols) || !act_ok(a->activation)) return AS_ERR_INVALID_ARG;
+  if (!rows_ok(a->x, a->rows, a->cols) || a->x.dtype != AS_DTYPE_BF16 || !rows_ok(a->w, a->out_cols, a->cols) || a->w.dtype != AS_DTYPE_BF16 || a->w.head_dim != a->cols ||
+      a->w.tokens != a->out_cols)
+    return AS_ERR_INVALID_ARG;
+  if (!rows_ok(a->out, a->rows, a->out_cols) || !apart(a->out, a->rows, a->out_cols)) return AS_ERR_INVALID_ARG;
+  if (a->residual.data != nullptr && !rows_ok(a->residual, a->rows, a->out_cols)) return AS_ERR_INVALID_ARG;
+  if (a->pre.data != nullptr && (!rows_ok(a->pre, a->rows, a->out_cols) || a->pre.dtype != AS_DTYPE_BF16 || !apart(a->pre, a->rows, a->out_cols))) return AS_ERR_INVALID_ARG;
+  if (!vector_ok(a->bias, a->bias_dtype) || !gate_ok(a->gate, a->gate_dtype, a->gates, a->gate_stride, a->rows, a->out_cols)) return AS_ERR_INVALID_ARG;
+  if (!heads_fit(a->x, a->cols) || !heads_fit(a->out, a->out_cols) || !heads_fit(a->residual, a->out_cols) || !heads_fit(a->pre, a->out_cols)) return AS_ERR_UNSUPPORTED;
+  return AS_OK;
+}
+
+struct LinearPlan { Operand x, w; Product q; bool few; uint64_t bytes; };
+LinearPlan plan_linear(as_fp8_context_t h, const as_linear_t& a) {
+  LinearPlan l{};
+  l.w = operand_of(a.w, a.out_cols, a.cols);
+  // few rows read x where it lies: 8 columns at a time
+  l.few = a.rows <= 16;
+  l.x = operand_of(a.x, a.rows, a.cols);
+  if (l.few && aligned(a.x.data, 16) && ((a.x.stride_batch | a.x.stride_head | a.x.stride_token) & 7) == 0 && (a.x.head_dim == a.cols || a.x.head_dim % 8 == 0)) l.x = Operand{a.x, false, a.x};
+  l.q = Product{l.x.rows, l.w.rows, false, false, a.rows, a.out_cols, a.cols, l.x.rows.tokens};
+  l.bytes = copy_bytes(l.x, a.rows) + copy_bytes(l.w, a.out_cols);
+  if (!l.few) l.bytes += part_bytes(l.q, plan_for(l.q, h->sms));
+  return l;
+}
+bool workspace_ok(const void* p, uint64_t has, uint64_t need) { return need == 0 || (p != nullptr && aligned(p, 256) && has >= need); }
+
+}  // namespace
+
+cudaError_t as_linear_init() {
+  cudaError_t e = cudaSuccess;
+  auto opt = [&](auto kernel, int bytes) { if (e == cudaSuccess) e = as_tc::opt_in_smem(kernel, bytes); };
+  opt(linear_kernel<1, false, false>, SMEM_MAX); opt(linear_kernel<1, false, true>, SMEM_MAX); opt(linear_kernel<1, true, true>, SMEM_MAX);
+  opt(linear_kernel<2, false, false>, SMEM_MAX); opt(linear_kernel<2, false, true>, SMEM_MAX); opt(linear_kernel<2, true, true>, SMEM_MAX);
+  opt(linear_few_kernel<1>, few_smem(1)); opt(linear_few_kernel<2>, few_smem(2));
+  return e;
+}
+
+extern "C" as_status_t as_linear_workspace_bytes(as_fp8_context_t h, const as_linear_t* a, uint64_t* bytes) {
+  if (bytes == nullptr) return AS_ERR_INVALID_ARG;
+  if (const as_status_t s = linear_ok(h, a); s != AS_OK) return s;
+  *bytes = a->rows == 0 ? 0 : plan_linear(h, *a).bytes;
+  return AS_OK;
+}
+
+extern "C" as_status_t as_linear(as_fp8_context_t h, const as_linear_t* a, void* cuda_stream) {
+  if (const as_status_t s = linear_ok(h, a); s != AS_OK) return s;
+  if (const as_status_t s = device_of(h); s != AS_OK) return s;
+  if (a->rows == 0) return AS_OK;
+  LinearPlan l = plan_linear(h, *a);
+  if (!workspace_ok(a->workspace, a->workspace_bytes, l.bytes)) return AS_ERR_WORKSPACE;
+  const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  uint8_t* room = static_cast<uint8_t*>(a->workspace);
+  if (run_copy(l.x, a->rows, a->cols, room, h->sms, st) != cudaSuccess || run_copy(l.w, a->out_cols, a->cols, room, h->sms, st) != cudaSuccess) return failed();
+  Epilogue e{};
+  e.out = rows_of(a->out, a->rows, a->out_cols);
+  if (a->residual.data != nullptr) e.res = rows_of(a->residual, a->rows, a->out_cols);
+  if (a->pre.data != nullptr) e.pre = rows_of(a->pre, a->rows, a->out_cols);
+  e.bias = a->bias; e.gate = a->gate;
+  e.gate_stride = a->gate_stride;
+  e.gate_rows = a->gate != nullptr && a->gates > 1 ? (unsigned)(a->rows / a->gates) : 0u;
+  e.N = (int)a->out_cols; e.act = a->activation;
+  e.out_f32 = a->out.dtype == AS_DTYPE_F32; e.res_f32 = a->residual.dtype == AS_DTYPE_F32; e.bias_f32 = a->bias_dtype == AS_DTYPE_F32; e.gate_f32 = a->gate_dtype == AS_DTYPE_F32;
+  e.vec = a->out_cols % 4 == 0 && vec4(a->out) && vec4(a->residual) && vec4(a->pre) &&
+          (a->gate == nullptr || (aligned(a->gate, e.gate_f32 ? 16 : 8) && (a->gates == 1 || a->gate_stride % 4 == 0)));
+  if (l.few) {
+    FewParams p{};
+    p.e = e;
+    p.x = rows_of(l.x.rows, a->rows, a->cols);
+    p.w = static_cast<const bf*>(l.w.rows.data); p.w_pitch = l.w.rows.stride_token;
+    p.M = (int)a->rows; p.K = (int)a->cols;
+    p.mt = 1;
+    p.units = (e.N + FEW_ROWS_W - 1) / FEW_ROWS_W * p.mt;
+    const dim3 grid((unsigned)std::min(p.units, h->sms)), block(FEW_WARPS * 32);
+    const cudaError_t err = a->rows <= 8 ? as_launch_dependent(linear_few_kernel<1>, grid, block, few_smem(1), st, p) : as_launch_dependent(linear_few_kernel<2>, grid, block, few_smem(2), st, p);
+    return err == cudaSuccess ? AS_OK : failed();
+  }
+  l.q.a = l.x.rows; l.q.b = l.w.rows;
+  return run_product(h, l.q, e, room, st) == cudaSuccess ? AS_OK : failed();
+}
+
+namespace {
+
+struct BackPlan {
+  Operand x, w, dy;
+  bool dz, sums;                             // dz is computed (else dy is the operand as it lies); sums are taken
+  long long pitch;
+  int runs;
+  Product dx, dw;
+  uint64_t bytes;
+};
+
+as_status_t back_ok(as_fp8_context_t h, const as_linear_backward_t* a) {
+  if (h == nullptr || a == nullptr || a->struct_size != sizeof(as_linear_backward_t) || !sizes_ok(a->rows, a->cols, a->out_cols) || !act_ok(a->activation)) return AS_ERR_INVALID_ARG;
+  if (!rows_ok(a->dy, a->rows, a->out_cols)) return AS_ERR_INVALID_ARG;
+  const bool dx = a->dx.data != nullptr, dw = a->dw.data != nullptr;
+  if (dx && (!rows_ok(a->w, a->out_cols, a->cols) || a->w.dtype != AS_DTYPE_BF16 || a->w.head_dim != a->cols || a->w.tokens != a->out_cols)) return AS_ERR_INVALID_ARG;
+  if (dx && (!rows_ok(a->dx, a->rows, a->cols) || a->dx.dtype != AS_DTYPE_BF16 || !apart(a->dx, a->rows, a->cols))) return AS_ERR_INVALID_ARG;
+  if (dw && (!rows_ok(a->x, a->rows, a->cols) || a->x.dtype != AS_DTYPE_BF16)) return AS_ERR_INVALID_ARG;
+  if (dw && (!rows_ok(a->dw, a->out_cols, a->cols) || a->dw.dtype != AS_DTYPE_BF16 || a->dw.head_dim != a->cols || a->dw.tokens != a->out_cols || !apart(a->dw, a->out_cols, a->cols)))
+    return AS_ERR_INVALID_ARG;
+  const bool pre = a->pre.data != nullptr;
+  if (pre && (!rows_ok(a->pre, a->rows, a->out_cols) || a->pre.dtype != AS_DTYPE_BF16)) return AS_ERR_INVALID_ARG;
+  if (!pre && (a->activation != AS_ACT_NONE || a->dgate != nullptr)) return AS_ERR_INVALID_ARG;
+  if (!vector_ok(a->dbias, a->bias_dtype) || !vector_ok(a->dgate, a->gate_dtype) || (a->dgate != nullptr && a->gate == nullptr)) return AS_ERR_INVALID_ARG;
+  if (!gate_ok(a->gate, a->gate_dtype, a->gates, a->gate_stride, a->rows, a->out_cols)) return AS_ERR_INVALID_ARG;
+  if (!heads_fit(a->dy, a->out_cols) || !heads_fit(a->pre, a->out_cols) || (dw && !heads_fit(a->x, a->cols)) || !heads_fit(a->dx, a->cols)) return AS_ERR_UNSUPPORTED;
+  return AS_OK;
+}
+
+BackPlan plan_back(as_fp8_context_t h, const as_linear_backward_t& a) {
+  BackPlan b{};
+  const bool dx = a.dx.data != nullptr, dw = a.dw.data != nullptr;
+  b.sums = a.dbias != nullptr || a.dgate != nullptr;
+  b.dy = operand_of(a.dy, a.rows, a.out_cols);
+  b.x = dw ? operand_of(a.x, a.rows, a.cols) : Operand{};
+  b.w = dx ? operand_of(a.w, a.out_cols, a.cols) : Operand{};
+  // entries of x and of dy that differ: dy goes through dz
+  b.dz = (dx || dw) && (a.activation != AS_ACT_NONE || a.gate != nullptr || b.dy.copy || (dw && b.dy.rows.tokens != a.rows && b.x.rows.tokens != b.dy.rows.tokens));
+  b.pitch = pitch_of(a.out_cols);
+  const long long gates = a.gate != nullptr ? a.gates : 1, across = (a.out_cols + DZ_COLS - 1) / DZ_COLS, rows_gate = a.rows / gates;
+  b.runs = (int)std::max<long long>(1, std::min<long long>((4ll * h->sms + across * gates - 1) / (across * gates), rows_gate / 16));
+  if (b.dz) b.bytes += up256((uint64_t)a.rows * (uint64_t)b.pitch * 2);
+  if (a.dbias != nullptr) b.bytes += up256((uint64_t)gates * b.runs * a.out_cols * 4);
+  if (a.dgate != nullptr) b.bytes += up256((uint64_t)gates * b.runs * a.out_cols * 4);
+  b.bytes += copy_bytes(b.x, a.rows) + copy_bytes(b.w, a.out_cols);
+  const as_rows_t dz = b.dz ? plain_rows(nullptr, a.rows, a.out_cols, b.pitch) : b.dy.rows;
+  uint64_t parts = 0;
+  if (dx) {
+    b.dx = Product{dz, b.w.rows, false, true, a.rows, a.cols, a.out_cols, dz.tokens};
+    parts = std::max(parts, part_bytes(b.dx, plan_for(b.dx, h->sms)));
+  }
+  if (dw) {
+    const long long T = std::min(dz.tokens, b.x.rows.tokens);
+    b.dw = Product{dz, b.x.rows, true, true, a.out_cols, a.cols, a.rows, T};
+    parts = std::max(parts, part_bytes(b.dw, plan_for(b.dw, h->sms)));
+  }
+  b.bytes += parts;                          // (the products run one after another)
+  return b;
+}
+
+as_status_t zero(void* p, long long n, int dtype, cudaStream_t st) {
+  if (p == nullptr) return AS_OK;
+  return cudaMemsetAsync(p, 0, (size_t)n * (dtype == AS_DTYPE_BF16 ? 2 : 4), st) == cudaSuccess ? AS_OK : failed();
+}
+
+}  // namespace
+
+extern "C" as_status_t as_linear_backward_workspace_bytes(as_fp8_context_t h, const as_linear_backward_t* a, uint64_t* bytes) {
+  if (bytes == nullptr) return AS_ERR_INVALID_ARG;
+  if (const as_status_t s = back_ok(h, a); s != AS_OK) return s;
+  *bytes = a->rows == 0 ? 0 : plan_back(h, *a).bytes;
+  return AS_OK;
+}
+
+extern "C" as_status_t as_linear_backward(as_fp8_context_t h, const as_linear_backward_t* a, void* cuda_stream) {
+  if (const as_status_t s = back_ok(h, a); s != AS_OK) return s;
+  if (const as_status_t s = device_of(h); s != AS_OK) return s;
+  const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  if (a->rows == 0) {                        // sums over nothing
+    as_status_t s = zero(a->dbias, a->out_cols, a->bias_dtype, st);
+    if (s == AS_OK) s = zero(a->dgate, a->out_cols * a->gates, a->gate_dtype, st);
+    if (s == AS_OK && a->dw.data != nullptr && cudaMemset2DAsync(a->dw.data, (size_t)std::max<int64_t>(a->dw.stride_token, a->cols) * 2, 0, (size_t)a->cols * 2, (size_t)a->out_cols, st) != cudaSuccess)
+      s = failed();
+    return s;
+  }
+  BackPlan b = plan_back(h, *a);
+  if (!workspace_ok(a->workspace, a->workspace_bytes, b.bytes)) return AS_ERR_WORKSPACE;
+  uint8_t* room = static_cast<uint8_t*>(a->workspace);
+  const long long gates = a->gate != nullptr ? a->gates : 1;
+  DzParams z{};
+  z.dy = rows_of(a->dy, a->rows, a->out_cols);
+  if (a->pre.data != nullptr) z.pre = rows_of(a->pre, a->rows, a->out_cols);
+  z.gate = a->gate;
+  z.gate_stride = a->gate_stride;
+  z.pitch = b.pitch;
+  z.N = (int)a->out_cols; z.act = a->activation;
+  z.rows_gate = (int)(a->rows / gates); z.runs = b.runs;
+  z.dy_f32 = a->dy.dtype == AS_DTYPE_F32; z.gate_f32 = a->gate_dtype == AS_DTYPE_F32;
+  z.vec = a->out_cols % 8 == 0 && a->dy.head_dim % 8 == 0 && vec4(a->dy) && (a->pre.data == nullptr || rows_vec(a->pre, 16));
+  if (b.dz) { z.dz = reinterpret_cast<bf*>(room); room += up256((uint64_t)a->rows * (uint64_t)b.pitch * 2); }
+  const uint64_t sum_bytes = up256((uint64_t)gates * b.runs * a->out_cols * 4);
+  if (a->dbias != nullptr) { z.part_b = reinterpret_cast<float*>(room); room += sum_bytes; }
+  if (a->dgate != nullptr) { z.part_g = reinterpret_cast<float*>(room); room += sum_bytes; }
+  if (gates * b.runs > 65535) return AS_ERR_UNSUPPORTED;
+  if (b.dz || b.sums) {
+    const dim3 grid((unsigned)((a->out_cols + DZ_COLS - 1) / DZ_COLS), (unsigned)(gates * b.runs));
+    if (as_launch_dependent(dz_kernel, grid, dim3(256), 0, st, z) != cudaSuccess) return failed();
+  }
+  if (b.sums) {
+    ColumnSumParams c{z.part_b, z.part_g, a->dbias, a->dgate, z.N, b.runs, (int)gates, a->bias_dtype == AS_DTYPE_F32, z.gate_f32};
+    if (as_launch_dependent(column_sum_kernel, dim3((unsigned)((z.N + 31) / 32), (unsigned)(1 + (a->dgate != nullptr ? gates : 0))), dim3(256), 0, st, c) != cudaSuccess) return failed();
+  }
+  if (run_copy(b.x, a->rows, a->cols, room, h->sms, st) != cudaSuccess || run_copy(b.w, a->out_cols, a->cols, room, h->sms, st) != cudaSuccess) return failed();
+  const as_rows_t dz = b.dz ? plain_rows(z.dz, a->rows, a->out_cols, b.pitch) : b.dy.rows;
+  Epilogue e{};
+  e.N = (int)a->cols; e.act = AS_ACT_NONE;
+  if (a->dx.data != nullptr) {
+    b.dx.a = dz; b.dx.b = b.w.rows;
+    e.out = rows_of(a->dx, a->rows, a->cols);
+    e.vec = a->cols % 4 == 0 && vec4(a->dx);
+    if (run_product(h, b.dx, e, room, st) != cudaSuccess) return failed();
+  }
+  if (a->dw.data != nullptr) {
+    b.dw.a = dz; b.dw.b = b.x.rows;
+    e.out = rows_of(a->dw, a->out_cols, a->cols);
+    e.vec = a->cols % 4 == 0 && vec4(a->dw);
+    if (run_product(h, b.dw, e, room, st) != cudaSuccess) return failed();
+  }
+  return AS_OK;
+}

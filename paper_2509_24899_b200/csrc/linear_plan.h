@@ -1,0 +1,52 @@
+// The shape of a product's tiles, and the tensor maps of its operands.  Host code without CUDA calls.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+
+#include "as_fp8.h"
+
+constexpr int LIN_BM = 128;                  // rows of results of a CTA
+constexpr int LIN_BK = 64;                   // steps of the summed index of a stage
+
+namespace as_lin {
+
+// cg: CTAs that share a tile's rows; bn: its columns; parts: of the summed index.
+struct Plan { int cg, bn, parts; double ns; };
+
+// By the time that the turns of all SMs take: turns x steps x ns a step, and what the reading out of the last turn and the meeting of a pair add.  A part more costs its sums'
+// way to the workspace and back, and a launch.
+inline Plan plan_of(long long entries, long long T, long long M, long long N, long long ksteps, bool b_mn, int sms) {
+  static const int ns[2][8] = {{230, 250, 265, 300, 345, 385, 440, 500}, {228, 230, 240, 262, 297, 320, 365, 410}};
+  Plan best{1, 64, 1, 1e300};
+  for (int cg = 1; cg <= 2; ++cg)
+    for (int i = 0; i < 8; ++i) {
+      const int bn = 32 * (i + 1);
+      if (b_mn && bn % (64 * cg) != 0) continue;
+      const long long tiles = entries * ((T + LIN_BM * cg - 1) / (LIN_BM * cg)) * ((N + bn - 1) / bn), units = sms / cg;
+      for (int parts = 1; parts <= 16 && parts <= ksteps; ++parts) {
+        if (parts > 1 && tiles * parts > 2 * units) break;
+        const long long all = tiles * parts, whole = (all + units - 1) / units;
+        const double turns = whole == 1 ? 1. : 0.5 * ((double)all / units + whole);
+        double t = turns * (double)((ksteps + parts - 1) / parts) * ns[cg - 1][i] + 10. * bn + (cg == 2 ? 400. : 0.);
+        if (parts > 1) t += 3000. + (double)M * (double)N * 4. * (parts + 1) / 6000.;
+        if (t < best.ns) best = {cg, bn, parts, t};
+      }
+    }
+  return best;
+}
+
+}  // namespace as_lin
+
+namespace as_tc {
+
+// A bf16 matrix [rows, cols] in rows or heads as a 4-D tensor: column of a head, token, head, batch entry; boxes of 64 columns x box_rows tokens with the 128-byte swizzle; what
+// lies outside reads as 0.  (Defined in tensor_init.cu.)
+bool make_map_boxes(CUtensorMap* m, const as_rows_t& x, long long rows, long long cols, int box_rows);
+
+}  // namespace as_tc
+
+// Per-device set-up of the linear layers' kernels (shared-memory opt-in).
+cudaError_t as_linear_init();

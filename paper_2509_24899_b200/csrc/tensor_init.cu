@@ -4,6 +4,7 @@
 
 #include "backward_common.h"
 #include "fp8_maps.h"
+#include "linear_plan.h"
 #include "tensor_common.cuh"
 
 namespace {
@@ -38,17 +39,24 @@ bool as_tc::make_map_bytes(CUtensorMap* m, const void* base, long long cols, lon
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-bool as_tc::make_map_rows(CUtensorMap* m, const as_rows_t& x, long long rows, long long cols, int box_rows) {
+namespace {
+
+bool map_rows(CUtensorMap* m, const as_rows_t& x, long long rows, long long cols, int box_cols, int box_rows, CUtensorMapSwizzle swizzle) {
   if (g_encode == nullptr) return false;
   cuuint64_t dims[4] = {(cuuint64_t)x.head_dim, (cuuint64_t)x.tokens, (cuuint64_t)(cols / x.head_dim), (cuuint64_t)(rows / x.tokens)};
   cuuint64_t strides[3] = {(cuuint64_t)x.stride_token * 2, (cuuint64_t)x.stride_head * 2, (cuuint64_t)x.stride_batch * 2};
   for (int i = 0; i < 3; ++i)
     if (dims[i + 1] == 1) strides[i] = (cuuint64_t)(x.head_dim * 2 + 15) / 16 * 16;         // of one entry: not used, but not 0
-  cuuint32_t box[4] = {32u, (cuuint32_t)box_rows, 1u, 1u};
+  cuuint32_t box[4] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1u, 1u};
   cuuint32_t estr[4] = {1u, 1u, 1u, 1u};
-  return g_encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, x.data, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B,
+  return g_encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, x.data, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+
+}  // namespace
+
+bool as_tc::make_map_rows(CUtensorMap* m, const as_rows_t& x, long long rows, long long cols, int box_rows) { return map_rows(m, x, rows, cols, 32, box_rows, CU_TENSOR_MAP_SWIZZLE_64B); }
+bool as_tc::make_map_boxes(CUtensorMap* m, const as_rows_t& x, long long rows, long long cols, int box_rows) { return map_rows(m, x, rows, cols, 64, box_rows, CU_TENSOR_MAP_SWIZZLE_128B); }
 
 namespace {
 
