@@ -1,7 +1,7 @@
 // Norms of queries and keys, their rotation by the tokens' positions, and the gradients of both.
 //
-// All of it reads a tensor once and writes it once: bound by HBM bytes.  A lane holds 16 elements of a head in two pieces of 8, chosen so that both elements of a pair are
-// its own: 16 in a run (interleaved pairs, and what is not turned) or 8 of each half (pairs of halves).  The lanes of a head are a power of two, so that a head's sum is a few
+// All of it reads a tensor once and writes it once: bound by HBM bytes.  A lane holds 16 elements of a head in two pieces of 8, one of each half of what is turned (or of what is not): both
+// elements of a pair are its own in either layout, and the lanes of a head move runs of 128 bytes (16 elements in a run a lane, 32 bytes apart an access, cost a third more).  The lanes of a head are a power of two, so that a head's sum is a few
 // exchanges; a warp holds 32 / lanes heads a vector and NV vectors, and where the norm is over a token's heads up to 8 warps hold a row.  A token's cos and sin are the same for
 // every head and for queries and keys: a lane reads those of its 8 pairs once for all of them.  Heads whose sizes, strides or addresses are no multiples of 16 bytes go pair by
 // pair (turn_elements_kernel).
@@ -33,8 +33,8 @@ struct TableParams {
 };
 constexpr int TABLE_ROWS = 64;                 // of a CTA
 
-// A thread has one pair and walks over rows: its angle a position, in turns, is taken once.  cos and sin of a quarter turn around the next multiple of one, from an angle that 64 bits hold to
-// 2^-53 of the position's turns; rounded to fp32 there, it is 2^-24 relative.
+// A thread has one pair and walks over rows: its angle a position is taken once, in 64 bits.  cos and sin are those of what is left behind the next multiple of a quarter turn, whose
+// rounding to fp32 is relative to it.  (With turns in fp64, whose conversions are slow, 65536 positions of 32 pairs took 14 us.)
 __global__ void __launch_bounds__(THREADS) table_kernel(const __grid_constant__ TableParams p) {
   griddep_launch();
   const int pair = blockIdx.y * 64 + threadIdx.x % 64;
@@ -58,20 +58,21 @@ __global__ void __launch_bounds__(THREADS) table_kernel(const __grid_constant__ 
     f = f * g + f / x.factor * (1. - g);
     amplitude = 0.1 * log(x.factor) + 1.;
   }
+  // a position's angle in turns, as a fraction of 2^64: positions times it, and the turns that are dropped, are exact
   f /= tau;
+  const unsigned long long step = (unsigned long long)((f - floor(f)) * 18446744073709551616.);
   const int end = a + 1 < p.axes ? p.axis[min(a + 1, AS_ROTARY_MAX_AXES - 1)].first_row : p.rows;
   griddep_wait();
   const int row0 = blockIdx.x * TABLE_ROWS;
   for (int r = row0 + threadIdx.x / 64; r < min(row0 + TABLE_ROWS, p.rows); r += THREADS / 64) {
     float2 v = make_float2(0.f, 0.f);
     if (r >= x.first_row && r < end) {
-      const double turns = (r - x.first_row) * f, t = 4. * (turns - rint(turns)), q = rint(t);
+      const unsigned long long turns = (unsigned long long)(r - x.first_row) * step, q = (turns + (1ull << 61)) >> 62;       // the next multiple of a quarter turn
       float s, c;
-      sincospif(0.5f * (float)(t - q), &s, &c);
-      const int n = (int)q & 3;
-      const float cc = n & 1 ? s : c, ss = n & 1 ? c : s;
-      v.x = (float)(amplitude * (n == 1 || n == 2 ? -cc : cc));
-      v.y = (float)(amplitude * (n >= 2 ? -ss : ss));
+      sincospif(ldexpf((float)(long long)(turns - (q << 62)), -63), &s, &c);
+      const float cc = q & 1 ? s : c, ss = q & 1 ? c : s;
+      v.x = (q == 1 || q == 2 ? -cc : cc) * (float)amplitude;
+      v.y = (q >= 2 ? -ss : ss) * (float)amplitude;
     }
     p.out[(long long)r * p.pairs + pair] = v;
   }
@@ -94,18 +95,27 @@ struct TurnParams {
   int n_t, rows, tokens, d;
   int pairs, axes, half, pos64;
   int size[AS_ROTARY_MAX_AXES], first_row[AS_ROTARY_MAX_AXES], end[AS_ROTARY_MAX_AXES];      // end: of the axes' pairs
+  unsigned long long by_size[AS_ROTARY_MAX_AXES], by_tokens;       // 2^64 / n, rounded up (0: n is 1): a quotient is the upper half of a product, exact below 2^32
   float sign;                                // of sin
+  float over_n[2];                           // 1 / elements that a sum of squares goes over, of either tensor
   int w_f32;
   int lanes_log;                             // lanes of a head: 2^lanes_log
   int W;                                     // warps of a row
   int chunks;                                // runs of heads that a warp takes at once, where the norm is not over rows
 };
+AS_DEV unsigned quotient(unsigned i, unsigned long long by) { return by == 0ull ? i : (unsigned)__umul64hi(by, i); }
+struct Token { unsigned b, t; };
+AS_DEV Token token_of(const TurnParams& p, unsigned r) {
+  const unsigned b = p.tokens == p.rows ? 0u : quotient(r, p.by_tokens);
+  return {b, r - b * (unsigned)p.tokens};
+}
+AS_DEV long long address(const Rows& m, const Token& k) { return (long long)k.b * m.sb + (long long)k.t * m.st; }
 
 struct Where { int at[AS_ROTARY_MAX_AXES]; };
 // Rows of the table for row r; -1: no such position.
-AS_DEV Where where_of(const TurnParams& p, unsigned r) {
+AS_DEV Where where_of(const TurnParams& p, const Token& k) {
   Where w{};
-  const unsigned b = r / (unsigned)p.tokens, t = r - b * (unsigned)p.tokens;
+  const unsigned b = k.b, t = k.t;
   if (p.pos != nullptr) {
     const long long at = (long long)b * p.pos_stride + (long long)t * p.axes;
 #pragma unroll
@@ -119,7 +129,7 @@ AS_DEV Where where_of(const TurnParams& p, unsigned r) {
 #pragma unroll
     for (int a = AS_ROTARY_MAX_AXES - 1; a > 0; --a)
       if (a < p.axes) {
-        const unsigned q = i / (unsigned)p.size[a];
+        const unsigned q = quotient(i, p.by_size[a]);
         w.at[a] = p.first_row[a] + (int)(i - q * (unsigned)p.size[a]);
         i = q;
       }
@@ -136,26 +146,69 @@ AS_DEV float2 factor_of(const TurnParams& p, const Where& w, int pair) {
   f.y *= p.sign;
   return f;
 }
-// Of 8 pairs from a multiple of 8 on.
-AS_DEV void factors(const TurnParams& p, const Where& w, int pair, float2 (&f)[8]) {
-  const int a = axis_of(p, pair);
-  if (a == axis_of(p, pair + 7)) {
-    const int row = pick(w, a);
-    const float4* at = reinterpret_cast<const float4*>(p.table + (long long)max(row, 0) * p.pairs + pair);
+// Of 4 pairs from a multiple of 4 on, which belong to one axis or to two neighbours (or, rarely, to more).
+AS_DEV void factors(const TurnParams& p, const Where& w, int pair, float2* f) {
+  const int a = axis_of(p, pair), b = axis_of(p, pair + 3);
+  if (b - a > 1) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float4 v = __ldg(at + i);
-      if (row < 0) v.x = v.y = v.z = v.w = __uint_as_float(0x7fc00000u);
-      f[2 * i] = make_float2(v.x, v.y * p.sign);
-      f[2 * i + 1] = make_float2(v.z, v.w * p.sign);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = factor_of(p, w, pair + i);
+    for (int i = 0; i < 4; ++i) f[i] = factor_of(p, w, pair + i);
+    return;
   }
+  auto row = [&](int r, float2* to) {
+    const float4* at = reinterpret_cast<const float4*>(p.table + (long long)max(r, 0) * p.pairs + pair);
+    const float4 x = __ldg(at), y = __ldg(at + 1);
+    to[0] = make_float2(x.x, x.y); to[1] = make_float2(x.z, x.w); to[2] = make_float2(y.x, y.y); to[3] = make_float2(y.z, y.w);
+    if (p.pos != nullptr && r < 0) to[0] = to[1] = to[2] = to[3] = make_float2(__uint_as_float(0x7fc00000u), __uint_as_float(0x7fc00000u));
+  };
+  row(pick(w, a), f);
+  if (b != a) {
+    float2 g[4];
+    row(pick(w, b), g);
+    const int end = a == 0 ? p.end[0] : a == 1 ? p.end[1] : p.end[2];
+#pragma unroll
+    for (int i = 1; i < 4; ++i)
+      if (pair + i >= end) f[i] = g[i];
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f[i].y *= p.sign;
 }
 
 // ---------------------------------------------------------------- vectors of a lane
+// 16 elements of a head as the first and the second elements of 8 pairs, two pairs a register pair: arithmetic goes two values at a time.
+struct Pairs { float2 a[4], b[4]; };
+AS_DEV float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+AS_DEV float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\tfma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+AS_DEV float2 both(float x) { return make_float2(x, x); }
+AS_DEV float2 sub2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tsub.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+AS_DEV void scale(Pairs& v, float2 f) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { v.a[i] = mul2(v.a[i], f); v.b[i] = mul2(v.b[i], f); }
+}
+AS_DEV void scale(Pairs& v, const Pairs& w) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { v.a[i] = mul2(v.a[i], w.a[i]); v.b[i] = mul2(v.b[i], w.b[i]); }
+}
+AS_DEV float2 dot(const Pairs& v, const Pairs& w, float2 s) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { s = fma2(v.a[i], w.a[i], s); s = fma2(v.b[i], w.b[i], s); }
+  return s;
+}
+
 template <typename T> struct Raw { uint4 v[sizeof(T)]; };        // 16 elements: two pieces of 8
 template <typename T>
 AS_DEV void load(Raw<T>& r, const T* at, int second) {
@@ -165,25 +218,44 @@ AS_DEV void load(Raw<T>& r, const T* at, int second) {
     r.v[sizeof(T) / 2 + i] = *reinterpret_cast<const uint4*>(at + second + i * (16 / sizeof(T)));
   }
 }
+// From here on the compiler takes the words for others: what it has unpacked from them is unpacked again where it is used again, instead of kept in registers that there are not.
 template <typename T>
-AS_DEV void values(const Raw<T>& r, float (&f)[16]) {
+AS_DEV void again(Raw<T>& r) {
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(T); ++i) asm volatile("" : "+r"(r.v[i].x), "+r"(r.v[i].y), "+r"(r.v[i].z), "+r"(r.v[i].w));
+}
+// HALF: the pieces are the first and the second elements of 8 pairs; else each is 4 pairs.  (What is not turned may be called either.)
+template <bool HALF, typename T>
+AS_DEV void values(const Raw<T>& r, Pairs& f) {
   const uint32_t* w = reinterpret_cast<const uint32_t*>(r.v);
-  if constexpr (sizeof(T) == 2) {
+  auto lo = [](uint32_t x) { return __uint_as_float(x << 16); };
+  auto hi = [](uint32_t x) { return __uint_as_float(x & 0xffff0000u); };
 #pragma unroll
-    for (int i = 0; i < 8; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(w[i]);
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 2) {
+      if constexpr (HALF) { f.a[i] = make_float2(lo(w[i]), hi(w[i])); f.b[i] = make_float2(lo(w[4 + i]), hi(w[4 + i])); }
+      else { f.a[i] = make_float2(lo(w[2 * i]), lo(w[2 * i + 1])); f.b[i] = make_float2(hi(w[2 * i]), hi(w[2 * i + 1])); }
+    } else {
+      auto at = [&](int j) { return __uint_as_float(w[j]); };
+      if constexpr (HALF) { f.a[i] = make_float2(at(2 * i), at(2 * i + 1)); f.b[i] = make_float2(at(8 + 2 * i), at(9 + 2 * i)); }
+      else { f.a[i] = make_float2(at(4 * i), at(4 * i + 2)); f.b[i] = make_float2(at(4 * i + 1), at(4 * i + 3)); }
+    }
   }
 }
-template <typename T>
-AS_DEV void store(T* at, int second, const float (&f)[16]) {
+template <bool HALF, typename T>
+AS_DEV void store(T* at, int second, const Pairs& f) {
   uint4 v[sizeof(T)];
   uint32_t* w = reinterpret_cast<uint32_t*>(v);
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    if constexpr (sizeof(T) == 2) { if (i % 2 == 0) w[i / 2] = sm100::pack_bf16(f[i], f[i + 1]); }
-    else w[i] = __float_as_uint(f[i]);
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 2) {
+      if constexpr (HALF) { w[i] = sm100::pack_bf16(f.a[i].x, f.a[i].y); w[4 + i] = sm100::pack_bf16(f.b[i].x, f.b[i].y); }
+      else { w[2 * i] = sm100::pack_bf16(f.a[i].x, f.b[i].x); w[2 * i + 1] = sm100::pack_bf16(f.a[i].y, f.b[i].y); }
+    } else {
+      auto put = [&](int j, float x) { w[j] = __float_as_uint(x); };
+      if constexpr (HALF) { put(2 * i, f.a[i].x); put(2 * i + 1, f.a[i].y); put(8 + 2 * i, f.b[i].x); put(9 + 2 * i, f.b[i].y); }
+      else { put(4 * i, f.a[i].x); put(4 * i + 1, f.b[i].x); put(4 * i + 2, f.a[i].y); put(4 * i + 3, f.b[i].y); }
+    }
   }
 #pragma unroll
   for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
@@ -191,68 +263,76 @@ AS_DEV void store(T* at, int second, const float (&f)[16]) {
     *reinterpret_cast<uint4*>(at + second + i * (16 / sizeof(T))) = v[sizeof(T) / 2 + i];
   }
 }
-AS_DEV void load_weights(const TurnParams& p, const void* w, int at, int second, float (&f)[16]) {
+template <bool HALF>
+AS_DEV void load_weights(const TurnParams& p, const void* w, int at, int second, Pairs& f) {
   if (p.w_f32) {
     Raw<float> r;
     load(r, static_cast<const float*>(w) + at, second);
-    values(r, f);
+    values<HALF>(r, f);
   } else {
     Raw<bf> r;
     load(r, static_cast<const bf*>(w) + at, second);
-    values(r, f);
+    values<HALF>(r, f);
   }
 }
-AS_DEV void turn(float (&f)[16], const float2 (&cs)[8], int half) {
-  if (half) {
+// cos and sin of a lane's 8 pairs.
+struct Factors { float2 c[4], s[4]; };
+template <bool HALF>
+AS_DEV Factors factors_of(const TurnParams& p, const Token& k, int slot) {
+  float2 f[8];
+  const Where w = where_of(p, k);
+  factors(p, w, HALF ? slot * 8 : slot * 4, f);
+  factors(p, w, HALF ? slot * 8 + 4 : p.pairs / 2 + slot * 4, f + 4);
+  Factors t;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float a = f[i], b = f[8 + i];
-      f[i] = a * cs[i].x - b * cs[i].y;
-      f[8 + i] = a * cs[i].y + b * cs[i].x;
-    }
-  } else {
+  for (int i = 0; i < 4; ++i) { t.c[i] = make_float2(f[2 * i].x, f[2 * i + 1].x); t.s[i] = make_float2(f[2 * i].y, f[2 * i + 1].y); }
+  return t;
+}
+AS_DEV void turn(Pairs& v, const Factors& f) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float a = f[2 * i], b = f[2 * i + 1];
-      f[2 * i] = a * cs[i].x - b * cs[i].y;
-      f[2 * i + 1] = a * cs[i].y + b * cs[i].x;
-    }
+  for (int i = 0; i < 4; ++i) {
+    const float2 a = v.a[i], b = v.b[i];
+    v.a[i] = sub2(mul2(a, f.c[i]), mul2(b, f.s[i]));
+    v.b[i] = fma2(a, f.s[i], mul2(b, f.c[i]));
   }
 }
 
 // What a lane works on: its head of vector 0, elements of a head, whether they are turned.
-struct Lane { int head, heads_a_vector, e0, second, pair; bool in_head, turned; };
+struct Lane { int head, heads_a_vector, slot, e0, second; bool in_head, turned; };
 AS_DEV Lane lane_of(const TurnParams& p, int lane) {
   Lane l;
-  const int slot = lane & ((1 << p.lanes_log) - 1);
+  l.slot = lane & ((1 << p.lanes_log) - 1);
   l.head = lane >> p.lanes_log;
   l.heads_a_vector = 32 >> p.lanes_log;
-  l.in_head = slot * 16 < p.d;
-  l.pair = slot * 8;
-  l.turned = p.table != nullptr && l.pair < p.pairs;
-  const bool halves = l.turned && p.half;
-  l.e0 = halves ? slot * 8 : slot * 16;
-  l.second = halves ? p.pairs : 8;
+  l.in_head = l.slot * 16 < p.d;
+  l.turned = l.slot * 8 < p.pairs;
+  l.e0 = l.turned ? l.slot * 8 : p.pairs + l.slot * 8;             // what is not turned begins at 2 P, its slots at P / 8
+  l.second = l.turned ? p.pairs : (p.d - 2 * p.pairs) / 2;
   return l;
 }
 
-// Sum over a head's lanes, or over a row's lanes and warps (in the order of the warps).
-template <int NORM>
-AS_DEV float sum_of(const TurnParams& p, float s, float* part, int slot, int warp, int lane) {
-  if constexpr (NORM == AS_NORM_HEAD) {
-    for (int o = 1 << p.lanes_log >> 1; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-  } else {
+// Sums over a head's lanes, or over a row's lanes and warps (in the order of the warps), N at once.
+template <int NORM, int N>
+AS_DEV void sums_of(const TurnParams& p, float (&s)[N], float (&part)[N][WARPS], int slot, int warp, int lane) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  for (int k = 4; k >= 0; --k) {
+    if (NORM == AS_NORM_HEAD && k >= p.lanes_log) continue;
+#pragma unroll
+    for (int i = 0; i < N; ++i) s[i] += __shfl_xor_sync(0xffffffffu, s[i], 1 << k);
+  }
+  if constexpr (NORM == AS_NORM_ROW)
     if (p.W > 1) {                             // the same for every thread of the launch
       __syncthreads();                         // the sums before these have been read
-      if (lane == 0) part[warp] = s;
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (lane == 0) part[i][warp] = s[i];
       __syncthreads();
-      s = 0.f;
-      for (int i = 0; i < p.W; ++i) s += part[min(slot * p.W + i, WARPS - 1)];
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        s[i] = 0.f;
+        for (int w = 0; w < p.W; ++w) s[i] += part[i][min(slot * p.W + w, WARPS - 1)];
+      }
     }
-  }
-  return s;
 }
 // Whether any lane that takes part in the same exchanges asks for it.
 template <int NORM>
@@ -261,140 +341,160 @@ AS_DEV bool any_of(const TurnParams& p, bool ask) {
     if (p.W > 1) return __syncthreads_or(ask);
   return __any_sync(0xffffffffu, ask);
 }
-
-// x * factor * scale is the normed value.  `squares(f)`: the lane's sum of (f x)^2.  Rows whose squares fp32 does not hold, or whose squares vanish together with eps, are summed
-// again times a power of two.
-struct Scale { float factor, scale; };
-template <int NORM, typename F>
-AS_DEV Scale scale_of(const TurnParams& p, float n, bool live, float* part, int slot, int warp, int lane, F squares) {
-  const float sum = sum_of<NORM>(p, squares(1.f), part, slot, warp, lane), mean = sum / n + p.eps;
-  Scale s{1.f, rsqrtf(mean)};
-  const bool over = !(sum <= MOST), under = live && mean < LEAST;
-  if (any_of<NORM>(p, over || under)) {
-    const float f = over ? DOWN : under ? UP : 1.f;
-    const float again = sum_of<NORM>(p, squares(f), part, slot, warp, lane);
-    s = {f, rsqrtf(again / n + p.eps * f * f)};
-  }
-  return s;
-}
+// The normed value is x * factor * scale; factor is 1 but for rows whose squares fp32 does not hold, or whose squares vanish together with eps: those are summed again times a power
+// of two.
+AS_DEV bool over(float sum) { return !(sum <= MOST); }
+AS_DEV float factor_for(float sum, float over_n, float eps, bool there) { return over(sum) ? DOWN : there && fmaf(sum, over_n, eps) < LEAST ? UP : 1.f; }
 
 // ---------------------------------------------------------------- forward
-template <typename T, int NORM, int NV>
+// A warp holds a row of queries and one of keys (or pieces of them) at once.  What counts beside the bytes is the number of instructions: one value at a time, each vector of 16 elements a
+// lane took 340 of them, and 32760 tokens of 2 x 12 heads 106 us.
+template <typename T, int NORM, int NV, bool HALF>
 __global__ void __launch_bounds__(THREADS, 2) turn_kernel(const __grid_constant__ TurnParams p) {
   griddep_launch();
-  __shared__ float part[WARPS];
+  __shared__ float part[1][WARPS];
+  constexpr bool ROW = NORM == AS_NORM_ROW;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int slot = 0, piece;
-  long long row;
-  if constexpr (NORM == AS_NORM_ROW) {
-    const int per = WARPS / p.W;
-    slot = warp / p.W;
-    piece = warp - slot * p.W;
-    row = slot < per ? (long long)blockIdx.x * per + slot : p.rows;
-  } else {
-    const long long unit = (long long)blockIdx.x * WARPS + warp;
-    row = unit / p.chunks;
-    piece = (int)(unit - row * p.chunks);
-  }
-  const bool live = row < p.rows;
-  const unsigned r = live ? (unsigned)row : 0u;
+  const int per = ROW ? WARPS / p.W : WARPS, slot = ROW ? warp / p.W : warp, piece = ROW ? warp - slot * p.W : (int)blockIdx.y;
   const Lane l = lane_of(p, lane);
   const int h0 = piece * NV * l.heads_a_vector + l.head;
-  griddep_wait();
   constexpr int AHEAD = sizeof(T) == 2 ? 2 : 1;          // tensors whose loads are under way at once
   Raw<T> raw[AHEAD][NV];
-  auto fetch = [&](const TurnTensor& t, Raw<T> (&x)[NV]) {
-    const T* base = static_cast<const T*>(t.x.data) + t.x.row(r) + l.e0;
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int h = h0 + j * l.heads_a_vector;
-      x[j] = Raw<T>{};
-      if (live && l.in_head && h < t.heads) load(x[j], base + h * t.x.sh, l.second);
-    }
+  for (int i = 0; i < AHEAD; ++i)
+#pragma unroll
+    for (int j = 0; j < NV; ++j) raw[i][j] = Raw<T>{};
+  // vector j of row r, where there is one
+  auto fetch = [&](const TurnTensor& t, Raw<T>& x, const T* base, bool live, int j) {
+    const int h = h0 + j * l.heads_a_vector;
+    if (live && l.in_head && h < t.heads) load(x, base + h * t.x.sh, l.second);
+    else if (AHEAD == 1) x = Raw<T>{};                   // (registers that held the other tensor, which may have more heads)
   };
-  fetch(p.t[0], raw[0]);
-  if constexpr (AHEAD == 2)
-    if (p.n_t == 2) fetch(p.t[1], raw[1]);
-  float2 cs[8];
-  if (l.turned) factors(p, where_of(p, r), l.pair, cs);
+  auto base_of = [&](const TurnTensor& t, const Token& k) { return static_cast<const T*>(t.x.data) + address(t.x, k) + l.e0; };
+  long long row = (long long)blockIdx.x * per + slot;
+  bool live = slot < per && row < p.rows;
+  Token k = token_of(p, live ? (unsigned)row : 0u);
+  griddep_wait();
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i)
+    if (i < p.n_t) {
+      const T* base = base_of(p.t[i], k);
+#pragma unroll
+      for (int j = 0; j < NV; ++j) fetch(p.t[i], raw[i][j], base, live, j);
+    }
+  for (long long first = (long long)blockIdx.x * per; first < p.rows; first += (long long)gridDim.x * per) {        // a turn is one for the whole CTA
+  row += (long long)gridDim.x * per;
+  const bool more = slot < per && row < p.rows;
+  const Token next = token_of(p, more ? (unsigned)row : 0u);
+  Factors cs;
+  if (l.turned) cs = factors_of<HALF>(p, k, l.slot);
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     if (i >= p.n_t) break;
     const TurnTensor& t = p.t[i];
     Raw<T> (&x)[NV] = raw[AHEAD == 2 ? i : 0];
-    if constexpr (AHEAD == 1)
-      if (i == 1) fetch(t, x);
-    T* out = static_cast<T*>(t.o.data) + t.o.row(r) + l.e0;
-    Scale s{1.f, 1.f};
-    if constexpr (NORM == AS_NORM_ROW)
-      s = scale_of<NORM>(p, (float)t.heads * (float)p.d, live, part, slot, warp, lane, [&](float f) {
-        float a = 0.f, b = 0.f;
+    const T* ahead = base_of(AHEAD == 2 ? t : p.t[p.n_t == 2 ? 1 - i : 0], AHEAD == 2 || i == p.n_t - 1 ? next : k);      // what comes into these registers next
+    const bool wanted = AHEAD == 2 || i == p.n_t - 1 ? more : live;
+    T* out = static_cast<T*>(t.o.data) + address(t.o, k) + l.e0;
+    Pairs w;
+    if constexpr (NORM == AS_NORM_HEAD)
+      if (t.w != nullptr && l.in_head) load_weights<HALF>(p, t.w, l.e0, l.second, w);
+    float factor = 1.f, sum[1];                          // (the sum, and then the scale)
+    auto settle = [&](bool there, auto squares) {
+      auto take = [&] {
+        const float2 s = squares();
+        sum[0] = s.x + s.y;
+        sums_of<NORM>(p, sum, part, slot, warp, lane);
+      };
+      take();
+      factor = factor_for(sum[0], p.over_n[i], p.eps, there);
+      if (any_of<NORM>(p, factor != 1.f)) take();
+      sum[0] = rsqrtf(fmaf(sum[0], p.over_n[i], p.eps * factor * factor));
+    };
+    if constexpr (ROW) {
+      settle(live, [&] {
+        float2 s = both(0.f);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-          float v[16];
-          values(x[j], v);
-#pragma unroll
-          for (int e = 0; e < 16; e += 2) { a = fmaf(v[e] * f, v[e] * f, a); b = fmaf(v[e + 1] * f, v[e + 1] * f, b); }
+          Pairs v;
+          again(x[j]);
+          values<HALF>(x[j], v);
+          if (factor != 1.f) scale(v, both(factor));
+          s = dot(v, v, s);
         }
-        return a + b;
+        return s;
       });
+    }
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int h = h0 + j * l.heads_a_vector;
       const bool there = live && l.in_head && h < t.heads;
-      float v[16];
-      values(x[j], v);
-      if constexpr (NORM == AS_NORM_HEAD)
-        s = scale_of<NORM>(p, (float)p.d, there, part, slot, warp, lane, [&](float f) {
-          float a = 0.f, b = 0.f;
-#pragma unroll
-          for (int e = 0; e < 16; e += 2) { a = fmaf(v[e] * f, v[e] * f, a); b = fmaf(v[e + 1] * f, v[e + 1] * f, b); }
-          return a + b;
+      Pairs v;
+      if constexpr (ROW) again(x[j]);
+      values<HALF>(x[j], v);
+      fetch(AHEAD == 2 ? t : p.t[p.n_t == 2 ? 1 - i : 0], x[j], ahead, wanted, j);
+      if constexpr (NORM == AS_NORM_HEAD) {
+        factor = 1.f;
+        settle(there, [&] {
+          if (factor != 1.f) scale(v, both(factor));
+          return dot(v, v, both(0.f));
         });
+      }
       if (!there) continue;
       if constexpr (NORM != AS_NORM_NONE) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) v[e] = v[e] * s.factor * s.scale;
+        if (ROW && factor != 1.f) scale(v, both(factor));
+        scale(v, both(sum[0]));
         if (t.w != nullptr) {
-          float w[16];
-          load_weights(p, t.w, (NORM == AS_NORM_ROW ? h * p.d : 0) + l.e0, l.second, w);
-#pragma unroll
-          for (int e = 0; e < 16; ++e) v[e] *= w[e];
+          if constexpr (ROW) load_weights<HALF>(p, t.w, h * p.d + l.e0, l.second, w);
+          scale(v, w);
         }
       }
-      if (l.turned) turn(v, cs, p.half);
-      store(out + h * t.o.sh, l.second, v);
+      if (l.turned) turn(v, cs);
+      store<HALF>(out + h * t.o.sh, l.second, v);
     }
+  }
+  live = more;
+  k = next;
   }
 }
 
 // ---------------------------------------------------------------- backward
-// dx = r (g - n mean(g n)), g = d w, d = R^T dy, n = x r.  A CTA goes on from row to row and keeps its sums of d n in registers: of a head's elements where heads share the weights, else of all
-// of a row's.  Both sums of a row, over x^2 and over g x, are taken at once.
-template <typename T, int NORM, int NV>
-__global__ void __launch_bounds__(THREADS) turn_back_kernel(const __grid_constant__ TurnParams p) {
+// dx = r (g - n mean(g n)), g = d w, d = R^T dy, n = x r.  A CTA goes on from row to row of one tensor.  Each warp has its sums of d n in shared
+// memory (in registers, up to 48 of them, they left room for one CTA an SM).  Both sums of a row, over x^2 and over g x, are taken at once.
+template <typename T, int NORM, int NV, bool HALF>
+__global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) turn_back_kernel(const __grid_constant__ TurnParams p) {
   griddep_launch();
-  __shared__ float part[WARPS], part2[WARPS];
-  extern __shared__ float sums[];                        // of the weights' gradient, a row of them
+  __shared__ float part[2][WARPS];
+  extern __shared__ float4 sums[];                       // of d n, of each warp: [vectors][4][32 lanes]
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const TurnTensor& t = p.t[blockIdx.y];
   constexpr bool ROW = NORM == AS_NORM_ROW;
-  constexpr int NA = ROW ? NV : 1;
   const int per = ROW ? WARPS / p.W : WARPS;
   const int slot = ROW ? warp / p.W : warp, fixed_piece = ROW ? warp - slot * p.W : 0;
   const Lane l = lane_of(p, lane);
-  float acc[NA][16] = {};
-  const long long units = ROW ? p.rows : (long long)p.rows * p.chunks;
+  const bool sums_wanted = t.part != nullptr;
+  constexpr int NA = ROW ? NV : 1;                       // vectors of sums: heads share them, or each has its own
+  float4* mine = sums + warp * (NA * 128) + lane;
+  if (sums_wanted) {
+#pragma unroll
+    for (int i = 0; i < NA * 4; ++i) mine[i * 32] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  const int chunk = ROW ? 0 : (int)(blockIdx.x % (unsigned)p.chunks);
+  const unsigned first_cta = ROW ? blockIdx.x : blockIdx.x / (unsigned)p.chunks, ctas = ROW ? gridDim.x : gridDim.x / (unsigned)p.chunks;      // (gridDim.x is a multiple of chunks)
+  const int h0 = (ROW ? fixed_piece : chunk) * NV * l.heads_a_vector + l.head;
+  const float over_n = p.over_n[blockIdx.y];
   griddep_wait();
-  for (long long u0 = (long long)blockIdx.x * per; u0 < units; u0 += (long long)gridDim.x * per) {       // a turn is one for the whole CTA
-    const long long u = u0 + slot;
-    const bool live = slot < per && u < units;
-    const unsigned r = live ? (unsigned)(ROW ? u : u / p.chunks) : 0u;
-    const int h0 = (ROW ? fixed_piece : live ? (int)(u - (long long)r * p.chunks) : 0) * NV * l.heads_a_vector + l.head;
+  Pairs w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w.a[i] = w.b[i] = both(1.f);
+  if (!ROW && t.w != nullptr && l.in_head) load_weights<HALF>(p, t.w, l.e0, l.second, w);
+  for (long long u0 = (long long)first_cta * per; u0 < p.rows; u0 += (long long)ctas * per) {       // a turn is one for the whole CTA
+    const bool live = slot < per && u0 + slot < p.rows;
+    const Token tk = token_of(p, live ? (unsigned)(u0 + slot) : 0u);
     Raw<T> x[NV], y[NV];
-    const T* bx = static_cast<const T*>(t.x.data) + t.x.row(r) + l.e0;
-    const T* by = static_cast<const T*>(t.dy.data) + t.dy.row(r) + l.e0;
-    T* out = static_cast<T*>(t.o.data) + t.o.row(r) + l.e0;
+    const T* bx = static_cast<const T*>(t.x.data) + address(t.x, tk) + l.e0;
+    const T* by = static_cast<const T*>(t.dy.data) + address(t.dy, tk) + l.e0;
+    T* out = static_cast<T*>(t.o.data) + address(t.o, tk) + l.e0;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int h = h0 + j * l.heads_a_vector;
@@ -405,108 +505,142 @@ __global__ void __launch_bounds__(THREADS) turn_back_kernel(const __grid_constan
         load(y[j], by + h * t.dy.sh, l.second);
       }
     }
-    float2 cs[8];
-    if (l.turned) factors(p, where_of(p, r), l.pair, cs);
-    auto weights = [&](int h, float (&w)[16]) {
-      if (t.w != nullptr && l.in_head && h < t.heads) {
-        load_weights(p, t.w, (ROW ? h * p.d : 0) + l.e0, l.second, w);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) w[e] = 1.f;
+    Factors cs;
+    if (l.turned) cs = factors_of<HALF>(p, tk, l.slot);
+    // x and d of vector j, and its weights
+    auto operands = [&](int j, Pairs& v, Pairs& d) {
+      values<HALF>(x[j], v);
+      values<HALF>(y[j], d);
+      if (l.turned) turn(d, cs);
+      if constexpr (ROW) {
+        const int h = h0 + j * l.heads_a_vector;
+        if (t.w != nullptr && live && l.in_head && h < t.heads) load_weights<HALF>(p, t.w, h * p.d + l.e0, l.second, w);
       }
     };
-    auto gradient = [&](int j, float (&d)[16]) {
-      values(y[j], d);
-      if (l.turned) turn(d, cs, p.half);
+    float factor = 1.f, sum[2];                          // of (f x)^2 and of g f x; then the scale, and the mean of g n
+    auto settle = [&](bool there, auto sums_now) {
+      auto take = [&] {
+        float2 s[2] = {both(0.f), both(0.f)};
+        sums_now(s);
+        sum[0] = s[0].x + s[0].y;
+        sum[1] = s[1].x + s[1].y;
+        sums_of<NORM>(p, sum, part, slot, warp, lane);
+      };
+      take();
+      factor = factor_for(sum[0], over_n, p.eps, there);
+      if (any_of<NORM>(p, factor != 1.f)) take();
+      sum[0] = rsqrtf(fmaf(sum[0], over_n, p.eps * factor * factor));
+      sum[1] = sum[1] * sum[0] * over_n;
     };
-    // sums of vectors [j0, j1) -> the lane's parts of sum (f x)^2 and sum g f x
-    auto both = [&](int j0, int j1, float f) {
-      float a = 0.f, b = 0.f;
+    auto add = [&](const Pairs& v, Pairs d, float2 (&s)[2]) {
+      s[0] = dot(v, v, s[0]);
+      scale(d, w);
+      s[1] = dot(d, v, s[1]);
+    };
+    if constexpr (ROW)
+      settle(live, [&](float2 (&s)[2]) {
 #pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        if (j < j0 || j >= j1) continue;
-        float v[16], d[16], w[16];
-        values(x[j], v);
-        gradient(j, d);
-        weights(h0 + j * l.heads_a_vector, w);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) { const float xf = v[e] * f; a = fmaf(xf, xf, a); b = fmaf(d[e] * w[e], xf, b); }
-      }
-      return make_float2(a, b);
-    };
-    auto reduce = [&](float2 s) { return make_float2(sum_of<NORM>(p, s.x, part, slot, warp, lane), sum_of<NORM>(p, s.y, part2, slot, warp, lane)); };
-    Scale s{1.f, 1.f};
-    float along = 0.f;
-    auto settle = [&](int j0, int j1, float n, bool there) {
-      float2 q = reduce(both(j0, j1, 1.f));
-      const float mean = q.x / n + p.eps;
-      s = {1.f, rsqrtf(mean)};
-      const bool over = !(q.x <= MOST), under = there && mean < LEAST;
-      if (any_of<NORM>(p, over || under)) {
-        const float f = over ? DOWN : under ? UP : 1.f;
-        q = reduce(both(j0, j1, f));
-        s = {f, rsqrtf(q.x / n + p.eps * f * f)};
-      }
-      along = q.y * s.scale / n;                         // the mean of g n
-    };
-    if constexpr (ROW) settle(0, NV, (float)t.heads * (float)p.d, live);
+        for (int j = 0; j < NV; ++j) {
+          Pairs v, d;
+          again(x[j]);
+          again(y[j]);
+          operands(j, v, d);
+          if (factor != 1.f) scale(v, both(factor));
+          add(v, d, s);
+        }
+      });
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int h = h0 + j * l.heads_a_vector;
       const bool there = live && l.in_head && h < t.heads;
-      if constexpr (!ROW) settle(j, j + 1, (float)p.d, there);
-      if (!there) continue;
-      float v[16], d[16], w[16];
-      values(x[j], v);
-      gradient(j, d);
-      weights(h, w);
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float n = v[e] * s.factor * s.scale;
-        acc[ROW ? j : 0][e] = fmaf(d[e], n, acc[ROW ? j : 0][e]);
-        v[e] = (d[e] * w[e] - n * along) * s.scale * s.factor;
+      Pairs v, d;
+      if constexpr (ROW) { again(x[j]); again(y[j]); }
+      operands(j, v, d);
+      if constexpr (!ROW) {
+        factor = 1.f;
+        settle(there, [&](float2 (&s)[2]) {
+          if (factor != 1.f) scale(v, both(factor));
+          add(v, d, s);
+        });
       }
-      store(out + h * t.o.sh, l.second, v);
+      if (!there) continue;
+      if (ROW && factor != 1.f) scale(v, both(factor));
+      scale(v, both(sum[0]));
+      if (sums_wanted) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float4 q = mine[((ROW ? j : 0) * 4 + i) * 32];
+          const float2 qa = fma2(d.a[i], v.a[i], make_float2(q.x, q.y)), qb = fma2(d.b[i], v.b[i], make_float2(q.z, q.w));
+          mine[((ROW ? j : 0) * 4 + i) * 32] = make_float4(qa.x, qa.y, qb.x, qb.y);
+        }
+      }
+      scale(d, w);
+      const float2 along = both(-sum[1]), r2 = both(sum[0]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { d.a[i] = mul2(fma2(v.a[i], along, d.a[i]), r2); d.b[i] = mul2(fma2(v.b[i], along, d.b[i]), r2); }
+      if (factor != 1.f) scale(d, both(factor));
+      store<HALF>(out + h * t.o.sh, l.second, d);
     }
   }
-  if (t.part == nullptr) return;
-  // rows (and heads) of the CTA in a fixed order, then its row of partial sums
-  const int cols = ROW ? t.heads * p.d : p.d;
-  if constexpr (!ROW) {
+  if (!sums_wanted) return;
+  // the warps' sums in their order: the CTA's row of partial sums.  Element e of a lane's 16, in the order of Pairs' words: pairs 2 i, 2 i + 1 first, then their second elements
+  auto element = [&](int i, int e) {                     // word e of group i
+    const int pair = 2 * i + (e & 1), second = e >> 1;
+    return HALF ? (second ? l.second + pair : pair) : (2 * pair + second < 8 ? 2 * pair + second : l.second + 2 * pair + second - 8);
+  };
+  if constexpr (ROW) {
+    __syncthreads();
+    if (slot == 0) {                                     // of the rows that the CTA had at once, those of slot 0 add the others' up
 #pragma unroll
-    for (int e = 0; e < 16; ++e)
-      for (int o = 16; o >= 1 << p.lanes_log; o >>= 1) acc[0][e] += __shfl_xor_sync(0xffffffffu, acc[0][e], o);
-  }
-  for (int i = 0; i < per; ++i) {
-    if (slot == i && l.in_head && (ROW || l.head == 0)) {
+      for (int j = 0; j < NV; ++j) {
+        const int h = (fixed_piece * NV + j) * l.heads_a_vector + l.head;
+        if (!l.in_head || h >= t.heads) continue;
+        float* to = t.part + ((long long)blockIdx.x * t.heads + h) * p.d + l.e0;
 #pragma unroll
-      for (int j = 0; j < NA; ++j) {
-        const int h = ROW ? (fixed_piece * NV + j) * l.heads_a_vector + l.head : 0;
-        if (ROW && h >= t.heads) continue;
-        float* at = sums + (ROW ? h * p.d : 0) + l.e0;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          float* to = at + (e < 8 ? e : l.second + e - 8);
-          *to = i == 0 ? acc[j][e] : *to + acc[j][e];
+        for (int i = 0; i < 4; ++i) {
+          float4 q = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int k = 0; k < per; ++k) {
+            const float4 x = sums[(k * p.W + fixed_piece) * (NV * 128) + (j * 4 + i) * 32 + lane];
+            q.x += x.x; q.y += x.y; q.z += x.z; q.w += x.w;
+          }
+          to[element(i, 0)] = q.x; to[element(i, 1)] = q.y; to[element(i, 2)] = q.z; to[element(i, 3)] = q.w;
         }
       }
     }
+  } else {
     __syncthreads();
+    if (warp == 0) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < WARPS; ++k) {
+          const float4 x = sums[k * 128 + i * 32 + lane];
+          f.x += x.x; f.y += x.y; f.z += x.z; f.w += x.w;
+        }
+        float q[4] = {f.x, f.y, f.z, f.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          for (int o = 16; o >= 1 << p.lanes_log; o >>= 1) q[e] += __shfl_xor_sync(0xffffffffu, q[e], o);
+          if (l.in_head && l.head == 0) t.part[(long long)blockIdx.x * p.d + l.e0 + element(i, e)] = q[e];
+        }
+      }
+    }
   }
-  for (int c = threadIdx.x; c < cols; c += THREADS) t.part[(long long)blockIdx.x * cols + c] = sums[c];
 }
 
-// The weights' gradient from the CTAs' rows of partial sums, in their order: 32 columns a CTA, 8 runs of rows side by side.
+// The weights' gradient from the CTAs' rows of partial sums, in their order: 32 columns a CTA, 32 runs of rows side by side (8 runs: 10 us for 296 rows, all of it latency).
 struct SumParams { const float* part[2]; void* out[2]; int cols[2]; int rows, f32; };
-__global__ void __launch_bounds__(THREADS) turn_sum_kernel(const __grid_constant__ SumParams p) {
+constexpr int SUM_RUNS = 32;
+__global__ void __launch_bounds__(SUM_RUNS * 32) turn_sum_kernel(const __grid_constant__ SumParams p) {
   griddep_launch();
-  __shared__ float some[WARPS][32];
+  __shared__ float some[SUM_RUNS][33];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, i = blockIdx.y, c = blockIdx.x * 32 + lane, cols = i == 0 ? p.cols[0] : p.cols[1];
   griddep_wait();
   const float* part = i == 0 ? p.part[0] : p.part[1];
   void* out = i == 0 ? p.out[0] : p.out[1];
   if (part == nullptr || blockIdx.x * 32 >= cols) return;
-  const int r0 = (int)((long long)p.rows * warp / WARPS), r1 = (int)((long long)p.rows * (warp + 1) / WARPS);
+  const int r0 = p.rows * warp / SUM_RUNS, r1 = p.rows * (warp + 1) / SUM_RUNS;
   float s = 0.f;
   if (c < cols) {
 #pragma unroll 8
@@ -517,7 +651,7 @@ __global__ void __launch_bounds__(THREADS) turn_sum_kernel(const __grid_constant
   if (warp == 0 && c < cols) {
     s = 0.f;
 #pragma unroll
-    for (int j = 0; j < WARPS; ++j) s += some[j][lane];
+    for (int j = 0; j < SUM_RUNS; ++j) s += some[j][lane];
     if (p.f32) static_cast<float*>(out)[c] = s;
     else static_cast<bf*>(out)[c] = __float2bfloat16_rn(s);
   }
@@ -539,14 +673,14 @@ template <typename T, int NORM, bool BACK>
 __global__ void __launch_bounds__(THREADS) turn_elements_kernel(const __grid_constant__ TurnParams p) {
   griddep_launch();
   __shared__ float part[WARPS], part2[WARPS];
-  extern __shared__ float sums[];                        // backward: of the weights' gradient, a row of them for each warp or for the CTA
+  extern __shared__ float room[];                        // backward: of the weights' gradient, a row of them for each warp or for the CTA
   constexpr bool ROW = NORM == AS_NORM_ROW;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int which = BACK ? blockIdx.y : 0, np = p.d - p.pairs;           // pieces of a head
   const int cols = ROW ? (which == 0 ? p.t[0] : p.t[1]).heads * p.d : p.d;
-  float* mine = sums + (ROW ? 0 : warp * p.d);
+  float* mine = room + (ROW ? 0 : warp * p.d);
   if constexpr (BACK) {
-    for (int c = threadIdx.x; c < (ROW ? cols : WARPS * p.d); c += THREADS) sums[c] = 0.f;
+    for (int c = threadIdx.x; c < (ROW ? cols : WARPS * p.d); c += THREADS) room[c] = 0.f;
     __syncthreads();
   }
   griddep_wait();
@@ -562,20 +696,21 @@ __global__ void __launch_bounds__(THREADS) turn_elements_kernel(const __grid_con
     const unsigned r = (unsigned)(ROW ? v : v / t.heads);
     const int h_of = ROW ? 0 : (int)(v - (long long)r * t.heads);
     const int pieces = ROW ? t.heads * np : np, from = ROW ? threadIdx.x : lane, by = ROW ? THREADS : 32;
-    const T* x = static_cast<const T*>(t.x.data) + t.x.row(r);
-    const T* y = BACK ? static_cast<const T*>(t.dy.data) + t.dy.row(r) : nullptr;
-    T* out = static_cast<T*>(t.o.data) + t.o.row(r);
-    const Where at = p.table != nullptr ? where_of(p, r) : Where{};
-    auto sum = [&](float s, float* room) {
+    const Token k = token_of(p, r);
+    const T* x = static_cast<const T*>(t.x.data) + address(t.x, k);
+    const T* y = BACK ? static_cast<const T*>(t.dy.data) + address(t.dy, k) : nullptr;
+    T* out = static_cast<T*>(t.o.data) + address(t.o, k);
+    const Where at = p.table != nullptr ? where_of(p, k) : Where{};
+    auto sum = [&](float s, float* of) {
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
       if constexpr (ROW) {
         __syncthreads();
-        if (lane == 0) room[warp] = s;
+        if (lane == 0) of[warp] = s;
         __syncthreads();
         s = 0.f;
 #pragma unroll
-        for (int i = 0; i < WARPS; ++i) s += room[i];
+        for (int i = 0; i < WARPS; ++i) s += of[i];
       }
       return s;
     };
@@ -590,7 +725,7 @@ __global__ void __launch_bounds__(THREADS) turn_elements_kernel(const __grid_con
         db = a * cs.y + db * cs.x;
       }
     };
-    auto both = [&](float f) {
+    auto sums_of_both = [&](float f) {
       float a = 0.f, b = 0.f;
       for (int i = from; i < pieces; i += by) {
         const int hh = ROW ? i / np : 0, h = h_of + hh, j = i - hh * np;
@@ -606,17 +741,16 @@ __global__ void __launch_bounds__(THREADS) turn_elements_kernel(const __grid_con
       }
       return make_float2(sum(a, part), BACK ? sum(b, part2) : 0.f);
     };
-    Scale s{1.f, 1.f};
+    struct { float factor, scale; } s{1.f, 1.f};
     float along = 0.f;
     if constexpr (NORM != AS_NORM_NONE) {
       const float n = ROW ? (float)t.heads * (float)p.d : (float)p.d;
-      float2 q = both(1.f);
+      float2 q = sums_of_both(1.f);
       const float mean = q.x / n + p.eps;
       s.scale = rsqrtf(mean);
-      const bool over = !(q.x <= MOST), under = mean < LEAST;
-      if (over || under) {                               // (one value for all that share the sum)
-        const float f = over ? DOWN : UP;
-        q = both(f);
+      if (over(q.x) || mean < LEAST) {                   // (one value for all that share the sum)
+        const float f = over(q.x) ? DOWN : UP;
+        q = sums_of_both(f);
         s = {f, rsqrtf(q.x / n + p.eps * f * f)};
       }
       along = q.y * s.scale / n;
@@ -657,9 +791,9 @@ __global__ void __launch_bounds__(THREADS) turn_elements_kernel(const __grid_con
     if (t.part == nullptr) return;
     __syncthreads();
     for (int c = threadIdx.x; c < cols; c += THREADS) {
-      float s = sums[c];
+      float s = room[c];
       if constexpr (!ROW)
-        for (int w = 1; w < WARPS; ++w) s += sums[w * p.d + c];
+        for (int w = 1; w < WARPS; ++w) s += room[w * p.d + c];
       t.part[(long long)blockIdx.x * cols + c] = s;
     }
   }
@@ -733,6 +867,9 @@ Shape turn_params(const as_qk_norm_rotary_t& a, const as_rotation_t& r, int sms,
   rotation_ok(r, 0, a.head_dim, &pairs);
   p.n_t = two ? 2 : 1;
   p.rows = (int)a.rows; p.tokens = (int)a.q.tokens; p.d = a.head_dim;
+  auto by = [](unsigned n) { return n == 1u ? 0ull : ~0ull / n + 1ull; };
+  p.by_tokens = by((unsigned)std::max(p.tokens, 1));
+  for (int i = 0; i < 2; ++i) p.over_n[i] = 1.f / ((float)a.head_dim * (a.norm == AS_NORM_ROW ? (float)std::max(i == 0 ? a.q_heads : a.k_heads, 1) : 1.f));
   p.eps = a.eps;
   p.w_f32 = a.weight_dtype == AS_DTYPE_F32;
   p.t[0].heads = a.q_heads;
@@ -741,7 +878,7 @@ Shape turn_params(const as_qk_norm_rotary_t& a, const as_rotation_t& r, int sms,
   if (two) p.t[1].x = rows_of(a.k, a.rows, (long long)a.k_heads * a.head_dim);
   if (a.norm != AS_NORM_NONE) { p.t[0].w = a.q_weight; p.t[1].w = two ? a.k_weight : nullptr; }
   p.table = reinterpret_cast<const float2*>(r.table);
-  p.pairs = pairs;
+  p.pairs = pairs;                           // (0 without a table)
   if (p.table != nullptr) {
     p.axes = r.n_axes;
     p.half = r.layout == AS_ROTARY_HALF;
@@ -750,7 +887,7 @@ Shape turn_params(const as_qk_norm_rotary_t& a, const as_rotation_t& r, int sms,
     int rows = 0, end = 0;
     for (int i = 0; i < AS_ROTARY_MAX_AXES; ++i) {
       p.first_row[i] = rows;
-      if (i < r.n_axes) { p.size[i] = r.size[i]; rows += r.size[i]; end += r.pairs[i]; }
+      if (i < r.n_axes) { p.size[i] = r.size[i]; p.by_size[i] = by((unsigned)r.size[i]); rows += r.size[i]; end += r.pairs[i]; }
       p.end[i] = end;
     }
   }
@@ -761,7 +898,7 @@ Shape turn_params(const as_qk_norm_rotary_t& a, const as_rotation_t& r, int sms,
   p.lanes_log = 0;
   while ((16 << p.lanes_log) < a.head_dim) ++p.lanes_log;
   const int heads = std::max(p.t[0].heads, p.t[1].heads), of_vector = std::max(1, 32 >> p.lanes_log), vectors = (heads + of_vector - 1) / of_vector;
-  const int most = back ? (a.q.dtype == AS_DTYPE_BF16 ? 3 : 2) : 3;
+  const int most = a.q.dtype == AS_DTYPE_BF16 ? 3 : 2;
   p.W = 1; p.chunks = 1;
   if (a.norm == AS_NORM_ROW) {
     p.W = (vectors + most - 1) / most;
@@ -772,8 +909,8 @@ Shape turn_params(const as_qk_norm_rotary_t& a, const as_rotation_t& r, int sms,
     // few rows: a vector a warp, so that all of them are under way at once
     s.NV = a.rows * ((vectors + most - 1) / most) <= 4ll * sms ? 1 : std::min(vectors, most);
     p.chunks = (vectors + s.NV - 1) / s.NV;
-    const long long units = s.vec ? a.rows * p.chunks : a.rows * (back ? heads : (long long)p.t[0].heads + p.t[1].heads);
-    s.ctas = (units + WARPS - 1) / WARPS;
+    if (p.chunks > 65535) s.vec = false;
+    s.ctas = s.vec ? (a.rows + WARPS - 1) / WARPS : (a.rows * (back ? heads : (long long)p.t[0].heads + p.t[1].heads) + WARPS - 1) / WARPS;
   }
   return s;
 }
@@ -781,11 +918,12 @@ Shape turn_params(const as_qk_norm_rotary_t& a, const as_rotation_t& r, int sms,
 template <typename T, int NORM>
 cudaError_t launch_turn(const TurnParams& p, const Shape& s, int sms, cudaStream_t st) {
   if (!s.vec) return as_launch_dependent(turn_elements_kernel<T, NORM, false>, dim3((unsigned)std::min<long long>(s.ctas, 8ll * sms)), dim3(THREADS), 0, st, p);
-  const dim3 grid((unsigned)s.ctas), block(THREADS);
+  const dim3 grid((unsigned)std::min<long long>(s.ctas, std::max(1, 2 * sms / p.chunks)), (unsigned)p.chunks), block(THREADS);        // CTAs go on from row to row
+  auto run = [&](auto interleaved, auto half) { return p.half ? as_launch_dependent(half, grid, block, 0, st, p) : as_launch_dependent(interleaved, grid, block, 0, st, p); };
   switch (s.NV) {
-    case 1: return as_launch_dependent(turn_kernel<T, NORM, 1>, grid, block, 0, st, p);
-    case 2: return as_launch_dependent(turn_kernel<T, NORM, 2>, grid, block, 0, st, p);
-    default: return as_launch_dependent(turn_kernel<T, NORM, 3>, grid, block, 0, st, p);
+    case 1: return run(turn_kernel<T, NORM, 1, false>, turn_kernel<T, NORM, 1, true>);
+    case 2: return run(turn_kernel<T, NORM, 2, false>, turn_kernel<T, NORM, 2, true>);
+    default: return run(turn_kernel<T, NORM, 3, false>, turn_kernel<T, NORM, 3, true>);
   }
 }
 template <typename T>
@@ -794,21 +932,28 @@ cudaError_t launch_norm(const TurnParams& p, const Shape& s, int norm, int sms, 
 }
 
 template <typename T, int NORM>
-cudaError_t launch_back(const TurnParams& p, const Shape& s, unsigned ctas, size_t smem, cudaStream_t st) {
+cudaError_t launch_back(const TurnParams& p, const Shape& s, unsigned ctas, cudaStream_t st) {
   const dim3 grid(ctas, (unsigned)p.n_t), block(THREADS);
+  const int heads = std::max(p.t[0].heads, p.t[1].heads);
+  const size_t smem = s.vec ? NORM == AS_NORM_ROW ? (size_t)WARPS * s.NV * 2048 : (size_t)WARPS * 2048 : (size_t)(NORM == AS_NORM_ROW ? heads : WARPS) * p.d * 4;
   auto run = [&](auto kernel) {
-    if (smem > 48 * 1024)
+    if (smem > 40 * 1024)                                // (beside what the kernels have of a fixed size, 48 KB are there without asking)
       if (const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); e != cudaSuccess) return e;
     return as_launch_dependent(kernel, grid, block, smem, st, p);
   };
   if (!s.vec) return run(turn_elements_kernel<T, NORM, true>);
+  auto choose = [&](auto interleaved, auto half) { return p.half ? run(half) : run(interleaved); };
   if constexpr (sizeof(T) == 2)
-    if (s.NV == 3) return run(turn_back_kernel<T, NORM, 3>);
-  return s.NV == 2 ? run(turn_back_kernel<T, NORM, 2>) : run(turn_back_kernel<T, NORM, 1>);
+    if (s.NV == 3) return choose(turn_back_kernel<T, NORM, 3, false>, turn_back_kernel<T, NORM, 3, true>);
+  return s.NV == 2 ? choose(turn_back_kernel<T, NORM, 2, false>, turn_back_kernel<T, NORM, 2, true>) : choose(turn_back_kernel<T, NORM, 1, false>, turn_back_kernel<T, NORM, 1, true>);
 }
 
-// CTAs of the backward pass, for each tensor: as many as the device holds at once.
-unsigned back_ctas(const Shape& s, int sms) { return (unsigned)std::min<long long>(s.ctas, 2ll * sms); }
+// CTAs of the backward pass, for each tensor: as many as the device holds at once (of vectors: a multiple of the chunks, which they take in turn).
+unsigned back_ctas(const TurnParams& p, const Shape& s, bool f32, int sms) {
+  const int most = std::max(1, (s.vec ? f32 ? 1 : 2 : 4) * sms / p.n_t);
+  if (!s.vec) return (unsigned)std::min<long long>(s.ctas, most);
+  return (unsigned)(std::min<long long>(s.ctas, std::max(1, most / p.chunks)) * p.chunks);
+}
 
 // The rows of the backward call that the shape looks at beside the inputs.
 int back_rows(const as_qk_norm_rotary_backward_t& b, as_rows_t (&more)[4]) {
@@ -886,7 +1031,7 @@ extern "C" as_status_t as_qk_norm_rotary_backward_workspace_bytes(const as_qk_no
   as_rows_t more[4];
   long long cols[2];
   const Shape s = turn_params(*b->fwd, b->fwd->rotation, sms, true, more, back_rows(*b, more), p);
-  *bytes = back_bytes(*b, back_ctas(s, sms), cols);
+  *bytes = back_bytes(*b, back_ctas(p, s, b->fwd->q.dtype == AS_DTYPE_F32, sms), cols);
   return AS_OK;
 }
 
@@ -907,7 +1052,7 @@ extern "C" as_status_t as_qk_norm_rotary_backward(const as_qk_norm_rotary_backwa
   TurnParams p{};
   as_rows_t more[4];
   const Shape s = turn_params(a, a.rotation, sms, true, more, back_rows(*b, more), p);
-  const unsigned ctas = back_ctas(s, sms);
+  const unsigned ctas = back_ctas(p, s, a.q.dtype == AS_DTYPE_F32, sms);
   const uint64_t need = back_bytes(*b, ctas, cols);
   if (need > 0 && (b->workspace == nullptr || !aligned(b->workspace, 16) || b->workspace_bytes < need)) return AS_ERR_WORKSPACE;
   float* part = static_cast<float*>(b->workspace);
@@ -915,21 +1060,19 @@ extern "C" as_status_t as_qk_norm_rotary_backward(const as_qk_norm_rotary_backwa
   const as_rows_t* out[2] = {&b->dq_out, &b->dk_out};
   void* dw[2] = {b->dq_weight, b->dk_weight};
   SumParams sum{};
-  size_t smem = 0;
   for (int i = 0; i < p.n_t; ++i) {
     const long long wide = (long long)p.t[i].heads * a.head_dim;
     p.t[i].dy = rows_of(*dy[i], a.rows, wide);
     p.t[i].o = rows_of(*out[i], a.rows, wide);
     if (cols[i] > 0) { p.t[i].part = part; sum.part[i] = part; sum.out[i] = dw[i]; sum.cols[i] = (int)cols[i]; part += ctas * cols[i]; }
-    smem = std::max(smem, (size_t)(a.norm == AS_NORM_ROW ? wide : s.vec ? a.head_dim : WARPS * a.head_dim) * 4);
   }
   cudaError_t e;
-  if (a.q.dtype == AS_DTYPE_BF16) e = a.norm == AS_NORM_HEAD ? launch_back<bf, AS_NORM_HEAD>(p, s, ctas, smem, st) : launch_back<bf, AS_NORM_ROW>(p, s, ctas, smem, st);
-  else e = a.norm == AS_NORM_HEAD ? launch_back<float, AS_NORM_HEAD>(p, s, ctas, smem, st) : launch_back<float, AS_NORM_ROW>(p, s, ctas, smem, st);
+  if (a.q.dtype == AS_DTYPE_BF16) e = a.norm == AS_NORM_HEAD ? launch_back<bf, AS_NORM_HEAD>(p, s, ctas, st) : launch_back<bf, AS_NORM_ROW>(p, s, ctas, st);
+  else e = a.norm == AS_NORM_HEAD ? launch_back<float, AS_NORM_HEAD>(p, s, ctas, st) : launch_back<float, AS_NORM_ROW>(p, s, ctas, st);
   if (e == cudaSuccess && cols[0] + cols[1] > 0) {
     sum.rows = (int)ctas;
     sum.f32 = a.weight_dtype == AS_DTYPE_F32;
-    e = as_launch_dependent(turn_sum_kernel, dim3((unsigned)((std::max(cols[0], cols[1]) + 31) / 32), 2), dim3(THREADS), 0, st, sum);
+    e = as_launch_dependent(turn_sum_kernel, dim3((unsigned)((std::max(cols[0], cols[1]) + 31) / 32), 2), dim3(SUM_RUNS * 32), 0, st, sum);
   }
   return e == cudaSuccess ? AS_OK : failed();
 }
