@@ -7,18 +7,20 @@
 //   warp 0       copies (TMA, 64 steps of the summed index a stage, 128-byte swizzle), told by the leading CTA's barrier
 //   warp 1       the MMAs (leading CTA only)
 //   warp 2       allocates tensor memory
-//   warps 4-11   results: tensor memory -> a strip of shared memory per warp (32 x 32 sums), read back so that 8 lanes hold a row's 32 columns: bias, activation, gate
-//                and residual go by 4 columns a lane, rows in runs of 64 or 128 bytes
+//   warps 4-19   results, 32 rows x 32 columns at a time: tensor memory -> registers, a lane a row: bias, activation, gate, bf16, a strip of shared memory, from where TMA takes
+//                them; with a residual, in fp32 or in layouts without boxes 16 columns at a time through the strip, from where 4 lanes move a row
 //
 // What bounds it is the tensor pipe and the operands' bytes into an SM, which for 256 x 256 are level: 64 bytes a clock beside 8192 operations.
 //
 // Where the tiles are too few for the SMs, the summed index is cut into parts; their sums go to the workspace in fp32 and finish_kernel adds them up in order.  Few rows of
 // x: linear_few_kernel, further down.
 #include <algorithm>
+#include <type_traits>
 
 #include "as_layer.h"
 #include "fp8_common.cuh"
 #include "fp8_context.h"
+#include "fp8_maps.h"
 #include "linear_plan.h"
 #include "sm100_pairs.cuh"
 #include "tensor_common.cuh"
@@ -29,16 +31,20 @@ using namespace as_fp8;
 using namespace sm100;
 typedef __nv_bfloat16 bf;
 
-constexpr int LIN_THREADS = 384;
+constexpr int RESULT_WARPS = 16, LIN_THREADS = (4 + RESULT_WARPS) * 32;
 constexpr int BM = LIN_BM, BK = LIN_BK;
 constexpr int MAX_STAGES = 10;
 constexpr int SMEM_MAX = 227 * 1024;
 constexpr uint32_t BOX = 64 * 128;          // bytes of a box of 64 x 64
 
 enum { B_FULL = 0, B_EMPTY = B_FULL + MAX_STAGES, B_AFULL = B_EMPTY + MAX_STAGES, B_AEMPTY = B_AFULL + 2, B_COUNT = B_AEMPTY + 2 };
-constexpr int STRIP = 32 * 128;
+// shared memory: barriers, tensor-memory address, abort flag; for each result warp a strip of 32 rows x 64 bytes, and 32 biases and gates; then the stages
+constexpr int STRIP = 32 * 64;
 constexpr int STRIPS_OFF = 1024;
-constexpr int STAGES_OFF = STRIPS_OFF + 8 * STRIP;
+constexpr int VECTORS_OFF = STRIPS_OFF + RESULT_WARPS * STRIP;
+constexpr int STAGES_OFF = VECTORS_OFF + RESULT_WARPS * 256;
+// Byte of 16-byte chunk `ch` of a strip's row: the 64-byte swizzle.
+AS_DEV uint32_t swz64(int row, int ch) { return (uint32_t)(row * 64 + ((ch ^ (row >> 1 & 3)) << 4)); }
 static_assert(B_COUNT * 8 + 8 <= STRIPS_OFF && STAGES_OFF % 1024 == 0, "");
 
 // ---------------------------------------------------------------- what follows a sum
@@ -50,6 +56,7 @@ struct Epilogue {
   int N, act;
   bool out_f32, res_f32, bias_f32, gate_f32;
   bool vec;                                  // four columns move at once
+  bool boxes, pre_boxes;                     // out (without a residual) and pre leave in boxes of 32 rows x 32 columns by TMA
 };
 
 AS_DEV float ld1(const void* p, bool f32, long long i) { return f32 ? static_cast<const float*>(p)[i] : __bfloat162float(static_cast<const bf*>(p)[i]); }
@@ -70,14 +77,41 @@ AS_DEV void st1(void* p, bool f32, long long i, float v) {
 // 1 / (1 + e^-x): e^-x is 2^(-x log2 e), infinite for what is far below 0, where the quotient is 0.
 AS_DEV float sigmoid(float x) { return __fdividef(1.f, 1.f + ex2(-1.442695041f * x)); }
 constexpr float GELU_A = 1.5957691216f, GELU_B = 0.044715f;      // 2 sqrt(2 / pi): gelu_tanh(z) = z sigmoid(A (z + B z^3)), as 1 + tanh(u) = 2 sigmoid(2 u)
-AS_DEV float activated(float z, int act) {
+// The normal distribution's function, with e = e^(-z^2 / 2): erfc(a) = e^(-a^2) f(a), a = |z| / sqrt 2, f a polynomial of t = 1 / (1 + 0.35 a), fitted to the least relative error over a up to 9.6 (7e-9;
+// in fp32 4e-7 of 1, and 8e-6 of itself far below 0, where the rounding of z^2 counts).
+AS_DEV float normal_cdf(float z, float& e) {
+  const float t = __fdividef(1.f, fmaf(fabsf(z), 0.35f * 0.7071067812f, 1.f));
+  e = ex2(-0.7213475204f * z * z);
+  float f = 0.0377782903f;
+  f = fmaf(f, t, -0.155430015f); f = fmaf(f, t, 0.172923096f); f = fmaf(f, t, -0.015841502f); f = fmaf(f, t, 0.076692656f); f = fmaf(f, t, 0.151870132f);
+  f = fmaf(f, t, 0.1490568f); f = fmaf(f, t, 0.188387351f); f = fmaf(f, t, 0.197075969f); f = fmaf(f, t, 0.197487229f);
+  const float half = 0.5f * f * t * e;
+  return z < 0.f ? half : 1.f - half;
+}
+// z times what is 0 far below 0 (there z may be minus infinity).
+AS_DEV float times(float z, float f) { return f == 0.f ? 0.f : z * f; }
+template <int ACT>
+AS_DEV float activated(float z) {
+  if constexpr (ACT == AS_ACT_RELU) return z < 0.f ? 0.f : z;     // (NaN stays)
+  else if constexpr (ACT == AS_ACT_SILU) return times(z, sigmoid(z));
+  else if constexpr (ACT == AS_ACT_GELU) { float e; return times(z, normal_cdf(z, e)); }
+  else if constexpr (ACT == AS_ACT_GELU_TANH) return times(z, sigmoid(GELU_A * z * fmaf(GELU_B * z, z, 1.f)));
+  else return z;
+}
+// f with the activation as a constant.
+template <typename F>
+AS_DEV void with_activation(int act, F f) {
   switch (act) {
-    case AS_ACT_RELU: return z < 0.f ? 0.f : z;                  // (NaN stays)
-    case AS_ACT_SILU: return z == -INFINITY ? 0.f : z * sigmoid(z);
-    case AS_ACT_GELU: return z == -INFINITY ? 0.f : 0.5f * z * erfcf(-0.7071067812f * z);
-    case AS_ACT_GELU_TANH: return z == -INFINITY ? 0.f : z * sigmoid(GELU_A * z * fmaf(GELU_B * z, z, 1.f));
-    default: return z;
+    case AS_ACT_RELU: f(std::integral_constant<int, AS_ACT_RELU>{}); break;
+    case AS_ACT_SILU: f(std::integral_constant<int, AS_ACT_SILU>{}); break;
+    case AS_ACT_GELU: f(std::integral_constant<int, AS_ACT_GELU>{}); break;
+    case AS_ACT_GELU_TANH: f(std::integral_constant<int, AS_ACT_GELU_TANH>{}); break;
+    default: break;
   }
+}
+AS_DEV float activated(float z, int act) {
+  with_activation(act, [&](auto a) { z = activated<decltype(a)::value>(z); });
+  return z;
 }
 // (act(z), act'(z))
 AS_DEV float2 activated2(float z, int act) {
@@ -85,15 +119,16 @@ AS_DEV float2 activated2(float z, int act) {
     case AS_ACT_RELU: return make_float2(z < 0.f ? 0.f : z, z > 0.f ? 1.f : z != z ? z : 0.f);
     case AS_ACT_SILU: {
       const float s = sigmoid(z), t = sigmoid(-z);
-      return make_float2(z == -INFINITY ? 0.f : z * s, fabsf(z) > 200.f ? s : s * fmaf(z, t, 1.f));
+      return make_float2(times(z, s), fabsf(z) > 200.f ? s : s * fmaf(z, t, 1.f));
     }
     case AS_ACT_GELU: {
-      const float c = 0.5f * erfcf(-0.7071067812f * z);
-      return make_float2(z == -INFINITY ? 0.f : z * c, fabsf(z) > 30.f ? c : fmaf(z * 0.3989422804f, ex2(-0.7213475204f * z * z), c));
+      float e;
+      const float c = normal_cdf(z, e);
+      return make_float2(times(z, c), fabsf(z) > 30.f ? c : fmaf(z * 0.3989422804f, e, c));
     }
     case AS_ACT_GELU_TANH: {
       const float q = GELU_B * z * z, u = GELU_A * z * (1.f + q), s = sigmoid(u), t = sigmoid(-u);
-      return make_float2(z == -INFINITY ? 0.f : z * s, fabsf(z) > 30.f ? s : fmaf(z * s, t * GELU_A * fmaf(3.f, q, 1.f), s));
+      return make_float2(times(z, s), fabsf(z) > 30.f ? s : fmaf(z * s, t * GELU_A * fmaf(3.f, q, 1.f), s));
     }
     default: return make_float2(z, 1.f);
   }
@@ -244,7 +279,10 @@ out:
   }
 }
 
-template <int CG, bool A_MN, bool B_MN>
+// LONG: sums of more than CHUNK steps go to the result warps in runs of as many, which add them up in fp32 rounded to nearest.  The tensor cores truncate: over 384 instructions (6144 columns) that
+// left 4e-6 of a product, in one direction, which a result in bf16 does not show but one in fp32 does.
+constexpr int CHUNK = 16;
+template <int CG, bool A_MN, bool B_MN, bool LONG>
 AS_DEV void lin_issue(const GemmParams& p, const Ctx<CG>& c) {
   const uint32_t stage_bytes = (uint32_t)(BM + p.bn / CG) * BK * 2;
   const uint32_t idesc = make_idesc(BM * CG, 0, A_MN, B_MN) | (uint32_t)(p.bn >> 3) << 17;
@@ -252,78 +290,240 @@ AS_DEV void lin_issue(const GemmParams& p, const Ctx<CG>& c) {
   uint32_t buf = 0, turn = 0;
   for (long long u = c.unit; u < p.units; u += c.step) {
     const Unit w = unit_of<CG>(p, u);
+    int k = w.k0;
+    do {
+    const int first = k, end = LONG ? min(w.k1, k + CHUNK) : w.k1;
     if (!c.wait(B_AEMPTY + buf, turn ^ 1u)) return;
     const uint32_t d = c.tmem + buf * 256u;
-    for (int k = w.k0; k < w.k1; ++k) {
+    for (; k < end; ++k) {
       if (!c.wait(B_FULL + r.slot, r.turn)) return;
       tc_fence_after();
       const uint32_t at = c.sbase + STAGES_OFF + (uint32_t)r.slot * stage_bytes;
       const uint64_t da = make_sdesc(at, A_MN ? BOX : 16, 1024), db = make_sdesc(at + BM * BK * 2, B_MN ? BOX : 16, 1024);
 #pragma unroll
-      for (int i = 0; i < BK / 16; ++i) mma<CG>(d, da + (A_MN ? 128 : 2) * i, db + (B_MN ? 128 : 2) * i, idesc, k > w.k0 || i > 0 ? 1u : 0u);
+      for (int i = 0; i < BK / 16; ++i) mma<CG>(d, da + (A_MN ? 128 : 2) * i, db + (B_MN ? 128 : 2) * i, idesc, k > first || i > 0 ? 1u : 0u);
       commit<CG>(c.bar(B_EMPTY + r.slot));
       r.next(p.stages);
     }
     commit<CG>(c.bar(B_AFULL + buf));
     buf ^= 1u;
     if (buf == 0) turn ^= 1u;
+    } while (LONG && k < w.k1);
   }
 }
 
-// Results of a tile: this warp's 32 rows, every second 32 columns.
-template <int CG>
-AS_DEV void lin_results(const GemmParams& p, const Ctx<CG>& c, int lane, int warp) {
-  const int quarter = warp & 3, half = warp >> 2;
+// 32 rows of a strip's width to one matrix by TMA, where they are of one entry, and fewer than 32 only at its end, where the copy is cut off.
+struct Box { unsigned batch, token; bool whole; };
+AS_DEV Box box_of(const Rows& m, bool boxes, int m0, int rows) {
+  if (!boxes) return {0u, 0u, false};
+  const unsigned b = m.batched ? (unsigned)m0 / m.tokens : 0u, t = (unsigned)m0 - b * m.tokens;
+  const unsigned end = t + (unsigned)max(rows, 0);
+  return {b, t, rows == 32 ? end <= m.tokens : end == m.tokens};
+}
+// This lane's row of 32 values as bf16 into the strip, and the strip to columns n .. n + 31.
+AS_DEV void leave_box(const CUtensorMap* map, const Rows& m, const Box& box, uint32_t strip, int lane, int rows, int n, int N, const float (&x)[32]) {
+  if (lane == 0) tma_store_wait_read();       // the copy before this one has read the strip
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = pack_bf16(x[8 * i + 2 * k], x[8 * i + 2 * k + 1]);
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(strip + swz64(lane, i)), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+  }
+  fence_proxy_async();
+  __syncwarp();
+  if (lane == 0 && rows > 0 && n < N) {
+    const unsigned head = m.hd == N ? 0u : (unsigned)n / (unsigned)m.hd;
+    store_box(map, strip, n - (int)head * m.hd, (int)box.token, (int)head, (int)box.batch);
+    tma_store_commit();
+  }
+}
+// 16 columns of 32 rows through the strip, plus a residual, four lanes a row: `at(row, n)` is where four (or fewer) columns go.
+struct Target { Rows m; bool f32; };
+AS_DEV void leave_rows(const Target& to, const Target& res, bool vec, uint32_t strip, int lane, int m0, int rows, int n0, int N, const float* x) {
+  const int n = n0 + 4 * (lane & 3);
+  const bool adds = res.m.data != nullptr, in = n < N;
+  const long long oc = in ? to.m.col((unsigned)n) : 0, rc = in && adds ? res.m.col((unsigned)n) : 0;
+  float4 r[4];
+  if (adds && vec) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = i * 8 + lane / 4;
+      r[i] = in && row < rows ? ld4(res.m.data, res.f32, res.m.row((unsigned)(m0 + row)) + rc) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+  }
+  if (lane == 0) tma_store_wait_read();       // (a box of pre may be on its way from the strip)
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(strip + swz64(lane, i)), "f"(x[4 * i]), "f"(x[4 * i + 1]), "f"(x[4 * i + 2]), "f"(x[4 * i + 3]) : "memory");
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = i * 8 + lane / 4;
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(strip + swz64(row, lane & 3)) : "memory");
+    if (!in || row >= rows) continue;
+    const unsigned m = (unsigned)(m0 + row);
+    if (vec) {
+      if (adds) { v.x += r[i].x; v.y += r[i].y; v.z += r[i].z; v.w += r[i].w; }
+      st4(to.m.data, to.f32, to.m.row(m) + oc, v);
+    } else {
+      const float f[4] = {v.x, v.y, v.z, v.w};
+      const long long ro = to.m.row(m), rr = adds ? res.m.row(m) : 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (n + k < N) st1(to.m.data, to.f32, ro + to.m.col((unsigned)(n + k)), adds ? f[k] + ld1(res.m.data, res.f32, rr + res.m.col((unsigned)(n + k))) : f[k]);
+    }
+  }
+  __syncwarp();
+}
+
+// Sums of 32 rows x 32 columns, on to out and pre.  `bias` and `gate`: this lane's column's; gates_alike: all rows have the same ones.
+AS_DEV void leave_strip(const Epilogue& e, const CUtensorMap* mo, const CUtensorMap* mp, const Box& out_box, const Box& pre_box, uint32_t strip, uint32_t vectors, int lane, int m0, int rows, int n0,
+                        float bias, float gate, bool gates_alike, uint32_t (&w)[32]) {
+  float(&x)[32] = reinterpret_cast<float(&)[32]>(w);
+  const bool biased = e.bias != nullptr, gated = e.gate != nullptr;
+  if (biased) asm volatile("st.shared.f32 [%0], %1;" ::"r"(vectors + lane * 4), "f"(bias) : "memory");
+  if (gated) asm volatile("st.shared.f32 [%0], %1;" ::"r"(vectors + 128 + lane * 4), "f"(gate) : "memory");
+  if (biased || gated) __syncwarp();
+  auto vector = [&](uint32_t at, int i) {
+    float4 b;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(b.x), "=f"(b.y), "=f"(b.z), "=f"(b.w) : "r"(at + i * 16) : "memory");
+    return b;
+  };
+  if (biased) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float4 b = vector(vectors, i);
+      x[4 * i] += b.x; x[4 * i + 1] += b.y; x[4 * i + 2] += b.z; x[4 * i + 3] += b.w;
+    }
+  }
+  if (e.pre.data != nullptr) {
+    if (pre_box.whole) leave_box(mp, e.pre, pre_box, strip, lane, rows, n0, e.N, x);
+    else
+#pragma unroll
+      for (int h = 0; h < 2; ++h) leave_rows({e.pre, false}, {}, e.vec, strip, lane, m0, rows, n0 + 16 * h, e.N, x + 16 * h);
+  }
+  with_activation(e.act, [&](auto a) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) x[i] = activated<decltype(a)::value>(x[i]);
+  });
+  if (gated) {
+    if (gates_alike) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float4 g = vector(vectors + 128, i);
+        x[4 * i] *= g.x; x[4 * i + 1] *= g.y; x[4 * i + 2] *= g.z; x[4 * i + 3] *= g.w;
+      }
+    } else {
+      const long long at = (long long)((unsigned)(m0 + min(lane, rows - 1)) / e.gate_rows) * e.gate_stride;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) x[i] *= n0 + i < e.N && rows > 0 ? ld1(e.gate, e.gate_f32, at + n0 + i) : 0.f;
+    }
+  }
+  if (out_box.whole) leave_box(mo, e.out, out_box, strip, lane, rows, n0, e.N, x);
+  else
+#pragma unroll
+    for (int h = 0; h < 2; ++h) leave_rows({e.out, e.out_f32}, {e.res, e.res_f32}, e.vec, strip, lane, m0, rows, n0 + 16 * h, e.N, x + 16 * h);
+}
+
+// Results of a tile: this warp's 32 rows, 32 of every 128 columns.  LONG: of a tile's sums, which come in runs of CHUNK steps.
+template <int CG, bool LONG>
+AS_DEV void lin_results(const GemmParams& p, const Ctx<CG>& c, const CUtensorMap* mo, const CUtensorMap* mp, int lane, int warp) {
+  const Epilogue& e = p.e;
+  const int quarter = warp & 3, group = warp >> 2;
   const uint32_t lanes = (uint32_t)quarter * 32u << 16;
-  const uint32_t strip = c.sbase + STRIPS_OFF + (uint32_t)warp * STRIP;
-  const int chunk = lane & 7;
+  const uint32_t strip = c.sbase + STRIPS_OFF + (uint32_t)warp * STRIP, vectors = c.sbase + VECTORS_OFF + (uint32_t)warp * 256;
   uint32_t buf = 0, turn = 0;
+  auto give_back = [&] {
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) arrive_leader<CG>(c.bar(B_AEMPTY + buf));
+  };
   for (long long u = c.unit; u < p.units; u += c.step) {
     const Unit w = unit_of<CG>(p, u);
     const int t0 = w.t0 + (int)c.rank * BM + quarter * 32, m0 = w.entry * p.T + t0, rows = min(32, p.T - t0);
-    if (!mbar_wait_warp(c.bar(B_AFULL + buf), turn, c.wc)) break;
-    tc_fence_after();
-    if (32 * half >= p.bn) {
-      __syncwarp();
-      if (lane == 0) arrive_leader<CG>(c.bar(B_AEMPTY + buf));
-    }
-    for (int c0 = 32 * half; c0 < p.bn; c0 += 64) {
-      const int n = w.n0 + c0 + 4 * chunk;
-      uint32_t x[32];
-      tmem_ld32(c.tmem + lanes + buf * 256u + c0, x);
-      Column4 cols{};
-      if (p.part == nullptr) cols = columns_of(p.e, n);
-      tmem_ld_wait(x);
-      if (c0 + 64 >= p.bn) {                  // this warp has read its part of the accumulator
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) arrive_leader<CG>(c.bar(B_AEMPTY + buf));
-      }
+    const Box out_box = box_of(e.out, e.boxes, m0, rows), pre_box = box_of(e.pre, e.pre_boxes, m0, rows);
+    // biases and gates of this lane's column in each strip, while the products run
+    float bias[2], gate[2];
+    const long long gate_row = e.gate_rows == 0u || rows <= 0 ? 0 : (long long)((unsigned)m0 / e.gate_rows);
+    const bool gates_alike = e.gate_rows == 0u || rows <= 0 || gate_row == (long long)((unsigned)(m0 + rows - 1) / e.gate_rows);
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(strip + swz128_chunk_offset(lane, i)), "r"(x[4 * i]), "r"(x[4 * i + 1]), "r"(x[4 * i + 2]), "r"(x[4 * i + 3]) : "memory");
-      __syncwarp();
-      if (n < p.e.N) {
-#pragma unroll 4
-        for (int i = 0; i < 8; ++i) {
-          const int r = i * 4 + lane / 8;
-          float4 v;
-          asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(strip + swz128_chunk_offset(r, chunk)) : "memory");
-          if (r >= rows) continue;
-          if (p.part != nullptr) *reinterpret_cast<float4*>(p.part + ((long long)w.part * p.M + m0 + r) * p.part_pitch + n) = v;
-          else finish4(p.e, cols, m0 + r, n, v);
-        }
-      }
-      __syncwarp();
+    for (int j = 0; j < 2; ++j) {
+      const int n = w.n0 + 32 * group + 128 * j + lane;
+      bias[j] = e.bias != nullptr && n < e.N ? ld1(e.bias, e.bias_f32, n) : 0.f;
+      gate[j] = e.gate != nullptr && n < e.N ? ld1(e.gate, e.gate_f32, gate_row * e.gate_stride + n) : 0.f;
     }
-    buf ^= 1u;
-    if (buf == 0) turn ^= 1u;
+    auto leave = [&](int j, uint32_t (&x)[32]) {
+      const int n0 = w.n0 + 32 * group + 128 * j;
+      if (p.part != nullptr) {
+        const Target to{Rows{p.part + (long long)w.part * p.M * p.part_pitch, 0, 0, p.part_pitch, 1u, 1, 0ull, false, false}, true};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) leave_rows(to, {}, true, strip, lane, m0, rows, n0 + 16 * h, e.N, reinterpret_cast<float*>(x) + 16 * h);
+      } else {
+        leave_strip(e, mo, mp, out_box, pre_box, strip, vectors, lane, m0, rows, n0, bias[j], gate[j], gates_alike, x);
+      }
+    };
+    if constexpr (!LONG) {
+      if (!mbar_wait_warp(c.bar(B_AFULL + buf), turn, c.wc)) break;
+      tc_fence_after();
+      if (32 * group >= p.bn) give_back();
+#pragma unroll 1
+      for (int j = 0; j < 2; ++j) {
+        const int c0 = 32 * group + 128 * j;
+        if (c0 >= p.bn) break;
+        uint32_t x[32];
+        tmem_ld32(c.tmem + lanes + buf * 256u + c0, x);
+        tmem_ld_wait(x);
+        if (c0 + 128 >= p.bn) give_back();    // this warp has read its part of the accumulator
+        leave(j, x);
+      }
+      buf ^= 1u;
+      if (buf == 0) turn ^= 1u;
+    } else {
+      uint32_t x[2][32];
+      bool ok = true;
+      for (int k = w.k0; k < w.k1 && ok; k += CHUNK) {
+        ok = mbar_wait_warp(c.bar(B_AFULL + buf), turn, c.wc);
+        if (!ok) break;
+        tc_fence_after();
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int c0 = 32 * group + 128 * j;
+          if (c0 >= p.bn) continue;
+          if (k == w.k0) {
+            tmem_ld32(c.tmem + lanes + buf * 256u + c0, x[j]);
+            tmem_ld_wait(x[j]);
+          } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              uint32_t y[16];
+              tmem_ld16(c.tmem + lanes + buf * 256u + c0 + 16 * h, y);
+              tmem_ld16_wait(y);
+#pragma unroll
+              for (int i = 0; i < 16; ++i) x[j][16 * h + i] = __float_as_uint(__uint_as_float(x[j][16 * h + i]) + __uint_as_float(y[i]));
+            }
+          }
+        }
+        give_back();
+        buf ^= 1u;
+        if (buf == 0) turn ^= 1u;
+      }
+      if (!ok) break;
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        if (32 * group + 128 * j < p.bn) leave(j, x[j]);
+    }
   }
+  if (lane == 0) tma_store_wait_read();       // (the writes land by the end of the kernel)
 }
 
-template <int CG, bool A_MN, bool B_MN>
+template <int CG, bool A_MN, bool B_MN, bool LONG>
 __global__ void __launch_bounds__(LIN_THREADS, 1)
-linear_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb, const __grid_constant__ GemmParams p) {
+linear_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb, const __grid_constant__ CUtensorMap mo, const __grid_constant__ CUtensorMap mp,
+              const __grid_constant__ GemmParams p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);      // the same in both CTAs of a pair
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + 8 * B_COUNT);
@@ -333,7 +533,7 @@ linear_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CU
   if (threadIdx.x == 0) {
     *abort_flag = 0u;
     for (int s = 0; s < MAX_STAGES; ++s) { mbar_init(c.bar(B_FULL + s), 1); mbar_init(c.bar(B_EMPTY + s), 1); }
-    for (int s = 0; s < 2; ++s) { mbar_init(c.bar(B_AFULL + s), 1); mbar_init(c.bar(B_AEMPTY + s), 8 * CG); }
+    for (int s = 0; s < 2; ++s) { mbar_init(c.bar(B_AFULL + s), 1); mbar_init(c.bar(B_AEMPTY + s), RESULT_WARPS * CG); }
     fence_barrier_init();
     fence_proxy_async();
     tma_prefetch_desc(&ma); tma_prefetch_desc(&mb);
@@ -349,10 +549,10 @@ linear_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CU
     if (elect_one()) lin_copies<CG, A_MN, B_MN>(p, c, &ma, &mb);
     __syncwarp();
   } else if (warp == 1) {
-    if (c.rank == 0 && elect_one()) lin_issue<CG, A_MN, B_MN>(p, c);
+    if (c.rank == 0 && elect_one()) lin_issue<CG, A_MN, B_MN, LONG>(p, c);
     __syncwarp();
   } else if (warp >= 4) {
-    lin_results<CG>(p, c, lane, warp - 4);
+    lin_results<CG, LONG>(p, c, &mo, &mp, lane, warp - 4);
   }
   if (*abort_flag != 0u) {                     // a wait ran out: copies and MMAs under way get 20 us (they take two) before memory is given back
     const long long t0 = clock64();
@@ -623,8 +823,9 @@ __global__ void __launch_bounds__(256) gather_kernel(const __grid_constant__ Gat
 using as_lin::Plan;
 using as_lin::plan_of;
 
-template <int CG, bool A_MN, bool B_MN>
-cudaError_t launch(const CUtensorMap& ma, const CUtensorMap& mb, const GemmParams& p, int units, size_t smem, cudaStream_t st) {
+struct Maps { CUtensorMap a, b, out, pre; };
+template <int CG, bool A_MN, bool B_MN, bool LONG>
+cudaError_t launch(const Maps& m, const GemmParams& p, int units, size_t smem, cudaStream_t st) {
   cudaLaunchAttribute attr[2]{};
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -633,7 +834,7 @@ cudaError_t launch(const CUtensorMap& ma, const CUtensorMap& mb, const GemmParam
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(units * CG)); cfg.blockDim = dim3(LIN_THREADS); cfg.dynamicSmemBytes = smem; cfg.stream = st;
   cfg.attrs = attr; cfg.numAttrs = CG == 1 ? 1 : 2;
-  return cudaLaunchKernelEx(&cfg, linear_kernel<CG, A_MN, B_MN>, ma, mb, p);
+  return cudaLaunchKernelEx(&cfg, linear_kernel<CG, A_MN, B_MN, LONG>, m.a, m.b, m.out, m.pre, p);
 }
 
 // Whether four columns of a matrix move at once.
@@ -715,7 +916,8 @@ Plan plan_for(const Product& q, int sms) {
   return plan_of(entries, q.a_mn ? q.M : q.T, q.M, q.N, ksteps, q.b_mn, sms);
 }
 
-cudaError_t run_product(as_fp8_context_t h, const Product& q, const Epilogue& e, void* part, cudaStream_t st) {
+// out, pre: what the epilogue's matrices are.
+cudaError_t run_product(as_fp8_context_t h, const Product& q, const Epilogue& e, const as_rows_t& out, const as_rows_t& pre, void* part, cudaStream_t st) {
   const Plan plan = plan_for(q, h->sms);
   GemmParams p{};
   p.e = e;
@@ -732,18 +934,30 @@ cudaError_t run_product(as_fp8_context_t h, const Product& q, const Epilogue& e,
   const int stage = (BM + plan.bn / plan.cg) * BK * 2;
   p.stages = std::min((SMEM_MAX - 1024 - STAGES_OFF) / stage, MAX_STAGES);
   const size_t smem = 1024 + STAGES_OFF + (size_t)p.stages * stage;
-  CUtensorMap ma, mb;
+  Maps m{};
+  auto boxes = [&](const as_rows_t& x, CUtensorMap* map) {             // (a map that the driver does not take leaves it to the warps)
+    return x.data != nullptr && x.dtype == AS_DTYPE_BF16 && rows_vec(x, 16) && (x.head_dim == q.N || x.head_dim % 32 == 0) && as_tc::make_map_rows(map, x, q.M, q.N, 32);
+  };
+  p.e.boxes = plan.parts == 1 && e.res.data == nullptr && boxes(out, &m.out);
+  p.e.pre_boxes = plan.parts == 1 && boxes(pre, &m.pre);
   const long long a_rows = q.a_mn ? q.K : q.M, a_cols = q.a_mn ? q.M : q.K, b_rows = q.b_mn ? q.K : q.N, b_cols = q.b_mn ? q.N : q.K;
   // (boxes behind the last column of a matrix without heads begin at their column, a multiple of 64, not at what is left of it behind a "head" of any width: a copy has to begin on 16 bytes)
   p.a_hd = q.a.head_dim == a_cols ? INT32_MAX : q.a.head_dim;
   p.b_hd = q.b.head_dim == b_cols ? INT32_MAX : q.b.head_dim;
-  if (!as_tc::make_map_boxes(&ma, in_entries(q.a, a_rows, q.T), a_rows, a_cols, q.a_mn ? 64 : BM) ||
-      !as_tc::make_map_boxes(&mb, q.a_mn ? in_entries(q.b, b_rows, q.T) : q.b, b_rows, b_cols, q.b_mn ? 64 : plan.bn / plan.cg))
+  if (!as_tc::make_map_boxes(&m.a, in_entries(q.a, a_rows, q.T), a_rows, a_cols, q.a_mn ? 64 : BM) ||
+      !as_tc::make_map_boxes(&m.b, q.a_mn ? in_entries(q.b, b_rows, q.T) : q.b, b_rows, b_cols, q.b_mn ? 64 : plan.bn / plan.cg))
     return cudaErrorInvalidValue;
   const int units = (int)std::min<long long>(p.units, h->sms / plan.cg);
   cudaError_t err;
-  if (plan.cg == 2) err = q.a_mn ? launch<2, true, true>(ma, mb, p, units, smem, st) : q.b_mn ? launch<2, false, true>(ma, mb, p, units, smem, st) : launch<2, false, false>(ma, mb, p, units, smem, st);
-  else err = q.a_mn ? launch<1, true, true>(ma, mb, p, units, smem, st) : q.b_mn ? launch<1, false, true>(ma, mb, p, units, smem, st) : launch<1, false, false>(ma, mb, p, units, smem, st);
+  // results in fp32 of long sums (operands of the forward product alone have them)
+  const bool is_long = e.out_f32 && (p.ksteps + p.parts - 1) / p.parts > CHUNK;
+  auto run = [&](auto cg) {
+    constexpr int CG = decltype(cg)::value;
+    if (q.a_mn) return launch<CG, true, true, false>(m, p, units, smem, st);
+    if (q.b_mn) return launch<CG, false, true, false>(m, p, units, smem, st);
+    return is_long ? launch<CG, false, false, true>(m, p, units, smem, st) : launch<CG, false, false, false>(m, p, units, smem, st);
+  };
+  err = plan.cg == 2 ? run(std::integral_constant<int, 2>{}) : run(std::integral_constant<int, 1>{});
   if (err != cudaSuccess || plan.parts == 1) return err;
   FinishParams f{};
   f.e = e; f.part = p.part; f.pitch = p.part_pitch; f.M = p.M; f.parts = p.parts;
@@ -802,8 +1016,8 @@ bool workspace_ok(const void* p, uint64_t has, uint64_t need) { return need == 0
 cudaError_t as_linear_init() {
   cudaError_t e = cudaSuccess;
   auto opt = [&](auto kernel, int bytes) { if (e == cudaSuccess) e = as_tc::opt_in_smem(kernel, bytes); };
-  opt(linear_kernel<1, false, false>, SMEM_MAX); opt(linear_kernel<1, false, true>, SMEM_MAX); opt(linear_kernel<1, true, true>, SMEM_MAX);
-  opt(linear_kernel<2, false, false>, SMEM_MAX); opt(linear_kernel<2, false, true>, SMEM_MAX); opt(linear_kernel<2, true, true>, SMEM_MAX);
+  opt(linear_kernel<1, false, false, false>, SMEM_MAX); opt(linear_kernel<1, false, false, true>, SMEM_MAX); opt(linear_kernel<1, false, true, false>, SMEM_MAX); opt(linear_kernel<1, true, true, false>, SMEM_MAX);
+  opt(linear_kernel<2, false, false, false>, SMEM_MAX); opt(linear_kernel<2, false, false, true>, SMEM_MAX); opt(linear_kernel<2, false, true, false>, SMEM_MAX); opt(linear_kernel<2, true, true, false>, SMEM_MAX);
   opt(linear_few_kernel<1>, few_smem(1)); opt(linear_few_kernel<2>, few_smem(2));
   return e;
 }
@@ -848,7 +1062,7 @@ extern "C" as_status_t as_linear(as_fp8_context_t h, const as_linear_t* a, void*
     return err == cudaSuccess ? AS_OK : failed();
   }
   l.q.a = l.x.rows; l.q.b = l.w.rows;
-  return run_product(h, l.q, e, room, st) == cudaSuccess ? AS_OK : failed();
+  return run_product(h, l.q, e, a->out, a->pre, room, st) == cudaSuccess ? AS_OK : failed();
 }
 
 namespace {
@@ -971,13 +1185,13 @@ extern "C" as_status_t as_linear_backward(as_fp8_context_t h, const as_linear_ba
     b.dx.a = dz; b.dx.b = b.w.rows;
     e.out = rows_of(a->dx, a->rows, a->cols);
     e.vec = a->cols % 4 == 0 && vec4(a->dx);
-    if (run_product(h, b.dx, e, room, st) != cudaSuccess) return failed();
+    if (run_product(h, b.dx, e, a->dx, as_rows_t{}, room, st) != cudaSuccess) return failed();
   }
   if (a->dw.data != nullptr) {
     b.dw.a = dz; b.dw.b = b.x.rows;
     e.out = rows_of(a->dw, a->out_cols, a->cols);
     e.vec = a->cols % 4 == 0 && vec4(a->dw);
-    if (run_product(h, b.dw, e, room, st) != cudaSuccess) return failed();
+    if (run_product(h, b.dw, e, a->dw, as_rows_t{}, room, st) != cudaSuccess) return failed();
   }
   return AS_OK;
 }
