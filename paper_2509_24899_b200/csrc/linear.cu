@@ -113,24 +113,23 @@ AS_DEV float activated(float z, int act) {
   with_activation(act, [&](auto a) { z = activated<decltype(a)::value>(z); });
   return z;
 }
-// (act(z), act'(z))
-AS_DEV float2 activated2(float z, int act) {
-  switch (act) {
-    case AS_ACT_RELU: return make_float2(z < 0.f ? 0.f : z, z > 0.f ? 1.f : z != z ? z : 0.f);
-    case AS_ACT_SILU: {
-      const float s = sigmoid(z), t = sigmoid(-z);
-      return make_float2(times(z, s), fabsf(z) > 200.f ? s : s * fmaf(z, t, 1.f));
-    }
-    case AS_ACT_GELU: {
-      float e;
-      const float c = normal_cdf(z, e);
-      return make_float2(times(z, c), fabsf(z) > 30.f ? c : fmaf(z * 0.3989422804f, e, c));
-    }
-    case AS_ACT_GELU_TANH: {
-      const float q = GELU_B * z * z, u = GELU_A * z * (1.f + q), s = sigmoid(u), t = sigmoid(-u);
-      return make_float2(times(z, s), fabsf(z) > 30.f ? s : fmaf(z * s, t * GELU_A * fmaf(3.f, q, 1.f), s));
-    }
-    default: return make_float2(z, 1.f);
+// (act(z), act'(z)).  sigmoid(-x) is e^-x sigmoid(x); arguments below -80 count as that, where both are 0 to fp32 beside anything that they are added to.
+template <int ACT>
+AS_DEV float2 activated2(float z) {
+  if constexpr (ACT == AS_ACT_RELU) {
+    return make_float2(z < 0.f ? 0.f : z, z > 0.f ? 1.f : z != z ? z : 0.f);
+  } else if constexpr (ACT == AS_ACT_SILU) {
+    const float e = ex2(-1.442695041f * (z < -80.f ? -80.f : z)), s = __fdividef(1.f, 1.f + e), t = e * s;
+    return make_float2(z < -80.f ? 0.f : z * s, z < -80.f ? 0.f : t == 0.f ? s : s * fmaf(z, t, 1.f));
+  } else if constexpr (ACT == AS_ACT_GELU) {
+    float e;
+    const float c = normal_cdf(z, e);
+    return make_float2(times(z, c), e == 0.f ? c : fmaf(z * 0.3989422804f, e, c));
+  } else if constexpr (ACT == AS_ACT_GELU_TANH) {
+    const float q = GELU_B * z * z, u = GELU_A * z * (1.f + q), e = ex2(-1.442695041f * (u < -80.f ? -80.f : u)), s = __fdividef(1.f, 1.f + e), t = e * s;
+    return make_float2(u < -80.f ? 0.f : z * s, u < -80.f ? 0.f : t == 0.f ? s : fmaf(z * s, t * GELU_A * fmaf(3.f, q, 1.f), s));
+  } else {
+    return make_float2(z, 1.f);
   }
 }
 
@@ -380,53 +379,70 @@ AS_DEV void leave_rows(const Target& to, const Target& res, bool vec, uint32_t s
   __syncwarp();
 }
 
-// Sums of 32 rows x 32 columns, on to out and pre.  `bias` and `gate`: this lane's column's; gates_alike: all rows have the same ones.
-AS_DEV void leave_strip(const Epilogue& e, const CUtensorMap* mo, const CUtensorMap* mp, const Box& out_box, const Box& pre_box, uint32_t strip, uint32_t vectors, int lane, int m0, int rows, int n0,
-                        float bias, float gate, bool gates_alike, uint32_t (&w)[32]) {
-  float(&x)[32] = reinterpret_cast<float(&)[32]>(w);
-  const bool biased = e.bias != nullptr, gated = e.gate != nullptr;
-  if (biased) asm volatile("st.shared.f32 [%0], %1;" ::"r"(vectors + lane * 4), "f"(bias) : "memory");
-  if (gated) asm volatile("st.shared.f32 [%0], %1;" ::"r"(vectors + 128 + lane * 4), "f"(gate) : "memory");
-  if (biased || gated) __syncwarp();
-  auto vector = [&](uint32_t at, int i) {
-    float4 b;
-    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(b.x), "=f"(b.y), "=f"(b.z), "=f"(b.w) : "r"(at + i * 16) : "memory");
-    return b;
-  };
-  if (biased) {
+// Biases and gates of 32 columns, a column a lane, to where the warp reads them four at a time.
+AS_DEV void keep_vectors(const Epilogue& e, uint32_t vectors, int lane, float bias, float gate) {
+  __syncwarp();
+  if (e.bias != nullptr) asm volatile("st.shared.f32 [%0], %1;" ::"r"(vectors + lane * 4), "f"(bias) : "memory");
+  if (e.gate != nullptr) asm volatile("st.shared.f32 [%0], %1;" ::"r"(vectors + 128 + lane * 4), "f"(gate) : "memory");
+  __syncwarp();
+}
+AS_DEV float4 read4(uint32_t at) {
+  float4 b;
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(b.x), "=f"(b.y), "=f"(b.z), "=f"(b.w) : "r"(at) : "memory");
+  return b;
+}
+template <int W>
+AS_DEV void add_bias(const Epilogue& e, uint32_t at, float (&x)[W]) {
+  if (e.bias == nullptr) return;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float4 b = vector(vectors, i);
-      x[4 * i] += b.x; x[4 * i + 1] += b.y; x[4 * i + 2] += b.z; x[4 * i + 3] += b.w;
-    }
+  for (int i = 0; i < W / 4; ++i) {
+    const float4 b = read4(at + i * 16);
+    x[4 * i] += b.x; x[4 * i + 1] += b.y; x[4 * i + 2] += b.z; x[4 * i + 3] += b.w;
   }
+}
+// Activation and gate; gates_alike: all rows have those that are kept, else this lane's row, m, has its own.
+template <int W>
+AS_DEV void activate_and_gate(const Epilogue& e, uint32_t at, bool gates_alike, int m, int n0, float (&x)[W]) {
+  with_activation(e.act, [&](auto a) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) x[i] = activated<decltype(a)::value>(x[i]);
+  });
+  if (e.gate == nullptr) return;
+  if (gates_alike) {
+#pragma unroll
+    for (int i = 0; i < W / 4; ++i) {
+      const float4 g = read4(at + i * 16);
+      x[4 * i] *= g.x; x[4 * i + 1] *= g.y; x[4 * i + 2] *= g.z; x[4 * i + 3] *= g.w;
+    }
+  } else {
+    const long long row = (long long)((unsigned)m / e.gate_rows) * e.gate_stride;
+#pragma unroll
+    for (int i = 0; i < W; ++i) x[i] *= n0 + i < e.N ? ld1(e.gate, e.gate_f32, row + n0 + i) : 0.f;
+  }
+}
+
+// Sums of 32 rows x 32 columns, on to out and pre.
+AS_DEV void leave_strip(const Epilogue& e, const CUtensorMap* mo, const CUtensorMap* mp, const Box& out_box, const Box& pre_box, uint32_t strip, uint32_t vectors, int lane, int m0, int rows, int n0,
+                        bool gates_alike, float (&x)[32]) {
+  add_bias(e, vectors, x);
   if (e.pre.data != nullptr) {
     if (pre_box.whole) leave_box(mp, e.pre, pre_box, strip, lane, rows, n0, e.N, x);
     else
 #pragma unroll
       for (int h = 0; h < 2; ++h) leave_rows({e.pre, false}, {}, e.vec, strip, lane, m0, rows, n0 + 16 * h, e.N, x + 16 * h);
   }
-  with_activation(e.act, [&](auto a) {
-#pragma unroll
-    for (int i = 0; i < 32; ++i) x[i] = activated<decltype(a)::value>(x[i]);
-  });
-  if (gated) {
-    if (gates_alike) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float4 g = vector(vectors + 128, i);
-        x[4 * i] *= g.x; x[4 * i + 1] *= g.y; x[4 * i + 2] *= g.z; x[4 * i + 3] *= g.w;
-      }
-    } else {
-      const long long at = (long long)((unsigned)(m0 + min(lane, rows - 1)) / e.gate_rows) * e.gate_stride;
-#pragma unroll
-      for (int i = 0; i < 32; ++i) x[i] *= n0 + i < e.N && rows > 0 ? ld1(e.gate, e.gate_f32, at + n0 + i) : 0.f;
-    }
-  }
+  activate_and_gate(e, vectors + 128, gates_alike, m0 + max(0, min(lane, rows - 1)), n0, x);
   if (out_box.whole) leave_box(mo, e.out, out_box, strip, lane, rows, n0, e.N, x);
   else
 #pragma unroll
     for (int h = 0; h < 2; ++h) leave_rows({e.out, e.out_f32}, {e.res, e.res_f32}, e.vec, strip, lane, m0, rows, n0 + 16 * h, e.N, x + 16 * h);
+}
+// The same of 16 columns, results in fp32.
+AS_DEV void leave_half(const Epilogue& e, uint32_t strip, uint32_t vectors, int lane, int m0, int rows, int n0, bool gates_alike, float (&x)[16]) {
+  add_bias(e, vectors, x);
+  if (e.pre.data != nullptr) leave_rows({e.pre, false}, {}, e.vec, strip, lane, m0, rows, n0, e.N, x);
+  activate_and_gate(e, vectors + 128, gates_alike, m0 + max(0, min(lane, rows - 1)), n0, x);
+  leave_rows({e.out, true}, {e.res, e.res_f32}, e.vec, strip, lane, m0, rows, n0, e.N, x);
 }
 
 // Results of a tile: this warp's 32 rows, 32 of every 128 columns.  LONG: of a tile's sums, which come in runs of CHUNK steps.
@@ -456,15 +472,9 @@ AS_DEV void lin_results(const GemmParams& p, const Ctx<CG>& c, const CUtensorMap
       bias[j] = e.bias != nullptr && n < e.N ? ld1(e.bias, e.bias_f32, n) : 0.f;
       gate[j] = e.gate != nullptr && n < e.N ? ld1(e.gate, e.gate_f32, gate_row * e.gate_stride + n) : 0.f;
     }
-    auto leave = [&](int j, uint32_t (&x)[32]) {
-      const int n0 = w.n0 + 32 * group + 128 * j;
-      if (p.part != nullptr) {
-        const Target to{Rows{p.part + (long long)w.part * p.M * p.part_pitch, 0, 0, p.part_pitch, 1u, 1, 0ull, false, false}, true};
-#pragma unroll
-        for (int h = 0; h < 2; ++h) leave_rows(to, {}, true, strip, lane, m0, rows, n0 + 16 * h, e.N, reinterpret_cast<float*>(x) + 16 * h);
-      } else {
-        leave_strip(e, mo, mp, out_box, pre_box, strip, vectors, lane, m0, rows, n0, bias[j], gate[j], gates_alike, x);
-      }
+    auto to_parts = [&](int n0, const float* x) {
+      const Target to{Rows{p.part + (long long)w.part * p.M * p.part_pitch, 0, 0, p.part_pitch, 1u, 1, 0ull, false, false}, true};
+      leave_rows(to, {}, true, strip, lane, m0, rows, n0, e.N, x);
     };
     if constexpr (!LONG) {
       if (!mbar_wait_warp(c.bar(B_AFULL + buf), turn, c.wc)) break;
@@ -478,34 +488,38 @@ AS_DEV void lin_results(const GemmParams& p, const Ctx<CG>& c, const CUtensorMap
         tmem_ld32(c.tmem + lanes + buf * 256u + c0, x);
         tmem_ld_wait(x);
         if (c0 + 128 >= p.bn) give_back();    // this warp has read its part of the accumulator
-        leave(j, x);
+        float(&f)[32] = reinterpret_cast<float(&)[32]>(x);
+        const int n0 = w.n0 + c0;
+        if (p.part != nullptr) {
+          to_parts(n0, f);
+          to_parts(n0 + 16, f + 16);
+        } else {
+          keep_vectors(e, vectors, lane, bias[j], gate[j]);
+          leave_strip(e, mo, mp, out_box, pre_box, strip, vectors, lane, m0, rows, n0, gates_alike, f);
+        }
       }
       buf ^= 1u;
       if (buf == 0) turn ^= 1u;
     } else {
-      uint32_t x[2][32];
+      float x[4][16];                         // columns 32 group + 128 (i / 2) + 16 (i % 2)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int k = 0; k < 16; ++k) x[i][k] = 0.f;
       bool ok = true;
-      for (int k = w.k0; k < w.k1 && ok; k += CHUNK) {
+      for (int k = w.k0; k < w.k1; k += CHUNK) {
         ok = mbar_wait_warp(c.bar(B_AFULL + buf), turn, c.wc);
         if (!ok) break;
         tc_fence_after();
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int c0 = 32 * group + 128 * j;
+        for (int i = 0; i < 4; ++i) {
+          const int c0 = 32 * group + 128 * (i / 2) + 16 * (i % 2);
           if (c0 >= p.bn) continue;
-          if (k == w.k0) {
-            tmem_ld32(c.tmem + lanes + buf * 256u + c0, x[j]);
-            tmem_ld_wait(x[j]);
-          } else {
+          uint32_t y[16];
+          tmem_ld16(c.tmem + lanes + buf * 256u + c0, y);
+          tmem_ld16_wait(y);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              uint32_t y[16];
-              tmem_ld16(c.tmem + lanes + buf * 256u + c0 + 16 * h, y);
-              tmem_ld16_wait(y);
-#pragma unroll
-              for (int i = 0; i < 16; ++i) x[j][16 * h + i] = __float_as_uint(__uint_as_float(x[j][16 * h + i]) + __uint_as_float(y[i]));
-            }
-          }
+          for (int q = 0; q < 16; ++q) x[i][q] += __uint_as_float(y[q]);
         }
         give_back();
         buf ^= 1u;
@@ -513,8 +527,13 @@ AS_DEV void lin_results(const GemmParams& p, const Ctx<CG>& c, const CUtensorMap
       }
       if (!ok) break;
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
-        if (32 * group + 128 * j < p.bn) leave(j, x[j]);
+      for (int i = 0; i < 4; ++i) {
+        const int c0 = 32 * group + 128 * (i / 2) + 16 * (i % 2), n0 = w.n0 + c0;
+        if (c0 >= p.bn) continue;
+        if (p.part != nullptr) { to_parts(n0, x[i]); continue; }
+        if (i % 2 == 0) keep_vectors(e, vectors, lane, bias[i / 2], gate[i / 2]);
+        leave_half(e, strip, vectors + 64 * (i % 2), lane, m0, rows, n0, gates_alike, x[i]);
+      }
     }
   }
   if (lane == 0) tma_store_wait_read();       // (the writes land by the end of the kernel)
@@ -698,7 +717,8 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 1) linear_few_kernel(const __g
 
 // ---------------------------------------------------------------- dz, and sums over rows
 // dz = dy * gate * act'(pre) in bf16, the sums of dz and of dy * act(pre) over runs of rows, which do not cross from one gate's rows to another's.  A lane has 8 columns, a warp
-// every eighth row of the run; the warps' sums meet in shared memory in their order.  One pass over dy and pre: HBM bytes.
+// every eighth row of the run, two at once; the warps' sums meet in shared memory in their order.  One pass over dy and pre: HBM bytes.  (With the activation chosen at every value, and both its
+// sigmoids from exponentials of their own, 7800 x 6144 took 254 us.)
 struct DzParams {
   Rows dy, pre;
   const void* gate;
@@ -706,59 +726,93 @@ struct DzParams {
   float *part_b, *part_g;                    // [gates * runs][N], or nullptr
   long long gate_stride, pitch;
   int N, act, rows_gate, runs;               // rows that share a gate; runs of them
-  bool dy_f32, gate_f32, vec;
+  bool gate_f32, vec;
 };
 constexpr int DZ_COLS = 256;
+AS_DEV void unpack8(const uint4& w, float (&f)[8]) {
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(u[i] << 16); f[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
+}
 
+template <int ACT, typename Y>
 __global__ void __launch_bounds__(256) dz_kernel(const __grid_constant__ DzParams p) {
   griddep_launch();
   __shared__ float room[8][DZ_COLS + 8];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int n = blockIdx.x * DZ_COLS + lane * 8, gate = blockIdx.y / p.runs, run = blockIdx.y - gate * p.runs;
-  const long long r0 = (long long)p.rows_gate * run / p.runs, r1 = (long long)p.rows_gate * (run + 1) / p.runs, first = (long long)gate * p.rows_gate;
+  const int r0 = (int)((long long)p.rows_gate * run / p.runs), r1 = (int)((long long)p.rows_gate * (run + 1) / p.runs);
+  const unsigned first = (unsigned)(gate * (long long)p.rows_gate);
   griddep_wait();
+  const bool keeps = p.pre.data != nullptr, gated = p.gate != nullptr, of_gate = p.part_g != nullptr;
   float g[8], sb[8] = {}, sg[8] = {};
 #pragma unroll
-  for (int i = 0; i < 8; ++i) g[i] = p.gate != nullptr && n + i < p.N ? ld1(p.gate, p.gate_f32, (long long)gate * p.gate_stride + n + i) : 1.f;
-  if (n < p.N) {
-#pragma unroll 2
-    for (long long r = r0 + warp; r < r1; r += 8) {
-      const unsigned m = (unsigned)(first + r);
-      float d[8], z[8] = {};
-      const long long dr = p.dy.row(m), pr = p.pre.data != nullptr ? p.pre.row(m) : 0;
-      if (p.vec) {
-        const long long dc = dr + p.dy.col((unsigned)n);
-        *reinterpret_cast<float4*>(d) = ld4(p.dy.data, p.dy_f32, dc);
-        *reinterpret_cast<float4*>(d + 4) = ld4(p.dy.data, p.dy_f32, dc + 4);
-        if (p.pre.data != nullptr) {
-          const uint4 w = *reinterpret_cast<const uint4*>(static_cast<const bf*>(p.pre.data) + pr + p.pre.col((unsigned)n));
-          const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+  for (int i = 0; i < 8; ++i) g[i] = gated && n + i < p.N ? ld1(p.gate, p.gate_f32, (long long)gate * p.gate_stride + n + i) : 1.f;
+  const Y* dy = static_cast<const Y*>(p.dy.data);
+  const bf* pre = static_cast<const bf*>(p.pre.data);
+  // one row's values on to dz and the sums
+  auto take = [&](unsigned m, float (&d)[8], const float (&z)[8]) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) { z[2 * i] = __uint_as_float(u[i] << 16); z[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
-        }
-      } else {
+    for (int i = 0; i < 8; ++i) {
+      const float2 a = activated2<ACT>(z[i]);
+      if (of_gate) sg[i] = fmaf(d[i], a.x, sg[i]);
+      d[i] = d[i] * g[i] * a.y;
+      sb[i] += d[i];
+    }
+    if (p.dz == nullptr) return;
+    bf* at = p.dz + (long long)m * p.pitch + n;
+    if (n + 8 <= p.N) {
+      *reinterpret_cast<uint4*>(at) = make_uint4(pack_bf16(d[0], d[1]), pack_bf16(d[2], d[3]), pack_bf16(d[4], d[5]), pack_bf16(d[6], d[7]));
+    } else {
+      for (int i = 0; i < 8; ++i)
+        if (n + i < p.N) at[i] = __float2bfloat16_rn(d[i]);
+    }
+  };
+  if (n < p.N && p.vec) {
+    const long long dc = p.dy.col((unsigned)n), pc = keeps ? p.pre.col((unsigned)n) : 0;
+    struct Row { uint4 d[sizeof(Y) / 2], z; };
+    auto fetch = [&](unsigned m, Row& v) {
+      const uint4* at = reinterpret_cast<const uint4*>(dy + p.dy.row(m) + dc);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          d[i] = n + i < p.N ? ld1(p.dy.data, p.dy_f32, dr + p.dy.col((unsigned)(n + i))) : 0.f;
-          if (p.pre.data != nullptr) z[i] = n + i < p.N ? ld1(p.pre.data, false, pr + p.pre.col((unsigned)(n + i))) : 0.f;
-        }
+      for (int i = 0; i < (int)sizeof(Y) / 2; ++i) v.d[i] = at[i];
+      v.z = keeps ? *reinterpret_cast<const uint4*>(pre + p.pre.row(m) + pc) : make_uint4(0u, 0u, 0u, 0u);
+    };
+    auto use = [&](unsigned m, const Row& v) {
+      float d[8], z[8];
+      if constexpr (sizeof(Y) == 2) unpack8(v.d[0], d);
+      else {
+        *reinterpret_cast<uint4*>(d) = v.d[0];
+        *reinterpret_cast<uint4*>(d + 4) = v.d[1];
       }
+      unpack8(v.z, z);
+      take(m, d, z);
+    };
+    Row now[2], next[2];
+    int r = r0 + warp;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (r + 8 * i < r1) fetch(first + (unsigned)(r + 8 * i), now[i]);
+    for (; r < r1; r += 16) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (r + 16 + 8 * i < r1) fetch(first + (unsigned)(r + 16 + 8 * i), next[i]);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (r + 8 * i < r1) use(first + (unsigned)(r + 8 * i), now[i]);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) now[i] = next[i];
+    }
+  } else if (n < p.N) {
+    for (int r = r0 + warp; r < r1; r += 8) {
+      const unsigned m = first + (unsigned)r;
+      const long long dr = p.dy.row(m), pr = keeps ? p.pre.row(m) : 0;
+      float d[8], z[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float2 a = activated2(z[i], p.act);
-        sg[i] = fmaf(d[i], a.x, sg[i]);
-        d[i] = d[i] * g[i] * a.y;
-        sb[i] += d[i];
+        d[i] = n + i < p.N ? (float)dy[dr + p.dy.col((unsigned)(n + i))] : 0.f;
+        z[i] = keeps && n + i < p.N ? __bfloat162float(pre[pr + p.pre.col((unsigned)(n + i))]) : 0.f;
       }
-      if (p.dz != nullptr) {
-        bf* at = p.dz + (long long)m * p.pitch + n;
-        if (n + 8 <= p.N) {
-          *reinterpret_cast<uint4*>(at) = make_uint4(pack_bf16(d[0], d[1]), pack_bf16(d[2], d[3]), pack_bf16(d[4], d[5]), pack_bf16(d[6], d[7]));
-        } else {
-          for (int i = 0; i < 8; ++i)
-            if (n + i < p.N) at[i] = __float2bfloat16_rn(d[i]);
-        }
-      }
+      take(m, d, z);
     }
   }
   auto leave = [&](const float (&s)[8], float* part) {
@@ -777,6 +831,17 @@ __global__ void __launch_bounds__(256) dz_kernel(const __grid_constant__ DzParam
   };
   leave(sb, p.part_b);
   leave(sg, p.part_g);
+}
+template <typename Y>
+cudaError_t launch_dz(const DzParams& p, dim3 grid, cudaStream_t st) {
+  const dim3 block(256);
+  switch (p.act) {
+    case AS_ACT_RELU: return as_launch_dependent(dz_kernel<AS_ACT_RELU, Y>, grid, block, 0, st, p);
+    case AS_ACT_SILU: return as_launch_dependent(dz_kernel<AS_ACT_SILU, Y>, grid, block, 0, st, p);
+    case AS_ACT_GELU: return as_launch_dependent(dz_kernel<AS_ACT_GELU, Y>, grid, block, 0, st, p);
+    case AS_ACT_GELU_TANH: return as_launch_dependent(dz_kernel<AS_ACT_GELU_TANH, Y>, grid, block, 0, st, p);
+    default: return as_launch_dependent(dz_kernel<AS_ACT_NONE, Y>, grid, block, 0, st, p);
+  }
 }
 
 // Columns' sums over runs of rows, in order: block row 0 all of them (the bias), 1 + i those of gate i.
@@ -841,6 +906,9 @@ cudaError_t launch(const Maps& m, const GemmParams& p, int units, size_t smem, c
 bool vec4(const as_rows_t& x) {
   return x.data == nullptr || (aligned(x.data, x.dtype == AS_DTYPE_BF16 ? 8 : 16) && ((x.head_dim | x.stride_batch | x.stride_head | x.stride_token) & 3) == 0);
 }
+
+// Whether 16 bytes of a matrix move at once.
+bool rows_vec16(const as_rows_t& x) { return aligned(x.data, 16) && ((x.stride_batch | x.stride_head | x.stride_token) & (x.dtype == AS_DTYPE_BF16 ? 7 : 3)) == 0; }
 
 // An operand as the copies read it: rows in entries of T.
 as_rows_t in_entries(as_rows_t x, long long rows, long long T) {
@@ -1105,7 +1173,7 @@ BackPlan plan_back(as_fp8_context_t h, const as_linear_backward_t& a) {
   b.dz = (dx || dw) && (a.activation != AS_ACT_NONE || a.gate != nullptr || b.dy.copy || (dw && b.dy.rows.tokens != a.rows && b.x.rows.tokens != b.dy.rows.tokens));
   b.pitch = pitch_of(a.out_cols);
   const long long gates = a.gate != nullptr ? a.gates : 1, across = (a.out_cols + DZ_COLS - 1) / DZ_COLS, rows_gate = a.rows / gates;
-  b.runs = (int)std::max<long long>(1, std::min<long long>((4ll * h->sms + across * gates - 1) / (across * gates), rows_gate / 16));
+  b.runs = (int)std::max<long long>(1, std::min<long long>((8ll * h->sms + across * gates - 1) / (across * gates), rows_gate / 32));
   if (b.dz) b.bytes += up256((uint64_t)a.rows * (uint64_t)b.pitch * 2);
   if (a.dbias != nullptr) b.bytes += up256((uint64_t)gates * b.runs * a.out_cols * 4);
   if (a.dgate != nullptr) b.bytes += up256((uint64_t)gates * b.runs * a.out_cols * 4);
@@ -1162,8 +1230,8 @@ extern "C" as_status_t as_linear_backward(as_fp8_context_t h, const as_linear_ba
   z.pitch = b.pitch;
   z.N = (int)a->out_cols; z.act = a->activation;
   z.rows_gate = (int)(a->rows / gates); z.runs = b.runs;
-  z.dy_f32 = a->dy.dtype == AS_DTYPE_F32; z.gate_f32 = a->gate_dtype == AS_DTYPE_F32;
-  z.vec = a->out_cols % 8 == 0 && a->dy.head_dim % 8 == 0 && vec4(a->dy) && (a->pre.data == nullptr || rows_vec(a->pre, 16));
+  z.gate_f32 = a->gate_dtype == AS_DTYPE_F32;
+  z.vec = a->out_cols % 8 == 0 && a->dy.head_dim % 8 == 0 && rows_vec16(a->dy) && (a->pre.data == nullptr || rows_vec(a->pre, 16));
   if (b.dz) { z.dz = reinterpret_cast<bf*>(room); room += up256((uint64_t)a->rows * (uint64_t)b.pitch * 2); }
   const uint64_t sum_bytes = up256((uint64_t)gates * b.runs * a->out_cols * 4);
   if (a->dbias != nullptr) { z.part_b = reinterpret_cast<float*>(room); room += sum_bytes; }
@@ -1171,7 +1239,7 @@ extern "C" as_status_t as_linear_backward(as_fp8_context_t h, const as_linear_ba
   if (gates * b.runs > 65535) return AS_ERR_UNSUPPORTED;
   if (b.dz || b.sums) {
     const dim3 grid((unsigned)((a->out_cols + DZ_COLS - 1) / DZ_COLS), (unsigned)(gates * b.runs));
-    if (as_launch_dependent(dz_kernel, grid, dim3(256), 0, st, z) != cudaSuccess) return failed();
+    if ((a->dy.dtype == AS_DTYPE_F32 ? launch_dz<float>(z, grid, st) : launch_dz<bf>(z, grid, st)) != cudaSuccess) return failed();
   }
   if (b.sums) {
     ColumnSumParams c{z.part_b, z.part_g, a->dbias, a->dgate, z.N, b.runs, (int)gates, a->bias_dtype == AS_DTYPE_F32, z.gate_f32};
