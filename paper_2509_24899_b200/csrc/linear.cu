@@ -7,7 +7,7 @@
 //   warp 0       copies (TMA, 64 steps of the summed index a stage, 128-byte swizzle), told by the leading CTA's barrier
 //   warp 1       the MMAs (leading CTA only)
 //   warp 2       allocates tensor memory
-//   warps 4-19   results, 32 rows x 32 columns at a time: tensor memory -> registers, a lane a row: bias, activation, gate, bf16, a strip of shared memory, from where TMA takes
+//   warps 3-18   results, 32 rows x 32 columns at a time: tensor memory -> registers, a lane a row: bias, activation, gate, bf16, a strip of shared memory, from where TMA takes
 //                them; with a residual, in fp32 or in layouts without boxes 16 columns at a time through the strip, from where 4 lanes move a row
 //
 // What bounds it is the tensor pipe and the operands' bytes into an SM, which for 256 x 256 are level: 64 bytes a clock beside 8192 operations.
@@ -31,18 +31,17 @@ using namespace as_fp8;
 using namespace sm100;
 typedef __nv_bfloat16 bf;
 
-constexpr int RESULT_WARPS = 16, LIN_THREADS = (4 + RESULT_WARPS) * 32;
+constexpr int RESULT_WARPS = 16, FIRST_RESULT = 3, LIN_THREADS = (FIRST_RESULT + RESULT_WARPS) * 32;
 constexpr int BM = LIN_BM, BK = LIN_BK;
 constexpr int MAX_STAGES = 10;
 constexpr int SMEM_MAX = 227 * 1024;
 constexpr uint32_t BOX = 64 * 128;          // bytes of a box of 64 x 64
 
-enum { B_FULL = 0, B_EMPTY = B_FULL + MAX_STAGES, B_AFULL = B_EMPTY + MAX_STAGES, B_AEMPTY = B_AFULL + 2, B_COUNT = B_AEMPTY + 2 };
-// shared memory: barriers, tensor-memory address, abort flag; for each result warp a strip of 32 rows x 64 bytes, and 32 biases and gates; then the stages
+enum { B_FULL = 0, B_EMPTY = B_FULL + MAX_STAGES, B_AFULL = B_EMPTY + MAX_STAGES, B_AEMPTY = B_AFULL + 2, B_RES = B_AEMPTY + 2, B_COUNT = B_RES + 2 * RESULT_WARPS };
+// shared memory: barriers, tensor-memory address, abort flag; for each result warp two strips of 32 rows x 64 bytes, which results leave from and residuals come to; then the stages
 constexpr int STRIP = 32 * 64;
 constexpr int STRIPS_OFF = 1024;
-constexpr int VECTORS_OFF = STRIPS_OFF + RESULT_WARPS * STRIP;
-constexpr int STAGES_OFF = VECTORS_OFF + RESULT_WARPS * 256;
+constexpr int STAGES_OFF = STRIPS_OFF + RESULT_WARPS * 2 * STRIP;
 // Byte of 16-byte chunk `ch` of a strip's row: the 64-byte swizzle.
 AS_DEV uint32_t swz64(int row, int ch) { return (uint32_t)(row * 64 + ((ch ^ (row >> 1 & 3)) << 4)); }
 static_assert(B_COUNT * 8 + 8 <= STRIPS_OFF && STAGES_OFF % 1024 == 0, "");
@@ -56,7 +55,7 @@ struct Epilogue {
   int N, act;
   bool out_f32, res_f32, bias_f32, gate_f32;
   bool vec;                                  // four columns move at once
-  bool boxes, pre_boxes;                     // out (without a residual) and pre leave in boxes of 32 rows x 32 columns by TMA
+  bool boxes, pre_boxes, res_boxes;          // out and pre leave, and the residual comes, in boxes of 32 rows x 64 bytes by TMA
 };
 
 AS_DEV float ld1(const void* p, bool f32, long long i) { return f32 ? static_cast<const float*>(p)[i] : __bfloat162float(static_cast<const bf*>(p)[i]); }
@@ -207,6 +206,16 @@ AS_DEV void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc
                  ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
 
+// 8 columns of a lane's row, waited for; and back.
+AS_DEV void tmem_ld8(uint32_t at, float (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n\ttcgen05.wait::ld.sync.aligned;"
+               : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]) : "r"(at) : "memory");
+}
+AS_DEV void tmem_st8(uint32_t at, const float (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"r"(at), "f"(r[0]), "f"(r[1]), "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]) : "memory");
+}
+
 template <int CG>
 struct Ctx {
   uint32_t sbase, tmem;
@@ -237,36 +246,47 @@ template <int CG, bool A_MN, bool B_MN>
 AS_DEV void lin_copies(const GemmParams& p, const Ctx<CG>& c, const CUtensorMap* ma, const CUtensorMap* mb) {
   const int rows_b = p.bn / CG;
   const uint32_t stage_bytes = (uint32_t)(BM + rows_b) * BK * 2;
+  constexpr int A_BOXES = A_MN ? BM / 64 : 1, B_BOXES = B_MN ? 256 / CG / 64 : 1;
   Ring r;
   for (long long u = c.unit; u < p.units; u += c.step) {
     const Unit w = unit_of<CG>(p, u);
     const int m0 = w.t0 + (int)c.rank * BM, n0 = w.n0 + (int)c.rank * rows_b;
+    // Where boxes begin.  What does not change from step to step is divided here: with the heads of every box looked for at every step this thread was what the products waited for (32760 x 6144 by
+    // 1536, columns of w in a run: 571 us, 423 us where a step has two boxes).
+    int ax[A_BOXES], ah[A_BOXES], bx[B_BOXES], bh[B_BOXES];
+    if constexpr (A_MN) {
+#pragma unroll
+      for (int i = 0; i < A_BOXES; ++i) { ah[i] = (m0 + 64 * i) / p.a_hd; ax[i] = m0 + 64 * i - ah[i] * p.a_hd; }
+    } else {
+      ah[0] = w.k0 * BK / p.a_hd;
+      ax[0] = w.k0 * BK - ah[0] * p.a_hd;
+    }
+    if constexpr (B_MN) {
+#pragma unroll
+      for (int i = 0; i < B_BOXES; ++i) { bh[i] = (n0 + 64 * i) / p.b_hd; bx[i] = n0 + 64 * i - bh[i] * p.b_hd; }
+    }
+    int ke = A_MN ? w.k0 / p.ks_entry : 0, kt = A_MN ? w.k0 - ke * p.ks_entry : w.k0;      // entry and step of the summed index
     for (int k = w.k0; k < w.k1; ++k) {
       if (!c.wait(B_EMPTY + r.slot, r.turn ^ 1u)) goto out;
-      {
-        const uint32_t at = c.sbase + STAGES_OFF + (uint32_t)r.slot * stage_bytes, bt = at + BM * BK * 2;
-        if (c.rank == 0) mbar_expect_tx(c.bar(B_FULL + r.slot), stage_bytes * CG);
-        const uint32_t bar = CG == 1 ? c.bar(B_FULL + r.slot) : leaders(c.bar(B_FULL + r.slot));
-        const int ke = A_MN ? k / p.ks_entry : 0, kt = (k - ke * p.ks_entry) * BK;       // entry and row of the summed index
-        if constexpr (A_MN) {
+      const uint32_t at = c.sbase + STAGES_OFF + (uint32_t)r.slot * stage_bytes, bt = at + BM * BK * 2;
+      if (c.rank == 0) mbar_expect_tx(c.bar(B_FULL + r.slot), stage_bytes * CG);
+      const uint32_t bar = CG == 1 ? c.bar(B_FULL + r.slot) : leaders(c.bar(B_FULL + r.slot));
+      if constexpr (A_MN) {
 #pragma unroll
-          for (int i = 0; i < BM / 64; ++i) {
-            const int col = m0 + 64 * i, h = col / p.a_hd;
-            load_box4<CG>(at + i * BOX, ma, bar, col - h * p.a_hd, kt, h, ke);
-          }
-        } else {
-          const int col = k * BK, h = col / p.a_hd;
-          load_box4<CG>(at, ma, bar, col - h * p.a_hd, m0, h, w.entry);
-        }
-        if constexpr (B_MN) {
-          for (int i = 0; i < rows_b / 64; ++i) {
-            const int col = n0 + 64 * i, h = col / p.b_hd;
-            load_box4<CG>(bt + i * BOX, mb, bar, col - h * p.b_hd, A_MN ? kt : k * BK, h, ke);
-          }
-        } else {
-          load_box4<CG>(bt, mb, bar, k * BK, n0, 0, 0);
-        }
+        for (int i = 0; i < A_BOXES; ++i) load_box4<CG>(at + i * BOX, ma, bar, ax[i], kt * BK, ah[i], ke);
+      } else {
+        load_box4<CG>(at, ma, bar, ax[0], m0, ah[0], w.entry);
+        ax[0] += BK;
+        if (ax[0] >= p.a_hd) { ax[0] = 0; ++ah[0]; }
       }
+      if constexpr (B_MN) {
+#pragma unroll
+        for (int i = 0; i < B_BOXES; ++i)
+          if (64 * i < rows_b) load_box4<CG>(bt + i * BOX, mb, bar, bx[i], kt * BK, bh[i], ke);
+      } else {
+        load_box4<CG>(bt, mb, bar, k * BK, n0, 0, 0);
+      }
+      if (++kt == p.ks_entry && A_MN) { kt = 0; ++ke; }
       r.next(p.stages);
     }
   }
@@ -278,9 +298,17 @@ out:
   }
 }
 
-// LONG: sums of more than CHUNK steps go to the result warps in runs of as many, which add them up in fp32 rounded to nearest.  The tensor cores truncate: over 384 instructions (6144 columns) that
-// left 4e-6 of a product, in one direction, which a result in bf16 does not show but one in fp32 does.
-constexpr int CHUNK = 16;
+// LONG: long sums go to the result warps in runs of about MOST_STEPS steps, which add them up in fp32 rounded to nearest.  The tensor cores truncate: over 384 instructions (6144 columns) that
+// left 7e-6 of a product, in one direction, which a result in bf16 does not show but one in fp32 does.  A tile's first run is the longest: the tile before it is read out meanwhile.
+constexpr int MOST_STEPS = 18;
+struct Runs {
+  int first, rest;
+  AS_DEV explicit Runs(int steps) {
+    const int n = (steps + MOST_STEPS - 1) / MOST_STEPS;
+    first = n == 1 ? steps : (4 * steps + 3 * n - 1) / (3 * n);
+    rest = n == 1 ? 1 : (steps - first + n - 2) / (n - 1);
+  }
+};
 template <int CG, bool A_MN, bool B_MN, bool LONG>
 AS_DEV void lin_issue(const GemmParams& p, const Ctx<CG>& c) {
   const uint32_t stage_bytes = (uint32_t)(BM + p.bn / CG) * BK * 2;
@@ -289,9 +317,10 @@ AS_DEV void lin_issue(const GemmParams& p, const Ctx<CG>& c) {
   uint32_t buf = 0, turn = 0;
   for (long long u = c.unit; u < p.units; u += c.step) {
     const Unit w = unit_of<CG>(p, u);
+    const Runs runs(w.k1 - w.k0);
     int k = w.k0;
     do {
-    const int first = k, end = LONG ? min(w.k1, k + CHUNK) : w.k1;
+    const int first = k, end = LONG ? min(w.k1, k + (k == w.k0 ? runs.first : runs.rest)) : w.k1;
     if (!c.wait(B_AEMPTY + buf, turn ^ 1u)) return;
     const uint32_t d = c.tmem + buf * 256u;
     for (; k < end; ++k) {
@@ -311,230 +340,297 @@ AS_DEV void lin_issue(const GemmParams& p, const Ctx<CG>& c) {
   }
 }
 
-// 32 rows of a strip's width to one matrix by TMA, where they are of one entry, and fewer than 32 only at its end, where the copy is cut off.
+// A box's rows in a matrix: they are of one entry, and fewer than 32 only at its end, where a copy is cut off; else there is none.
 struct Box { unsigned batch, token; bool whole; };
 AS_DEV Box box_of(const Rows& m, bool boxes, int m0, int rows) {
   if (!boxes) return {0u, 0u, false};
-  const unsigned b = m.batched ? (unsigned)m0 / m.tokens : 0u, t = (unsigned)m0 - b * m.tokens;
-  const unsigned end = t + (unsigned)max(rows, 0);
+  const unsigned b = m.batched ? (unsigned)m0 / m.tokens : 0u, t = (unsigned)m0 - b * m.tokens, end = t + (unsigned)max(rows, 0);
   return {b, t, rows == 32 ? end <= m.tokens : end == m.tokens};
 }
-// This lane's row of 32 values as bf16 into the strip, and the strip to columns n .. n + 31.
-AS_DEV void leave_box(const CUtensorMap* map, const Rows& m, const Box& box, uint32_t strip, int lane, int rows, int n, int N, const float (&x)[32]) {
-  if (lane == 0) tma_store_wait_read();       // the copy before this one has read the strip
-  __syncwarp();
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    uint32_t w[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) w[k] = pack_bf16(x[8 * i + 2 * k], x[8 * i + 2 * k + 1]);
-    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(strip + swz64(lane, i)), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
-  }
+struct At { int x, t, h, b; };
+AS_DEV At at_of(const Rows& m, const Box& box, int n, int N) {
+  const unsigned head = m.hd == N ? 0u : (unsigned)n / (unsigned)m.hd;
+  return {n - (int)head * m.hd, (int)box.token, (int)head, (int)box.batch};
+}
+// A warp's two strips, used in turn.
+struct Strips {
+  uint32_t at, bar;                           // the first one; its barrier, told when a residual has come
+  uint32_t slot, turns;                       // the one that is used next; parities of both barriers
+  AS_DEV uint32_t strip() const { return at + slot * STRIP; }
+};
+// 16 bytes of this lane's row of the strip.
+AS_DEV void put16(uint32_t strip, int lane, int i, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(strip + swz64(lane, i)), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+AS_DEV void get16(uint32_t strip, int lane, int i, uint32_t (&w)[4]) {
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(strip + swz64(lane, i)) : "memory");
+}
+// The strip, as it has been written by its warp, to columns n ... of a matrix.
+AS_DEV void send_box(const CUtensorMap* map, const Rows& m, const Box& box, Strips& s, int lane, int rows, int n, int N) {
   fence_proxy_async();
   __syncwarp();
   if (lane == 0 && rows > 0 && n < N) {
-    const unsigned head = m.hd == N ? 0u : (unsigned)n / (unsigned)m.hd;
-    store_box(map, strip, n - (int)head * m.hd, (int)box.token, (int)head, (int)box.batch);
-    tma_store_commit();
+    const At a = at_of(m, box, n, N);
+    store_box(map, s.strip(), a.x, a.t, a.h, a.b);
   }
+  if (lane == 0) tma_store_commit();          // (one group for every use of a strip, whether there is something to store or not)
+  s.slot ^= 1u;
 }
-// 16 columns of 32 rows through the strip, plus a residual, four lanes a row: `at(row, n)` is where four (or fewer) columns go.
-struct Target { Rows m; bool f32; };
-AS_DEV void leave_rows(const Target& to, const Target& res, bool vec, uint32_t strip, int lane, int m0, int rows, int n0, int N, const float* x) {
-  const int n = n0 + 4 * (lane & 3);
-  const bool adds = res.m.data != nullptr, in = n < N;
-  const long long oc = in ? to.m.col((unsigned)n) : 0, rc = in && adds ? res.m.col((unsigned)n) : 0;
-  float4 r[4];
-  if (adds && vec) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int row = i * 8 + lane / 4;
-      r[i] = in && row < rows ? ld4(res.m.data, res.f32, res.m.row((unsigned)(m0 + row)) + rc) : make_float4(0.f, 0.f, 0.f, 0.f);
-    }
-  }
-  if (lane == 0) tma_store_wait_read();       // (a box of pre may be on its way from the strip)
+// The strip that is used next has been read by the copy out of it, the last but one.
+AS_DEV void wait_strip(int lane) {
+  if (lane == 0) tma_store_wait_read_but_last();
   __syncwarp();
+}
+// This lane's row of 32 values as bf16 through a strip.
+AS_DEV void leave_bf16(const CUtensorMap* map, const Rows& m, const Box& box, Strips& s, int lane, int rows, int n, int N, const float (&x)[32]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(strip + swz64(lane, i)), "f"(x[4 * i]), "f"(x[4 * i + 1]), "f"(x[4 * i + 2]), "f"(x[4 * i + 3]) : "memory");
+    put16(s.strip(), lane, i, pack_bf16(x[8 * i], x[8 * i + 1]), pack_bf16(x[8 * i + 2], x[8 * i + 3]), pack_bf16(x[8 * i + 4], x[8 * i + 5]), pack_bf16(x[8 * i + 6], x[8 * i + 7]));
+  send_box(map, m, box, s, lane, rows, n, N);
+}
+AS_DEV void leave_f32(const CUtensorMap* map, const Rows& m, const Box& box, Strips& s, int lane, int rows, int n, int N, const float* x) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) put16(s.strip(), lane, i, __float_as_uint(x[4 * i]), __float_as_uint(x[4 * i + 1]), __float_as_uint(x[4 * i + 2]), __float_as_uint(x[4 * i + 3]));
+  send_box(map, m, box, s, lane, rows, n, N);
+}
+// The residual's box of columns n ... on its way to the strip that is used next, which is free.
+AS_DEV void fetch_box(const CUtensorMap* map, const Rows& m, const Box& box, const Strips& s, int lane, int n, int N) {
+  if (lane == 0) {
+    const uint32_t bar = s.bar + 8 * s.slot;
+    const At a = at_of(m, box, n, N);
+    mbar_expect_tx(bar, STRIP);
+    load_box4<1>(s.strip(), map, bar, a.x, a.t, a.h, a.b);
+  }
+}
+AS_DEV bool wait_box(Strips& s, const WaitCtx& wc) {
+  const bool ok = mbar_wait_warp(s.bar + 8 * s.slot, s.turns >> s.slot & 1u, wc);
+  s.turns ^= 1u << s.slot;
+  return ok;
+}
+
+// 16 columns of 32 rows through a strip, plus a residual, four lanes a row: layouts, alignments and mixtures of types that have no boxes, and sums of parts.
+struct Target { Rows m; bool f32; };
+AS_DEV void leave_rows(const Target& to, const Target& res, bool vec, uint32_t strip, int lane, int m0, int rows, int n0, int N, const float* x) {
+  const int n = n0 + 4 * (lane & 3), row = lane / 4;
+  const bool adds = res.m.data != nullptr;
+  if (lane == 0) tma_store_wait_read();
   __syncwarp();
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int row = i * 8 + lane / 4;
-    float4 v;
-    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(strip + swz64(row, lane & 3)) : "memory");
-    if (!in || row >= rows) continue;
-    const unsigned m = (unsigned)(m0 + row);
+  for (int i = 0; i < 4; ++i) put16(strip, lane, i, __float_as_uint(x[4 * i]), __float_as_uint(x[4 * i + 1]), __float_as_uint(x[4 * i + 2]), __float_as_uint(x[4 * i + 3]));
+  __syncwarp();
+  if (n < N) {
+    auto value = [&](int i) {
+      uint32_t w[4];
+      get16(strip, i * 8 + row, lane & 3, w);
+      return make_float4(__uint_as_float(w[0]), __uint_as_float(w[1]), __uint_as_float(w[2]), __uint_as_float(w[3]));
+    };
     if (vec) {
-      if (adds) { v.x += r[i].x; v.y += r[i].y; v.z += r[i].z; v.w += r[i].w; }
-      st4(to.m.data, to.f32, to.m.row(m) + oc, v);
+      const long long oc = to.m.col((unsigned)n), rc = adds ? res.m.col((unsigned)n) : 0;
+      float4 r[4];
+      if (adds) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = i * 8 + row < rows ? ld4(res.m.data, res.f32, res.m.row((unsigned)(m0 + i * 8 + row)) + rc) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float4 v = value(i);
+        if (adds) { v.x += r[i].x; v.y += r[i].y; v.z += r[i].z; v.w += r[i].w; }
+        if (i * 8 + row < rows) st4(to.m.data, to.f32, to.m.row((unsigned)(m0 + i * 8 + row)) + oc, v);
+      }
     } else {
-      const float f[4] = {v.x, v.y, v.z, v.w};
-      const long long ro = to.m.row(m), rr = adds ? res.m.row(m) : 0;
+#pragma unroll 1
+      for (int i = 0; i < 4; ++i) {
+        if (i * 8 + row >= rows) break;
+        const unsigned m = (unsigned)(m0 + i * 8 + row);
+        const float4 v = value(i);
+        const float f[4] = {v.x, v.y, v.z, v.w};
+        const long long ro = to.m.row(m), rr = adds ? res.m.row(m) : 0;
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (n + k < N) st1(to.m.data, to.f32, ro + to.m.col((unsigned)(n + k)), adds ? f[k] + ld1(res.m.data, res.f32, rr + res.m.col((unsigned)(n + k))) : f[k]);
+        for (int k = 0; k < 4; ++k)
+          if (n + k < N) st1(to.m.data, to.f32, ro + to.m.col((unsigned)(n + k)), adds ? f[k] + ld1(res.m.data, res.f32, rr + res.m.col((unsigned)(n + k))) : f[k]);
+      }
     }
   }
   __syncwarp();
 }
 
-// Biases and gates of 32 columns, a column a lane, to where the warp reads them four at a time.
-AS_DEV void keep_vectors(const Epilogue& e, uint32_t vectors, int lane, float bias, float gate) {
-  __syncwarp();
-  if (e.bias != nullptr) asm volatile("st.shared.f32 [%0], %1;" ::"r"(vectors + lane * 4), "f"(bias) : "memory");
-  if (e.gate != nullptr) asm volatile("st.shared.f32 [%0], %1;" ::"r"(vectors + 128 + lane * 4), "f"(gate) : "memory");
-  __syncwarp();
-}
-AS_DEV float4 read4(uint32_t at) {
-  float4 b;
-  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(b.x), "=f"(b.y), "=f"(b.z), "=f"(b.w) : "r"(at) : "memory");
-  return b;
-}
-template <int W>
-AS_DEV void add_bias(const Epilogue& e, uint32_t at, float (&x)[W]) {
-  if (e.bias == nullptr) return;
+// A vector's values of this strip, a column a lane: x = f(x, value).  (Exchanged between the lanes: there is no room beside the stages to read them from, and from global memory, the same
+// 16 bytes for all lanes at a time, they made a tile's results a quarter longer.)
+template <typename F>
+AS_DEV void with_vector(float mine, float (&x)[32], F f) {
 #pragma unroll
-  for (int i = 0; i < W / 4; ++i) {
-    const float4 b = read4(at + i * 16);
-    x[4 * i] += b.x; x[4 * i + 1] += b.y; x[4 * i + 2] += b.z; x[4 * i + 3] += b.w;
-  }
+  for (int i = 0; i < 32; ++i) x[i] = f(x[i], __shfl_sync(0xffffffffu, mine, i));
 }
-// Activation and gate; gates_alike: all rows have those that are kept, else this lane's row, m, has its own.
-template <int W>
-AS_DEV void activate_and_gate(const Epilogue& e, uint32_t at, bool gates_alike, int m, int n0, float (&x)[W]) {
-  with_activation(e.act, [&](auto a) {
-#pragma unroll
-    for (int i = 0; i < W; ++i) x[i] = activated<decltype(a)::value>(x[i]);
-  });
-  if (e.gate == nullptr) return;
-  if (gates_alike) {
-#pragma unroll
-    for (int i = 0; i < W / 4; ++i) {
-      const float4 g = read4(at + i * 16);
-      x[4 * i] *= g.x; x[4 * i + 1] *= g.y; x[4 * i + 2] *= g.z; x[4 * i + 3] *= g.w;
-    }
-  } else {
-    const long long row = (long long)((unsigned)m / e.gate_rows) * e.gate_stride;
-#pragma unroll
-    for (int i = 0; i < W; ++i) x[i] *= n0 + i < e.N ? ld1(e.gate, e.gate_f32, row + n0 + i) : 0.f;
-  }
-}
+AS_DEV float add_(float a, float b) { return a + b; }
+AS_DEV float mul_(float a, float b) { return a * b; }
 
-// Sums of 32 rows x 32 columns, on to out and pre.
-AS_DEV void leave_strip(const Epilogue& e, const CUtensorMap* mo, const CUtensorMap* mp, const Box& out_box, const Box& pre_box, uint32_t strip, uint32_t vectors, int lane, int m0, int rows, int n0,
-                        bool gates_alike, float (&x)[32]) {
-  add_bias(e, vectors, x);
-  if (e.pre.data != nullptr) {
-    if (pre_box.whole) leave_box(mp, e.pre, pre_box, strip, lane, rows, n0, e.N, x);
-    else
-#pragma unroll
-      for (int h = 0; h < 2; ++h) leave_rows({e.pre, false}, {}, e.vec, strip, lane, m0, rows, n0 + 16 * h, e.N, x + 16 * h);
-  }
-  activate_and_gate(e, vectors + 128, gates_alike, m0 + max(0, min(lane, rows - 1)), n0, x);
-  if (out_box.whole) leave_box(mo, e.out, out_box, strip, lane, rows, n0, e.N, x);
-  else
-#pragma unroll
-    for (int h = 0; h < 2; ++h) leave_rows({e.out, e.out_f32}, {e.res, e.res_f32}, e.vec, strip, lane, m0, rows, n0 + 16 * h, e.N, x + 16 * h);
-}
-// The same of 16 columns, results in fp32.
-AS_DEV void leave_half(const Epilogue& e, uint32_t strip, uint32_t vectors, int lane, int m0, int rows, int n0, bool gates_alike, float (&x)[16]) {
-  add_bias(e, vectors, x);
-  if (e.pre.data != nullptr) leave_rows({e.pre, false}, {}, e.vec, strip, lane, m0, rows, n0, e.N, x);
-  activate_and_gate(e, vectors + 128, gates_alike, m0 + max(0, min(lane, rows - 1)), n0, x);
-  leave_rows({e.out, true}, {e.res, e.res_f32}, e.vec, strip, lane, m0, rows, n0, e.N, x);
-}
-
-// Results of a tile: this warp's 32 rows, 32 of every 128 columns.  LONG: of a tile's sums, which come in runs of CHUNK steps.
+// Results of a tile: this warp's 32 rows, 32 of every 128 columns.  LONG: of sums that come in runs.
+struct ResultMaps { const CUtensorMap *out, *pre, *res; };
 template <int CG, bool LONG>
-AS_DEV void lin_results(const GemmParams& p, const Ctx<CG>& c, const CUtensorMap* mo, const CUtensorMap* mp, int lane, int warp) {
+AS_DEV void lin_results(const GemmParams& p, const Ctx<CG>& c, const ResultMaps& maps, int lane, int warp) {
   const Epilogue& e = p.e;
-  const int quarter = warp & 3, group = warp >> 2;
+  const int quarter = (warp + FIRST_RESULT) & 3, group = warp >> 2;         // (a warp reaches the quarter of tensor memory that its number in the CTA says)
   const uint32_t lanes = (uint32_t)quarter * 32u << 16;
-  const uint32_t strip = c.sbase + STRIPS_OFF + (uint32_t)warp * STRIP, vectors = c.sbase + VECTORS_OFF + (uint32_t)warp * 256;
+  Strips strips{c.sbase + STRIPS_OFF + (uint32_t)warp * (2 * STRIP), c.bar(B_RES + 2 * warp), 0u, 0u};
   uint32_t buf = 0, turn = 0;
   auto give_back = [&] {
     tc_fence_before();
     __syncwarp();
     if (lane == 0) arrive_leader<CG>(c.bar(B_AEMPTY + buf));
   };
+  auto next_buffer = [&] {
+    buf ^= 1u;
+    if (buf == 0) turn ^= 1u;
+  };
   for (long long u = c.unit; u < p.units; u += c.step) {
     const Unit w = unit_of<CG>(p, u);
     const int t0 = w.t0 + (int)c.rank * BM + quarter * 32, m0 = w.entry * p.T + t0, rows = min(32, p.T - t0);
-    const Box out_box = box_of(e.out, e.boxes, m0, rows), pre_box = box_of(e.pre, e.pre_boxes, m0, rows);
-    // biases and gates of this lane's column in each strip, while the products run
-    float bias[2], gate[2];
-    const long long gate_row = e.gate_rows == 0u || rows <= 0 ? 0 : (long long)((unsigned)m0 / e.gate_rows);
-    const bool gates_alike = e.gate_rows == 0u || rows <= 0 || gate_row == (long long)((unsigned)(m0 + rows - 1) / e.gate_rows);
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
+    // The residual comes a box ahead of its sums, the first one while the products run.  (From the warps' own loads, four lanes a row, 32760 x 6144 by 1536 onto fp32 took 543 us.)
+    const bool boxed = [&] { return e.res_boxes && box_of(e.out, e.boxes, m0, rows).whole && box_of(e.res, true, m0, rows).whole; }();
+    const int wide = e.out_f32 ? 16 : 32, boxes = 32 / wide;                  // columns of a box, boxes of a strip's width
+    auto fetch = [&](int n) { fetch_box(maps.res, e.res, box_of(e.res, true, m0, rows), strips, lane, n, e.N); };
+    // biases and gates, a column a lane; gates of rows that do not share them are read row by row
+    const unsigned gate_row = e.gate_rows == 0u || rows <= 0 ? 0u : (unsigned)m0 / e.gate_rows;
+    const bool gates_alike = e.gate_rows == 0u || rows <= 0 || gate_row == (unsigned)(m0 + rows - 1) / e.gate_rows;
+    auto mine = [&](const void* v, bool f32, long long at, int j) {
       const int n = w.n0 + 32 * group + 128 * j + lane;
-      bias[j] = e.bias != nullptr && n < e.N ? ld1(e.bias, e.bias_f32, n) : 0.f;
-      gate[j] = e.gate != nullptr && n < e.N ? ld1(e.gate, e.gate_f32, gate_row * e.gate_stride + n) : 0.f;
-    }
-    auto to_parts = [&](int n0, const float* x) {
-      const Target to{Rows{p.part + (long long)w.part * p.M * p.part_pitch, 0, 0, p.part_pitch, 1u, 1, 0ull, false, false}, true};
-      leave_rows(to, {}, true, strip, lane, m0, rows, n0, e.N, x);
+      return v != nullptr && n < e.N ? ld1(v, f32, at + n) : 0.f;
     };
-    if constexpr (!LONG) {
+    bool fetched = boxed && rows > 0 && 32 * group < p.bn;
+    if (fetched) {
+      wait_strip(lane);
+      fetch(w.n0 + 32 * group);
+    }
+    float bias[2], gate[2];
+    auto vectors = [&] {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        bias[j] = mine(e.bias, e.bias_f32, 0, j);
+        gate[j] = mine(e.gate, e.gate_f32, gate_row * e.gate_stride, j);
+      }
+    };
+    if constexpr (!LONG) vectors();
+    if constexpr (LONG) {
+      // the runs' sums, in registers; with the last run's they go back to where that one lies
+      const Runs runs(w.k1 - w.k0);
+      if (runs.first < w.k1 - w.k0) {
+        float x[8][8];                        // columns 32 group + 128 (i / 4) + 8 (i % 4)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+          for (int k = 0; k < 8; ++k) x[i][k] = 0.f;
+        bool ok = true;
+        for (int k = w.k0 + runs.first;; k += runs.rest) {               // where the run ends
+          ok = mbar_wait_warp(c.bar(B_AFULL + buf), turn, c.wc);
+          if (!ok) break;
+          tc_fence_after();
+          const bool last = k >= w.k1;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int c0 = 32 * group + 128 * (i / 4) + 8 * (i % 4);
+            if (c0 < p.bn) {
+              float y[8];
+              tmem_ld8(c.tmem + lanes + buf * 256u + c0, y);
+#pragma unroll
+              for (int q = 0; q < 8; ++q) x[i][q] += y[q];
+              if (last) tmem_st8(c.tmem + lanes + buf * 256u + c0, x[i]);
+            }
+          }
+          if (last) break;
+          give_back();
+          next_buffer();
+        }
+        if (!ok) break;
+        tmem_st_wait();
+      } else {
+        if (!mbar_wait_warp(c.bar(B_AFULL + buf), turn, c.wc)) break;
+        tc_fence_after();
+      }
+    } else {
       if (!mbar_wait_warp(c.bar(B_AFULL + buf), turn, c.wc)) break;
       tc_fence_after();
-      if (32 * group >= p.bn) give_back();
+    }
+    if constexpr (LONG) vectors();
+    if (32 * group >= p.bn) give_back();
+    bool ok = true;
 #pragma unroll 1
-      for (int j = 0; j < 2; ++j) {
-        const int c0 = 32 * group + 128 * j;
-        if (c0 >= p.bn) break;
-        uint32_t x[32];
-        tmem_ld32(c.tmem + lanes + buf * 256u + c0, x);
-        tmem_ld_wait(x);
-        if (c0 + 128 >= p.bn) give_back();    // this warp has read its part of the accumulator
-        float(&f)[32] = reinterpret_cast<float(&)[32]>(x);
-        const int n0 = w.n0 + c0;
-        if (p.part != nullptr) {
-          to_parts(n0, f);
-          to_parts(n0 + 16, f + 16);
+    for (int j = 0; j < 2; ++j) {
+      const int c0 = 32 * group + 128 * j, n0 = w.n0 + c0;
+      if (c0 >= p.bn) break;
+      uint32_t raw[32];
+      tmem_ld32(c.tmem + lanes + buf * 256u + c0, raw);
+      tmem_ld_wait(raw);
+      if (c0 + 128 >= p.bn) give_back();      // this warp has read its part of the accumulator
+      float(&x)[32] = reinterpret_cast<float(&)[32]>(raw);
+      if (p.part != nullptr) {
+        const Target to{Rows{p.part + (long long)w.part * p.M * p.part_pitch, 0, 0, p.part_pitch, 1u, 1, 0ull, false, false}, true};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) leave_rows(to, {}, true, strips.at, lane, m0, rows, n0 + 16 * h, e.N, x + 16 * h);
+        continue;
+      }
+      if (e.bias != nullptr) with_vector(j == 0 ? bias[0] : bias[1], x, add_);
+      if (e.pre.data != nullptr) {
+        const Box box = box_of(e.pre, e.pre_boxes, m0, rows);
+        if (box.whole) {
+          wait_strip(lane);
+          leave_bf16(maps.pre, e.pre, box, strips, lane, rows, n0, e.N, x);
         } else {
-          keep_vectors(e, vectors, lane, bias[j], gate[j]);
-          leave_strip(e, mo, mp, out_box, pre_box, strip, vectors, lane, m0, rows, n0, gates_alike, f);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) leave_rows({e.pre, false}, {}, e.vec, strips.at, lane, m0, rows, n0 + 16 * h, e.N, x + 16 * h);
         }
       }
-      buf ^= 1u;
-      if (buf == 0) turn ^= 1u;
-    } else {
-      float x[4][16];                         // columns 32 group + 128 (i / 2) + 16 (i % 2)
+      with_activation(e.act, [&](auto a) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 32; ++i) x[i] = activated<decltype(a)::value>(x[i]);
+      });
+      if (e.gate != nullptr && gates_alike) {
+        with_vector(j == 0 ? gate[0] : gate[1], x, mul_);
+      } else if (e.gate != nullptr) {
+        const long long at = (long long)((unsigned)(m0 + min(lane, rows - 1)) / e.gate_rows) * e.gate_stride;
 #pragma unroll
-        for (int k = 0; k < 16; ++k) x[i][k] = 0.f;
-      bool ok = true;
-      for (int k = w.k0; k < w.k1; k += CHUNK) {
-        ok = mbar_wait_warp(c.bar(B_AFULL + buf), turn, c.wc);
+        for (int i = 0; i < 32; ++i) x[i] *= n0 + i < e.N ? ld1(e.gate, e.gate_f32, at + n0 + i) : 0.f;
+      }
+      const Box box = box_of(e.out, e.boxes, m0, rows);
+      if (box.whole && (boxed || e.res.data == nullptr)) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          if (q >= boxes) break;
+          const int n = n0 + 16 * q;
+          if (fetched) {
+            ok = wait_box(strips, c.wc);
+            if (!ok) break;
+            uint32_t r[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              get16(strips.strip(), lane, i, r);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                if (wide == 16) {
+                  x[16 * q + 4 * i + k] += __uint_as_float(r[k]);
+                } else if (q == 0) {
+                  x[8 * i + 2 * k] += __uint_as_float(r[k] << 16);
+                  x[8 * i + 2 * k + 1] += __uint_as_float(r[k] & 0xffff0000u);
+                }
+              }
+            }
+          } else {
+            wait_strip(lane);
+          }
+          if (wide == 16) leave_f32(maps.out, e.out, box, strips, lane, rows, n, e.N, x + 16 * q);
+          else if (q == 0) leave_bf16(maps.out, e.out, box, strips, lane, rows, n, e.N, x);
+          if (fetched && (q + 1 < boxes || c0 + 128 < p.bn && j == 0)) {
+            wait_strip(lane);
+            fetch(q + 1 < boxes ? n + 16 : n0 + 128);
+          }
+        }
         if (!ok) break;
-        tc_fence_after();
+      } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int c0 = 32 * group + 128 * (i / 2) + 16 * (i % 2);
-          if (c0 >= p.bn) continue;
-          uint32_t y[16];
-          tmem_ld16(c.tmem + lanes + buf * 256u + c0, y);
-          tmem_ld16_wait(y);
-#pragma unroll
-          for (int q = 0; q < 16; ++q) x[i][q] += __uint_as_float(y[q]);
-        }
-        give_back();
-        buf ^= 1u;
-        if (buf == 0) turn ^= 1u;
-      }
-      if (!ok) break;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int c0 = 32 * group + 128 * (i / 2) + 16 * (i % 2), n0 = w.n0 + c0;
-        if (c0 >= p.bn) continue;
-        if (p.part != nullptr) { to_parts(n0, x[i]); continue; }
-        if (i % 2 == 0) keep_vectors(e, vectors, lane, bias[i / 2], gate[i / 2]);
-        leave_half(e, strip, vectors + 64 * (i % 2), lane, m0, rows, n0, gates_alike, x[i]);
+        for (int h = 0; h < 2; ++h) leave_rows({e.out, e.out_f32}, {e.res, e.res_f32}, e.vec, strips.at, lane, m0, rows, n0 + 16 * h, e.N, x + 16 * h);
       }
     }
+    if (!ok) break;
+    next_buffer();
   }
   if (lane == 0) tma_store_wait_read();       // (the writes land by the end of the kernel)
 }
@@ -542,7 +638,7 @@ AS_DEV void lin_results(const GemmParams& p, const Ctx<CG>& c, const CUtensorMap
 template <int CG, bool A_MN, bool B_MN, bool LONG>
 __global__ void __launch_bounds__(LIN_THREADS, 1)
 linear_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb, const __grid_constant__ CUtensorMap mo, const __grid_constant__ CUtensorMap mp,
-              const __grid_constant__ GemmParams p) {
+              const __grid_constant__ CUtensorMap mr, const __grid_constant__ GemmParams p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);      // the same in both CTAs of a pair
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + 8 * B_COUNT);
@@ -553,6 +649,7 @@ linear_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CU
     *abort_flag = 0u;
     for (int s = 0; s < MAX_STAGES; ++s) { mbar_init(c.bar(B_FULL + s), 1); mbar_init(c.bar(B_EMPTY + s), 1); }
     for (int s = 0; s < 2; ++s) { mbar_init(c.bar(B_AFULL + s), 1); mbar_init(c.bar(B_AEMPTY + s), RESULT_WARPS * CG); }
+    for (int s = 0; s < 2 * RESULT_WARPS; ++s) mbar_init(c.bar(B_RES + s), 1);
     fence_barrier_init();
     fence_proxy_async();
     tma_prefetch_desc(&ma); tma_prefetch_desc(&mb);
@@ -570,8 +667,8 @@ linear_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CU
   } else if (warp == 1) {
     if (c.rank == 0 && elect_one()) lin_issue<CG, A_MN, B_MN, LONG>(p, c);
     __syncwarp();
-  } else if (warp >= 4) {
-    lin_results<CG, LONG>(p, c, &mo, &mp, lane, warp - 4);
+  } else if (warp >= FIRST_RESULT) {
+    lin_results<CG, LONG>(p, c, ResultMaps{&mo, &mp, &mr}, lane, warp - FIRST_RESULT);
   }
   if (*abort_flag != 0u) {                     // a wait ran out: copies and MMAs under way get 20 us (they take two) before memory is given back
     const long long t0 = clock64();
@@ -888,7 +985,7 @@ __global__ void __launch_bounds__(256) gather_kernel(const __grid_constant__ Gat
 using as_lin::Plan;
 using as_lin::plan_of;
 
-struct Maps { CUtensorMap a, b, out, pre; };
+struct Maps { CUtensorMap a, b, out, pre, res; };
 template <int CG, bool A_MN, bool B_MN, bool LONG>
 cudaError_t launch(const Maps& m, const GemmParams& p, int units, size_t smem, cudaStream_t st) {
   cudaLaunchAttribute attr[2]{};
@@ -899,7 +996,7 @@ cudaError_t launch(const Maps& m, const GemmParams& p, int units, size_t smem, c
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(units * CG)); cfg.blockDim = dim3(LIN_THREADS); cfg.dynamicSmemBytes = smem; cfg.stream = st;
   cfg.attrs = attr; cfg.numAttrs = CG == 1 ? 1 : 2;
-  return cudaLaunchKernelEx(&cfg, linear_kernel<CG, A_MN, B_MN, LONG>, m.a, m.b, m.out, m.pre, p);
+  return cudaLaunchKernelEx(&cfg, linear_kernel<CG, A_MN, B_MN, LONG>, m.a, m.b, m.out, m.pre, m.res, p);
 }
 
 // Whether four columns of a matrix move at once.
@@ -984,8 +1081,8 @@ Plan plan_for(const Product& q, int sms) {
   return plan_of(entries, q.a_mn ? q.M : q.T, q.M, q.N, ksteps, q.b_mn, sms);
 }
 
-// out, pre: what the epilogue's matrices are.
-cudaError_t run_product(as_fp8_context_t h, const Product& q, const Epilogue& e, const as_rows_t& out, const as_rows_t& pre, void* part, cudaStream_t st) {
+// out, pre, res: what the epilogue's matrices are.
+cudaError_t run_product(as_fp8_context_t h, const Product& q, const Epilogue& e, const as_rows_t& out, const as_rows_t& pre, const as_rows_t& res, void* part, cudaStream_t st) {
   const Plan plan = plan_for(q, h->sms);
   GemmParams p{};
   p.e = e;
@@ -1004,10 +1101,12 @@ cudaError_t run_product(as_fp8_context_t h, const Product& q, const Epilogue& e,
   const size_t smem = 1024 + STAGES_OFF + (size_t)p.stages * stage;
   Maps m{};
   auto boxes = [&](const as_rows_t& x, CUtensorMap* map) {             // (a map that the driver does not take leaves it to the warps)
-    return x.data != nullptr && x.dtype == AS_DTYPE_BF16 && rows_vec(x, 16) && (x.head_dim == q.N || x.head_dim % 32 == 0) && as_tc::make_map_rows(map, x, q.M, q.N, 32);
+    const bool spread = (x.tokens == 1 || x.stride_token > 0) && (x.tokens == q.M || x.stride_batch > 0) && (x.head_dim == q.N || x.stride_head > 0);
+    return plan.parts == 1 && x.data != nullptr && spread && rows_vec16(x) && (x.head_dim == q.N || x.head_dim % 32 == 0) && as_tc::make_map_strips(map, x, q.M, q.N);
   };
-  p.e.boxes = plan.parts == 1 && e.res.data == nullptr && boxes(out, &m.out);
-  p.e.pre_boxes = plan.parts == 1 && boxes(pre, &m.pre);
+  p.e.boxes = boxes(out, &m.out);
+  p.e.pre_boxes = boxes(pre, &m.pre);
+  p.e.res_boxes = p.e.boxes && pre.data == nullptr && res.dtype == out.dtype && boxes(res, &m.res);
   const long long a_rows = q.a_mn ? q.K : q.M, a_cols = q.a_mn ? q.M : q.K, b_rows = q.b_mn ? q.K : q.N, b_cols = q.b_mn ? q.N : q.K;
   // (boxes behind the last column of a matrix without heads begin at their column, a multiple of 64, not at what is left of it behind a "head" of any width: a copy has to begin on 16 bytes)
   p.a_hd = q.a.head_dim == a_cols ? INT32_MAX : q.a.head_dim;
@@ -1018,7 +1117,7 @@ cudaError_t run_product(as_fp8_context_t h, const Product& q, const Epilogue& e,
   const int units = (int)std::min<long long>(p.units, h->sms / plan.cg);
   cudaError_t err;
   // results in fp32 of long sums (operands of the forward product alone have them)
-  const bool is_long = e.out_f32 && (p.ksteps + p.parts - 1) / p.parts > CHUNK;
+  const bool is_long = e.out_f32 && (p.ksteps + p.parts - 1) / p.parts > MOST_STEPS;
   auto run = [&](auto cg) {
     constexpr int CG = decltype(cg)::value;
     if (q.a_mn) return launch<CG, true, true, false>(m, p, units, smem, st);
@@ -1130,7 +1229,7 @@ extern "C" as_status_t as_linear(as_fp8_context_t h, const as_linear_t* a, void*
     return err == cudaSuccess ? AS_OK : failed();
   }
   l.q.a = l.x.rows; l.q.b = l.w.rows;
-  return run_product(h, l.q, e, a->out, a->pre, room, st) == cudaSuccess ? AS_OK : failed();
+  return run_product(h, l.q, e, a->out, a->pre, a->residual, room, st) == cudaSuccess ? AS_OK : failed();
 }
 
 namespace {
@@ -1253,13 +1352,13 @@ extern "C" as_status_t as_linear_backward(as_fp8_context_t h, const as_linear_ba
     b.dx.a = dz; b.dx.b = b.w.rows;
     e.out = rows_of(a->dx, a->rows, a->cols);
     e.vec = a->cols % 4 == 0 && vec4(a->dx);
-    if (run_product(h, b.dx, e, a->dx, as_rows_t{}, room, st) != cudaSuccess) return failed();
+    if (run_product(h, b.dx, e, a->dx, as_rows_t{}, as_rows_t{}, room, st) != cudaSuccess) return failed();
   }
   if (a->dw.data != nullptr) {
     b.dw.a = dz; b.dw.b = b.x.rows;
     e.out = rows_of(a->dw, a->out_cols, a->cols);
     e.vec = a->cols % 4 == 0 && vec4(a->dw);
-    if (run_product(h, b.dw, e, a->dw, as_rows_t{}, room, st) != cudaSuccess) return failed();
+    if (run_product(h, b.dw, e, a->dw, as_rows_t{}, as_rows_t{}, room, st) != cudaSuccess) return failed();
   }
   return AS_OK;
 }

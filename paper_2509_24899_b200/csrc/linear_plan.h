@@ -45,6 +45,8 @@ namespace as_tc {
 // A bf16 matrix [rows, cols] in rows or heads as a 4-D tensor: column of a head, token, head, batch entry; boxes of 64 columns x box_rows tokens with the 128-byte swizzle; what
 // lies outside reads as 0.  (Defined in tensor_init.cu.)
 bool make_map_boxes(CUtensorMap* m, const as_rows_t& x, long long rows, long long cols, int box_rows);
+// A matrix in bf16 or fp32 the same way, in boxes of 64 bytes x 32 tokens with the 64-byte swizzle.
+bool make_map_strips(CUtensorMap* m, const as_rows_t& x, long long rows, long long cols);
 
 }  // namespace as_tc
 

@@ -43,19 +43,22 @@ namespace {
 
 bool map_rows(CUtensorMap* m, const as_rows_t& x, long long rows, long long cols, int box_cols, int box_rows, CUtensorMapSwizzle swizzle) {
   if (g_encode == nullptr) return false;
+  const bool f32 = x.dtype == AS_DTYPE_F32;
+  const cuuint64_t size = f32 ? 4 : 2;
   cuuint64_t dims[4] = {(cuuint64_t)x.head_dim, (cuuint64_t)x.tokens, (cuuint64_t)(cols / x.head_dim), (cuuint64_t)(rows / x.tokens)};
-  cuuint64_t strides[3] = {(cuuint64_t)x.stride_token * 2, (cuuint64_t)x.stride_head * 2, (cuuint64_t)x.stride_batch * 2};
+  cuuint64_t strides[3] = {(cuuint64_t)x.stride_token * size, (cuuint64_t)x.stride_head * size, (cuuint64_t)x.stride_batch * size};
   for (int i = 0; i < 3; ++i)
-    if (dims[i + 1] == 1) strides[i] = (cuuint64_t)(x.head_dim * 2 + 15) / 16 * 16;         // of one entry: not used, but not 0
+    if (dims[i + 1] == 1) strides[i] = ((cuuint64_t)x.head_dim * size + 15) / 16 * 16;      // of one entry: not used, but not 0
   cuuint32_t box[4] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1u, 1u};
   cuuint32_t estr[4] = {1u, 1u, 1u, 1u};
-  return g_encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, x.data, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+  return g_encode(m, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, x.data, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 }  // namespace
 
 bool as_tc::make_map_rows(CUtensorMap* m, const as_rows_t& x, long long rows, long long cols, int box_rows) { return map_rows(m, x, rows, cols, 32, box_rows, CU_TENSOR_MAP_SWIZZLE_64B); }
+bool as_tc::make_map_strips(CUtensorMap* m, const as_rows_t& x, long long rows, long long cols) { return map_rows(m, x, rows, cols, x.dtype == AS_DTYPE_F32 ? 16 : 32, 32, CU_TENSOR_MAP_SWIZZLE_64B); }
 bool as_tc::make_map_boxes(CUtensorMap* m, const as_rows_t& x, long long rows, long long cols, int box_rows) { return map_rows(m, x, rows, cols, 64, box_rows, CU_TENSOR_MAP_SWIZZLE_128B); }
 
 namespace {
