@@ -703,8 +703,8 @@ __global__ void __launch_bounds__(256) finish_kernel(const __grid_constant__ Fin
 
 // ---------------------------------------------------------------- few rows
 // Few rows of x: w is read by all SMs, into the operands of the warps' own matrix instructions (16 rows of w, 8 of x, 16 columns), as a tile of the pair would be empty but for some rows
-// and few CTAs would walk all columns.  A CTA takes units of 16 rows of w by 8 NT of x; its warps take every sixteenth block of 64 columns each.  Which columns an instruction calls its
-// k-th does not matter as long as both operands agree: a lane holds columns 16 q .. 16 q + 15 of its rows' block.  The warps' sums meet in shared memory, in the order of the warps.
+// and few CTAs would walk all columns.  `split` warps share 16 rows of w (of 8 NT of x), every split-th block of 64 columns each, a CTA has 16 / split such tiles at once.  Which columns an instruction
+// calls its k-th does not matter as long as both operands agree: a lane holds columns 16 q .. 16 q + 15 of its rows' block.  The warps' sums meet in shared memory, in the order of the warps.
 // Bound by the bytes of w and the latency of memory: operands come by asynchronous copies into slots that a warp alone reads, blocks ahead and on into the next unit.
 constexpr int FEW_WARPS = 16, FEW_ROWS_W = 16;
 __host__ __device__ constexpr int few_ahead(int nt) { return nt == 1 ? 4 : 3; }
@@ -716,7 +716,7 @@ struct FewParams {
   Rows x;
   const bf* w;
   long long w_pitch;
-  int M, K, units, mt;                      // mt: units of 16 rows of w, one for each 8 NT rows of x
+  int M, K, units, split;                   // units: a CTA's tiles of 16 rows of w
 };
 AS_DEV void few_copy_w(uint32_t dst, const void* src, int bytes) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory"); }
 AS_DEV void few_copy_x(uint32_t dst, const void* src, int bytes) { asm volatile("cp.async.ca.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory"); }
@@ -733,13 +733,13 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 1) linear_few_kernel(const __g
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane / 4, q = lane % 4;
   const int kb = (p.K + BK - 1) / BK;
   const uint32_t mine = smem_u32(slots) + (uint32_t)warp * (AHEAD * SLOT);
+  const int part = warp & (p.split - 1), tile = warp / p.split, tiles = FEW_WARPS / p.split;
   griddep_wait();
-  int unit = blockIdx.x, block = warp, slot = 0;                      // what is asked for next, and its first rows of w and x
-  int n1 = unit / p.mt * FEW_ROWS_W, m1 = unit % p.mt * (8 * NT);
+  int unit = blockIdx.x, block = part, slot = 0;                      // what is asked for next
   auto ask = [&] {
     if (block < kb && unit < p.units) {
       const uint32_t own = mine + slot * SLOT + lane * 16;
-      const int c = block * BK + q * 16, n = n1 + g;
+      const int c = block * BK + q * 16, n = (unit * tiles + tile) * FEW_ROWS_W + g;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {                                   // 8 columns each
         const int bytes = 2 * max(0, min(8, p.K - c - 8 * i)), c1 = bytes > 0 ? c + 8 * i : 0;
@@ -748,14 +748,12 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 1) linear_few_kernel(const __g
         const long long col = p.x.col((unsigned)c1);
 #pragma unroll
         for (int t = 0; t < NT; ++t)        // (a row that is not there leaves its results, which are not written, to chance)
-          if (m1 + 8 * t + g < p.M) few_copy_x(own + (4 + 2 * t + i) * 512, static_cast<const bf*>(p.x.data) + p.x.row((unsigned)(m1 + 8 * t + g)) + col, bytes);
+          if (8 * t + g < p.M) few_copy_x(own + (4 + 2 * t + i) * 512, static_cast<const bf*>(p.x.data) + p.x.row((unsigned)(8 * t + g)) + col, bytes);
       }
       if (++slot == AHEAD) slot = 0;
-      if ((block += FEW_WARPS) >= kb) {
-        block = warp;
+      if ((block += p.split) >= kb) {
+        block = part;
         unit += gridDim.x;
-        n1 = unit / p.mt * FEW_ROWS_W;
-        m1 = unit % p.mt * (8 * NT);
       }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");              // (an empty group where there is nothing left: the waits below count groups)
@@ -765,7 +763,7 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 1) linear_few_kernel(const __g
   int take = 0, turn = 0;
   for (int u = blockIdx.x; u < p.units; u += gridDim.x, turn ^= 1) {
     float acc[NT][4] = {};
-    for (int k = warp; k < kb; k += FEW_WARPS) {
+    for (int k = part; k < kb; k += p.split) {
       ask();                                                          // (a lane fills and reads its own 16 bytes of each piece: nothing to wait for in the other lanes)
       asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD - 1) : "memory");
       const uint32_t own = mine + take * SLOT + lane * 16;
@@ -794,12 +792,11 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 1) linear_few_kernel(const __g
 #pragma unroll
       for (int j = 0; j < 4; ++j) sums[turn][warp][8 * t + 2 * q + j % 2][g + 8 * (j / 2)] = acc[t][j];
     __syncthreads();                                                  // (one for a unit: the next one's sums go to the other half)
-    if (threadIdx.x < 8 * NT * FEW_ROWS_W) {
-      const int i0 = threadIdx.x / FEW_ROWS_W, j = threadIdx.x % FEW_ROWS_W, n = u / p.mt * FEW_ROWS_W + j, m = u % p.mt * (8 * NT) + i0;
+    for (int i = threadIdx.x; i < tiles * 8 * NT * FEW_ROWS_W; i += FEW_WARPS * 32) {
+      const int ti = i / (8 * NT * FEW_ROWS_W), m = i / FEW_ROWS_W % (8 * NT), j = i % FEW_ROWS_W, n = (u * tiles + ti) * FEW_ROWS_W + j;
       if (m < p.M && n < p.e.N) {
         float f = 0.f;
-#pragma unroll
-        for (int i = 0; i < FEW_WARPS; ++i) f += sums[turn][i][i0][j];
+        for (int k = 0; k < p.split; ++k) f += sums[turn][ti * p.split + k][m][j];
         const Epilogue& e = p.e;
         if (e.bias != nullptr) f += ld1(e.bias, e.bias_f32, n);
         if (e.pre.data != nullptr) st1(e.pre.data, false, e.pre.row((unsigned)m) + e.pre.col((unsigned)n), f);
@@ -814,7 +811,7 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 1) linear_few_kernel(const __g
 
 // ---------------------------------------------------------------- dz, and sums over rows
 // dz = dy * gate * act'(pre) in bf16, the sums of dz and of dy * act(pre) over runs of rows, which do not cross from one gate's rows to another's.  A lane has 8 columns, a warp
-// every eighth row of the run, two at once; the warps' sums meet in shared memory in their order.  One pass over dy and pre: HBM bytes.  (With the activation chosen at every value, and both its
+// every eighth row of the run, the next one under way; the warps' sums meet in shared memory in their order.  One pass over dy and pre: HBM bytes.  (With the activation chosen at every value, and both its
 // sigmoids from exponentials of their own, 7800 x 6144 took 254 us.)
 struct DzParams {
   Rows dy, pre;
@@ -832,8 +829,8 @@ AS_DEV void unpack8(const uint4& w, float (&f)[8]) {
   for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(u[i] << 16); f[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
 }
 
-template <int ACT, typename Y>
-__global__ void __launch_bounds__(256) dz_kernel(const __grid_constant__ DzParams p) {
+template <int ACT, typename Y, bool OF_GATE>
+__global__ void __launch_bounds__(256, 3) dz_kernel(const __grid_constant__ DzParams p) {
   griddep_launch();
   __shared__ float room[8][DZ_COLS + 8];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -841,7 +838,7 @@ __global__ void __launch_bounds__(256) dz_kernel(const __grid_constant__ DzParam
   const int r0 = (int)((long long)p.rows_gate * run / p.runs), r1 = (int)((long long)p.rows_gate * (run + 1) / p.runs);
   const unsigned first = (unsigned)(gate * (long long)p.rows_gate);
   griddep_wait();
-  const bool keeps = p.pre.data != nullptr, gated = p.gate != nullptr, of_gate = p.part_g != nullptr;
+  const bool keeps = p.pre.data != nullptr, gated = p.gate != nullptr;
   float g[8], sb[8] = {}, sg[8] = {};
 #pragma unroll
   for (int i = 0; i < 8; ++i) g[i] = gated && n + i < p.N ? ld1(p.gate, p.gate_f32, (long long)gate * p.gate_stride + n + i) : 1.f;
@@ -852,7 +849,7 @@ __global__ void __launch_bounds__(256) dz_kernel(const __grid_constant__ DzParam
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float2 a = activated2<ACT>(z[i]);
-      if (of_gate) sg[i] = fmaf(d[i], a.x, sg[i]);
+      if constexpr (OF_GATE) sg[i] = fmaf(d[i], a.x, sg[i]);
       d[i] = d[i] * g[i] * a.y;
       sb[i] += d[i];
     }
@@ -884,20 +881,13 @@ __global__ void __launch_bounds__(256) dz_kernel(const __grid_constant__ DzParam
       unpack8(v.z, z);
       take(m, d, z);
     };
-    Row now[2], next[2];
+    Row now, next;
     int r = r0 + warp;
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      if (r + 8 * i < r1) fetch(first + (unsigned)(r + 8 * i), now[i]);
-    for (; r < r1; r += 16) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-        if (r + 16 + 8 * i < r1) fetch(first + (unsigned)(r + 16 + 8 * i), next[i]);
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-        if (r + 8 * i < r1) use(first + (unsigned)(r + 8 * i), now[i]);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) now[i] = next[i];
+    if (r < r1) fetch(first + (unsigned)r, now);
+    for (; r < r1; r += 8) {
+      if (r + 8 < r1) fetch(first + (unsigned)(r + 8), next);
+      use(first + (unsigned)r, now);
+      now = next;
     }
   } else if (n < p.N) {
     for (int r = r0 + warp; r < r1; r += 8) {
@@ -927,17 +917,20 @@ __global__ void __launch_bounds__(256) dz_kernel(const __grid_constant__ DzParam
     }
   };
   leave(sb, p.part_b);
-  leave(sg, p.part_g);
+  if constexpr (OF_GATE) leave(sg, p.part_g);
 }
 template <typename Y>
 cudaError_t launch_dz(const DzParams& p, dim3 grid, cudaStream_t st) {
-  const dim3 block(256);
+  auto run = [&](auto act) {
+    constexpr int ACT = decltype(act)::value;
+    return p.part_g != nullptr ? as_launch_dependent(dz_kernel<ACT, Y, true>, grid, dim3(256), 0, st, p) : as_launch_dependent(dz_kernel<ACT, Y, false>, grid, dim3(256), 0, st, p);
+  };
   switch (p.act) {
-    case AS_ACT_RELU: return as_launch_dependent(dz_kernel<AS_ACT_RELU, Y>, grid, block, 0, st, p);
-    case AS_ACT_SILU: return as_launch_dependent(dz_kernel<AS_ACT_SILU, Y>, grid, block, 0, st, p);
-    case AS_ACT_GELU: return as_launch_dependent(dz_kernel<AS_ACT_GELU, Y>, grid, block, 0, st, p);
-    case AS_ACT_GELU_TANH: return as_launch_dependent(dz_kernel<AS_ACT_GELU_TANH, Y>, grid, block, 0, st, p);
-    default: return as_launch_dependent(dz_kernel<AS_ACT_NONE, Y>, grid, block, 0, st, p);
+    case AS_ACT_RELU: return run(std::integral_constant<int, AS_ACT_RELU>{});
+    case AS_ACT_SILU: return run(std::integral_constant<int, AS_ACT_SILU>{});
+    case AS_ACT_GELU: return run(std::integral_constant<int, AS_ACT_GELU>{});
+    case AS_ACT_GELU_TANH: return run(std::integral_constant<int, AS_ACT_GELU_TANH>{});
+    default: return run(std::integral_constant<int, AS_ACT_NONE>{});
   }
 }
 
@@ -1163,6 +1156,19 @@ as_status_t linear_ok(as_fp8_context_t h, const as_linear_t* a) {
   return AS_OK;
 }
 
+// Warps that share a tile of w: by turns of all SMs x blocks of a warp, of which a turn's first costs about one more.
+int few_split(int N, int K, int sms) {
+  const int tiles = (N + FEW_ROWS_W - 1) / FEW_ROWS_W, kb = (K + BK - 1) / BK;
+  int best = 1;
+  long long least = -1;
+  for (int split = 1; split <= FEW_WARPS; split *= 2) {
+    const int units = (tiles + FEW_WARPS / split - 1) / (FEW_WARPS / split);
+    const long long t = (long long)((units + sms - 1) / sms) * ((kb + split - 1) / split + 1);
+    if (least < 0 || t <= least) { best = split; least = t; }
+  }
+  return best;
+}
+
 struct LinearPlan { Operand x, w; Product q; bool few; uint64_t bytes; };
 LinearPlan plan_linear(as_fp8_context_t h, const as_linear_t& a) {
   LinearPlan l{};
@@ -1222,8 +1228,8 @@ extern "C" as_status_t as_linear(as_fp8_context_t h, const as_linear_t* a, void*
     p.x = rows_of(l.x.rows, a->rows, a->cols);
     p.w = static_cast<const bf*>(l.w.rows.data); p.w_pitch = l.w.rows.stride_token;
     p.M = (int)a->rows; p.K = (int)a->cols;
-    p.mt = 1;
-    p.units = (e.N + FEW_ROWS_W - 1) / FEW_ROWS_W * p.mt;
+    p.split = few_split(e.N, p.K, h->sms);
+    p.units = ((e.N + FEW_ROWS_W - 1) / FEW_ROWS_W + FEW_WARPS / p.split - 1) / (FEW_WARPS / p.split);
     const dim3 grid((unsigned)std::min(p.units, h->sms)), block(FEW_WARPS * 32);
     const cudaError_t err = a->rows <= 8 ? as_launch_dependent(linear_few_kernel<1>, grid, block, few_smem(1), st, p) : as_launch_dependent(linear_few_kernel<2>, grid, block, few_smem(2), st, p);
     return err == cudaSuccess ? AS_OK : failed();
