@@ -704,7 +704,8 @@ __global__ void __launch_bounds__(256) finish_kernel(const __grid_constant__ Fin
 // ---------------------------------------------------------------- few rows
 // Few rows of x: w is read by all SMs, into the operands of the warps' own matrix instructions (16 rows of w, 8 of x, 16 columns), as a tile of the pair would be empty but for some rows
 // and few CTAs would walk all columns.  `split` warps share 16 rows of w (of 8 NT of x), every split-th block of 64 columns each, a CTA has 16 / split such tiles at once.  Which columns an instruction
-// calls its k-th does not matter as long as both operands agree: a lane holds columns 16 q .. 16 q + 15 of its rows' block.  The warps' sums meet in shared memory, in the order of the warps.
+// calls its k-th does not matter as long as both operands agree: a lane holds columns 8 q .. 8 q + 7 of each half of its rows' block, so that four
+// lanes copy 64 bytes in a run.  The warps' sums meet in shared memory, in the order of the warps.
 // Bound by the bytes of w and the latency of memory: operands come by asynchronous copies into slots that a warp alone reads, blocks ahead and on into the next unit.
 constexpr int FEW_WARPS = 16, FEW_ROWS_W = 16;
 __host__ __device__ constexpr int few_ahead(int nt) { return nt == 1 ? 4 : 3; }
@@ -739,10 +740,10 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 1) linear_few_kernel(const __g
   auto ask = [&] {
     if (block < kb && unit < p.units) {
       const uint32_t own = mine + slot * SLOT + lane * 16;
-      const int c = block * BK + q * 16, n = (unit * tiles + tile) * FEW_ROWS_W + g;
+      const int c = block * BK + q * 8, n = (unit * tiles + tile) * FEW_ROWS_W + g;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {                                   // 8 columns each
-        const int bytes = 2 * max(0, min(8, p.K - c - 8 * i)), c1 = bytes > 0 ? c + 8 * i : 0;
+        const int bytes = 2 * max(0, min(8, p.K - c - 32 * i)), c1 = bytes > 0 ? c + 32 * i : 0;
 #pragma unroll
         for (int h = 0; h < 2; ++h) few_copy_w(own + (2 * h + i) * 512, p.w + (long long)min(n + 8 * h, p.e.N - 1) * p.w_pitch + c1, bytes);
         const long long col = p.x.col((unsigned)c1);
