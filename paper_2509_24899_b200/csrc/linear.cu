@@ -12,8 +12,8 @@
 //
 // What bounds it is the tensor pipe and the operands' bytes into an SM, which for 256 x 256 are level: 64 bytes a clock beside 8192 operations.
 //
-// Where the tiles are too few for the SMs, the summed index is cut into parts; their sums go to the workspace in fp32 and finish_kernel adds them up in order.  Few rows of
-// x: linear_few_kernel, further down.
+// Where the tiles are too few for the SMs, a cluster of CTAs shares the summed index of a tile (SHARED), or it is cut into parts whose sums go to the workspace in fp32 and finish_kernel adds them
+// up in order.  Few rows of x: linear_few_kernel, further down.
 #include <algorithm>
 #include <type_traits>
 
@@ -635,7 +635,61 @@ AS_DEV void lin_results(const GemmParams& p, const Ctx<CG>& c, const ResultMaps&
   if (lane == 0) tma_store_wait_read();       // (the writes land by the end of the kernel)
 }
 
-template <int CG, bool A_MN, bool B_MN, bool LONG>
+// A tile whose summed index is shared by a cluster of CTAs: each leaves its sums in its shared memory, in fp32 and where the stages were, and adds up a part of the tile's 4-column pieces over all of
+// them, in the order of their ranks, and does what follows.
+constexpr int PART_PAD = 16;                  // bytes behind a row of sums, so that rows begin in other banks
+AS_DEV void part_leave(const GemmParams& p, const Ctx<1>& c, int lane, int warp) {
+  const int quarter = (warp + FIRST_RESULT) & 3, group = warp >> 2;
+  if (!mbar_wait_warp(c.bar(B_AFULL), 0, c.wc)) return;
+  tc_fence_after();
+  const uint32_t row = c.sbase + STAGES_OFF + (uint32_t)(quarter * 32 + lane) * (uint32_t)(p.bn * 4 + PART_PAD);
+  for (int c0 = 32 * group; c0 < p.bn; c0 += 128) {
+    uint32_t x[32];
+    tmem_ld32(c.tmem + ((uint32_t)quarter * 32u << 16) + c0, x);
+    tmem_ld_wait(x);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(row + c0 * 4 + i * 16), "r"(x[4 * i]), "r"(x[4 * i + 1]), "r"(x[4 * i + 2]), "r"(x[4 * i + 3]) : "memory");
+  }
+}
+// A thread keeps to its columns, whose vectors it fetches ahead of the meeting, and takes two rows at once: what this step costs is latency, of the cluster's shared memory and of what follows.
+AS_DEV void part_add(const GemmParams& p, const Ctx<1>& c, const Unit& w, const Column4& cols, int rank) {
+  const int across = p.bn / 4, rows = LIN_THREADS / across, piece = threadIdx.x % across, n = w.n0 + 4 * piece;
+  const int first = BM * rank / p.parts + threadIdx.x / across, end = min(BM * (rank + 1) / p.parts, p.T - w.t0);
+  if (threadIdx.x >= rows * across || n >= p.e.N) return;
+  const uint32_t at = c.sbase + STAGES_OFF + (uint32_t)piece * 16u, pitch = (uint32_t)(p.bn * 4 + PART_PAD);
+  for (int r = first; r < end; r += 2 * rows) {
+    float4 f[2];
+    for (int q0 = 0; q0 < p.parts; q0 += 4) {
+      float4 v[4][2];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if (q0 + q >= p.parts) continue;
+        uint32_t from;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(from) : "r"(at), "r"(q0 + q));
+#pragma unroll
+        for (int i = 0; i < 2; ++i)           // (a row behind the last one is read where it would be, in the same tile or its stages, and not used)
+          asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                       : "=f"(v[q][i].x), "=f"(v[q][i].y), "=f"(v[q][i].z), "=f"(v[q][i].w) : "r"(from + (uint32_t)min(r + i * rows, BM - 1) * pitch) : "memory");
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if (q0 + q >= p.parts) continue;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          if (q0 + q == 0) f[i] = v[0][i];
+          else { f[i].x += v[q][i].x; f[i].y += v[q][i].y; f[i].z += v[q][i].z; f[i].w += v[q][i].w; }
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (r + i * rows < end) finish4(p.e, cols, w.entry * p.T + w.t0 + r + i * rows, n, f[i]);
+  }
+}
+
+enum { PLAIN = 0, LONG_SUMS = 1, SHARED = 2 };  // SHARED: p.parts CTAs of a cluster share a tile, one tile each cluster (CG == 1)
+template <int CG, bool A_MN, bool B_MN, int MODE>
 __global__ void __launch_bounds__(LIN_THREADS, 1)
 linear_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb, const __grid_constant__ CUtensorMap mo, const __grid_constant__ CUtensorMap mp,
               const __grid_constant__ CUtensorMap mr, const __grid_constant__ GemmParams p) {
@@ -644,14 +698,16 @@ linear_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CU
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + 8 * B_COUNT);
   volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem + 8 * B_COUNT + 4);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  constexpr bool LONG = MODE == LONG_SUMS;
   Ctx<CG> c{smem_u32(smem), 0u, WaitCtx{p.status, abort_flag}, CG == 1 ? 0u : cta_rank(), blockIdx.x / CG, gridDim.x / CG};
-  if (threadIdx.x == 0) {
-    *abort_flag = 0u;
-    for (int s = 0; s < MAX_STAGES; ++s) { mbar_init(c.bar(B_FULL + s), 1); mbar_init(c.bar(B_EMPTY + s), 1); }
-    for (int s = 0; s < 2; ++s) { mbar_init(c.bar(B_AFULL + s), 1); mbar_init(c.bar(B_AEMPTY + s), RESULT_WARPS * CG); }
-    for (int s = 0; s < 2 * RESULT_WARPS; ++s) mbar_init(c.bar(B_RES + s), 1);
+  if (threadIdx.x < B_COUNT) {                 // a barrier a thread
+    const bool given_back = threadIdx.x == B_AEMPTY || threadIdx.x == B_AEMPTY + 1;
+    mbar_init(c.bar((int)threadIdx.x), given_back ? RESULT_WARPS * CG : 1);
     fence_barrier_init();
     fence_proxy_async();
+  }
+  if (threadIdx.x == LIN_THREADS - 1) {
+    *abort_flag = 0u;
     tma_prefetch_desc(&ma); tma_prefetch_desc(&mb);
   }
   if (warp == 2) { alloc_tmem<CG>(smem_u32(tmem_slot)); griddep_launch(); }
@@ -668,7 +724,14 @@ linear_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CU
     if (c.rank == 0 && elect_one()) lin_issue<CG, A_MN, B_MN, LONG>(p, c);
     __syncwarp();
   } else if (warp >= FIRST_RESULT) {
-    lin_results<CG, LONG>(p, c, ResultMaps{&mo, &mp, &mr}, lane, warp - FIRST_RESULT);
+    if constexpr (MODE == SHARED) part_leave(p, c, lane, warp - FIRST_RESULT);
+    else lin_results<CG, LONG>(p, c, ResultMaps{&mo, &mp, &mr}, lane, warp - FIRST_RESULT);
+  }
+  if constexpr (MODE == SHARED) {
+    const Unit w = unit_of<1>(p, c.unit);
+    const Column4 cols = columns_of(p.e, w.n0 + 4 * (threadIdx.x % (p.bn / 4)));
+    cluster_sync();                            // all sums of the tile stand
+    part_add(p, c, w, cols, (int)cta_rank());
   }
   if (*abort_flag != 0u) {                     // a wait ran out: copies and MMAs under way get 20 us (they take two) before memory is given back
     const long long t0 = clock64();
@@ -676,7 +739,7 @@ linear_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CU
   }
   tc_fence_before();
   __syncthreads();
-  if constexpr (CG == 2) cluster_sync();       // nothing of this CTA is reached from the other any more
+  if constexpr (CG == 2 || MODE == SHARED) cluster_sync();       // nothing of this CTA is reached from the others any more
   if (warp == 2) {
     tc_fence_after();
     free_tmem<CG>(c.tmem);
@@ -684,20 +747,25 @@ linear_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CU
 }
 
 // Sums of parts, in their order, and what follows them: four columns a thread.
-struct FinishParams { Epilogue e; const float* part; long long pitch; int M, parts; };
+struct FinishParams { Epilogue e; const float* part; long long pitch; int M, parts; unsigned pieces; };
 __global__ void __launch_bounds__(256) finish_kernel(const __grid_constant__ FinishParams p) {
   griddep_launch();
   const int across = (int)(p.pitch / 4);
   griddep_wait();
-  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < (long long)p.M * across; i += (long long)gridDim.x * 256) {
-    const int m = (int)(i / across), n = (int)(i - (long long)m * across) * 4;
+  for (unsigned i = blockIdx.x * 256u + threadIdx.x; i < (unsigned)p.pieces; i += gridDim.x * 256u) {
+    const int m = (int)(i / (unsigned)across), n = (int)(i - (unsigned)m * (unsigned)across) * 4;
     if (n >= p.e.N) continue;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int q = 0; q < p.parts; ++q) {
-      const float4 x = *reinterpret_cast<const float4*>(p.part + ((long long)q * p.M + m) * p.pitch + n);
-      v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+    const Column4 cols = columns_of(p.e, n);
+    for (int q0 = 0; q0 < p.parts; q0 += 8) {
+      float4 x[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+        x[q] = q0 + q < p.parts ? *reinterpret_cast<const float4*>(p.part + ((long long)(q0 + q) * p.M + m) * p.pitch + n) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) { v.x += x[q].x; v.y += x[q].y; v.z += x[q].z; v.w += x[q].w; }
     }
-    finish4(p.e, columns_of(p.e, n), m, n, v);
+    finish4(p.e, cols, m, n, v);
   }
 }
 
@@ -734,7 +802,7 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 1) linear_few_kernel(const __g
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane / 4, q = lane % 4;
   const int kb = (p.K + BK - 1) / BK;
   const uint32_t mine = smem_u32(slots) + (uint32_t)warp * (AHEAD * SLOT);
-  const int part = warp & (p.split - 1), tile = warp / p.split, tiles = FEW_WARPS / p.split;
+  const int part = warp & (p.split - 1), tile = warp / p.split, tiles = FEW_WARPS / p.split, m0 = blockIdx.y * (8 * NT);
   griddep_wait();
   int unit = blockIdx.x, block = part, slot = 0;                      // what is asked for next
   auto ask = [&] {
@@ -749,7 +817,7 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 1) linear_few_kernel(const __g
         const long long col = p.x.col((unsigned)c1);
 #pragma unroll
         for (int t = 0; t < NT; ++t)        // (a row that is not there leaves its results, which are not written, to chance)
-          if (8 * t + g < p.M) few_copy_x(own + (4 + 2 * t + i) * 512, static_cast<const bf*>(p.x.data) + p.x.row((unsigned)(8 * t + g)) + col, bytes);
+          if (m0 + 8 * t + g < p.M) few_copy_x(own + (4 + 2 * t + i) * 512, static_cast<const bf*>(p.x.data) + p.x.row((unsigned)(m0 + 8 * t + g)) + col, bytes);
       }
       if (++slot == AHEAD) slot = 0;
       if ((block += p.split) >= kb) {
@@ -794,10 +862,10 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 1) linear_few_kernel(const __g
       for (int j = 0; j < 4; ++j) sums[turn][warp][8 * t + 2 * q + j % 2][g + 8 * (j / 2)] = acc[t][j];
     __syncthreads();                                                  // (one for a unit: the next one's sums go to the other half)
     for (int i = threadIdx.x; i < tiles * 8 * NT * FEW_ROWS_W; i += FEW_WARPS * 32) {
-      const int ti = i / (8 * NT * FEW_ROWS_W), m = i / FEW_ROWS_W % (8 * NT), j = i % FEW_ROWS_W, n = (u * tiles + ti) * FEW_ROWS_W + j;
+      const int ti = i / (8 * NT * FEW_ROWS_W), mi = i / FEW_ROWS_W % (8 * NT), j = i % FEW_ROWS_W, m = m0 + mi, n = (u * tiles + ti) * FEW_ROWS_W + j;
       if (m < p.M && n < p.e.N) {
         float f = 0.f;
-        for (int k = 0; k < p.split; ++k) f += sums[turn][ti * p.split + k][m][j];
+        for (int k = 0; k < p.split; ++k) f += sums[turn][ti * p.split + k][mi][j];
         const Epilogue& e = p.e;
         if (e.bias != nullptr) f += ld1(e.bias, e.bias_f32, n);
         if (e.pre.data != nullptr) st1(e.pre.data, false, e.pre.row((unsigned)m) + e.pre.col((unsigned)n), f);
@@ -980,17 +1048,18 @@ using as_lin::Plan;
 using as_lin::plan_of;
 
 struct Maps { CUtensorMap a, b, out, pre, res; };
-template <int CG, bool A_MN, bool B_MN, bool LONG>
+template <int CG, bool A_MN, bool B_MN, int MODE>
 cudaError_t launch(const Maps& m, const GemmParams& p, int units, size_t smem, cudaStream_t st) {
+  const int together = MODE == SHARED ? p.parts : CG;        // (SHARED: units are CTAs)
   cudaLaunchAttribute attr[2]{};
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = CG; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  attr[1].val.clusterDim.x = together; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(units * CG)); cfg.blockDim = dim3(LIN_THREADS); cfg.dynamicSmemBytes = smem; cfg.stream = st;
-  cfg.attrs = attr; cfg.numAttrs = CG == 1 ? 1 : 2;
-  return cudaLaunchKernelEx(&cfg, linear_kernel<CG, A_MN, B_MN, LONG>, m.a, m.b, m.out, m.pre, m.res, p);
+  cfg.attrs = attr; cfg.numAttrs = together == 1 ? 1 : 2;
+  return cudaLaunchKernelEx(&cfg, linear_kernel<CG, A_MN, B_MN, MODE>, m.a, m.b, m.out, m.pre, m.res, p);
 }
 
 // Whether four columns of a matrix move at once.
@@ -1068,16 +1137,16 @@ struct Product {
   long long M, N, K;                         // K: the summed index
   long long T;                               // entries of the rows of results, or of the summed index where a_mn
 };
-uint64_t part_bytes(const Product& q, const Plan& plan) { return plan.parts == 1 ? 0 : up256((uint64_t)plan.parts * (uint64_t)q.M * (uint64_t)((q.N + 3) / 4 * 4) * 4); }
-Plan plan_for(const Product& q, int sms) {
+uint64_t part_bytes(const Product& q, const Plan& plan) { return plan.parts == 1 || plan.shared ? 0 : up256((uint64_t)plan.parts * (uint64_t)q.M * (uint64_t)((q.N + 3) / 4 * 4) * 4); }
+Plan plan_for(const Product& q, bool f32, as_fp8_context_t h) {
   const long long entries = q.a_mn ? 1 : q.M / q.T;
   const long long ksteps = q.a_mn ? (q.K / q.T) * ((q.T + BK - 1) / BK) : (q.K + BK - 1) / BK;
-  return plan_of(entries, q.a_mn ? q.M : q.T, q.M, q.N, ksteps, q.b_mn, sms);
+  return plan_of(entries, q.a_mn ? q.M : q.T, q.M, q.N, ksteps, q.b_mn, f32 ? MOST_STEPS : 1 << 30, h->sms, h->clusters);
 }
 
 // out, pre, res: what the epilogue's matrices are.
 cudaError_t run_product(as_fp8_context_t h, const Product& q, const Epilogue& e, const as_rows_t& out, const as_rows_t& pre, const as_rows_t& res, void* part, cudaStream_t st) {
-  const Plan plan = plan_for(q, h->sms);
+  const Plan plan = plan_for(q, e.out_f32, h);
   GemmParams p{};
   p.e = e;
   p.status = h->status;
@@ -1089,7 +1158,7 @@ cudaError_t run_product(as_fp8_context_t h, const Product& q, const Epilogue& e,
   p.ks_entry = (int)(q.a_mn ? (q.T + BK - 1) / BK : 1);
   p.ksteps = (int)(q.a_mn ? (q.K / q.T) * p.ks_entry : (q.K + BK - 1) / BK);
   p.units = (q.a_mn ? 1 : q.M / q.T) * p.mt_entry * (long long)p.nt * p.parts;
-  if (plan.parts > 1) { p.part = static_cast<float*>(part); p.part_pitch = (q.N + 3) / 4 * 4; }
+  if (plan.parts > 1 && !plan.shared) { p.part = static_cast<float*>(part); p.part_pitch = (q.N + 3) / 4 * 4; }
   const int stage = (BM + plan.bn / plan.cg) * BK * 2;
   p.stages = std::min((SMEM_MAX - 1024 - STAGES_OFF) / stage, MAX_STAGES);
   const size_t smem = 1024 + STAGES_OFF + (size_t)p.stages * stage;
@@ -1108,21 +1177,24 @@ cudaError_t run_product(as_fp8_context_t h, const Product& q, const Epilogue& e,
   if (!as_tc::make_map_boxes(&m.a, in_entries(q.a, a_rows, q.T), a_rows, a_cols, q.a_mn ? 64 : BM) ||
       !as_tc::make_map_boxes(&m.b, q.a_mn ? in_entries(q.b, b_rows, q.T) : q.b, b_rows, b_cols, q.b_mn ? 64 : plan.bn / plan.cg))
     return cudaErrorInvalidValue;
-  const int units = (int)std::min<long long>(p.units, h->sms / plan.cg);
+  const int units = plan.shared ? (int)p.units : (int)std::min<long long>(p.units, h->sms / plan.cg);
   cudaError_t err;
   // results in fp32 of long sums (operands of the forward product alone have them)
   const bool is_long = e.out_f32 && (p.ksteps + p.parts - 1) / p.parts > MOST_STEPS;
   auto run = [&](auto cg) {
     constexpr int CG = decltype(cg)::value;
-    if (q.a_mn) return launch<CG, true, true, false>(m, p, units, smem, st);
-    if (q.b_mn) return launch<CG, false, true, false>(m, p, units, smem, st);
-    return is_long ? launch<CG, false, false, true>(m, p, units, smem, st) : launch<CG, false, false, false>(m, p, units, smem, st);
+    if (q.a_mn) return launch<CG, true, true, PLAIN>(m, p, units, smem, st);
+    if (q.b_mn) return launch<CG, false, true, PLAIN>(m, p, units, smem, st);
+    return is_long ? launch<CG, false, false, LONG_SUMS>(m, p, units, smem, st) : launch<CG, false, false, PLAIN>(m, p, units, smem, st);
   };
+  if (plan.shared)
+    return q.a_mn ? launch<1, true, true, SHARED>(m, p, units, smem, st) : q.b_mn ? launch<1, false, true, SHARED>(m, p, units, smem, st) : launch<1, false, false, SHARED>(m, p, units, smem, st);
   err = plan.cg == 2 ? run(std::integral_constant<int, 2>{}) : run(std::integral_constant<int, 1>{});
   if (err != cudaSuccess || plan.parts == 1) return err;
   FinishParams f{};
   f.e = e; f.part = p.part; f.pitch = p.part_pitch; f.M = p.M; f.parts = p.parts;
-  const long long pieces = (q.M * (p.part_pitch / 4) + 255) / 256;
+  f.pieces = (unsigned)(q.M * (p.part_pitch / 4));          // (parts are of results that leave SMs idle: far below 2^32)
+  const long long pieces = (f.pieces + 255ll) / 256;
   return as_launch_dependent(finish_kernel, dim3((unsigned)std::min<long long>(pieces, 8ll * h->sms)), dim3(256), 0, st, f);
 }
 
@@ -1157,15 +1229,17 @@ as_status_t linear_ok(as_fp8_context_t h, const as_linear_t* a) {
   return AS_OK;
 }
 
-// Warps that share a tile of w: by turns of all SMs x blocks of a warp, of which a turn's first costs about one more.
-int few_split(int N, int K, int sms) {
-  const int tiles = (N + FEW_ROWS_W - 1) / FEW_ROWS_W, kb = (K + BK - 1) / BK;
-  int best = 1;
-  long long least = -1;
+// Warps that share a tile of w, and how long that takes: turns of all SMs x blocks of a warp, of which a turn's first costs about one more, at 0.95 us a block (up to 8 rows 0.75; 2 rows by
+// 9216 x 1536 6.3 us, 16 rows 9.0, by 1536 x 1536 3.2 and 4.3, by 6144 x 6144 14 and 24), from 1.2 us on.  Up to 16 rows always; more of them in parts of 16 where the tile kernel, whose time is its
+// plan's and 4.5 us, takes longer (64 rows by 1536 x 1536 8.3, 512 rows 10.4).
+struct Few { int split, mt; double ns; };
+Few few_of(int M, int N, int K, int sms) {
+  const int tiles = (N + FEW_ROWS_W - 1) / FEW_ROWS_W, kb = (K + BK - 1) / BK, mt = M <= 8 ? 1 : (M + 15) / 16;
+  Few best{1, mt, 1e300};
   for (int split = 1; split <= FEW_WARPS; split *= 2) {
-    const int units = (tiles + FEW_WARPS / split - 1) / (FEW_WARPS / split);
-    const long long t = (long long)((units + sms - 1) / sms) * ((kb + split - 1) / split + 1);
-    if (least < 0 || t <= least) { best = split; least = t; }
+    const long long units = (tiles + FEW_WARPS / split - 1) / (FEW_WARPS / split) * (long long)mt;
+    const double t = 1200. + (M <= 8 ? 750. : 950.) * (double)((units + sms - 1) / sms) * ((kb + split - 1) / split + 1);
+    if (t <= best.ns) best = {split, mt, t};
   }
   return best;
 }
@@ -1175,12 +1249,12 @@ LinearPlan plan_linear(as_fp8_context_t h, const as_linear_t& a) {
   LinearPlan l{};
   l.w = operand_of(a.w, a.out_cols, a.cols);
   // few rows read x where it lies: 8 columns at a time
-  l.few = a.rows <= 16;
   l.x = operand_of(a.x, a.rows, a.cols);
-  if (l.few && aligned(a.x.data, 16) && ((a.x.stride_batch | a.x.stride_head | a.x.stride_token) & 7) == 0 && (a.x.head_dim == a.cols || a.x.head_dim % 8 == 0)) l.x = Operand{a.x, false, a.x};
   l.q = Product{l.x.rows, l.w.rows, false, false, a.rows, a.out_cols, a.cols, l.x.rows.tokens};
+  l.few = a.rows <= 16 || (a.rows <= 256 && few_of((int)a.rows, (int)a.out_cols, (int)a.cols, h->sms).ns < plan_for(l.q, a.out.dtype == AS_DTYPE_F32, h).ns + 4500.);
+  if (l.few && aligned(a.x.data, 16) && ((a.x.stride_batch | a.x.stride_head | a.x.stride_token) & 7) == 0 && (a.x.head_dim == a.cols || a.x.head_dim % 8 == 0)) l.x = Operand{a.x, false, a.x};
   l.bytes = copy_bytes(l.x, a.rows) + copy_bytes(l.w, a.out_cols);
-  if (!l.few) l.bytes += part_bytes(l.q, plan_for(l.q, h->sms));
+  if (!l.few) l.bytes += part_bytes(l.q, plan_for(l.q, a.out.dtype == AS_DTYPE_F32, h));
   return l;
 }
 bool workspace_ok(const void* p, uint64_t has, uint64_t need) { return need == 0 || (p != nullptr && aligned(p, 256) && has >= need); }
@@ -1190,8 +1264,9 @@ bool workspace_ok(const void* p, uint64_t has, uint64_t need) { return need == 0
 cudaError_t as_linear_init() {
   cudaError_t e = cudaSuccess;
   auto opt = [&](auto kernel, int bytes) { if (e == cudaSuccess) e = as_tc::opt_in_smem(kernel, bytes); };
-  opt(linear_kernel<1, false, false, false>, SMEM_MAX); opt(linear_kernel<1, false, false, true>, SMEM_MAX); opt(linear_kernel<1, false, true, false>, SMEM_MAX); opt(linear_kernel<1, true, true, false>, SMEM_MAX);
-  opt(linear_kernel<2, false, false, false>, SMEM_MAX); opt(linear_kernel<2, false, false, true>, SMEM_MAX); opt(linear_kernel<2, false, true, false>, SMEM_MAX); opt(linear_kernel<2, true, true, false>, SMEM_MAX);
+  opt(linear_kernel<1, false, false, PLAIN>, SMEM_MAX); opt(linear_kernel<1, false, false, LONG_SUMS>, SMEM_MAX); opt(linear_kernel<1, false, true, PLAIN>, SMEM_MAX); opt(linear_kernel<1, true, true, PLAIN>, SMEM_MAX);
+  opt(linear_kernel<2, false, false, PLAIN>, SMEM_MAX); opt(linear_kernel<2, false, false, LONG_SUMS>, SMEM_MAX); opt(linear_kernel<2, false, true, PLAIN>, SMEM_MAX); opt(linear_kernel<2, true, true, PLAIN>, SMEM_MAX);
+  opt(linear_kernel<1, false, false, SHARED>, SMEM_MAX); opt(linear_kernel<1, false, true, SHARED>, SMEM_MAX); opt(linear_kernel<1, true, true, SHARED>, SMEM_MAX);
   opt(linear_few_kernel<1>, few_smem(1)); opt(linear_few_kernel<2>, few_smem(2));
   return e;
 }
@@ -1229,9 +1304,10 @@ extern "C" as_status_t as_linear(as_fp8_context_t h, const as_linear_t* a, void*
     p.x = rows_of(l.x.rows, a->rows, a->cols);
     p.w = static_cast<const bf*>(l.w.rows.data); p.w_pitch = l.w.rows.stride_token;
     p.M = (int)a->rows; p.K = (int)a->cols;
-    p.split = few_split(e.N, p.K, h->sms);
+    const Few few = few_of(p.M, e.N, p.K, h->sms);
+    p.split = few.split;
     p.units = ((e.N + FEW_ROWS_W - 1) / FEW_ROWS_W + FEW_WARPS / p.split - 1) / (FEW_WARPS / p.split);
-    const dim3 grid((unsigned)std::min(p.units, h->sms)), block(FEW_WARPS * 32);
+    const dim3 grid((unsigned)std::min(p.units, std::max(1, h->sms / few.mt)), (unsigned)few.mt), block(FEW_WARPS * 32);
     const cudaError_t err = a->rows <= 8 ? as_launch_dependent(linear_few_kernel<1>, grid, block, few_smem(1), st, p) : as_launch_dependent(linear_few_kernel<2>, grid, block, few_smem(2), st, p);
     return err == cudaSuccess ? AS_OK : failed();
   }
@@ -1288,12 +1364,12 @@ BackPlan plan_back(as_fp8_context_t h, const as_linear_backward_t& a) {
   uint64_t parts = 0;
   if (dx) {
     b.dx = Product{dz, b.w.rows, false, true, a.rows, a.cols, a.out_cols, dz.tokens};
-    parts = std::max(parts, part_bytes(b.dx, plan_for(b.dx, h->sms)));
+    parts = std::max(parts, part_bytes(b.dx, plan_for(b.dx, false, h)));
   }
   if (dw) {
     const long long T = std::min(dz.tokens, b.x.rows.tokens);
     b.dw = Product{dz, b.x.rows, true, true, a.out_cols, a.cols, a.rows, T};
-    parts = std::max(parts, part_bytes(b.dw, plan_for(b.dw, h->sms)));
+    parts = std::max(parts, part_bytes(b.dw, plan_for(b.dw, false, h)));
   }
   b.bytes += parts;                          // (the products run one after another)
   return b;

@@ -7,32 +7,40 @@
 #include <algorithm>
 
 #include "as_fp8.h"
+#include "fp8_context.h"
 
 constexpr int LIN_BM = 128;                  // rows of results of a CTA
 constexpr int LIN_BK = 64;                   // steps of the summed index of a stage
 
 namespace as_lin {
 
-// cg: CTAs that share a tile's rows; bn: its columns; parts: of the summed index.
-struct Plan { int cg, bn, parts; double ns; };
+// cg: CTAs that share a tile's rows; bn: its columns; parts: of the summed index, shared by a cluster of CTAs or left in the workspace.
+struct Plan { int cg, bn, parts; bool shared; double ns; };
 
-// By the time that the turns of all SMs take: turns x steps x ns a step, and what the reading out of the last turn and the meeting of a pair add.  A part more costs its sums'
-// way to the workspace and back, and a launch.
-inline Plan plan_of(long long entries, long long T, long long M, long long N, long long ksteps, bool b_mn, int sms) {
+// By the time that the turns of all SMs take: turns x steps x ns a step, and what the reading out of the last turn and the meeting of a pair add.  What a step takes is its bytes into an SM, 64 a
+// clock, and beside them, from 256 x 256 on, its MMAs.  A part more costs its sums' way to the workspace and back, and a launch; a cluster costs the meeting and the sums, and more with every CTA beyond
+// two, and holds as many tiles at once as the device has such clusters.  most_steps: that a cluster's CTA may add up by itself.
+inline Plan plan_of(long long entries, long long T, long long M, long long N, long long ksteps, bool b_mn, int most_steps, int sms, const int* clusters) {
   static const int ns[2][8] = {{230, 250, 265, 300, 345, 385, 440, 500}, {228, 230, 240, 262, 297, 320, 365, 410}};
-  Plan best{1, 64, 1, 1e300};
+  Plan best{1, 64, 1, false, 1e300};
   for (int cg = 1; cg <= 2; ++cg)
     for (int i = 0; i < 8; ++i) {
       const int bn = 32 * (i + 1);
       if (b_mn && bn % (64 * cg) != 0) continue;
       const long long tiles = entries * ((T + LIN_BM * cg - 1) / (LIN_BM * cg)) * ((N + bn - 1) / bn), units = sms / cg;
       for (int parts = 1; parts <= 16 && parts <= ksteps; ++parts) {
-        if (parts > 1 && tiles * parts > 2 * units) break;
-        const long long all = tiles * parts, whole = (all + units - 1) / units;
-        const double turns = whole == 1 ? 1. : 0.5 * ((double)all / units + whole);
-        double t = turns * (double)((ksteps + parts - 1) / parts) * ns[cg - 1][i] + 10. * bn + (cg == 2 ? 400. : 0.);
-        if (parts > 1) t += 3000. + (double)M * (double)N * 4. * (parts + 1) / 6000.;
-        if (t < best.ns) best = {cg, bn, parts, t};
+        const long long steps = (ksteps + parts - 1) / parts;
+        if (parts == 1 || tiles * parts <= 2 * units) {
+          const long long all = tiles * parts, whole = (all + units - 1) / units;
+          const double turns = whole == 1 ? 1. : 0.5 * ((double)all / units + whole);
+          double t = turns * (double)steps * ns[cg - 1][i] + 10. * bn + (cg == 2 ? 400. : 0.);
+          if (parts > 1) t += 3000. + (double)M * (double)N * 4. * (parts + 1) / 6000.;
+          if (t < best.ns) best = {cg, bn, parts, false, t};
+        }
+        if (cg == 1 && parts > 1 && parts <= MAX_PARTS && tiles <= clusters[parts] && steps <= most_steps) {
+          const double t = (double)steps * ns[0][i] + 10. * bn + 1700. + 8. * std::max(bn - 64, 0) + (parts - 2) * (100. + 4. * bn);
+          if (t < best.ns) best = {1, bn, parts, true, t};
+        }
       }
     }
   return best;
