@@ -210,12 +210,26 @@ AS_DEV float2 dot(const Pairs& v, const Pairs& w, float2 s) {
 }
 
 template <typename T> struct Raw { uint4 v[sizeof(T)]; };        // 16 elements: two pieces of 8
+// What is read once passes the first-level cache by: the weights and the table, which every row reads, stay there.
+AS_DEV uint4 load_once(const void* at) {
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(at) : "memory");
+  return v;
+}
 template <typename T>
 AS_DEV void load(Raw<T>& r, const T* at, int second) {
 #pragma unroll
   for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
-    r.v[i] = *reinterpret_cast<const uint4*>(at + i * (16 / sizeof(T)));
-    r.v[sizeof(T) / 2 + i] = *reinterpret_cast<const uint4*>(at + second + i * (16 / sizeof(T)));
+    r.v[i] = load_once(at + i * (16 / sizeof(T)));
+    r.v[sizeof(T) / 2 + i] = load_once(at + second + i * (16 / sizeof(T)));
+  }
+}
+template <typename T>
+AS_DEV void load_kept(Raw<T>& r, const T* at, int second) {
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+    r.v[i] = __ldg(reinterpret_cast<const uint4*>(at + i * (16 / sizeof(T))));
+    r.v[sizeof(T) / 2 + i] = __ldg(reinterpret_cast<const uint4*>(at + second + i * (16 / sizeof(T))));
   }
 }
 // From here on the compiler takes the words for others: what it has unpacked from them is unpacked again where it is used again, instead of kept in registers that there are not.
@@ -267,11 +281,11 @@ template <bool HALF>
 AS_DEV void load_weights(const TurnParams& p, const void* w, int at, int second, Pairs& f) {
   if (p.w_f32) {
     Raw<float> r;
-    load(r, static_cast<const float*>(w) + at, second);
+    load_kept(r, static_cast<const float*>(w) + at, second);
     values<HALF>(r, f);
   } else {
     Raw<bf> r;
-    load(r, static_cast<const bf*>(w) + at, second);
+    load_kept(r, static_cast<const bf*>(w) + at, second);
     values<HALF>(r, f);
   }
 }
