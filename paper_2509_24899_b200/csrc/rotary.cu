@@ -474,7 +474,7 @@ __global__ void __launch_bounds__(THREADS, 2) turn_kernel(const __grid_constant_
 
 // ---------------------------------------------------------------- backward
 // dx = r (g - n mean(g n)), g = d w, d = R^T dy, n = x r.  A CTA goes on from row to row of one tensor.  Each warp has its sums of d n in shared
-// memory (in registers, up to 48 of them, they left room for one CTA an SM).  Both sums of a row, over x^2 and over g x, are taken at once.
+// memory (in registers, up to 48 of them, they left room for one CTA an SM), and the rows that it works on come there by asynchronous copies.  Both sums of a row, over x^2 and over g x, are taken at once.
 template <typename T, int NORM, int NV, bool HALF>
 __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) turn_back_kernel(const __grid_constant__ TurnParams p) {
   griddep_launch();
@@ -502,29 +502,52 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) turn_back_ker
 #pragma unroll
   for (int i = 0; i < 4; ++i) w.a[i] = w.b[i] = both(1.f);
   if (!ROW && t.w != nullptr && l.in_head) load_weights<HALF>(p, t.w, l.e0, l.second, w);
-  for (long long u0 = (long long)first_cta * per; u0 < p.rows; u0 += (long long)ctas * per) {       // a turn is one for the whole CTA
-    const bool live = slot < per && u0 + slot < p.rows;
-    const Token tk = token_of(p, live ? (unsigned)(u0 + slot) : 0u);
-    Raw<T> x[NV], y[NV];
-    const T* bx = static_cast<const T*>(t.x.data) + address(t.x, tk) + l.e0;
-    const T* by = static_cast<const T*>(t.dy.data) + address(t.dy, tk) + l.e0;
-    T* out = static_cast<T*>(t.o.data) + address(t.o, tk) + l.e0;
+  // x and dy of a row, in this lane's own pieces of 16 bytes: the next row's are asked for as soon as this one's have been read for the last time
+  constexpr int PIECES = sizeof(T);
+  const uint32_t room = sm100::smem_u32(sums + WARPS * (NA * 128)) + (uint32_t)(warp * (NV * 2 * PIECES * 512) + lane * 16);
+  auto place = [&](int j, int tensor, int piece) { return room + (uint32_t)((j * 2 + tensor) * PIECES + piece) * 512u; };
+  auto ask = [&](const T* bx, const T* by, bool live, int j) {
+    const int h = h0 + j * l.heads_a_vector;
+    if (!(live && l.in_head && h < t.heads)) return;
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int h = h0 + j * l.heads_a_vector;
-      x[j] = Raw<T>{};
-      y[j] = Raw<T>{};
-      if (live && l.in_head && h < t.heads) {
-        load(x[j], bx + h * t.x.sh, l.second);
-        load(y[j], by + h * t.dy.sh, l.second);
-      }
+    for (int i = 0; i < PIECES; ++i) {
+      const int e = (i < PIECES / 2 ? 0 : l.second) + i % (PIECES / 2) * (16 / (int)sizeof(T));
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(place(j, 0, i)), "l"(bx + h * t.x.sh + e) : "memory");
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(place(j, 1, i)), "l"(by + h * t.dy.sh + e) : "memory");
     }
+  };
+  auto take_raw = [&](int j, int tensor, Raw<T>& r) {
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i)
+      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.v[i].x), "=r"(r.v[i].y), "=r"(r.v[i].z), "=r"(r.v[i].w) : "r"(place(j, tensor, i)) : "memory");
+  };
+  auto x_of = [&](const Token& k) { return static_cast<const T*>(t.x.data) + address(t.x, k) + l.e0; };
+  auto y_of = [&](const Token& k) { return static_cast<const T*>(t.dy.data) + address(t.dy, k) + l.e0; };
+  long long row = (long long)first_cta * per + slot;
+  bool live = slot < per && row < p.rows;
+  Token tk = token_of(p, live ? (unsigned)row : 0u);
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    if (!l.in_head || h0 + j * l.heads_a_vector >= t.heads)                  // heads that are not there are 0
+#pragma unroll
+      for (int i = 0; i < 2 * PIECES; ++i) asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(place(j, 0, i)), "r"(0) : "memory");
+    ask(x_of(tk), y_of(tk), live, j);
+  }
+  for (long long u0 = (long long)first_cta * per; u0 < p.rows; u0 += (long long)ctas * per) {       // a turn is one for the whole CTA
+    row += (long long)ctas * per;
+    const bool more = slot < per && row < p.rows;
+    const Token next = token_of(p, more ? (unsigned)row : 0u);
+    T* out = static_cast<T*>(t.o.data) + address(t.o, tk) + l.e0;
+    asm volatile("cp.async.wait_all;" ::: "memory");
     Factors cs;
     if (l.turned) cs = factors_of<HALF>(p, tk, l.slot);
     // x and d of vector j, and its weights
     auto operands = [&](int j, Pairs& v, Pairs& d) {
-      values<HALF>(x[j], v);
-      values<HALF>(y[j], d);
+      Raw<T> r;
+      take_raw(j, 0, r);
+      values<HALF>(r, v);
+      take_raw(j, 1, r);
+      values<HALF>(r, d);
       if (l.turned) turn(d, cs);
       if constexpr (ROW) {
         const int h = h0 + j * l.heads_a_vector;
@@ -556,8 +579,6 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) turn_back_ker
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
           Pairs v, d;
-          again(x[j]);
-          again(y[j]);
           operands(j, v, d);
           if (factor != 1.f) scale(v, both(factor));
           add(v, d, s);
@@ -568,8 +589,8 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) turn_back_ker
       const int h = h0 + j * l.heads_a_vector;
       const bool there = live && l.in_head && h < t.heads;
       Pairs v, d;
-      if constexpr (ROW) { again(x[j]); again(y[j]); }
       operands(j, v, d);
+      if (more) ask(x_of(next), y_of(next), true, j);
       if constexpr (!ROW) {
         factor = 1.f;
         settle(there, [&](float2 (&s)[2]) {
@@ -595,6 +616,8 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) turn_back_ker
       if (factor != 1.f) scale(d, both(factor));
       store<HALF>(out + h * t.o.sh, l.second, d);
     }
+    live = more;
+    tk = next;
   }
   if (!sums_wanted) return;
   // the warps' sums in their order: the CTA's row of partial sums.  Element e of a lane's 16, in the order of Pairs' words: pairs 2 i, 2 i + 1 first, then their second elements
@@ -912,7 +935,7 @@ Shape turn_params(const as_qk_norm_rotary_t& a, const as_rotation_t& r, int sms,
   p.lanes_log = 0;
   while ((16 << p.lanes_log) < a.head_dim) ++p.lanes_log;
   const int heads = std::max(p.t[0].heads, p.t[1].heads), of_vector = std::max(1, 32 >> p.lanes_log), vectors = (heads + of_vector - 1) / of_vector;
-  const int most = a.q.dtype == AS_DTYPE_BF16 ? 3 : 2;
+    const int most = a.q.dtype == AS_DTYPE_BF16 ? 3 : 2;
   p.W = 1; p.chunks = 1;
   if (a.norm == AS_NORM_ROW) {
     p.W = (vectors + most - 1) / most;
@@ -949,7 +972,7 @@ template <typename T, int NORM>
 cudaError_t launch_back(const TurnParams& p, const Shape& s, unsigned ctas, cudaStream_t st) {
   const dim3 grid(ctas, (unsigned)p.n_t), block(THREADS);
   const int heads = std::max(p.t[0].heads, p.t[1].heads);
-  const size_t smem = s.vec ? NORM == AS_NORM_ROW ? (size_t)WARPS * s.NV * 2048 : (size_t)WARPS * 2048 : (size_t)(NORM == AS_NORM_ROW ? heads : WARPS) * p.d * 4;
+  const size_t smem = s.vec ? NORM == AS_NORM_ROW ? (size_t)WARPS * s.NV * (2048 + 1024 * sizeof(T)) : (size_t)WARPS * (2048 + s.NV * 1024 * sizeof(T)) : (size_t)(NORM == AS_NORM_ROW ? heads : WARPS) * p.d * 4;
   auto run = [&](auto kernel) {
     if (smem > 40 * 1024)                                // (beside what the kernels have of a fixed size, 48 KB are there without asking)
       if (const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); e != cudaSuccess) return e;
