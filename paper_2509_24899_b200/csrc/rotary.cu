@@ -102,6 +102,7 @@ struct TurnParams {
   int lanes_log;                             // lanes of a head: 2^lanes_log
   int W;                                     // warps of a row
   int chunks;                                // runs of heads that a warp takes at once, where the norm is not over rows
+  int kept;                                  // rows' weights are kept in shared memory: bytes of the first tensor's (0: they are not)
 };
 AS_DEV unsigned quotient(unsigned i, unsigned long long by) { return by == 0ull ? i : (unsigned)__umul64hi(by, i); }
 struct Token { unsigned b, t; };
@@ -146,31 +147,24 @@ AS_DEV float2 factor_of(const TurnParams& p, const Where& w, int pair) {
   f.y *= p.sign;
   return f;
 }
-// Of 4 pairs from a multiple of 4 on, which belong to one axis or to two neighbours (or, rarely, to more).
-AS_DEV void factors(const TurnParams& p, const Where& w, int pair, float2* f) {
-  const int a = axis_of(p, pair), b = axis_of(p, pair + 3);
-  if (b - a > 1) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) f[i] = factor_of(p, w, pair + i);
-    return;
+// A token's cos and sin in its warp's shared memory, two pairs (16 bytes) a lane, asked for a row ahead: read by every lane from the table they were 100 instructions and two waits a row.
+// Chunks of two pairs lie so that the lanes of a head, which read one of every two or four, meet no bank twice.
+AS_DEV uint32_t chunk_at(uint32_t room, int c) { return room + (uint32_t)((c ^ (c >> 3 & 7)) << 4); }
+AS_DEV void ask_factors(const TurnParams& p, const Where& w, uint32_t room, int lane) {
+  for (int pair = 2 * lane; pair < p.pairs; pair += 64) {
+    const int a = pick(w, axis_of(p, pair)), b = pick(w, axis_of(p, pair + 1));
+    const uint32_t to = chunk_at(room, pair / 2);
+    if (a == b && a >= 0) {
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(to), "l"(p.table + (long long)a * p.pairs + pair) : "memory");
+    } else {
+      auto one = [&](uint32_t at, int row, int i) {
+        if (row >= 0) asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(at), "l"(p.table + (long long)row * p.pairs + i) : "memory");
+        else asm volatile("st.shared.v2.u32 [%0], {%1, %1};" ::"r"(at), "r"(0x7fc00000u) : "memory");
+      };
+      one(to, a, pair);
+      one(to + 8, b, pair + 1);
+    }
   }
-  auto row = [&](int r, float2* to) {
-    const float4* at = reinterpret_cast<const float4*>(p.table + (long long)max(r, 0) * p.pairs + pair);
-    const float4 x = __ldg(at), y = __ldg(at + 1);
-    to[0] = make_float2(x.x, x.y); to[1] = make_float2(x.z, x.w); to[2] = make_float2(y.x, y.y); to[3] = make_float2(y.z, y.w);
-    if (p.pos != nullptr && r < 0) to[0] = to[1] = to[2] = to[3] = make_float2(__uint_as_float(0x7fc00000u), __uint_as_float(0x7fc00000u));
-  };
-  row(pick(w, a), f);
-  if (b != a) {
-    float2 g[4];
-    row(pick(w, b), g);
-    const int end = a == 0 ? p.end[0] : a == 1 ? p.end[1] : p.end[2];
-#pragma unroll
-    for (int i = 1; i < 4; ++i)
-      if (pair + i >= end) f[i] = g[i];
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) f[i].y *= p.sign;
 }
 
 // ---------------------------------------------------------------- vectors of a lane
@@ -210,20 +204,6 @@ AS_DEV float2 dot(const Pairs& v, const Pairs& w, float2 s) {
 }
 
 template <typename T> struct Raw { uint4 v[sizeof(T)]; };        // 16 elements: two pieces of 8
-// What is read once passes the first-level cache by: the weights and the table, which every row reads, stay there.
-AS_DEV uint4 load_once(const void* at) {
-  uint4 v;
-  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(at) : "memory");
-  return v;
-}
-template <typename T>
-AS_DEV void load(Raw<T>& r, const T* at, int second) {
-#pragma unroll
-  for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
-    r.v[i] = load_once(at + i * (16 / sizeof(T)));
-    r.v[sizeof(T) / 2 + i] = load_once(at + second + i * (16 / sizeof(T)));
-  }
-}
 template <typename T>
 AS_DEV void load_kept(Raw<T>& r, const T* at, int second) {
 #pragma unroll
@@ -231,12 +211,6 @@ AS_DEV void load_kept(Raw<T>& r, const T* at, int second) {
     r.v[i] = __ldg(reinterpret_cast<const uint4*>(at + i * (16 / sizeof(T))));
     r.v[sizeof(T) / 2 + i] = __ldg(reinterpret_cast<const uint4*>(at + second + i * (16 / sizeof(T))));
   }
-}
-// From here on the compiler takes the words for others: what it has unpacked from them is unpacked again where it is used again, instead of kept in registers that there are not.
-template <typename T>
-AS_DEV void again(Raw<T>& r) {
-#pragma unroll
-  for (int i = 0; i < (int)sizeof(T); ++i) asm volatile("" : "+r"(r.v[i].x), "+r"(r.v[i].y), "+r"(r.v[i].z), "+r"(r.v[i].w));
 }
 // HALF: the pieces are the first and the second elements of 8 pairs; else each is 4 pairs.  (What is not turned may be called either.)
 template <bool HALF, typename T>
@@ -277,31 +251,49 @@ AS_DEV void store(T* at, int second, const Pairs& f) {
     *reinterpret_cast<uint4*>(at + second + i * (16 / sizeof(T))) = v[sizeof(T) / 2 + i];
   }
 }
-template <bool HALF>
-AS_DEV void load_weights(const TurnParams& p, const void* w, int at, int second, Pairs& f) {
-  if (p.w_f32) {
-    Raw<float> r;
-    load_kept(r, static_cast<const float*>(w) + at, second);
-    values<HALF>(r, f);
+// KEPT: from shared memory, where `w` is an address of it.
+template <bool HALF, bool KEPT, typename W>
+AS_DEV void load_weights(const W* w, uint32_t kept, int at, int second, Pairs& f) {
+  Raw<W> r;
+  if constexpr (KEPT) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(W); ++i) {
+      const int e = at + (i < (int)sizeof(W) / 2 ? 0 : second) + i % ((int)sizeof(W) / 2) * (16 / (int)sizeof(W));
+      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.v[i].x), "=r"(r.v[i].y), "=r"(r.v[i].z), "=r"(r.v[i].w) : "r"(kept + (uint32_t)e * (uint32_t)sizeof(W)) : "memory");
+    }
   } else {
-    Raw<bf> r;
-    load_kept(r, static_cast<const bf*>(w) + at, second);
-    values<HALF>(r, f);
+    load_kept(r, w + at, second);
   }
+  values<HALF>(r, f);
+}
+template <bool HALF, bool KEPT>
+AS_DEV void load_weights(const TurnParams& p, const void* w, uint32_t kept, int at, int second, Pairs& f) {
+  if (p.w_f32) load_weights<HALF, KEPT>(static_cast<const float*>(w), kept, at, second, f);
+  else load_weights<HALF, KEPT>(static_cast<const bf*>(w), kept, at, second, f);
+}
+// A row's weights to shared memory, by the whole CTA, which meets behind it.
+AS_DEV void keep_weights(const TurnParams& p, const TurnTensor& t, uint8_t* to) {
+  if (t.w == nullptr) return;
+  const int n = t.heads * p.d * (p.w_f32 ? 4 : 2) / 16;
+  for (int i = threadIdx.x; i < n; i += THREADS) reinterpret_cast<uint4*>(to)[i] = __ldg(static_cast<const uint4*>(t.w) + i);
 }
 // cos and sin of a lane's 8 pairs.
 struct Factors { float2 c[4], s[4]; };
 template <bool HALF>
-AS_DEV Factors factors_of(const TurnParams& p, const Token& k, int slot) {
-  float2 f[8];
-  const Where w = where_of(p, k);
-  factors(p, w, HALF ? slot * 8 : slot * 4, f);
-  factors(p, w, HALF ? slot * 8 + 4 : p.pairs / 2 + slot * 4, f + 4);
+AS_DEV Factors factors_of(const TurnParams& p, uint32_t room, int slot) {
   Factors t;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) { t.c[i] = make_float2(f[2 * i].x, f[2 * i + 1].x); t.s[i] = make_float2(f[2 * i].y, f[2 * i + 1].y); }
+  for (int i = 0; i < 4; ++i) {
+    const int c = HALF ? slot * 4 + i : i < 2 ? slot * 2 + i : p.pairs / 4 + slot * 2 + i - 2;
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(chunk_at(room, c)) : "memory");
+    t.c[i] = make_float2(v.x, v.z);
+    t.s[i] = mul2(make_float2(v.y, v.w), both(p.sign));
+  }
   return t;
 }
+// Behind the copies that this thread has asked for, and, where the factors are among them, those of its warp.
+AS_DEV void wait_copies() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 AS_DEV void turn(Pairs& v, const Factors& f) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -367,72 +359,99 @@ template <typename T, int NORM, int NV, bool HALF>
 __global__ void __launch_bounds__(THREADS, 2) turn_kernel(const __grid_constant__ TurnParams p) {
   griddep_launch();
   __shared__ float part[1][WARPS];
+  extern __shared__ uint4 dynamic[];                     // factors of each warp's row; weights of both tensors
   constexpr bool ROW = NORM == AS_NORM_ROW;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int per = ROW ? WARPS / p.W : WARPS, slot = ROW ? warp / p.W : warp, piece = ROW ? warp - slot * p.W : (int)blockIdx.y;
   const Lane l = lane_of(p, lane);
   const int h0 = piece * NV * l.heads_a_vector + l.head;
-  constexpr int AHEAD = sizeof(T) == 2 ? 2 : 1;          // tensors whose loads are under way at once
-  Raw<T> raw[AHEAD][NV];
-#pragma unroll
-  for (int i = 0; i < AHEAD; ++i)
-#pragma unroll
-    for (int j = 0; j < NV; ++j) raw[i][j] = Raw<T>{};
-  // vector j of row r, where there is one
-  auto fetch = [&](const TurnTensor& t, Raw<T>& x, const T* base, bool live, int j) {
-    const int h = h0 + j * l.heads_a_vector;
-    if (live && l.in_head && h < t.heads) load(x, base + h * t.x.sh, l.second);
-    else if (AHEAD == 1) x = Raw<T>{};                   // (registers that held the other tensor, which may have more heads)
-  };
-  auto base_of = [&](const TurnTensor& t, const Token& k) { return static_cast<const T*>(t.x.data) + address(t.x, k) + l.e0; };
   long long row = (long long)blockIdx.x * per + slot;
   bool live = slot < per && row < p.rows;
   Token k = token_of(p, live ? (unsigned)row : 0u);
+  // rows of both tensors, in this lane's own pieces of 16 bytes: the next row's are asked for as soon as this one's have been read for the last time
+  constexpr int PIECES = sizeof(T);
+  const uint32_t rows_at = sm100::smem_u32(dynamic) + (uint32_t)(warp * (NV * 2 * PIECES * 512) + lane * 16);
+  const uint32_t room = sm100::smem_u32(dynamic) + (uint32_t)(WARPS * (NV * 2 * PIECES * 512) + warp * p.pairs * 8);
+  uint8_t* kept = reinterpret_cast<uint8_t*>(dynamic) + WARPS * (NV * 2 * PIECES * 512 + p.pairs * 8);
+  auto place = [&](int i, int j, int piece) { return rows_at + (uint32_t)((i * NV + j) * PIECES + piece) * 512u; };
+  auto ask = [&](const TurnTensor& t, int i, int j, const T* base) {
+    const int h = h0 + j * l.heads_a_vector;
+    if (!l.in_head || h >= t.heads) return;
+#pragma unroll
+    for (int q = 0; q < PIECES; ++q) {
+      const int e = (q < PIECES / 2 ? 0 : l.second) + q % (PIECES / 2) * (16 / (int)sizeof(T));
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(place(i, j, q)), "l"(base + h * t.x.sh + e) : "memory");
+    }
+  };
+  auto take = [&](int i, int j, Pairs& v) {
+    Raw<T> r;
+#pragma unroll
+    for (int q = 0; q < PIECES; ++q)
+      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.v[q].x), "=r"(r.v[q].y), "=r"(r.v[q].z), "=r"(r.v[q].w) : "r"(place(i, j, q)) : "memory");
+    values<HALF>(r, v);
+  };
+  auto base_of = [&](const TurnTensor& t, const Token& k) { return static_cast<const T*>(t.x.data) + address(t.x, k) + l.e0; };
   griddep_wait();
+  if (p.table != nullptr && live) ask_factors(p, where_of(p, k), room, lane);
 #pragma unroll
-  for (int i = 0; i < AHEAD; ++i)
+  for (int i = 0; i < 2; ++i)
     if (i < p.n_t) {
-      const T* base = base_of(p.t[i], k);
+      const TurnTensor& t = p.t[i];
 #pragma unroll
-      for (int j = 0; j < NV; ++j) fetch(p.t[i], raw[i][j], base, live, j);
+      for (int j = 0; j < NV; ++j) {
+        if (!l.in_head || h0 + j * l.heads_a_vector >= t.heads)              // heads that are not there are 0
+#pragma unroll
+          for (int q = 0; q < PIECES; ++q) asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(place(i, j, q)), "r"(0) : "memory");
+        if (live) ask(t, i, j, base_of(t, k));
+      }
+    }
+  if constexpr (ROW)
+    if (p.kept > 0) {
+      keep_weights(p, p.t[0], kept);
+      if (p.n_t == 2) keep_weights(p, p.t[1], kept + p.kept);
+      __syncthreads();
     }
   for (long long first = (long long)blockIdx.x * per; first < p.rows; first += (long long)gridDim.x * per) {        // a turn is one for the whole CTA
   row += (long long)gridDim.x * per;
   const bool more = slot < per && row < p.rows;
   const Token next = token_of(p, more ? (unsigned)row : 0u);
   Factors cs;
-  if (l.turned) cs = factors_of<HALF>(p, k, l.slot);
+  wait_copies();
+  if (p.table != nullptr) {
+    __syncwarp();
+    if (l.turned) cs = factors_of<HALF>(p, room, l.slot);
+    __syncwarp();
+    if (more) ask_factors(p, where_of(p, next), room, lane);
+  }
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     if (i >= p.n_t) break;
     const TurnTensor& t = p.t[i];
-    Raw<T> (&x)[NV] = raw[AHEAD == 2 ? i : 0];
-    const T* ahead = base_of(AHEAD == 2 ? t : p.t[p.n_t == 2 ? 1 - i : 0], AHEAD == 2 || i == p.n_t - 1 ? next : k);      // what comes into these registers next
-    const bool wanted = AHEAD == 2 || i == p.n_t - 1 ? more : live;
+    const T* ahead = base_of(t, next);
     T* out = static_cast<T*>(t.o.data) + address(t.o, k) + l.e0;
     Pairs w;
     if constexpr (NORM == AS_NORM_HEAD)
-      if (t.w != nullptr && l.in_head) load_weights<HALF>(p, t.w, l.e0, l.second, w);
+      if (t.w != nullptr && l.in_head) load_weights<HALF, false>(p, t.w, 0u, l.e0, l.second, w);
+    const uint32_t kept_at = sm100::smem_u32(kept) + (i == 0 ? 0u : (uint32_t)p.kept);
     float factor = 1.f, sum[1];                          // (the sum, and then the scale)
     auto settle = [&](bool there, auto squares) {
-      auto take = [&] {
+      auto sum_up = [&] {
         const float2 s = squares();
         sum[0] = s.x + s.y;
         sums_of<NORM>(p, sum, part, slot, warp, lane);
       };
-      take();
+      sum_up();
       factor = factor_for(sum[0], p.over_n[i], p.eps, there);
-      if (any_of<NORM>(p, factor != 1.f)) take();
+      if (any_of<NORM>(p, factor != 1.f)) sum_up();
       sum[0] = rsqrtf(fmaf(sum[0], p.over_n[i], p.eps * factor * factor));
     };
+    Pairs v;
     if constexpr (ROW) {
       settle(live, [&] {
         float2 s = both(0.f);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-          Pairs v;
-          again(x[j]);
-          values<HALF>(x[j], v);
+          take(i, j, v);
           if (factor != 1.f) scale(v, both(factor));
           s = dot(v, v, s);
         }
@@ -440,13 +459,11 @@ __global__ void __launch_bounds__(THREADS, 2) turn_kernel(const __grid_constant_
       });
     }
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int h = h0 + j * l.heads_a_vector;
+    for (int jj = 0; jj < NV; ++jj) {
+      const int j = ROW ? NV - 1 - jj : jj, h = h0 + j * l.heads_a_vector;             // (over rows: the last one is still at hand, times its factor)
       const bool there = live && l.in_head && h < t.heads;
-      Pairs v;
-      if constexpr (ROW) again(x[j]);
-      values<HALF>(x[j], v);
-      fetch(AHEAD == 2 ? t : p.t[p.n_t == 2 ? 1 - i : 0], x[j], ahead, wanted, j);
+      if (!ROW || jj > 0) take(i, j, v);
+      if (more) ask(t, i, j, ahead);
       if constexpr (NORM == AS_NORM_HEAD) {
         factor = 1.f;
         settle(there, [&] {
@@ -456,10 +473,13 @@ __global__ void __launch_bounds__(THREADS, 2) turn_kernel(const __grid_constant_
       }
       if (!there) continue;
       if constexpr (NORM != AS_NORM_NONE) {
-        if (ROW && factor != 1.f) scale(v, both(factor));
+        if (ROW && jj > 0 && factor != 1.f) scale(v, both(factor));
         scale(v, both(sum[0]));
         if (t.w != nullptr) {
-          if constexpr (ROW) load_weights<HALF>(p, t.w, h * p.d + l.e0, l.second, w);
+          if constexpr (ROW) {
+            if (p.kept > 0) load_weights<HALF, true>(p, t.w, kept_at, h * p.d + l.e0, l.second, w);
+            else load_weights<HALF, false>(p, t.w, 0u, h * p.d + l.e0, l.second, w);
+          }
           scale(v, w);
         }
       }
@@ -501,10 +521,18 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) turn_back_ker
   Pairs w;
 #pragma unroll
   for (int i = 0; i < 4; ++i) w.a[i] = w.b[i] = both(1.f);
-  if (!ROW && t.w != nullptr && l.in_head) load_weights<HALF>(p, t.w, l.e0, l.second, w);
+  if (!ROW && t.w != nullptr && l.in_head) load_weights<HALF, false>(p, t.w, 0u, l.e0, l.second, w);
   // x and dy of a row, in this lane's own pieces of 16 bytes: the next row's are asked for as soon as this one's have been read for the last time
   constexpr int PIECES = sizeof(T);
-  const uint32_t room = sm100::smem_u32(sums + WARPS * (NA * 128)) + (uint32_t)(warp * (NV * 2 * PIECES * 512) + lane * 16);
+  float4* behind = sums + WARPS * (NA * 128);
+  const uint32_t room = sm100::smem_u32(behind) + (uint32_t)(warp * (NV * 2 * PIECES * 512) + lane * 16);
+  behind += WARPS * (NV * 2 * PIECES * 32);
+  const uint32_t factors = sm100::smem_u32(behind) + (uint32_t)(warp * p.pairs * 8), kept = sm100::smem_u32(behind) + (uint32_t)(WARPS * p.pairs * 8);
+  if constexpr (ROW)
+    if (p.kept > 0) {
+      keep_weights(p, t, reinterpret_cast<uint8_t*>(behind) + WARPS * p.pairs * 8);
+      __syncthreads();
+    }
   auto place = [&](int j, int tensor, int piece) { return room + (uint32_t)((j * 2 + tensor) * PIECES + piece) * 512u; };
   auto ask = [&](const T* bx, const T* by, bool live, int j) {
     const int h = h0 + j * l.heads_a_vector;
@@ -526,6 +554,7 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) turn_back_ker
   long long row = (long long)first_cta * per + slot;
   bool live = slot < per && row < p.rows;
   Token tk = token_of(p, live ? (unsigned)row : 0u);
+  if (p.table != nullptr && live) ask_factors(p, where_of(p, tk), factors, lane);
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     if (!l.in_head || h0 + j * l.heads_a_vector >= t.heads)                  // heads that are not there are 0
@@ -538,9 +567,14 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) turn_back_ker
     const bool more = slot < per && row < p.rows;
     const Token next = token_of(p, more ? (unsigned)row : 0u);
     T* out = static_cast<T*>(t.o.data) + address(t.o, tk) + l.e0;
-    asm volatile("cp.async.wait_all;" ::: "memory");
+    wait_copies();
     Factors cs;
-    if (l.turned) cs = factors_of<HALF>(p, tk, l.slot);
+    if (p.table != nullptr) {
+      __syncwarp();
+      if (l.turned) cs = factors_of<HALF>(p, factors, l.slot);
+      __syncwarp();
+      if (more) ask_factors(p, where_of(p, next), factors, lane);
+    }
     // x and d of vector j, and its weights
     auto operands = [&](int j, Pairs& v, Pairs& d) {
       Raw<T> r;
@@ -551,7 +585,10 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) turn_back_ker
       if (l.turned) turn(d, cs);
       if constexpr (ROW) {
         const int h = h0 + j * l.heads_a_vector;
-        if (t.w != nullptr && live && l.in_head && h < t.heads) load_weights<HALF>(p, t.w, h * p.d + l.e0, l.second, w);
+        if (t.w != nullptr && live && l.in_head && h < t.heads) {
+          if (p.kept > 0) load_weights<HALF, true>(p, t.w, kept, h * p.d + l.e0, l.second, w);
+          else load_weights<HALF, false>(p, t.w, 0u, h * p.d + l.e0, l.second, w);
+        }
       }
     };
     float factor = 1.f, sum[2];                          // of (f x)^2 and of g f x; then the scale, and the mean of g n
@@ -574,22 +611,21 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) turn_back_ker
       scale(d, w);
       s[1] = dot(d, v, s[1]);
     };
+    Pairs v, d;
     if constexpr (ROW)
       settle(live, [&](float2 (&s)[2]) {
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-          Pairs v, d;
           operands(j, v, d);
           if (factor != 1.f) scale(v, both(factor));
           add(v, d, s);
         }
       });
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int h = h0 + j * l.heads_a_vector;
+    for (int jj = 0; jj < NV; ++jj) {
+      const int j = ROW ? NV - 1 - jj : jj, h = h0 + j * l.heads_a_vector;             // (over rows: the last one is still at hand, times its factor)
       const bool there = live && l.in_head && h < t.heads;
-      Pairs v, d;
-      operands(j, v, d);
+      if (!ROW || jj > 0) operands(j, v, d);
       if (more) ask(x_of(next), y_of(next), true, j);
       if constexpr (!ROW) {
         factor = 1.f;
@@ -599,7 +635,7 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) turn_back_ker
         });
       }
       if (!there) continue;
-      if (ROW && factor != 1.f) scale(v, both(factor));
+      if (ROW && jj > 0 && factor != 1.f) scale(v, both(factor));
       scale(v, both(sum[0]));
       if (sums_wanted) {
 #pragma unroll
@@ -896,7 +932,7 @@ as_status_t turn_ok(const as_qk_norm_rotary_t* a, bool back) {
 // Whether pieces of 8 elements move 16 bytes at a time.
 bool heads_vec(const as_rows_t& x) { return aligned(x.data, 16) && ((x.stride_batch | x.stride_head | x.stride_token) & (x.dtype == AS_DTYPE_BF16 ? 7 : 3)) == 0; }
 
-struct Shape { bool vec; int NV, chunks; long long ctas; };
+struct Shape { bool vec; int NV, chunks; long long ctas; size_t kept; };       // kept: bytes of both tensors' weights
 // Fills in what the kernels share; `most`: vectors that a lane's registers hold.
 Shape turn_params(const as_qk_norm_rotary_t& a, const as_rotation_t& r, int sms, bool back, const as_rows_t* more, int n_more, TurnParams& p) {
   const bool two = a.k.data != nullptr;
@@ -942,6 +978,11 @@ Shape turn_params(const as_qk_norm_rotary_t& a, const as_rotation_t& r, int sms,
     if (p.W > WARPS) s.vec = false;
     else s.NV = (vectors + p.W - 1) / p.W;
     s.ctas = s.vec ? (a.rows + WARPS / p.W - 1) / (WARPS / p.W) : a.rows * (back ? 1 : p.n_t);
+    // weights in shared memory, as far as two CTAs an SM have the room
+    const size_t size = p.w_f32 ? 4 : 2, of_q = (size_t)p.t[0].heads * a.head_dim * size, of_k = (size_t)p.t[1].heads * a.head_dim * size;
+    s.kept = back ? std::max(of_q, of_k) : of_q + of_k;
+    if (s.vec && s.kept <= 12 * 1024) p.kept = (int)of_q;
+    else s.kept = 0;
   } else {
     // few rows: a vector a warp, so that all of them are under way at once
     s.NV = a.rows * ((vectors + most - 1) / most) <= 4ll * sms ? 1 : std::min(vectors, most);
@@ -956,7 +997,13 @@ template <typename T, int NORM>
 cudaError_t launch_turn(const TurnParams& p, const Shape& s, int sms, cudaStream_t st) {
   if (!s.vec) return as_launch_dependent(turn_elements_kernel<T, NORM, false>, dim3((unsigned)std::min<long long>(s.ctas, 8ll * sms)), dim3(THREADS), 0, st, p);
   const dim3 grid((unsigned)std::min<long long>(s.ctas, std::max(1, 2 * sms / p.chunks)), (unsigned)p.chunks), block(THREADS);        // CTAs go on from row to row
-  auto run = [&](auto interleaved, auto half) { return p.half ? as_launch_dependent(half, grid, block, 0, st, p) : as_launch_dependent(interleaved, grid, block, 0, st, p); };
+  const size_t smem = WARPS * (s.NV * 1024 * sizeof(T) + (size_t)p.pairs * 8) + s.kept;
+  auto launch = [&](auto kernel) {
+    if (smem > 40 * 1024)                                // (48 KB are there without asking)
+      if (const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); e != cudaSuccess) return e;
+    return as_launch_dependent(kernel, grid, block, smem, st, p);
+  };
+  auto run = [&](auto interleaved, auto half) { return p.half ? launch(half) : launch(interleaved); };
   switch (s.NV) {
     case 1: return run(turn_kernel<T, NORM, 1, false>, turn_kernel<T, NORM, 1, true>);
     case 2: return run(turn_kernel<T, NORM, 2, false>, turn_kernel<T, NORM, 2, true>);
@@ -972,7 +1019,8 @@ template <typename T, int NORM>
 cudaError_t launch_back(const TurnParams& p, const Shape& s, unsigned ctas, cudaStream_t st) {
   const dim3 grid(ctas, (unsigned)p.n_t), block(THREADS);
   const int heads = std::max(p.t[0].heads, p.t[1].heads);
-  const size_t smem = s.vec ? NORM == AS_NORM_ROW ? (size_t)WARPS * s.NV * (2048 + 1024 * sizeof(T)) : (size_t)WARPS * (2048 + s.NV * 1024 * sizeof(T)) : (size_t)(NORM == AS_NORM_ROW ? heads : WARPS) * p.d * 4;
+  const size_t sums = NORM == AS_NORM_ROW ? s.NV : 1;
+  const size_t smem = s.vec ? WARPS * (sums * 2048 + s.NV * 1024 * sizeof(T) + (size_t)p.pairs * 8) + s.kept : (size_t)(NORM == AS_NORM_ROW ? heads : WARPS) * p.d * 4;
   auto run = [&](auto kernel) {
     if (smem > 40 * 1024)                                // (beside what the kernels have of a fixed size, 48 KB are there without asking)
       if (const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); e != cudaSuccess) return e;
