@@ -831,7 +831,8 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 1) linear_few_kernel(const __g
   for (int i = 0; i < AHEAD - 1; ++i) ask();
   int take = 0, turn = 0;
   for (int u = blockIdx.x; u < p.units; u += gridDim.x, turn ^= 1) {
-    float acc[NT][4] = {};
+    float acc[NT][4] = {}, run[NT][4] = {};                           // (matrix instructions truncate their sums: runs of 32 of them are added up rounded to nearest)
+    int in_run = 0;
     for (int k = part; k < kb; k += p.split) {
       ask();                                                          // (a lane fills and reads its own 16 bytes of each piece: nothing to wait for in the other lanes)
       asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD - 1) : "memory");
@@ -851,9 +852,16 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 1) linear_few_kernel(const __g
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                       : "+f"(acc[t][0]), "+f"(acc[t][1]), "+f"(acc[t][2]), "+f"(acc[t][3])
+                       : "+f"(run[t][0]), "+f"(run[t][1]), "+f"(run[t][2]), "+f"(run[t][3])
                        : "r"(w[0][i / 2][2 * (i % 2)]), "r"(w[1][i / 2][2 * (i % 2)]), "r"(w[0][i / 2][2 * (i % 2) + 1]), "r"(w[1][i / 2][2 * (i % 2) + 1]),
                          "r"(x[i / 2][2 * (i % 2)]), "r"(x[i / 2][2 * (i % 2) + 1]));
+      }
+      if (++in_run == 8 || k + p.split >= kb) {
+        in_run = 0;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) { acc[t][j] += run[t][j]; run[t][j] = 0.f; }
       }
     }
 #pragma unroll

@@ -1,14 +1,13 @@
 """The attention half of a converted layer, its linear layers in 8 bits: what `HybridAttention` and the 8-bit projections do together.
 
     t = hidden + residual;  x = norm(t)                                  rms_norm: x in 8-bit form, t is the next residual
-    q, k = norm_q(x Wq + bq), norm_k(x Wk + bk);  v = x Wv + bv          matmul_fp8; the norms and v land in heads
+    q, k = norm_q(x Wq + bq), norm_k(x Wk + bk);  v = x Wv + bv          matmul_fp8; the norms and v land in heads; with a table, turned by the tokens' positions in the same pass (qk_norm_rotary)
     o = hybrid attention of q, k, v                                      HybridAttention.forward
     y = o Wo + bo                                                        quantize_fp8 from heads, matmul_fp8
 
 No tensor is copied or permuted between the calls.  Weights are frozen: they are brought to their 8-bit form once.
 
-Nothing stands between the norms of q and k and the attention: a model that turns them there (a rotary embedding) makes the same calls itself, with its own step in between.  q, k and
-v come from three products, each of which lands where it is needed; one product with the three weights on top of each other gives rows [B N, 3 H d], of which the norms take their
+q, k and v come from three products, each of which lands where it is needed; one product with the three weights on top of each other gives rows [B N, 3 H d], of which the norms take their
 thirds as they lie, but v would be copied into heads (the attention takes contiguous ones).
 """
 from __future__ import annotations
@@ -17,15 +16,16 @@ import torch
 
 from . import HybridAttention
 from .block_fp8 import matmul_fp8, quantize_fp8, rms_norm
+from .rotation import qk_norm_rotary
 
 
 class Fp8AttentionLayer:
     """`attention`: the layer's HybridAttention, of B x H x N x d.  `weights`: name -> bf16 CUDA tensor: "q", "k", "v", "o" [H d, H d] and
     optionally "bias_q", ..., "bias_o" [H d], "norm", "norm_q", "norm_k" [H d], all on the current device; `phi`: the feature maps' weights, the
-    keyword arguments that `HybridAttention.forward` takes (wq, wk, ...)."""
+    keyword arguments that `HybridAttention.forward` takes (wq, wk, ...); `table`: a RotaryTable of the layer's grid, by which q and k are turned, in `layout`."""
 
-    def __init__(self, attention: HybridAttention, weights, phi, eps=1e-6):
-        self.attention, self.phi, self.eps = attention, phi, eps
+    def __init__(self, attention: HybridAttention, weights, phi, eps=1e-6, table=None, layout="interleaved"):
+        self.attention, self.phi, self.eps, self.table, self.layout = attention, phi, eps, table, layout
         B, H, N, d = attention.shape
         for name in "qkvo":
             if tuple(weights[name].shape) != (H * d, H * d):
@@ -43,9 +43,14 @@ class Fp8AttentionLayer:
         x8, residual = rms_norm(hidden, self._norm["norm"], residual=residual, eps=self.eps, fp8=True)
         shape = self.attention.shape
         q, k, v = (torch.empty(shape, dtype=torch.bfloat16, device=hidden.device) for _ in range(3))
-        for name, out in (("q", q), ("k", k)):
-            rows = matmul_fp8(x8, self._w8[name], bias=self._bias[name])
-            rms_norm(rows, self._norm["norm_" + name], eps=self.eps, out=out)
+        rows = [matmul_fp8(x8, self._w8[name], bias=self._bias[name]) for name in "qk"]
+        if self.table is None:
+            for name, r, out in zip("qk", rows, (q, k)):
+                rms_norm(r, self._norm["norm_" + name], eps=self.eps, out=out)
+        else:
+            B, H, N, d = shape
+            heads = [r.view(B, N, H, d).permute(0, 2, 1, 3) for r in rows]
+            qk_norm_rotary(*heads, self._norm["norm_q"], self._norm["norm_k"], self.table, norm="row", eps=self.eps, layout=self.layout, q_out=q, k_out=k)
         matmul_fp8(x8, self._w8["v"], bias=self._bias["v"], out=v)
         o = self.attention.forward(q, k, v, **self.phi)
         return matmul_fp8(quantize_fp8(o), self._w8["o"], bias=self._bias["o"]), residual

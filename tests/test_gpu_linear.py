@@ -64,6 +64,17 @@ def test_larger_products(ops, m, k, n):
     assert torch.equal(y, ops.linear(x, w, bias=b, activation="gelu_tanh", residual=r))
 
 
+@pytest.mark.parametrize("m", [4, 40, 300, 2000])
+@pytest.mark.parametrize("k", [1536, 6144, 20000])
+def test_long_sums_in_fp32(ops, m, k):
+    """The matrix instructions truncate what they add up, 2^-23 of it at most and half of that in the mean, always towards 0: sums come in runs of 72 instructions at most (18 steps of 64 columns, and
+    a third more in a tile's first run), so that the whole is off by less than 96 * 2^-24 in the mean.  (In one run of 384, for 6144 columns, it was 7e-6, of 1250, for 20000, 2e-5.)"""
+    x, w = randn(m, k, seed=1).abs(), weights(192, k).abs()
+    y = ops.linear(x, w, out=torch.empty(m, 192, dtype=F32, device="cuda"))
+    ref = x.to(R.F64) @ w.to(R.F64).T
+    assert float((y.to(R.F64) - ref).norm() / ref.norm()) <= 96 * 2.0 ** -24
+
+
 @pytest.mark.parametrize("B,H,N,d", [(1, 2, 300, 64), (2, 12, 150, 128), (3, 5, 7, 40), (2, 3, 31, 8), (1, 9, 20, 17), (40, 4, 1, 64), (2, 4, 1030, 64), (1, 3, 9, 128), (5, 2, 3, 128)])
 def test_heads(ops, B, H, N, d):
     """x, residual, out and pre in heads, each beside rows of the others; a gate for each entry."""
