@@ -102,6 +102,7 @@ struct TurnParams {
   int lanes_log;                             // lanes of a head: 2^lanes_log
   int W;                                     // warps of a row
   int chunks;                                // runs of heads that a warp takes at once, where the norm is not over rows
+  int room;                                  // bytes of a warp's factors: chunks of two pairs, in whole groups of eight
   int kept;                                  // rows' weights are kept in shared memory: bytes of the first tensor's (0: they are not)
 };
 AS_DEV unsigned quotient(unsigned i, unsigned long long by) { return by == 0ull ? i : (unsigned)__umul64hi(by, i); }
@@ -148,7 +149,7 @@ AS_DEV float2 factor_of(const TurnParams& p, const Where& w, int pair) {
   return f;
 }
 // A token's cos and sin in its warp's shared memory, two pairs (16 bytes) a lane, asked for a row ahead: read by every lane from the table they were 100 instructions and two waits a row.
-// Chunks of two pairs lie so that the lanes of a head, which read one of every two or four, meet no bank twice.
+// Chunks of two pairs lie so that the lanes of a head, which read one of every two or four, meet no bank twice (within their group of eight).
 AS_DEV uint32_t chunk_at(uint32_t room, int c) { return room + (uint32_t)((c ^ (c >> 3 & 7)) << 4); }
 AS_DEV void ask_factors(const TurnParams& p, const Where& w, uint32_t room, int lane) {
   for (int pair = 2 * lane; pair < p.pairs; pair += 64) {
@@ -168,8 +169,8 @@ AS_DEV void ask_factors(const TurnParams& p, const Where& w, uint32_t room, int 
 }
 
 // ---------------------------------------------------------------- vectors of a lane
-// 16 elements of a head as the first and the second elements of 8 pairs, two pairs a register pair: arithmetic goes two values at a time.
-struct Pairs { float2 a[4], b[4]; };
+// E elements of a head (16, or 8) as the first and the second elements of E / 2 pairs, two pairs a register pair: arithmetic goes two values at a time.
+template <int E> struct PairsOf { float2 a[E / 4], b[E / 4]; };
 AS_DEV float2 mul2(float2 a, float2 b) {
   float2 d;
   asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
@@ -189,87 +190,104 @@ AS_DEV float2 sub2(float2 a, float2 b) {
       : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
   return d;
 }
-AS_DEV void scale(Pairs& v, float2 f) {
+template <int E>
+AS_DEV void scale(PairsOf<E>& v, float2 f) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) { v.a[i] = mul2(v.a[i], f); v.b[i] = mul2(v.b[i], f); }
+  for (int i = 0; i < E / 4; ++i) { v.a[i] = mul2(v.a[i], f); v.b[i] = mul2(v.b[i], f); }
 }
-AS_DEV void scale(Pairs& v, const Pairs& w) {
+template <int E>
+AS_DEV void scale(PairsOf<E>& v, const PairsOf<E>& w) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) { v.a[i] = mul2(v.a[i], w.a[i]); v.b[i] = mul2(v.b[i], w.b[i]); }
+  for (int i = 0; i < E / 4; ++i) { v.a[i] = mul2(v.a[i], w.a[i]); v.b[i] = mul2(v.b[i], w.b[i]); }
 }
-AS_DEV float2 dot(const Pairs& v, const Pairs& w, float2 s) {
+template <int E>
+AS_DEV float2 dot(const PairsOf<E>& v, const PairsOf<E>& w, float2 s) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) { s = fma2(v.a[i], w.a[i], s); s = fma2(v.b[i], w.b[i], s); }
+  for (int i = 0; i < E / 4; ++i) { s = fma2(v.a[i], w.a[i], s); s = fma2(v.b[i], w.b[i], s); }
   return s;
 }
 
-template <typename T> struct Raw { uint4 v[sizeof(T)]; };        // 16 elements: two pieces of 8
-template <typename T>
-AS_DEV void load_kept(Raw<T>& r, const T* at, int second) {
-#pragma unroll
-  for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
-    r.v[i] = __ldg(reinterpret_cast<const uint4*>(at + i * (16 / sizeof(T))));
-    r.v[sizeof(T) / 2 + i] = __ldg(reinterpret_cast<const uint4*>(at + second + i * (16 / sizeof(T))));
-  }
+// A lane's E elements as they lie: two pieces of E / 2, in words, and in what moves at once: 16 bytes, or 8 (8 elements in bf16).
+template <typename T, int E> struct Raw { uint32_t w[E * sizeof(T) / 4]; };
+template <typename T, int E> constexpr int PIECE = E / 2 * (int)sizeof(T);          // bytes of a piece
+template <typename T, int E> constexpr int MOVE = PIECE<T, E> < 16 ? 8 : 16;         // bytes that move at once
+template <typename T, int E> constexpr int MOVES = E * (int)sizeof(T) / MOVE<T, E>;  // of a lane's elements
+// Where move i begins: elements behind the first piece's first one.
+template <typename T, int E>
+AS_DEV int element_of(int i, int second) { return (i < MOVES<T, E> / 2 ? 0 : second) + i % (MOVES<T, E> / 2) * (MOVE<T, E> / (int)sizeof(T)); }
+template <int BYTES>
+AS_DEV void read_shared(uint32_t at, uint32_t* w) {
+  if constexpr (BYTES == 16) asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
+  else asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at) : "memory");
 }
-// HALF: the pieces are the first and the second elements of 8 pairs; else each is 4 pairs.  (What is not turned may be called either.)
-template <bool HALF, typename T>
-AS_DEV void values(const Raw<T>& r, Pairs& f) {
-  const uint32_t* w = reinterpret_cast<const uint32_t*>(r.v);
+template <int BYTES>
+AS_DEV void copy_shared(uint32_t to, const void* from) {
+  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory");
+}
+template <int BYTES>
+AS_DEV void clear_shared(uint32_t to) {
+  if constexpr (BYTES == 16) asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(to), "r"(0) : "memory");
+  else asm volatile("st.shared.v2.u32 [%0], {%1, %1};" ::"r"(to), "r"(0) : "memory");
+}
+// HALF: the pieces are the first and the second elements of E / 2 pairs; else each is E / 4 pairs.  (What is not turned may be called either.)
+template <bool HALF, typename T, int E>
+AS_DEV void values(const Raw<T, E>& r, PairsOf<E>& f) {
+  const uint32_t* w = r.w;
   auto lo = [](uint32_t x) { return __uint_as_float(x << 16); };
   auto hi = [](uint32_t x) { return __uint_as_float(x & 0xffff0000u); };
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < E / 4; ++i) {
     if constexpr (sizeof(T) == 2) {
-      if constexpr (HALF) { f.a[i] = make_float2(lo(w[i]), hi(w[i])); f.b[i] = make_float2(lo(w[4 + i]), hi(w[4 + i])); }
+      if constexpr (HALF) { f.a[i] = make_float2(lo(w[i]), hi(w[i])); f.b[i] = make_float2(lo(w[E / 4 + i]), hi(w[E / 4 + i])); }
       else { f.a[i] = make_float2(lo(w[2 * i]), lo(w[2 * i + 1])); f.b[i] = make_float2(hi(w[2 * i]), hi(w[2 * i + 1])); }
     } else {
       auto at = [&](int j) { return __uint_as_float(w[j]); };
-      if constexpr (HALF) { f.a[i] = make_float2(at(2 * i), at(2 * i + 1)); f.b[i] = make_float2(at(8 + 2 * i), at(9 + 2 * i)); }
+      if constexpr (HALF) { f.a[i] = make_float2(at(2 * i), at(2 * i + 1)); f.b[i] = make_float2(at(E / 2 + 2 * i), at(E / 2 + 1 + 2 * i)); }
       else { f.a[i] = make_float2(at(4 * i), at(4 * i + 2)); f.b[i] = make_float2(at(4 * i + 1), at(4 * i + 3)); }
     }
   }
 }
-template <bool HALF, typename T>
-AS_DEV void store(T* at, int second, const Pairs& f) {
-  uint4 v[sizeof(T)];
-  uint32_t* w = reinterpret_cast<uint32_t*>(v);
+template <bool HALF, typename T, int E>
+AS_DEV void store(T* at, int second, const PairsOf<E>& f) {
+  uint32_t w[E * sizeof(T) / 4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < E / 4; ++i) {
     if constexpr (sizeof(T) == 2) {
-      if constexpr (HALF) { w[i] = sm100::pack_bf16(f.a[i].x, f.a[i].y); w[4 + i] = sm100::pack_bf16(f.b[i].x, f.b[i].y); }
+      if constexpr (HALF) { w[i] = sm100::pack_bf16(f.a[i].x, f.a[i].y); w[E / 4 + i] = sm100::pack_bf16(f.b[i].x, f.b[i].y); }
       else { w[2 * i] = sm100::pack_bf16(f.a[i].x, f.b[i].x); w[2 * i + 1] = sm100::pack_bf16(f.a[i].y, f.b[i].y); }
     } else {
       auto put = [&](int j, float x) { w[j] = __float_as_uint(x); };
-      if constexpr (HALF) { put(2 * i, f.a[i].x); put(2 * i + 1, f.a[i].y); put(8 + 2 * i, f.b[i].x); put(9 + 2 * i, f.b[i].y); }
+      if constexpr (HALF) { put(2 * i, f.a[i].x); put(2 * i + 1, f.a[i].y); put(E / 2 + 2 * i, f.b[i].x); put(E / 2 + 1 + 2 * i, f.b[i].y); }
       else { put(4 * i, f.a[i].x); put(4 * i + 1, f.b[i].x); put(4 * i + 2, f.a[i].y); put(4 * i + 3, f.b[i].y); }
     }
   }
 #pragma unroll
-  for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
-    *reinterpret_cast<uint4*>(at + i * (16 / sizeof(T))) = v[i];
-    *reinterpret_cast<uint4*>(at + second + i * (16 / sizeof(T))) = v[sizeof(T) / 2 + i];
+  for (int i = 0; i < MOVES<T, E>; ++i) {
+    T* to = at + element_of<T, E>(i, second);
+    const uint32_t* x = w + i * (MOVE<T, E> / 4);
+    if constexpr (MOVE<T, E> == 16) *reinterpret_cast<uint4*>(to) = make_uint4(x[0], x[1], x[2], x[3]);
+    else *reinterpret_cast<uint2*>(to) = make_uint2(x[0], x[1]);
   }
 }
-// KEPT: from shared memory, where `w` is an address of it.
-template <bool HALF, bool KEPT, typename W>
-AS_DEV void load_weights(const W* w, uint32_t kept, int at, int second, Pairs& f) {
-  Raw<W> r;
-  if constexpr (KEPT) {
+// KEPT: from shared memory, at the address `kept`.
+template <bool HALF, bool KEPT, typename W, int E>
+AS_DEV void load_weights_of(const W* w, uint32_t kept, int at, int second, PairsOf<E>& f) {
+  Raw<W, E> r;
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(W); ++i) {
-      const int e = at + (i < (int)sizeof(W) / 2 ? 0 : second) + i % ((int)sizeof(W) / 2) * (16 / (int)sizeof(W));
-      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.v[i].x), "=r"(r.v[i].y), "=r"(r.v[i].z), "=r"(r.v[i].w) : "r"(kept + (uint32_t)e * (uint32_t)sizeof(W)) : "memory");
-    }
-  } else {
-    load_kept(r, w + at, second);
+  for (int i = 0; i < MOVES<W, E>; ++i) {
+    const int e = at + element_of<W, E>(i, second);
+    uint32_t* to = r.w + i * (MOVE<W, E> / 4);
+    if constexpr (KEPT) read_shared<MOVE<W, E>>(kept + (uint32_t)e * (uint32_t)sizeof(W), to);
+    else if constexpr (MOVE<W, E> == 16) *reinterpret_cast<uint4*>(to) = __ldg(reinterpret_cast<const uint4*>(w + e));
+    else *reinterpret_cast<uint2*>(to) = __ldg(reinterpret_cast<const uint2*>(w + e));
   }
   values<HALF>(r, f);
 }
-template <bool HALF, bool KEPT>
-AS_DEV void load_weights(const TurnParams& p, const void* w, uint32_t kept, int at, int second, Pairs& f) {
-  if (p.w_f32) load_weights<HALF, KEPT>(static_cast<const float*>(w), kept, at, second, f);
-  else load_weights<HALF, KEPT>(static_cast<const bf*>(w), kept, at, second, f);
+template <bool HALF, bool KEPT, int E>
+AS_DEV void load_weights(const TurnParams& p, const void* w, uint32_t kept, int at, int second, PairsOf<E>& f) {
+  if (p.w_f32) load_weights_of<HALF, KEPT>(static_cast<const float*>(w), kept, at, second, f);
+  else load_weights_of<HALF, KEPT>(static_cast<const bf*>(w), kept, at, second, f);
 }
 // A row's weights to shared memory, by the whole CTA, which meets behind it.
 AS_DEV void keep_weights(const TurnParams& p, const TurnTensor& t, uint8_t* to) {
@@ -277,14 +295,14 @@ AS_DEV void keep_weights(const TurnParams& p, const TurnTensor& t, uint8_t* to) 
   const int n = t.heads * p.d * (p.w_f32 ? 4 : 2) / 16;
   for (int i = threadIdx.x; i < n; i += THREADS) reinterpret_cast<uint4*>(to)[i] = __ldg(static_cast<const uint4*>(t.w) + i);
 }
-// cos and sin of a lane's 8 pairs.
-struct Factors { float2 c[4], s[4]; };
-template <bool HALF>
-AS_DEV Factors factors_of(const TurnParams& p, uint32_t room, int slot) {
-  Factors t;
+// cos and sin of a lane's E / 2 pairs.
+template <int E> struct FactorsOf { float2 c[E / 4], s[E / 4]; };
+template <bool HALF, int E>
+AS_DEV FactorsOf<E> factors_of(const TurnParams& p, uint32_t room, int slot) {
+  FactorsOf<E> t;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int c = HALF ? slot * 4 + i : i < 2 ? slot * 2 + i : p.pairs / 4 + slot * 2 + i - 2;
+  for (int i = 0; i < E / 4; ++i) {                      // chunks of two pairs
+    const int c = HALF ? slot * (E / 4) + i : i < E / 8 ? slot * (E / 8) + i : p.pairs / 4 + slot * (E / 8) + i - E / 8;
     float4 v;
     asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(chunk_at(room, c)) : "memory");
     t.c[i] = make_float2(v.x, v.z);
@@ -294,9 +312,10 @@ AS_DEV Factors factors_of(const TurnParams& p, uint32_t room, int slot) {
 }
 // Behind the copies that this thread has asked for, and, where the factors are among them, those of its warp.
 AS_DEV void wait_copies() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-AS_DEV void turn(Pairs& v, const Factors& f) {
+template <int E>
+AS_DEV void turn(PairsOf<E>& v, const FactorsOf<E>& f) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < E / 4; ++i) {
     const float2 a = v.a[i], b = v.b[i];
     v.a[i] = sub2(mul2(a, f.c[i]), mul2(b, f.s[i]));
     v.b[i] = fma2(a, f.s[i], mul2(b, f.c[i]));
@@ -305,14 +324,15 @@ AS_DEV void turn(Pairs& v, const Factors& f) {
 
 // What a lane works on: its head of vector 0, elements of a head, whether they are turned.
 struct Lane { int head, heads_a_vector, slot, e0, second; bool in_head, turned; };
+template <int E>
 AS_DEV Lane lane_of(const TurnParams& p, int lane) {
   Lane l;
   l.slot = lane & ((1 << p.lanes_log) - 1);
   l.head = lane >> p.lanes_log;
   l.heads_a_vector = 32 >> p.lanes_log;
-  l.in_head = l.slot * 16 < p.d;
-  l.turned = l.slot * 8 < p.pairs;
-  l.e0 = l.turned ? l.slot * 8 : p.pairs + l.slot * 8;             // what is not turned begins at 2 P, its slots at P / 8
+  l.in_head = l.slot * E < p.d;
+  l.turned = l.slot * (E / 2) < p.pairs;
+  l.e0 = l.turned ? l.slot * (E / 2) : p.pairs + l.slot * (E / 2);       // what is not turned begins at 2 P, its slots at 2 P / E
   l.second = l.turned ? p.pairs : (p.d - 2 * p.pairs) / 2;
   return l;
 }
@@ -355,39 +375,37 @@ AS_DEV float factor_for(float sum, float over_n, float eps, bool there) { return
 // ---------------------------------------------------------------- forward
 // A warp holds a row of queries and one of keys (or pieces of them) at once.  What counts beside the bytes is the number of instructions: one value at a time, each vector of 16 elements a
 // lane took 340 of them, and 32760 tokens of 2 x 12 heads 106 us.
-template <typename T, int NORM, int NV, bool HALF>
+template <typename T, int NORM, int NV, bool HALF, int E>
 __global__ void __launch_bounds__(THREADS, 2) turn_kernel(const __grid_constant__ TurnParams p) {
+  typedef PairsOf<E> Pairs;
+  typedef FactorsOf<E> Factors;
   griddep_launch();
   __shared__ float part[1][WARPS];
   extern __shared__ uint4 dynamic[];                     // factors of each warp's row; weights of both tensors
   constexpr bool ROW = NORM == AS_NORM_ROW;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int per = ROW ? WARPS / p.W : WARPS, slot = ROW ? warp / p.W : warp, piece = ROW ? warp - slot * p.W : (int)blockIdx.y;
-  const Lane l = lane_of(p, lane);
+  const Lane l = lane_of<E>(p, lane);
   const int h0 = piece * NV * l.heads_a_vector + l.head;
   long long row = (long long)blockIdx.x * per + slot;
   bool live = slot < per && row < p.rows;
   Token k = token_of(p, live ? (unsigned)row : 0u);
   // rows of both tensors, in this lane's own pieces of 16 bytes: the next row's are asked for as soon as this one's have been read for the last time
-  constexpr int PIECES = sizeof(T);
-  const uint32_t rows_at = sm100::smem_u32(dynamic) + (uint32_t)(warp * (NV * 2 * PIECES * 512) + lane * 16);
-  const uint32_t room = sm100::smem_u32(dynamic) + (uint32_t)(WARPS * (NV * 2 * PIECES * 512) + warp * p.pairs * 8);
-  uint8_t* kept = reinterpret_cast<uint8_t*>(dynamic) + WARPS * (NV * 2 * PIECES * 512 + p.pairs * 8);
-  auto place = [&](int i, int j, int piece) { return rows_at + (uint32_t)((i * NV + j) * PIECES + piece) * 512u; };
+  constexpr int PIECES = MOVES<T, E>, STEP = 32 * MOVE<T, E>;            // moves of a vector, bytes of one by a warp
+  const uint32_t rows_at = sm100::smem_u32(dynamic) + (uint32_t)(warp * (NV * 2 * PIECES * STEP) + lane * MOVE<T, E>);
+  const uint32_t room = sm100::smem_u32(dynamic) + (uint32_t)(WARPS * (NV * 2 * PIECES * STEP) + warp * p.room);
+  uint8_t* kept = reinterpret_cast<uint8_t*>(dynamic) + WARPS * (NV * 2 * PIECES * STEP + p.room);
+  auto place = [&](int i, int j, int piece) { return rows_at + (uint32_t)(((i * NV + j) * PIECES + piece) * STEP); };
   auto ask = [&](const TurnTensor& t, int i, int j, const T* base) {
     const int h = h0 + j * l.heads_a_vector;
     if (!l.in_head || h >= t.heads) return;
 #pragma unroll
-    for (int q = 0; q < PIECES; ++q) {
-      const int e = (q < PIECES / 2 ? 0 : l.second) + q % (PIECES / 2) * (16 / (int)sizeof(T));
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(place(i, j, q)), "l"(base + h * t.x.sh + e) : "memory");
-    }
+    for (int q = 0; q < PIECES; ++q) copy_shared<MOVE<T, E>>(place(i, j, q), base + h * t.x.sh + element_of<T, E>(q, l.second));
   };
   auto take = [&](int i, int j, Pairs& v) {
-    Raw<T> r;
+    Raw<T, E> r;
 #pragma unroll
-    for (int q = 0; q < PIECES; ++q)
-      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.v[q].x), "=r"(r.v[q].y), "=r"(r.v[q].z), "=r"(r.v[q].w) : "r"(place(i, j, q)) : "memory");
+    for (int q = 0; q < PIECES; ++q) read_shared<MOVE<T, E>>(place(i, j, q), r.w + q * (MOVE<T, E> / 4));
     values<HALF>(r, v);
   };
   auto base_of = [&](const TurnTensor& t, const Token& k) { return static_cast<const T*>(t.x.data) + address(t.x, k) + l.e0; };
@@ -401,7 +419,7 @@ __global__ void __launch_bounds__(THREADS, 2) turn_kernel(const __grid_constant_
       for (int j = 0; j < NV; ++j) {
         if (!l.in_head || h0 + j * l.heads_a_vector >= t.heads)              // heads that are not there are 0
 #pragma unroll
-          for (int q = 0; q < PIECES; ++q) asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(place(i, j, q)), "r"(0) : "memory");
+          for (int q = 0; q < PIECES; ++q) clear_shared<MOVE<T, E>>(place(i, j, q));
         if (live) ask(t, i, j, base_of(t, k));
       }
     }
@@ -419,7 +437,7 @@ __global__ void __launch_bounds__(THREADS, 2) turn_kernel(const __grid_constant_
   wait_copies();
   if (p.table != nullptr) {
     __syncwarp();
-    if (l.turned) cs = factors_of<HALF>(p, room, l.slot);
+    if (l.turned) cs = factors_of<HALF, E>(p, room, l.slot);
     __syncwarp();
     if (more) ask_factors(p, where_of(p, next), room, lane);
   }
@@ -495,8 +513,10 @@ __global__ void __launch_bounds__(THREADS, 2) turn_kernel(const __grid_constant_
 // ---------------------------------------------------------------- backward
 // dx = r (g - n mean(g n)), g = d w, d = R^T dy, n = x r.  A CTA goes on from row to row of one tensor.  Each warp has its sums of d n in shared
 // memory (in registers, up to 48 of them, they left room for one CTA an SM), and the rows that it works on come there by asynchronous copies.  Both sums of a row, over x^2 and over g x, are taken at once.
-template <typename T, int NORM, int NV, bool HALF>
+template <typename T, int NORM, int NV, bool HALF, int E>
 __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) turn_back_kernel(const __grid_constant__ TurnParams p) {
+  typedef PairsOf<E> Pairs;
+  typedef FactorsOf<E> Factors;
   griddep_launch();
   __shared__ float part[2][WARPS];
   extern __shared__ float4 sums[];                       // of d n, of each warp: [vectors][4][32 lanes]
@@ -505,13 +525,14 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) turn_back_ker
   constexpr bool ROW = NORM == AS_NORM_ROW;
   const int per = ROW ? WARPS / p.W : WARPS;
   const int slot = ROW ? warp / p.W : warp, fixed_piece = ROW ? warp - slot * p.W : 0;
-  const Lane l = lane_of(p, lane);
+  const Lane l = lane_of<E>(p, lane);
   const bool sums_wanted = t.part != nullptr;
   constexpr int NA = ROW ? NV : 1;                       // vectors of sums: heads share them, or each has its own
-  float4* mine = sums + warp * (NA * 128) + lane;
+  constexpr int G = E / 4;                                // groups of two pairs, four sums each
+  float4* mine = sums + warp * (NA * G * 32) + lane;
   if (sums_wanted) {
 #pragma unroll
-    for (int i = 0; i < NA * 4; ++i) mine[i * 32] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = 0; i < NA * G; ++i) mine[i * 32] = make_float4(0.f, 0.f, 0.f, 0.f);
   }
   const int chunk = ROW ? 0 : (int)(blockIdx.x % (unsigned)p.chunks);
   const unsigned first_cta = ROW ? blockIdx.x : blockIdx.x / (unsigned)p.chunks, ctas = ROW ? gridDim.x : gridDim.x / (unsigned)p.chunks;      // (gridDim.x is a multiple of chunks)
@@ -520,34 +541,33 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) turn_back_ker
   griddep_wait();
   Pairs w;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) w.a[i] = w.b[i] = both(1.f);
+  for (int i = 0; i < G; ++i) w.a[i] = w.b[i] = both(1.f);
   if (!ROW && t.w != nullptr && l.in_head) load_weights<HALF, false>(p, t.w, 0u, l.e0, l.second, w);
   // x and dy of a row, in this lane's own pieces of 16 bytes: the next row's are asked for as soon as this one's have been read for the last time
-  constexpr int PIECES = sizeof(T);
-  float4* behind = sums + WARPS * (NA * 128);
-  const uint32_t room = sm100::smem_u32(behind) + (uint32_t)(warp * (NV * 2 * PIECES * 512) + lane * 16);
-  behind += WARPS * (NV * 2 * PIECES * 32);
-  const uint32_t factors = sm100::smem_u32(behind) + (uint32_t)(warp * p.pairs * 8), kept = sm100::smem_u32(behind) + (uint32_t)(WARPS * p.pairs * 8);
+  constexpr int PIECES = MOVES<T, E>, STEP = 32 * MOVE<T, E>;            // moves of a vector, bytes of one by a warp
+  float4* behind = sums + WARPS * (NA * G * 32);
+  const uint32_t room = sm100::smem_u32(behind) + (uint32_t)(warp * (NV * 2 * PIECES * STEP) + lane * MOVE<T, E>);
+  behind += WARPS * (NV * 2 * PIECES * STEP / 16);
+  const uint32_t factors = sm100::smem_u32(behind) + (uint32_t)(warp * p.room), kept = sm100::smem_u32(behind) + (uint32_t)(WARPS * p.room);
   if constexpr (ROW)
     if (p.kept > 0) {
-      keep_weights(p, t, reinterpret_cast<uint8_t*>(behind) + WARPS * p.pairs * 8);
+      keep_weights(p, t, reinterpret_cast<uint8_t*>(behind) + WARPS * p.room);
       __syncthreads();
     }
-  auto place = [&](int j, int tensor, int piece) { return room + (uint32_t)((j * 2 + tensor) * PIECES + piece) * 512u; };
+  auto place = [&](int j, int tensor, int piece) { return room + (uint32_t)(((j * 2 + tensor) * PIECES + piece) * STEP); };
   auto ask = [&](const T* bx, const T* by, bool live, int j) {
     const int h = h0 + j * l.heads_a_vector;
     if (!(live && l.in_head && h < t.heads)) return;
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-      const int e = (i < PIECES / 2 ? 0 : l.second) + i % (PIECES / 2) * (16 / (int)sizeof(T));
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(place(j, 0, i)), "l"(bx + h * t.x.sh + e) : "memory");
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(place(j, 1, i)), "l"(by + h * t.dy.sh + e) : "memory");
+      const int e = element_of<T, E>(i, l.second);
+      copy_shared<MOVE<T, E>>(place(j, 0, i), bx + h * t.x.sh + e);
+      copy_shared<MOVE<T, E>>(place(j, 1, i), by + h * t.dy.sh + e);
     }
   };
-  auto take_raw = [&](int j, int tensor, Raw<T>& r) {
+  auto take_raw = [&](int j, int tensor, Raw<T, E>& r) {
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i)
-      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.v[i].x), "=r"(r.v[i].y), "=r"(r.v[i].z), "=r"(r.v[i].w) : "r"(place(j, tensor, i)) : "memory");
+    for (int i = 0; i < PIECES; ++i) read_shared<MOVE<T, E>>(place(j, tensor, i), r.w + i * (MOVE<T, E> / 4));
   };
   auto x_of = [&](const Token& k) { return static_cast<const T*>(t.x.data) + address(t.x, k) + l.e0; };
   auto y_of = [&](const Token& k) { return static_cast<const T*>(t.dy.data) + address(t.dy, k) + l.e0; };
@@ -559,7 +579,7 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) turn_back_ker
   for (int j = 0; j < NV; ++j) {
     if (!l.in_head || h0 + j * l.heads_a_vector >= t.heads)                  // heads that are not there are 0
 #pragma unroll
-      for (int i = 0; i < 2 * PIECES; ++i) asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(place(j, 0, i)), "r"(0) : "memory");
+      for (int i = 0; i < 2 * PIECES; ++i) clear_shared<MOVE<T, E>>(place(j, 0, i));
     ask(x_of(tk), y_of(tk), live, j);
   }
   for (long long u0 = (long long)first_cta * per; u0 < p.rows; u0 += (long long)ctas * per) {       // a turn is one for the whole CTA
@@ -571,13 +591,13 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) turn_back_ker
     Factors cs;
     if (p.table != nullptr) {
       __syncwarp();
-      if (l.turned) cs = factors_of<HALF>(p, factors, l.slot);
+      if (l.turned) cs = factors_of<HALF, E>(p, factors, l.slot);
       __syncwarp();
       if (more) ask_factors(p, where_of(p, next), factors, lane);
     }
     // x and d of vector j, and its weights
     auto operands = [&](int j, Pairs& v, Pairs& d) {
-      Raw<T> r;
+      Raw<T, E> r;
       take_raw(j, 0, r);
       values<HALF>(r, v);
       take_raw(j, 1, r);
@@ -639,16 +659,16 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) turn_back_ker
       scale(v, both(sum[0]));
       if (sums_wanted) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float4 q = mine[((ROW ? j : 0) * 4 + i) * 32];
+        for (int i = 0; i < G; ++i) {
+          const float4 q = mine[((ROW ? j : 0) * G + i) * 32];
           const float2 qa = fma2(d.a[i], v.a[i], make_float2(q.x, q.y)), qb = fma2(d.b[i], v.b[i], make_float2(q.z, q.w));
-          mine[((ROW ? j : 0) * 4 + i) * 32] = make_float4(qa.x, qa.y, qb.x, qb.y);
+          mine[((ROW ? j : 0) * G + i) * 32] = make_float4(qa.x, qa.y, qb.x, qb.y);
         }
       }
       scale(d, w);
       const float2 along = both(-sum[1]), r2 = both(sum[0]);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) { d.a[i] = mul2(fma2(v.a[i], along, d.a[i]), r2); d.b[i] = mul2(fma2(v.b[i], along, d.b[i]), r2); }
+      for (int i = 0; i < G; ++i) { d.a[i] = mul2(fma2(v.a[i], along, d.a[i]), r2); d.b[i] = mul2(fma2(v.b[i], along, d.b[i]), r2); }
       if (factor != 1.f) scale(d, both(factor));
       store<HALF>(out + h * t.o.sh, l.second, d);
     }
@@ -656,10 +676,10 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) turn_back_ker
     tk = next;
   }
   if (!sums_wanted) return;
-  // the warps' sums in their order: the CTA's row of partial sums.  Element e of a lane's 16, in the order of Pairs' words: pairs 2 i, 2 i + 1 first, then their second elements
+  // the warps' sums in their order: the CTA's row of partial sums.  A group is the first elements of pairs 2 i and 2 i + 1, and then their second ones
   auto element = [&](int i, int e) {                     // word e of group i
     const int pair = 2 * i + (e & 1), second = e >> 1;
-    return HALF ? (second ? l.second + pair : pair) : (2 * pair + second < 8 ? 2 * pair + second : l.second + 2 * pair + second - 8);
+    return HALF ? (second ? l.second + pair : pair) : (2 * pair + second < E / 2 ? 2 * pair + second : l.second + 2 * pair + second - E / 2);
   };
   if constexpr (ROW) {
     __syncthreads();
@@ -670,10 +690,10 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) turn_back_ker
         if (!l.in_head || h >= t.heads) continue;
         float* to = t.part + ((long long)blockIdx.x * t.heads + h) * p.d + l.e0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < G; ++i) {
           float4 q = make_float4(0.f, 0.f, 0.f, 0.f);
           for (int k = 0; k < per; ++k) {
-            const float4 x = sums[(k * p.W + fixed_piece) * (NV * 128) + (j * 4 + i) * 32 + lane];
+            const float4 x = sums[(k * p.W + fixed_piece) * (NV * G * 32) + (j * G + i) * 32 + lane];
             q.x += x.x; q.y += x.y; q.z += x.z; q.w += x.w;
           }
           to[element(i, 0)] = q.x; to[element(i, 1)] = q.y; to[element(i, 2)] = q.z; to[element(i, 3)] = q.w;
@@ -684,11 +704,11 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 2 ? 2 : 1) turn_back_ker
     __syncthreads();
     if (warp == 0) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < G; ++i) {
         float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int k = 0; k < WARPS; ++k) {
-          const float4 x = sums[k * 128 + i * 32 + lane];
+          const float4 x = sums[k * (G * 32) + i * 32 + lane];
           f.x += x.x; f.y += x.y; f.z += x.z; f.w += x.w;
         }
         float q[4] = {f.x, f.y, f.z, f.w};
@@ -929,10 +949,13 @@ as_status_t turn_ok(const as_qk_norm_rotary_t* a, bool back) {
   return AS_OK;
 }
 
-// Whether pieces of 8 elements move 16 bytes at a time.
-bool heads_vec(const as_rows_t& x) { return aligned(x.data, 16) && ((x.stride_batch | x.stride_head | x.stride_token) & (x.dtype == AS_DTYPE_BF16 ? 7 : 3)) == 0; }
+// Whether pieces of 4 or 8 elements move at once.
+bool heads_vec(const as_rows_t& x, int elements) {
+  const int bytes = elements * (x.dtype == AS_DTYPE_BF16 ? 2 : 4) < 16 ? 8 : 16;
+  return aligned(x.data, bytes) && ((x.stride_batch | x.stride_head | x.stride_token) & (bytes / (x.dtype == AS_DTYPE_BF16 ? 2 : 4) - 1)) == 0;
+}
 
-struct Shape { bool vec; int NV, chunks; long long ctas; size_t kept; };       // kept: bytes of both tensors' weights
+struct Shape { bool vec; int E, NV, chunks; long long ctas; size_t kept; };       // kept: bytes of both tensors' weights
 // Fills in what the kernels share; `most`: vectors that a lane's registers hold.
 Shape turn_params(const as_qk_norm_rotary_t& a, const as_rotation_t& r, int sms, bool back, const as_rows_t* more, int n_more, TurnParams& p) {
   const bool two = a.k.data != nullptr;
@@ -952,6 +975,7 @@ Shape turn_params(const as_qk_norm_rotary_t& a, const as_rotation_t& r, int sms,
   if (a.norm != AS_NORM_NONE) { p.t[0].w = a.q_weight; p.t[1].w = two ? a.k_weight : nullptr; }
   p.table = reinterpret_cast<const float2*>(r.table);
   p.pairs = pairs;                           // (0 without a table)
+  p.room = (pairs / 2 + 7) / 8 * 128;
   if (p.table != nullptr) {
     p.axes = r.n_axes;
     p.half = r.layout == AS_ROTARY_HALF;
@@ -965,11 +989,18 @@ Shape turn_params(const as_qk_norm_rotary_t& a, const as_rotation_t& r, int sms,
     }
   }
   Shape s{};
-  s.vec = a.head_dim % 16 == 0 && a.head_dim <= 512 && pairs % 8 == 0 && aligned(r.table, 16) && heads_vec(a.q) && (!two || heads_vec(a.k));
-  for (int i = 0; i < n_more; ++i) s.vec = s.vec && (more[i].data == nullptr || heads_vec(more[i]));
-  if (a.norm != AS_NORM_NONE) s.vec = s.vec && aligned(a.q_weight, 16) && (!two || aligned(a.k_weight, 16));
+  // 16 elements a lane, or 8, where sizes, pairs, strides and addresses allow it
+  auto fits = [&](int E) {
+    const int piece = E / 2, of_weights = piece * (p.w_f32 ? 4 : 2) < 16 ? 8 : 16;
+    if (a.head_dim % E != 0 || a.head_dim > 32 * E || pairs % piece != 0 || !aligned(r.table, 16) || !heads_vec(a.q, piece) || (two && !heads_vec(a.k, piece))) return false;
+    for (int i = 0; i < n_more; ++i)
+      if (more[i].data != nullptr && !heads_vec(more[i], piece)) return false;
+    return a.norm == AS_NORM_NONE || (aligned(a.q_weight, of_weights) && (!two || aligned(a.k_weight, of_weights)));
+  };
+  s.E = fits(16) ? 16 : 8;
+  s.vec = s.E == 16 || fits(8);
   p.lanes_log = 0;
-  while ((16 << p.lanes_log) < a.head_dim) ++p.lanes_log;
+  while ((s.E << p.lanes_log) < a.head_dim) ++p.lanes_log;
   const int heads = std::max(p.t[0].heads, p.t[1].heads), of_vector = std::max(1, 32 >> p.lanes_log), vectors = (heads + of_vector - 1) / of_vector;
     const int most = a.q.dtype == AS_DTYPE_BF16 ? 3 : 2;
   p.W = 1; p.chunks = 1;
@@ -981,7 +1012,7 @@ Shape turn_params(const as_qk_norm_rotary_t& a, const as_rotation_t& r, int sms,
     // weights in shared memory, as far as two CTAs an SM have the room
     const size_t size = p.w_f32 ? 4 : 2, of_q = (size_t)p.t[0].heads * a.head_dim * size, of_k = (size_t)p.t[1].heads * a.head_dim * size;
     s.kept = back ? std::max(of_q, of_k) : of_q + of_k;
-    if (s.vec && s.kept <= 12 * 1024) p.kept = (int)of_q;
+    if (s.vec && s.kept <= 12 * 1024 && of_q % 16 == 0 && of_k % 16 == 0 && aligned(a.q_weight, 16) && (!two || aligned(a.k_weight, 16))) p.kept = (int)of_q;
     else s.kept = 0;
   } else {
     // few rows: a vector a warp, so that all of them are under way at once
@@ -993,11 +1024,10 @@ Shape turn_params(const as_qk_norm_rotary_t& a, const as_rotation_t& r, int sms,
   return s;
 }
 
-template <typename T, int NORM>
-cudaError_t launch_turn(const TurnParams& p, const Shape& s, int sms, cudaStream_t st) {
-  if (!s.vec) return as_launch_dependent(turn_elements_kernel<T, NORM, false>, dim3((unsigned)std::min<long long>(s.ctas, 8ll * sms)), dim3(THREADS), 0, st, p);
+template <typename T, int NORM, int E>
+cudaError_t launch_lanes(const TurnParams& p, const Shape& s, int sms, cudaStream_t st) {
   const dim3 grid((unsigned)std::min<long long>(s.ctas, std::max(1, 2 * sms / p.chunks)), (unsigned)p.chunks), block(THREADS);        // CTAs go on from row to row
-  const size_t smem = WARPS * (s.NV * 1024 * sizeof(T) + (size_t)p.pairs * 8) + s.kept;
+  const size_t smem = WARPS * (s.NV * (E * 64) * sizeof(T) + (size_t)p.room) + s.kept;
   auto launch = [&](auto kernel) {
     if (smem > 40 * 1024)                                // (48 KB are there without asking)
       if (const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); e != cudaSuccess) return e;
@@ -1005,32 +1035,41 @@ cudaError_t launch_turn(const TurnParams& p, const Shape& s, int sms, cudaStream
   };
   auto run = [&](auto interleaved, auto half) { return p.half ? launch(half) : launch(interleaved); };
   switch (s.NV) {
-    case 1: return run(turn_kernel<T, NORM, 1, false>, turn_kernel<T, NORM, 1, true>);
-    case 2: return run(turn_kernel<T, NORM, 2, false>, turn_kernel<T, NORM, 2, true>);
-    default: return run(turn_kernel<T, NORM, 3, false>, turn_kernel<T, NORM, 3, true>);
+    case 1: return run(turn_kernel<T, NORM, 1, false, E>, turn_kernel<T, NORM, 1, true, E>);
+    case 2: return run(turn_kernel<T, NORM, 2, false, E>, turn_kernel<T, NORM, 2, true, E>);
+    default: return run(turn_kernel<T, NORM, 3, false, E>, turn_kernel<T, NORM, 3, true, E>);
   }
+}
+template <typename T, int NORM>
+cudaError_t launch_turn(const TurnParams& p, const Shape& s, int sms, cudaStream_t st) {
+  if (!s.vec) return as_launch_dependent(turn_elements_kernel<T, NORM, false>, dim3((unsigned)std::min<long long>(s.ctas, 8ll * sms)), dim3(THREADS), 0, st, p);
+  return s.E == 16 ? launch_lanes<T, NORM, 16>(p, s, sms, st) : launch_lanes<T, NORM, 8>(p, s, sms, st);
 }
 template <typename T>
 cudaError_t launch_norm(const TurnParams& p, const Shape& s, int norm, int sms, cudaStream_t st) {
   return norm == AS_NORM_NONE ? launch_turn<T, AS_NORM_NONE>(p, s, sms, st) : norm == AS_NORM_HEAD ? launch_turn<T, AS_NORM_HEAD>(p, s, sms, st) : launch_turn<T, AS_NORM_ROW>(p, s, sms, st);
 }
 
-template <typename T, int NORM>
-cudaError_t launch_back(const TurnParams& p, const Shape& s, unsigned ctas, cudaStream_t st) {
-  const dim3 grid(ctas, (unsigned)p.n_t), block(THREADS);
-  const int heads = std::max(p.t[0].heads, p.t[1].heads);
-  const size_t sums = NORM == AS_NORM_ROW ? s.NV : 1;
-  const size_t smem = s.vec ? WARPS * (sums * 2048 + s.NV * 1024 * sizeof(T) + (size_t)p.pairs * 8) + s.kept : (size_t)(NORM == AS_NORM_ROW ? heads : WARPS) * p.d * 4;
+template <typename T, int NORM, int E>
+cudaError_t launch_back_lanes(const TurnParams& p, const Shape& s, unsigned ctas, cudaStream_t st) {
+  const size_t sums = NORM == AS_NORM_ROW ? s.NV : 1, smem = WARPS * (sums * (E * 128) + s.NV * (E * 64) * sizeof(T) + (size_t)p.room) + s.kept;
   auto run = [&](auto kernel) {
-    if (smem > 40 * 1024)                                // (beside what the kernels have of a fixed size, 48 KB are there without asking)
+    if (smem > 40 * 1024)
       if (const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); e != cudaSuccess) return e;
-    return as_launch_dependent(kernel, grid, block, smem, st, p);
+    return as_launch_dependent(kernel, dim3(ctas, (unsigned)p.n_t), dim3(THREADS), smem, st, p);
   };
-  if (!s.vec) return run(turn_elements_kernel<T, NORM, true>);
   auto choose = [&](auto interleaved, auto half) { return p.half ? run(half) : run(interleaved); };
   if constexpr (sizeof(T) == 2)
-    if (s.NV == 3) return choose(turn_back_kernel<T, NORM, 3, false>, turn_back_kernel<T, NORM, 3, true>);
-  return s.NV == 2 ? choose(turn_back_kernel<T, NORM, 2, false>, turn_back_kernel<T, NORM, 2, true>) : choose(turn_back_kernel<T, NORM, 1, false>, turn_back_kernel<T, NORM, 1, true>);
+    if (s.NV == 3) return choose(turn_back_kernel<T, NORM, 3, false, E>, turn_back_kernel<T, NORM, 3, true, E>);
+  return s.NV == 2 ? choose(turn_back_kernel<T, NORM, 2, false, E>, turn_back_kernel<T, NORM, 2, true, E>) : choose(turn_back_kernel<T, NORM, 1, false, E>, turn_back_kernel<T, NORM, 1, true, E>);
+}
+template <typename T, int NORM>
+cudaError_t launch_back(const TurnParams& p, const Shape& s, unsigned ctas, cudaStream_t st) {
+  if (s.vec) return s.E == 16 ? launch_back_lanes<T, NORM, 16>(p, s, ctas, st) : launch_back_lanes<T, NORM, 8>(p, s, ctas, st);
+  const size_t smem = (size_t)(NORM == AS_NORM_ROW ? std::max(p.t[0].heads, p.t[1].heads) : WARPS) * p.d * 4;
+  if (smem > 40 * 1024)
+    if (const cudaError_t e = cudaFuncSetAttribute(turn_elements_kernel<T, NORM, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); e != cudaSuccess) return e;
+  return as_launch_dependent(turn_elements_kernel<T, NORM, true>, dim3(ctas, (unsigned)p.n_t), dim3(THREADS), smem, st, p);
 }
 
 // CTAs of the backward pass, for each tensor: as many as the device holds at once (of vectors: a multiple of the chunks, which they take in turn).

@@ -51,7 +51,7 @@ def test_table_of_one_choice_for_each_axis(ops):
 
 # ------------------------------------------------------------------------------------------------ rotation
 SHAPES = [(1, 1, 1, 2), (1, 2, 33, 64), (2, 12, 50, 128), (3, 5, 7, 40), (2, 3, 31, 8), (1, 9, 20, 17), (2, 4, 9, 96), (1, 3, 70, 256), (1, 2, 5, 512), (1, 1, 3, 1000), (1, 40, 300, 80),
-          (4, 6, 1, 128), (1, 1, 2000, 64), (1, 7, 3, 1024)]
+          (4, 6, 1, 128), (1, 1, 2000, 64), (1, 7, 3, 1024), (1, 5, 9, 144), (2, 3, 11, 176), (1, 3, 40, 24), (2, 9, 30, 72), (1, 2, 7, 272), (1, 3, 300, 384), (1, 4, 5, 248)]
 
 
 @pytest.mark.parametrize("layout", ["interleaved", "half"])
@@ -148,7 +148,7 @@ def test_turned_and_turned_back(ops):
 
 # ------------------------------------------------------------------------------------------------ norms
 QK = [(1, 1, 1, 1, 2), (1, 12, 12, 5, 128), (2, 12, 3, 50, 128), (3, 5, 2, 7, 40), (1, 24, 24, 19, 64), (1, 9, 9, 20, 17), (2, 4, 1, 9, 96), (1, 3, 3, 30, 256), (1, 2, 2, 5, 512),
-      (1, 64, 8, 11, 128), (1, 128, 128, 3, 128), (1, 1, 1, 700, 1000), (4, 6, 6, 1, 128), (1, 12, 12, 700, 128), (1, 1, 7, 33, 80)]
+      (1, 64, 8, 11, 128), (1, 128, 128, 3, 128), (1, 1, 1, 700, 1000), (4, 6, 6, 1, 128), (1, 12, 12, 700, 128), (1, 1, 7, 33, 80), (1, 5, 2, 9, 144), (2, 3, 3, 11, 176), (1, 9, 9, 40, 24), (2, 12, 4, 300, 72), (1, 30, 30, 9, 248), (1, 2, 1, 30, 384)]
 
 
 @pytest.mark.parametrize("norm", ["head", "row"])
