@@ -418,13 +418,13 @@ AS_DEV void leave_rows(const Target& to, const Target& res, bool vec, uint32_t s
 #pragma unroll
   for (int i = 0; i < 4; ++i) put16(strip, lane, i, __float_as_uint(x[4 * i]), __float_as_uint(x[4 * i + 1]), __float_as_uint(x[4 * i + 2]), __float_as_uint(x[4 * i + 3]));
   __syncwarp();
-  if (n < N) {
+  if (vec && n < N) {
     auto value = [&](int i) {
       uint32_t w[4];
       get16(strip, i * 8 + row, lane & 3, w);
       return make_float4(__uint_as_float(w[0]), __uint_as_float(w[1]), __uint_as_float(w[2]), __uint_as_float(w[3]));
     };
-    if (vec) {
+    {
       const long long oc = to.m.col((unsigned)n), rc = adds ? res.m.col((unsigned)n) : 0;
       float4 r[4];
       if (adds) {
@@ -437,18 +437,21 @@ AS_DEV void leave_rows(const Target& to, const Target& res, bool vec, uint32_t s
         if (adds) { v.x += r[i].x; v.y += r[i].y; v.z += r[i].z; v.w += r[i].w; }
         if (i * 8 + row < rows) st4(to.m.data, to.f32, to.m.row((unsigned)(m0 + i * 8 + row)) + oc, v);
       }
-    } else {
-#pragma unroll 1
-      for (int i = 0; i < 4; ++i) {
-        if (i * 8 + row >= rows) break;
-        const unsigned m = (unsigned)(m0 + i * 8 + row);
-        const float4 v = value(i);
-        const float f[4] = {v.x, v.y, v.z, v.w};
-        const long long ro = to.m.row(m), rr = adds ? res.m.row(m) : 0;
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (n + k < N) st1(to.m.data, to.f32, ro + to.m.col((unsigned)(n + k)), adds ? f[k] + ld1(res.m.data, res.f32, rr + res.m.col((unsigned)(n + k))) : f[k]);
-      }
+    }
+  }
+  if (!vec) {                                 // element by element, so that 16 lanes move a row's run
+    const int c = lane & 15, col = n0 + c;
+    const bool in = col < N;
+    const long long oc = in ? to.m.col((unsigned)col) : 0, rc = in && adds ? res.m.col((unsigned)col) : 0;
+#pragma unroll 4
+    for (int i = 0; i < 16; ++i) {
+      const int r = 2 * i + lane / 16;
+      float v;
+      asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(strip + swz64(r, c / 4) + (uint32_t)(c % 4) * 4u) : "memory");
+      if (!in || r >= rows) continue;
+      const unsigned m = (unsigned)(m0 + r);
+      if (adds) v += ld1(res.m.data, res.f32, res.m.row(m) + rc);
+      st1(to.m.data, to.f32, to.m.row(m) + oc, v);
     }
   }
   __syncwarp();
@@ -895,9 +898,10 @@ struct DzParams {
   const void* gate;
   bf* dz;                                    // [M][pitch], or nullptr
   float *part_b, *part_g;                    // [gates * runs][N], or nullptr
+  void *dbias, *dgate;                       // where there is one run in all: the sums themselves (bias_f32: dbias's type)
   long long gate_stride, pitch;
   int N, act, rows_gate, runs;               // rows that share a gate; runs of them
-  bool gate_f32, vec;
+  bool gate_f32, bias_f32, vec;
 };
 constexpr int DZ_COLS = 256;
 AS_DEV void unpack8(const uint4& w, float (&f)[8]) {
@@ -979,8 +983,8 @@ __global__ void __launch_bounds__(256, 3) dz_kernel(const __grid_constant__ DzPa
       take(m, d, z);
     }
   }
-  auto leave = [&](const float (&s)[8], float* part) {
-    if (part == nullptr) return;
+  auto leave = [&](const float (&s)[8], float* part, void* sum, bool f32) {
+    if (part == nullptr && sum == nullptr) return;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 8; ++i) room[warp][lane * 8 + i] = s[i];
@@ -990,17 +994,18 @@ __global__ void __launch_bounds__(256, 3) dz_kernel(const __grid_constant__ DzPa
       float f = 0.f;
 #pragma unroll
       for (int w = 0; w < 8; ++w) f += room[w][threadIdx.x];
-      part[(long long)blockIdx.y * p.N + c] = f;
+      if (sum != nullptr) st1(sum, f32, c, f);
+      else part[(long long)blockIdx.y * p.N + c] = f;
     }
   };
-  leave(sb, p.part_b);
-  if constexpr (OF_GATE) leave(sg, p.part_g);
+  leave(sb, p.part_b, p.dbias, p.bias_f32);
+  if constexpr (OF_GATE) leave(sg, p.part_g, p.dgate, p.gate_f32);
 }
 template <typename Y>
 cudaError_t launch_dz(const DzParams& p, dim3 grid, cudaStream_t st) {
   auto run = [&](auto act) {
     constexpr int ACT = decltype(act)::value;
-    return p.part_g != nullptr ? as_launch_dependent(dz_kernel<ACT, Y, true>, grid, dim3(256), 0, st, p) : as_launch_dependent(dz_kernel<ACT, Y, false>, grid, dim3(256), 0, st, p);
+    return p.part_g != nullptr || p.dgate != nullptr ? as_launch_dependent(dz_kernel<ACT, Y, true>, grid, dim3(256), 0, st, p) : as_launch_dependent(dz_kernel<ACT, Y, false>, grid, dim3(256), 0, st, p);
   };
   switch (p.act) {
     case AS_ACT_RELU: return run(std::integral_constant<int, AS_ACT_RELU>{});
@@ -1042,8 +1047,10 @@ __global__ void __launch_bounds__(256) column_sum_kernel(const __grid_constant__
 // A matrix into rows a multiple of 16 bytes apart, for operands that the copies cannot read as they lie: 8 elements a thread, from two aligned pieces of 16 bytes where both lie within the row, else
 // element by element.  (Element by element throughout 2000 x 1535 took 8 us.)
 struct GatherParams { Rows x; bf* out; long long pitch; unsigned rows, across; int cols, run; };       // across: pieces of 8 columns; run: columns that lie in a run
-__global__ void __launch_bounds__(256) gather_kernel(const __grid_constant__ GatherParams p) {
+struct Gathers { GatherParams of[2]; };      // of one operand or two, at once
+__global__ void __launch_bounds__(256) gather_kernel(const __grid_constant__ Gathers g) {
   griddep_launch();
+  const GatherParams& p = blockIdx.y == 0 ? g.of[0] : g.of[1];
   griddep_wait();
   const long long pieces = (long long)p.rows * p.across;
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < pieces; i += (long long)gridDim.x * 256) {
@@ -1144,17 +1151,24 @@ Operand operand_of(const as_rows_t& x, long long rows, long long cols) {
 }
 uint64_t copy_bytes(const Operand& o, long long rows) { return o.copy ? up256((uint64_t)rows * (uint64_t)o.rows.stride_token * 2) : 0; }
 
-cudaError_t run_copy(Operand& o, long long rows, long long cols, uint8_t*& room, int sms, cudaStream_t st) {
-  if (!o.copy) return cudaSuccess;
-  o.rows.data = room;
-  GatherParams g{};
-  g.x = rows_of(o.from, rows, cols);
-  g.out = reinterpret_cast<bf*>(room); g.pitch = o.rows.stride_token;
-  g.rows = (unsigned)rows; g.across = (unsigned)((cols + 7) / 8); g.cols = (int)cols;
-  g.run = g.x.split ? o.from.head_dim : (int)cols;
-  room += copy_bytes(o, rows);
-  const long long ctas = (rows * (long long)g.across + 255) / 256;
-  return as_launch_dependent(gather_kernel, dim3((unsigned)std::min<long long>(ctas, 16ll * sms)), dim3(256), 0, st, g);
+// Brings operands that need it into the workspace, in one launch.
+struct Copy { Operand* o; long long rows, cols; };
+cudaError_t run_copies(const Copy (&c)[2], uint8_t*& room, int sms, cudaStream_t st) {
+  Gathers g{};
+  int n = 0;
+  long long ctas = 0;
+  for (const Copy& i : c) {
+    if (!i.o->copy) continue;
+    GatherParams& p = g.of[n++];
+    i.o->rows.data = room;
+    p.x = rows_of(i.o->from, i.rows, i.cols);
+    p.out = reinterpret_cast<bf*>(room); p.pitch = i.o->rows.stride_token;
+    p.rows = (unsigned)i.rows; p.across = (unsigned)((i.cols + 7) / 8); p.cols = (int)i.cols;
+    p.run = p.x.split ? i.o->from.head_dim : (int)i.cols;
+    room += copy_bytes(*i.o, i.rows);
+    ctas = std::max(ctas, (i.rows * (long long)p.across + 255) / 256);
+  }
+  return n == 0 ? cudaSuccess : as_launch_dependent(gather_kernel, dim3((unsigned)std::min<long long>(ctas, 16ll * sms), (unsigned)n), dim3(256), 0, st, g);
 }
 
 // One product on the tensor cores.  a [M, K] and b [N, K] by their meaning; A_MN, B_MN: they lie with M (N) in a run, as [K rows, M columns].
@@ -1313,7 +1327,8 @@ extern "C" as_status_t as_linear(as_fp8_context_t h, const as_linear_t* a, void*
   if (!workspace_ok(a->workspace, a->workspace_bytes, l.bytes)) return AS_ERR_WORKSPACE;
   const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   uint8_t* room = static_cast<uint8_t*>(a->workspace);
-  if (run_copy(l.x, a->rows, a->cols, room, h->sms, st) != cudaSuccess || run_copy(l.w, a->out_cols, a->cols, room, h->sms, st) != cudaSuccess) return failed();
+  const Copy copies[2] = {{&l.x, a->rows, a->cols}, {&l.w, a->out_cols, a->cols}};
+  if (run_copies(copies, room, h->sms, st) != cudaSuccess) return failed();
   Epilogue e{};
   e.out = rows_of(a->out, a->rows, a->out_cols);
   if (a->residual.data != nullptr) e.res = rows_of(a->residual, a->rows, a->out_cols);
@@ -1346,7 +1361,7 @@ namespace {
 
 struct BackPlan {
   Operand x, w, dy;
-  bool dz, sums;                             // dz is computed (else dy is the operand as it lies); sums are taken
+  bool dz, sums, direct;                     // dz is computed (else dy is the operand as it lies); sums are taken, in one step
   long long pitch;
   int runs;
   Product dx, dw;
@@ -1382,10 +1397,12 @@ BackPlan plan_back(as_fp8_context_t h, const as_linear_backward_t& a) {
   b.dz = (dx || dw) && (a.activation != AS_ACT_NONE || a.gate != nullptr || b.dy.copy || (dw && b.dy.rows.tokens != a.rows && b.x.rows.tokens != b.dy.rows.tokens));
   b.pitch = pitch_of(a.out_cols);
   const long long gates = a.gate != nullptr ? a.gates : 1, across = (a.out_cols + DZ_COLS - 1) / DZ_COLS, rows_gate = a.rows / gates;
-  b.runs = (int)std::max<long long>(1, std::min<long long>((8ll * h->sms + across * gates - 1) / (across * gates), rows_gate / 16));
+  // a run for every 16 rows as far as that fills the SMs; up to 64 rows are one, which needs no second step
+  b.runs = rows_gate <= 64 && gates == 1 ? 1 : (int)std::max<long long>(1, std::min<long long>((8ll * h->sms + across * gates - 1) / (across * gates), rows_gate / 16));
   if (b.dz) b.bytes += up256((uint64_t)a.rows * (uint64_t)b.pitch * 2);
-  if (a.dbias != nullptr) b.bytes += up256((uint64_t)gates * b.runs * a.out_cols * 4);
-  if (a.dgate != nullptr) b.bytes += up256((uint64_t)gates * b.runs * a.out_cols * 4);
+  b.direct = gates * b.runs == 1;
+  if (a.dbias != nullptr && !b.direct) b.bytes += up256((uint64_t)gates * b.runs * a.out_cols * 4);
+  if (a.dgate != nullptr && !b.direct) b.bytes += up256((uint64_t)gates * b.runs * a.out_cols * 4);
   b.bytes += copy_bytes(b.x, a.rows) + copy_bytes(b.w, a.out_cols);
   const as_rows_t dz = b.dz ? plain_rows(nullptr, a.rows, a.out_cols, b.pitch) : b.dy.rows;
   uint64_t parts = 0;
@@ -1443,18 +1460,24 @@ extern "C" as_status_t as_linear_backward(as_fp8_context_t h, const as_linear_ba
   z.vec = a->out_cols % 8 == 0 && a->dy.head_dim % 8 == 0 && rows_vec16(a->dy) && (a->pre.data == nullptr || rows_vec(a->pre, 16));
   if (b.dz) { z.dz = reinterpret_cast<bf*>(room); room += up256((uint64_t)a->rows * (uint64_t)b.pitch * 2); }
   const uint64_t sum_bytes = up256((uint64_t)gates * b.runs * a->out_cols * 4);
-  if (a->dbias != nullptr) { z.part_b = reinterpret_cast<float*>(room); room += sum_bytes; }
-  if (a->dgate != nullptr) { z.part_g = reinterpret_cast<float*>(room); room += sum_bytes; }
+  if (b.direct) {
+    z.dbias = a->dbias; z.bias_f32 = a->bias_dtype == AS_DTYPE_F32;
+    z.dgate = a->dgate;
+  } else {
+    if (a->dbias != nullptr) { z.part_b = reinterpret_cast<float*>(room); room += sum_bytes; }
+    if (a->dgate != nullptr) { z.part_g = reinterpret_cast<float*>(room); room += sum_bytes; }
+  }
   if (gates * b.runs > 65535) return AS_ERR_UNSUPPORTED;
   if (b.dz || b.sums) {
     const dim3 grid((unsigned)((a->out_cols + DZ_COLS - 1) / DZ_COLS), (unsigned)(gates * b.runs));
     if ((a->dy.dtype == AS_DTYPE_F32 ? launch_dz<float>(z, grid, st) : launch_dz<bf>(z, grid, st)) != cudaSuccess) return failed();
   }
-  if (b.sums) {
+  if (b.sums && !b.direct) {
     ColumnSumParams c{z.part_b, z.part_g, a->dbias, a->dgate, z.N, b.runs, (int)gates, a->bias_dtype == AS_DTYPE_F32, z.gate_f32};
     if (as_launch_dependent(column_sum_kernel, dim3((unsigned)((z.N + 31) / 32), (unsigned)(1 + (a->dgate != nullptr ? gates : 0))), dim3(256), 0, st, c) != cudaSuccess) return failed();
   }
-  if (run_copy(b.x, a->rows, a->cols, room, h->sms, st) != cudaSuccess || run_copy(b.w, a->out_cols, a->cols, room, h->sms, st) != cudaSuccess) return failed();
+  const Copy copies[2] = {{&b.x, a->rows, a->cols}, {&b.w, a->out_cols, a->cols}};
+  if (run_copies(copies, room, h->sms, st) != cudaSuccess) return failed();
   const as_rows_t dz = b.dz ? plain_rows(z.dz, a->rows, a->out_cols, b.pitch) : b.dy.rows;
   Epilogue e{};
   e.N = (int)a->cols; e.act = AS_ACT_NONE;
