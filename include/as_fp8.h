@@ -103,7 +103,7 @@ AS_API as_status_t as_rms_norm(const as_rms_norm_t* args, void* cuda_stream);
 /* The 8-bit form of x. */
 AS_API as_status_t as_quantize_fp8(const as_quantize_fp8_t* args, void* cuda_stream);
 
-/* What as_matmul_fp8 keeps on a device: the status word of its bounded waits.  Create it on the device that the calls run on
+/* What the products (as_matmul_fp8, and as_layer.h's as_linear and as_linear_backward) keep on a device: the status word of their bounded waits.  Create it on the device that the calls run on
  * (AS_ERR_ARCH when that is not sm_100); calls that use one context may overlap. */
 typedef struct as_fp8_context_s* as_fp8_context_t;
 AS_API as_status_t as_fp8_create(as_fp8_context_t* out);

@@ -11,7 +11,7 @@
  *   as_linear_backward          the gradients of x, w, bias and gate
  *
  * Conventions as in as_fp8.h: device pointers, the caller's buffers and stream, nothing allocated, no synchronisation, calls can be
- * captured; on error nothing has been launched.  Sums are fp32 in an order that depends on sizes and layouts alone.
+ * captured; on error nothing has been launched.  Sums are fp32 in an order that depends on sizes, types and layouts alone: results are run-to-run identical.
  */
 #ifndef AS_LAYER_H_
 #define AS_LAYER_H_
@@ -119,8 +119,8 @@ typedef struct {
   const void* bias;         /* [N], or NULL */
   const void* gate;         /* [gates][N], gate_stride elements apart, or NULL; rows / gates rows in turn share one */
   int32_t bias_dtype, gate_dtype;
-  int64_t gates, gate_stride;
-  void* workspace;          /* 256-byte aligned, as_linear_workspace_bytes of it (which may be 0) */
+  int64_t gates, gate_stride;   /* gates: 1 .. 65534, a divisor of rows */
+  void* workspace;          /* 256-byte aligned, as_linear_workspace_bytes of it (which may be 0); calls in flight at once have one each */
   uint64_t workspace_bytes;
 } as_linear_t;
 AS_API as_status_t as_linear_workspace_bytes(as_fp8_context_t ctx, const as_linear_t* args, uint64_t* bytes);
