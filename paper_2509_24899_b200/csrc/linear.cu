@@ -186,6 +186,7 @@ struct GemmParams {
   int M, T, mt_entry;                       // rows of results in entries of T, of mt_entry tiles each
   int bn, nt, stages, parts;
   int ksteps, ks_entry;                     // steps of BK of the summed index, where it is rows: of an entry
+  unsigned long long by_nt, by_mt;          // 2^64 / nt and 2^64 / mt_entry, rounded up (0: 1): a quotient is the upper half of a product, exact below 2^32
   int a_hd, b_hd;                           // columns of a head of the operands, multiples of 64 (INT32_MAX: there are no heads)
 };
 
@@ -227,17 +228,23 @@ struct Ctx {
 };
 // A unit of work: a tile and a part of the summed index.
 struct Unit { int entry, t0, n0, k0, k1, part; };
+// (With 64-bit divisions here, in every warp and for every unit, tiles of one step took a tenth longer.)
+AS_DEV unsigned quotient(unsigned i, unsigned long long by) { return by == 0ull ? i : (unsigned)__umul64hi(by, i); }
 template <int CG>
 AS_DEV Unit unit_of(const GemmParams& p, long long u) {
-  Unit w;
-  const long long tile = u / p.parts;
-  w.part = (int)(u - tile * p.parts);
-  const int mt = (int)(tile / p.nt);
-  w.n0 = (int)(tile - (long long)mt * p.nt) * p.bn;
-  w.entry = mt / p.mt_entry;
-  w.t0 = (mt - w.entry * p.mt_entry) * (BM * CG);
-  w.k0 = (int)((long long)p.ksteps * w.part / p.parts);
-  w.k1 = (int)((long long)p.ksteps * (w.part + 1) / p.parts);
+  Unit w{};
+  unsigned tile = (unsigned)u;
+  w.k1 = p.ksteps;
+  if (p.parts > 1) {
+    tile = (unsigned)u / (unsigned)p.parts;
+    w.part = (int)((unsigned)u - tile * (unsigned)p.parts);
+    w.k0 = (int)((long long)p.ksteps * w.part / p.parts);
+    w.k1 = (int)((long long)p.ksteps * (w.part + 1) / p.parts);
+  }
+  const unsigned mt = quotient(tile, p.by_nt);
+  w.n0 = (int)(tile - mt * (unsigned)p.nt) * p.bn;
+  w.entry = (int)quotient(mt, p.by_mt);
+  w.t0 = (int)(mt - (unsigned)w.entry * (unsigned)p.mt_entry) * (BM * CG);
   return w;
 }
 
@@ -256,16 +263,16 @@ AS_DEV void lin_copies(const GemmParams& p, const Ctx<CG>& c, const CUtensorMap*
     int ax[A_BOXES], ah[A_BOXES], bx[B_BOXES], bh[B_BOXES];
     if constexpr (A_MN) {
 #pragma unroll
-      for (int i = 0; i < A_BOXES; ++i) { ah[i] = (m0 + 64 * i) / p.a_hd; ax[i] = m0 + 64 * i - ah[i] * p.a_hd; }
+      for (int i = 0; i < A_BOXES; ++i) { ah[i] = p.a_hd == INT32_MAX ? 0 : (m0 + 64 * i) / p.a_hd; ax[i] = m0 + 64 * i - ah[i] * p.a_hd; }
     } else {
-      ah[0] = w.k0 * BK / p.a_hd;
+      ah[0] = w.k0 == 0 ? 0 : w.k0 * BK / p.a_hd;
       ax[0] = w.k0 * BK - ah[0] * p.a_hd;
     }
     if constexpr (B_MN) {
 #pragma unroll
-      for (int i = 0; i < B_BOXES; ++i) { bh[i] = (n0 + 64 * i) / p.b_hd; bx[i] = n0 + 64 * i - bh[i] * p.b_hd; }
+      for (int i = 0; i < B_BOXES; ++i) { bh[i] = p.b_hd == INT32_MAX ? 0 : (n0 + 64 * i) / p.b_hd; bx[i] = n0 + 64 * i - bh[i] * p.b_hd; }
     }
-    int ke = A_MN ? w.k0 / p.ks_entry : 0, kt = A_MN ? w.k0 - ke * p.ks_entry : w.k0;      // entry and step of the summed index
+    int ke = A_MN && w.k0 != 0 ? w.k0 / p.ks_entry : 0, kt = A_MN ? w.k0 - ke * p.ks_entry : w.k0;      // entry and step of the summed index
     for (int k = w.k0; k < w.k1; ++k) {
       if (!c.wait(B_EMPTY + r.slot, r.turn ^ 1u)) goto out;
       const uint32_t at = c.sbase + STAGES_OFF + (uint32_t)r.slot * stage_bytes, bt = at + BM * BK * 2;
@@ -1196,6 +1203,9 @@ cudaError_t run_product(as_fp8_context_t h, const Product& q, const Epilogue& e,
   p.mt_entry = (p.T + BM * plan.cg - 1) / (BM * plan.cg);
   p.bn = plan.bn; p.parts = plan.parts;
   p.nt = (int)((q.N + plan.bn - 1) / plan.bn);
+  auto reciprocal = [](unsigned n) { return n == 1u ? 0ull : ~0ull / n + 1ull; };
+  p.by_nt = reciprocal((unsigned)p.nt);
+  p.by_mt = reciprocal((unsigned)p.mt_entry);
   p.ks_entry = (int)(q.a_mn ? (q.T + BK - 1) / BK : 1);
   p.ksteps = (int)(q.a_mn ? (q.K / q.T) * p.ks_entry : (q.K + BK - 1) / BK);
   p.units = (q.a_mn ? 1 : q.M / q.T) * p.mt_entry * (long long)p.nt * p.parts;
@@ -1249,6 +1259,8 @@ bool gate_ok(const void* gate, int dtype, long long gates, long long stride, lon
   if (gate == nullptr) return true;
   return vector_ok(gate, dtype) && gates >= 1 && gates <= 65534 && rows % gates == 0 && (gates == 1 || stride >= 0) && n >= 1;
 }
+// Units of work are counted in 32 bits: an entry's tile of 64 columns for each row at the worst.  (What a device holds has fewer.)
+bool units_fit(long long rows, long long cols) { return rows * ((cols + 63) / 64) < (1ll << 32); }
 bool heads_fit(const as_rows_t& x, long long cols) { return x.data == nullptr || x.head_dim == cols || cols * (long long)x.head_dim <= (1ll << 32); }
 
 as_status_t device_of(as_fp8_context_t h) {
@@ -1266,7 +1278,7 @@ as_status_t linear_ok(as_fp8_context_t h, const as_linear_t* a) {
   if (a->residual.data != nullptr && !rows_ok(a->residual, a->rows, a->out_cols)) return AS_ERR_INVALID_ARG;
   if (a->pre.data != nullptr && (!rows_ok(a->pre, a->rows, a->out_cols) || a->pre.dtype != AS_DTYPE_BF16 || !apart(a->pre, a->rows, a->out_cols))) return AS_ERR_INVALID_ARG;
   if (!vector_ok(a->bias, a->bias_dtype) || !gate_ok(a->gate, a->gate_dtype, a->gates, a->gate_stride, a->rows, a->out_cols)) return AS_ERR_INVALID_ARG;
-  if (!heads_fit(a->x, a->cols) || !heads_fit(a->out, a->out_cols) || !heads_fit(a->residual, a->out_cols) || !heads_fit(a->pre, a->out_cols)) return AS_ERR_UNSUPPORTED;
+  if (!units_fit(a->rows, a->out_cols) || !heads_fit(a->x, a->cols) || !heads_fit(a->out, a->out_cols) || !heads_fit(a->residual, a->out_cols) || !heads_fit(a->pre, a->out_cols)) return AS_ERR_UNSUPPORTED;
   return AS_OK;
 }
 
@@ -1382,7 +1394,7 @@ as_status_t back_ok(as_fp8_context_t h, const as_linear_backward_t* a) {
   if (!pre && (a->activation != AS_ACT_NONE || a->dgate != nullptr)) return AS_ERR_INVALID_ARG;
   if (!vector_ok(a->dbias, a->bias_dtype) || !vector_ok(a->dgate, a->gate_dtype) || (a->dgate != nullptr && a->gate == nullptr)) return AS_ERR_INVALID_ARG;
   if (!gate_ok(a->gate, a->gate_dtype, a->gates, a->gate_stride, a->rows, a->out_cols)) return AS_ERR_INVALID_ARG;
-  if (!heads_fit(a->dy, a->out_cols) || !heads_fit(a->pre, a->out_cols) || (dw && !heads_fit(a->x, a->cols)) || !heads_fit(a->dx, a->cols)) return AS_ERR_UNSUPPORTED;
+  if (!units_fit(a->rows, a->cols) || !units_fit(a->out_cols, a->cols) || !heads_fit(a->dy, a->out_cols) || !heads_fit(a->pre, a->out_cols) || (dw && !heads_fit(a->x, a->cols)) || !heads_fit(a->dx, a->cols)) return AS_ERR_UNSUPPORTED;
   return AS_OK;
 }
 

@@ -18,7 +18,8 @@ namespace as_lin {
 struct Plan { int cg, bn, parts; bool shared; double ns; };
 
 // By the time that the turns of all SMs take: turns x steps x ns a step, and what the reading out of the last turn and the meeting of a pair add.  What a step takes is its bytes into an SM, 64 a
-// clock, and beside them, from 256 x 256 on, its MMAs.  A part more costs its sums' way to the workspace and back, and a launch; a cluster costs the meeting and the sums, and more with every CTA beyond
+// clock, and beside them, from 256 x 256 on, its MMAs.  A tile's results take the warps 1.9 us (two strips of 32 columns each: 3.3), which a short sum does not hide: 6144 x 1280 from 3 rows takes 18 us in
+// tiles of 128 x 64 and 11 of 128 x 256.  A part more costs its sums' way to the workspace and back, and a launch; a cluster costs the meeting and the sums, and more with every CTA beyond
 // two, and holds as many tiles at once as the device has such clusters.  most_steps: that a cluster's CTA may add up by itself.
 inline Plan plan_of(long long entries, long long T, long long M, long long N, long long ksteps, bool b_mn, int most_steps, int sms, const int* clusters) {
   static const int ns[2][8] = {{230, 250, 265, 300, 345, 385, 440, 500}, {228, 230, 240, 262, 297, 320, 365, 410}};
@@ -33,8 +34,9 @@ inline Plan plan_of(long long entries, long long T, long long M, long long N, lo
         if (parts == 1 || tiles * parts <= 2 * units) {
           const long long all = tiles * parts, whole = (all + units - 1) / units;
           const double turns = whole == 1 ? 1. : 0.5 * ((double)all / units + whole);
-          double t = turns * (double)steps * ns[cg - 1][i] + 10. * bn + (cg == 2 ? 400. : 0.);
-          if (parts > 1) t += 3000. + (double)M * (double)N * 4. * (parts + 1) / 6000.;
+          const double step = (double)steps * ns[cg - 1][i];
+          double t = (turns - 1.) * std::max(step, bn <= 128 ? 1900. : 3300.) + step + 10. * bn + (cg == 2 ? 400. : 0.);
+          if (parts > 1) t += 3000. + 200. * parts + (double)M * (double)N * 4. * (parts + 1) / 6000.;
           if (t < best.ns) best = {cg, bn, parts, false, t};
         }
         if (cg == 1 && parts > 1 && parts <= MAX_PARTS && tiles <= clusters[parts] && steps <= most_steps) {
