@@ -66,7 +66,7 @@ enum { AS_NORM_NONE = 0, AS_NORM_HEAD = 1, AS_NORM_ROW = 2 };
 
 /* out = R (x * rsqrt(mean(x^2) + eps) * weight), the mean over a head (weight: [head_dim]) or over all heads of a token (weight: [heads * head_dim]).
  * Matrices are as_rows_t of `rows` tokens (rows / tokens entries) and heads * head_dim columns, head_dim the same in all of them, q and k of as many rows
- * and tokens; types bf16 or fp32, the same for all of a call.  out may be x itself in the same layout.  fp32 throughout, one rounding at the end.  Holds for every finite x,
+ * and tokens; types bf16 or fp32, the same for all of a call.  A result may be its own input itself in the same layout, and overlaps no other tensor.  fp32 throughout, one rounding at the end.  Holds for every finite x,
  * whatever its squares are in fp32; a head (row) of zeros with eps == 0 is NaN. */
 typedef struct {
   uint32_t struct_size;     /* sizeof(as_qk_norm_rotary_t) */
@@ -114,7 +114,7 @@ typedef struct {
   as_rows_t x;              /* [M, K] bf16 */
   as_rows_t w;              /* [N, K] bf16, rows (head_dim == cols) */
   as_rows_t residual;       /* [M, N] bf16 or fp32, or data == NULL */
-  as_rows_t out;            /* [M, N] bf16 or fp32; may be the residual itself */
+  as_rows_t out;            /* [M, N] bf16 or fp32; may be the residual itself in the same layout; out and pre overlap nothing else */
   as_rows_t pre;            /* [M, N] bf16, or data == NULL */
   const void* bias;         /* [N], or NULL */
   const void* gate;         /* [gates][N], gate_stride elements apart, or NULL; rows / gates rows in turn share one */

@@ -63,6 +63,13 @@ inline bool apart(const as_rows_t& x, long long rows, long long cols) {
   return true;
 }
 
+// Whether an output at an input's address is that input itself, element by element; elsewhere it is taken to lie apart from it.
+inline bool in_place_ok(const as_rows_t& out, const as_rows_t& in, long long rows, long long cols) {
+  if (out.data != in.data || out.data == nullptr || rows == 0) return true;
+  return out.dtype == in.dtype && out.head_dim == in.head_dim && out.tokens == in.tokens && (out.tokens == 1 || out.stride_token == in.stride_token) &&
+         (cols == out.head_dim || out.stride_head == in.stride_head) && (rows == out.tokens || out.stride_batch == in.stride_batch);
+}
+
 // Whether rows can move `bytes` at a time (16, 32), with 8 or 16 bf16 columns: address, strides and heads are multiples of as much.
 inline bool rows_vec(const as_rows_t& x, int bytes) {
   return aligned(x.data, bytes) && ((x.head_dim | x.stride_batch | x.stride_head | x.stride_token) & (bytes / 2 - 1)) == 0;

@@ -1277,6 +1277,11 @@ as_status_t linear_ok(as_fp8_context_t h, const as_linear_t* a) {
   if (!rows_ok(a->out, a->rows, a->out_cols) || !apart(a->out, a->rows, a->out_cols)) return AS_ERR_INVALID_ARG;
   if (a->residual.data != nullptr && !rows_ok(a->residual, a->rows, a->out_cols)) return AS_ERR_INVALID_ARG;
   if (a->pre.data != nullptr && (!rows_ok(a->pre, a->rows, a->out_cols) || a->pre.dtype != AS_DTYPE_BF16 || !apart(a->pre, a->rows, a->out_cols))) return AS_ERR_INVALID_ARG;
+  if (a->rows > 0) {                         // results over the residual itself only
+    const void *out = a->out.data, *pre = a->pre.data;
+    if (out == a->x.data || out == a->w.data || out == pre || !in_place_ok(a->out, a->residual, a->rows, a->out_cols)) return AS_ERR_INVALID_ARG;
+    if (pre != nullptr && (pre == a->x.data || pre == a->w.data || pre == a->residual.data)) return AS_ERR_INVALID_ARG;
+  }
   if (!vector_ok(a->bias, a->bias_dtype) || !gate_ok(a->gate, a->gate_dtype, a->gates, a->gate_stride, a->rows, a->out_cols)) return AS_ERR_INVALID_ARG;
   if (!units_fit(a->rows, a->out_cols) || !heads_fit(a->x, a->cols) || !heads_fit(a->out, a->out_cols) || !heads_fit(a->residual, a->out_cols) || !heads_fit(a->pre, a->out_cols)) return AS_ERR_UNSUPPORTED;
   return AS_OK;
@@ -1389,6 +1394,16 @@ as_status_t back_ok(as_fp8_context_t h, const as_linear_backward_t* a) {
   if (dw && (!rows_ok(a->x, a->rows, a->cols) || a->x.dtype != AS_DTYPE_BF16)) return AS_ERR_INVALID_ARG;
   if (dw && (!rows_ok(a->dw, a->out_cols, a->cols) || a->dw.dtype != AS_DTYPE_BF16 || a->dw.head_dim != a->cols || a->dw.tokens != a->out_cols || !apart(a->dw, a->out_cols, a->cols)))
     return AS_ERR_INVALID_ARG;
+  if (a->rows > 0) {                         // results over none of the inputs, nor over each other
+    const void* to[] = {a->dx.data, a->dw.data, a->dbias, a->dgate};
+    for (int i = 0; i < 4; ++i) {
+      if (to[i] == nullptr) continue;
+      for (const void* in : {(const void*)a->dy.data, (const void*)a->x.data, (const void*)a->w.data, (const void*)a->pre.data, a->gate})
+        if (to[i] == in) return AS_ERR_INVALID_ARG;
+      for (int j = 0; j < i; ++j)
+        if (to[i] == to[j]) return AS_ERR_INVALID_ARG;
+    }
+  }
   const bool pre = a->pre.data != nullptr;
   if (pre && (!rows_ok(a->pre, a->rows, a->out_cols) || a->pre.dtype != AS_DTYPE_BF16)) return AS_ERR_INVALID_ARG;
   if (!pre && (a->activation != AS_ACT_NONE || a->dgate != nullptr)) return AS_ERR_INVALID_ARG;

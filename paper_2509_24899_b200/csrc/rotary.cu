@@ -946,6 +946,10 @@ as_status_t turn_ok(const as_qk_norm_rotary_t* a, bool back) {
     const int size = a->weight_dtype == AS_DTYPE_BF16 ? 2 : 4;
     if (!aligned(a->q_weight, size) || !aligned(a->k_weight, size)) return AS_ERR_INVALID_ARG;
   }
+  if (!back && a->rows > 0) {                // results over their own inputs only
+    if (!in_place_ok(a->q_out, a->q, a->rows, (long long)a->q_heads * a->head_dim) || (two && !in_place_ok(a->k_out, a->k, a->rows, (long long)a->k_heads * a->head_dim))) return AS_ERR_INVALID_ARG;
+    if (two && (a->q_out.data == a->k.data || a->k_out.data == a->q.data || a->q_out.data == a->k_out.data)) return AS_ERR_INVALID_ARG;
+  }
   int pairs;
   if (const as_status_t s = rotation_ok(a->rotation, a->rows > 0 ? a->q.tokens : 0, a->head_dim, &pairs); s != AS_OK) return s;
   if (a->norm == AS_NORM_ROW && (long long)std::max(a->q_heads, two ? a->k_heads : 0) * a->head_dim > 16384) return AS_ERR_UNSUPPORTED;
@@ -1095,6 +1099,13 @@ as_status_t back_ok(const as_qk_norm_rotary_backward_t* b) {
   const bool two = a.k.data != nullptr;
   if (!heads_ok(b->dq, a, a.q_heads, false) || !heads_ok(b->dq_out, a, a.q_heads, true)) return AS_ERR_INVALID_ARG;
   if (two != (b->dk.data != nullptr) || two != (b->dk_out.data != nullptr) || (two && (!heads_ok(b->dk, a, a.k_heads, false) || !heads_ok(b->dk_out, a, a.k_heads, true)))) return AS_ERR_INVALID_ARG;
+  if (a.rows > 0) {
+    const long long cols[2] = {(long long)a.q_heads * a.head_dim, (long long)a.k_heads * a.head_dim};
+    if (!in_place_ok(b->dq_out, b->dq, a.rows, cols[0]) || !in_place_ok(b->dq_out, a.q, a.rows, cols[0])) return AS_ERR_INVALID_ARG;
+    if (two && (!in_place_ok(b->dk_out, b->dk, a.rows, cols[1]) || !in_place_ok(b->dk_out, a.k, a.rows, cols[1]))) return AS_ERR_INVALID_ARG;
+    const void *q_out = b->dq_out.data, *k_out = b->dk_out.data;
+    if (two && (q_out == k_out || q_out == b->dk.data || q_out == a.k.data || k_out == b->dq.data || k_out == a.q.data)) return AS_ERR_INVALID_ARG;
+  }
   const int size = a.weight_dtype == AS_DTYPE_BF16 ? 2 : 4;
   if ((b->dq_weight != nullptr && (a.q_weight == nullptr || !aligned(b->dq_weight, size))) || (b->dk_weight != nullptr && (!two || a.k_weight == nullptr || !aligned(b->dk_weight, size))))
     return AS_ERR_INVALID_ARG;

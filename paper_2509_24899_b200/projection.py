@@ -35,7 +35,7 @@ def linear(x, w, bias=None, activation=None, gate=None, residual=None, out=None,
     bias        [N]; gate: [N], or [entries, N] where each entry's rows (M / entries in turn) have their own; bf16 or fp32
     activation  None, "relu", "silu", "gelu" (by the error function) or "gelu_tanh"
     residual    [M, N] or heads, bf16 or fp32
-    out         where the result goes, bf16 or fp32, rows or heads; may be `residual` itself.  None: a new tensor in the residual's shape and type, else bf16 [M, N]
+    out         where the result goes, bf16 or fp32, rows or heads; may be `residual` itself, and overlaps nothing else.  None: a new tensor in the residual's shape and type, else bf16 [M, N]
     keep_pre    True, or a bf16 tensor to put it in: x w^T + bias as well, rounded to bf16, for `linear_backward`
 
     Returns the result, or (result, pre).  The first call on a device sets the device's context up (it allocates 256 bytes and synchronises): make it outside of a stream capture.  A

@@ -5,7 +5,7 @@
     y = rotary(x, table, layout="half", positions=positions)             # single tokens at positions of their own
 
 Tensors are [B, H, N, d] in bf16 or fp32 with any strides whose innermost one is 1; where sizes, strides and addresses are multiples of 16 bytes (and the pairs of 8), rows move
-faster.  Outputs are new tensors in [B, H, N, d] order unless they are given; one may be its input itself.  Tensors that require gradients are refused unless gradients are off or they are
+faster.  Outputs are new tensors in [B, H, N, d] order unless they are given; one may be its input itself, and overlaps no other tensor.  Tensors that require gradients are refused unless gradients are off or they are
 detached: a program that trains calls the `_backward` functions.
 """
 from __future__ import annotations

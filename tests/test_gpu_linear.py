@@ -297,3 +297,17 @@ def test_refusals(ops):
     version = r._version
     ops.linear(x, w, out=r)
     assert r._version > version
+
+
+def test_refuses_results_over_other_tensors(ops):
+    """A result at an input's address, but for the residual's own."""
+    x, w, r = randn(32, 32), weights(32, 32), randn(32, 32)
+    r4 = randn(2, 4, 4, 32)
+    for f in (lambda: ops.linear(x, w, out=x), lambda: ops.linear(x, w, out=w), lambda: ops.linear(x, w, out=r, keep_pre=r), lambda: ops.linear(x, w, keep_pre=x), lambda: ops.linear(x, w, residual=r, keep_pre=r),
+              lambda: ops.linear(x, w, residual=r, out=r.view(1, 4, 32, 8)),
+              lambda: ops.linear(randn(8, 32), weights(128, 32), residual=r4, out=r4.view(8, 128))):
+        with pytest.raises(ops.AsError):
+            f()
+    want = ops.linear(x, w, residual=r)
+    ops.linear(x, w, residual=r, out=r)
+    assert torch.equal(r, want)

@@ -336,3 +336,18 @@ def test_refusals(ops):
     assert out._version > version
     with torch.no_grad():
         ops.rotary(q.clone().requires_grad_(), table)
+
+
+def test_refuses_results_over_other_tensors(ops):
+    """A result at an input's address, but for its own input's in the same layout."""
+    q, k, w, table = randn(1, 2, 2, 64), randn(1, 2, 2, 64, seed=1), randn(64, seed=2), plain_table((2,), (32,))
+    crossed = q.transpose(1, 2)                          # [1, 2, 2, 64] again, tokens and heads exchanged
+    for f in (lambda: ops.rotary(q, table, out=crossed), lambda: ops.qk_norm_rotary(q, k, w, w, table, q_out=k), lambda: ops.qk_norm_rotary(q, k, w, w, table, k_out=q),
+              lambda: ops.qk_norm_rotary(q, q, w, w, table, q_out=q), lambda: ops.qk_norm_rotary(q, k, w, w, table, q_out=torch.empty_like(q), k_out=k.transpose(1, 2)),
+              lambda: ops.qk_norm_rotary_backward(q, k, q.clone(), k.clone(), w, w, table, dq_out=k), lambda: ops.qk_norm_rotary_backward(q, k, q.clone(), k.clone(), w, w, table, dk_out=q),
+              lambda: ops.qk_norm_rotary_backward(q, k, q.clone(), k.clone(), w, w, table, dq_out=crossed)):
+        with pytest.raises(ops.AsError):
+            f()
+    want = ops.qk_norm_rotary(q, k, w, w, table)
+    ops.qk_norm_rotary(q, k, w, w, table, q_out=q, k_out=k)
+    assert torch.equal(q, want[0]) and torch.equal(k, want[1])
