@@ -251,6 +251,32 @@ def test_nothing_to_do(ops):
     assert got.x.shape == (0, 64) and not bool(got.w.any()) and not bool(got.bias.any())
 
 
+def test_offsets_past_32_bits(ops):
+    """Results, their gradients and weights of 2^32 elements and more: the rows at the end, of which gradients are the only ones that are not 0."""
+    m, n, k = (1 << 22) + 130, 1032, 72
+    last = slice(m - 130, m)
+    x, w, b = randn(m, k), weights(n, k), randn(n, seed=3)
+    y, z = ops.linear(x, w, bias=b, activation="silu", keep_pre=True)
+    R.check_linear(y[last], x[last], w, b, "silu", pre=z[last])
+    del z
+    dy = y.zero_()
+    dy[last] = randn(130, n, seed=4)
+    pre = torch.zeros(m, n, dtype=BF16, device="cuda")
+    pre[last] = randn(130, n, seed=5)
+    got = ops.linear_backward(dy, x, w, pre=pre, activation="silu", bias=b)
+    assert not bool(got.x[:-130].any())
+    R.check_linear_backward(ops.LinearGradients(got.x[last], got.w, got.bias, None), dy[last], x[last], w, pre[last], "silu", None, b)
+    del x, y, dy, pre, got
+    n, k = 1 << 20, 4104
+    w = torch.zeros(n, k, dtype=BF16, device="cuda")
+    w[-40:] = weights(40, k)
+    for rows in (2, 300):
+        x = randn(rows, k, seed=rows)
+        y = ops.linear(x, w)
+        assert not bool(y[:, :-40].any())
+        R.check_linear(y[:, -40:], x, w[-40:])
+
+
 def test_streams_and_graphs(ops):
     """Calls with workspaces on two streams and in two graphs, replayed one after the other."""
     x, w, dy, pre = randn(300, 4096, seed=1), weights(128, 4096), randn(300, 128, seed=2), randn(300, 128, seed=3)
