@@ -701,17 +701,16 @@ AS_DEV void part_add(const GemmParams& p, const Ctx<1>& c, const Unit& w, const 
 }
 
 enum { PLAIN = 0, LONG_SUMS = 1, SHARED = 2 };  // SHARED: p.parts CTAs of a cluster share a tile, one tile each cluster (CG == 1)
+// A CTA's (or a pair's) units: `first`, first + step, ...
 template <int CG, bool A_MN, bool B_MN, int MODE>
-__global__ void __launch_bounds__(LIN_THREADS, 1)
-linear_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb, const __grid_constant__ CUtensorMap mo, const __grid_constant__ CUtensorMap mp,
-              const __grid_constant__ CUtensorMap mr, const __grid_constant__ GemmParams p) {
+AS_DEV void lin_run(const CUtensorMap* ma, const CUtensorMap* mb, const ResultMaps& results, const GemmParams& p, unsigned first, unsigned step) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);      // the same in both CTAs of a pair
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + 8 * B_COUNT);
   volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem + 8 * B_COUNT + 4);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   constexpr bool LONG = MODE == LONG_SUMS;
-  Ctx<CG> c{smem_u32(smem), 0u, WaitCtx{p.status, abort_flag}, CG == 1 ? 0u : cta_rank(), blockIdx.x / CG, gridDim.x / CG};
+  Ctx<CG> c{smem_u32(smem), 0u, WaitCtx{p.status, abort_flag}, CG == 1 ? 0u : cta_rank(), first, step};
   if (threadIdx.x < B_COUNT) {                 // a barrier a thread
     const bool given_back = threadIdx.x == B_AEMPTY || threadIdx.x == B_AEMPTY + 1;
     mbar_init(c.bar((int)threadIdx.x), given_back ? RESULT_WARPS * CG : 1);
@@ -720,7 +719,7 @@ linear_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CU
   }
   if (threadIdx.x == LIN_THREADS - 1) {
     *abort_flag = 0u;
-    tma_prefetch_desc(&ma); tma_prefetch_desc(&mb);
+    tma_prefetch_desc(ma); tma_prefetch_desc(mb);
   }
   if (warp == 2) { alloc_tmem<CG>(smem_u32(tmem_slot)); griddep_launch(); }
   tc_fence_before();
@@ -730,14 +729,14 @@ linear_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CU
   c.tmem = *tmem_slot;
   griddep_wait();
   if (warp == 0) {
-    if (elect_one()) lin_copies<CG, A_MN, B_MN>(p, c, &ma, &mb);
+    if (elect_one()) lin_copies<CG, A_MN, B_MN>(p, c, ma, mb);
     __syncwarp();
   } else if (warp == 1) {
     if (c.rank == 0 && elect_one()) lin_issue<CG, A_MN, B_MN, LONG>(p, c);
     __syncwarp();
   } else if (warp >= FIRST_RESULT) {
     if constexpr (MODE == SHARED) part_leave(p, c, lane, warp - FIRST_RESULT);
-    else lin_results<CG, LONG>(p, c, ResultMaps{&mo, &mp, &mr}, lane, warp - FIRST_RESULT);
+    else lin_results<CG, LONG>(p, c, results, lane, warp - FIRST_RESULT);
   }
   if constexpr (MODE == SHARED) {
     const Unit w = unit_of<1>(p, c.unit);
@@ -756,6 +755,20 @@ linear_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CU
     tc_fence_after();
     free_tmem<CG>(c.tmem);
   }
+}
+template <int CG, bool A_MN, bool B_MN, int MODE>
+__global__ void __launch_bounds__(LIN_THREADS, 1)
+linear_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb, const __grid_constant__ CUtensorMap mo, const __grid_constant__ CUtensorMap mp,
+              const __grid_constant__ CUtensorMap mr, const __grid_constant__ GemmParams p) {
+  lin_run<CG, A_MN, B_MN, MODE>(&ma, &mb, ResultMaps{&mo, &mp, &mr}, p, blockIdx.x / CG, gridDim.x / CG);
+}
+// Both products of a backward pass at once, dx by the first CTAs and dw by the others: small ones, each of which is mostly its launch, set-up, first copies and read-out (300 x 512 by 256, dx and dw one
+// after the other 13.8 us, at once 7.0; 1000 x 1536 by 1536 23 and 14; 7800 rows 72 and 62; 16 x 4096 by 4096, a stream of w that half of the SMs ask for, 28 and 30).
+struct Two { CUtensorMap a[2], b[2], out[2]; GemmParams p[2]; int first; };
+__global__ void __launch_bounds__(LIN_THREADS, 1) linear_two_kernel(const __grid_constant__ Two t) {
+  const unsigned first = (unsigned)t.first;
+  if (blockIdx.x < first) lin_run<1, false, true, PLAIN>(&t.a[0], &t.b[0], ResultMaps{&t.out[0], &t.out[0], &t.out[0]}, t.p[0], blockIdx.x, first);
+  else lin_run<1, true, true, PLAIN>(&t.a[1], &t.b[1], ResultMaps{&t.out[1], &t.out[1], &t.out[1]}, t.p[1], blockIdx.x - first, gridDim.x - first);
 }
 
 // Sums of parts, in their order, and what follows them: four columns a thread.
@@ -1187,18 +1200,21 @@ struct Product {
   bool a_mn, b_mn;
   long long M, N, K;                         // K: the summed index
   long long T;                               // entries of the rows of results, or of the summed index where a_mn
+  Plan plan;
 };
-uint64_t part_bytes(const Product& q, const Plan& plan) { return plan.parts == 1 || plan.shared ? 0 : up256((uint64_t)plan.parts * (uint64_t)q.M * (uint64_t)((q.N + 3) / 4 * 4) * 4); }
-Plan plan_for(const Product& q, bool f32, as_fp8_context_t h) {
+uint64_t part_bytes(const Product& q) { return q.plan.parts == 1 || q.plan.shared ? 0 : up256((uint64_t)q.plan.parts * (uint64_t)q.M * (uint64_t)((q.N + 3) / 4 * 4) * 4); }
+// sms: that it has to itself; alone: beside another product of the same launch, by single CTAs.
+Plan plan_for(const Product& q, bool f32, as_fp8_context_t h, int sms, bool alone = true) {
   const long long entries = q.a_mn ? 1 : q.M / q.T;
   const long long ksteps = q.a_mn ? (q.K / q.T) * ((q.T + BK - 1) / BK) : (q.K + BK - 1) / BK;
-  return plan_of(entries, q.a_mn ? q.M : q.T, q.M, q.N, ksteps, q.b_mn, f32 ? MOST_STEPS : 1 << 30, h->sms, h->clusters);
+  return plan_of(entries, q.a_mn ? q.M : q.T, q.M, q.N, ksteps, q.b_mn, f32 ? MOST_STEPS : 1 << 30, sms, alone ? h->clusters : nullptr);
 }
 
+struct Prepared { Maps m; GemmParams p; size_t smem; };
 // out, pre, res: what the epilogue's matrices are.
-cudaError_t run_product(as_fp8_context_t h, const Product& q, const Epilogue& e, const as_rows_t& out, const as_rows_t& pre, const as_rows_t& res, void* part, cudaStream_t st) {
-  const Plan plan = plan_for(q, e.out_f32, h);
-  GemmParams p{};
+cudaError_t prepare(as_fp8_context_t h, const Product& q, const Epilogue& e, const as_rows_t& out, const as_rows_t& pre, const as_rows_t& res, void* part, Prepared& r) {
+  const Plan& plan = q.plan;
+  GemmParams& p = r.p;
   p.e = e;
   p.status = h->status;
   p.M = (int)q.M;
@@ -1215,8 +1231,8 @@ cudaError_t run_product(as_fp8_context_t h, const Product& q, const Epilogue& e,
   if (plan.parts > 1 && !plan.shared) { p.part = static_cast<float*>(part); p.part_pitch = (q.N + 3) / 4 * 4; }
   const int stage = (BM + plan.bn / plan.cg) * BK * 2;
   p.stages = std::min((SMEM_MAX - 1024 - STAGES_OFF) / stage, MAX_STAGES);
-  const size_t smem = 1024 + STAGES_OFF + (size_t)p.stages * stage;
-  Maps m{};
+  r.smem = 1024 + STAGES_OFF + (size_t)p.stages * stage;
+  Maps& m = r.m;
   auto boxes = [&](const as_rows_t& x, CUtensorMap* map) {             // (a map that the driver does not take leaves it to the warps)
     const bool spread = (x.tokens == 1 || x.stride_token > 0) && (x.tokens == q.M || x.stride_batch > 0) && (x.head_dim == q.N || x.stride_head > 0);
     return plan.parts == 1 && x.data != nullptr && spread && rows_vec16(x) && (x.head_dim == q.N || x.head_dim % 32 == 0) && as_tc::make_map_strips(map, x, q.M, q.N);
@@ -1231,6 +1247,24 @@ cudaError_t run_product(as_fp8_context_t h, const Product& q, const Epilogue& e,
   if (!as_tc::make_map_boxes(&m.a, in_entries(q.a, a_rows, q.T), a_rows, a_cols, q.a_mn ? 64 : BM) ||
       !as_tc::make_map_boxes(&m.b, q.a_mn ? in_entries(q.b, b_rows, q.T) : q.b, b_rows, b_cols, q.b_mn ? 64 : plan.bn / plan.cg))
     return cudaErrorInvalidValue;
+  return cudaSuccess;
+}
+// Sums of parts, where there are any, behind their product.
+cudaError_t finish(as_fp8_context_t h, const Product& q, const GemmParams& p, cudaStream_t st) {
+  if (p.part == nullptr) return cudaSuccess;
+  FinishParams f{};
+  f.e = p.e; f.part = p.part; f.pitch = p.part_pitch; f.M = p.M; f.parts = p.parts;
+  f.pieces = (unsigned)(q.M * (p.part_pitch / 4));          // (parts are of results that leave SMs idle: far below 2^32)
+  const long long pieces = (f.pieces + 255ll) / 256;
+  return as_launch_dependent(finish_kernel, dim3((unsigned)std::min<long long>(pieces, 8ll * h->sms)), dim3(256), 0, st, f);
+}
+cudaError_t run_product(as_fp8_context_t h, const Product& q, const Epilogue& e, const as_rows_t& out, const as_rows_t& pre, const as_rows_t& res, void* part, cudaStream_t st) {
+  const Plan& plan = q.plan;
+  Prepared r{};
+  if (const cudaError_t err = prepare(h, q, e, out, pre, res, part, r); err != cudaSuccess) return err;
+  const Maps& m = r.m;
+  const GemmParams& p = r.p;
+  const size_t smem = r.smem;
   const int units = plan.shared ? (int)p.units : (int)std::min<long long>(p.units, h->sms / plan.cg);
   cudaError_t err;
   // results in fp32 of long sums (operands of the forward product alone have them)
@@ -1244,12 +1278,23 @@ cudaError_t run_product(as_fp8_context_t h, const Product& q, const Epilogue& e,
   if (plan.shared)
     return q.a_mn ? launch<1, true, true, SHARED>(m, p, units, smem, st) : q.b_mn ? launch<1, false, true, SHARED>(m, p, units, smem, st) : launch<1, false, false, SHARED>(m, p, units, smem, st);
   err = plan.cg == 2 ? run(std::integral_constant<int, 2>{}) : run(std::integral_constant<int, 1>{});
-  if (err != cudaSuccess || plan.parts == 1) return err;
-  FinishParams f{};
-  f.e = e; f.part = p.part; f.pitch = p.part_pitch; f.M = p.M; f.parts = p.parts;
-  f.pieces = (unsigned)(q.M * (p.part_pitch / 4));          // (parts are of results that leave SMs idle: far below 2^32)
-  const long long pieces = (f.pieces + 255ll) / 256;
-  return as_launch_dependent(finish_kernel, dim3((unsigned)std::min<long long>(pieces, 8ll * h->sms)), dim3(256), 0, st, f);
+  return err != cudaSuccess ? err : finish(h, q, p, st);
+}
+// Two products at once.
+cudaError_t run_two(as_fp8_context_t h, const Product (&q)[2], const Epilogue (&e)[2], const as_rows_t (&out)[2], void* const (&part)[2], cudaStream_t st) {
+  Prepared r[2]{};
+  Two t{};
+  int ctas[2];
+  for (int i = 0; i < 2; ++i) {
+    if (const cudaError_t err = prepare(h, q[i], e[i], out[i], as_rows_t{}, as_rows_t{}, part[i], r[i]); err != cudaSuccess) return err;
+    t.a[i] = r[i].m.a; t.b[i] = r[i].m.b; t.out[i] = r[i].m.out; t.p[i] = r[i].p;
+    ctas[i] = (int)std::min<long long>(r[i].p.units, h->sms / 2);
+  }
+  t.first = ctas[0];
+  if (const cudaError_t err = as_launch_dependent(linear_two_kernel, dim3((unsigned)(ctas[0] + ctas[1])), dim3(LIN_THREADS), std::max(r[0].smem, r[1].smem), st, t); err != cudaSuccess) return err;
+  for (int i = 0; i < 2; ++i)
+    if (const cudaError_t err = finish(h, q[i], r[i].p, st); err != cudaSuccess) return err;
+  return cudaSuccess;
 }
 
 bool dtype_ok(int t) { return t == AS_DTYPE_BF16 || t == AS_DTYPE_F32; }
@@ -1312,10 +1357,14 @@ LinearPlan plan_linear(as_fp8_context_t h, const as_linear_t& a) {
   // few rows read x where it lies: 8 columns at a time
   l.x = operand_of(a.x, a.rows, a.cols);
   l.q = Product{l.x.rows, l.w.rows, false, false, a.rows, a.out_cols, a.cols, l.x.rows.tokens};
-  l.few = a.rows <= 16 || (a.rows <= 256 && few_of((int)a.rows, (int)a.out_cols, (int)a.cols, h->sms).ns < plan_for(l.q, a.out.dtype == AS_DTYPE_F32, h).ns + 4500.);
+  l.few = a.rows <= 16;
+  if (!l.few) {
+    l.q.plan = plan_for(l.q, a.out.dtype == AS_DTYPE_F32, h, h->sms);
+    l.few = a.rows <= 256 && few_of((int)a.rows, (int)a.out_cols, (int)a.cols, h->sms).ns < l.q.plan.ns + 4500.;
+  }
   if (l.few && aligned(a.x.data, 16) && ((a.x.stride_batch | a.x.stride_head | a.x.stride_token) & 7) == 0 && (a.x.head_dim == a.cols || a.x.head_dim % 8 == 0)) l.x = Operand{a.x, false, a.x};
   l.bytes = copy_bytes(l.x, a.rows) + copy_bytes(l.w, a.out_cols);
-  if (!l.few) l.bytes += part_bytes(l.q, plan_for(l.q, a.out.dtype == AS_DTYPE_F32, h));
+  if (!l.few) l.bytes += part_bytes(l.q);
   return l;
 }
 bool workspace_ok(const void* p, uint64_t has, uint64_t need) { return need == 0 || (p != nullptr && aligned(p, 256) && has >= need); }
@@ -1328,6 +1377,7 @@ cudaError_t as_linear_init() {
   opt(linear_kernel<1, false, false, PLAIN>, SMEM_MAX); opt(linear_kernel<1, false, false, LONG_SUMS>, SMEM_MAX); opt(linear_kernel<1, false, true, PLAIN>, SMEM_MAX); opt(linear_kernel<1, true, true, PLAIN>, SMEM_MAX);
   opt(linear_kernel<2, false, false, PLAIN>, SMEM_MAX); opt(linear_kernel<2, false, false, LONG_SUMS>, SMEM_MAX); opt(linear_kernel<2, false, true, PLAIN>, SMEM_MAX); opt(linear_kernel<2, true, true, PLAIN>, SMEM_MAX);
   opt(linear_kernel<1, false, false, SHARED>, SMEM_MAX); opt(linear_kernel<1, false, true, SHARED>, SMEM_MAX); opt(linear_kernel<1, true, true, SHARED>, SMEM_MAX);
+  opt(linear_two_kernel, SMEM_MAX);
   opt(linear_few_kernel<1>, few_smem(1)); opt(linear_few_kernel<2>, few_smem(2));
   return e;
 }
@@ -1381,6 +1431,7 @@ namespace {
 
 struct BackPlan {
   Operand x, w, dy;
+  bool two;                                  // both products in one launch
   bool dz, sums, direct;                     // dz is computed (else dy is the operand as it lies); sums are taken, in one step
   long long pitch;
   int runs;
@@ -1445,17 +1496,22 @@ BackPlan plan_back(as_fp8_context_t h, const as_linear_backward_t& a) {
   if (a.dgate != nullptr && !b.direct) b.bytes += up256((uint64_t)gates * b.runs * a.out_cols * 4);
   b.bytes += copy_bytes(b.x, a.rows) + copy_bytes(b.w, a.out_cols);
   const as_rows_t dz = b.dz ? plain_rows(nullptr, a.rows, a.out_cols, b.pitch) : b.dy.rows;
-  uint64_t parts = 0;
   if (dx) {
     b.dx = Product{dz, b.w.rows, false, true, a.rows, a.cols, a.out_cols, dz.tokens};
-    parts = std::max(parts, part_bytes(b.dx, plan_for(b.dx, false, h)));
+    b.dx.plan = plan_for(b.dx, false, h, h->sms);
   }
   if (dw) {
     const long long T = std::min(dz.tokens, b.x.rows.tokens);
     b.dw = Product{dz, b.x.rows, true, true, a.out_cols, a.cols, a.rows, T};
-    parts = std::max(parts, part_bytes(b.dw, plan_for(b.dw, false, h)));
+    b.dw.plan = plan_for(b.dw, false, h, h->sms);
   }
-  b.bytes += parts;                          // (the products run one after another)
+  if (dx && dw) {                            // at once, by half of the SMs each, where that is the sooner: a launch of its own is 4.5 us beside what the plans count
+    const Plan x = plan_for(b.dx, false, h, h->sms / 2, false), w = plan_for(b.dw, false, h, h->sms / 2, false);
+    b.two = std::max(x.ns, w.ns) < b.dx.plan.ns + b.dw.plan.ns + 4500.;
+    if (b.two) { b.dx.plan = x; b.dw.plan = w; }
+  }
+  const uint64_t of_dx = dx ? part_bytes(b.dx) : 0, of_dw = dw ? part_bytes(b.dw) : 0;
+  b.bytes += b.two ? of_dx + of_dw : std::max(of_dx, of_dw);
   return b;
 }
 
@@ -1519,19 +1575,21 @@ extern "C" as_status_t as_linear_backward(as_fp8_context_t h, const as_linear_ba
   const Copy copies[2] = {{&b.x, a->rows, a->cols}, {&b.w, a->out_cols, a->cols}};
   if (run_copies(copies, room, h->sms, st) != cudaSuccess) return failed();
   const as_rows_t dz = b.dz ? plain_rows(z.dz, a->rows, a->out_cols, b.pitch) : b.dy.rows;
-  Epilogue e{};
-  e.N = (int)a->cols; e.act = AS_ACT_NONE;
-  if (a->dx.data != nullptr) {
-    b.dx.a = dz; b.dx.b = b.w.rows;
-    e.out = rows_of(a->dx, a->rows, a->cols);
-    e.vec = a->cols % 4 == 0 && vec4(a->dx);
-    if (run_product(h, b.dx, e, a->dx, as_rows_t{}, as_rows_t{}, room, st) != cudaSuccess) return failed();
+  Epilogue e[2]{};
+  const as_rows_t to[2] = {a->dx, a->dw};
+  Product q[2] = {b.dx, b.dw};
+  q[0].b = b.w.rows; q[1].b = b.x.rows;
+  for (int i = 0; i < 2; ++i) {
+    if (to[i].data == nullptr) continue;
+    q[i].a = dz;
+    e[i].N = (int)a->cols; e[i].act = AS_ACT_NONE;
+    e[i].out = rows_of(to[i], i == 0 ? a->rows : a->out_cols, a->cols);
+    e[i].vec = a->cols % 4 == 0 && vec4(to[i]);
+    if (!b.two && run_product(h, q[i], e[i], to[i], as_rows_t{}, as_rows_t{}, room, st) != cudaSuccess) return failed();
   }
-  if (a->dw.data != nullptr) {
-    b.dw.a = dz; b.dw.b = b.x.rows;
-    e.out = rows_of(a->dw, a->out_cols, a->cols);
-    e.vec = a->cols % 4 == 0 && vec4(a->dw);
-    if (run_product(h, b.dw, e, a->dw, as_rows_t{}, as_rows_t{}, room, st) != cudaSuccess) return failed();
+  if (b.two) {
+    void* const part[2] = {room, room + part_bytes(q[0])};
+    if (run_two(h, q, e, to, part, st) != cudaSuccess) return failed();
   }
   return AS_OK;
 }

@@ -20,11 +20,11 @@ struct Plan { int cg, bn, parts; bool shared; double ns; };
 // By the time that the turns of all SMs take: turns x steps x ns a step, and what the reading out of the last turn and the meeting of a pair add.  What a step takes is its bytes into an SM, 64 a
 // clock, and beside them, from 256 x 256 on, its MMAs.  A tile's results take the warps 1.9 us (two strips of 32 columns each: 3.3), which a short sum does not hide: 6144 x 1280 from 3 rows takes 18 us in
 // tiles of 128 x 64 and 11 of 128 x 256.  A part more costs its sums' way to the workspace and back, and a launch; a cluster costs the meeting and the sums, and more with every CTA beyond
-// two, and holds as many tiles at once as the device has such clusters.  most_steps: that a cluster's CTA may add up by itself.
+// two, and holds as many tiles at once as the device has such clusters.  most_steps: that a cluster's CTA may add up by itself.  clusters == nullptr: single CTAs alone.
 inline Plan plan_of(long long entries, long long T, long long M, long long N, long long ksteps, bool b_mn, int most_steps, int sms, const int* clusters) {
   static const int ns[2][8] = {{230, 250, 265, 300, 345, 385, 440, 500}, {228, 230, 240, 262, 297, 320, 365, 410}};
   Plan best{1, 64, 1, false, 1e300};
-  for (int cg = 1; cg <= 2; ++cg)
+  for (int cg = 1; cg <= (clusters != nullptr ? 2 : 1); ++cg)
     for (int i = 0; i < 8; ++i) {
       const int bn = 32 * (i + 1);
       if (b_mn && bn % (64 * cg) != 0) continue;
@@ -39,7 +39,7 @@ inline Plan plan_of(long long entries, long long T, long long M, long long N, lo
           if (parts > 1) t += 3000. + 200. * parts + (double)M * (double)N * 4. * (parts + 1) / 6000.;
           if (t < best.ns) best = {cg, bn, parts, false, t};
         }
-        if (cg == 1 && parts > 1 && parts <= MAX_PARTS && tiles <= clusters[parts] && steps <= most_steps) {
+        if (clusters != nullptr && cg == 1 && parts > 1 && parts <= MAX_PARTS && tiles <= clusters[parts] && steps <= most_steps) {
           const double t = (double)steps * ns[0][i] + 10. * bn + 1700. + 8. * std::max(bn - 64, 0) + (parts - 2) * (100. + 4. * bn);
           if (t < best.ns) best = {1, bn, parts, true, t};
         }
