@@ -188,6 +188,7 @@ struct GemmParams {
   int M, T, mt_entry;                       // rows of results in entries of T, of mt_entry tiles each
   int bn, nt, stages, parts;
   int ksteps, ks_entry;                     // steps of BK of the summed index, where it is rows: of an entry
+  int run;                                  // LONG: steps of a run of sums
   unsigned long long by_nt, by_mt;          // 2^64 / nt and 2^64 / mt_entry, rounded up (0: 1): a quotient is the upper half of a product, exact below 2^32
   int a_hd, b_hd;                           // columns of a head of the operands, multiples of 64 (INT32_MAX: there are no heads)
 };
@@ -307,13 +308,15 @@ out:
   }
 }
 
-// LONG: long sums go to the result warps in runs of about MOST_STEPS steps, which add them up in fp32 rounded to nearest.  The tensor cores truncate: over 384 instructions (6144 columns) that
-// left 7e-6 of a product, in one direction, which a result in bf16 does not show but one in fp32 does.  A tile's first run is the longest: the tile before it is read out meanwhile.
-constexpr int MOST_STEPS = 18;
+// LONG: long sums go to the result warps in runs of about most_steps steps, which add them up in fp32 rounded to nearest.  The tensor cores truncate, in one direction: over 384 instructions (6144
+// columns) that left 7e-6 of a product, which a result in fp32 shows.  One in bf16, whose rounding is 2^-8 at most, does not; but what is left grows with the sum, and a weight's gradient would carry it in
+// every element: of products of one sign 8e-5 over 16384 elements, 1.9e-4 over 32768, 3.9e-4 over 65536, 3.5e-3 over 524288, in runs of 256 steps 1e-4 at any length (65536 x 2048 by 2048 in one run 412 us,
+// in runs 421).  A tile's first run is the longest: the tile before it is read out meanwhile.
+constexpr int most_steps(bool f32) { return f32 ? 18 : 256; }
 struct Runs {
   int first, rest;
-  AS_DEV explicit Runs(int steps) {
-    const int n = (steps + MOST_STEPS - 1) / MOST_STEPS;
+  AS_DEV Runs(int steps, int most) {
+    const int n = (steps + most - 1) / most;
     first = n == 1 ? steps : (4 * steps + 3 * n - 1) / (3 * n);
     rest = n == 1 ? 1 : (steps - first + n - 2) / (n - 1);
   }
@@ -326,7 +329,7 @@ AS_DEV void lin_issue(const GemmParams& p, const Ctx<CG>& c) {
   uint32_t buf = 0, turn = 0;
   for (long long u = c.unit; u < p.units; u += c.step) {
     const Unit w = unit_of<CG>(p, u);
-    const Runs runs(w.k1 - w.k0);
+    const Runs runs(w.k1 - w.k0, p.run);
     int k = w.k0;
     do {
     const int first = k, end = LONG ? min(w.k1, k + (k == w.k0 ? runs.first : runs.rest)) : w.k1;
@@ -524,7 +527,7 @@ AS_DEV void lin_results(const GemmParams& p, const Ctx<CG>& c, const ResultMaps&
     if constexpr (!LONG) vectors();
     if constexpr (LONG) {
       // the runs' sums, in registers; with the last run's they go back to where that one lies
-      const Runs runs(w.k1 - w.k0);
+      const Runs runs(w.k1 - w.k0, p.run);
       if (runs.first < w.k1 - w.k0) {
         float x[8][8];                        // columns 32 group + 128 (i / 4) + 8 (i % 4)
 #pragma unroll
@@ -1203,11 +1206,14 @@ struct Product {
   Plan plan;
 };
 uint64_t part_bytes(const Product& q) { return q.plan.parts == 1 || q.plan.shared ? 0 : up256((uint64_t)q.plan.parts * (uint64_t)q.M * (uint64_t)((q.N + 3) / 4 * 4) * 4); }
+// Steps of the summed index, which end with its entries.
+long long ksteps_of(const Product& q) { return q.a_mn ? (q.K / q.T) * ((q.T + BK - 1) / BK) : (q.K + BK - 1) / BK; }
+// Whether a unit's sum is longer than one run.
+bool long_sums(const Product& q, const Plan& plan, bool f32) { return (ksteps_of(q) + plan.parts - 1) / plan.parts > most_steps(f32); }
 // sms: that it has to itself; alone: beside another product of the same launch, by single CTAs.
 Plan plan_for(const Product& q, bool f32, as_fp8_context_t h, int sms, bool alone = true) {
   const long long entries = q.a_mn ? 1 : q.M / q.T;
-  const long long ksteps = q.a_mn ? (q.K / q.T) * ((q.T + BK - 1) / BK) : (q.K + BK - 1) / BK;
-  return plan_of(entries, q.a_mn ? q.M : q.T, q.M, q.N, ksteps, q.b_mn, f32 ? MOST_STEPS : 1 << 30, sms, alone ? h->clusters : nullptr);
+  return plan_of(entries, q.a_mn ? q.M : q.T, q.M, q.N, ksteps_of(q), q.b_mn, most_steps(f32), sms, alone ? h->clusters : nullptr);
 }
 
 struct Prepared { Maps m; GemmParams p; size_t smem; };
@@ -1226,7 +1232,8 @@ cudaError_t prepare(as_fp8_context_t h, const Product& q, const Epilogue& e, con
   p.by_nt = reciprocal((unsigned)p.nt);
   p.by_mt = reciprocal((unsigned)p.mt_entry);
   p.ks_entry = (int)(q.a_mn ? (q.T + BK - 1) / BK : 1);
-  p.ksteps = (int)(q.a_mn ? (q.K / q.T) * p.ks_entry : (q.K + BK - 1) / BK);
+  p.ksteps = (int)ksteps_of(q);
+  p.run = most_steps(e.out_f32);
   p.units = (q.a_mn ? 1 : q.M / q.T) * p.mt_entry * (long long)p.nt * p.parts;
   if (plan.parts > 1 && !plan.shared) { p.part = static_cast<float*>(part); p.part_pitch = (q.N + 3) / 4 * 4; }
   const int stage = (BM + plan.bn / plan.cg) * BK * 2;
@@ -1267,13 +1274,15 @@ cudaError_t run_product(as_fp8_context_t h, const Product& q, const Epilogue& e,
   const size_t smem = r.smem;
   const int units = plan.shared ? (int)p.units : (int)std::min<long long>(p.units, h->sms / plan.cg);
   cudaError_t err;
-  // results in fp32 of long sums (operands of the forward product alone have them)
-  const bool is_long = e.out_f32 && (p.ksteps + p.parts - 1) / p.parts > MOST_STEPS;
   auto run = [&](auto cg) {
     constexpr int CG = decltype(cg)::value;
-    if (q.a_mn) return launch<CG, true, true, PLAIN>(m, p, units, smem, st);
-    if (q.b_mn) return launch<CG, false, true, PLAIN>(m, p, units, smem, st);
-    return is_long ? launch<CG, false, false, LONG_SUMS>(m, p, units, smem, st) : launch<CG, false, false, PLAIN>(m, p, units, smem, st);
+    auto by_length = [&](auto mode) {
+      constexpr int MODE = decltype(mode)::value;
+      if (q.a_mn) return launch<CG, true, true, MODE>(m, p, units, smem, st);
+      if (q.b_mn) return launch<CG, false, true, MODE>(m, p, units, smem, st);
+      return launch<CG, false, false, MODE>(m, p, units, smem, st);
+    };
+    return long_sums(q, plan, e.out_f32) ? by_length(std::integral_constant<int, LONG_SUMS>{}) : by_length(std::integral_constant<int, PLAIN>{});
   };
   if (plan.shared)
     return q.a_mn ? launch<1, true, true, SHARED>(m, p, units, smem, st) : q.b_mn ? launch<1, false, true, SHARED>(m, p, units, smem, st) : launch<1, false, false, SHARED>(m, p, units, smem, st);
@@ -1374,8 +1383,13 @@ bool workspace_ok(const void* p, uint64_t has, uint64_t need) { return need == 0
 cudaError_t as_linear_init() {
   cudaError_t e = cudaSuccess;
   auto opt = [&](auto kernel, int bytes) { if (e == cudaSuccess) e = as_tc::opt_in_smem(kernel, bytes); };
-  opt(linear_kernel<1, false, false, PLAIN>, SMEM_MAX); opt(linear_kernel<1, false, false, LONG_SUMS>, SMEM_MAX); opt(linear_kernel<1, false, true, PLAIN>, SMEM_MAX); opt(linear_kernel<1, true, true, PLAIN>, SMEM_MAX);
-  opt(linear_kernel<2, false, false, PLAIN>, SMEM_MAX); opt(linear_kernel<2, false, false, LONG_SUMS>, SMEM_MAX); opt(linear_kernel<2, false, true, PLAIN>, SMEM_MAX); opt(linear_kernel<2, true, true, PLAIN>, SMEM_MAX);
+  auto opt_modes = [&](auto cg) {
+    constexpr int CG = decltype(cg)::value;
+    opt(linear_kernel<CG, false, false, PLAIN>, SMEM_MAX); opt(linear_kernel<CG, false, true, PLAIN>, SMEM_MAX); opt(linear_kernel<CG, true, true, PLAIN>, SMEM_MAX);
+    opt(linear_kernel<CG, false, false, LONG_SUMS>, SMEM_MAX); opt(linear_kernel<CG, false, true, LONG_SUMS>, SMEM_MAX); opt(linear_kernel<CG, true, true, LONG_SUMS>, SMEM_MAX);
+  };
+  opt_modes(std::integral_constant<int, 1>{});
+  opt_modes(std::integral_constant<int, 2>{});
   opt(linear_kernel<1, false, false, SHARED>, SMEM_MAX); opt(linear_kernel<1, false, true, SHARED>, SMEM_MAX); opt(linear_kernel<1, true, true, SHARED>, SMEM_MAX);
   opt(linear_two_kernel, SMEM_MAX);
   opt(linear_few_kernel<1>, few_smem(1)); opt(linear_few_kernel<2>, few_smem(2));
@@ -1507,7 +1521,7 @@ BackPlan plan_back(as_fp8_context_t h, const as_linear_backward_t& a) {
   }
   if (dx && dw) {                            // at once, by half of the SMs each, where that is the sooner: a launch of its own is 4.5 us beside what the plans count
     const Plan x = plan_for(b.dx, false, h, h->sms / 2, false), w = plan_for(b.dw, false, h, h->sms / 2, false);
-    b.two = std::max(x.ns, w.ns) < b.dx.plan.ns + b.dw.plan.ns + 4500.;
+    b.two = std::max(x.ns, w.ns) < b.dx.plan.ns + b.dw.plan.ns + 4500. && !long_sums(b.dx, x, false) && !long_sums(b.dw, w, false);
     if (b.two) { b.dx.plan = x; b.dw.plan = w; }
   }
   const uint64_t of_dx = dx ? part_bytes(b.dx) : 0, of_dw = dw ? part_bytes(b.dw) : 0;

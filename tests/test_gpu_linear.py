@@ -337,3 +337,26 @@ def test_refuses_results_over_other_tensors(ops):
     want = ops.linear(x, w, residual=r)
     ops.linear(x, w, residual=r, out=r)
     assert torch.equal(r, want)
+
+
+# what is computed, summed elements, rows of results, columns of results
+@pytest.mark.parametrize("what,k,m,n", [("w", 1 << 23, 128, 128), ("w", 1 << 19, 2560, 2048), ("x", 1 << 19, 2560, 2048), ("y", 1 << 19, 2560, 2048)])
+def test_long_sums_in_bf16_lean_to_no_side(ops, what, k, m, n):
+    """Sums of 8192 steps (and of 16 times as many in 16 parts), all products of one sign.  The matrix instructions truncate what they add up, 2^-23 of it at most, in runs of at most 4 * 342 (256 steps and a
+    third more in a first run), and the runs are added up rounded to nearest; a result's rounding to bf16 is at most 2^-8, independent from one to the next, so that the mean of 128 x 128 of them is off by
+    less than four times 2^-8 / 3 ** 0.5 / 128.  In one run the sums were off by 3.5e-3 in the mean, always towards 0."""
+    if what == "w":                                              # [m, n] = dy [k, m]^T x [k, n]
+        dy, x = (randn(k, c, seed=c).abs_() for c in (m, n))
+        got = ops.linear_backward(dy, x, weights(m, n), x_grad=k > 1 << 20).w
+        a, b = dy[:, :128].T, x[:, :128].T
+    elif what == "x":                                            # [m, n] = dy [m, k] w [k, n]
+        dy, w = randn(m, k, seed=1).abs_(), randn(k, n, seed=2).abs_()
+        got = ops.linear_backward(dy, randn(m, n), w, w_grad=False).x
+        a, b = dy[:128], w[:, :128].T
+    else:
+        x, w = randn(m, k, seed=1).abs_(), randn(n, k, seed=2).abs_()
+        got = ops.linear(x, w)
+        a, b = x[:128], w[:128]
+    ref = sum(a[:, i:i + (1 << 17)].to(R.F64) @ b[:, i:i + (1 << 17)].to(R.F64).T for i in range(0, k, 1 << 17))
+    off = float(((got[:128, :128].to(R.F64) - ref) / ref).mean())
+    assert abs(off) <= 4 * 342 * 2.0 ** -23 + 4 * 2.0 ** -8 / 3 ** 0.5 / 128, off
