@@ -9,6 +9,7 @@
 // 32760 tokens of 2 x 12 heads of 128 in bf16, from the fused projection's rows into heads, norm by heads: 74 us, 5.5 TB/s; its gradient 111 us, 5.4 TB/s.  7800 tokens, norm over rows: 24 us,
 // 3.9 TB/s (3.3 rows a warp, each of which is a chain of latencies), its gradient 55 us (shared memory: the rows twice, the weights twice and the sums of d n).
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 
 #include "as_layer.h"
@@ -962,6 +963,24 @@ bool heads_vec(const as_rows_t& x, int elements) {
   return aligned(x.data, bytes) && ((x.stride_batch | x.stride_head | x.stride_token) & (bytes / (x.dtype == AS_DTYPE_BF16 ? 2 : 4) - 1)) == 0;
 }
 
+constexpr size_t KEPT_MOST = 12 * 1024;      // of rows' weights
+// Shared memory of a kernel's calls: more than 48 KB has to be asked for.  It is, once for a kernel and a device, for the most that any call of it takes: a limit that each call set to its own size
+// would be lowered by one thread between another one's setting and its launch.
+template <auto KERNEL>
+cudaError_t allow_smem(size_t smem, size_t most) {
+  if (smem <= 40 * 1024) return cudaSuccess;
+  static std::atomic<uint64_t> done{0};                  // a bit for each device
+  int dev = 0;
+  if (const cudaError_t e = cudaGetDevice(&dev); e != cudaSuccess) return e;
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0ull;
+  if (done.load(std::memory_order_acquire) & bit) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
+  return e;
+}
+// A warp's factors at the most: of heads of 32 lanes, all of them turned.
+constexpr size_t room_most(int E) { return (size_t)(16 * E / 2 + 7) / 8 * 128; }
+
 struct Shape { bool vec; int E, NV, chunks; long long ctas; size_t kept; };       // kept: bytes of both tensors' weights
 // Fills in what the kernels share; `most`: vectors that a lane's registers hold.
 Shape turn_params(const as_qk_norm_rotary_t& a, const as_rotation_t& r, int sms, bool back, const as_rows_t* more, int n_more, TurnParams& p) {
@@ -1019,7 +1038,7 @@ Shape turn_params(const as_qk_norm_rotary_t& a, const as_rotation_t& r, int sms,
     // weights in shared memory, as far as two CTAs an SM have the room
     const size_t size = p.w_f32 ? 4 : 2, of_q = (size_t)p.t[0].heads * a.head_dim * size, of_k = (size_t)p.t[1].heads * a.head_dim * size;
     s.kept = back ? std::max(of_q, of_k) : of_q + of_k;
-    if (s.vec && s.kept <= 12 * 1024 && of_q % 16 == 0 && of_k % 16 == 0 && aligned(a.q_weight, 16) && (!two || aligned(a.k_weight, 16))) p.kept = (int)of_q;
+    if (s.vec && s.kept <= KEPT_MOST && of_q % 16 == 0 && of_k % 16 == 0 && aligned(a.q_weight, 16) && (!two || aligned(a.k_weight, 16))) p.kept = (int)of_q;
     else s.kept = 0;
   } else {
     // few rows: a vector a warp, so that all of them are under way at once
@@ -1035,16 +1054,17 @@ template <typename T, int NORM, int E>
 cudaError_t launch_lanes(const TurnParams& p, const Shape& s, int sms, cudaStream_t st) {
   const dim3 grid((unsigned)std::min<long long>(s.ctas, std::max(1, 2 * sms / p.chunks)), (unsigned)p.chunks), block(THREADS);        // CTAs go on from row to row
   const size_t smem = WARPS * (s.NV * (E * 64) * sizeof(T) + (size_t)p.room) + s.kept;
-  auto launch = [&](auto kernel) {
-    if (smem > 40 * 1024)                                // (48 KB are there without asking)
-      if (const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); e != cudaSuccess) return e;
+  auto launch = [&](auto nv, auto half) {
+    constexpr int NV = decltype(nv)::value;
+    constexpr auto kernel = turn_kernel<T, NORM, NV, decltype(half)::value, E>;
+    if (const cudaError_t e = allow_smem<kernel>(smem, WARPS * (NV * (E * 64) * sizeof(T) + room_most(E)) + KEPT_MOST); e != cudaSuccess) return e;
     return as_launch_dependent(kernel, grid, block, smem, st, p);
   };
-  auto run = [&](auto interleaved, auto half) { return p.half ? launch(half) : launch(interleaved); };
+  auto run = [&](auto nv) { return p.half ? launch(nv, std::true_type{}) : launch(nv, std::false_type{}); };
   switch (s.NV) {
-    case 1: return run(turn_kernel<T, NORM, 1, false, E>, turn_kernel<T, NORM, 1, true, E>);
-    case 2: return run(turn_kernel<T, NORM, 2, false, E>, turn_kernel<T, NORM, 2, true, E>);
-    default: return run(turn_kernel<T, NORM, 3, false, E>, turn_kernel<T, NORM, 3, true, E>);
+    case 1: return run(std::integral_constant<int, 1>{});
+    case 2: return run(std::integral_constant<int, 2>{});
+    default: return run(std::integral_constant<int, 3>{});
   }
 }
 template <typename T, int NORM>
@@ -1059,24 +1079,25 @@ cudaError_t launch_norm(const TurnParams& p, const Shape& s, int norm, int sms, 
 
 template <typename T, int NORM, int E>
 cudaError_t launch_back_lanes(const TurnParams& p, const Shape& s, unsigned ctas, cudaStream_t st) {
-  const size_t sums = NORM == AS_NORM_ROW ? s.NV : 1, smem = WARPS * (sums * (E * 128) + s.NV * (E * 64) * sizeof(T) + (size_t)p.room) + s.kept;
-  auto run = [&](auto kernel) {
-    if (smem > 40 * 1024)
-      if (const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); e != cudaSuccess) return e;
+  const size_t smem = WARPS * ((NORM == AS_NORM_ROW ? s.NV : 1) * (E * 128) + s.NV * (E * 64) * sizeof(T) + (size_t)p.room) + s.kept;
+  auto launch = [&](auto nv, auto half) {
+    constexpr int NV = decltype(nv)::value;
+    constexpr auto kernel = turn_back_kernel<T, NORM, NV, decltype(half)::value, E>;
+    if (const cudaError_t e = allow_smem<kernel>(smem, WARPS * ((NORM == AS_NORM_ROW ? NV : 1) * (E * 128) + NV * (E * 64) * sizeof(T) + room_most(E)) + KEPT_MOST); e != cudaSuccess) return e;
     return as_launch_dependent(kernel, dim3(ctas, (unsigned)p.n_t), dim3(THREADS), smem, st, p);
   };
-  auto choose = [&](auto interleaved, auto half) { return p.half ? run(half) : run(interleaved); };
+  auto run = [&](auto nv) { return p.half ? launch(nv, std::true_type{}) : launch(nv, std::false_type{}); };
   if constexpr (sizeof(T) == 2)
-    if (s.NV == 3) return choose(turn_back_kernel<T, NORM, 3, false, E>, turn_back_kernel<T, NORM, 3, true, E>);
-  return s.NV == 2 ? choose(turn_back_kernel<T, NORM, 2, false, E>, turn_back_kernel<T, NORM, 2, true, E>) : choose(turn_back_kernel<T, NORM, 1, false, E>, turn_back_kernel<T, NORM, 1, true, E>);
+    if (s.NV == 3) return run(std::integral_constant<int, 3>{});
+  return s.NV == 2 ? run(std::integral_constant<int, 2>{}) : run(std::integral_constant<int, 1>{});
 }
 template <typename T, int NORM>
 cudaError_t launch_back(const TurnParams& p, const Shape& s, unsigned ctas, cudaStream_t st) {
   if (s.vec) return s.E == 16 ? launch_back_lanes<T, NORM, 16>(p, s, ctas, st) : launch_back_lanes<T, NORM, 8>(p, s, ctas, st);
   const size_t smem = (size_t)(NORM == AS_NORM_ROW ? std::max(p.t[0].heads, p.t[1].heads) : WARPS) * p.d * 4;
-  if (smem > 40 * 1024)
-    if (const cudaError_t e = cudaFuncSetAttribute(turn_elements_kernel<T, NORM, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); e != cudaSuccess) return e;
-  return as_launch_dependent(turn_elements_kernel<T, NORM, true>, dim3(ctas, (unsigned)p.n_t), dim3(THREADS), smem, st, p);
+  constexpr auto kernel = turn_elements_kernel<T, NORM, true>;
+  if (const cudaError_t e = allow_smem<kernel>(smem, 16384 * 4); e != cudaSuccess) return e;             // (over rows: of 16384 columns; by heads: 8 x 1024)
+  return as_launch_dependent(kernel, dim3(ctas, (unsigned)p.n_t), dim3(THREADS), smem, st, p);
 }
 
 // CTAs of the backward pass, for each tensor: as many as the device holds at once (of vectors: a multiple of the chunks, which they take in turn).

@@ -351,3 +351,43 @@ def test_refuses_results_over_other_tensors(ops):
     want = ops.qk_norm_rotary(q, k, w, w, table)
     ops.qk_norm_rotary(q, k, w, w, table, q_out=q, k_out=k)
     assert torch.equal(q, want[0]) and torch.equal(k, want[1])
+
+
+def test_host_threads_with_calls_of_different_sizes(ops):
+    """Two threads launch the same kernels, one with 64 pairs (52 KB of shared memory and more), one with 32 (50 KB): neither call changes what the other one may take.  Through the C entries, which
+    hold no lock (with a limit set by each call, 1566 of 80000 launches failed)."""
+    import ctypes as C
+    import threading
+    from paper_2509_24899_b200 import binding as b
+    n, d = 1000, 128
+    wrong, turns = [], 8000
+
+    def of(t):
+        return b.as_rows_t(t.data_ptr(), b.AS_DTYPE_BF16, d, n, t.stride(0), t.stride(1), t.stride(2))
+
+    def prepare(pairs):
+        table = ops.rotary_table((n,), (pairs,))
+        q, dq, out = randn(1, 12, n, d, seed=pairs), randn(1, 12, n, d, seed=pairs + 1), torch.empty(1, 12, n, d, dtype=BF16, device="cuda")
+        a = b.as_qk_norm_rotary_t(struct_size=C.sizeof(b.as_qk_norm_rotary_t), norm=b.AS_NORM_HEAD, rows=n, head_dim=d, q_heads=12, eps=1e-6, q=of(q), q_out=of(out))
+        a.rotation.table, a.rotation.n_axes, a.rotation.size[0], a.rotation.pairs[0] = table.factors.data_ptr(), 1, n, pairs
+        back = b.as_qk_norm_rotary_backward_t(struct_size=C.sizeof(b.as_qk_norm_rotary_backward_t), fwd=C.pointer(a), dq=of(dq), dq_out=of(out))
+        return a, back, (table, q, dq, out), torch.cuda.Stream()
+
+    def work(a, back, keep, stream):
+        for i in range(turns):
+            for call, args in ((b.lib().as_qk_norm_rotary, a), (b.lib().as_qk_norm_rotary_backward, back)):
+                status = call(C.addressof(args), stream.cuda_stream)
+                if status != b.AS_OK:
+                    wrong.append(status)
+
+    calls = [prepare(pairs) for pairs in (64, 32, 64, 32)]
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=work, args=c) for c in calls]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not wrong, (len(wrong), set(wrong))
+    for pairs, (_, _, (table, q, dq, out), _) in zip((64, 32, 64, 32), calls):
+        assert torch.equal(out, ops.qk_norm_rotary_backward(dq, None, q, None, None, None, table).q)
