@@ -513,6 +513,7 @@ AS_DEV void lin_results(const GemmParams& p, const Ctx<CG>& c, const ResultMaps&
     };
     bool fetched = boxed && rows > 0 && 32 * group < p.bn;
     if (fetched) {
+      fence_proxy_async();                    // the tile before this one may have left its rows through the strip without a copy: its reads come ahead of the copy's writes
       wait_strip(lane);
       fetch(w.n0 + 32 * group);
     }

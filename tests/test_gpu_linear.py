@@ -360,3 +360,17 @@ def test_long_sums_in_bf16_lean_to_no_side(ops, what, k, m, n):
     ref = sum(a[:, i:i + (1 << 17)].to(R.F64) @ b[:, i:i + (1 << 17)].to(R.F64).T for i in range(0, k, 1 << 17))
     off = float(((got[:128, :128].to(R.F64) - ref) / ref).mean())
     assert abs(off) <= 4 * 342 * 2.0 ** -23 + 4 * 2.0 ** -8 / 3 ** 0.5 / 128, off
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N", [48, 80, 104])
+def test_residuals_in_heads_that_tiles_cross(ops, N, dtype):
+    """Entries of tokens that 32 does not divide: a warp's rows come and go by copies where they are of one entry, by its own loads and stores where they are of two, from tile to tile by turns."""
+    B, H, d, k = 9600 // N, 12, 128, 64
+    x, w, r = randn(B * N, k, seed=1), weights(H * d, k), randn(B, H, N, d, dtype=dtype, seed=2)
+    want = r.clone()
+    y = ops.linear(x, w, residual=r)
+    R.check_linear(y, x, w, None, None, None, r)
+    for _ in range(5):
+        r.copy_(want)
+        assert torch.equal(ops.linear(x, w, residual=r, out=r), y)
