@@ -67,8 +67,9 @@ __global__ void __launch_bounds__(THREADS) table_kernel(const __grid_constant__ 
   const unsigned long long step = (unsigned long long)((f - floor(f)) * 18446744073709551616.);
   const int end = a + 1 < p.axes ? p.axis[min(a + 1, AS_ROTARY_MAX_AXES - 1)].first_row : p.rows;
   griddep_wait();
-  const int row0 = blockIdx.x * TABLE_ROWS;
-  for (int r = row0 + threadIdx.x / 64; r < min(row0 + TABLE_ROWS, p.rows); r += THREADS / 64) {
+  const int row0 = blockIdx.x * TABLE_ROWS, n = min(TABLE_ROWS, p.rows - row0);       // (row0 + TABLE_ROWS may lie past 2^31)
+  for (int j = threadIdx.x / 64; j < n; j += THREADS / 64) {
+    const int r = row0 + j;
     float2 v = make_float2(0.f, 0.f);
     if (r >= x.first_row && r < end) {
       const unsigned long long turns = (unsigned long long)(r - x.first_row) * step, q = (turns + (1ull << 61)) >> 62;       // the next multiple of a quarter turn

@@ -391,3 +391,14 @@ def test_host_threads_with_calls_of_different_sizes(ops):
     assert not wrong, (len(wrong), set(wrong))
     for pairs, (_, _, (table, q, dq, out), _) in zip((64, 32, 64, 32), calls):
         assert torch.equal(out, ops.qk_norm_rotary_backward(dq, None, q, None, None, None, table).q)
+
+
+def test_table_of_the_most_rows(ops):
+    """2^31 - 1 positions of a pair: the last ones are there as well.  (An angle of 2^-53 relative over 2^31 / 2 pi turns: 2^-24 of a turn.)"""
+    n = (1 << 31) - 1
+    if torch.cuda.mem_get_info()[0] < n * 8 + (1 << 30):
+        pytest.skip("not enough memory")
+    torch.full((n, 1, 2), float("nan"), device="cuda")            # what the next tensor of this size lies over
+    last = ops.rotary_table((n,), (1,)).factors[-200:].cpu()
+    ref = torch.tensor([[[math.cos(r), math.sin(r)]] for r in range(n - 200, n)], dtype=R.F64)
+    R.within(last, ref, ref.abs() * 2.0 ** -21 + math.tau * 2.0 ** -24 * 1.5)
