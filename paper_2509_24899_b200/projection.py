@@ -6,7 +6,7 @@
 
 A matrix is a tensor [rows, cols], or [B, H, N, d] as the attention has it, which stands for [B * N, H * d].  Any strides are taken whose innermost one is 1; operands whose strides and
 addresses are no multiples of 16 bytes, or whose heads are no multiples of 64, are copied first.  Tensors that require gradients are refused unless gradients are off or they are
-detached: a program that trains keeps `pre` and calls `linear_backward`.
+detached, and so are those with a forward-mode tangent: a program that trains keeps `pre` and calls `linear_backward`.
 """
 from __future__ import annotations
 

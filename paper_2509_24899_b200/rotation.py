@@ -6,7 +6,7 @@
 
 Tensors are [B, H, N, d] in bf16 or fp32 with any strides whose innermost one is 1; where sizes, strides and addresses are multiples of 16 bytes (and the pairs of 8), rows move
 faster.  Outputs are new tensors in [B, H, N, d] order unless they are given; one may be its input itself, and overlaps no other tensor.  Tensors that require gradients are refused unless gradients are off or they are
-detached: a program that trains calls the `_backward` functions.
+detached, and so are those with a forward-mode tangent: a program that trains calls the `_backward` functions.
 """
 from __future__ import annotations
 
