@@ -7,7 +7,7 @@
 A matrix is a tensor [rows, cols], or [B, H, N, d] as the attention has it, which stands for [B * N, H * d].  Any strides are taken
 whose innermost one is 1; where those of a call's tensors, and their addresses, are multiples of 16 bytes, rows move faster.
 
-The calls have no gradients: a tensor that requires one is refused unless gradients are off (torch.no_grad()) or it is detached.  Tensors that are given for outputs count as
+The calls have no gradients: a tensor that requires one is refused unless gradients are off (torch.no_grad()) or it is detached, one with a forward-mode tangent always.  Tensors that are given for outputs count as
 modified in place.
 """
 from __future__ import annotations

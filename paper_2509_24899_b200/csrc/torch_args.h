@@ -52,6 +52,7 @@ inline const at::Tensor* tensor_of(PyObject* o, int here, const char* where, con
   const at::Tensor& t = THPVariable_Unpack(o);
   if (!t.is_cuda() || t.get_device() != here || t.layout() != at::kStrided) { refuse(where, name, "is not a strided tensor on the current CUDA device"); return nullptr; }
   if (t.requires_grad() && at::GradMode::is_enabled()) { refuse(where, name, "requires a gradient, which these calls have none of: detach it, or call under torch.no_grad()"); return nullptr; }
+  if (t.is_neg()) { refuse(where, name, "is a view whose values count negated: resolve_neg() writes them out"); return nullptr; }
   if (t._fw_grad(0).defined() && c10::AutogradState::get_tls_state().get_fw_grad_mode()) { refuse(where, name, "carries a forward-mode tangent, which these calls would drop"); return nullptr; }
   return &t;
 }

@@ -45,3 +45,16 @@ def test_tensors_with_a_forward_mode_tangent_are_refused(ops):
         x, w, out = randn(6, 64), randn(32, 64), fwad.make_dual(randn(6, 32), randn(6, 32))
         with pytest.raises(ValueError, match="tangent"):
             ops.linear(x, w, out=out)
+
+
+def test_views_whose_values_count_negated_are_refused(ops):
+    """(The imaginary part of a conjugate is one: what lies in memory has the other sign.)"""
+    column = torch.complex(randn(5, 1, dtype=F32), randn(5, 1, dtype=F32)).conj().imag
+    assert column.is_neg()
+    with pytest.raises(ValueError, match="negated"):
+        ops.rms_norm(column)
+    for name, call, t in calls(ops):
+        with pytest.raises(ValueError, match="negated"):
+            call(torch._neg_view(t))
+            print("not refused:", name)
+        call(torch._neg_view(t).resolve_neg())
