@@ -43,14 +43,13 @@ class Fp8AttentionLayer:
         x8, residual = rms_norm(hidden, self._norm["norm"], residual=residual, eps=self.eps, fp8=True)
         shape = self.attention.shape
         q, k, v = (torch.empty(shape, dtype=torch.bfloat16, device=hidden.device) for _ in range(3))
-        rows = [matmul_fp8(x8, self._w8[name], bias=self._bias[name]) for name in "qk"]
-        if self.table is None:
-            for name, r, out in zip("qk", rows, (q, k)):
-                rms_norm(r, self._norm["norm_" + name], eps=self.eps, out=out)
+        if self.table is None:                               # one after the other: the rows of one product are held at a time
+            for name, out in (("q", q), ("k", k)):
+                rms_norm(matmul_fp8(x8, self._w8[name], bias=self._bias[name]), self._norm["norm_" + name], eps=self.eps, out=out)
         else:
             B, H, N, d = shape
-            heads = [r.view(B, N, H, d).permute(0, 2, 1, 3) for r in rows]
-            qk_norm_rotary(*heads, self._norm["norm_q"], self._norm["norm_k"], self.table, norm="row", eps=self.eps, layout=self.layout, q_out=q, k_out=k)
+            qk_norm_rotary(*[matmul_fp8(x8, self._w8[name], bias=self._bias[name]).view(B, N, H, d).permute(0, 2, 1, 3) for name in "qk"], self._norm["norm_q"], self._norm["norm_k"], self.table,
+                           norm="row", eps=self.eps, layout=self.layout, q_out=q, k_out=k)
         matmul_fp8(x8, self._w8["v"], bias=self._bias["v"], out=v)
         o = self.attention.forward(q, k, v, **self.phi)
         return matmul_fp8(quantize_fp8(o), self._w8["o"], bias=self._bias["o"]), residual
