@@ -16,16 +16,18 @@ import torch
 
 from . import HybridAttention
 from .block_fp8 import matmul_fp8, quantize_fp8, rms_norm
-from .rotation import qk_norm_rotary
+from .rotation import _where, qk_norm_rotary
 
 
 class Fp8AttentionLayer:
     """`attention`: the layer's HybridAttention, of B x H x N x d.  `weights`: name -> bf16 CUDA tensor: "q", "k", "v", "o" [H d, H d] and
     optionally "bias_q", ..., "bias_o" [H d], "norm", "norm_q", "norm_k" [H d], all on the current device; `phi`: the feature maps' weights, the
-    keyword arguments that `HybridAttention.forward` takes (wq, wk, ...); `table`: a RotaryTable of the layer's grid, by which q and k are turned, in `layout`."""
+    keyword arguments that `HybridAttention.forward` takes (wq, wk, ...); `table`: a RotaryTable of the layer's grid, by which q and k are turned, in `layout`;
+    `first`, `positions`: as for `qk_norm_rotary`, with None the attention's tokens begin at its `n0` (a SeqShardedAttention's range of them), or at 0."""
 
-    def __init__(self, attention: HybridAttention, weights, phi, eps=1e-6, table=None, layout="interleaved"):
+    def __init__(self, attention: HybridAttention, weights, phi, eps=1e-6, table=None, layout="interleaved", first=None, positions=None):
         self.attention, self.phi, self.eps, self.table, self.layout = attention, phi, eps, table, layout
+        self._where = _where(attention, first, positions)
         B, H, N, d = attention.shape
         for name in "qkvo":
             if tuple(weights[name].shape) != (H * d, H * d):
@@ -49,7 +51,7 @@ class Fp8AttentionLayer:
         else:
             B, H, N, d = shape
             qk_norm_rotary(*[matmul_fp8(x8, self._w8[name], bias=self._bias[name]).view(B, N, H, d).permute(0, 2, 1, 3) for name in "qk"], self._norm["norm_q"], self._norm["norm_k"], self.table,
-                           norm="row", eps=self.eps, layout=self.layout, q_out=q, k_out=k)
+                           norm="row", eps=self.eps, layout=self.layout, q_out=q, k_out=k, **self._where)
         matmul_fp8(x8, self._w8["v"], bias=self._bias["v"], out=v)
         o = self.attention.forward(q, k, v, **self.phi)
         return matmul_fp8(quantize_fp8(o), self._w8["o"], bias=self._bias["o"]), residual

@@ -16,7 +16,7 @@ import torch
 from . import HybridAttention
 from .block_fp8 import rms_norm
 from .projection import linear, linear_backward
-from .rotation import qk_norm_rotary, qk_norm_rotary_backward
+from .rotation import _where, qk_norm_rotary, qk_norm_rotary_backward
 
 
 def _frozen(weights, name):
@@ -27,7 +27,8 @@ class QkProjection:
     """Queries and keys from a layer's input: one product for both, norms (over a token's heads, `norm="row"`, or for each head) and rotation.
 
     shape    (B, H, N, d);  w: [2 H d, K] bf16, queries' rows first, bias: [2 H d] or None
-    norm_q, norm_k: [H d] ([d] with norm="head"), or None;  table, layout: as for `qk_norm_rotary`; table=None: no rotation
+    norm_q, norm_k: [H d] ([d] with norm="head"), or None;  table, layout, first, positions: as for `qk_norm_rotary`; table=None: no rotation.  A range of a clip's tokens has the clip's table and its
+    own `first`
     """
 
     class Gradients(NamedTuple):
@@ -37,12 +38,12 @@ class QkProjection:
         norm_q: torch.Tensor | None
         norm_k: torch.Tensor | None
 
-    def __init__(self, shape, w, bias=None, norm_q=None, norm_k=None, table=None, norm="row", eps=1e-6, layout="interleaved"):
+    def __init__(self, shape, w, bias=None, norm_q=None, norm_k=None, table=None, norm="row", eps=1e-6, layout="interleaved", first=0, positions=None):
         B, H, N, d = shape
         if w.shape[0] != 2 * H * d:
             raise ValueError("QkProjection: w has %d rows, not %d" % (w.shape[0], 2 * H * d))
         self.shape, self.w, self.bias, self.norms = tuple(shape), w, bias, (norm_q, norm_k)
-        self._how = dict(table=table, norm=norm, eps=eps, layout=layout)
+        self._how = dict(table=table, norm=norm, eps=eps, layout=layout, first=first, positions=positions)
 
     def _heads(self, rows):
         """The queries' and the keys' part of rows [B N, 2 H d], each as [B, H, N, d]."""
@@ -102,9 +103,10 @@ class FeedForward:
 class AttentionLayer:
     """`attention`: the layer's HybridAttention, of B x H x N x d.  `weights`: name -> bf16 CUDA tensor: "q", "k", "v", "o" [H d, H d], "up" [F, H d], "down" [H d, F] and optionally "bias_q", ...,
     "bias_down", "norm", "norm_ff" [H d], "norm_q", "norm_k" [H d] ([d] with norm="head"); `phi`: the keyword arguments that `HybridAttention.forward` takes (wq, wk, ...); `table`: a
-    RotaryTable of the layer's grid, or None."""
+    RotaryTable of the layer's grid, or None; `first`, `positions`: as for `qk_norm_rotary`, with None the attention's tokens begin at its `n0` (a SeqShardedAttention's range of them), or at 0.
+    Weights are taken when the layer is made (queries' and keys' are put together, the others stay where they are): one that they change for is made again."""
 
-    def __init__(self, attention: HybridAttention, weights, phi, table=None, norm="row", eps=1e-6, activation="gelu_tanh", layout="interleaved"):
+    def __init__(self, attention: HybridAttention, weights, phi, table=None, norm="row", eps=1e-6, activation="gelu_tanh", layout="interleaved", first=None, positions=None):
         self.attention, self.phi, self.eps = attention, phi, eps
         B, H, N, d = attention.shape
         w = {name: _frozen(weights, name) for name in ("q", "k", "v", "o", "up", "down", "norm", "norm_ff", "norm_q", "norm_k")}
@@ -112,7 +114,7 @@ class AttentionLayer:
         if (b["q"] is None) != (b["k"] is None):
             raise ValueError("AttentionLayer: a bias of queries goes with one of keys")
         qk_bias = None if b["q"] is None else torch.cat((b["q"], b["k"]))
-        self.qk = QkProjection(attention.shape, torch.cat((w["q"], w["k"])), qk_bias, w["norm_q"], w["norm_k"], table, norm, eps, layout)
+        self.qk = QkProjection(attention.shape, torch.cat((w["q"], w["k"])), qk_bias, w["norm_q"], w["norm_k"], table, norm, eps, layout, **_where(attention, first, positions))
         self.feed_forward = FeedForward(w["up"], w["down"], b["up"], b["down"], activation)
         self._w, self._b = w, b
 

@@ -41,6 +41,13 @@ class QkGradients(NamedTuple):
     k_weight: torch.Tensor | None
 
 
+def _where(attention, first, positions):
+    """`first` and `positions` of a layer's tokens for the calls: where `first` is None, the tokens begin where the attention's do."""
+    if first is None:
+        first = 0 if positions is not None else getattr(attention, "n0", 0)
+    return dict(first=first, positions=positions)
+
+
 def _choice(table, key, where, name):
     try:
         return table[key]

@@ -176,3 +176,50 @@ def test_the_8_bit_layer_with_a_rotation(ops):
     q, k = (ops.qk_norm_rotary(R.heads_of(r, B, d), None, n, None, table, norm="row") for r, n in ((q, w["norm_q"]), (k, w["norm_k"])))
     o = attention.forward(q, k, v, **phi)
     assert torch.equal(ops.matmul_fp8(ops.quantize_fp8(o), w8["o"], bias=w["bias_o"]), turned)
+
+
+@pytest.mark.parametrize("way", ["first", "positions"])
+def test_ranges_of_a_clips_tokens(ops, way):
+    """Two ranges of a clip's tokens, as two ranks have them, turned by the clip's table: queries, keys and gradients are the whole clip's; so are the results of both layers."""
+    from paper_2509_24899_b200.fp8_layer import Fp8AttentionLayer
+    from paper_2509_24899_b200.layer import AttentionLayer, QkProjection
+    H, d, sizes = 3, 64, (3, 5, 6)
+    N, hd = 90, H * d
+    table = table_of(ops, sizes, d)
+    grid = torch.stack(torch.meshgrid(*(torch.arange(s) for s in sizes), indexing="ij"), -1).reshape(N, 3).int().cuda()
+    ranges = ((0, 37), (37, N))
+
+    def where(a, b):
+        return dict(first=a) if way == "first" else dict(positions=grid[a:b])
+
+    x, w = randn(N, 96, seed=1), randn(2 * hd, 96, seed=2, gain=96 ** -0.5)
+    norms = [1 + 0.2 * randn(hd, dtype=F32, seed=4 + i) for i in range(2)]
+    dq, dk = randn(1, H, N, d, seed=8), randn(1, H, N, d, seed=9)
+
+    def parts(shape, x, dq, dk, **how):
+        p = QkProjection(shape, w, None, *norms, table, **how)
+        qk, kept = p.forward(x, keep=True)
+        return qk, p.backward(dq, dk, kept)
+
+    qk, g = parts((1, H, N, d), x, dq, dk)
+    some = [parts((1, H, b - a, d), x[a:b], dq[:, :, a:b], dk[:, :, a:b], **where(a, b)) for a, b in ranges]
+    for i in range(2):
+        near(torch.cat([s[0][i] for s in some], 2), qk[i], "qk"[i])
+    near(torch.cat([s[1].x for s in some]), g.x, "x")
+    for name in ("w", "norm_q", "norm_k"):
+        near(sum(getattr(s[1], name).to(F64) for s in some), getattr(g, name), name)
+
+    class Attention:                                          # of a range: its queries, keys and values for the results
+        def __init__(self, a, b):
+            self.shape, self.n0 = (1, H, b - a, d), a
+
+        def forward(self, q, k, v):
+            return q + k + v
+
+    weights, rows = layer_weights(H, d, 128), randn(N, hd, seed=10)
+    for make, call in ((AttentionLayer, lambda l, r: l.forward(r)), (Fp8AttentionLayer, lambda l, r: l.forward(r, r)[0])):
+        def result(a, b, **how):
+            return call(make(Attention(a, b), weights, {}, table=table, **how), rows[a:b])
+        whole = result(0, N)
+        near(torch.cat([result(a, b, **(where(a, b) if way == "positions" else {})) for a, b in ranges]), whole, make.__name__)
+        assert float((result(37, N, first=0).to(F64) - whole[37:].to(F64)).norm() / whole[37:].to(F64).norm()) > 2 * CHAIN      # (what a range at another place gives)

@@ -51,3 +51,34 @@ def test_the_8_bit_layer_holds_one_product_at_a_time(monkeypatch):
     layer = fp8_layer(monkeypatch, log, shape)
     layer.forward(torch.zeros(3, 8, dtype=BF16), torch.zeros(3, 8, dtype=BF16))
     assert log == [("norm", None), ("product", "q"), ("norm", "q"), ("product", "k"), ("norm", "k"), ("product", "v"), ("product", "o")]
+
+
+@pytest.mark.parametrize("attention,how,want", [({}, {}, (0, None)), ({}, dict(first=7), (7, None)), (dict(n0=5), {}, (5, None)), (dict(n0=5), dict(first=0), (0, None)), (dict(n0=5), dict(positions="here"), (0, "here"))])
+def test_where_a_layers_tokens_begin(monkeypatch, attention, how, want):
+    """In the grid of the layer's table: where it is said, else where the attention's range of a clip begins."""
+    from paper_2509_24899_b200 import layer as module
+    shape, log = (1, 2, 3, 4), []
+    fp8_layer(monkeypatch, log, shape, Attention(shape, **attention), table="table", **how).forward(torch.zeros(3, 8, dtype=BF16), torch.zeros(3, 8, dtype=BF16))
+    turns = [e for e in log if e[0] == "turn"]
+
+    def linear(x, w, bias=None, out=None, **kw):
+        return torch.zeros(x.shape[0] if x.dim() == 2 else 3, w.shape[0], dtype=BF16) if out is None else out
+
+    def qk_norm_rotary(q, k, wq, wk, table=None, **kw):
+        turns.append(("turn", table, kw))
+        return q, k
+
+    def qk_norm_rotary_backward(dq, dk, q, k, wq, wk, table=None, **kw):
+        turns.append(("turn", table, kw))
+        raise InterruptedError
+
+    for f in (linear, qk_norm_rotary, qk_norm_rotary_backward):
+        monkeypatch.setattr(module, f.__name__, f)
+    monkeypatch.setattr(module, "rms_norm", lambda x, w, eps: x)
+    w = {n: torch.zeros(8, 8, dtype=BF16) for n in ("q", "k", "v", "o", "up", "down")}
+    layer = module.AttentionLayer(Attention(shape, **attention), w, {}, "table", **how)
+    layer.forward(torch.zeros(3, 8, dtype=BF16))
+    _, kept = layer.qk.forward(torch.zeros(3, 8, dtype=BF16), keep=True)
+    with pytest.raises(InterruptedError):
+        layer.qk.backward(None, None, kept)
+    assert [(t[1], t[2]["first"], t[2]["positions"]) for t in turns] == [("table", *want)] * 4
