@@ -32,7 +32,7 @@ def linear(x, w, bias=None, activation=None, gate=None, residual=None, out=None,
     """residual + gate * act(x w^T + bias), products of bf16 values summed in fp32, one rounding at the end.
 
     x           [M, K] or [B, H, N, d], bf16; w: [N, K], bf16
-    bias        [N]; gate: [N], or [entries, N] where each entry's rows (M / entries in turn) have their own; bf16 or fp32
+    bias        [N]; gate: [N], or [entries, N] where each entry's rows (M / entries in turn) have their own (up to 65534 of them); bf16 or fp32
     activation  None, "relu", "silu", "gelu" (by the error function) or "gelu_tanh"
     residual    [M, N] or heads, bf16 or fp32
     out         where the result goes, bf16 or fp32, rows or heads; may be `residual` itself, and overlaps nothing else.  None: a new tensor in the residual's shape and type, else bf16 [M, N]

@@ -59,7 +59,8 @@ def rotary_table(sizes, pairs, base=10000.0, scaling=None, factor=1.0, original=
     """The table of axes with `sizes` positions, of which each turns its number of `pairs`: pair i of n by position * base^(-i / n).
 
     scaling   for positions beyond those that a model was trained on: None, "linear" (positions over `factor`), "ntk" (the base times factor^(n / (n - 1))) or "yarn" (pairs of few turns over
-              `original` positions over `factor`, those of 32 and more left alone, a ramp between them; cos and sin times 0.1 ln(factor) + 1)
+              `original` positions over `factor`, those of 32 and more left alone, a ramp over turns between them; cos and sin times 0.1 ln(factor) + 1).  A model whose ramp goes over the pairs' indices, or whose angles are others, makes
+              a table of its own
     base, scaling, factor, original: one for all axes, or a tuple with one for each."""
     sizes, pairs = tuple(sizes), tuple(pairs)
 

@@ -402,3 +402,20 @@ def test_table_of_the_most_rows(ops):
     last = ops.rotary_table((n,), (1,)).factors[-200:].cpu()
     ref = torch.tensor([[[math.cos(r), math.sin(r)]] for r in range(n - 200, n)], dtype=R.F64)
     R.within(last, ref, ref.abs() * 2.0 ** -21 + math.tau * 2.0 ** -24 * 1.5)
+
+
+def test_in_place_past_32_bits(ops):
+    """Tokens that lie 2^32 elements into their tensor, turned where they are, in vectors and pair by pair."""
+    need = (1 << 32) + 4096
+    if torch.cuda.mem_get_info()[0] < need * 2 + (1 << 30):
+        pytest.skip("not enough memory")
+    flat = torch.zeros(need, dtype=BF16, device="cuda")
+    for d, pairs in ((64, 32), (50, 11)):
+        x = flat.as_strided((1, 2, 2, d), (0, d, 1 << 32, 1))
+        was = randn(1, 2, 2, d, seed=d)
+        x.copy_(was)
+        table = plain_table((2,), (pairs,))
+        assert ops.rotary(x, table, out=x) is x
+        R.check_forward(x, was, None, R.factors64(table, 1, 2), None, 0, "interleaved")
+        flat[:2 * d], flat[1 << 32:(1 << 32) + 2 * d] = 0, 0
+        assert not bool(flat.view(torch.int16).any())            # nothing else has been written

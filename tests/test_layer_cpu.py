@@ -1,6 +1,8 @@
 """The bf16 steps around the attention without a GPU: the plain forms against values worked by hand, and the refusals of the C entries, which come before any CUDA call."""
 import ctypes as C
 import math
+import os
+import re
 
 import pytest
 import torch
@@ -211,3 +213,12 @@ def test_calls_without_a_device_fail_loudly(lib):
 
 def test_struct_sizes():
     assert [C.sizeof(s) for s in (binding.as_rotary_axis_t, binding.as_rotation_t, binding.as_qk_norm_rotary_t, binding.as_qk_norm_rotary_backward_t, binding.as_linear_t, binding.as_linear_backward_t)] == [40, 80, 328, 240, 328, 384]
+
+
+def test_no_failed_cuda_call_leaves_its_error_behind():
+    """Calls that give up because one of CUDA's has failed say so through `failed`, which takes the pending error away; and no call sets a kernel's limits for itself alone."""
+    for name in ("rotary.cu", "linear.cu"):
+        with open(os.path.join(build.CSRC, name)) as f:
+            text = re.sub(r"//[^\n]*", "", f.read())
+        assert "failed()" in text and "AS_ERR_CUDA" not in text, name
+        assert text.count("cudaFuncSetAttribute") == (1 if name == "rotary.cu" else 0), name
