@@ -11,7 +11,8 @@
  *   as_linear_backward          the gradients of x, w, bias and gate
  *
  * Conventions as in as_fp8.h: device pointers, the caller's buffers and stream, nothing allocated, no synchronisation, calls can be
- * captured; on error nothing has been launched.  Sums are fp32 in an order that depends on sizes, types and layouts alone: results are run-to-run identical.
+ * captured; on error nothing has been launched.  Sums are fp32 in an order that depends on sizes, types, layouts, the alignment of
+ * addresses and the device alone: results are run-to-run identical.
  */
 #ifndef AS_LAYER_H_
 #define AS_LAYER_H_

@@ -3,8 +3,9 @@
 // One kernel does the three products; they differ in which of an operand's two indices lies in a run in memory, which the copies (boxes of 64 elements by rows) and the operand
 // descriptors say.  A pair of CTAs (cta_group::2) computes a tile of 256 rows by up to 256 columns: each holds 128 rows of the first operand, half of the tile's columns of the second
 // and 128 rows of results.  The grid is persistent, one CTA an SM; a tile's results are read out while the next one is computed, from the other of two accumulators.
-// 32760 x 1536 by 6144 x 1536 with a bias and gelu_tanh 425 us, 1.45 PFLOP/s, the tensor pipe active 92 % of the time at the 1.44 GHz that the power limit leaves; 32760 x 6144 by 1536 x 6144 onto a
-// residual in fp32 471 us, 1.31 PFLOP/s; the gradients' products of 7800 x 1536 by 6144 x 1536 113 us (dx) and 97 us (dw).
+// The kernel alone: 32760 x 1536 by 6144 x 1536 with a bias and gelu_tanh 427 us, 1.45 PFLOP/s, the tensor pipe active 92 % of the time at the 1.44 GHz that the power limit leaves; 32760 x 6144 by
+// 1536 x 6144 onto a residual in fp32 477 us, 1.30 PFLOP/s (with nothing behind the products 412 and 439; the library's bf16 products of these sizes 420 and 462); the gradients' products of 7800 x 1536 by
+// 6144 x 1536 113 us (dx) and 97 us (dw).  In calls one after another, of which the power limit leaves a lower clock, 497, 573 and, the whole gradient, 320.
 //
 //   warp 0       copies (TMA, 64 steps of the summed index a stage, 128-byte swizzle), told by the leading CTA's barrier
 //   warp 1       the MMAs (leading CTA only)
@@ -916,8 +917,9 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 1) linear_few_kernel(const __g
 }
 
 // ---------------------------------------------------------------- dz, and sums over rows
-// dz = dy * gate * act'(pre) in bf16, the sums of dz and of dy * act(pre) over runs of rows, which do not cross from one gate's rows to another's.  A lane has 8 columns, a warp
-// every eighth row of the run, the next one under way; the warps' sums meet in shared memory in their order.  One pass over dy and pre: HBM bytes (32760 x 6144 from fp32 with silu and a gate's
+// dz = dy * gate * act'(pre) in bf16, as the other operand of both products is (the tensor cores take two of one type; in tf32, or as the sum of two bf16 values, the products would take twice as long):
+// beside the results' own rounding, 1.66e-3 in the mean square, that is another of the same size, 2.34e-3 in all.  With it the sums of dz and
+// of dy * act(pre), from the unrounded values, over runs of rows, which do not cross from one gate's rows to another's.  A lane has 8 columns, a warp every eighth row of the run, the next one under way; the warps' sums meet in shared memory in their order.  One pass over dy and pre: HBM bytes (32760 x 6144 from fp32 with silu and a gate's
 // gradient 261 us, 6.2 TB/s), in bf16 with an activation the instructions beside them (7800 x 6144 with gelu_tanh 70 us, 4.1 TB/s; with the activation chosen at every value, and both its sigmoids from
 // exponentials of their own, 254; with runs for 2.7 turns of the SMs instead of one 76).
 struct DzParams {

@@ -6,8 +6,9 @@
 // worked on, and so do a token's cos and sin, which are the same for every head and for queries and keys.  Three vectors a lane: what a row costs once (positions, addresses, factors) is a third of the whole
 // with one (81 frames by heads: 106 us with one, 104 with two, 74 with three).  Heads whose sizes, strides or addresses do not allow it go pair by pair (turn_elements_kernel).
 //
-// 32760 tokens of 2 x 12 heads of 128 in bf16, from the fused projection's rows into heads, norm by heads: 74 us, 5.5 TB/s; its gradient 111 us, 5.4 TB/s.  7800 tokens, norm over rows: 24 us,
-// 3.9 TB/s (3.3 rows a warp, each of which is a chain of latencies), its gradient 55 us (shared memory: the rows twice, the weights twice and the sums of d n).
+// The kernels alone: 32760 tokens of 2 x 12 heads of 128 in bf16, from the fused projection's rows into heads, norm by heads: 74 us, 5.4 TB/s; its gradient 111 us, 5.4 TB/s (calls one after another 78 and
+// 121).  In fp32 235 us, 3.4 TB/s, and 354 (one CTA an SM).  7800 tokens, norm over rows: 24 us, 3.9 TB/s (3.3 rows a warp, each of which is a chain of latencies), its gradient 55 us (issue slots
+// used 38 % with 14 warps an SM; of 7.8 cycles between a warp's instructions 2.2 wait for memory, 1.3 for an instruction before, 1.0 for shared memory, which the rows are read from twice).
 #include <algorithm>
 #include <atomic>
 #include <cmath>
@@ -1029,14 +1030,14 @@ Shape turn_params(const as_qk_norm_rotary_t& a, const as_rotation_t& r, int sms,
   p.lanes_log = 0;
   while ((s.E << p.lanes_log) < a.head_dim) ++p.lanes_log;
   const int heads = std::max(p.t[0].heads, p.t[1].heads), of_vector = std::max(1, 32 >> p.lanes_log), vectors = (heads + of_vector - 1) / of_vector;
-    const int most = a.q.dtype == AS_DTYPE_BF16 ? 3 : 2;
+  const int most = a.q.dtype == AS_DTYPE_BF16 ? 3 : 2;
   p.W = 1; p.chunks = 1;
   if (a.norm == AS_NORM_ROW) {
     p.W = (vectors + most - 1) / most;
     if (p.W > WARPS) s.vec = false;
     else s.NV = (vectors + p.W - 1) / p.W;
     s.ctas = s.vec ? (a.rows + WARPS / p.W - 1) / (WARPS / p.W) : a.rows * (back ? 1 : p.n_t);
-    // weights in shared memory, as far as two CTAs an SM have the room
+    // weights in shared memory, up to what has been measured: two vectors of 1536 in fp32 (two CTAs an SM would have the room for more)
     const size_t size = p.w_f32 ? 4 : 2, of_q = (size_t)p.t[0].heads * a.head_dim * size, of_k = (size_t)p.t[1].heads * a.head_dim * size;
     s.kept = back ? std::max(of_q, of_k) : of_q + of_k;
     if (s.vec && s.kept <= KEPT_MOST && of_q % 16 == 0 && of_k % 16 == 0 && aligned(a.q_weight, 16) && (!two || aligned(a.k_weight, 16))) p.kept = (int)of_q;

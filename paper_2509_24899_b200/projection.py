@@ -46,6 +46,8 @@ def linear(x, w, bias=None, activation=None, gate=None, residual=None, out=None,
 def linear_backward(dy, x, w, pre=None, activation=None, gate=None, bias=None, x_grad=True, w_grad=True, gate_grad=True, stream=None) -> LinearGradients:
     """From the gradient dy [M, N] (bf16 or fp32, rows or heads) of `linear`'s result and its arguments: the gradients of its inputs, in their types; dx in x's shape.
 
+    The gradient of x w^T + bias, dy * gate * act'(pre), is rounded to bf16 as an operand of the products behind dx and dw, in fp32 dy's as well; the gradients of bias and gate come from its unrounded values.
+
     pre   what `linear` kept; needed with an activation, and for the gate's gradient
     bias  the bias, or any vector of its size and type: its gradient is wanted.  x_grad, w_grad, gate_grad: whether those are"""
     return LinearGradients(*_on(stream, _calls.linear_backward, dy, x, w, pre, _choice(_ACTIVATIONS, activation, "linear_backward", "activation"), gate, bias, x_grad, w_grad, gate_grad))
